@@ -1,0 +1,515 @@
+"""Cases of the operators that stand on both sides of a language model's gradient, for timing.
+
+A case is one pass of one operator, through the public entry points:
+
+    norm      layer norm of `rows` vectors of `cols` values: forward alone (serving), or forward and backward with
+              the weight's and bias's gradients (training)
+    token     log probabilities of given tokens with entropy and the `top` largest alternatives (serving, scoring);
+              `how` "loss": logp, entropy and the gradient of the logits in one call, the coefficients known before
+              (pre-training); `how` "policy": forward, then the gradient of logp and entropy (policy gradients)
+    adamw     one AdamW step over all tensors of a model, with moments in 32 or 8 bits, with or without clipping by the
+              global norm.  Moments in 8 bits are read back after the step, as a checkpoint or a log does.
+
+Moments in 8 bits: blocks of 256 values of a tensor share the exponent field of their largest magnitude (at least
+16), 16 binades below and including it are told apart.  First moment: sign, 4 exponent and 3 fraction bits.  Root of the
+second moment: 4 exponent and 4 fraction bits; a root that is not 0 is at least code 1.  Code 0 is the value 0; rounding is
+to nearest, halves away from 0, up to the largest code.  Codes and exponent bytes are tensors of their own.
+
+The tensors of a model start at multiples of 256 values of one buffer, which is what a pass returns (what lies between two
+tensors is 0 and stays so).
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+SIZE = {"f32": 4, "bf16": 2, "f16": 2}
+EPS = 1e-5
+LR, BETA1, BETA2, ADAM_EPS, DECAY = 1e-3, 0.9, 0.98, 1e-8, 0.01
+STEP = 1000                              # steps done before the one of a pass
+
+
+def _norm(rows, cols, dtype, w, grad, pad=0, name=None):
+    case = {"kind": "norm", "rows": rows, "cols": cols, "dtype": dtype, "w": w, "grad": grad, "pad": pad}
+    if name:
+        case["name"] = name
+    return case
+
+
+def _token(how, rows, vocab, dtype, top=0, scale=1.0, masked=False, pad=0, name=None):
+    case = {"kind": "token", "how": how, "rows": rows, "vocab": vocab, "dtype": dtype, "top": top, "scale": scale,
+            "masked": masked, "pad": pad}
+    if name:
+        case["name"] = name
+    return case
+
+
+def _adamw(hidden, layers, tables, vocab, p, g, bits, clip, name=None):
+    case = {"kind": "adamw", "hidden": hidden, "layers": layers, "tables": tables, "vocab": vocab, "p": p, "g": g,
+            "bits": bits, "clip": clip}
+    if name:
+        case["name"] = name
+    return case
+
+
+def listed():
+    return [
+        # one token through a small model that is served: nothing but the launch and the call
+        _norm(1, 512, "f32", "f32", False, name="norm-1x512"),
+        # odd sizes, rows further apart than they are long (a slice of a wider activation)
+        _norm(3001, 1999, "f16", "f16", True, pad=12, name="norm-3001x1999-f16"),
+        # a training step's activations in the 90 M transformer: 32 sentences of 256 tokens, width 512
+        _norm(8192, 512, "f32", "f32", True, name="norm-8192x512"),
+        # a larger model in mixed precision: activations in bf16, weights in 32 bits
+        _norm(32768, 4096, "bf16", "f32", True, name="norm-32768x4096-bf16"),
+        # one token sampled by a server that shows alternatives
+        _token("forward", 1, 32768, "f32", 20, 0.8, name="token-1x32768-top20"),
+        # a batch of constrained decoding: most of a large vocabulary is masked, one row entirely
+        _token("forward", 64, 131072, "bf16", 8, masked=True, name="token-64x131072-top8"),
+        # scoring a prompt; a vocabulary that is no multiple of anything, rows padded to one that is
+        _token("forward", 2047, 50021, "f16", 0, pad=27, name="token-2047x50021-f16"),
+        # pre-training loss and its gradient
+        _token("loss", 8192, 34000, "bf16", name="token-loss-8192x34000"),
+        # policy gradients with an entropy bonus, logits in 32 bits, a softmax temperature
+        _token("policy", 4096, 32001, "f32", 0, 0.9, name="token-policy-4096x32001"),
+        # a small model: many little tensors, latency counts
+        _adamw(64, 2, 1, 1000, "f32", "f32", 32, False, name="adamw-0.2M"),
+        # the 90 M transformer of the sketched training runs: 12 layers of width 512 and three tables of a vocabulary
+        _adamw(512, 12, 3, 34001, "f32", "f32", 32, True, name="adamw-90M-clip"),
+        # the same with moments in 8 bits, gradients in bf16
+        _adamw(512, 12, 3, 34001, "f32", "bf16", 8, True, name="adamw-90M-8bit"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.999))))
+
+
+def _not_round(n):
+    """(one width is left out of the cases; the next one is as good)"""
+    return n + 1 if n == 3072 else n
+
+
+def draw(rng):
+    """One more case: norms of 1 to 65 536 rows of 16 to 16 384 values, 1 to 16 384 rows of logits of vocabularies of
+    100 to 262 144, models of 10 thousand to 90 million parameters; all types and ways of use."""
+    kind = rng.choice(["norm", "token", "adamw"])
+    if kind == "norm":
+        rows = _not_round(_log(rng, 1, 65536))
+        cols = _not_round(_log(rng, 16, min(16384, 100_000_000 // rows)))
+        if rng.random() < 0.5:
+            cols = _not_round(max(16, cols // 64 * 64))
+        dtype = rng.choice(["f32", "bf16", "f16"])
+        return _norm(rows, cols, dtype, rng.choice(["f32", dtype]), rng.random() < 0.7, rng.choice([0, 0, 1, 8, 24]))
+    if kind == "token":
+        how = rng.choice(["forward", "forward", "loss", "policy"])
+        vocab = _log(rng, 100, 262144)
+        if rng.random() < 0.5:
+            vocab = max(128, vocab // 128 * 128)
+        vocab = _not_round(vocab)
+        rows = _not_round(_log(rng, 1, min(16384, max(1, 100_000_000 // vocab))))
+        top = rng.choice([0, 1, 5, 20]) if how == "forward" else 0
+        return _token(how, rows, vocab, rng.choice(["f32", "bf16", "f16"]), top, rng.choice([1.0, 0.7, 1.3]),
+                      rng.random() < 0.3, rng.choice([0, 0, 3, 40]))
+    hidden = _log(rng, 16, 1024)
+    hidden = _not_round(hidden if rng.random() < 0.5 else max(16, hidden // 16 * 16))
+    hidden += 1 if 4 * hidden == 3072 else 0
+    layers = min(rng.randint(1, 24), max(1, 40_000_000 // (12 * hidden * hidden)))
+    vocab = _not_round(min(_log(rng, 100, 60_000), max(100, 40_000_000 // hidden)))
+    return _adamw(hidden, layers, 1, vocab, rng.choice(["f32", "f32", "bf16"]), rng.choice(["f32", "bf16", "f16"]),
+                  rng.choice([32, 8]), rng.random() < 0.6)
+
+
+def _shapes(case):
+    """the tensors of a transformer: tables, then each layer's attention, feed-forward and two norms, then the last norm"""
+    h = case["hidden"]
+    layer = [(h, h), (h,)] * 4 + [(4 * h, h), (4 * h,), (h, 4 * h), (h,)] + [(h,)] * 4
+    return [(case["vocab"], h)] * case["tables"] + layer * case["layers"] + [(h,)] * 2
+
+
+# ------------------------------------------------------------------------------------------
+class _State:
+    pass
+
+
+def _views(flat, at, shapes):
+    return [flat[i:i + math.prod(x)].view(x) for i, x in zip(at, shapes)]
+
+
+def _padded(rows, cols, pad, dtype, fill):
+    """rows `cols + pad` apart"""
+    whole = torch.zeros(rows, cols + pad, dtype=dtype, device=DEV)
+    whole[:, :cols] = fill
+    return whole[:, :cols]
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    s = _State()
+    s.case = case
+
+    def normal(*shape):
+        return torch.empty(*shape, device=DEV).normal_(generator=gen)
+
+    if case["kind"] == "norm":
+        rows, cols, dtype, w = case["rows"], case["cols"], TYPES[case["dtype"]], TYPES[case["w"]]
+        x = normal(rows, cols) * (0.3 * normal(rows, 1)).exp() + 0.2 * normal(rows, 1)
+        x[:, :: max(1, cols // 7)] *= 12.0               # a few channels are much larger than the others
+        s.x = _padded(rows, cols, case["pad"], dtype, x)
+        s.weight, s.bias = (1.0 + 0.1 * normal(cols)).to(w), (0.1 * normal(cols)).to(w)
+        f32 = dict(dtype=torch.float32, device=DEV)
+        if case["grad"]:
+            s.dy = _padded(rows, cols, case["pad"], dtype, 0.02 * normal(rows, cols))
+        if own:
+            s.y = torch.empty(rows, cols, dtype=dtype, device=DEV)
+            s.mean = s.rstd = s.workspace = None
+            if case["grad"]:
+                from paper_1903_04488_amd import binding as B
+                s.mean, s.rstd = torch.empty(rows, **f32), torch.empty(rows, **f32)
+                s.dx = torch.empty(rows, cols, dtype=dtype, device=DEV)
+                s.dweight, s.dbias = torch.empty_like(s.weight), torch.empty_like(s.bias)
+                s.workspace = torch.empty(B.cs_layer_norm_grad_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    elif case["kind"] == "token":
+        rows, vocab, dtype = case["rows"], case["vocab"], TYPES[case["dtype"]]
+        x = normal(rows, vocab)
+        x *= 2.0
+        # what a trained model gives: a few tokens stand out, and the right one is mostly among them
+        few = torch.randint(0, vocab, (rows, 6), device=DEV, generator=gen)
+        x.scatter_reduce_(1, few, math.log(vocab) + 1.0 + 0.7 * normal(rows, 6), "amax")
+        pick = torch.rand(rows, device=DEV, generator=gen)
+        s.target = torch.where(pick < 0.7, few[:, 0], torch.randint(0, vocab, (rows,), device=DEV, generator=gen))
+        if case["masked"]:
+            closed = torch.rand(rows, vocab, device=DEV, generator=gen) < 0.9
+            x.masked_fill_(closed.scatter_(1, few, False), -math.inf)
+            x[rows // 2] = -math.inf
+        if case["how"] != "forward":
+            s.target[pick > 0.95] = -1                    # padding: left out
+        s.logits = _padded(rows, vocab, case["pad"], dtype, x)
+        del x
+        if case["how"] == "loss":
+            # (gradients in binary16 are scaled up, as a training step does it)
+            s.g_logp = torch.full((rows,), -(4096.0 if case["dtype"] == "f16" else 1.0) / rows, device=DEV)
+            s.g_entropy = None
+        elif case["how"] == "policy":
+            s.g_logp, s.g_entropy = normal(rows) / rows, torch.full((rows,), -0.01 / rows, device=DEV)
+        if own:
+            f32 = dict(dtype=torch.float32, device=DEV)
+            s.logp, s.entropy, s.lse = (torch.empty(rows, **f32) for _ in range(3))
+            s.top_idx = s.top_logp = s.workspace = None
+            if case["how"] != "forward":
+                s.dlogits = torch.empty(rows, vocab, dtype=dtype, device=DEV)
+            if case["how"] != "loss":
+                from paper_1903_04488_amd import binding as B
+                k = case["top"]
+                if k:
+                    s.top_idx = torch.empty(rows, k, dtype=torch.int64, device=DEV)
+                    s.top_logp = torch.empty(rows, k, **f32)
+                n = B.cs_token_logprobs_workspace_bytes(rows, vocab, k)
+                s.workspace = torch.empty(n, dtype=torch.uint8, device=DEV)
+    else:
+        shapes = _shapes(case)
+        at, n = [], 0
+        for shape in shapes:
+            at.append(n)
+            n += -(-math.prod(shape) // 256) * 256
+        inside = torch.zeros(n, device=DEV)             # 1 in the tensors, 0 between them
+        torch._foreach_add_(_views(inside, at, shapes), 1.0)
+        s.p = (0.02 * normal(n) * inside).to(TYPES[case["p"]])
+        spread = (1.5 * normal(n) - 8.0).exp_() * inside   # the usual size of each parameter's gradient
+        s.g = (normal(n) * spread).to(TYPES[case["g"]])
+        s.m, s.v = normal(n) * spread * 0.3, (spread * (0.2 * normal(n)).exp_()) ** 2
+        s.step = STEP
+        s.max_norm = 0.5 if case["clip"] else None
+        s.m_exp = s.v_exp = None
+        if case["bits"] == 8:
+            (s.m, s.m_exp), (s.v, s.v_exp) = _encode(s.m, True), _encode(s.v.sqrt_(), False)
+        if own:
+            from paper_1903_04488_amd.training import AdamW
+            p, g, m, v = (_views(x, at, shapes) for x in (s.p, s.g, s.m, s.v))
+            exps = {}
+            if case["bits"] == 8:
+                s.m16, s.root_v16 = (torch.zeros(n, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+                s.moments = [_views(x, at, shapes) for x in (s.m16, s.root_v16)]
+                blocks = [(-(-math.prod(x) // 256),) for x in shapes]
+                exps = {name: _views(x, [i // 256 for i in at], blocks) for name, x in (("m_exp", s.m_exp), ("v_exp", s.v_exp))}
+            s.optimizer = AdamW(p, g, lr=LR, betas=(BETA1, BETA2), eps=ADAM_EPS, weight_decay=DECAY, max_norm=s.max_norm,
+                                bits=case["bits"], m=m, v=v, step_count=STEP, **exps)
+    return s
+
+
+# ------------------------------------------------------------------------------------------ moments in 8 bits
+def _encode(x, signed):
+    """(codes of the values x, blocks of 256 after one another, and every block's exponent byte)"""
+    u = x.view(torch.int32)
+    mag = u & 0x7FFFFFFF
+    ex = (mag.view(-1, 256).amax(1, keepdim=True) >> 23).clamp_(min=16)
+    rel = (mag.view(-1, 256) - ((ex - 15) << 23)).view(-1)
+    if signed:
+        code = ((rel + (1 << 19)) >> 20).clamp_(0, 127)
+        code |= (u >> 24) & 0x80
+    else:
+        code = ((rel + (1 << 18)) >> 19).clamp_(1, 255)
+        code *= mag != 0
+    return code.to(torch.uint8), ex.view(-1).to(torch.uint8)
+
+
+def _decode(code, ex, signed):
+    """the values, in 32 bits"""
+    code = code.int()
+    mag = code & 0x7F if signed else code
+    base = (ex.int()[:, None] - 15) << 23
+    x = ((mag << (20 if signed else 19)).view(-1, 256) + base).view(torch.float32).view(-1) * (mag != 0)
+    return torch.where(code >= 128, -x, x) if signed else x
+
+
+# ------------------------------------------------------------------------------------------ plain forms
+def _plain_norm(s):
+    x, w, b = s.x.float(), s.weight.float(), s.bias.float()
+    mean = x.mean(1, keepdim=True)
+    xh = x - mean
+    rstd = 1.0 / (xh.square().mean(1, keepdim=True) + EPS).sqrt()
+    xh = xh * rstd
+    out = {"y": (xh * w + b).to(s.x.dtype)}
+    if s.case["grad"]:
+        dy = s.dy.float()
+        a = dy * w
+        dx = rstd * (a - a.mean(1, keepdim=True) - xh * (a * xh).mean(1, keepdim=True))
+        out |= {"mean": mean[:, 0], "rstd": rstd[:, 0], "dx": dx.to(s.x.dtype),
+                "dweight": (dy * xh).sum(0).to(s.weight.dtype), "dbias": dy.sum(0).to(s.bias.dtype)}
+    return out
+
+
+def _top(x, k):
+    """positions of the k largest of each row, equal ones in order"""
+    u = (x + 0.0).view(torch.int32)
+    key = torch.where(u < 0, u ^ 0x7FFFFFFF, u).long()
+    order = torch.arange(x.shape[1], device=x.device)
+    return torch.topk((key << 32) + (0xFFFFFFFF - order), k, dim=1).indices
+
+
+def _plain_token(s):
+    how, k, scale = s.case["how"], s.case["top"], s.case["scale"]
+    x = s.logits.float()
+    z = x * scale
+    most = z.amax(1, keepdim=True)
+    empty = most == -math.inf
+    d = z - torch.where(empty, 0.0, most)
+    e = d.exp()
+    total = torch.where(empty, 1.0, e.sum(1, keepdim=True))
+    log_total = total.log()
+    lse = most + log_total
+    mean = torch.where(e > 0, e * d, 0.0).sum(1, keepdim=True) / total
+    entropy = log_total - mean
+    counts = ((s.target >= 0) & (s.target < z.shape[1]))[:, None]
+    at = s.target[:, None].clamp(0, z.shape[1] - 1)
+    logp = torch.where(counts, d.gather(1, at) - log_total, 0.0)
+    out = {"logp": logp[:, 0], "entropy": entropy[:, 0], "lse": lse[:, 0]}
+    if k:
+        idx = _top(x, k)
+        out |= {"top_idx": idx, "top_logp": d.gather(1, idx) - log_total}
+    if how != "forward":
+        p = e / total
+        g = torch.where(counts & ~empty, s.g_logp[:, None], 0.0)
+        dz = p * -g
+        if s.g_entropy is not None:
+            dz -= s.g_entropy[:, None] * torch.where(p > 0, p * (d - log_total + entropy), 0.0)
+        dz.scatter_add_(1, at, g)
+        out["dlogits"] = (dz * scale).to(s.logits.dtype)
+    return out
+
+
+def _plain_adamw(s):
+    """(all tensors at once: they lie in one buffer)"""
+    bits8 = s.case["bits"] == 8
+    p, g = s.p.float(), s.g.float()
+    out = {}
+    if s.max_norm is not None:
+        norm = g.double().square().sum().sqrt()
+        out["norm"] = norm.float()
+        g = g * torch.clamp(s.max_norm / (norm + 1e-6), max=1.0).float()
+    m, v = (_decode(s.m, s.m_exp, True), _decode(s.v, s.v_exp, False).square()) if bits8 else (s.m, s.v)
+    s.step += 1
+    c1, c2 = 1.0 / (1.0 - BETA1 ** s.step), 1.0 / math.sqrt(1.0 - BETA2 ** s.step)
+    m = m * BETA1 + g * (1.0 - BETA1)
+    v = v * BETA2 + g * g * (1.0 - BETA2)
+    root = v.sqrt()
+    s.p.copy_(p * (1.0 - LR * DECAY) - (m / (root * c2 + ADAM_EPS)) * (LR * c1))
+    if not bits8:
+        s.m, s.v = m, v
+        return out | {"p": s.p, "m": m, "v": v}
+    (s.m, s.m_exp), (s.v, s.v_exp) = _encode(m, True), _encode(root, False)
+    # (8 bits of a value are exact in bf16)
+    return out | {"p": s.p, "m": _decode(s.m, s.m_exp, True).bfloat16(), "root_v": _decode(s.v, s.v_exp, False).bfloat16()}
+
+
+# ------------------------------------------------------------------------------------------ the framework's calls
+def _own_norm(s):
+    from paper_1903_04488_amd import binding as B
+    B.cs_layer_norm(s.x, s.weight, s.bias, s.y, s.mean, s.rstd, EPS)
+    if not s.case["grad"]:
+        return {"y": s.y}
+    B.cs_layer_norm_grad(s.dy, s.x, s.weight, s.mean, s.rstd, s.dx, s.dweight, s.dbias, s.workspace)
+    return {"y": s.y, "mean": s.mean, "rstd": s.rstd, "dx": s.dx, "dweight": s.dweight, "dbias": s.dbias}
+
+
+def _own_token(s):
+    from paper_1903_04488_amd import binding as B
+    how, scale = s.case["how"], s.case["scale"]
+    out = {"logp": s.logp, "entropy": s.entropy, "lse": s.lse}
+    if how == "loss":
+        B.cs_token_loss(s.logits, s.target, s.g_logp, s.g_entropy, s.logp, s.entropy, s.lse, s.dlogits, scale)
+        return out | {"dlogits": s.dlogits}
+    B.cs_token_logprobs(s.logits, s.target, s.logp, s.entropy, s.lse, s.top_idx, s.top_logp, s.workspace, scale)
+    if how == "policy":
+        B.cs_token_logprobs_grad(s.logits, s.target, s.lse, s.entropy, s.g_logp, s.g_entropy, s.dlogits, scale)
+        return out | {"dlogits": s.dlogits}
+    return out | ({"top_idx": s.top_idx, "top_logp": s.top_logp} if s.case["top"] else {})
+
+
+def _own_adamw(s):
+    opt = s.optimizer
+    opt.step()
+    out = {} if s.max_norm is None else {"norm": opt.norm}
+    if s.case["bits"] == 8:
+        opt.moments(*s.moments)
+        return out | {"p": s.p, "m": s.m16, "root_v": s.root_v16}
+    return out | {"p": s.p, "m": s.m, "v": s.v}
+
+
+def run(s):
+    kind = s.case["kind"]
+    if kind == "norm":
+        return _own_norm(s) if own else _plain_norm(s)
+    if kind == "token":
+        return _own_token(s) if own else _plain_token(s)
+    return _own_adamw(s) if own else _plain_adamw(s)
+
+
+# ------------------------------------------------------------------------------------------
+def work(case):
+    """Bytes: every input read once, every output written once (logits read once by forward and once more by a gradient
+    that is asked for later)."""
+    if case["kind"] == "norm":
+        rows, cols = case["rows"], case["cols"]
+        n, one, weights = rows * cols, SIZE[case["dtype"]], cols * SIZE[case["w"]]
+        if not case["grad"]:
+            return {"bytes": 2 * n * one + 2 * weights, "flops": 8 * n}
+        return {"bytes": 5 * n * one + 5 * weights + 16 * rows, "flops": 22 * n}
+    if case["kind"] == "token":
+        rows, n, one = case["rows"], case["rows"] * case["vocab"], SIZE[case["dtype"]]
+        reads = {"forward": 1, "loss": 2, "policy": 3}[case["how"]]
+        return {"bytes": reads * n * one + rows * (20 + 12 * case["top"]), "flops": (6 if reads == 1 else 12) * n}
+    sizes = [math.prod(x) for x in _shapes(case)]
+    n = sum(sizes)
+    states = 16 * n if case["bits"] == 32 else 4 * n + 6 * n + 6 * sum(-(-x // 256) for x in sizes)
+    return {"bytes": n * (2 * SIZE[case["p"]] + SIZE[case["g"]]) + states, "flops": 16 * n}
+
+
+# ------------------------------------------------------------------------------------------ in 64 bits
+def _exact_norm(s):
+    x = s.x.double()
+    mean, var = x.mean(1), x.var(1, unbiased=False)
+    sd = (var + EPS) ** 0.5
+    unit = (x - mean[:, None]) / sd[:, None]
+    out = {"y": torch.addcmul(s.bias.double(), unit, s.weight.double())}
+    if s.case["grad"]:
+        dy, n = s.dy.double(), x.shape[1]
+        h = dy * s.weight.double()
+        along = (h * unit).sum(1) / n
+        out |= {"mean": mean, "rstd": 1 / sd, "dx": (h - (h.sum(1) / n)[:, None] - unit * along[:, None]) / sd[:, None],
+                "dweight": (dy * unit).sum(0), "dbias": dy.sum(0)}
+    return out
+
+
+def _exact_token(s):
+    """a piece of the rows at a time"""
+    how, k, scale = s.case["how"], s.case["top"], s.case["scale"]
+    parts = []
+    step = max(1, (1 << 25) // s.case["vocab"])
+    for a in range(0, s.case["rows"], step):
+        logits = s.logits[a:a + step].double() * scale
+        t = s.target[a:a + step]
+        lse = torch.logsumexp(logits, 1)
+        none = torch.isneginf(lse)
+        lp = torch.where(none[:, None], -math.inf, logits - lse[:, None])
+        p = lp.exp()
+        plp = torch.nan_to_num(p * lp, nan=0.0)
+        H = -plp.sum(1)
+        valid = (t >= 0) & (t < logits.shape[1])
+        row = torch.arange(len(t), device=DEV)
+        got = {"logp": torch.where(valid, lp[row, t.clamp(min=0)], 0.0), "entropy": H, "lse": lse}
+        if k:
+            got["top_logp"] = lp.sort(1, descending=True).values[:, :k]
+        if how != "forward":
+            g = torch.where(valid & ~none, s.g_logp[a:a + step].double(), 0.0)
+            d = -g[:, None] * p
+            d[row, t.clamp(min=0)] += g
+            if s.g_entropy is not None:
+                d -= s.g_entropy[a:a + step].double()[:, None] * (plp + p * H[:, None])
+            got["dlogits"] = d * scale
+        parts.append(got)
+    out = {name: torch.cat([x[name] for x in parts]) for name in parts[0]}
+    if k:
+        out["top_idx"] = None
+    # (in the order of run's outputs)
+    return {name: out[name] for name in ("logp", "entropy", "lse", "top_idx", "top_logp", "dlogits") if name in out}
+
+
+def _values_of_codes(signed):
+    """the value of every code for the exponent byte 127, from the format's definition"""
+    values = []
+    for code in range(256):
+        mag, bits = (code & 127, 3) if signed else (code, 4)
+        v = 2.0 ** ((mag >> bits) - 15) * (1 + (mag % (1 << bits)) / (1 << bits)) if mag else 0.0
+        values.append(-v if signed and code & 128 else v)
+    return torch.tensor(values, dtype=torch.float64, device=DEV)
+
+
+def _rounded8(x, signed):
+    """the values that 8 bits hold for x"""
+    x = x.view(-1, 256)
+    top = torch.frexp(x.abs().amax(1, keepdim=True).clamp(min=2.0 ** -111)).exponent - 1
+    values = _values_of_codes(signed)[:128 if signed else 256].contiguous()
+    # the value of a code is that of the one below up to the middle of both; code 0 stands where the format's exponent 0 is
+    grid = values.clone()
+    grid[0] = 2.0 ** -15
+    code = torch.bucketize(torch.ldexp(x.abs(), -top), (grid[1:] + grid[:-1]) / 2, right=True)
+    if not signed:
+        code = torch.where(x == 0, 0, code.clamp(min=1))
+    return (torch.ldexp(values[code], top) * x.sign()).view(-1)
+
+
+def _exact_adamw(s):
+    bits8 = s.case["bits"] == 8
+    p, g = s.p.double(), s.g.double()
+    out = {}
+    if s.max_norm is not None:
+        out["norm"] = g.dot(g) ** 0.5
+        g *= torch.clamp(s.max_norm / (out["norm"] + 1e-6), max=1.0)
+    if bits8:
+        def read(code, ex, signed):
+            return _values_of_codes(signed)[code.long()] * (2.0 ** (ex.double() - 127)).repeat_interleave(256)
+        m, v = read(s.m, s.m_exp, True), read(s.v, s.v_exp, False) ** 2
+    else:
+        m, v = s.m.double(), s.v.double()
+    t = s.step + 1
+    m = BETA1 * m + (1 - BETA1) * g
+    v = BETA2 * v + (1 - BETA2) * g ** 2
+    update = (m / (1 - BETA1 ** t)) / ((v / (1 - BETA2 ** t)) ** 0.5 + ADAM_EPS)
+    out["p"] = p - LR * (update + DECAY * p)
+    if bits8:
+        return out | {"m": _rounded8(m, True), "root_v": _rounded8(v ** 0.5, False)}
+    return out | {"m": m, "v": v}
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["kind"] == "norm":
+        return _exact_norm(s)
+    return _exact_token(s) if case["kind"] == "token" else _exact_adamw(s)
