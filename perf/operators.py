@@ -201,17 +201,15 @@ def prepare(case, seed):
         if own:
             f32 = dict(dtype=torch.float32, device=DEV)
             s.logp, s.entropy, s.lse = (torch.empty(rows, **f32) for _ in range(3))
-            s.top_idx = s.top_logp = s.workspace = None
+            s.top_idx = s.top_logp = None
             if case["how"] != "forward":
                 s.dlogits = torch.empty(rows, vocab, dtype=dtype, device=DEV)
-            if case["how"] != "loss":
-                from paper_1903_04488_amd import binding as B
-                k = case["top"]
-                if k:
-                    s.top_idx = torch.empty(rows, k, dtype=torch.int64, device=DEV)
-                    s.top_logp = torch.empty(rows, k, **f32)
-                n = B.cs_token_logprobs_workspace_bytes(rows, vocab, k)
-                s.workspace = torch.empty(n, dtype=torch.uint8, device=DEV)
+            from paper_1903_04488_amd import binding as B
+            k = case["top"]
+            if k:
+                s.top_idx = torch.empty(rows, k, dtype=torch.int64, device=DEV)
+                s.top_logp = torch.empty(rows, k, **f32)
+            s.workspace = torch.empty(B.cs_token_workspace_bytes(rows, vocab, k), dtype=torch.uint8, device=DEV)
     else:
         shapes = _shapes(case)
         at, n = [], 0
@@ -363,7 +361,8 @@ def _own_token(s):
     how, scale = s.case["how"], s.case["scale"]
     out = {"logp": s.logp, "entropy": s.entropy, "lse": s.lse}
     if how == "loss":
-        B.cs_token_loss(s.logits, s.target, s.g_logp, s.g_entropy, s.logp, s.entropy, s.lse, s.dlogits, scale)
+        B.cs_token_loss(s.logits, s.target, s.g_logp, s.g_entropy, s.logp, s.entropy, s.lse, s.dlogits, s.workspace,
+                        scale)
         return out | {"dlogits": s.dlogits}
     B.cs_token_logprobs(s.logits, s.target, s.logp, s.entropy, s.lse, s.top_idx, s.top_logp, s.workspace, scale)
     if how == "policy":
