@@ -228,16 +228,17 @@ def prepare(case, seed):
         if case["bits"] == 8:
             (s.m, s.m_exp), (s.v, s.v_exp) = _encode(s.m, True), _encode(s.v.sqrt_(), False)
         if own:
-            from paper_1903_04488_amd.training import AdamW
+            from paper_1903_04488_amd.training import AdamW, MomentReader
             p, g, m, v = (_views(x, at, shapes) for x in (s.p, s.g, s.m, s.v))
             exps = {}
             if case["bits"] == 8:
                 s.m16, s.root_v16 = (torch.zeros(n, dtype=torch.bfloat16, device=DEV) for _ in range(2))
-                s.moments = [_views(x, at, shapes) for x in (s.m16, s.root_v16)]
                 blocks = [(-(-math.prod(x) // 256),) for x in shapes]
                 exps = {name: _views(x, [i // 256 for i in at], blocks) for name, x in (("m_exp", s.m_exp), ("v_exp", s.v_exp))}
             s.optimizer = AdamW(p, g, lr=LR, betas=(BETA1, BETA2), eps=ADAM_EPS, weight_decay=DECAY, max_norm=s.max_norm,
-                                bits=case["bits"], m=m, v=v, step_count=STEP, **exps)
+                                bits=case["bits"], m=m, v=v, steps=STEP, **exps)
+            if case["bits"] == 8:
+                s.reader = MomentReader(s.optimizer, *(_views(x, at, shapes) for x in (s.m16, s.root_v16)))
     return s
 
 
@@ -376,7 +377,7 @@ def _own_adamw(s):
     opt.step()
     out = {} if s.max_norm is None else {"norm": opt.norm}
     if s.case["bits"] == 8:
-        opt.moments(*s.moments)
+        s.reader.read()
         return out | {"p": s.p, "m": s.m16, "root_v": s.root_v16}
     return out | {"p": s.p, "m": s.m, "v": s.v}
 
