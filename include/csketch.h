@@ -521,6 +521,116 @@ int cs_sketch_feedback_pair(const cs_params* p, float* S_v, float* S_u, const in
 int cs_gather_feedback(const cs_params* p, const float* const* vec, int32_t W, const int64_t* idx, int64_t k, float alpha,
                        float* out, float* S_v, float* S_u, float* val_v, float* val_u, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * What stands on both sides of a language model's gradient in a training step: its last operators (layer norm, the
+ * loss over the vocabulary), and the optimizer.  The first two also serve (forward alone, single tokens).
+ *
+ * Types are CS_FMT_BF16, CS_FMT_F16 and CS_FMT_F32.  Rows are `cols` (`vocab`) values next to each other, a row begins
+ * `stride` values (>= cols) behind the one before; any alignment that the type has will do.  Sums are taken in binary32 or
+ * more, outputs rounded to their type once, to nearest.  An output array may be null where that is said, may be the input
+ * itself where that is said, and must not meet an input or another output otherwise (CS_EINVAL).  Every result is a
+ * deterministic function of its inputs. */
+#define CS_FMT_F32 2
+
+/* Layer norm of `rows` vectors of `cols` values:  mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *     y = (x - mean) rstd weight + bias
+ * x, y: device, type fmt, 1 <= cols <= 2^30; y may be x (same stride).  weight, bias: device, cols values each, type w_fmt
+ * (fmt or CS_FMT_F32), each may be NULL (1 and 0).  mean, rstd: device float[rows], for the gradient, or both NULL. */
+int cs_layer_norm(const void* x, int64_t rows, int64_t cols, int64_t x_stride, int32_t fmt, const void* weight,
+                  const void* bias, int32_t w_fmt, float eps, void* y, int64_t y_stride, float* mean, float* rstd,
+                  void* stream);
+/* Its gradient, from dy and what the forward pass left.  With xh = (x - mean) rstd, a = dy weight:
+ *     dx = rstd (a - sum a / cols - xh sum(a xh) / cols),  dweight = sum over rows of dy xh,  dbias = sum over rows of dy
+ * dx (may be dy or x, with the same stride), dweight, dbias: each may be NULL and is not computed then.  With no rows
+ * dweight and dbias are 0.  workspace: device, cs_layer_norm_grad_workspace_bytes, 4-byte aligned; not read or
+ * written where dweight and dbias are NULL. */
+int cs_layer_norm_grad_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes);
+int cs_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x, int64_t x_stride, int64_t rows, int64_t cols,
+                       int32_t fmt, const void* weight, int32_t w_fmt, const float* mean, const float* rstd, void* dx,
+                       int64_t dx_stride, void* dweight, void* dbias, void* workspace, size_t ws_bytes, void* stream);
+
+/* Log probabilities of given tokens under rows of logits.  With z = scale x (scale > 0 and finite, 1 / temperature):
+ *     lse = ln sum_v exp z_v,  logp = z_target - lse,  entropy = -sum_v p_v ln p_v,  p_v = exp(z_v - lse)
+ * and the `top` tokens with the largest logits, largest first, equal ones lower index first, with their log probabilities.
+ * logits: device, 1 <= vocab <= 2^30, rows <= 2^24.  target: device int64[rows]; one outside [0, vocab) leaves its row
+ * out (logp 0).  logp, entropy, lse: device float[rows], each may be NULL (target too, with logp).  0 <= top <= min(vocab,
+ * CS_TOKEN_MAX_TOP); top_idx, top_logp: device int64 / float[rows][top].
+ * A logit of -inf is a token that cannot be.  A row of nothing else is empty: lse and every log probability are -inf, the
+ * entropy is 0, the alternatives are 0, 1, ...  A NaN or +inf makes its row's lse, logp and entropy NaN; as an
+ * alternative a NaN ranks with -inf.
+ * workspace: device, cs_token_workspace_bytes(rows, vocab, top), 8-byte aligned (may be NULL where that is 0). */
+#define CS_TOKEN_MAX_TOP 64
+int cs_token_workspace_bytes(int64_t rows, int64_t vocab, int32_t top, size_t* bytes);
+int cs_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale,
+                      const int64_t* target, float* logp, float* entropy, float* lse, int32_t top, int64_t* top_idx,
+                      float* top_logp, void* workspace, size_t ws_bytes, void* stream);
+/* The gradient of sum over rows of g_logp logp + g_entropy entropy with respect to the logits:
+ *     dlogits_v = scale (g_logp ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy))
+ * lse, entropy: what cs_token_logprobs gave for these logits and this scale.  g_logp (with target), g_entropy (with
+ * entropy): device float[rows], each may be NULL (0).  dlogits: type of the logits; may be the logits (same stride).
+ * Rows without a target have no g_logp; an empty row's gradient is 0. */
+int cs_token_logprobs_grad(const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale,
+                           const int64_t* target, const float* lse, const float* entropy, const float* g_logp,
+                           const float* g_entropy, void* dlogits, int64_t d_stride, void* stream);
+/* Both at once, where the coefficients are known before (a loss that is a weighted sum of log probabilities): the logits are
+ * read from memory once.  g_entropy may be NULL, nothing else.  workspace: cs_token_workspace_bytes(rows, vocab, 0). */
+int cs_token_loss(const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale,
+                  const int64_t* target, const float* g_logp, const float* g_entropy, float* logp, float* entropy,
+                  float* lse, void* dlogits, int64_t d_stride, void* workspace, size_t ws_bytes, void* stream);
+
+/* Many tensors, for one launch over all of them.  cs_tensor_list_build writes `count` tensors' addresses and lengths into
+ * `memory` (device, cs_tensor_list_bytes, 8-byte aligned) and fills *list (host), which is handed to the calls below.  Both are
+ * the caller's; the list holds while the tensors stay where they are, and is built again (a few small launches) when they
+ * move.  n, p, g, m, v, m_exp, v_exp: HOST arrays of `count` lengths (>= 0) and device pointers; the build has read them when it
+ * returns.
+ *   p: parameters, p_fmt.  g: gradients, g_fmt.
+ *   m, v, bits = 32: first and second moments, float.
+ *   bits = 8: m holds codes of the first moment, v codes of the second moment's ROOT, a byte each; m_exp, v_exp a byte for each
+ *   CS_ADAMW_BLOCK values.  In a block with exponent byte E (16 .. 255), a first moment's code is a sign bit, then c of
+ *   7 bits, 4 of them exponent e and 3 fraction f: 2^(E - 127 + e - 15) (1 + f / 8); a root's code is c of 8 bits, 4 and 4:
+ *   2^(E - 127 + e - 15) (1 + f / 16); c = 0 is the value 0.  E is the exponent field of the block's largest magnitude, or
+ *   16; values are rounded to nearest, halves away from 0, up to the largest code, and a root that is not 0 is at
+ *   least code 1.  All bytes 0 in m and v, E = 16: moments of 0.
+ * Different tensors must lie apart, as must the arrays of one tensor (the latter is checked). */
+#define CS_ADAMW_BLOCK 256
+typedef struct cs_tensor_list {
+    void* memory;               /* device */
+    int64_t chunks;             /* pieces of work */
+    int32_t count, p_fmt, g_fmt, bits;
+} cs_tensor_list;
+int cs_tensor_list_bytes(const int64_t* n, int32_t count, size_t* bytes);
+int cs_tensor_list_build(const int64_t* n, int32_t count, void* const* p, int32_t p_fmt, const void* const* g,
+                         int32_t g_fmt, void* const* m, void* const* v, int32_t bits, uint8_t* const* m_exp,
+                         uint8_t* const* v_exp, void* memory, size_t bytes, cs_tensor_list* list, void* stream);
+
+/* Global norm of the gradients of a list, and the coefficient that clips it:
+ *     out[0] = sqrt(sum of squares over all tensors)   (in binary64, rounded once)
+ *     out[1] = min(1, max_norm / (out[0] + 1e-6)), NaN where the norm is not finite
+ * out: device float[2].  max_norm > 0 (infinity: the norm alone).  workspace: device, 8-byte aligned. */
+int cs_grad_norm_workspace_bytes(const cs_tensor_list* list, size_t* bytes);
+int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, void* stream);
+
+/* One AdamW step, the step-th (from 1), over all tensors of a list:
+ *     m = beta1 m + (1 - beta1) s g,  v = beta2 v + (1 - beta2) (s g)^2
+ *     p = p (1 - lr weight_decay) - lr c1 (m / (sqrt(v) c2 + eps)),  c1 = 1 / (1 - beta1^step),  c2 = 1 / sqrt(1 - beta2^step)
+ * in binary32, every operation rounded by itself in this order (constants in binary64, rounded once); p takes the
+ * moments as they are before they are rounded to 8 bits.  s: 1, or *grad_scale_or_null (device: clipping, loss scale); where
+ * that is not finite nothing is written.
+ * coefs_or_null: device float[CS_ADAMW_COEFS] that cs_adamw_advance filled, in place of step and of what h says (for steps
+ * that are replayed from a graph): it counts *step up (device int64) and takes lr from *lr_or_null (device double) if given. */
+#define CS_ADAMW_COEFS 8
+typedef struct cs_adamw {
+    double lr, beta1, beta2, eps, weight_decay;      /* all finite and >= 0, betas below 1 */
+} cs_adamw;
+int cs_adamw_advance(const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream);
+int cs_adamw_step(const cs_adamw* h, int64_t step, const cs_tensor_list* list, const float* coefs_or_null,
+                  const float* grad_scale_or_null, void* stream);
+/* Moments in 8 bits out of and into a list whose p stands for the first moment's values and g for the root's:
+ * cs_moments_read writes them in bf16, which holds them exactly (p_fmt, g_fmt CS_FMT_BF16); cs_moments_write takes them in
+ * binary32 (CS_FMT_F32; roots >= 0) and rounds them to 8 bits. */
+int cs_moments_read(const cs_tensor_list* list, void* stream);
+int cs_moments_write(const cs_tensor_list* list, void* stream);
+
 const char* cs_status_string(int status);
 
 #ifdef __cplusplus

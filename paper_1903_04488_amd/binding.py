@@ -82,6 +82,15 @@ class CsParams(ctypes.Structure):
                 ("lists", _CsLists)]
 
 
+class CsTensorList(ctypes.Structure):
+    _fields_ = [("memory", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("count", ctypes.c_int32),
+                ("p_fmt", ctypes.c_int32), ("g_fmt", ctypes.c_int32), ("bits", ctypes.c_int32)]
+
+
+class CsAdamw(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -201,6 +210,32 @@ _SIGNATURES = {
                              ctypes.c_void_p, ctypes.c_void_p],
     "cs_dense_mask": [ctypes.POINTER(ctypes.c_void_p), ctypes.POINTER(ctypes.c_void_p),
                       ctypes.c_int32, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p],
+    "cs_layer_norm": [ctypes.c_void_p, *[ctypes.c_int64] * 3, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p,
+                      ctypes.c_int32, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, *[ctypes.c_void_p] * 3],
+    "cs_layer_norm_grad_workspace_bytes": [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_layer_norm_grad": [ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, *[ctypes.c_int64] * 3, ctypes.c_int32,
+                           ctypes.c_void_p, ctypes.c_int32, *[ctypes.c_void_p] * 3, ctypes.c_int64,
+                           *[ctypes.c_void_p] * 3, ctypes.c_size_t, ctypes.c_void_p],
+    "cs_token_workspace_bytes": [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_token_logprobs": [ctypes.c_void_p, *[ctypes.c_int64] * 3, ctypes.c_int32, ctypes.c_float,
+                          *[ctypes.c_void_p] * 4, ctypes.c_int32, *[ctypes.c_void_p] * 3, ctypes.c_size_t, ctypes.c_void_p],
+    "cs_token_logprobs_grad": [ctypes.c_void_p, *[ctypes.c_int64] * 3, ctypes.c_int32, ctypes.c_float,
+                               *[ctypes.c_void_p] * 6, ctypes.c_int64, ctypes.c_void_p],
+    "cs_token_loss": [ctypes.c_void_p, *[ctypes.c_int64] * 3, ctypes.c_int32, ctypes.c_float, *[ctypes.c_void_p] * 7,
+                      ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
+    "cs_tensor_list_bytes": [ctypes.POINTER(ctypes.c_int64), ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_tensor_list_build": [ctypes.POINTER(ctypes.c_int64), ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p), ctypes.c_int32,
+                             ctypes.POINTER(ctypes.c_void_p), ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p),
+                             ctypes.POINTER(ctypes.c_void_p), ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p),
+                             ctypes.POINTER(ctypes.c_void_p), ctypes.c_void_p, ctypes.c_size_t,
+                             ctypes.POINTER(CsTensorList), ctypes.c_void_p],
+    "cs_grad_norm_workspace_bytes": [ctypes.POINTER(CsTensorList), ctypes.POINTER(ctypes.c_size_t)],
+    "cs_grad_norm": [ctypes.POINTER(CsTensorList), ctypes.c_double, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                     ctypes.c_void_p],
+    "cs_adamw_advance": [ctypes.POINTER(CsAdamw), *[ctypes.c_void_p] * 4],
+    "cs_adamw_step": [ctypes.POINTER(CsAdamw), ctypes.c_int64, ctypes.POINTER(CsTensorList), *[ctypes.c_void_p] * 3],
+    "cs_moments_read": [ctypes.POINTER(CsTensorList), ctypes.c_void_p],
+    "cs_moments_write": [ctypes.POINTER(CsTensorList), ctypes.c_void_p],
     "cs_sketch_feedback": [ctypes.POINTER(CsParams), ctypes.c_void_p, ctypes.c_void_p,
                            ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p],
 }
@@ -647,7 +682,7 @@ def cs_select_exact_topk(cand, x, k: int, idx_out, val_out, workspace):
         "cs_select_exact_topk")
 
 
-CS_FMT_BF16, CS_FMT_F16 = 0, 1
+CS_FMT_BF16, CS_FMT_F16, CS_FMT_F32 = 0, 1, 2
 
 
 def cs_quantize16(x, out, fmt: int):
@@ -739,3 +774,207 @@ def cs_sketch_feedback(p, S, idx, val):
     _check(load_library().cs_sketch_feedback(
         ctypes.byref(p), _dev(S, torch.float32, "S", _cells(p)), _dev(idx, torch.int64, "idx"),
         k, _dev(val, torch.float32, "val", k), _stream(S)), "cs_sketch_feedback")
+
+
+# ------------------------------------------------------------------------------------------
+# layer norm, token log probabilities, AdamW
+CS_TOKEN_MAX_TOP = 64
+CS_ADAMW_BLOCK = 256
+CS_ADAMW_COEFS = 8
+_FMT = {torch.bfloat16: CS_FMT_BF16, torch.float16: CS_FMT_F16, torch.float32: CS_FMT_F32}
+
+
+def _rows(t, name: str, like=None):
+    """(address, row stride) of a 2-d tensor whose rows are contiguous; of the shape and type of `like`"""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise CsError(f"{name} must be a tensor on the GPU")
+    if t.dtype not in _FMT:
+        raise CsError(f"{name} must have dtype bfloat16, float16 or float32, got {t.dtype}")
+    shape = t.shape
+    if len(shape) != 2 or shape[1] == 0:
+        raise CsError(f"{name} must have two dimensions, rows of at least one value, got {tuple(shape)}")
+    if like is not None and (shape != like.shape or t.dtype is not like.dtype):
+        raise CsError(f"{name} must have shape {tuple(like.shape)} and dtype {like.dtype}, got {tuple(shape)}, {t.dtype}")
+    cols = shape[1]
+    step, one = t.stride()
+    if one != 1 and cols > 1:
+        raise CsError(f"{name} must have contiguous rows")
+    if shape[0] <= 1:
+        step = cols
+    if step < cols:
+        raise CsError(f"{name} must have rows that do not overlap")
+    return t.data_ptr(), step
+
+
+def _maybe(t, dtype, name: str, numel: int):
+    return _dev(t, dtype, name, numel) if t is not None else None
+
+
+def _weights(weight, bias, x):
+    """(address, address, format) of what scales and shifts a norm's columns"""
+    given = [w for w in (weight, bias) if w is not None]
+    dtype = given[0].dtype if given else torch.float32
+    if dtype is not x.dtype and dtype is not torch.float32:
+        raise CsError(f"weight and bias must have dtype {x.dtype} or float32, got {dtype}")
+    cols = x.shape[1]
+    return _maybe(weight, dtype, "weight", cols), _maybe(bias, dtype, "bias", cols), _FMT[dtype]
+
+
+def cs_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5):
+    """x, y: [rows, cols], contiguous rows; weight, bias: [cols] or None; mean, rstd: [rows] float32 or both None"""
+    at, step = _rows(x, "x")
+    out, out_step = _rows(y, "y", x)
+    rows, cols = x.shape
+    w, b, w_fmt = _weights(weight, bias, x)
+    _check(load_library().cs_layer_norm(
+        at, rows, cols, step, _FMT[x.dtype], w, b, w_fmt, eps, out, out_step, _maybe(mean, torch.float32, "mean", rows),
+        _maybe(rstd, torch.float32, "rstd", rows), _stream(x)), "cs_layer_norm")
+
+
+def cs_layer_norm_grad_workspace_bytes(rows: int, cols: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_layer_norm_grad_workspace_bytes(rows, cols, ctypes.byref(n)), "cs_layer_norm_grad_workspace_bytes")
+    return n.value
+
+
+def cs_layer_norm_grad(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace):
+    """dx, dweight, dbias: each may be None (workspace too, without the last two)"""
+    at, step = _rows(x, "x")
+    d, d_step = _rows(dy, "dy", x)
+    out, out_step = _rows(dx, "dx", x) if dx is not None else (None, 0)
+    rows, cols = x.shape
+    dtype = next((w.dtype for w in (weight, dweight, dbias) if w is not None), torch.float32)
+    if dtype is not x.dtype and dtype is not torch.float32:
+        raise CsError(f"weights must have dtype {x.dtype} or float32, got {dtype}")
+    _check(load_library().cs_layer_norm_grad(
+        d, d_step, at, step, rows, cols, _FMT[x.dtype], _maybe(weight, dtype, "weight", cols), _FMT[dtype],
+        _dev(mean, torch.float32, "mean", rows), _dev(rstd, torch.float32, "rstd", rows), out, out_step,
+        _maybe(dweight, dtype, "dweight", cols), _maybe(dbias, dtype, "dbias", cols),
+        _maybe(workspace, torch.uint8, "workspace", None), workspace.numel() if workspace is not None else 0, _stream(x)),
+        "cs_layer_norm_grad")
+
+
+def cs_token_workspace_bytes(rows: int, vocab: int, top: int = 0) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_token_workspace_bytes(rows, vocab, top, ctypes.byref(n)), "cs_token_workspace_bytes")
+    return n.value
+
+
+def cs_token_logprobs(logits, target, logp, entropy, lse, top_idx, top_logp, workspace, scale: float = 1.0):
+    """logits: [rows, vocab]; target: [rows] int64; logp, entropy, lse: [rows] float32; top_idx, top_logp: [rows, top] int64
+    and float32.  None where it is not wanted."""
+    at, step = _rows(logits, "logits")
+    rows, vocab = logits.shape
+    top = 0
+    if top_idx is not None or top_logp is not None:
+        if top_idx is None or top_logp is None or top_idx.shape != top_logp.shape or top_idx.dim() != 2 or len(top_idx) != rows:
+            raise CsError(f"top_idx and top_logp must be [{rows}, top] both")
+        top = top_idx.shape[1]
+    f32 = torch.float32
+    _check(load_library().cs_token_logprobs(
+        at, rows, vocab, step, _FMT[logits.dtype], scale, _maybe(target, torch.int64, "target", rows),
+        _maybe(logp, f32, "logp", rows), _maybe(entropy, f32, "entropy", rows), _maybe(lse, f32, "lse", rows), top,
+        _maybe(top_idx, torch.int64, "top_idx", None), _maybe(top_logp, f32, "top_logp", None),
+        _maybe(workspace, torch.uint8, "workspace", None), workspace.numel() if workspace is not None else 0,
+        _stream(logits)), "cs_token_logprobs")
+
+
+def cs_token_logprobs_grad(logits, target, lse, entropy, g_logp, g_entropy, dlogits, scale: float = 1.0):
+    at, step = _rows(logits, "logits")
+    out, out_step = _rows(dlogits, "dlogits", logits)
+    rows, vocab = logits.shape
+    f32 = torch.float32
+    _check(load_library().cs_token_logprobs_grad(
+        at, rows, vocab, step, _FMT[logits.dtype], scale, _maybe(target, torch.int64, "target", rows),
+        _dev(lse, f32, "lse", rows), _maybe(entropy, f32, "entropy", rows), _maybe(g_logp, f32, "g_logp", rows),
+        _maybe(g_entropy, f32, "g_entropy", rows), out, out_step, _stream(logits)), "cs_token_logprobs_grad")
+
+
+def cs_token_loss(logits, target, g_logp, g_entropy, logp, entropy, lse, dlogits, workspace, scale: float = 1.0):
+    at, step = _rows(logits, "logits")
+    out, out_step = _rows(dlogits, "dlogits", logits)
+    rows, vocab = logits.shape
+    f32 = torch.float32
+    _check(load_library().cs_token_loss(
+        at, rows, vocab, step, _FMT[logits.dtype], scale, _dev(target, torch.int64, "target", rows),
+        _dev(g_logp, f32, "g_logp", rows), _maybe(g_entropy, f32, "g_entropy", rows), _dev(logp, f32, "logp", rows),
+        _dev(entropy, f32, "entropy", rows), _dev(lse, f32, "lse", rows), out, out_step,
+        _maybe(workspace, torch.uint8, "workspace", None), workspace.numel() if workspace is not None else 0,
+        _stream(logits)), "cs_token_loss")
+
+
+def _same_dtype(tensors, name):
+    dtype = tensors[0].dtype if tensors else torch.float32
+    if dtype not in _FMT:
+        raise CsError(f"{name} must have dtype bfloat16, float16 or float32, got {dtype}")
+    return dtype
+
+
+class TensorList:
+    """Many tensors checked once and laid out on the GPU for one launch over all of them (cs_tensor_list_build).  Holds the
+    tensors; `refresh` where some have moved.  m_exp and v_exp say that the moments are in 8 bits."""
+
+    def __init__(self, p, g, m, v, m_exp=None, v_exp=None):
+        self.memory = None
+        self.c = CsTensorList()
+        self.refresh(p, g, m, v, m_exp, v_exp)
+
+    def refresh(self, p, g, m, v, m_exp=None, v_exp=None):
+        bits = 32 if m_exp is None and v_exp is None else 8
+        n = [x.numel() for x in p]
+        each = {"p": (p, _same_dtype(p, "p")), "g": (g, _same_dtype(g, "g")),
+                "m": (m, torch.uint8 if bits == 8 else torch.float32), "v": (v, torch.uint8 if bits == 8 else torch.float32)}
+        if bits == 8:
+            each |= {"m_exp": (m_exp, torch.uint8), "v_exp": (v_exp, torch.uint8)}
+        ptrs = {}
+        for name, (tensors, dtype) in each.items():
+            if tensors is None or len(tensors) != len(n):
+                raise CsError(f"{name} must have {len(n)} tensors")
+            size = [-(-x // CS_ADAMW_BLOCK) for x in n] if name.endswith("_exp") else n
+            ptrs[name] = (ctypes.c_void_p * len(n))(*[_dev(t, dtype, f"{name}[{i}]", k)
+                                                      for i, (t, k) in enumerate(zip(tensors, size))])
+        sizes, need = (ctypes.c_int64 * len(n))(*n), ctypes.c_size_t()
+        _check(load_library().cs_tensor_list_bytes(sizes, len(n), ctypes.byref(need)), "cs_tensor_list_bytes")
+        self.device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
+        if any(t.device != self.device for tensors, _ in each.values() for t in tensors):
+            raise CsError("the tensors of a list must be on one GPU")
+        if self.memory is None or self.memory.numel() < need.value or self.memory.device != self.device:
+            self.memory = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        self.tensors = {name: list(tensors) for name, (tensors, _) in each.items()}
+        _check(load_library().cs_tensor_list_build(
+            sizes, len(n), ptrs["p"], _FMT[each["p"][1]], ptrs["g"], _FMT[each["g"][1]], ptrs["m"], ptrs["v"], bits,
+            ptrs.get("m_exp"), ptrs.get("v_exp"), self.memory.data_ptr(), self.memory.numel(), ctypes.byref(self.c),
+            _stream(self.memory)), "cs_tensor_list_build")
+
+
+def cs_grad_norm_workspace_bytes(tensors: TensorList) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_grad_norm_workspace_bytes(ctypes.byref(tensors.c), ctypes.byref(n)), "cs_grad_norm_workspace_bytes")
+    return n.value
+
+
+def cs_grad_norm(tensors: TensorList, max_norm: float, out, workspace):
+    _check(load_library().cs_grad_norm(
+        ctypes.byref(tensors.c), max_norm, _dev(out, torch.float32, "out", 2), _dev(workspace, torch.uint8, "workspace"),
+        workspace.numel(), _stream(tensors.memory)), "cs_grad_norm")
+
+
+def cs_adamw_advance(h: CsAdamw, step, coefs, lr=None):
+    """step: int64 tensor of one value, counted up; lr: float64 tensor of one value, or None for h.lr"""
+    _check(load_library().cs_adamw_advance(
+        ctypes.byref(h), _dev(step, torch.int64, "step", 1), _maybe(lr, torch.float64, "lr", 1),
+        _dev(coefs, torch.float32, "coefs", CS_ADAMW_COEFS), _stream(step)), "cs_adamw_advance")
+
+
+def cs_adamw_step(h: CsAdamw, step: int, tensors: TensorList, coefs=None, grad_scale=None):
+    _check(load_library().cs_adamw_step(
+        ctypes.byref(h), step, ctypes.byref(tensors.c), _maybe(coefs, torch.float32, "coefs", CS_ADAMW_COEFS),
+        _maybe(grad_scale, torch.float32, "grad_scale", 1), _stream(tensors.memory)), "cs_adamw_step")
+
+
+def cs_moments_read(tensors: TensorList):
+    _check(load_library().cs_moments_read(ctypes.byref(tensors.c), _stream(tensors.memory)), "cs_moments_read")
+
+
+def cs_moments_write(tensors: TensorList):
+    _check(load_library().cs_moments_write(ctypes.byref(tensors.c), _stream(tensors.memory)), "cs_moments_write")

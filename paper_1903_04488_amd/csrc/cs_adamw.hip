@@ -1,0 +1,493 @@
+// AdamW over many tensors in one launch, with moments in 32 or 8 bits, and the gradients' global norm.
+//     m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g g,  p = p (1 - lr wd) - lr c1 (m / (sqrt(v) c2 + eps))
+//     c1 = 1 / (1 - b1^t),  c2 = 1 / sqrt(1 - b2^t)
+// Every product and sum is rounded by itself, in the order above (no fused multiply-add), so that a plain program
+// gives the same bits: a moment held in 8 bits then never falls to the other side of a rounding boundary.
+//
+// Moments in 8 bits: a block of 256 values of a tensor keeps the exponent field ex of its largest magnitude (at least 16), which
+// stands for 2^(ex - 127); a code's bits are the top bits of the value's own binary32 pattern, its exponent counted from ex - 15.
+// First moment: sign, 4 exponent bits, 3 fraction bits.  Root of the second moment: 4 and 4.  (The
+// root, as its square has twice the range; and a root that is not 0 never becomes code 0, as m / eps would be a leap.)
+// Rounded to nearest, halves away from 0: half a step is 1/16 of a first moment, 1/32 of a root.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "cs_rows.h"
+#include "csketch.h"
+
+namespace cs {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlock8 = CS_ADAMW_BLOCK;              // values that share an exponent
+constexpr int kChunk = 4096;                         // values that a workgroup takes
+constexpr int kBatch = 56;                           // tensors that one launch writes into a list (4 KB of arguments)
+
+// A list in device memory: this, then Tensor[count], then Chunk[chunks].
+struct Tensor {
+    void* p;
+    const void* g;
+    void *m, *v;
+    uint8_t *m_exp, *v_exp;
+    int64_t n;
+    int64_t first_chunk;
+};
+struct Chunk {
+    int32_t tensor, part;
+};
+struct Batch {
+    Tensor t[kBatch];
+};
+static_assert(sizeof(Batch) < 3800, "kernel arguments are limited to 4 KB");
+
+__global__ void __launch_bounds__(64) k_list_tensors(Batch b, Tensor* out, int count) {
+    if (static_cast<int>(threadIdx.x) < count) out[threadIdx.x] = b.t[threadIdx.x];
+}
+// every chunk's tensor: the last that begins at or before it
+__global__ void __launch_bounds__(kThreads) k_list_chunks(const Tensor* tensors, int count, Chunk* out, int64_t chunks) {
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (c >= chunks) return;
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (tensors[mid].first_chunk <= c) lo = mid;
+        else hi = mid - 1;
+    }
+    out[c] = Chunk{lo, static_cast<int32_t>(c - tensors[lo].first_chunk)};
+}
+
+// ---------------------------------------------------------------------------------------
+// 8 bits
+// ---------------------------------------------------------------------------------------
+__device__ __forceinline__ int32_t bits_of(float x) { return __float_as_int(x); }
+__device__ __forceinline__ int32_t base_of(int32_t ex) { return (ex - 15) << 23; }
+
+__device__ __forceinline__ float first_of(uint32_t code, int32_t base) {
+    const uint32_t mag = code & 0x7f;
+    const float x = __int_as_float(static_cast<int32_t>(mag << 20) + base);
+    return mag ? (code & 0x80 ? -x : x) : 0.f;
+}
+__device__ __forceinline__ float root_of(uint32_t code, int32_t base) {
+    return code ? __int_as_float(static_cast<int32_t>(code << 19) + base) : 0.f;
+}
+// (magnitudes are patterns of at most 31 bits and base is at least 1 << 23: no difference or sum leaves 32 bits)
+__device__ __forceinline__ uint32_t code_of_first(float x, int32_t base) {
+    const int32_t rel = (bits_of(x) & 0x7fffffff) - base;
+    const int32_t c = (rel + (1 << 19)) >> 20;
+    return static_cast<uint32_t>(min(max(c, 0), 127)) | (static_cast<uint32_t>(bits_of(x)) >> 24 & 0x80u);
+}
+__device__ __forceinline__ uint32_t code_of_root(float x, int32_t base) {
+    const int32_t mag = bits_of(x) & 0x7fffffff;
+    const int32_t c = (mag - base + (1 << 18)) >> 19;
+    return mag ? static_cast<uint32_t>(min(max(c, 1), 255)) : 0u;
+}
+__device__ __forceinline__ int32_t wave_max_bits(int32_t v) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = max(v, __shfl_xor(v, d));
+    return v;
+}
+__device__ __forceinline__ int32_t exponent_of(int32_t most_bits) { return max(most_bits >> 23, 16); }
+
+// ---------------------------------------------------------------------------------------
+// the step
+// ---------------------------------------------------------------------------------------
+struct Coefs {
+    float b1, one_b1, b2, one_b2, keep, c2, rate, eps;
+};
+
+struct Moved {
+    float p, m, v, root;
+};
+__device__ __forceinline__ Moved move(float p, float g, float m, float v, const Coefs& c) {
+#pragma clang fp contract(off)
+    Moved r;
+    r.m = m * c.b1 + g * c.one_b1;
+    r.v = v * c.b2 + g * g * c.one_b2;
+    r.root = sqrtf(r.v);
+    r.p = p * c.keep - (r.m / (r.root * c.c2 + c.eps)) * c.rate;
+    return r;
+}
+
+// four values of a lane, the first of them at `at`; beyond n: 0
+template <typename T>
+__device__ __forceinline__ void load4(const T* x, int64_t at, int64_t n, float (&v)[4]) {
+    if (at + 4 <= n) {
+        load_pack<T, 4>(x + at, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = at + e < n ? static_cast<float>(x[at + e]) : 0.f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T* x, int64_t at, int64_t n, const float (&v)[4]) {
+    if (at + 4 <= n) {
+        store_pack<T, 4>(x + at, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) x[at + e] = static_cast<T>(v[e]);
+    }
+}
+__device__ __forceinline__ uint32_t load4_codes(const uint8_t* x, int64_t at, int64_t n) {
+    uint32_t c = 0;
+    if (at + 4 <= n) {
+        __builtin_memcpy(&c, x + at, 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) c |= static_cast<uint32_t>(x[at + e]) << (8 * e);
+    }
+    return c;
+}
+__device__ __forceinline__ void store4_codes(uint8_t* x, int64_t at, int64_t n, uint32_t c) {
+    if (at + 4 <= n) {
+        __builtin_memcpy(x + at, &c, 4);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (at + e < n) x[at + e] = static_cast<uint8_t>(c >> (8 * e));
+    }
+}
+
+// A wavefront takes blocks of 256 values, four a lane.
+template <typename P, typename G, bool EIGHT>
+__global__ void __launch_bounds__(kThreads)
+k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs, const float* grad_scale) {
+    float scale = 1.f;
+    if (grad_scale) {
+        scale = *grad_scale;
+        if (!(fabsf(scale) < INFINITY)) return;       // gradients that are not finite: no step
+    }
+    if (coefs) c = *coefs;
+    const Chunk ch = chunks[blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t begin = static_cast<int64_t>(ch.part) * kChunk;
+    for (int k = wave; k < kChunk / kBlock8; k += kThreads / 64) {
+        const int64_t block = begin + k * kBlock8, at = block + lane * 4;
+        if (block >= t.n) return;                     // (the whole wavefront)
+        float p[4], g[4], m[4], v[4], root[4];
+        load4(static_cast<const P*>(t.p), at, t.n, p);
+        load4(static_cast<const G*>(t.g), at, t.n, g);
+        if (EIGHT) {
+            const int32_t mb = base_of(t.m_exp[block / kBlock8]), vb = base_of(t.v_exp[block / kBlock8]);
+            const uint32_t mc = load4_codes(static_cast<const uint8_t*>(t.m), at, t.n);
+            const uint32_t vc = load4_codes(static_cast<const uint8_t*>(t.v), at, t.n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[e] = first_of(mc >> (8 * e) & 0xff, mb);
+                const float r = root_of(vc >> (8 * e) & 0xff, vb);
+                v[e] = r * r;
+            }
+        } else {
+            load4(static_cast<const float*>(t.m), at, t.n, m);
+            load4(static_cast<const float*>(t.v), at, t.n, v);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const Moved r = move(p[e], grad_scale ? g[e] * scale : g[e], m[e], v[e], c);
+            p[e] = r.p, m[e] = r.m, v[e] = r.v, root[e] = r.root;
+        }
+        store4(static_cast<P*>(t.p), at, t.n, p);
+        if (EIGHT) {
+            // (values beyond n are 0 all along)
+            int32_t mm = 0, vm = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mm = max(mm, bits_of(m[e]) & 0x7fffffff);
+                vm = max(vm, bits_of(root[e]) & 0x7fffffff);
+            }
+            const int32_t me = exponent_of(wave_max_bits(mm)), ve = exponent_of(wave_max_bits(vm));
+            uint32_t mc = 0, vc = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mc |= code_of_first(m[e], base_of(me)) << (8 * e);
+                vc |= code_of_root(root[e], base_of(ve)) << (8 * e);
+            }
+            store4_codes(static_cast<uint8_t*>(t.m), at, t.n, mc);
+            store4_codes(static_cast<uint8_t*>(t.v), at, t.n, vc);
+            if (lane == 0) {
+                t.m_exp[block / kBlock8] = static_cast<uint8_t>(me);
+                t.v_exp[block / kBlock8] = static_cast<uint8_t>(ve);
+            }
+        } else {
+            store4(static_cast<float*>(t.m), at, t.n, m);
+            store4(static_cast<float*>(t.v), at, t.n, v);
+        }
+    }
+}
+
+// The list's p and g take the moments' values: 8 bits into bf16 (exactly), or (WRITE) binary32 values p, g into 8 bits.
+template <bool WRITE>
+__global__ void __launch_bounds__(kThreads) k_moments(const Tensor* tensors, const Chunk* chunks) {
+    const Chunk ch = chunks[blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t begin = static_cast<int64_t>(ch.part) * kChunk;
+    for (int k = wave; k < kChunk / kBlock8; k += kThreads / 64) {
+        const int64_t block = begin + k * kBlock8, at = block + lane * 4;
+        if (block >= t.n) return;
+        float m[4], v[4];
+        if (WRITE) {
+            load4(static_cast<const float*>(t.p), at, t.n, m);
+            load4(static_cast<const float*>(t.g), at, t.n, v);
+            int32_t mm = 0, vm = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mm = max(mm, bits_of(m[e]) & 0x7fffffff);
+                vm = max(vm, bits_of(v[e]) & 0x7fffffff);
+            }
+            const int32_t me = exponent_of(wave_max_bits(mm)), ve = exponent_of(wave_max_bits(vm));
+            uint32_t mc = 0, vc = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mc |= code_of_first(m[e], base_of(me)) << (8 * e);
+                vc |= code_of_root(v[e], base_of(ve)) << (8 * e);
+            }
+            store4_codes(static_cast<uint8_t*>(t.m), at, t.n, mc);
+            store4_codes(static_cast<uint8_t*>(t.v), at, t.n, vc);
+            if (lane == 0) {
+                t.m_exp[block / kBlock8] = static_cast<uint8_t>(me);
+                t.v_exp[block / kBlock8] = static_cast<uint8_t>(ve);
+            }
+        } else {
+            const int32_t mb = base_of(t.m_exp[block / kBlock8]), vb = base_of(t.v_exp[block / kBlock8]);
+            const uint32_t mc = load4_codes(static_cast<const uint8_t*>(t.m), at, t.n);
+            const uint32_t vc = load4_codes(static_cast<const uint8_t*>(t.v), at, t.n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                m[e] = first_of(mc >> (8 * e) & 0xff, mb);
+                v[e] = root_of(vc >> (8 * e) & 0xff, vb);
+            }
+            store4(static_cast<bf16*>(t.p), at, t.n, m);
+            store4(static_cast<bf16*>(const_cast<void*>(t.g)), at, t.n, v);
+        }
+    }
+}
+
+__device__ __forceinline__ double block_sum(double s, double* lds) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// squares and their sums in binary64: no overflow, and nothing lost between large and small tensors
+template <typename G>
+__global__ void __launch_bounds__(kThreads) k_grad_squares(const Tensor* tensors, const Chunk* chunks, double* partials) {
+    __shared__ double lds[4];
+    const Chunk ch = chunks[blockIdx.x];
+    const Tensor t = tensors[ch.tensor];
+    const int64_t begin = static_cast<int64_t>(ch.part) * kChunk, end = min(begin + kChunk, t.n);
+    double s = 0.;
+    for (int64_t at = begin + threadIdx.x * 4; at < end; at += kThreads * 4) {
+        float g[4];
+        load4(static_cast<const G*>(t.g), at, t.n, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = fma(static_cast<double>(g[e]), static_cast<double>(g[e]), s);
+    }
+    s = block_sum(s, lds);
+    if (threadIdx.x == 0) partials[blockIdx.x] = s;
+}
+__global__ void __launch_bounds__(kThreads) k_grad_norm(const double* partials, int64_t chunks, double max_norm, float* out) {
+    __shared__ double lds[4];
+    double s = 0.;
+    for (int64_t i = threadIdx.x; i < chunks; i += kThreads) s += partials[i];
+    s = block_sum(s, lds);
+    if (threadIdx.x) return;
+    const double norm = sqrt(s), c = max_norm / (norm + 1e-6);
+    out[0] = static_cast<float>(norm);
+    out[1] = norm < INFINITY ? static_cast<float>(c < 1. ? c : 1.) : NAN;
+}
+
+__global__ void k_adamw_coefs(cs_adamw h, int64_t* step, const double* lr, Coefs* out) {
+    const int64_t t = ++*step;
+    const double rate = lr ? *lr : h.lr;
+    const double c1 = 1. / (1. - pow(h.beta1, static_cast<double>(t)));
+    const double c2 = 1. / sqrt(1. - pow(h.beta2, static_cast<double>(t)));
+    *out = Coefs{static_cast<float>(h.beta1), static_cast<float>(1. - h.beta1), static_cast<float>(h.beta2),
+                 static_cast<float>(1. - h.beta2), static_cast<float>(1. - rate * h.weight_decay), static_cast<float>(c2),
+                 static_cast<float>(rate * c1), static_cast<float>(h.eps)};
+}
+static_assert(sizeof(Coefs) == 4 * CS_ADAMW_COEFS, "csketch.h");
+
+// ---------------------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------------------
+constexpr int64_t kMaxValues = static_cast<int64_t>(1) << 40;
+
+int64_t chunks_of(const int64_t* n, int32_t count, bool& ok) {
+    int64_t chunks = 0, values = 0;
+    ok = true;
+    for (int32_t i = 0; i < count; ++i) {
+        if (n[i] < 0 || n[i] > kMaxValues || (values += n[i]) > kMaxValues) {
+            ok = false;
+            return 0;
+        }
+        chunks += (n[i] + kChunk - 1) / kChunk;
+    }
+    return chunks;
+}
+
+// what a cs_tensor_list says of its device memory
+struct List {
+    const Tensor* tensors;
+    const Chunk* chunks;
+};
+List list_of(const cs_tensor_list* l) {
+    const Tensor* t = static_cast<const Tensor*>(l->memory);
+    return List{t, reinterpret_cast<const Chunk*>(t + l->count)};
+}
+bool list_ok(const cs_tensor_list* l) {
+    return l && l->count >= 0 && l->chunks >= 0 && l->chunks < (static_cast<int64_t>(1) << 31) && (l->chunks == 0 || l->memory);
+}
+
+template <typename P, typename G>
+int adamw(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
+    const List at = list_of(l);
+    const unsigned grid = static_cast<unsigned>(l->chunks);
+    if (l->bits == 8) k_adamw<P, G, true><<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, c, coefs, grad_scale);
+    else k_adamw<P, G, false><<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, c, coefs, grad_scale);
+    return launched();
+}
+template <typename P>
+int adamw_p(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
+    if (l->g_fmt == CS_FMT_F32) return adamw<P, float>(l, c, coefs, grad_scale, stream);
+    if (l->g_fmt == CS_FMT_BF16) return adamw<P, bf16>(l, c, coefs, grad_scale, stream);
+    return adamw<P, f16>(l, c, coefs, grad_scale, stream);
+}
+
+bool hyper_ok(const cs_adamw* h) {
+    return h && h->lr >= 0. && h->lr < INFINITY && h->beta1 >= 0. && h->beta1 < 1. && h->beta2 >= 0. && h->beta2 < 1. &&
+           h->eps >= 0. && h->eps < INFINITY && h->weight_decay >= 0. && h->weight_decay < INFINITY;
+}
+
+}  // namespace
+}  // namespace cs
+
+using namespace cs;
+
+extern "C" int cs_tensor_list_bytes(const int64_t* n, int32_t count, size_t* bytes) {
+    bool ok = false;
+    if (count < 0 || (count && !n) || !bytes) return CS_EINVAL;
+    const int64_t chunks = chunks_of(n, count, ok);
+    if (!ok || chunks >= (static_cast<int64_t>(1) << 31)) return CS_EINVAL;
+    *bytes = static_cast<size_t>(count) * sizeof(Tensor) + static_cast<size_t>(chunks) * sizeof(Chunk);
+    return CS_OK;
+}
+
+extern "C" int cs_tensor_list_build(const int64_t* n, int32_t count, void* const* p, int32_t p_fmt, const void* const* g,
+                                    int32_t g_fmt, void* const* m, void* const* v, int32_t bits, uint8_t* const* m_exp,
+                                    uint8_t* const* v_exp, void* memory, size_t bytes, cs_tensor_list* list, void* stream) {
+    size_t need = 0;
+    if (int rc = cs_tensor_list_bytes(n, count, &need)) return rc;
+    if (!list || !fmt_ok(p_fmt) || !fmt_ok(g_fmt) || (bits != 8 && bits != 32)) return CS_EINVAL;
+    if (count && (!p || !g || !m || !v || (bits == 8 && (!m_exp || !v_exp)))) return CS_EINVAL;
+    if (bytes < need) return CS_EWORKSPACE;
+    if (need && (!memory || (reinterpret_cast<uintptr_t>(memory) & 7))) return CS_EINVAL;
+    const int64_t pb = fmt_bytes(p_fmt), gb = fmt_bytes(g_fmt), sb = bits / 8;
+    for (int32_t i = 0; i < count; ++i) {
+        if (n[i] == 0) continue;
+        const uintptr_t all[] = {reinterpret_cast<uintptr_t>(p[i]), reinterpret_cast<uintptr_t>(g[i]),
+                                 reinterpret_cast<uintptr_t>(m[i]), reinterpret_cast<uintptr_t>(v[i])};
+        if (!all[0] || !all[1] || !all[2] || !all[3] || all[0] % pb || all[1] % gb || (bits == 32 && (all[2] % 4 || all[3] % 4)))
+            return CS_EINVAL;
+        if (bits == 8 && (!m_exp[i] || !v_exp[i])) return CS_EINVAL;
+        // what a step writes of one tensor lies apart from the rest of it
+        const int64_t blocks = (n[i] + kBlock8 - 1) / kBlock8;
+        const void* at[] = {p[i], m[i], v[i], bits == 8 ? m_exp[i] : nullptr, bits == 8 ? v_exp[i] : nullptr, g[i]};
+        const int64_t size[] = {pb * n[i], sb * n[i], sb * n[i], blocks, blocks, gb * n[i]};
+        for (int a = 0; a < 6; ++a)
+            for (int b = 0; b < a; ++b)
+                if (spans_meet(at[a], size[a], at[b], size[b])) return CS_EINVAL;
+    }
+    bool ok = false;
+    *list = cs_tensor_list{memory, chunks_of(n, count, ok), count, p_fmt, g_fmt, bits};
+    if (count == 0) return CS_OK;
+    Tensor* tensors = static_cast<Tensor*>(memory);
+    int64_t chunk = 0;
+    for (int32_t i = 0; i < count; i += kBatch) {
+        Batch b = {};
+        const int k = count - i < kBatch ? count - i : kBatch;
+        for (int j = 0; j < k; ++j) {
+            b.t[j] = Tensor{p[i + j], g[i + j], m[i + j], v[i + j], bits == 8 ? m_exp[i + j] : nullptr,
+                            bits == 8 ? v_exp[i + j] : nullptr, n[i + j], chunk};
+            chunk += (n[i + j] + kChunk - 1) / kChunk;
+        }
+        k_list_tensors<<<1, 64, 0, stream_of(stream)>>>(b, tensors + i, k);
+        if (int rc = launched()) return rc;
+    }
+    if (chunk == 0) return CS_OK;
+    k_list_chunks<<<static_cast<unsigned>((chunk + kThreads - 1) / kThreads), kThreads, 0, stream_of(stream)>>>(
+        tensors, count, reinterpret_cast<Chunk*>(tensors + count), chunk);
+    return launched();
+}
+
+extern "C" int cs_grad_norm_workspace_bytes(const cs_tensor_list* list, size_t* bytes) {
+    if (!list_ok(list) || !bytes) return CS_EINVAL;
+    *bytes = static_cast<size_t>(list->chunks) * sizeof(double);
+    return CS_OK;
+}
+
+extern "C" int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, void* stream) {
+    if (!list_ok(list) || !out || !(max_norm > 0.)) return CS_EINVAL;
+    const size_t need = static_cast<size_t>(list->chunks) * sizeof(double);
+    if (ws_bytes < need) return CS_EWORKSPACE;
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7))) return CS_EINVAL;
+    if (spans_meet(out, 8, workspace, static_cast<int64_t>(need))) return CS_EINVAL;
+    const List at = list_of(list);
+    double* partials = static_cast<double*>(workspace);
+    const unsigned grid = static_cast<unsigned>(list->chunks);
+    const hipStream_t s = stream_of(stream);
+    if (grid) {
+        if (list->g_fmt == CS_FMT_F32) k_grad_squares<float><<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, partials);
+        else if (list->g_fmt == CS_FMT_BF16) k_grad_squares<bf16><<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, partials);
+        else k_grad_squares<f16><<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, partials);
+        if (int rc = launched()) return rc;
+    }
+    k_grad_norm<<<1, kThreads, 0, s>>>(partials, list->chunks, max_norm, out);
+    return launched();
+}
+
+extern "C" int cs_adamw_advance(const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream) {
+    if (!hyper_ok(h) || !step || !coefs) return CS_EINVAL;
+    k_adamw_coefs<<<1, 1, 0, stream_of(stream)>>>(*h, step, lr_or_null, reinterpret_cast<Coefs*>(coefs));
+    return launched();
+}
+
+extern "C" int cs_adamw_step(const cs_adamw* h, int64_t step, const cs_tensor_list* list, const float* coefs_or_null,
+                             const float* grad_scale_or_null, void* stream) {
+    if (!hyper_ok(h) || !list_ok(list) || (!coefs_or_null && step < 1)) return CS_EINVAL;
+    if (list->chunks == 0) return CS_OK;
+    Coefs c = {};
+    if (!coefs_or_null) {
+        const double c1 = 1. / (1. - pow(h->beta1, static_cast<double>(step)));
+        const double c2 = 1. / sqrt(1. - pow(h->beta2, static_cast<double>(step)));
+        c = Coefs{static_cast<float>(h->beta1), static_cast<float>(1. - h->beta1), static_cast<float>(h->beta2),
+                  static_cast<float>(1. - h->beta2), static_cast<float>(1. - h->lr * h->weight_decay),
+                  static_cast<float>(c2), static_cast<float>(h->lr * c1), static_cast<float>(h->eps)};
+    }
+    const Coefs* dc = reinterpret_cast<const Coefs*>(coefs_or_null);
+    const hipStream_t s = stream_of(stream);
+    if (list->p_fmt == CS_FMT_F32) return adamw_p<float>(list, c, dc, grad_scale_or_null, s);
+    if (list->p_fmt == CS_FMT_BF16) return adamw_p<bf16>(list, c, dc, grad_scale_or_null, s);
+    return adamw_p<f16>(list, c, dc, grad_scale_or_null, s);
+}
+
+extern "C" int cs_moments_read(const cs_tensor_list* list, void* stream) {
+    if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_BF16 || list->g_fmt != CS_FMT_BF16) return CS_EINVAL;
+    if (list->chunks == 0) return CS_OK;
+    const List at = list_of(list);
+    k_moments<false><<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
+    return launched();
+}
+
+extern "C" int cs_moments_write(const cs_tensor_list* list, void* stream) {
+    if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_F32 || list->g_fmt != CS_FMT_F32) return CS_EINVAL;
+    if (list->chunks == 0) return CS_OK;
+    const List at = list_of(list);
+    k_moments<true><<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
+    return launched();
+}
