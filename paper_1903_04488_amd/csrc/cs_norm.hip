@@ -100,25 +100,223 @@ k_norm_columns_any(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride,
             (lds[part][0][lane] + lds[part][1][lane]) + (lds[part][2][lane] + lds[part][3][lane]);
 }
 
-// dweight and dbias from the shares' partial sums, in a fixed order: 16 columns a workgroup, 16 shares at a time
+// dweight and dbias from the shares' partial sums, in a fixed order: 16 columns a workgroup, 64 shares at a time
+constexpr int kWeightsBlock = 1024;
 template <typename W>
-__global__ void __launch_bounds__(kNormBlock)
+__global__ void __launch_bounds__(kWeightsBlock)
 k_norm_weights(const float* partials, int shares, int64_t cols, W* dweight, W* dbias) {
-    __shared__ float lds[16][17];
+    __shared__ float lds[64][17];
     W* out = blockIdx.y ? dbias : dweight;
     if (!out) return;
     const int at = threadIdx.x & 15, part = threadIdx.x >> 4;
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 16 + at;
     float s = 0.f;
-    if (c < cols)
-        for (int g = part; g < shares; g += 16) s += partials[(static_cast<int64_t>(g) * 2 + blockIdx.y) * cols + c];
+    if (c < cols) {
+        const float* p = partials + static_cast<int64_t>(blockIdx.y) * cols + c;
+        int g = part;
+        for (; g + 3 * 64 < shares; g += 4 * 64) {
+            float v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = p[static_cast<int64_t>(g + 64 * k) * 2 * cols];
+            s += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        for (; g < shares; g += 64) s += p[static_cast<int64_t>(g) * 2 * cols];
+    }
     lds[part][at] = s;
     __syncthreads();
-    if (part == 0 && c < cols) {
-        s = 0.f;
+    for (int k = 32; k; k >>= 1) {
+        if (part < k) lds[part][at] += lds[part + k][at];
+        __syncthreads();
+    }
+    if (part == 0 && c < cols) out[c] = static_cast<W>(lds[0][at]);
+}
+
+// ---------------------------------------------------------------------------------------
+// Rows in registers, 16-byte packs: TPR threads hold a row, ITEMS packs each (thread t packs t, t + TPR, ...).
+// ---------------------------------------------------------------------------------------
+// A thread's columns.  A row that ends inside a pack has its last pack moved back to end with the row: the columns that it then
+// shares with the pack before are masked in sums (first: values of the last pack before it are another thread's) and written
+// twice with the same value.
+template <typename T, int TPR, int ITEMS>
+struct Slots {
+    static constexpr int P = kPack<T>;
+    int last, first;                     // column of the last pack; its values from `first` on are this thread's (P: none)
+    int t;
+    __device__ __forceinline__ Slots(int thread, int cols) : t(thread) {
+        const int at = (thread + TPR * (ITEMS - 1)) * P;
+        last = min(at, cols - P);
+        first = at < cols ? at - last : P;
+    }
+    __device__ __forceinline__ bool has(int i) const { return i < ITEMS - 1 || first < P; }
+    __device__ __forceinline__ int at(int i) const { return i < ITEMS - 1 ? (t + TPR * i) * P : last; }
+    __device__ __forceinline__ bool own(int i, int e) const { return i < ITEMS - 1 || e >= first; }
+};
+
+template <int TPR>
+constexpr int threads_of() { return TPR < kNormBlock ? kNormBlock : TPR; }
+
+template <typename T, typename W, int TPR, int ITEMS>
+__global__ void __launch_bounds__(threads_of<TPR>())
+k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, const W* bias, float eps, T* y,
+       int64_t y_stride, float* mean, float* rstd) {
+    constexpr int P = kPack<T>, ROWS = threads_of<TPR>() / TPR;
+    __shared__ float lds[2][1][16];
+    int turn = 0;
+    const int t = threadIdx.x % TPR;
+    const Slots<T, TPR, ITEMS> slot(t, cols);
+    const float per = 1.0f / static_cast<float>(cols);
+    const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    Raw<T, P> next[ITEMS];
+    const auto request = [&](int64_t r) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) s += lds[k][at];
-        out[c] = static_cast<W>(s);
+        for (int i = 0; i < ITEMS; ++i)
+            if (slot.has(i)) next[i].load(x + r * x_stride + slot.at(i));
+    };
+    if (row < rows) request(row);
+    for (; row < rows; row += step) {
+        float v[ITEMS][P];
+        float s[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                v[i][e] = next[i][e];
+                s[0] += slot.own(i, e) ? v[i][e] : 0.f;
+            }
+        if (row + step < rows) request(row + step);          // under way while this row is worked on
+        block_sums<TPR>(s, lds, turn);
+        const float mu = s[0] * per;
+        float q[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                v[i][e] -= mu;
+                const float d = slot.own(i, e) ? v[i][e] : 0.f;
+                q[0] = fmaf(d, d, q[0]);
+            }
+        block_sums<TPR>(q, lds, turn);
+        const float rs = 1.0f / sqrtf(fmaf(q[0], per, eps));
+        T* yr = y + row * y_stride;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (!slot.has(i)) continue;
+            float w[P], b[P];
+            if (weight) load_pack<W, P>(weight + slot.at(i), w);
+            if (bias) load_pack<W, P>(bias + slot.at(i), b);
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[i][e] = fmaf(v[i][e] * rs, weight ? w[e] : 1.f, bias ? b[e] : 0.f);
+            store_pack<T, P>(yr + slot.at(i), v[i]);
+        }
+        if (mean && t == 0) {
+            mean[row] = mu;
+            rstd[row] = rs;
+        }
+    }
+}
+
+// Each workgroup (for TPR = 64 each of its four wavefronts) takes rows of its own and keeps the sums of its columns'
+// gradients in registers until its last row; SUMS: they are wanted.
+template <typename T, typename W, int TPR, int ITEMS, bool SUMS>
+__global__ void __launch_bounds__(threads_of<TPR>())
+k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight,
+            const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* partials) {
+    constexpr int P = kPack<T>, ROWS = threads_of<TPR>() / TPR;
+    __shared__ float lds[2][2][16];
+    int turn = 0;
+    const int t = threadIdx.x % TPR;
+    const Slots<T, TPR, ITEMS> slot(t, cols);
+    const float per = 1.0f / static_cast<float>(cols);
+    float dw[ITEMS][P] = {}, db[ITEMS][P] = {};
+    const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    Raw<T, P> next_x[ITEMS], next_dy[ITEMS];
+    float next_mu = 0.f, next_rs = 0.f;
+    const auto request = [&](int64_t r) {
+        next_mu = mean[r], next_rs = rstd[r];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            if (slot.has(i)) {
+                next_x[i].load(x + r * x_stride + slot.at(i));
+                next_dy[i].load(dy + r * dy_stride + slot.at(i));
+            }
+    };
+    if (row < rows) request(row);
+    for (; row < rows; row += step) {
+        float v[ITEMS][P], a[ITEMS][P];
+        const float mu = next_mu, rs = next_rs;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[i][e] = next_x[i][e], a[i][e] = next_dy[i][e];
+        if (row + step < rows) request(row + step);          // under way while this row is worked on
+        float s[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float w[P];
+            if (weight && slot.has(i)) load_pack<W, P>(weight + slot.at(i), w);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const float xh = slot.own(i, e) ? (v[i][e] - mu) * rs : 0.f, d = slot.own(i, e) ? a[i][e] : 0.f;
+                if (SUMS) {
+                    dw[i][e] = fmaf(d, xh, dw[i][e]);
+                    db[i][e] += d;
+                }
+                const float h = weight ? d * w[e] : d;
+                s[0] += slot.own(i, e) ? h : 0.f;
+                s[1] = fmaf(slot.own(i, e) ? h : 0.f, xh, s[1]);
+            }
+        }
+        if (!dx) continue;
+        block_sums<TPR>(s, lds, turn);
+        const float m1 = s[0] * per, m2 = s[1] * per;
+        T* out = dx + row * dx_stride;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (!slot.has(i)) continue;
+            float w[P];
+            if (weight) load_pack<W, P>(weight + slot.at(i), w);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const float h = weight ? a[i][e] * w[e] : a[i][e], xh = (v[i][e] - mu) * rs;
+                a[i][e] = rs * (h - m1 - xh * m2);
+            }
+            store_pack<T, P>(out + slot.at(i), a[i]);
+        }
+    }
+    if (!SUMS) return;
+    float* mine = partials + static_cast<int64_t>(blockIdx.x) * 2 * cols;
+    if (ROWS == 1) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < P; ++e)
+                if (slot.own(i, e)) {
+                    mine[slot.at(i) + e] = dw[i][e];
+                    mine[cols + slot.at(i) + e] = db[i][e];
+                }
+    } else {
+        // the four wavefronts' sums, one after the other
+        __shared__ float sums[ROWS == 1 ? 1 : 2][ROWS == 1 ? 1 : TPR * ITEMS * P];
+        for (int w = 0; w < ROWS; ++w) {
+            if (static_cast<int>(threadIdx.x) / TPR == w) {
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                    for (int e = 0; e < P; ++e)
+                        if (slot.own(i, e)) {
+                            const int c = slot.at(i) + e;
+                            sums[0][c] = w ? sums[0][c] + dw[i][e] : dw[i][e];
+                            sums[1][c] = w ? sums[1][c] + db[i][e] : db[i][e];
+                        }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < cols; c += threads_of<TPR>()) {
+            mine[c] = sums[0][c];
+            mine[cols + c] = sums[1][c];
+        }
     }
 }
 
@@ -136,48 +334,137 @@ struct NormArgs {
     hipStream_t stream;
 };
 
+// How rows of `cols` values are held: threads a row and packs a thread, or threads = 0 (a value at a time).
+struct Held {
+    int threads, items;
+};
+Held held(int64_t cols, int32_t fmt) {
+    const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
+    if (cols < p) return {0, 0};
+    for (const int threads : {64, 256, 512}) {
+        const int64_t items = (packs + threads - 1) / threads;
+        if (items <= 4) return {threads, static_cast<int>(items)};
+    }
+    return {0, 0};
+}
+// The same for the backward pass, which keeps two sums a column besides: as few packs a thread as there are threads for.
+Held held_grad(int64_t cols, int32_t fmt) {
+    const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
+    if (cols < p) return {0, 0};
+    for (const int threads : {64, 256, 512}) {
+        const int64_t items = (packs + threads - 1) / threads;
+        if (items <= (threads == 64 ? 2 : threads == 256 ? 1 : 4)) return {threads, static_cast<int>(items)};
+    }
+    return {0, 0};
+}
+
+unsigned norm_grid(int64_t rows) { return static_cast<unsigned>(rows < 4096 ? rows : 4096); }
+// workgroups of the backward pass over rows that are held in registers; each leaves partial sums of the weights' gradients
+int grad_grid(int64_t rows, const Held& h) {
+    const int64_t groups = h.threads == 64 ? (rows + 3) / 4 : rows;
+    const int64_t most = h.threads == 512 ? (h.items == 1 ? 512 : 256) : (h.items == 1 ? 1024 : 768);
+    return static_cast<int>(groups < most ? groups : most);
+}
 // shares of the rows whose partial sums of the weights' gradients are added up at the end
-int norm_shares(int64_t rows, int64_t cols) {
+int norm_shares(int64_t rows, int64_t cols, int32_t fmt) {
+    const Held h = held_grad(cols, fmt);
+    if (h.threads) return grad_grid(rows, h);
     const int64_t blocks = (cols + 63) / 64;
     int64_t want = blocks >= 1024 ? 1 : (1024 + blocks - 1) / blocks;
     if (want > (rows + 15) / 16) want = (rows + 15) / 16;
     return static_cast<int>(want < 1 ? 1 : want);
 }
 
-unsigned norm_grid(int64_t rows) { return static_cast<unsigned>(rows < 4096 ? rows : 4096); }
+template <typename T, typename W, int TPR, int ITEMS>
+int norm_forward_held(const NormArgs& a) {
+    const int64_t groups = TPR == 64 ? (a.rows + 3) / 4 : a.rows;
+    const unsigned grid = static_cast<unsigned>(groups < 4096 ? groups : 4096);
+    k_norm<T, W, TPR, ITEMS><<<grid, threads_of<TPR>(), 0, a.stream>>>(
+        static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols), static_cast<const W*>(a.weight),
+        static_cast<const W*>(a.bias), a.eps, static_cast<T*>(a.out), a.out_stride, a.mean, a.rstd);
+    return launched();
+}
+template <typename T, typename W, int TPR, int ITEMS>
+int norm_grad_held(const NormArgs& a, const Held& h) {
+    const bool sums = a.dweight || a.dbias;
+    const auto kernel = sums ? k_norm_grad<T, W, TPR, ITEMS, true> : k_norm_grad<T, W, TPR, ITEMS, false>;
+    kernel<<<static_cast<unsigned>(grad_grid(a.rows, h)), threads_of<TPR>(), 0, a.stream>>>(
+        static_cast<const T*>(a.dy), a.dy_stride, static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols),
+        static_cast<const W*>(a.weight), a.mean, a.rstd, static_cast<T*>(a.out), a.out_stride, a.partials);
+    return launched();
+}
+#define CS_HELD(h, CALL)                                                                               \
+    switch ((h).threads * 8 + (h).items) {                                                             \
+        case 64 * 8 + 1: return CALL(64, 1);                                                           \
+        case 64 * 8 + 2: return CALL(64, 2);                                                           \
+        case 64 * 8 + 3: return CALL(64, 3);                                                           \
+        case 64 * 8 + 4: return CALL(64, 4);                                                           \
+        case 256 * 8 + 2: return CALL(256, 2);                                                         \
+        case 256 * 8 + 3: return CALL(256, 3);                                                         \
+        case 256 * 8 + 4: return CALL(256, 4);                                                         \
+        case 512 * 8 + 3: return CALL(512, 3);                                                         \
+        case 512 * 8 + 4: return CALL(512, 4);                                                         \
+        default: return CS_EINVAL;                                                                     \
+    }
+#define CS_HELD_GRAD(h, CALL)                                                                          \
+    switch ((h).threads * 8 + (h).items) {                                                             \
+        case 64 * 8 + 1: return CALL(64, 1);                                                           \
+        case 64 * 8 + 2: return CALL(64, 2);                                                           \
+        case 256 * 8 + 1: return CALL(256, 1);                                                         \
+        case 512 * 8 + 1: return CALL(512, 1);                                                         \
+        case 512 * 8 + 2: return CALL(512, 2);                                                         \
+        case 512 * 8 + 3: return CALL(512, 3);                                                         \
+        case 512 * 8 + 4: return CALL(512, 4);                                                         \
+        default: return CS_EINVAL;                                                                     \
+    }
 
 template <typename T, typename W>
 int norm_forward(const NormArgs& a) {
+    const Held h = held(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
+    if (h.threads) {
+#define CS_CALL(TPR, ITEMS) (norm_forward_held<T, W, TPR, ITEMS>(a))
+        CS_HELD(h, CS_CALL)
+#undef CS_CALL
+    }
     k_norm_any<T, W><<<norm_grid(a.rows), kNormBlock, 0, a.stream>>>(
         static_cast<const T*>(a.x), a.x_stride, a.rows, a.cols, static_cast<const W*>(a.weight),
         static_cast<const W*>(a.bias), a.eps, static_cast<T*>(a.out), a.out_stride, a.mean, a.rstd);
     return launched();
 }
 
+// dx and the shares' partial sums
 template <typename T, typename W>
-int norm_backward(const NormArgs& a) {
+int norm_grad(const NormArgs& a, int shares) {
     const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
+    const Held h = held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
+    if (h.threads) {
+#define CS_CALL(TPR, ITEMS) (norm_grad_held<T, W, TPR, ITEMS>(a, h))
+        CS_HELD_GRAD(h, CS_CALL)
+#undef CS_CALL
+    }
     if (a.dweight || a.dbias) {
-        int shares = 0;
-        if (a.rows) {
-            shares = norm_shares(a.rows, a.cols);
-            const dim3 grid(static_cast<unsigned>((a.cols + 63) / 64), shares);
-            k_norm_columns_any<T><<<grid, kNormBlock, 0, a.stream>>>(dy, a.dy_stride, x, a.x_stride, a.rows, a.cols, a.mean,
-                                                                     a.rstd, a.partials);
-            if (int rc = launched()) return rc;
-        }
-        const dim3 grid(static_cast<unsigned>((a.cols + 15) / 16), 2);
-        k_norm_weights<W><<<grid, kNormBlock, 0, a.stream>>>(a.partials, shares, a.cols, static_cast<W*>(a.dweight),
-                                                             static_cast<W*>(a.dbias));
+        const dim3 grid(static_cast<unsigned>((a.cols + 63) / 64), shares);
+        k_norm_columns_any<T><<<grid, kNormBlock, 0, a.stream>>>(dy, a.dy_stride, x, a.x_stride, a.rows, a.cols, a.mean,
+                                                                 a.rstd, a.partials);
         if (int rc = launched()) return rc;
     }
-    if (a.out && a.rows) {
-        k_norm_grad_any<T, W><<<norm_grid(a.rows), kNormBlock, 0, a.stream>>>(
-            dy, a.dy_stride, x, a.x_stride, a.rows, a.cols, static_cast<const W*>(a.weight), a.mean, a.rstd,
-            static_cast<T*>(a.out), a.out_stride);
-        return launched();
-    }
-    return CS_OK;
+    if (!a.out) return CS_OK;
+    k_norm_grad_any<T, W><<<norm_grid(a.rows), kNormBlock, 0, a.stream>>>(
+        dy, a.dy_stride, x, a.x_stride, a.rows, a.cols, static_cast<const W*>(a.weight), a.mean, a.rstd,
+        static_cast<T*>(a.out), a.out_stride);
+    return launched();
+}
+
+template <typename T, typename W>
+int norm_backward(const NormArgs& a) {
+    const int shares = a.rows ? norm_shares(a.rows, a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16) : 0;
+    if (a.rows)
+        if (int rc = norm_grad<T, W>(a, shares)) return rc;
+    if (!a.dweight && !a.dbias) return CS_OK;
+    const dim3 grid(static_cast<unsigned>((a.cols + 15) / 16), 2);
+    k_norm_weights<W><<<grid, kWeightsBlock, 0, a.stream>>>(a.partials, shares, a.cols, static_cast<W*>(a.dweight),
+                                                         static_cast<W*>(a.dbias));
+    return launched();
 }
 
 // weights in 32 bits, or in the rows' type
@@ -235,7 +522,9 @@ extern "C" int cs_layer_norm(const void* x, int64_t rows, int64_t cols, int64_t 
 
 extern "C" int cs_layer_norm_grad_workspace_bytes(int64_t rows, int64_t cols, size_t* bytes) {
     if (rows < 0 || cols < 1 || cols > kNormMaxCols || !bytes) return CS_EINVAL;
-    *bytes = static_cast<size_t>(norm_shares(rows, cols)) * 2 * cols * sizeof(float);
+    // (of either width of the rows' type)
+    const int a = norm_shares(rows, cols, CS_FMT_F32), b = norm_shares(rows, cols, CS_FMT_BF16);
+    *bytes = static_cast<size_t>(a > b ? a : b) * 2 * cols * sizeof(float);
     return CS_OK;
 }
 
@@ -256,7 +545,7 @@ extern "C" int cs_layer_norm_grad(const void* dy, int64_t dy_stride, const void*
     cs_layer_norm_grad_workspace_bytes(rows, cols, &need);
     const bool sums = dweight || dbias;
     if (sums && ws_bytes < need) return CS_EWORKSPACE;
-    if (sums && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3))) return CS_EINVAL;
+    if (sums && need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 3))) return CS_EINVAL;
     // what is written must not lie in what is still to be read
     const void* written[] = {dweight, dbias, sums ? workspace : nullptr};
     const int64_t size[] = {wb, wb, static_cast<int64_t>(need)};

@@ -19,11 +19,17 @@ constexpr int kPack = 16 / static_cast<int>(sizeof(T));
 // N values of type T from an address that is aligned to T alone: one 16-byte (or shorter) request, also where a row begins
 // off a 16-byte boundary (global memory is read and written at any alignment).
 template <typename T, int N>
+struct Raw {
+    T v[N];
+    __device__ __forceinline__ void load(const T* __restrict__ p) { __builtin_memcpy(v, p, sizeof(v)); }
+    __device__ __forceinline__ float operator[](int e) const { return static_cast<float>(v[e]); }
+};
+template <typename T, int N>
 __device__ __forceinline__ void load_pack(const T* __restrict__ p, float (&v)[N]) {
-    T raw[N];
-    __builtin_memcpy(raw, p, sizeof(raw));
+    Raw<T, N> raw;
+    raw.load(p);
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = static_cast<float>(raw[e]);
+    for (int e = 0; e < N; ++e) v[e] = raw[e];
 }
 // rounded to nearest, ties to even, once
 template <typename T, int N>
