@@ -216,24 +216,26 @@ k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, co
     }
 }
 
-// Each workgroup (for TPR = 64 each of its four wavefronts) takes rows of its own and keeps the sums of its columns'
-// gradients in registers until its last row; SUMS: they are wanted.
+// Each group of TPR threads of a workgroup takes rows of its own and keeps the sums of its columns' gradients in registers
+// until its last row; SUMS: they are wanted.
+constexpr int kGradBlock = 512;
 template <typename T, typename W, int TPR, int ITEMS, bool SUMS>
-__global__ void __launch_bounds__(threads_of<TPR>())
+__global__ void __launch_bounds__(kGradBlock)
 k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight,
             const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* partials) {
-    constexpr int P = kPack<T>, ROWS = threads_of<TPR>() / TPR;
+    constexpr int P = kPack<T>, ROWS = kGradBlock / TPR;
     __shared__ float lds[2][2][16];
     int turn = 0;
-    const int t = threadIdx.x % TPR;
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const Slots<T, TPR, ITEMS> slot(t, cols);
     const float per = 1.0f / static_cast<float>(cols);
     float dw[ITEMS][P] = {}, db[ITEMS][P] = {};
     const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
-    int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
+    int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS;         // of the workgroup's rows
     Raw<T, P> next_x[ITEMS], next_dy[ITEMS];
     float next_mu = 0.f, next_rs = 0.f;
-    const auto request = [&](int64_t r) {
+    const auto request = [&](int64_t of) {
+        const int64_t r = min(of + group, rows - 1);                 // (a group without a row left: in bounds)
         next_mu = mean[r], next_rs = rstd[r];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
@@ -242,15 +244,17 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
                 next_dy[i].load(dy + r * dy_stride + slot.at(i));
             }
     };
-    if (row < rows) request(row);
-    for (; row < rows; row += step) {
+    if (first < rows) request(first);
+    for (; first < rows; first += step) {
+        const int64_t row = first + group;
+        const bool has_row = ROWS == 1 || row < rows;
         float v[ITEMS][P], a[ITEMS][P];
         const float mu = next_mu, rs = next_rs;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-            for (int e = 0; e < P; ++e) v[i][e] = next_x[i][e], a[i][e] = next_dy[i][e];
-        if (row + step < rows) request(row + step);          // under way while this row is worked on
+            for (int e = 0; e < P; ++e) v[i][e] = next_x[i][e], a[i][e] = has_row ? next_dy[i][e] : 0.f;
+        if (first + step < rows) request(first + step);          // under way while this row is worked on
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -271,6 +275,7 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
         if (!dx) continue;
         block_sums<TPR>(s, lds, turn);
         const float m1 = s[0] * per, m2 = s[1] * per;
+        if (!has_row) continue;
         T* out = dx + row * dx_stride;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
@@ -297,10 +302,10 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
                     mine[cols + slot.at(i) + e] = db[i][e];
                 }
     } else {
-        // the four wavefronts' sums, one after the other
+        // the groups' sums, one after the other
         __shared__ float sums[ROWS == 1 ? 1 : 2][ROWS == 1 ? 1 : TPR * ITEMS * P];
         for (int w = 0; w < ROWS; ++w) {
-            if (static_cast<int>(threadIdx.x) / TPR == w) {
+            if (group == w) {
 #pragma unroll
                 for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
@@ -313,7 +318,7 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < cols; c += threads_of<TPR>()) {
+        for (int c = threadIdx.x; c < cols; c += kGradBlock) {
             mine[c] = sums[0][c];
             mine[cols + c] = sums[1][c];
         }
@@ -351,24 +356,23 @@ Held held(int64_t cols, int32_t fmt) {
 Held held_grad(int64_t cols, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
     if (cols < p) return {0, 0};
-    for (const int threads : {64, 256, 512}) {
+    for (const int threads : {64, 128, 256, 512}) {
         const int64_t items = (packs + threads - 1) / threads;
-        if (items <= (threads == 64 ? 2 : threads == 256 ? 1 : 4)) return {threads, static_cast<int>(items)};
+        if (items <= (threads == 512 ? 4 : 1)) return {threads, static_cast<int>(items)};
     }
     return {0, 0};
 }
 
 unsigned norm_grid(int64_t rows) { return static_cast<unsigned>(rows < 4096 ? rows : 4096); }
 // workgroups of the backward pass over rows that are held in registers; each leaves partial sums of the weights' gradients
-int grad_grid(int64_t rows, const Held& h) {
-    const int64_t groups = h.threads == 64 ? (rows + 3) / 4 : rows;
-    const int64_t most = h.threads == 512 ? (h.items == 1 ? 512 : 256) : (h.items == 1 ? 1024 : 768);
-    return static_cast<int>(groups < most ? groups : most);
+int grad_grid(int64_t rows, const Held& h, int32_t fmt) {
+    const int64_t groups = kGradBlock / h.threads, n = (rows + groups - 1) / groups, most = h.items * (16 / fmt_bytes(fmt)) <= 8 ? 512 : 256;
+    return static_cast<int>(n < most ? n : most);
 }
 // shares of the rows whose partial sums of the weights' gradients are added up at the end
 int norm_shares(int64_t rows, int64_t cols, int32_t fmt) {
     const Held h = held_grad(cols, fmt);
-    if (h.threads) return grad_grid(rows, h);
+    if (h.threads) return grad_grid(rows, h, fmt);
     const int64_t blocks = (cols + 63) / 64;
     int64_t want = blocks >= 1024 ? 1 : (1024 + blocks - 1) / blocks;
     if (want > (rows + 15) / 16) want = (rows + 15) / 16;
@@ -385,10 +389,10 @@ int norm_forward_held(const NormArgs& a) {
     return launched();
 }
 template <typename T, typename W, int TPR, int ITEMS>
-int norm_grad_held(const NormArgs& a, const Held& h) {
+int norm_grad_held(const NormArgs& a, int shares) {
     const bool sums = a.dweight || a.dbias;
     const auto kernel = sums ? k_norm_grad<T, W, TPR, ITEMS, true> : k_norm_grad<T, W, TPR, ITEMS, false>;
-    kernel<<<static_cast<unsigned>(grad_grid(a.rows, h)), threads_of<TPR>(), 0, a.stream>>>(
+    kernel<<<static_cast<unsigned>(shares), kGradBlock, 0, a.stream>>>(
         static_cast<const T*>(a.dy), a.dy_stride, static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols),
         static_cast<const W*>(a.weight), a.mean, a.rstd, static_cast<T*>(a.out), a.out_stride, a.partials);
     return launched();
@@ -409,7 +413,7 @@ int norm_grad_held(const NormArgs& a, const Held& h) {
 #define CS_HELD_GRAD(h, CALL)                                                                          \
     switch ((h).threads * 8 + (h).items) {                                                             \
         case 64 * 8 + 1: return CALL(64, 1);                                                           \
-        case 64 * 8 + 2: return CALL(64, 2);                                                           \
+        case 128 * 8 + 1: return CALL(128, 1);                                                         \
         case 256 * 8 + 1: return CALL(256, 1);                                                         \
         case 512 * 8 + 1: return CALL(512, 1);                                                         \
         case 512 * 8 + 2: return CALL(512, 2);                                                         \
@@ -438,7 +442,7 @@ int norm_grad(const NormArgs& a, int shares) {
     const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
     const Held h = held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
     if (h.threads) {
-#define CS_CALL(TPR, ITEMS) (norm_grad_held<T, W, TPR, ITEMS>(a, h))
+#define CS_CALL(TPR, ITEMS) (norm_grad_held<T, W, TPR, ITEMS>(a, shares))
         CS_HELD_GRAD(h, CS_CALL)
 #undef CS_CALL
     }

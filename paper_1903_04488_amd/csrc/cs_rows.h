@@ -61,8 +61,9 @@ __device__ __forceinline__ float wave_max(float v) {
     return v;
 }
 
-// Sums of THREADS threads, the same in every thread; `turn` counts the calls of a kernel (two buffers take turns, so that
-// one barrier a call is enough).  THREADS = 64: one wavefront, no barrier.
+// Sums over groups of THREADS threads of a workgroup, the same in every thread of a group; `turn` counts the calls of a kernel
+// (two buffers take turns, so that one barrier a call is enough; every group of the workgroup makes the same calls).
+// THREADS = 64: one wavefront, no barrier.
 template <int THREADS, int N>
 __device__ __forceinline__ void block_sums(float (&v)[N], float (&lds)[2][N][16], int& turn) {
 #pragma unroll
@@ -70,7 +71,7 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (&lds)[2][N][16]
     if (THREADS == 64) return;
     float(&buf)[N][16] = lds[turn & 1];
     ++turn;
-    const int wave = threadIdx.x >> 6;
+    const int wave = threadIdx.x >> 6, first = threadIdx.x / THREADS * (THREADS / 64);
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
         for (int k = 0; k < N; ++k) buf[k][wave] = v[k];
@@ -79,7 +80,7 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (&lds)[2][N][16]
     for (int k = 0; k < N; ++k) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < THREADS / 64; ++w) s += buf[k][w];
+        for (int w = 0; w < THREADS / 64; ++w) s += buf[k][first + w];
         v[k] = s;
     }
 }
