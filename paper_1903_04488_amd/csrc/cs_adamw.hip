@@ -122,7 +122,7 @@ __device__ __forceinline__ void load4(const T* x, int64_t at, int64_t n, float (
 template <typename T>
 __device__ __forceinline__ void store4(T* x, int64_t at, int64_t n, const float (&v)[4]) {
     if (at + 4 <= n) {
-        store_pack<T, 4>(x + at, v);
+        store_pack<false>(x + at, v);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -160,7 +160,8 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
         if (!(fabsf(scale) < INFINITY)) return;       // gradients that are not finite: no step
     }
     if (coefs) c = *coefs;
-    const Chunk ch = chunks[blockIdx.x];
+    // (from the last chunk down: the gradients' norm has just read them upwards, and the caches hold the end of them)
+    const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
     const Tensor t = tensors[ch.tensor];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t begin = static_cast<int64_t>(ch.part) * kChunk;
@@ -274,27 +275,40 @@ __device__ __forceinline__ double block_sum(double s, double* lds) {
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// squares and their sums in binary64: no overflow, and nothing lost between large and small tensors
+// Squares and their sums in binary64: no overflow, and nothing lost between large and small tensors.  Workgroup w takes chunks
+// w, w + gridDim, ...; a thread's four requests of a chunk are under way together.
+constexpr int kSquares = 2048;                       // workgroups, and partial sums
 template <typename G>
-__global__ void __launch_bounds__(kThreads) k_grad_squares(const Tensor* tensors, const Chunk* chunks, double* partials) {
+__global__ void __launch_bounds__(kThreads)
+k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double* partials) {
     __shared__ double lds[4];
-    const Chunk ch = chunks[blockIdx.x];
-    const Tensor t = tensors[ch.tensor];
-    const int64_t begin = static_cast<int64_t>(ch.part) * kChunk, end = min(begin + kChunk, t.n);
     double s = 0.;
-    for (int64_t at = begin + threadIdx.x * 4; at < end; at += kThreads * 4) {
-        float g[4];
-        load4(static_cast<const G*>(t.g), at, t.n, g);
+    for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
+        const Chunk ch = chunks[c];
+        const int64_t n = tensors[ch.tensor].n, begin = static_cast<int64_t>(ch.part) * kChunk;
+        const G* g = static_cast<const G*>(tensors[ch.tensor].g);
+        constexpr int PER = kChunk / kThreads / 4;
+        float v[PER][4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = fma(static_cast<double>(g[e]), static_cast<double>(g[e]), s);
+        for (int k = 0; k < PER; ++k) load4(g, begin + (k * kThreads + threadIdx.x) * 4, n, v[k]);
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = fma(static_cast<double>(v[k][e]), static_cast<double>(v[k][e]), s);
     }
     s = block_sum(s, lds);
     if (threadIdx.x == 0) partials[blockIdx.x] = s;
 }
-__global__ void __launch_bounds__(kThreads) k_grad_norm(const double* partials, int64_t chunks, double max_norm, float* out) {
+__global__ void __launch_bounds__(kThreads) k_grad_norm(const double* partials, int count, double max_norm, float* out) {
     __shared__ double lds[4];
-    double s = 0.;
-    for (int64_t i = threadIdx.x; i < chunks; i += kThreads) s += partials[i];
+    double v[kSquares / kThreads], s = 0.;
+#pragma unroll
+    for (int k = 0; k < kSquares / kThreads; ++k) {
+        const int i = k * kThreads + threadIdx.x;
+        v[k] = i < count ? partials[i] : 0.;
+    }
+#pragma unroll
+    for (int k = 0; k < kSquares / kThreads; ++k) s += v[k];
     s = block_sum(s, lds);
     if (threadIdx.x) return;
     const double norm = sqrt(s), c = max_norm / (norm + 1e-6);
@@ -340,6 +354,7 @@ List list_of(const cs_tensor_list* l) {
     const Tensor* t = static_cast<const Tensor*>(l->memory);
     return List{t, reinterpret_cast<const Chunk*>(t + l->count)};
 }
+int partials_of(const cs_tensor_list* l) { return static_cast<int>(l->chunks < kSquares ? l->chunks : kSquares); }
 bool list_ok(const cs_tensor_list* l) {
     return l && l->count >= 0 && l->chunks >= 0 && l->chunks < (static_cast<int64_t>(1) << 31) && (l->chunks == 0 || l->memory);
 }
@@ -427,27 +442,28 @@ extern "C" int cs_tensor_list_build(const int64_t* n, int32_t count, void* const
 
 extern "C" int cs_grad_norm_workspace_bytes(const cs_tensor_list* list, size_t* bytes) {
     if (!list_ok(list) || !bytes) return CS_EINVAL;
-    *bytes = static_cast<size_t>(list->chunks) * sizeof(double);
+    *bytes = static_cast<size_t>(partials_of(list)) * sizeof(double);
     return CS_OK;
 }
 
 extern "C" int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, void* stream) {
     if (!list_ok(list) || !out || !(max_norm > 0.)) return CS_EINVAL;
-    const size_t need = static_cast<size_t>(list->chunks) * sizeof(double);
+    const size_t need = static_cast<size_t>(partials_of(list)) * sizeof(double);
     if (ws_bytes < need) return CS_EWORKSPACE;
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7))) return CS_EINVAL;
     if (spans_meet(out, 8, workspace, static_cast<int64_t>(need))) return CS_EINVAL;
     const List at = list_of(list);
     double* partials = static_cast<double*>(workspace);
-    const unsigned grid = static_cast<unsigned>(list->chunks);
+    const int grid = partials_of(list);
     const hipStream_t s = stream_of(stream);
     if (grid) {
-        if (list->g_fmt == CS_FMT_F32) k_grad_squares<float><<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, partials);
-        else if (list->g_fmt == CS_FMT_BF16) k_grad_squares<bf16><<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, partials);
-        else k_grad_squares<f16><<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, partials);
+        const auto kernel = list->g_fmt == CS_FMT_F32    ? k_grad_squares<float>
+                            : list->g_fmt == CS_FMT_BF16 ? k_grad_squares<bf16>
+                                                         : k_grad_squares<f16>;
+        kernel<<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, list->chunks, partials);
         if (int rc = launched()) return rc;
     }
-    k_grad_norm<<<1, kThreads, 0, s>>>(partials, list->chunks, max_norm, out);
+    k_grad_norm<<<1, kThreads, 0, s>>>(partials, grid, max_norm, out);
     return launched();
 }
 

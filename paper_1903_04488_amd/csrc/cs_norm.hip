@@ -155,7 +155,7 @@ struct Slots {
 template <int TPR>
 constexpr int threads_of() { return TPR < kNormBlock ? kNormBlock : TPR; }
 
-template <typename T, typename W, int TPR, int ITEMS>
+template <typename T, typename W, int TPR, int ITEMS, bool PAST>
 __global__ void __launch_bounds__(threads_of<TPR>())
 k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, const W* bias, float eps, T* y,
        int64_t y_stride, float* mean, float* rstd) {
@@ -207,7 +207,7 @@ k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, co
             if (bias) load_pack<W, P>(bias + slot.at(i), b);
 #pragma unroll
             for (int e = 0; e < P; ++e) v[i][e] = fmaf(v[i][e] * rs, weight ? w[e] : 1.f, bias ? b[e] : 0.f);
-            store_pack<T, P>(yr + slot.at(i), v[i]);
+            store_pack<PAST>(yr + slot.at(i), v[i]);
         }
         if (mean && t == 0) {
             mean[row] = mu;
@@ -219,7 +219,7 @@ k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, co
 // Each group of TPR threads of a workgroup takes rows of its own and keeps the sums of its columns' gradients in registers
 // until its last row; SUMS: they are wanted.
 constexpr int kGradBlock = 512;
-template <typename T, typename W, int TPR, int ITEMS, bool SUMS>
+template <typename T, typename W, int TPR, int ITEMS, bool SUMS, bool PAST>
 __global__ void __launch_bounds__(kGradBlock)
 k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight,
             const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* partials) {
@@ -287,7 +287,7 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
                 const float h = weight ? a[i][e] * w[e] : a[i][e], xh = (v[i][e] - mu) * rs;
                 a[i][e] = rs * (h - m1 - xh * m2);
             }
-            store_pack<T, P>(out + slot.at(i), a[i]);
+            store_pack<PAST>(out + slot.at(i), a[i]);
         }
     }
     if (!SUMS) return;
@@ -383,7 +383,8 @@ template <typename T, typename W, int TPR, int ITEMS>
 int norm_forward_held(const NormArgs& a) {
     const int64_t groups = TPR == 64 ? (a.rows + 3) / 4 : a.rows;
     const unsigned grid = static_cast<unsigned>(groups < 4096 ? groups : 4096);
-    k_norm<T, W, TPR, ITEMS><<<grid, threads_of<TPR>(), 0, a.stream>>>(
+    const auto kernel = past_caches(a.rows * a.cols * sizeof(T)) ? k_norm<T, W, TPR, ITEMS, true> : k_norm<T, W, TPR, ITEMS, false>;
+    kernel<<<grid, threads_of<TPR>(), 0, a.stream>>>(
         static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols), static_cast<const W*>(a.weight),
         static_cast<const W*>(a.bias), a.eps, static_cast<T*>(a.out), a.out_stride, a.mean, a.rstd);
     return launched();
@@ -391,7 +392,9 @@ int norm_forward_held(const NormArgs& a) {
 template <typename T, typename W, int TPR, int ITEMS>
 int norm_grad_held(const NormArgs& a, int shares) {
     const bool sums = a.dweight || a.dbias;
-    const auto kernel = sums ? k_norm_grad<T, W, TPR, ITEMS, true> : k_norm_grad<T, W, TPR, ITEMS, false>;
+    const bool past = past_caches(a.rows * a.cols * sizeof(T));
+    const auto kernel = sums ? (past ? k_norm_grad<T, W, TPR, ITEMS, true, true> : k_norm_grad<T, W, TPR, ITEMS, true, false>)
+                             : (past ? k_norm_grad<T, W, TPR, ITEMS, false, true> : k_norm_grad<T, W, TPR, ITEMS, false, false>);
     kernel<<<static_cast<unsigned>(shares), kGradBlock, 0, a.stream>>>(
         static_cast<const T*>(a.dy), a.dy_stride, static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols),
         static_cast<const W*>(a.weight), a.mean, a.rstd, static_cast<T*>(a.out), a.out_stride, a.partials);

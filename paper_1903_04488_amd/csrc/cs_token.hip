@@ -407,7 +407,7 @@ struct RowGrad {
     }
 };
 
-template <typename T>
+template <bool PAST, typename T>
 __device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int64_t first, int64_t last, const RowGrad& row) {
     constexpr int P = kPack<T>;
     for (int64_t q = first + threadIdx.x; q < last; q += kThreads) {
@@ -417,14 +417,14 @@ __device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int
             load_pack<T, P>(x + at, v);
 #pragma unroll
             for (int e = 0; e < P; ++e) v[e] = row.of(v[e], at + e == row.target);
-            store_pack<T, P>(dx + at, v);
+            store_pack<PAST>(dx + at, v);
         } else {
             for (int64_t i = at; i < vocab; ++i) dx[i] = static_cast<T>(row.of(static_cast<float>(x[i]), i == row.target));
         }
     }
 }
 
-template <typename T>
+template <typename T, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, const float* lse,
              const float* entropy, const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int pieces,
@@ -432,11 +432,11 @@ k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     const int64_t row = blockIdx.x / static_cast<unsigned>(pieces);
     const int64_t each = (packs + pieces - 1) / pieces, first = each * (blockIdx.x % static_cast<unsigned>(pieces));
     const RowGrad r(row, vocab, scale, target, lse[row], entropy ? entropy[row] : 0.f, g_logp, g_entropy);
-    grad_packs(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
+    grad_packs<PAST>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
 }
 
 // forward and gradient of a row in one workgroup: the row's second read comes from the caches
-template <typename T>
+template <typename T, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out,
              const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs) {
@@ -451,7 +451,7 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
     const RowGrad g(row, vocab, scale, target, empty ? -INFINITY : fmaf(r.m, scale, log_sum),
                     empty ? 0.f : log_sum - kLn2 * (r.U / r.S), g_logp, g_entropy);
-    grad_packs(x, dlogits + row * d_stride, vocab, 0, packs, g);
+    grad_packs<PAST>(x, dlogits + row * d_stride, vocab, 0, packs, g);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -520,7 +520,8 @@ int token_grad(const TokenArgs& a) {
     const int64_t most = ((static_cast<int64_t>(1) << 31) - 1) / a.rows;
     int64_t pieces = (packs + 4 * kThreads - 1) / (4 * kThreads);
     if (pieces > most) pieces = most;
-    k_token_grad<T><<<static_cast<unsigned>(a.rows * pieces), kThreads, 0, a.stream>>>(
+    const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_grad<T, true> : k_token_grad<T, false>;
+    kernel<<<static_cast<unsigned>(a.rows * pieces), kThreads, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.vocab, a.stride, a.scale, a.target, a.lse, a.entropy, a.g_logp, a.g_entropy,
         static_cast<T*>(a.dlogits), a.d_stride, static_cast<int>(pieces), packs);
     return launched();
@@ -532,7 +533,8 @@ int token_loss(TokenArgs a) {
         a.lse = a.out.lse, a.entropy = a.out.entropy;
         return token_grad<T>(a);
     }
-    k_token_loss<T><<<static_cast<unsigned>(a.rows), kThreads, 0, a.stream>>>(
+    const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_loss<T, true> : k_token_loss<T, false>;
+    kernel<<<static_cast<unsigned>(a.rows), kThreads, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.vocab, a.stride, a.scale, a.target, a.out, a.g_logp, a.g_entropy,
         static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt));
     return launched();
