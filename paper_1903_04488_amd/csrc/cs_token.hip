@@ -16,12 +16,14 @@
 namespace cs {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;                // of a row among many, and of the kernels that go by packs
+constexpr int kFewThreads = 1024;            // of a row among few, or of its part
 constexpr int kMaxTop = CS_TOKEN_MAX_TOP;
 constexpr int kList = 1024;                  // candidates for the alternatives of a part
 constexpr int kMaxParts = 64;                // workgroups that share a row
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kLog2e = 1.44269504088896341f;
 constexpr float kFar = -200.f;               // 2^kFar is 0 beside any sum
+constexpr float kPlain = -1e30f;             // values above this leave no product in the infinite
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -30,31 +32,45 @@ struct Sums {
     float m, S, U;
 };
 
-// candidates before others: larger values first, among equal ones the lower index; a NaN counts as -inf
-__device__ __forceinline__ float ranked(float v) { return v == v ? v : -INFINITY; }
+// Values in order as whole numbers; -0 is 0, a NaN counts as -inf.  With the index below it, what is larger comes first
+// among alternatives; 0 is none.
+__device__ __forceinline__ uint32_t order_of(float v) {
+    v = v == v ? v + 0.0f : -INFINITY;
+    const uint32_t u = __float_as_uint(v);
+    return u ^ (static_cast<uint32_t>(static_cast<int32_t>(u) >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t order) {
+    return __uint_as_float(order & 0x80000000u ? order ^ 0x80000000u : ~order);
+}
+__device__ __forceinline__ uint64_t key_of(float v, int64_t at) {
+    return static_cast<uint64_t>(order_of(v)) << 32 | (0xffffffffu - static_cast<uint32_t>(at));
+}
+__device__ __forceinline__ int64_t index_of(uint64_t key) { return 0xffffffffu - static_cast<uint32_t>(key); }
+// bits at the lower end of an order that a type's values have alike
+template <typename T>
+constexpr int kAlike = sizeof(T) == 4 ? 0 : sizeof(T) == 2 && static_cast<float>(static_cast<T>(65536.f)) == 65536.f ? 16 : 13;
 
+template <int THREADS>
 struct TokenShared {
     float f[3][16];
-    float value[kThreads];
-    int32_t pack[kThreads];
-    int32_t chosen[kMaxTop];
-    float list_value[kList];
-    int64_t list_at[kList];
+    int32_t order[THREADS / 4], pack[THREADS / 4];
+    uint64_t list[kList];
     int32_t n;
-    float best_value[16];
-    int64_t best_at[16];
+    uint64_t best[16];
 };
 
+template <int THREADS>
 __device__ __forceinline__ float block_max(float v, float (&buf)[16]) {
     v = wave_max(v);
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
     v = buf[0];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) v = fmaxf(v, buf[w]);
+    for (int w = 1; w < THREADS / 64; ++w) v = fmaxf(v, buf[w]);
     return v;
 }
 // (buffers of its own: no barrier before)
+template <int THREADS>
 __device__ __forceinline__ void block_add2(float& a, float& b, float (&ba)[16], float (&bb)[16]) {
     a = wave_sum(a);
     b = wave_sum(b);
@@ -65,32 +81,41 @@ __device__ __forceinline__ void block_add2(float& a, float& b, float (&ba)[16], 
     __syncthreads();
     a = b = 0.f;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
+    for (int w = 0; w < THREADS / 64; ++w) {
         a += ba[w];
         b += bb[w];
     }
 }
 
-// What a thread has seen of its part of a row: packs first, first + kThreads, ...
+// What a thread has seen of its part of a row: packs first, first + THREADS, ...
 template <typename T, bool TOP>
 struct Scan {
     static constexpr int P = kPack<T>;
-    float B = -FLT_MAX, s = 0.f, u = 0.f, most = -INFINITY, best = -INFINITY;
-    int32_t best_pack = INT32_MAX;
+    float B = -FLT_MAX, s = 0.f, u = 0.f, most = -INFINITY;
+    int32_t most_pack = INT32_MAX;           // TOP: the first pack with that value
 
-    __device__ __forceinline__ void meet(const float (&v)[P], float k, int32_t pack) {
-        float top = fmaxf(v[0], v[1]);
+    // N packs, the first `count` of which there are; number j is pack + j * step
+    template <int N>
+    __device__ __forceinline__ void meet(const float (&v)[N][P], int count, float k, int32_t pack, int32_t step) {
+        float top = -INFINITY, low = INFINITY;
 #pragma unroll
-        for (int e = 2; e < P; e += 2) top = fmaxf(fmaxf(v[e], v[e + 1]), top);
-        if (TOP) {
-            // (the first pack counts also where it holds nothing above -inf)
-            if (top > best || best_pack == INT32_MAX) {
-                best = ranked(top);
-                best_pack = pack;
+        for (int j = 0; j < N; ++j) {
+            if (j >= count) break;
+            float t = fmaxf(v[j][0], v[j][1]);
+#pragma unroll
+            for (int e = 2; e < P; e += 2) t = fmaxf(fmaxf(v[j][e], v[j][e + 1]), t);
+#pragma unroll
+            for (int e = 0; e < P; e += 2) low = fminf(fminf(v[j][e], v[j][e + 1]), low);
+            if (TOP) {
+                // (the first pack counts also where it holds nothing above -inf)
+                if (t > most || most_pack == INT32_MAX) {
+                    most = t == t ? t : -INFINITY;
+                    most_pack = pack + j * step;
+                }
             }
-        } else {
-            most = fmaxf(most, top);
+            top = fmaxf(top, t);
         }
+        if (!TOP) most = fmaxf(most, top);
         const float b = top * k;
         if (b > B) {
             const float f = exp2_of(B - b);
@@ -98,14 +123,30 @@ struct Scan {
             s *= f;
             B = b;
         }
+        if (low > kPlain) {
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            const float d = fmaf(v[e], k, -B), x = exp2_of(d);
-            s += x;
-            u = fmaf(x, fmaxf(d, kFar), u);
+            for (int j = 0; j < N; ++j) {
+                if (j >= count) break;
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float d = fmaf(v[j][e], k, -B), x = exp2_of(d);
+                    s += x;
+                    u = fmaf(x, d, u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                if (j >= count) break;
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const float d = fmaf(v[j][e], k, -B), x = exp2_of(d);
+                    s += x;
+                    u = fmaf(x, fmaxf(d, kFar), u);
+                }
+            }
         }
     }
-    __device__ __forceinline__ float largest() const { return TOP ? best : most; }
 };
 
 // the last pack of a row, where the row ends inside it
@@ -115,30 +156,45 @@ __device__ __forceinline__ void load_tail(const T* row, int64_t at, int64_t voca
     for (int e = 0; e < kPack<T>; ++e) v[e] = at + e < vocab ? static_cast<float>(row[at + e]) : -INFINITY;
 }
 
-// Packs [first, last) of a row (`last` may be one that the row ends in).
-template <typename T, bool TOP>
-__device__ __forceinline__ Sums scan_part(const T* row, int64_t vocab, int32_t first, int32_t last, float k, TokenShared& sh,
-                                          Scan<T, TOP>& scan) {
-    constexpr int P = kPack<T>;
+// Packs [first, last) of a row (`last` may be one that the row ends in): the thread's own sums.
+template <typename T, bool TOP, int THREADS>
+__device__ __forceinline__ void scan_packs(const T* row, int64_t vocab, int32_t first, int32_t last, float k, Scan<T, TOP>& scan) {
+    constexpr int P = kPack<T>, N = 4;
     const int32_t whole = static_cast<int32_t>(vocab / P);         // packs before one that the row ends in
     const int32_t stop = last < whole ? last : whole;
-    for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < stop; q += kThreads) {
-        float v[P];
-        load_pack<T, P>(row + static_cast<int64_t>(q) * P, v);
-        scan.meet(v, k, q);
+    for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < stop; q += N * THREADS) {
+        const int32_t count = min(N, (stop - q + THREADS - 1) / THREADS);
+        Raw<T, P> raw[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < count) raw[j].load(row + static_cast<int64_t>(q + j * THREADS) * P);
+        float v[N][P];
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[j][e] = raw[j][e];
+        if (count == N) scan.template meet<N>(v, N, k, q, THREADS);
+        else scan.template meet<N>(v, count, k, q, THREADS);
     }
-    if (last > whole && first <= whole && (whole - first) % kThreads == static_cast<int32_t>(threadIdx.x)) {
-        float v[P];
-        load_tail(row, static_cast<int64_t>(whole) * P, vocab, v);
-        scan.meet(v, k, whole);
+    if (last > whole && first <= whole && (whole - first) % THREADS == static_cast<int32_t>(threadIdx.x)) {
+        float v[1][P];
+        load_tail(row, static_cast<int64_t>(whole) * P, vocab, v[0]);
+        scan.template meet<1>(v, 1, k, whole, THREADS);
     }
+}
+
+// the sums of all threads
+template <typename T, bool TOP, int THREADS>
+__device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_t first, int32_t last, float k,
+                                             TokenShared<THREADS>& sh, const Scan<T, TOP>& scan) {
+    constexpr int P = kPack<T>;
     Sums r;
-    r.m = block_max(scan.largest(), sh.f[0]);
-    const float B = block_max(scan.B, sh.f[1]);
+    r.m = block_max<THREADS>(scan.most, sh.f[0]);
+    const float B = block_max<THREADS>(scan.B, sh.f[1]);
     __syncthreads();
     const float f = exp2_of(scan.B - B);
     float s = scan.s * f, u = f * fmaf(scan.s, fmaxf(scan.B - B, kFar), scan.u);
-    block_add2(s, u, sh.f[0], sh.f[2]);
+    block_add2<THREADS>(s, u, sh.f[0], sh.f[2]);
     // from B to the largest value itself
     const float off = fmaf(r.m, k, -B), g = exp2_of(-off);
     r.S = s * g;
@@ -150,12 +206,12 @@ __device__ __forceinline__ Sums scan_part(const T* row, int64_t vocab, int32_t f
         __syncthreads();
         s = u = 0.f;
         const int64_t end = static_cast<int64_t>(last) * P < vocab ? static_cast<int64_t>(last) * P : vocab;
-        for (int64_t i = static_cast<int64_t>(first) * P + threadIdx.x; i < end; i += kThreads) {
+        for (int64_t i = static_cast<int64_t>(first) * P + threadIdx.x; i < end; i += THREADS) {
             const float d = (static_cast<float>(row[i]) - r.m) * k, x = exp2_of(d);
             s += x;
             u = fmaf(x, fmaxf(d, kFar), u);
         }
-        block_add2(s, u, sh.f[0], sh.f[2]);
+        block_add2<THREADS>(s, u, sh.f[0], sh.f[2]);
         r.S = s;
         r.U = u;
     } else if (r.m == -INFINITY && !(s == s)) {      // NaN and -inf alone
@@ -166,48 +222,95 @@ __device__ __forceinline__ Sums scan_part(const T* row, int64_t vocab, int32_t f
     return r;
 }
 
-// The `top` largest of packs [first, last) of a row, in order, by `emit(rank, value, index)`.  Of the threads' largest values
-// the top-th in order (equal ones: lower pack first) is a bound that `top` values reach, so the largest are
-// among those of the `top` threads before it that reach it too: usually hardly more than `top` values, which are
-// then ranked by counting.
-template <typename T, typename Emit>
+// `n` keys ranked by counting; those before `top` go to emit(rank, key)
+template <int THREADS, typename Emit>
+__device__ __forceinline__ void rank_list(const uint64_t* list, int32_t n, int top, Emit emit) {
+    for (int32_t i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t key = list[i];
+        int32_t before = 0, j = 0;
+        for (; j + 8 <= n; j += 8)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) before += list[j + e] > key;
+        for (; j < n; ++j) before += list[j] > key;
+        if (before < top) emit(before, key);
+    }
+}
+
+// The `top` largest of packs [first, last) of a row, in order, by emit(rank, key).  Four neighbouring threads are a unit; of the
+// units' largest values the top-th in order (equal ones: lower pack first) is a bound that `top` values reach, so the
+// largest are among the values of the `top` units before it that reach it too: usually hardly more than `top` values, which
+// those threads list and which are then ranked by counting.  The bound is found bit by bit, in every wavefront by itself, a
+// unit (or four) a lane.
+template <typename T, int THREADS, typename Emit>
 __device__ __forceinline__ void largest_of_part(const T* row, int64_t vocab, int32_t first, int32_t last, int top,
-                                                const Scan<T, true>& scan, TokenShared& sh, Emit emit) {
-    constexpr int P = kPack<T>;
-    const int tid = threadIdx.x;
-    sh.value[tid] = scan.best;
-    sh.pack[tid] = scan.best_pack;
+                                                const Scan<T, true>& scan, TokenShared<THREADS>& sh, Emit emit) {
+    constexpr int P = kPack<T>, LOW = kAlike<T>, PER = THREADS / 256;
+    const int tid = threadIdx.x, lane = tid & 63;
+    // (orders compare as signed numbers once the top bit is turned; packs too)
+    int32_t most = static_cast<int32_t>(order_of(scan.most) ^ 0x80000000u) >> LOW, pack = scan.most_pack;
+#pragma unroll
+    for (int d = 1; d <= 2; d <<= 1) {
+        const int32_t m = __shfl_xor(most, d), q = __shfl_xor(pack, d);
+        if (m > most || (m == most && q < pack)) {
+            most = m;
+            pack = q;
+        }
+    }
+    if ((tid & 3) == 0) {
+        sh.order[tid >> 2] = most;
+        sh.pack[tid >> 2] = pack;
+    }
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    int rank = 0;
-    for (int j = 0; j < kThreads; ++j) {
-        const float v = sh.value[j];
-        const int32_t q = sh.pack[j];
-        // (threads without a pack have none to lose: by their number)
-        rank += v > scan.best || (v == scan.best && (q < scan.best_pack || (q == scan.best_pack && j < tid)));
-    }
-    if (rank < top) sh.chosen[rank] = tid;
-    __syncthreads();
-    const float bound = sh.value[sh.chosen[top - 1]];
-    const int32_t bound_pack = sh.pack[sh.chosen[top - 1]];
-    const int32_t each = (last - first + kThreads - 1) / kThreads;         // packs of a thread
-    // (pack q of candidate number w, and whether it exists)
-    auto pack_of = [&](int32_t w) { return first + sh.chosen[w / each] + (w % each) * kThreads; };
-    for (int32_t w = tid; w < top * each; w += kThreads) {
-        const int32_t q = pack_of(w);
-        if (q >= last) continue;
-        const int64_t at = static_cast<int64_t>(q) * P;
-        float v[P];
-        if (at + P <= vocab) load_pack<T, P>(row + at, v);
-        else load_tail(row, at, vocab, v);
+    int32_t o[PER], q[PER];
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            const float x = ranked(v[e]);
-            if (at + e < vocab && (x > bound || (x == bound && q <= bound_pack))) {
-                const int32_t slot = atomicAdd(&sh.n, 1);
-                if (slot < kList) {
-                    sh.list_value[slot] = x;
-                    sh.list_at[slot] = at + e;
+    for (int k = 0; k < PER; ++k) {
+        o[k] = sh.order[lane + 64 * k];
+        q[k] = sh.pack[lane + 64 * k];
+    }
+    // the largest bound that at least `top` units reach
+    int32_t bound = INT32_MIN >> LOW;
+#pragma unroll
+    for (int bit = 31 - LOW; bit >= 0; --bit) {
+        // (the sign's bit first: from the lowest number up to 0)
+        const int32_t next = bit == 31 - LOW ? 0 : bound + (1 << bit);
+        int reach = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) reach += __popcll(__ballot(o[k] >= next));
+        if (reach >= top) bound = next;
+    }
+    int reach = 0, beyond = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        reach += __popcll(__ballot(o[k] >= bound));
+        beyond += __popcll(__ballot(o[k] > bound));
+    }
+    // of units that are equal to the bound, those with the lowest packs
+    int32_t bound_pack = INT32_MAX;
+    if (reach > top) {
+        bound_pack = 0;
+#pragma unroll 1
+        for (int bit = 30; bit >= 0; --bit) {
+            const int32_t below = bound_pack + (1 << bit);           // are there enough below this pack?
+            int n = beyond;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) n += __popcll(__ballot(o[k] == bound && q[k] < below));
+            if (n < top) bound_pack = below;
+        }
+    }
+    const bool chosen = most > bound || (most == bound && pack <= bound_pack);
+    if (chosen) {
+        for (int32_t at_pack = first + tid; at_pack < last; at_pack += THREADS) {
+            const int64_t at = static_cast<int64_t>(at_pack) * P;
+            float v[P];
+            if (at + P <= vocab) load_pack<T, P>(row + at, v);
+            else load_tail(row, at, vocab, v);
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const int32_t x = static_cast<int32_t>(order_of(v[e]) ^ 0x80000000u) >> LOW;
+                if (at + e < vocab && (x > bound || (x == bound && at_pack <= bound_pack))) {
+                    const int32_t slot = atomicAdd(&sh.n, 1);
+                    if (slot < kList) sh.list[slot] = key_of(v[e], at + e);
                 }
             }
         }
@@ -215,68 +318,41 @@ __device__ __forceinline__ void largest_of_part(const T* row, int64_t vocab, int
     __syncthreads();
     const int32_t n = sh.n;
     if (n <= kList) {
-        for (int32_t i = tid; i < n; i += kThreads) {
-            const float x = sh.list_value[i];
-            const int64_t at = sh.list_at[i];
-            int32_t before = 0;
-            for (int32_t j = 0; j < n; ++j) {
-                const float v = sh.list_value[j];
-                before += v > x || (v == x && sh.list_at[j] < at);
-            }
-            if (before < top) emit(before, x, at);
-        }
-        for (int32_t i = n + tid; i < top; i += kThreads) emit(i, -INFINITY, static_cast<int64_t>(-1));
+        rank_list<THREADS>(sh.list, n, top, emit);
+        for (int32_t i = n + tid; i < top; i += THREADS) emit(i, 0);
         return;
     }
-    // More than the list holds (long runs of equal values): one after the other, each the first behind the one before.
-    float prev = INFINITY;
-    int64_t prev_at = -1;
+    // More than the list holds (long runs of equal values): one after the other, each the largest below the one before.
+    uint64_t prev = ~0ull;
     for (int r = 0; r < top; ++r) {
-        float best = -INFINITY;
-        int64_t best_at = INT64_MAX;
-        for (int32_t w = tid; w < top * each; w += kThreads) {
-            const int32_t q = pack_of(w);
-            if (q >= last) continue;
-            const int64_t at = static_cast<int64_t>(q) * P;
-            for (int e = 0; e < P && at + e < vocab; ++e) {
-                const float x = ranked(static_cast<float>(row[at + e]));
-                if ((x < prev || (x == prev && at + e > prev_at)) && (x > best || (x == best && at + e < best_at))) {
-                    best = x;
-                    best_at = at + e;
+        uint64_t best = 0;
+        if (chosen)
+            for (int32_t at_pack = first + tid; at_pack < last; at_pack += THREADS) {
+                const int64_t at = static_cast<int64_t>(at_pack) * P;
+                for (int e = 0; e < P && at + e < vocab; ++e) {
+                    const uint64_t key = key_of(static_cast<float>(row[at + e]), at + e);
+                    if (key < prev && key > best) best = key;
                 }
             }
-        }
 #pragma unroll
         for (int d = 32; d; d >>= 1) {
-            const float v = __shfl_xor(best, d);
-            const int64_t a = __shfl_xor(best_at, d);
-            if (v > best || (v == best && a < best_at)) {
-                best = v;
-                best_at = a;
-            }
+            const uint64_t other = __shfl_xor(best, d);
+            if (other > best) best = other;
         }
         __syncthreads();
-        if ((tid & 63) == 0) {
-            sh.best_value[tid >> 6] = best;
-            sh.best_at[tid >> 6] = best_at;
-        }
+        if (lane == 0) sh.best[tid >> 6] = best;
         __syncthreads();
-        for (int w = 0; w < kThreads / 64; ++w)
-            if (sh.best_value[w] > best || (sh.best_value[w] == best && sh.best_at[w] < best_at)) {
-                best = sh.best_value[w];
-                best_at = sh.best_at[w];
-            }
+        for (int w = 0; w < THREADS / 64; ++w)
+            if (sh.best[w] > best) best = sh.best[w];
         prev = best;
-        prev_at = best_at;
-        if (tid == 0) emit(r, best, best_at);
+        if (tid == 0) emit(r, best);
     }
 }
 
-// Where a part of a row leaves what it found: parts x 3 sums, then parts x top values, then as many indices (-1: none)
+// Where a part of a row leaves what it found: parts x top keys (0: none), then parts x 3 sums
 struct Parts {
+    uint64_t* key;
     Sums* sums;
-    float* value;
-    int64_t* at;
 };
 struct TokenOut {
     float *logp, *entropy, *lse;
@@ -290,46 +366,55 @@ __device__ __forceinline__ float logp_of(float x, const Sums& r, float log_sum, 
     return r.m == -INFINITY && r.S == r.S ? -INFINITY : fmaf(x - r.m, scale, -log_sum);
 }
 
+// the logit of a row's target; counts: there is one
 template <typename T>
-__device__ __forceinline__ void row_results(const T* logits, int64_t vocab, int64_t row, const int64_t* target, float scale,
-                                            const Sums& r, float log_sum, const TokenOut& out) {
+struct Target {
+    float x = 0.f;
+    bool counts = false;
+    __device__ __forceinline__ void load(const T* row, int64_t vocab, int64_t t) {
+        counts = t >= 0 && t < vocab;
+        if (counts) x = static_cast<float>(row[t]);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void row_results(int64_t row, const Target<T>& target, float scale, const Sums& r, float log_sum,
+                                            const TokenOut& out) {
     const bool empty = r.m == -INFINITY && r.S == r.S;
     if (out.lse) out.lse[row] = empty ? -INFINITY : fmaf(r.m, scale, log_sum);
-    if (out.entropy) out.entropy[row] = empty ? 0.f : log_sum - kLn2 * (r.U / r.S);
-    if (out.logp) {
-        const int64_t t = target[row];
-        const bool counts = t >= 0 && t < vocab;
-        out.logp[row] = counts ? logp_of(static_cast<float>(logits[t]), r, log_sum, scale) : 0.f;
-    }
+    if (out.entropy) out.entropy[row] = empty ? 0.f : log_sum - 0.69314718055994531f * (r.U / r.S);
+    if (out.logp) out.logp[row] = target.counts ? logp_of(target.x, r, log_sum, scale) : 0.f;
 }
 
-template <typename T, bool TOP>
-__global__ void __launch_bounds__(kThreads)
+template <typename T, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 k_token(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out, int top, int parts,
         int32_t packs, Parts ws) {
-    __shared__ TokenShared sh;
+    __shared__ TokenShared<THREADS> sh;
     const int64_t row = blockIdx.x / static_cast<unsigned>(parts);
     const int part = blockIdx.x % static_cast<unsigned>(parts);
     const T* x = logits + row * stride;
     const int32_t each = (packs + parts - 1) / parts;
     const int32_t first = min(part * each, packs), last = min(first + each, packs);
     const float k = scale * kLog2e;
+    const bool results = parts == 1 && threadIdx.x == 0;
+    const int64_t t = results && out.logp ? target[row] : -1;
     Scan<T, TOP> scan;
-    const Sums r = scan_part<T, TOP>(x, vocab, first, last, k, sh, scan);
+    scan_packs<T, TOP, THREADS>(x, vocab, first, last, k, scan);
+    Target<T> hit;
+    hit.load(x, vocab, t);
+    const Sums r = join_threads<T, TOP, THREADS>(x, vocab, first, last, k, sh, scan);
     const float log_sum = logf(r.S);
     const int64_t at = row * parts + part;
-    if (threadIdx.x == 0) {
-        if (parts > 1) ws.sums[at] = r;
-        else row_results(x, vocab, row, target, scale, r, log_sum, out);
-    }
+    if (results) row_results(row, hit, scale, r, log_sum, out);
+    else if (threadIdx.x == 0) ws.sums[at] = r;
     if constexpr (TOP) {
-        largest_of_part<T>(x, vocab, first, last, top, scan, sh, [&](int rank, float v, int64_t i) {
+        largest_of_part<T, THREADS>(x, vocab, first, last, top, scan, sh, [&](int rank, uint64_t key) {
             if (parts > 1) {
-                ws.value[at * top + rank] = v;
-                ws.at[at * top + rank] = i;
+                ws.key[at * top + rank] = key;
             } else {
-                out.top_idx[row * top + rank] = i;
-                out.top_logp[row * top + rank] = logp_of(v, r, log_sum, scale);
+                out.top_idx[row * top + rank] = index_of(key);
+                out.top_logp[row * top + rank] = logp_of(value_of(static_cast<uint32_t>(key >> 32)), r, log_sum, scale);
             }
         });
     }
@@ -340,49 +425,50 @@ template <typename T, bool TOP>
 __global__ void __launch_bounds__(kThreads)
 k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out, int top,
              int parts, Parts ws) {
-    __shared__ float value[kMaxParts * kMaxTop];
-    __shared__ int64_t index[kMaxParts * kMaxTop];
+    __shared__ uint64_t list[TOP ? kMaxParts * kMaxTop : 1];
     __shared__ int32_t n;
     const int64_t row = blockIdx.x;
     const float k = scale * kLog2e;
     const int lane = threadIdx.x & 63;
     // every wavefront joins the sums for itself: a part a lane
     Sums p = {-INFINITY, 0.f, 0.f};
-    if (lane < parts) p = ws.sums[row * parts + lane];
+    uint64_t bound = 0, key = 0;
+    const int keys = parts * top;
+    const int64_t t = out.logp ? target[row] : -1;
+    if (lane < parts) {
+        p = ws.sums[row * parts + lane];
+        // `top` values reach the last one of any part's list
+        if (TOP) bound = ws.key[(row * parts + lane) * top + top - 1];
+    }
+    if (TOP && static_cast<int>(threadIdx.x) < keys) key = ws.key[row * keys + threadIdx.x];
+    Target<T> hit;
+    hit.load(logits + row * stride, vocab, t);
     Sums r;
     r.m = wave_max(p.m);
     const float d = p.m == r.m ? 0.f : (p.m - r.m) * k, f = exp2_of(d);
     r.S = wave_sum(p.S * f);
     r.U = wave_sum(f * fmaf(p.S, fmaxf(d, kFar), p.U));
     const float log_sum = logf(r.S);
-    if (threadIdx.x == 0) row_results(logits + row * stride, vocab, row, target, scale, r, log_sum, out);
-    if (TOP) {
-        if (threadIdx.x == 0) n = 0;
-        // `top` values reach the last one of any part's list
-        float bound = -INFINITY;
-        if (lane < parts) bound = ws.value[(row * parts + lane) * top + top - 1];
-        bound = wave_max(bound);
-        __syncthreads();
-        for (int i = threadIdx.x; i < parts * top; i += kThreads) {
-            const float v = ws.value[row * parts * top + i];
-            const int64_t at = ws.at[row * parts * top + i];
-            if (at >= 0 && v >= bound) {
-                const int32_t slot = atomicAdd(&n, 1);
-                value[slot] = v;
-                index[slot] = at;
-            }
+    if (threadIdx.x == 0) {
+        row_results(row, hit, scale, r, log_sum, out);
+        n = 0;
+    }
+    if constexpr (TOP) {
+#pragma unroll
+        for (int s = 32; s; s >>= 1) {
+            const uint64_t other = __shfl_xor(bound, s);
+            if (other > bound) bound = other;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const float v = value[i];
-            const int64_t at = index[i];
-            int before = 0;
-            for (int j = 0; j < n; ++j) before += value[j] > v || (value[j] == v && index[j] < at);
-            if (before < top) {
-                out.top_idx[row * top + before] = at;
-                out.top_logp[row * top + before] = logp_of(v, r, log_sum, scale);
-            }
+        for (int i = threadIdx.x; i < keys; i += kThreads) {
+            if (i >= kThreads) key = ws.key[row * keys + i];
+            if (key && key >= bound) list[atomicAdd(&n, 1)] = key;
         }
+        __syncthreads();
+        rank_list<kThreads>(list, n, top, [&](int rank, uint64_t best) {
+            out.top_idx[row * top + rank] = index_of(best);
+            out.top_logp[row * top + rank] = logp_of(value_of(static_cast<uint32_t>(best >> 32)), r, log_sum, scale);
+        });
     }
 }
 
@@ -440,17 +526,21 @@ template <typename T, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out,
              const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs) {
-    __shared__ TokenShared sh;
+    __shared__ TokenShared<kThreads> sh;
     const int64_t row = blockIdx.x;
     const T* x = logits + row * stride;
+    const int64_t t = target[row];
     Scan<T, false> scan;
-    const Sums r = scan_part<T, false>(x, vocab, 0, packs, scale * kLog2e, sh, scan);
+    scan_packs<T, false, kThreads>(x, vocab, 0, packs, scale * kLog2e, scan);
+    Target<T> hit;
+    hit.load(x, vocab, t);
+    const Sums r = join_threads<T, false, kThreads>(x, vocab, 0, packs, scale * kLog2e, sh, scan);
     const float log_sum = logf(r.S);
     const bool empty = r.m == -INFINITY && r.S == r.S;
-    if (threadIdx.x == 0) row_results(x, vocab, row, target, scale, r, log_sum, out);
+    if (threadIdx.x == 0) row_results(row, hit, scale, r, log_sum, out);
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
     const RowGrad g(row, vocab, scale, target, empty ? -INFINITY : fmaf(r.m, scale, log_sum),
-                    empty ? 0.f : log_sum - kLn2 * (r.U / r.S), g_logp, g_entropy);
+                    empty ? 0.f : log_sum - 0.69314718055994531f * (r.U / r.S), g_logp, g_entropy);
     grad_packs<PAST>(x, dlogits + row * d_stride, vocab, 0, packs, g);
 }
 
@@ -466,23 +556,25 @@ int32_t packs_of(int64_t vocab, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt);
     return static_cast<int32_t>((vocab + p - 1) / p);
 }
-// workgroups that share a row: so many that 512 are under way, none with less than 4096 values
+// Workgroups of kThreads take a row each where there are enough rows; few rows have workgroups of kFewThreads, and share
+// those of long rows
+bool few_rows(int64_t rows) { return rows < 512; }
 int parts_of(int64_t rows, int64_t vocab) {
-    int64_t parts = rows >= 512 ? 1 : 512 / (rows ? rows : 1);
-    if (parts > vocab / 4096) parts = vocab / 4096;
+    if (!few_rows(rows)) return 1;
+    int64_t parts = 512 / (rows ? rows : 1);
+    if (parts > vocab / 32768) parts = vocab / 32768;
     if (parts > kMaxParts) parts = kMaxParts;
     return static_cast<int>(parts < 1 ? 1 : parts);
 }
 size_t token_bytes(int64_t rows, int64_t vocab, int top) {
     const int64_t parts = parts_of(rows, vocab);
     if (parts == 1) return 0;
-    return static_cast<size_t>(rows * parts) * (16 + static_cast<size_t>(top) * 12);
+    return static_cast<size_t>(rows * parts) * (sizeof(Sums) + static_cast<size_t>(top) * 8);
 }
 Parts parts_in(void* ws, int64_t rows, int parts, int top) {
     Parts p;
-    p.at = static_cast<int64_t*>(ws);
-    p.value = reinterpret_cast<float*>(p.at + rows * parts * top);
-    p.sums = reinterpret_cast<Sums*>(p.value + rows * parts * top);
+    p.key = static_cast<uint64_t*>(ws);
+    p.sums = reinterpret_cast<Sums*>(p.key + rows * parts * top);
     return p;
 }
 
@@ -506,7 +598,9 @@ int token_forward(const TokenArgs& a) {
     const int parts = parts_of(a.rows, a.vocab);
     const Parts ws = parts > 1 ? parts_in(a.ws, a.rows, parts, a.top) : Parts{};
     const T* x = static_cast<const T*>(a.logits);
-    k_token<T, TOP><<<static_cast<unsigned>(a.rows * parts), kThreads, 0, a.stream>>>(
+    const bool few = few_rows(a.rows);
+    const auto kernel = few ? k_token<T, TOP, kFewThreads> : k_token<T, TOP, kThreads>;
+    kernel<<<static_cast<unsigned>(a.rows * parts), few ? kFewThreads : kThreads, 0, a.stream>>>(
         x, a.vocab, a.stride, a.scale, a.target, a.out, a.top, parts, packs_of(a.vocab, a.fmt), ws);
     if (int rc = launched()) return rc;
     if (parts == 1) return CS_OK;
@@ -528,7 +622,7 @@ int token_grad(const TokenArgs& a) {
 }
 template <typename T>
 int token_loss(TokenArgs a) {
-    if (parts_of(a.rows, a.vocab) > 1) {              // few rows
+    if (few_rows(a.rows)) {
         if (int rc = token_forward<T, false>(a)) return rc;
         a.lse = a.out.lse, a.entropy = a.out.entropy;
         return token_grad<T>(a);
