@@ -159,7 +159,7 @@ __device__ __forceinline__ void load_tail(const T* row, int64_t at, int64_t voca
 // Packs [first, last) of a row (`last` may be one that the row ends in): the thread's own sums.
 template <typename T, bool TOP, int THREADS>
 __device__ __forceinline__ void scan_packs(const T* row, int64_t vocab, int32_t first, int32_t last, float k, Scan<T, TOP>& scan) {
-    constexpr int P = kPack<T>, N = 4;
+    constexpr int P = kPack<T>, N = THREADS == kFewThreads || sizeof(T) == 4 ? 4 : 1;
     const int32_t whole = static_cast<int32_t>(vocab / P);         // packs before one that the row ends in
     const int32_t stop = last < whole ? last : whole;
     for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < stop; q += N * THREADS) {
@@ -472,40 +472,52 @@ k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     }
 }
 
-// Gradient of a value: constants of its row.  ln p = x scale - lse.
+// Gradient of a row's values: p (a + b max(l, far)), with what scale, g, h, entropy and the target make of a and b.
+//   from a log of p: l = x mul - add = ln p, p = 2^(l log2(e)):           a = -scale (g + h H),               b = -scale h
+//   from the sums:   l = x mul - add = log2 p + log2 s, p = 2^l / s:      a = -scale (g + h (H - ln s)) / s,  b = -scale h ln2 / s
+// (a value with no probability has p = 0, l = -inf and the gradient 0).  The target's value has hot = scale g more.
 struct RowGrad {
-    float scale, lse, H, g, h;       // g = 0 where the row has no target
-    int64_t target;
-    bool empty;
-    __device__ __forceinline__ RowGrad(int64_t row, int64_t vocab, float scale_, const int64_t* target_, float lse_, float H_,
-                                       const float* g_logp, const float* g_entropy)
-        : scale(scale_), lse(lse_), H(H_), g(0.f), h(g_entropy ? g_entropy[row] : 0.f), target(target_ ? target_[row] : -1),
-          empty(lse_ == -INFINITY) {
-        if (target < 0 || target >= vocab) target = -1;
-        else if (g_logp) g = g_logp[row];
+    float mul, add, a, b, hot;
+    int64_t target;                  // -1: none
+    bool empty;                      // the row has no probabilities: gradient 0
+
+    __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const float* g_logp,
+                                                  const float* g_entropy) {
+        target = t >= 0 && t < vocab ? t : -1;
+        const float g = target >= 0 && g_logp ? g_logp[row] : 0.f;
+        hot = scale * g;
+        a = -hot;
+        b = g_entropy ? -scale * g_entropy[row] : 0.f;
     }
-    __device__ __forceinline__ float of(float x, bool is_target) const {
-        const float l = fmaf(x, scale, -lse), p = exp2_of(l * kLog2e);
-        // p (ln p + H) of a value with no probability is 0
-        float d = -p * fmaf(h, fmaxf(l, kFar) + H, g);
-        if (is_target) d += g;
-        return empty ? 0.f : d * scale;
+    // LOGS: l is ln p; ENTROPY: b is not 0
+    template <bool LOGS, bool ENTROPY>
+    __device__ __forceinline__ float of(float x) const {
+        const float l = fmaf(x, mul, -add), p = exp2_of(LOGS ? l * kLog2e : l);
+        return ENTROPY ? p * fmaf(fmaxf(l, kFar), b, a) : p * a;
     }
 };
 
-template <bool PAST, typename T>
-__device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int64_t first, int64_t last, const RowGrad& row) {
+// packs [first, last) of a row
+template <bool PAST, bool LOGS, bool ENTROPY, int THREADS, typename T>
+__device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int32_t first, int32_t last, const RowGrad& row) {
     constexpr int P = kPack<T>;
-    for (int64_t q = first + threadIdx.x; q < last; q += kThreads) {
-        const int64_t at = q * P;
+    const int32_t hot = row.target >= 0 ? static_cast<int32_t>(row.target / P) : -1;
+    for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < last; q += THREADS) {
+        const int64_t at = static_cast<int64_t>(q) * P;
         float v[P];
-        if (at + P <= vocab) {
-            load_pack<T, P>(x + at, v);
+        if (at + P <= vocab) load_pack<T, P>(x + at, v);
+        else load_tail(x, at, vocab, v);
 #pragma unroll
-            for (int e = 0; e < P; ++e) v[e] = row.of(v[e], at + e == row.target);
+        for (int e = 0; e < P; ++e) v[e] = row.empty ? 0.f : row.template of<LOGS, ENTROPY>(v[e]);
+        if (q == hot && !row.empty)
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[e] += at + e == row.target ? row.hot : 0.f;
+        if (at + P <= vocab) {
             store_pack<PAST>(dx + at, v);
         } else {
-            for (int64_t i = at; i < vocab; ++i) dx[i] = static_cast<T>(row.of(static_cast<float>(x[i]), i == row.target));
+#pragma unroll
+            for (int e = 0; e < P; ++e)
+                if (at + e < vocab) dx[at + e] = static_cast<T>(v[e]);
         }
     }
 }
@@ -514,11 +526,21 @@ template <typename T, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, const float* lse,
              const float* entropy, const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int pieces,
-             int64_t packs) {
+             int32_t packs) {
     const int64_t row = blockIdx.x / static_cast<unsigned>(pieces);
-    const int64_t each = (packs + pieces - 1) / pieces, first = each * (blockIdx.x % static_cast<unsigned>(pieces));
-    const RowGrad r(row, vocab, scale, target, lse[row], entropy ? entropy[row] : 0.f, g_logp, g_entropy);
-    grad_packs<PAST>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
+    const int32_t each = (packs + pieces - 1) / pieces;
+    const int32_t first = min(each * static_cast<int32_t>(blockIdx.x % static_cast<unsigned>(pieces)), packs);
+    RowGrad r;
+    r.coefficients(row, vocab, scale, target ? target[row] : -1, g_logp, g_entropy);
+    r.mul = scale;
+    r.add = lse[row];
+    r.empty = r.add == -INFINITY;
+    if (g_entropy) {
+        r.a = fmaf(r.b, entropy[row], r.a);
+        grad_packs<PAST, true, true, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
+    } else {
+        grad_packs<PAST, true, false, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
+    }
 }
 
 // forward and gradient of a row in one workgroup: the row's second read comes from the caches
@@ -529,19 +551,36 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     __shared__ TokenShared<kThreads> sh;
     const int64_t row = blockIdx.x;
     const T* x = logits + row * stride;
+    T* dx = dlogits + row * d_stride;
     const int64_t t = target[row];
+    const float k = scale * kLog2e;
     Scan<T, false> scan;
-    scan_packs<T, false, kThreads>(x, vocab, 0, packs, scale * kLog2e, scan);
+    scan_packs<T, false, kThreads>(x, vocab, 0, packs, k, scan);
     Target<T> hit;
     hit.load(x, vocab, t);
-    const Sums r = join_threads<T, false, kThreads>(x, vocab, 0, packs, scale * kLog2e, sh, scan);
+    const Sums r = join_threads<T, false, kThreads>(x, vocab, 0, packs, k, sh, scan);
     const float log_sum = logf(r.S);
-    const bool empty = r.m == -INFINITY && r.S == r.S;
     if (threadIdx.x == 0) row_results(row, hit, scale, r, log_sum, out);
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
-    const RowGrad g(row, vocab, scale, target, empty ? -INFINITY : fmaf(r.m, scale, log_sum),
-                    empty ? 0.f : log_sum - 0.69314718055994531f * (r.U / r.S), g_logp, g_entropy);
-    grad_packs<PAST>(x, dlogits + row * d_stride, vocab, 0, packs, g);
+    RowGrad g;
+    g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
+    g.empty = r.m == -INFINITY && r.S == r.S;
+    const float H = log_sum - 0.69314718055994531f * (r.U / r.S);
+    // relative to a binary32 number next to m k: s is S but for what that is off
+    g.mul = k;
+    g.add = r.m * k;
+    const float off = fmaf(r.m, k, -g.add), s = r.S * exp2_of(off), one = 1.f / s;
+    if (fabsf(g.add) < INFINITY) {
+        g.a = one * fmaf(g.b, H - logf(s), g.a);
+        g.b *= one * 0.69314718055994531f;
+        if (g_entropy) grad_packs<PAST, false, true, kThreads>(x, dx, vocab, 0, packs, g);
+        else grad_packs<PAST, false, false, kThreads>(x, dx, vocab, 0, packs, g);
+    } else {                                          // (a largest value beyond 2e38, or none)
+        g.mul = scale;
+        g.add = fmaf(r.m, scale, log_sum);
+        g.a = fmaf(g.b, H, g.a);
+        grad_packs<PAST, true, true, kThreads>(x, dx, vocab, 0, packs, g);
+    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -610,7 +649,7 @@ int token_forward(const TokenArgs& a) {
 }
 template <typename T>
 int token_grad(const TokenArgs& a) {
-    const int64_t packs = packs_of(a.vocab, a.fmt);
+    const int32_t packs = packs_of(a.vocab, a.fmt);
     const int64_t most = ((static_cast<int64_t>(1) << 31) - 1) / a.rows;
     int64_t pieces = (packs + 4 * kThreads - 1) / (4 * kThreads);
     if (pieces > most) pieces = most;
