@@ -59,10 +59,19 @@ __device__ __forceinline__ float wave_sum(float v) {
     v += dpp<0x143, 0xc>(v);     // into rows 2 and 3
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp_or_self(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+// (fmaxf: a NaN only where there is nothing else)
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    return v;
+    v = fmaxf(v, dpp_or_self<0xB1, 0xf>(v));
+    v = fmaxf(v, dpp_or_self<0x4E, 0xf>(v));
+    v = fmaxf(v, dpp_or_self<0x141, 0xf>(v));
+    v = fmaxf(v, dpp_or_self<0x140, 0xf>(v));
+    v = fmaxf(v, dpp_or_self<0x142, 0xa>(v));
+    v = fmaxf(v, dpp_or_self<0x143, 0xc>(v));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
 // Sums over groups of THREADS threads of a workgroup, the same in every thread of a group; `turn` counts the calls of a kernel

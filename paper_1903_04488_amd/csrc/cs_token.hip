@@ -21,7 +21,7 @@ constexpr int kFewThreads = 1024;            // of a row among few, or of its pa
 constexpr int kMaxTop = CS_TOKEN_MAX_TOP;
 constexpr int kList = 1024;                  // candidates for the alternatives of a part
 constexpr int kMaxParts = 64;                // workgroups that share a row
-constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 constexpr float kFar = -200.f;               // 2^kFar is 0 beside any sum
 constexpr float kPlain = -1e30f;             // values above this leave no product in the infinite
 
@@ -50,18 +50,33 @@ __device__ __forceinline__ int64_t index_of(uint64_t key) { return 0xffffffffu -
 template <typename T>
 constexpr int kAlike = sizeof(T) == 4 ? 0 : sizeof(T) == 2 && static_cast<float>(static_cast<T>(65536.f)) == 65536.f ? 16 : 13;
 
+// THREADS threads hold or share a row; 64: a wavefront, which needs no barrier
 template <int THREADS>
 struct TokenShared {
+    static constexpr int UNIT = THREADS == 64 ? 1 : 4, LIST = THREADS == 64 ? 256 : kList;
     float f[3][16];
-    int32_t order[THREADS / 4], pack[THREADS / 4];
-    uint64_t list[kList];
+    int32_t order[THREADS / UNIT], pack[THREADS / UNIT];
+    uint64_t list[LIST];
     int32_t n;
     uint64_t best[16];
 };
+template <int THREADS>
+__device__ __forceinline__ int thread_of_row() { return threadIdx.x % THREADS; }
+template <int THREADS>
+__device__ __forceinline__ void row_sync() {
+    if (THREADS == 64) {
+        // (a wavefront's accesses to LDS are served in order)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
 
 template <int THREADS>
 __device__ __forceinline__ float block_max(float v, float (&buf)[16]) {
     v = wave_max(v);
+    if (THREADS == 64) return v;
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
     __syncthreads();
     v = buf[0];
@@ -74,6 +89,7 @@ template <int THREADS>
 __device__ __forceinline__ void block_add2(float& a, float& b, float (&ba)[16], float (&bb)[16]) {
     a = wave_sum(a);
     b = wave_sum(b);
+    if (THREADS == 64) return;
     if ((threadIdx.x & 63) == 0) {
         ba[threadIdx.x >> 6] = a;
         bb[threadIdx.x >> 6] = b;
@@ -191,7 +207,7 @@ __device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_
     Sums r;
     r.m = block_max<THREADS>(scan.most, sh.f[0]);
     const float B = block_max<THREADS>(scan.B, sh.f[1]);
-    __syncthreads();
+    row_sync<THREADS>();
     const float f = exp2_of(scan.B - B);
     float s = scan.s * f, u = f * fmaf(scan.s, fmaxf(scan.B - B, kFar), scan.u);
     block_add2<THREADS>(s, u, sh.f[0], sh.f[2]);
@@ -203,10 +219,10 @@ __device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_
     // else) and where the row holds a NaN or +inf, once more with differences of the values themselves.  (The largest
     // value adds 1 to S.)
     if (!(r.S >= 0.5f && r.S < INFINITY) && r.m > -INFINITY) {
-        __syncthreads();
+        row_sync<THREADS>();
         s = u = 0.f;
         const int64_t end = static_cast<int64_t>(last) * P < vocab ? static_cast<int64_t>(last) * P : vocab;
-        for (int64_t i = static_cast<int64_t>(first) * P + threadIdx.x; i < end; i += THREADS) {
+        for (int64_t i = static_cast<int64_t>(first) * P + thread_of_row<THREADS>(); i < end; i += THREADS) {
             const float d = (static_cast<float>(row[i]) - r.m) * k, x = exp2_of(d);
             s += x;
             u = fmaf(x, fmaxf(d, kFar), u);
@@ -225,7 +241,7 @@ __device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_
 // `n` keys ranked by counting; those before `top` go to emit(rank, key)
 template <int THREADS, typename Emit>
 __device__ __forceinline__ void rank_list(const uint64_t* list, int32_t n, int top, Emit emit) {
-    for (int32_t i = threadIdx.x; i < n; i += THREADS) {
+    for (int32_t i = thread_of_row<THREADS>(); i < n; i += THREADS) {
         const uint64_t key = list[i];
         int32_t before = 0, j = 0;
         for (; j + 8 <= n; j += 8)
@@ -236,32 +252,34 @@ __device__ __forceinline__ void rank_list(const uint64_t* list, int32_t n, int t
     }
 }
 
-// The `top` largest of packs [first, last) of a row, in order, by emit(rank, key).  Four neighbouring threads are a unit; of the
+// The `top` largest of packs [first, last) of a row, in order, by emit(rank, key).  A thread (of a wavefront that has the row
+// to itself) or four neighbouring ones are a unit; of the
 // units' largest values the top-th in order (equal ones: lower pack first) is a bound that `top` values reach, so the
 // largest are among the values of the `top` units before it that reach it too: usually hardly more than `top` values, which
 // those threads list and which are then ranked by counting.  The bound is found bit by bit, in every wavefront by itself, a
 // unit (or four) a lane.
-template <typename T, int THREADS, typename Emit>
-__device__ __forceinline__ void largest_of_part(const T* row, int64_t vocab, int32_t first, int32_t last, int top,
-                                                const Scan<T, true>& scan, TokenShared<THREADS>& sh, Emit emit) {
-    constexpr int P = kPack<T>, LOW = kAlike<T>, PER = THREADS / 256;
-    const int tid = threadIdx.x, lane = tid & 63;
+template <typename T, int THREADS, typename PackAt, typename Emit>
+__device__ __forceinline__ void largest_of_part(int64_t vocab, int32_t first, int32_t last, int top,
+                                                const Scan<T, true>& scan, TokenShared<THREADS>& sh, PackAt pack_at, Emit emit) {
+    constexpr int P = kPack<T>, LOW = kAlike<T>, UNIT = TokenShared<THREADS>::UNIT, PER = THREADS / UNIT / 64;
+    constexpr int32_t LIST = TokenShared<THREADS>::LIST;
+    const int tid = thread_of_row<THREADS>(), lane = tid & 63;
     // (orders compare as signed numbers once the top bit is turned; packs too)
     int32_t most = static_cast<int32_t>(order_of(scan.most) ^ 0x80000000u) >> LOW, pack = scan.most_pack;
 #pragma unroll
-    for (int d = 1; d <= 2; d <<= 1) {
+    for (int d = 1; d < UNIT; d <<= 1) {
         const int32_t m = __shfl_xor(most, d), q = __shfl_xor(pack, d);
         if (m > most || (m == most && q < pack)) {
             most = m;
             pack = q;
         }
     }
-    if ((tid & 3) == 0) {
-        sh.order[tid >> 2] = most;
-        sh.pack[tid >> 2] = pack;
+    if (tid % UNIT == 0) {
+        sh.order[tid / UNIT] = most;
+        sh.pack[tid / UNIT] = pack;
     }
     if (tid == 0) sh.n = 0;
-    __syncthreads();
+    row_sync<THREADS>();
     int32_t o[PER], q[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
@@ -303,21 +321,20 @@ __device__ __forceinline__ void largest_of_part(const T* row, int64_t vocab, int
         for (int32_t at_pack = first + tid; at_pack < last; at_pack += THREADS) {
             const int64_t at = static_cast<int64_t>(at_pack) * P;
             float v[P];
-            if (at + P <= vocab) load_pack<T, P>(row + at, v);
-            else load_tail(row, at, vocab, v);
+            pack_at(at_pack, v);
 #pragma unroll
             for (int e = 0; e < P; ++e) {
                 const int32_t x = static_cast<int32_t>(order_of(v[e]) ^ 0x80000000u) >> LOW;
                 if (at + e < vocab && (x > bound || (x == bound && at_pack <= bound_pack))) {
                     const int32_t slot = atomicAdd(&sh.n, 1);
-                    if (slot < kList) sh.list[slot] = key_of(v[e], at + e);
+                    if (slot < LIST) sh.list[slot] = key_of(v[e], at + e);
                 }
             }
         }
     }
-    __syncthreads();
+    row_sync<THREADS>();
     const int32_t n = sh.n;
-    if (n <= kList) {
+    if (n <= LIST) {
         rank_list<THREADS>(sh.list, n, top, emit);
         for (int32_t i = n + tid; i < top; i += THREADS) emit(i, 0);
         return;
@@ -329,8 +346,11 @@ __device__ __forceinline__ void largest_of_part(const T* row, int64_t vocab, int
         if (chosen)
             for (int32_t at_pack = first + tid; at_pack < last; at_pack += THREADS) {
                 const int64_t at = static_cast<int64_t>(at_pack) * P;
-                for (int e = 0; e < P && at + e < vocab; ++e) {
-                    const uint64_t key = key_of(static_cast<float>(row[at + e]), at + e);
+                float v[P];
+                pack_at(at_pack, v);
+#pragma unroll
+                for (int e = 0; e < P; ++e) {
+                    const uint64_t key = at + e < vocab ? key_of(v[e], at + e) : 0;
                     if (key < prev && key > best) best = key;
                 }
             }
@@ -339,11 +359,13 @@ __device__ __forceinline__ void largest_of_part(const T* row, int64_t vocab, int
             const uint64_t other = __shfl_xor(best, d);
             if (other > best) best = other;
         }
-        __syncthreads();
-        if (lane == 0) sh.best[tid >> 6] = best;
-        __syncthreads();
-        for (int w = 0; w < THREADS / 64; ++w)
-            if (sh.best[w] > best) best = sh.best[w];
+        if (THREADS > 64) {
+            __syncthreads();
+            if (lane == 0) sh.best[tid >> 6] = best;
+            __syncthreads();
+            for (int w = 0; w < THREADS / 64; ++w)
+                if (sh.best[w] > best) best = sh.best[w];
+        }
         prev = best;
         if (tid == 0) emit(r, best);
     }
@@ -382,7 +404,7 @@ __device__ __forceinline__ void row_results(int64_t row, const Target<T>& target
                                             const TokenOut& out) {
     const bool empty = r.m == -INFINITY && r.S == r.S;
     if (out.lse) out.lse[row] = empty ? -INFINITY : fmaf(r.m, scale, log_sum);
-    if (out.entropy) out.entropy[row] = empty ? 0.f : log_sum - 0.69314718055994531f * (r.U / r.S);
+    if (out.entropy) out.entropy[row] = empty ? 0.f : log_sum - kLn2 * (r.U / r.S);
     if (out.logp) out.logp[row] = target.counts ? logp_of(target.x, r, log_sum, scale) : 0.f;
 }
 
@@ -409,7 +431,11 @@ k_token(const T* logits, int64_t vocab, int64_t stride, float scale, const int64
     if (results) row_results(row, hit, scale, r, log_sum, out);
     else if (threadIdx.x == 0) ws.sums[at] = r;
     if constexpr (TOP) {
-        largest_of_part<T, THREADS>(x, vocab, first, last, top, scan, sh, [&](int rank, uint64_t key) {
+        const auto pack_at = [&](int32_t q, float(&v)[kPack<T>]) {
+            if ((static_cast<int64_t>(q) + 1) * kPack<T> <= vocab) load_pack<T, kPack<T>>(x + static_cast<int64_t>(q) * kPack<T>, v);
+            else load_tail(x, static_cast<int64_t>(q) * kPack<T>, vocab, v);
+        };
+        largest_of_part<T, THREADS>(vocab, first, last, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
             if (parts > 1) {
                 ws.key[at * top + rank] = key;
             } else {
@@ -478,12 +504,12 @@ k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const 
 // (a value with no probability has p = 0, l = -inf and the gradient 0).  The target's value has hot = scale g more.
 struct RowGrad {
     float mul, add, a, b, hot;
-    int64_t target;                  // -1: none
+    int32_t target;                  // -1: none
     bool empty;                      // the row has no probabilities: gradient 0
 
     __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const float* g_logp,
                                                   const float* g_entropy) {
-        target = t >= 0 && t < vocab ? t : -1;
+        target = t >= 0 && t < vocab ? static_cast<int32_t>(t) : -1;
         const float g = target >= 0 && g_logp ? g_logp[row] : 0.f;
         hot = scale * g;
         a = -hot;
@@ -497,28 +523,38 @@ struct RowGrad {
     }
 };
 
+// pack q of a row with the values v
+template <bool PAST, bool LOGS, bool ENTROPY, typename T, int P>
+__device__ __forceinline__ void grad_pack(float (&v)[P], T* dx, int32_t vocab, int32_t q, const RowGrad& row) {
+    const int32_t at = q * P;
+#pragma unroll
+    for (int e = 0; e < P; ++e) v[e] = row.template of<LOGS, ENTROPY>(v[e]);
+    // (none: -1 lies in no pack)
+    if (static_cast<uint32_t>(row.target - at) < static_cast<uint32_t>(P))
+#pragma unroll
+        for (int e = 0; e < P; ++e) v[e] += at + e == row.target ? row.hot : 0.f;
+    if (row.empty)
+#pragma unroll
+        for (int e = 0; e < P; ++e) v[e] = 0.f;
+    if (at + P <= vocab) {
+        store_pack<PAST>(dx + at, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+            if (at + e < vocab) dx[at + e] = static_cast<T>(v[e]);
+    }
+}
+
 // packs [first, last) of a row
 template <bool PAST, bool LOGS, bool ENTROPY, int THREADS, typename T>
 __device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int32_t first, int32_t last, const RowGrad& row) {
     constexpr int P = kPack<T>;
-    const int32_t hot = row.target >= 0 ? static_cast<int32_t>(row.target / P) : -1;
     for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < last; q += THREADS) {
-        const int64_t at = static_cast<int64_t>(q) * P;
+        const int32_t at = q * P;
         float v[P];
         if (at + P <= vocab) load_pack<T, P>(x + at, v);
         else load_tail(x, at, vocab, v);
-#pragma unroll
-        for (int e = 0; e < P; ++e) v[e] = row.empty ? 0.f : row.template of<LOGS, ENTROPY>(v[e]);
-        if (q == hot && !row.empty)
-#pragma unroll
-            for (int e = 0; e < P; ++e) v[e] += at + e == row.target ? row.hot : 0.f;
-        if (at + P <= vocab) {
-            store_pack<PAST>(dx + at, v);
-        } else {
-#pragma unroll
-            for (int e = 0; e < P; ++e)
-                if (at + e < vocab) dx[at + e] = static_cast<T>(v[e]);
-        }
+        grad_pack<PAST, LOGS, ENTROPY>(v, dx, static_cast<int32_t>(vocab), q, row);
     }
 }
 
@@ -543,6 +579,132 @@ k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     }
 }
 
+// What a row's gradient is computed from, with its sums at hand: relative to a binary32 number next to m k, for which s is S
+// but for what that is off; where m k leaves binary32 (or there is no m), from the logarithms.  True: the former.
+__device__ __forceinline__ bool grad_from_sums(RowGrad& g, const Sums& r, float log_sum, float scale) {
+    const float H = log_sum - kLn2 * (r.U / r.S);
+    g.empty = r.m == -INFINITY && r.S == r.S;
+    g.mul = scale * kLog2e;
+    g.add = r.m * g.mul;
+    if (!(fabsf(g.add) < INFINITY)) {
+        g.mul = scale;
+        g.add = fmaf(r.m, scale, log_sum);
+        g.a = fmaf(g.b, H, g.a);
+        return false;
+    }
+    const float s = r.S * exp2_of(fmaf(r.m, g.mul, -g.add)), one = 1.f / s;
+    g.a = one * fmaf(g.b, H - logf(s), g.a);
+    g.b *= one * kLn2;
+    return true;
+}
+
+enum { kForward, kAlternatives, kLoss };
+
+// A row held in registers by THREADS threads, up to ITEMS packs each: one read of it for everything.
+template <typename T, int THREADS, int ITEMS>
+struct HeldRow {
+    static constexpr int P = kPack<T>;
+    uint32_t word[ITEMS][4];
+    __device__ __forceinline__ void load(const T* x, int32_t vocab, int32_t packs) {
+        const int32_t t = thread_of_row<THREADS>(), whole = vocab / P;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+            if (t + i * THREADS < whole) __builtin_memcpy(word[i], x + i * THREADS * P + t * P, 16);
+        if (packs > whole && t == whole % THREADS) {         // the pack that the row ends in
+            T v[P];
+            uint32_t last[4];
+#pragma unroll
+            for (int e = 0; e < P; ++e) v[e] = whole * P + e < vocab ? x[whole * P + e] : static_cast<T>(-INFINITY);
+            __builtin_memcpy(last, v, 16);
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (t + i * THREADS == whole) __builtin_memcpy(word[i], last, 16);
+        }
+    }
+    __device__ __forceinline__ void values(int i, float (&v)[P]) const {
+        T raw[P];
+        __builtin_memcpy(raw, word[i], 16);
+#pragma unroll
+        for (int e = 0; e < P; ++e) v[e] = static_cast<float>(raw[e]);
+    }
+    // what is made of the values from here on is made anew: the words stay in registers, not the values in binary32, which
+    // take twice as many (1024 threads, 5 packs of bf16: 94 registers without this)
+    __device__ __forceinline__ void forget_values() {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(word[i][e]));
+    }
+};
+
+template <bool PAST, bool LOGS, bool ENTROPY, int THREADS, int ITEMS, typename T>
+__device__ __forceinline__ void grad_held(const HeldRow<T, THREADS, ITEMS>& held, T* dx, int32_t vocab, int32_t packs, const RowGrad& row) {
+    constexpr int P = kPack<T>;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int32_t q = thread_of_row<THREADS>() + i * THREADS;
+        if (q < packs) {
+            float v[P];
+            held.values(i, v);
+            grad_pack<PAST, LOGS, ENTROPY>(v, dx, vocab, q, row);
+        }
+        __builtin_amdgcn_sched_barrier(0);            // (a pack at a time: the registers for several are wanted for other rows)
+    }
+}
+
+template <typename T, int MODE, int THREADS, int ITEMS, bool PAST>
+__global__ void __launch_bounds__(THREADS == 64 ? kThreads : THREADS)
+k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out, int top,
+             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs) {
+    constexpr int ROWS = THREADS == 64 ? kThreads / 64 : 1, P = kPack<T>;
+    __shared__ TokenShared<THREADS> shared[ROWS];
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + (THREADS == 64 ? threadIdx.x >> 6 : 0);
+    if (row >= rows) return;                          // (a wavefront: nothing waits for it)
+    TokenShared<THREADS>& sh = shared[THREADS == 64 ? threadIdx.x >> 6 : 0];
+    const T* x = logits + row * stride;
+    const int64_t t = MODE == kLoss || out.logp ? target[row] : -1;
+    const float k = scale * kLog2e;
+    HeldRow<T, THREADS, ITEMS> held;
+    held.load(x, vocab, packs);
+    Target<T> hit;
+    hit.load(x, vocab, t);
+    Scan<T, MODE == kAlternatives> scan;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int32_t q = thread_of_row<THREADS>() + i * THREADS;
+        if (q < packs) {
+            float v[1][P];
+            held.values(i, v[0]);
+            scan.template meet<1>(v, 1, k, q, THREADS);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    held.forget_values();
+    const Sums r = join_threads<T, MODE == kAlternatives, THREADS>(x, vocab, 0, packs, k, sh, scan);
+    const float log_sum = logf(r.S);
+    if (thread_of_row<THREADS>() == 0) row_results(row, hit, scale, r, log_sum, out);
+    if constexpr (MODE == kAlternatives) {
+        const auto pack_at = [&](int32_t q, float(&v)[P]) {
+            // (constant indexes: registers have no others)
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+                if (q == thread_of_row<THREADS>() + i * THREADS) held.values(i, v);
+        };
+        largest_of_part<T, THREADS>(vocab, 0, packs, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
+            out.top_idx[row * top + rank] = index_of(key);
+            out.top_logp[row * top + rank] = logp_of(value_of(static_cast<uint32_t>(key >> 32)), r, log_sum, scale);
+        });
+    }
+    if constexpr (MODE == kLoss) {
+        T* dx = dlogits + row * d_stride;
+        RowGrad g;
+        g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
+        if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, true, true, THREADS, ITEMS>(held, dx, vocab, packs, g);
+        else if (g_entropy) grad_held<PAST, false, true, THREADS, ITEMS>(held, dx, vocab, packs, g);
+        else grad_held<PAST, false, false, THREADS, ITEMS>(held, dx, vocab, packs, g);
+    }
+}
+
 // forward and gradient of a row in one workgroup: the row's second read comes from the caches
 template <typename T, bool PAST>
 __global__ void __launch_bounds__(kThreads)
@@ -564,23 +726,9 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
     RowGrad g;
     g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
-    g.empty = r.m == -INFINITY && r.S == r.S;
-    const float H = log_sum - 0.69314718055994531f * (r.U / r.S);
-    // relative to a binary32 number next to m k: s is S but for what that is off
-    g.mul = k;
-    g.add = r.m * k;
-    const float off = fmaf(r.m, k, -g.add), s = r.S * exp2_of(off), one = 1.f / s;
-    if (fabsf(g.add) < INFINITY) {
-        g.a = one * fmaf(g.b, H - logf(s), g.a);
-        g.b *= one * 0.69314718055994531f;
-        if (g_entropy) grad_packs<PAST, false, true, kThreads>(x, dx, vocab, 0, packs, g);
-        else grad_packs<PAST, false, false, kThreads>(x, dx, vocab, 0, packs, g);
-    } else {                                          // (a largest value beyond 2e38, or none)
-        g.mul = scale;
-        g.add = fmaf(r.m, scale, log_sum);
-        g.a = fmaf(g.b, H, g.a);
-        grad_packs<PAST, true, true, kThreads>(x, dx, vocab, 0, packs, g);
-    }
+    if (!grad_from_sums(g, r, log_sum, scale)) grad_packs<PAST, true, true, kThreads>(x, dx, vocab, 0, packs, g);
+    else if (g_entropy) grad_packs<PAST, false, true, kThreads>(x, dx, vocab, 0, packs, g);
+    else grad_packs<PAST, false, false, kThreads>(x, dx, vocab, 0, packs, g);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -632,8 +780,55 @@ struct TokenArgs {
     hipStream_t stream;
 };
 
+// rows that are held in registers: threads a row and packs a thread (threads = 0: they are not)
+struct Held {
+    int threads, items;
+};
+Held held(int64_t rows, int64_t vocab, int32_t fmt, bool loss) {
+    const int32_t packs = packs_of(vocab, fmt);
+    if (packs <= 256) return {64, (packs + 63) / 64};
+    if (!loss || parts_of(rows, vocab) > 1) return {0, 0};
+    if (packs <= 2048) return {256, packs <= 512 ? 2 : packs <= 1024 ? 4 : 8};
+    if (packs <= 5120) return {512, packs <= 512 * 6 ? 6 : packs <= 512 * 8 ? 8 : packs <= 512 * 9 ? 9 : 10};
+    if (packs <= 8192) return {1024, packs <= 6144 ? 6 : 8};
+    return {0, 0};
+}
+template <typename T, int MODE, int THREADS, int ITEMS>
+int token_held_as(const TokenArgs& a) {
+    const auto kernel = MODE == kLoss && past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_held<T, MODE, THREADS, ITEMS, MODE == kLoss>
+                                                                                   : k_token_held<T, MODE, THREADS, ITEMS, false>;
+    const int64_t grid = THREADS == 64 ? (a.rows + 3) / 4 : a.rows;
+    kernel<<<static_cast<unsigned>(grid), THREADS == 64 ? kThreads : THREADS, 0, a.stream>>>(
+        static_cast<const T*>(a.logits), a.rows, static_cast<int32_t>(a.vocab), a.stride, a.scale, a.target, a.out, a.top, a.g_logp, a.g_entropy,
+        static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt));
+    return launched();
+}
+template <typename T, int MODE>
+int token_held(const TokenArgs& a, const Held& h) {
+    switch (h.threads * 32 + h.items) {
+        case 64 * 32 + 1: return token_held_as<T, MODE, 64, 1>(a);
+        case 64 * 32 + 2: return token_held_as<T, MODE, 64, 2>(a);
+        case 64 * 32 + 3: return token_held_as<T, MODE, 64, 3>(a);
+        case 64 * 32 + 4: return token_held_as<T, MODE, 64, 4>(a);
+    }
+    if constexpr (MODE == kLoss) switch (h.threads * 32 + h.items) {
+        case 256 * 32 + 2: return token_held_as<T, MODE, 256, 2>(a);
+        case 256 * 32 + 4: return token_held_as<T, MODE, 256, 4>(a);
+        case 256 * 32 + 8: return token_held_as<T, MODE, 256, 8>(a);
+        case 512 * 32 + 6: return token_held_as<T, MODE, 512, 6>(a);
+        case 512 * 32 + 8: return token_held_as<T, MODE, 512, 8>(a);
+        case 512 * 32 + 9: return token_held_as<T, MODE, 512, 9>(a);
+        case 512 * 32 + 10: return token_held_as<T, MODE, 512, 10>(a);
+        case 1024 * 32 + 6: return token_held_as<T, MODE, 1024, 6>(a);
+        case 1024 * 32 + 8: return token_held_as<T, MODE, 1024, 8>(a);
+    }
+    return CS_EINVAL;
+}
+
 template <typename T, bool TOP>
 int token_forward(const TokenArgs& a) {
+    const Held h = held(a.rows, a.vocab, a.fmt, false);
+    if (h.threads) return token_held<T, TOP ? kAlternatives : kForward>(a, h);
     const int parts = parts_of(a.rows, a.vocab);
     const Parts ws = parts > 1 ? parts_in(a.ws, a.rows, parts, a.top) : Parts{};
     const T* x = static_cast<const T*>(a.logits);
@@ -661,6 +856,8 @@ int token_grad(const TokenArgs& a) {
 }
 template <typename T>
 int token_loss(TokenArgs a) {
+    const Held h = held(a.rows, a.vocab, a.fmt, true);
+    if (h.threads) return token_held<T, kLoss>(a, h);
     if (few_rows(a.rows)) {
         if (int rc = token_forward<T, false>(a)) return rc;
         a.lse = a.out.lse, a.entropy = a.out.entropy;
