@@ -110,27 +110,24 @@ struct Scan {
     float B = -FLT_MAX, s = 0.f, u = 0.f, most = -INFINITY;
     int32_t most_pack = INT32_MAX;           // TOP: the first pack with that value
 
-    // N packs, the first `count` of which there are; number j is pack + j * step
-    template <int N>
-    __device__ __forceinline__ void meet(const float (&v)[N][P], int count, float k, int32_t pack, int32_t step) {
-        float top = -INFINITY, low = INFINITY;
+    // a pack's largest and lowest value into top and low
+    __device__ __forceinline__ void look(const float (&v)[P], int32_t pack, float& top, float& low) {
+        float t = fmaxf(v[0], v[1]);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            if (j >= count) break;
-            float t = fmaxf(v[j][0], v[j][1]);
+        for (int e = 2; e < P; e += 2) t = fmaxf(fmaxf(v[e], v[e + 1]), t);
 #pragma unroll
-            for (int e = 2; e < P; e += 2) t = fmaxf(fmaxf(v[j][e], v[j][e + 1]), t);
-#pragma unroll
-            for (int e = 0; e < P; e += 2) low = fminf(fminf(v[j][e], v[j][e + 1]), low);
-            if (TOP) {
-                // (the first pack counts also where it holds nothing above -inf)
-                if (t > most || most_pack == INT32_MAX) {
-                    most = t == t ? t : -INFINITY;
-                    most_pack = pack + j * step;
-                }
+        for (int e = 0; e < P; e += 2) low = fminf(fminf(v[e], v[e + 1]), low);
+        if (TOP) {
+            // (the first pack counts also where it holds nothing above -inf)
+            if (t > most || most_pack == INT32_MAX) {
+                most = t == t ? t : -INFINITY;
+                most_pack = pack;
             }
-            top = fmaxf(top, t);
         }
+        top = fmaxf(top, t);
+    }
+    // the largest value yet: sums relative to it
+    __device__ __forceinline__ void raise(float top, float k) {
         if (!TOP) most = fmaxf(most, top);
         const float b = top * k;
         if (b > B) {
@@ -139,28 +136,33 @@ struct Scan {
             s *= f;
             B = b;
         }
+    }
+    // GUARDED: values may be -inf
+    template <bool GUARDED>
+    __device__ __forceinline__ void add(const float (&v)[P], float k) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            const float d = fmaf(v[e], k, -B), x = exp2_of(d);
+            s += x;
+            u = fmaf(x, GUARDED ? fmaxf(d, kFar) : d, u);
+        }
+    }
+    // N packs, the first `count` of which there are; number j is pack + j * step
+    template <int N>
+    __device__ __forceinline__ void meet(const float (&v)[N][P], int count, float k, int32_t pack, int32_t step) {
+        float top = -INFINITY, low = INFINITY;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j < count) look(v[j], pack + j * step, top, low);
+        raise(top, k);
         if (low > kPlain) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if (j >= count) break;
-#pragma unroll
-                for (int e = 0; e < P; ++e) {
-                    const float d = fmaf(v[j][e], k, -B), x = exp2_of(d);
-                    s += x;
-                    u = fmaf(x, d, u);
-                }
-            }
+            for (int j = 0; j < N; ++j)
+                if (j < count) add<false>(v[j], k);
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if (j >= count) break;
-#pragma unroll
-                for (int e = 0; e < P; ++e) {
-                    const float d = fmaf(v[j][e], k, -B), x = exp2_of(d);
-                    s += x;
-                    u = fmaf(x, fmaxf(d, kFar), u);
-                }
-            }
+            for (int j = 0; j < N; ++j)
+                if (j < count) add<true>(v[j], k);
         }
     }
 };
@@ -600,16 +602,21 @@ __device__ __forceinline__ bool grad_from_sums(RowGrad& g, const Sums& r, float 
 
 enum { kForward, kAlternatives, kLoss };
 
-// A row held in registers by THREADS threads, up to ITEMS packs each: one read of it for everything.
+// A row held in registers by THREADS threads, up to ITEMS packs each: one read of it for everything.  All but the last EITHER
+// packs of a thread there are.
 template <typename T, int THREADS, int ITEMS>
 struct HeldRow {
-    static constexpr int P = kPack<T>;
+    static constexpr int P = kPack<T>, EITHER = THREADS == 64 ? 1 : 2;
     uint32_t word[ITEMS][4];
-    __device__ __forceinline__ void load(const T* x, int32_t vocab, int32_t packs) {
+    int32_t packs;
+    __device__ __forceinline__ static int32_t pack(int i) { return thread_of_row<THREADS>() + i * THREADS; }
+    __device__ __forceinline__ bool has(int i) const { return i < ITEMS - EITHER || pack(i) < packs; }
+    __device__ __forceinline__ void load(const T* x, int32_t vocab, int32_t n) {
         const int32_t t = thread_of_row<THREADS>(), whole = vocab / P;
+        packs = n;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
-            if (t + i * THREADS < whole) __builtin_memcpy(word[i], x + i * THREADS * P + t * P, 16);
+            if (i < ITEMS - EITHER || pack(i) < whole) __builtin_memcpy(word[i], x + i * THREADS * P + t * P, 16);
         if (packs > whole && t == whole % THREADS) {         // the pack that the row ends in
             T v[P];
             uint32_t last[4];
@@ -617,39 +624,55 @@ struct HeldRow {
             for (int e = 0; e < P; ++e) v[e] = whole * P + e < vocab ? x[whole * P + e] : static_cast<T>(-INFINITY);
             __builtin_memcpy(last, v, 16);
 #pragma unroll
-            for (int i = 0; i < ITEMS; ++i)
-                if (t + i * THREADS == whole) __builtin_memcpy(word[i], last, 16);
+            for (int i = ITEMS - EITHER; i < ITEMS; ++i)
+                if (pack(i) == whole) __builtin_memcpy(word[i], last, 16);
         }
     }
+    // (The empty statement has the values made from the words each time: kept in binary32 they would take twice the registers,
+    // and registers are rows of other workgroups.)
     __device__ __forceinline__ void values(int i, float (&v)[P]) const {
         T raw[P];
-        __builtin_memcpy(raw, word[i], 16);
+        uint32_t w[4] = {word[i][0], word[i][1], word[i][2], word[i][3]};
+        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3]));
+        __builtin_memcpy(raw, w, 16);
 #pragma unroll
         for (int e = 0; e < P; ++e) v[e] = static_cast<float>(raw[e]);
     }
-    // what is made of the values from here on is made anew: the words stay in registers, not the values in binary32, which
-    // take twice as many (1024 threads, 5 packs of bf16: 94 registers without this)
-    __device__ __forceinline__ void forget_values() {
+    template <bool TOP>
+    __device__ __forceinline__ void scan(Scan<T, TOP>& scan, float k) const {
+        float top = -INFINITY, low = INFINITY;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
+            if (has(i)) {
+                float v[P];
+                values(i, v);
+                scan.look(v, pack(i), top, low);
+            }
+        scan.raise(top, k);
+        if (low > kPlain) add<false>(scan, k);
+        else add<true>(scan, k);
+    }
+    template <bool GUARDED, bool TOP>
+    __device__ __forceinline__ void add(Scan<T, TOP>& scan, float k) const {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(word[i][e]));
+        for (int i = 0; i < ITEMS; ++i)
+            if (has(i)) {
+                float v[P];
+                values(i, v);
+                scan.template add<GUARDED>(v, k);
+            }
     }
 };
 
 template <bool PAST, bool LOGS, bool ENTROPY, int THREADS, int ITEMS, typename T>
-__device__ __forceinline__ void grad_held(const HeldRow<T, THREADS, ITEMS>& held, T* dx, int32_t vocab, int32_t packs, const RowGrad& row) {
-    constexpr int P = kPack<T>;
+__device__ __forceinline__ void grad_held(const HeldRow<T, THREADS, ITEMS>& held, T* dx, int32_t vocab, const RowGrad& row) {
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int32_t q = thread_of_row<THREADS>() + i * THREADS;
-        if (q < packs) {
-            float v[P];
+    for (int i = 0; i < ITEMS; ++i)
+        if (held.has(i)) {
+            float v[kPack<T>];
             held.values(i, v);
-            grad_pack<PAST, LOGS, ENTROPY>(v, dx, vocab, q, row);
+            grad_pack<PAST, LOGS, ENTROPY>(v, dx, vocab, held.pack(i), row);
         }
-        __builtin_amdgcn_sched_barrier(0);            // (a pack at a time: the registers for several are wanted for other rows)
-    }
 }
 
 template <typename T, int MODE, int THREADS, int ITEMS, bool PAST>
@@ -669,17 +692,7 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
     Target<T> hit;
     hit.load(x, vocab, t);
     Scan<T, MODE == kAlternatives> scan;
-#pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int32_t q = thread_of_row<THREADS>() + i * THREADS;
-        if (q < packs) {
-            float v[1][P];
-            held.values(i, v[0]);
-            scan.template meet<1>(v, 1, k, q, THREADS);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    held.forget_values();
+    held.scan(scan, k);
     const Sums r = join_threads<T, MODE == kAlternatives, THREADS>(x, vocab, 0, packs, k, sh, scan);
     const float log_sum = logf(r.S);
     if (thread_of_row<THREADS>() == 0) row_results(row, hit, scale, r, log_sum, out);
@@ -688,7 +701,7 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
             // (constant indexes: registers have no others)
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i)
-                if (q == thread_of_row<THREADS>() + i * THREADS) held.values(i, v);
+                if (q == held.pack(i)) held.values(i, v);
         };
         largest_of_part<T, THREADS>(vocab, 0, packs, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
             out.top_idx[row * top + rank] = index_of(key);
@@ -699,9 +712,9 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
         T* dx = dlogits + row * d_stride;
         RowGrad g;
         g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
-        if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, true, true, THREADS, ITEMS>(held, dx, vocab, packs, g);
-        else if (g_entropy) grad_held<PAST, false, true, THREADS, ITEMS>(held, dx, vocab, packs, g);
-        else grad_held<PAST, false, false, THREADS, ITEMS>(held, dx, vocab, packs, g);
+        if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, true, true, THREADS, ITEMS>(held, dx, vocab, g);
+        else if (g_entropy) grad_held<PAST, false, true, THREADS, ITEMS>(held, dx, vocab, g);
+        else grad_held<PAST, false, false, THREADS, ITEMS>(held, dx, vocab, g);
     }
 }
 
@@ -788,9 +801,10 @@ Held held(int64_t rows, int64_t vocab, int32_t fmt, bool loss) {
     const int32_t packs = packs_of(vocab, fmt);
     if (packs <= 256) return {64, (packs + 63) / 64};
     if (!loss || parts_of(rows, vocab) > 1) return {0, 0};
-    if (packs <= 2048) return {256, packs <= 512 ? 2 : packs <= 1024 ? 4 : 8};
-    if (packs <= 5120) return {512, packs <= 512 * 6 ? 6 : packs <= 512 * 8 ? 8 : packs <= 512 * 9 ? 9 : 10};
-    if (packs <= 8192) return {1024, packs <= 6144 ? 6 : 8};
+    for (const int threads : {256, 512, 1024}) {
+        const int items = (packs + 2 * threads - 1) / (2 * threads) * 2;
+        if (items <= (threads == 512 ? 10 : 8)) return {threads, items};
+    }
     return {0, 0};
 }
 template <typename T, int MODE, int THREADS, int ITEMS>
@@ -814,10 +828,10 @@ int token_held(const TokenArgs& a, const Held& h) {
     if constexpr (MODE == kLoss) switch (h.threads * 32 + h.items) {
         case 256 * 32 + 2: return token_held_as<T, MODE, 256, 2>(a);
         case 256 * 32 + 4: return token_held_as<T, MODE, 256, 4>(a);
+        case 256 * 32 + 6: return token_held_as<T, MODE, 256, 6>(a);
         case 256 * 32 + 8: return token_held_as<T, MODE, 256, 8>(a);
         case 512 * 32 + 6: return token_held_as<T, MODE, 512, 6>(a);
         case 512 * 32 + 8: return token_held_as<T, MODE, 512, 8>(a);
-        case 512 * 32 + 9: return token_held_as<T, MODE, 512, 9>(a);
         case 512 * 32 + 10: return token_held_as<T, MODE, 512, 10>(a);
         case 1024 * 32 + 6: return token_held_as<T, MODE, 1024, 6>(a);
         case 1024 * 32 + 8: return token_held_as<T, MODE, 1024, 8>(a);
