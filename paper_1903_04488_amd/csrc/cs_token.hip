@@ -803,7 +803,7 @@ Held held(int64_t rows, int64_t vocab, int32_t fmt, bool loss) {
     if (!loss || parts_of(rows, vocab) > 1) return {0, 0};
     for (const int threads : {256, 512, 1024}) {
         const int items = (packs + 2 * threads - 1) / (2 * threads) * 2;
-        if (items <= (threads == 512 ? 10 : 8)) return {threads, items};
+        if (items <= (threads == 256 ? 8 : 16)) return {threads, items};
     }
     return {0, 0};
 }
@@ -833,8 +833,13 @@ int token_held(const TokenArgs& a, const Held& h) {
         case 512 * 32 + 6: return token_held_as<T, MODE, 512, 6>(a);
         case 512 * 32 + 8: return token_held_as<T, MODE, 512, 8>(a);
         case 512 * 32 + 10: return token_held_as<T, MODE, 512, 10>(a);
-        case 1024 * 32 + 6: return token_held_as<T, MODE, 1024, 6>(a);
-        case 1024 * 32 + 8: return token_held_as<T, MODE, 1024, 8>(a);
+        case 512 * 32 + 12: return token_held_as<T, MODE, 512, 12>(a);
+        case 512 * 32 + 14: return token_held_as<T, MODE, 512, 14>(a);
+        case 512 * 32 + 16: return token_held_as<T, MODE, 512, 16>(a);
+        case 1024 * 32 + 10: return token_held_as<T, MODE, 1024, 10>(a);
+        case 1024 * 32 + 12: return token_held_as<T, MODE, 1024, 12>(a);
+        case 1024 * 32 + 14: return token_held_as<T, MODE, 1024, 14>(a);
+        case 1024 * 32 + 16: return token_held_as<T, MODE, 1024, 16>(a);
     }
     return CS_EINVAL;
 }
