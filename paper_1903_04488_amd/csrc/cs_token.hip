@@ -57,7 +57,8 @@ struct TokenShared {
     float f[3][16];
     int32_t order[THREADS / UNIT], pack[THREADS / UNIT];
     uint64_t list[LIST];
-    int32_t n;
+    int32_t chosen[kMaxTop * UNIT];
+    int32_t n, chosen_n;
     uint64_t best[16];
 };
 template <int THREADS>
@@ -177,7 +178,7 @@ __device__ __forceinline__ void load_tail(const T* row, int64_t at, int64_t voca
 // Packs [first, last) of a row (`last` may be one that the row ends in): the thread's own sums.
 template <typename T, bool TOP, int THREADS>
 __device__ __forceinline__ void scan_packs(const T* row, int64_t vocab, int32_t first, int32_t last, float k, Scan<T, TOP>& scan) {
-    constexpr int P = kPack<T>, N = THREADS == kFewThreads || sizeof(T) == 4 ? 4 : 1;
+    constexpr int P = kPack<T>, N = sizeof(T) == 4 ? 4 : THREADS == kFewThreads ? 2 : 1;
     const int32_t whole = static_cast<int32_t>(vocab / P);         // packs before one that the row ends in
     const int32_t stop = last < whole ? last : whole;
     for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < stop; q += N * THREADS) {
@@ -260,7 +261,7 @@ __device__ __forceinline__ void rank_list(const uint64_t* list, int32_t n, int t
 // largest are among the values of the `top` units before it that reach it too: usually hardly more than `top` values, which
 // those threads list and which are then ranked by counting.  The bound is found bit by bit, in every wavefront by itself, a
 // unit (or four) a lane.
-template <typename T, int THREADS, typename PackAt, typename Emit>
+template <typename T, int THREADS, bool HELD, typename PackAt, typename Emit>
 __device__ __forceinline__ void largest_of_part(int64_t vocab, int32_t first, int32_t last, int top,
                                                 const Scan<T, true>& scan, TokenShared<THREADS>& sh, PackAt pack_at, Emit emit) {
     constexpr int P = kPack<T>, LOW = kAlike<T>, UNIT = TokenShared<THREADS>::UNIT, PER = THREADS / UNIT / 64;
@@ -280,7 +281,7 @@ __device__ __forceinline__ void largest_of_part(int64_t vocab, int32_t first, in
         sh.order[tid / UNIT] = most;
         sh.pack[tid / UNIT] = pack;
     }
-    if (tid == 0) sh.n = 0;
+    if (tid == 0) sh.n = sh.chosen_n = 0;
     row_sync<THREADS>();
     int32_t o[PER], q[PER];
 #pragma unroll
@@ -319,19 +320,41 @@ __device__ __forceinline__ void largest_of_part(int64_t vocab, int32_t first, in
         }
     }
     const bool chosen = most > bound || (most == bound && pack <= bound_pack);
-    if (chosen) {
-        for (int32_t at_pack = first + tid; at_pack < last; at_pack += THREADS) {
-            const int64_t at = static_cast<int64_t>(at_pack) * P;
-            float v[P];
-            pack_at(at_pack, v);
+    const auto list = [&](const float(&v)[P], int32_t at_pack) {
+        const int64_t at = static_cast<int64_t>(at_pack) * P;
 #pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const int32_t x = static_cast<int32_t>(order_of(v[e]) ^ 0x80000000u) >> LOW;
-                if (at + e < vocab && (x > bound || (x == bound && at_pack <= bound_pack))) {
-                    const int32_t slot = atomicAdd(&sh.n, 1);
-                    if (slot < LIST) sh.list[slot] = key_of(v[e], at + e);
-                }
+        for (int e = 0; e < P; ++e) {
+            const int32_t x = static_cast<int32_t>(order_of(v[e]) ^ 0x80000000u) >> LOW;
+            if (at + e < vocab && (x > bound || (x == bound && at_pack <= bound_pack))) {
+                const int32_t slot = atomicAdd(&sh.n, 1);
+                if (slot < LIST) sh.list[slot] = key_of(v[e], at + e);
             }
+        }
+    };
+    if (HELD) {
+        if (chosen)
+            for (int32_t at_pack = first + tid; at_pack < last; at_pack += THREADS) {
+                float v[P];
+                pack_at(at_pack, v);
+                list(v, at_pack);
+            }
+    } else {
+        // the chosen threads' packs are read again by all threads, two requests each under way
+        if (chosen) sh.chosen[atomicAdd(&sh.chosen_n, 1)] = tid;
+        __syncthreads();
+        const uint32_t threads = sh.chosen_n, each = (last - first + THREADS - 1) / THREADS, all = threads * each;
+        for (uint32_t w = tid; w < all; w += 2 * THREADS) {
+            float v[2][P];
+            int32_t at_pack[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t i = w + j * THREADS;
+                at_pack[j] = i < all ? first + sh.chosen[i % threads] + static_cast<int32_t>(i / threads) * THREADS : last;
+                if (at_pack[j] < last) pack_at(at_pack[j], v[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (at_pack[j] < last) list(v[j], at_pack[j]);
         }
     }
     row_sync<THREADS>();
@@ -437,7 +460,7 @@ k_token(const T* logits, int64_t vocab, int64_t stride, float scale, const int64
             if ((static_cast<int64_t>(q) + 1) * kPack<T> <= vocab) load_pack<T, kPack<T>>(x + static_cast<int64_t>(q) * kPack<T>, v);
             else load_tail(x, static_cast<int64_t>(q) * kPack<T>, vocab, v);
         };
-        largest_of_part<T, THREADS>(vocab, first, last, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
+        largest_of_part<T, THREADS, false>(vocab, first, last, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
             if (parts > 1) {
                 ws.key[at * top + rank] = key;
             } else {
@@ -703,7 +726,7 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
             for (int i = 0; i < ITEMS; ++i)
                 if (q == held.pack(i)) held.values(i, v);
         };
-        largest_of_part<T, THREADS>(vocab, 0, packs, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
+        largest_of_part<T, THREADS, true>(vocab, 0, packs, top, scan, sh, pack_at, [&](int rank, uint64_t key) {
             out.top_idx[row * top + rank] = index_of(key);
             out.top_logp[row * top + rank] = logp_of(value_of(static_cast<uint32_t>(key >> 32)), r, log_sum, scale);
         });
@@ -758,7 +781,7 @@ int32_t packs_of(int64_t vocab, int32_t fmt) {
 }
 // Workgroups of kThreads take a row each where there are enough rows; few rows have workgroups of kFewThreads, and share
 // those of long rows
-bool few_rows(int64_t rows) { return rows < 512; }
+bool few_rows(int64_t rows) { return rows < 1024; }
 int parts_of(int64_t rows, int64_t vocab) {
     if (!few_rows(rows)) return 1;
     int64_t parts = 512 / (rows ? rows : 1);
