@@ -786,6 +786,16 @@ _FMT = {torch.bfloat16: CS_FMT_BF16, torch.float16: CS_FMT_F16, torch.float32: C
 
 def _rows(t, name: str, like=None):
     """(address, row stride) of a 2-d tensor whose rows are contiguous; of the shape and type of `like`"""
+    # (a call for one token waits for the host: what is fine is seen first)
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2 and t.dtype in _FMT and t.is_contiguous()
+            and (like is None or (t.dtype is like.dtype and t.shape == like.shape))):
+        cols = t.size(1)
+        if cols:
+            return t.data_ptr(), cols
+    return _rows_address(t, name, like)
+
+
+def _rows_address(t, name: str, like):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise CsError(f"{name} must be a tensor on the GPU")
     if t.dtype not in _FMT:
@@ -807,16 +817,20 @@ def _rows(t, name: str, like=None):
 
 
 def _maybe(t, dtype, name: str, numel: int):
-    return _dev(t, dtype, name, numel) if t is not None else None
+    if t is None:
+        return None
+    if (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()
+            and (numel is None or t.numel() == numel)):
+        return t.data_ptr()
+    return _address(t, dtype, name, numel)
 
 
 def _weights(weight, bias, x):
     """(address, address, format) of what scales and shifts a norm's columns"""
-    given = [w for w in (weight, bias) if w is not None]
-    dtype = given[0].dtype if given else torch.float32
+    dtype = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
     if dtype is not x.dtype and dtype is not torch.float32:
         raise CsError(f"weight and bias must have dtype {x.dtype} or float32, got {dtype}")
-    cols = x.shape[1]
+    cols = x.size(1)
     return _maybe(weight, dtype, "weight", cols), _maybe(bias, dtype, "bias", cols), _FMT[dtype]
 
 
