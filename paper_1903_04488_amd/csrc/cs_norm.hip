@@ -219,11 +219,13 @@ k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, co
 // Each group of TPR threads of a workgroup takes rows of its own and keeps the sums of its columns' gradients in registers
 // until its last row; SUMS: they are wanted.
 constexpr int kGradBlock = 512;
+template <int TPR>
+constexpr int grad_threads() { return TPR < kGradBlock ? kGradBlock : TPR; }
 template <typename T, typename W, int TPR, int ITEMS, bool SUMS, bool PAST>
-__global__ void __launch_bounds__(kGradBlock)
+__global__ void __launch_bounds__(grad_threads<TPR>())
 k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight,
             const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* partials) {
-    constexpr int P = kPack<T>, ROWS = kGradBlock / TPR;
+    constexpr int P = kPack<T>, ROWS = grad_threads<TPR>() / TPR;
     __shared__ float lds[2][2][16];
     int turn = 0;
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
@@ -318,7 +320,7 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
             }
             __syncthreads();
         }
-        for (int c = threadIdx.x; c < cols; c += kGradBlock) {
+        for (int c = threadIdx.x; c < cols; c += grad_threads<TPR>()) {
             mine[c] = sums[0][c];
             mine[cols + c] = sums[1][c];
         }
@@ -346,7 +348,7 @@ struct Held {
 Held held(int64_t cols, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
     if (cols < p) return {0, 0};
-    for (const int threads : {64, 256, 512}) {
+    for (const int threads : {64, 256, 512, 1024}) {
         const int64_t items = (packs + threads - 1) / threads;
         if (items <= 4) return {threads, static_cast<int>(items)};
     }
@@ -356,9 +358,11 @@ Held held(int64_t cols, int32_t fmt) {
 Held held_grad(int64_t cols, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
     if (cols < p) return {0, 0};
-    for (const int threads : {64, 128, 256, 512}) {
+    for (const int threads : {64, 128, 256, 512, 1024}) {
         const int64_t items = (packs + threads - 1) / threads;
-        if (items <= (threads == 512 ? 4 : 1)) return {threads, static_cast<int>(items)};
+        // (1024 threads have 128 registers each: enough for four packs of four values, not for two of eight)
+        if (threads == 1024 && p > 4) break;
+        if (items <= (threads >= 512 ? 4 : 1)) return {threads, static_cast<int>(items)};
     }
     return {0, 0};
 }
@@ -366,7 +370,7 @@ Held held_grad(int64_t cols, int32_t fmt) {
 unsigned norm_grid(int64_t rows) { return static_cast<unsigned>(rows < 4096 ? rows : 4096); }
 // workgroups of the backward pass over rows that are held in registers; each leaves partial sums of the weights' gradients
 int grad_grid(int64_t rows, const Held& h, int32_t fmt) {
-    const int64_t groups = kGradBlock / h.threads, n = (rows + groups - 1) / groups, most = h.items * (16 / fmt_bytes(fmt)) <= 8 ? 512 : 256;
+    const int64_t groups = h.threads < kGradBlock ? kGradBlock / h.threads : 1, n = (rows + groups - 1) / groups, most = h.items * (16 / fmt_bytes(fmt)) <= 8 ? 512 : 256;
     return static_cast<int>(n < most ? n : most);
 }
 // shares of the rows whose partial sums of the weights' gradients are added up at the end
@@ -395,7 +399,7 @@ int norm_grad_held(const NormArgs& a, int shares) {
     const bool past = past_caches(a.rows * a.cols * sizeof(T));
     const auto kernel = sums ? (past ? k_norm_grad<T, W, TPR, ITEMS, true, true> : k_norm_grad<T, W, TPR, ITEMS, true, false>)
                              : (past ? k_norm_grad<T, W, TPR, ITEMS, false, true> : k_norm_grad<T, W, TPR, ITEMS, false, false>);
-    kernel<<<static_cast<unsigned>(shares), kGradBlock, 0, a.stream>>>(
+    kernel<<<static_cast<unsigned>(shares), grad_threads<TPR>(), 0, a.stream>>>(
         static_cast<const T*>(a.dy), a.dy_stride, static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols),
         static_cast<const W*>(a.weight), a.mean, a.rstd, static_cast<T*>(a.out), a.out_stride, a.partials);
     return launched();
@@ -411,6 +415,8 @@ int norm_grad_held(const NormArgs& a, int shares) {
         case 256 * 8 + 4: return CALL(256, 4);                                                         \
         case 512 * 8 + 3: return CALL(512, 3);                                                         \
         case 512 * 8 + 4: return CALL(512, 4);                                                         \
+        case 1024 * 8 + 3: return CALL(1024, 3);                                                       \
+        case 1024 * 8 + 4: return CALL(1024, 4);                                                       \
         default: return CS_EINVAL;                                                                     \
     }
 #define CS_HELD_GRAD(h, CALL)                                                                          \
@@ -446,6 +452,8 @@ int norm_grad(const NormArgs& a, int shares) {
     const Held h = held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
     if (h.threads) {
 #define CS_CALL(TPR, ITEMS) (norm_grad_held<T, W, TPR, ITEMS>(a, shares))
+        if constexpr (sizeof(T) == 4)
+            if (h.threads == 1024) return h.items == 3 ? CS_CALL(1024, 3) : CS_CALL(1024, 4);
         CS_HELD_GRAD(h, CS_CALL)
 #undef CS_CALL
     }
