@@ -304,10 +304,21 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
                     mine[cols + slot.at(i) + e] = db[i][e];
                 }
     } else {
-        // the groups' sums, one after the other
+        // the groups' sums, one after the other (those of a wavefront, if it has several, by exchanges before)
+        constexpr int PER = TPR < 64 ? 64 : TPR;
         __shared__ float sums[ROWS == 1 ? 1 : 2][ROWS == 1 ? 1 : TPR * ITEMS * P];
-        for (int w = 0; w < ROWS; ++w) {
-            if (group == w) {
+        if (TPR < 64)
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                for (int e = 0; e < P; ++e)
+#pragma unroll
+                    for (int d = TPR; d < 64; d <<= 1) {
+                        dw[i][e] += __shfl_xor(dw[i][e], d);
+                        db[i][e] += __shfl_xor(db[i][e], d);
+                    }
+        for (int w = 0; w < grad_threads<TPR>() / PER; ++w) {
+            if (static_cast<int>(threadIdx.x) / PER == w && threadIdx.x % PER < TPR) {
 #pragma unroll
                 for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
@@ -348,6 +359,7 @@ struct Held {
 Held held(int64_t cols, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
     if (cols < p) return {0, 0};
+    if (packs <= 16) return {16, 1};
     for (const int threads : {64, 256, 512, 1024}) {
         const int64_t items = (packs + threads - 1) / threads;
         if (items <= 4) return {threads, static_cast<int>(items)};
@@ -358,6 +370,7 @@ Held held(int64_t cols, int32_t fmt) {
 Held held_grad(int64_t cols, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
     if (cols < p) return {0, 0};
+    if (packs <= 16) return {16, 1};
     for (const int threads : {64, 128, 256, 512, 1024}) {
         const int64_t items = (packs + threads - 1) / threads;
         // (1024 threads have 128 registers each: enough for four packs of four values, not for two of eight)
@@ -385,7 +398,7 @@ int norm_shares(int64_t rows, int64_t cols, int32_t fmt) {
 
 template <typename T, typename W, int TPR, int ITEMS>
 int norm_forward_held(const NormArgs& a) {
-    const int64_t groups = TPR == 64 ? (a.rows + 3) / 4 : a.rows;
+    const int64_t each = threads_of<TPR>() / TPR, groups = (a.rows + each - 1) / each;
     const unsigned grid = static_cast<unsigned>(groups < 4096 ? groups : 4096);
     const auto kernel = past_caches(a.rows * a.cols * sizeof(T)) ? k_norm<T, W, TPR, ITEMS, true> : k_norm<T, W, TPR, ITEMS, false>;
     kernel<<<grid, threads_of<TPR>(), 0, a.stream>>>(
@@ -406,6 +419,7 @@ int norm_grad_held(const NormArgs& a, int shares) {
 }
 #define CS_HELD(h, CALL)                                                                               \
     switch ((h).threads * 8 + (h).items) {                                                             \
+        case 16 * 8 + 1: return CALL(16, 1);                                                           \
         case 64 * 8 + 1: return CALL(64, 1);                                                           \
         case 64 * 8 + 2: return CALL(64, 2);                                                           \
         case 64 * 8 + 3: return CALL(64, 3);                                                           \
@@ -421,6 +435,7 @@ int norm_grad_held(const NormArgs& a, int shares) {
     }
 #define CS_HELD_GRAD(h, CALL)                                                                          \
     switch ((h).threads * 8 + (h).items) {                                                             \
+        case 16 * 8 + 1: return CALL(16, 1);                                                           \
         case 64 * 8 + 1: return CALL(64, 1);                                                           \
         case 128 * 8 + 1: return CALL(128, 1);                                                         \
         case 256 * 8 + 1: return CALL(256, 1);                                                         \

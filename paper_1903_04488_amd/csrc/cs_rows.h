@@ -76,9 +76,20 @@ __device__ __forceinline__ float wave_max(float v) {
 
 // Sums over groups of THREADS threads of a workgroup, the same in every thread of a group; `turn` counts the calls of a kernel
 // (two buffers take turns, so that one barrier a call is enough; every group of the workgroup makes the same calls).
-// THREADS = 64: one wavefront, no barrier.
+// THREADS = 64 and 16: a wavefront, or a quarter, no barrier.
 template <int THREADS, int N>
 __device__ __forceinline__ void block_sums(float (&v)[N], float (&lds)[2][N][16], int& turn) {
+    static_assert(THREADS == 16 || THREADS % 64 == 0, "");
+    if (THREADS == 16) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] += dpp<0xB1, 0xf>(v[k]);
+            v[k] += dpp<0x4E, 0xf>(v[k]);
+            v[k] += dpp<0x141, 0xf>(v[k]);
+            v[k] += dpp<0x140, 0xf>(v[k]);
+        }
+        return;
+    }
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = wave_sum(v[k]);
     if (THREADS == 64) return;
