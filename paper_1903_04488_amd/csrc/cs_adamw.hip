@@ -110,19 +110,19 @@ __device__ __forceinline__ Moved move(float p, float g, float m, float v, const 
 }
 
 // four values of a lane, the first of them at `at`; beyond n: 0
-template <typename T>
+template <bool PAST = false, typename T>
 __device__ __forceinline__ void load4(const T* x, int64_t at, int64_t n, float (&v)[4]) {
     if (at + 4 <= n) {
-        load_pack<T, 4>(x + at, v);
+        load_pack<T, 4, PAST>(x + at, v);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = at + e < n ? static_cast<float>(x[at + e]) : 0.f;
     }
 }
-template <typename T>
+template <bool PAST = false, typename T>
 __device__ __forceinline__ void store4(T* x, int64_t at, int64_t n, const float (&v)[4]) {
     if (at + 4 <= n) {
-        store_pack<false>(x + at, v);
+        store_pack<PAST>(x + at, v);
     } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -151,7 +151,7 @@ __device__ __forceinline__ void store4_codes(uint8_t* x, int64_t at, int64_t n, 
 }
 
 // A wavefront takes blocks of 256 values, four a lane.
-template <typename P, typename G, bool EIGHT>
+template <typename P, typename G, bool EIGHT, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs, const float* grad_scale) {
     float scale = 1.f;
@@ -169,7 +169,7 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
         const int64_t block = begin + k * kBlock8, at = block + lane * 4;
         if (block >= t.n) return;                     // (the whole wavefront)
         float p[4], g[4], m[4], v[4], root[4];
-        load4(static_cast<const P*>(t.p), at, t.n, p);
+        load4<PAST>(static_cast<const P*>(t.p), at, t.n, p);
         load4(static_cast<const G*>(t.g), at, t.n, g);
         if (EIGHT) {
             const int32_t mb = base_of(t.m_exp[block / kBlock8]), vb = base_of(t.v_exp[block / kBlock8]);
@@ -182,15 +182,15 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
                 v[e] = r * r;
             }
         } else {
-            load4(static_cast<const float*>(t.m), at, t.n, m);
-            load4(static_cast<const float*>(t.v), at, t.n, v);
+            load4<PAST>(static_cast<const float*>(t.m), at, t.n, m);
+            load4<PAST>(static_cast<const float*>(t.v), at, t.n, v);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const Moved r = move(p[e], grad_scale ? g[e] * scale : g[e], m[e], v[e], c);
             p[e] = r.p, m[e] = r.m, v[e] = r.v, root[e] = r.root;
         }
-        store4(static_cast<P*>(t.p), at, t.n, p);
+        store4<PAST>(static_cast<P*>(t.p), at, t.n, p);
         if (EIGHT) {
             // (values beyond n are 0 all along)
             int32_t mm = 0, vm = 0;
@@ -213,8 +213,8 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
                 t.v_exp[block / kBlock8] = static_cast<uint8_t>(ve);
             }
         } else {
-            store4(static_cast<float*>(t.m), at, t.n, m);
-            store4(static_cast<float*>(t.v), at, t.n, v);
+            store4<PAST>(static_cast<float*>(t.m), at, t.n, m);
+            store4<PAST>(static_cast<float*>(t.v), at, t.n, v);
         }
     }
 }
@@ -283,14 +283,27 @@ __global__ void __launch_bounds__(kThreads)
 k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double* partials) {
     __shared__ double lds[4];
     double s = 0.;
-    for (int64_t c = blockIdx.x; c < count; c += gridDim.x) {
-        const Chunk ch = chunks[c];
-        const int64_t n = tensors[ch.tensor].n, begin = static_cast<int64_t>(ch.part) * kChunk;
-        const G* g = static_cast<const G*>(tensors[ch.tensor].g);
+    // (where the next chunk lies is looked up while this one's values are on their way)
+    Chunk ch = chunks[blockIdx.x];
+    int64_t n = tensors[ch.tensor].n, begin = static_cast<int64_t>(ch.part) * kChunk;
+    const G* g = static_cast<const G*>(tensors[ch.tensor].g);
+    for (int64_t c = blockIdx.x; c < count;) {
         constexpr int PER = kChunk / kThreads / 4;
         float v[PER][4];
+        if (begin + kChunk <= n) {
 #pragma unroll
-        for (int k = 0; k < PER; ++k) load4(g, begin + (k * kThreads + threadIdx.x) * 4, n, v[k]);
+            for (int k = 0; k < PER; ++k) load_pack<G, 4>(g + begin + (k * kThreads + threadIdx.x) * 4, v[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < PER; ++k) load4(g, begin + (k * kThreads + threadIdx.x) * 4, n, v[k]);
+        }
+        c += gridDim.x;
+        if (c < count) {
+            ch = chunks[c];
+            n = tensors[ch.tensor].n;
+            begin = static_cast<int64_t>(ch.part) * kChunk;
+            g = static_cast<const G*>(tensors[ch.tensor].g);
+        }
 #pragma unroll
         for (int k = 0; k < PER; ++k)
 #pragma unroll
@@ -363,8 +376,13 @@ template <typename P, typename G>
 int adamw(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
     const List at = list_of(l);
     const unsigned grid = static_cast<unsigned>(l->chunks);
-    if (l->bits == 8) k_adamw<P, G, true><<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, c, coefs, grad_scale);
-    else k_adamw<P, G, false><<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, c, coefs, grad_scale);
+    // Parameters and moments that the memory-side cache cannot keep are read and written past it: what it keeps is
+    // the gradients that their norm has just read.
+    const int64_t each = fmt_bytes(l->p_fmt) + (l->bits == 8 ? 2 : 8);
+    const bool past = past_caches(l->chunks * kChunk * each);
+    const auto kernel = l->bits == 8 ? (past ? k_adamw<P, G, true, true> : k_adamw<P, G, true, false>)
+                                     : (past ? k_adamw<P, G, false, true> : k_adamw<P, G, false, false>);
+    kernel<<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, c, coefs, grad_scale);
     return launched();
 }
 template <typename P>

@@ -24,10 +24,16 @@ struct Raw {
     __device__ __forceinline__ void load(const T* __restrict__ p) { __builtin_memcpy(v, p, sizeof(v)); }
     __device__ __forceinline__ float operator[](int e) const { return static_cast<float>(v[e]); }
 };
-template <typename T, int N>
+template <typename T, int N, bool PAST = false>
 __device__ __forceinline__ void load_pack(const T* __restrict__ p, float (&v)[N]) {
+    typedef uint32_t Words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
     Raw<T, N> raw;
-    raw.load(p);
+    if (PAST) {
+        const Words w = __builtin_nontemporal_load(reinterpret_cast<const Words*>(p));
+        __builtin_memcpy(raw.v, &w, sizeof(raw.v));
+    } else {
+        raw.load(p);
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) v[e] = raw[e];
 }
