@@ -220,7 +220,7 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
 }
 
 // The list's p and g take the moments' values: 8 bits into bf16 (exactly), or (WRITE) binary32 values p, g into 8 bits.
-template <bool WRITE>
+template <bool WRITE, bool PAST>
 __global__ void __launch_bounds__(kThreads) k_moments(const Tensor* tensors, const Chunk* chunks) {
     const Chunk ch = chunks[blockIdx.x];
     const Tensor t = tensors[ch.tensor];
@@ -261,8 +261,8 @@ __global__ void __launch_bounds__(kThreads) k_moments(const Tensor* tensors, con
                 m[e] = first_of(mc >> (8 * e) & 0xff, mb);
                 v[e] = root_of(vc >> (8 * e) & 0xff, vb);
             }
-            store4(static_cast<bf16*>(t.p), at, t.n, m);
-            store4(static_cast<bf16*>(const_cast<void*>(t.g)), at, t.n, v);
+            store4<PAST>(static_cast<bf16*>(t.p), at, t.n, m);
+            store4<PAST>(static_cast<bf16*>(const_cast<void*>(t.g)), at, t.n, v);
         }
     }
 }
@@ -514,7 +514,8 @@ extern "C" int cs_moments_read(const cs_tensor_list* list, void* stream) {
     if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_BF16 || list->g_fmt != CS_FMT_BF16) return CS_EINVAL;
     if (list->chunks == 0) return CS_OK;
     const List at = list_of(list);
-    k_moments<false><<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
+    const auto kernel = past_caches(list->chunks * kChunk * 4) ? k_moments<false, true> : k_moments<false, false>;
+    kernel<<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
     return launched();
 }
 
@@ -522,6 +523,6 @@ extern "C" int cs_moments_write(const cs_tensor_list* list, void* stream) {
     if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_F32 || list->g_fmt != CS_FMT_F32) return CS_EINVAL;
     if (list->chunks == 0) return CS_OK;
     const List at = list_of(list);
-    k_moments<true><<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
+    k_moments<true, false><<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
     return launched();
 }
