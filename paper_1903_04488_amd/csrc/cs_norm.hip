@@ -221,18 +221,80 @@ k_norm(const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight, co
 constexpr int kGradBlock = 512;
 template <int TPR>
 constexpr int grad_threads() { return TPR < kGradBlock ? kGradBlock : TPR; }
-template <typename T, typename W, int TPR, int ITEMS, bool SUMS, bool PAST>
+// Gradients of weight and bias of 8 packs of columns, by a workgroup for itself: eight threads side by side in a row, the rows in
+// turn, four under way.
+template <typename T, typename W, int THREADS>
+__device__ __forceinline__ void norm_columns(int part, const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols,
+                                             const float* mean, const float* rstd, W* dweight, W* dbias) {
+    constexpr int P = kPack<T>, RT = THREADS / 8, N = 4;
+    __shared__ float sums[THREADS / 64][8][2 * P];
+    const int c = threadIdx.x & 7, first_row = threadIdx.x >> 3;
+    const int begin = (part * 8 + c) * P, at = min(begin, cols - P);
+    float dw[P] = {}, db[P] = {};
+    if (begin < cols)
+        for (int64_t row = first_row; row < rows; row += N * RT) {
+            Raw<T, P> rx[N], rd[N];
+            float mu[N], rs[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int64_t r = min(row + j * RT, rows - 1);
+                rx[j].load(x + r * x_stride + at);
+                rd[j].load(dy + r * dy_stride + at);
+                mu[j] = mean[r], rs[j] = rstd[r];
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (row + j * RT < rows)
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        dw[e] = fmaf(rd[j][e], (rx[j][e] - mu[j]) * rs[j], dw[e]);
+                        db[e] += rd[j][e];
+                    }
+        }
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+#pragma unroll
+        for (int d = 8; d < 64; d <<= 1) {
+            dw[e] += __shfl_xor(dw[e], d);
+            db[e] += __shfl_xor(db[e], d);
+        }
+        if ((threadIdx.x & 63) < 8) {
+            sums[threadIdx.x >> 6][c][e] = dw[e];
+            sums[threadIdx.x >> 6][c][P + e] = db[e];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < 8 * 2 * P) {
+        const int pack = threadIdx.x / (2 * P), e = threadIdx.x % (2 * P), from = (part * 8 + pack) * P, to = min(from, cols - P);
+        W* out = e < P ? dweight : dbias;
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < THREADS / 64; ++w) s += sums[w][pack][e];
+        if (out && from < cols && e % P >= from - to) out[to + e % P] = static_cast<W>(s);
+    }
+}
+
+// How the weights' gradients are taken: not at all; as partial sums, added up by k_norm_weights; or, of few rows, by
+// workgroups of the same launch behind the `row_blocks` that take rows.
+enum { kNoSums, kPartialSums, kOwnSums };
+template <typename T, typename W, int TPR, int ITEMS, int SUMS, bool PAST>
 __global__ void __launch_bounds__(grad_threads<TPR>())
 k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_t rows, int cols, const W* weight,
-            const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* partials) {
+            const float* mean, const float* rstd, T* dx, int64_t dx_stride, float* partials, int row_blocks, W* dweight, W* dbias) {
     constexpr int P = kPack<T>, ROWS = grad_threads<TPR>() / TPR;
+    if constexpr (SUMS == kOwnSums)
+        if (static_cast<int>(blockIdx.x) >= row_blocks) {
+            norm_columns<T, W, grad_threads<TPR>()>(blockIdx.x - row_blocks, dy, dy_stride, x, x_stride, rows, cols, mean, rstd, dweight,
+                                                    dbias);
+            return;
+        }
     __shared__ float lds[2][2][16];
     int turn = 0;
     const int t = threadIdx.x % TPR, group = threadIdx.x / TPR;
     const Slots<T, TPR, ITEMS> slot(t, cols);
     const float per = 1.0f / static_cast<float>(cols);
     float dw[ITEMS][P] = {}, db[ITEMS][P] = {};
-    const int64_t step = static_cast<int64_t>(gridDim.x) * ROWS;
+    const int64_t step = static_cast<int64_t>(row_blocks) * ROWS;
     int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS;         // of the workgroup's rows
     Raw<T, P> next_x[ITEMS], next_dy[ITEMS];
     float next_mu = 0.f, next_rs = 0.f;
@@ -265,7 +327,7 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
 #pragma unroll
             for (int e = 0; e < P; ++e) {
                 const float xh = slot.own(i, e) ? (v[i][e] - mu) * rs : 0.f, d = slot.own(i, e) ? a[i][e] : 0.f;
-                if (SUMS) {
+                if (SUMS == kPartialSums) {
                     dw[i][e] = fmaf(d, xh, dw[i][e]);
                     db[i][e] += d;
                 }
@@ -292,7 +354,7 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
             store_pack<PAST>(out + slot.at(i), a[i]);
         }
     }
-    if (!SUMS) return;
+    if (SUMS != kPartialSums) return;
     float* mine = partials + static_cast<int64_t>(blockIdx.x) * 2 * cols;
     if (ROWS == 1) {
 #pragma unroll
@@ -406,16 +468,29 @@ int norm_forward_held(const NormArgs& a) {
         static_cast<const W*>(a.bias), a.eps, static_cast<T*>(a.out), a.out_stride, a.mean, a.rstd);
     return launched();
 }
+// Few rows: the weights' gradients by workgroups of their own (the rows are read twice, the second time from the caches), in
+// the same launch where dx is not written over what they read.
+bool own_sums(const NormArgs& a) { return a.rows <= 1024 && (a.dweight || a.dbias); }
 template <typename T, typename W, int TPR, int ITEMS>
 int norm_grad_held(const NormArgs& a, int shares) {
-    const bool sums = a.dweight || a.dbias;
     const bool past = past_caches(a.rows * a.cols * sizeof(T));
-    const auto kernel = sums ? (past ? k_norm_grad<T, W, TPR, ITEMS, true, true> : k_norm_grad<T, W, TPR, ITEMS, true, false>)
-                             : (past ? k_norm_grad<T, W, TPR, ITEMS, false, true> : k_norm_grad<T, W, TPR, ITEMS, false, false>);
-    kernel<<<static_cast<unsigned>(shares), grad_threads<TPR>(), 0, a.stream>>>(
-        static_cast<const T*>(a.dy), a.dy_stride, static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols),
-        static_cast<const W*>(a.weight), a.mean, a.rstd, static_cast<T*>(a.out), a.out_stride, a.partials);
-    return launched();
+    const auto launch = [&](auto kernel, int row_blocks, int64_t more) {
+        kernel<<<static_cast<unsigned>(row_blocks + more), grad_threads<TPR>(), 0, a.stream>>>(
+            static_cast<const T*>(a.dy), a.dy_stride, static_cast<const T*>(a.x), a.x_stride, a.rows, static_cast<int>(a.cols),
+            static_cast<const W*>(a.weight), a.mean, a.rstd, static_cast<T*>(a.out), a.out_stride, a.partials, row_blocks,
+            static_cast<W*>(a.dweight), static_cast<W*>(a.dbias));
+        return launched();
+    };
+    if (own_sums(a)) {
+        const int64_t columns = (a.cols + 8 * kPack<T> - 1) / (8 * kPack<T>);
+        const bool apart = a.out != a.dy && a.out != a.x;
+        if (int rc = launch(k_norm_grad<T, W, TPR, ITEMS, kOwnSums, false>, a.out && apart ? shares : 0, columns)) return rc;
+        if (!a.out || apart) return CS_OK;
+        return launch(k_norm_grad<T, W, TPR, ITEMS, kNoSums, false>, shares, 0);
+    }
+    if (a.dweight || a.dbias)
+        return launch(past ? k_norm_grad<T, W, TPR, ITEMS, kPartialSums, true> : k_norm_grad<T, W, TPR, ITEMS, kPartialSums, false>, shares, 0);
+    return launch(past ? k_norm_grad<T, W, TPR, ITEMS, kNoSums, true> : k_norm_grad<T, W, TPR, ITEMS, kNoSums, false>, shares, 0);
 }
 #define CS_HELD(h, CALL)                                                                               \
     switch ((h).threads * 8 + (h).items) {                                                             \
@@ -491,6 +566,7 @@ int norm_backward(const NormArgs& a) {
     if (a.rows)
         if (int rc = norm_grad<T, W>(a, shares)) return rc;
     if (!a.dweight && !a.dbias) return CS_OK;
+    if (a.rows && own_sums(a) && held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16).threads) return CS_OK;
     const dim3 grid(static_cast<unsigned>((a.cols + 15) / 16), 2);
     k_norm_weights<W><<<grid, kWeightsBlock, 0, a.stream>>>(a.partials, shares, a.cols, static_cast<W*>(a.dweight),
                                                          static_cast<W*>(a.dbias));
