@@ -468,11 +468,15 @@ int norm_forward_held(const NormArgs& a) {
         static_cast<const W*>(a.bias), a.eps, static_cast<T*>(a.out), a.out_stride, a.mean, a.rstd);
     return launched();
 }
-// Few rows: the weights' gradients by workgroups of their own (the rows are read twice, the second time from the caches), in
-// the same launch where dx is not written over what they read.
-bool own_sums(const NormArgs& a) { return a.rows <= 1024 && (a.dweight || a.dbias); }
+// Few rows, or up to 2048 wide ones: the weights' gradients by workgroups of their own (the rows are read twice, the second time
+// from the caches), in the same launch where dx is not written over what they read.  Rows of more than 8192 values in 32 bits
+// always: 1024 threads have no registers for sums beside them.  (us a pass, own workgroups / partial sums: 1000 x 1024 bf16
+// 18 / 22, 1500 x 1024 bf16 26 / 21, 1500 x 4096 bf16 27 / 33, 3000 x 8192 f32 125 / 110, 6000 x 16000 f32 509 / 641.)
+bool own_sums(const NormArgs& a, const Held& h) {
+    return (a.dweight || a.dbias) && (h.threads == 1024 || a.rows <= (h.threads == 512 ? 2048 : 1024));
+}
 template <typename T, typename W, int TPR, int ITEMS>
-int norm_grad_held(const NormArgs& a, int shares) {
+int norm_grad_held(const NormArgs& a, const Held& h, int shares) {
     const bool past = past_caches(a.rows * a.cols * sizeof(T));
     const auto launch = [&](auto kernel, int row_blocks, int64_t more) {
         kernel<<<static_cast<unsigned>(row_blocks + more), grad_threads<TPR>(), 0, a.stream>>>(
@@ -481,15 +485,18 @@ int norm_grad_held(const NormArgs& a, int shares) {
             static_cast<W*>(a.dweight), static_cast<W*>(a.dbias));
         return launched();
     };
-    if (own_sums(a)) {
+    if (own_sums(a, h)) {
         const int64_t columns = (a.cols + 8 * kPack<T> - 1) / (8 * kPack<T>);
         const bool apart = a.out != a.dy && a.out != a.x;
-        if (int rc = launch(k_norm_grad<T, W, TPR, ITEMS, kOwnSums, false>, a.out && apart ? shares : 0, columns)) return rc;
+        if (int rc = launch(past ? k_norm_grad<T, W, TPR, ITEMS, kOwnSums, TPR == 1024> : k_norm_grad<T, W, TPR, ITEMS, kOwnSums, false>,
+                            a.out && apart ? shares : 0, columns))
+            return rc;
         if (!a.out || apart) return CS_OK;
-        return launch(k_norm_grad<T, W, TPR, ITEMS, kNoSums, false>, shares, 0);
+    } else if constexpr (TPR < 1024) {
+        if (a.dweight || a.dbias)
+            return launch(past ? k_norm_grad<T, W, TPR, ITEMS, kPartialSums, true> : k_norm_grad<T, W, TPR, ITEMS, kPartialSums, false>,
+                          shares, 0);
     }
-    if (a.dweight || a.dbias)
-        return launch(past ? k_norm_grad<T, W, TPR, ITEMS, kPartialSums, true> : k_norm_grad<T, W, TPR, ITEMS, kPartialSums, false>, shares, 0);
     return launch(past ? k_norm_grad<T, W, TPR, ITEMS, kNoSums, true> : k_norm_grad<T, W, TPR, ITEMS, kNoSums, false>, shares, 0);
 }
 #define CS_HELD(h, CALL)                                                                               \
@@ -541,7 +548,7 @@ int norm_grad(const NormArgs& a, int shares) {
     const T *dy = static_cast<const T*>(a.dy), *x = static_cast<const T*>(a.x);
     const Held h = held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
     if (h.threads) {
-#define CS_CALL(TPR, ITEMS) (norm_grad_held<T, W, TPR, ITEMS>(a, shares))
+#define CS_CALL(TPR, ITEMS) (norm_grad_held<T, W, TPR, ITEMS>(a, h, shares))
         if constexpr (sizeof(T) == 4)
             if (h.threads == 1024) return h.items == 3 ? CS_CALL(1024, 3) : CS_CALL(1024, 4);
         CS_HELD_GRAD(h, CS_CALL)
@@ -566,7 +573,8 @@ int norm_backward(const NormArgs& a) {
     if (a.rows)
         if (int rc = norm_grad<T, W>(a, shares)) return rc;
     if (!a.dweight && !a.dbias) return CS_OK;
-    if (a.rows && own_sums(a) && held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16).threads) return CS_OK;
+    const Held h = held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
+    if (a.rows && h.threads && own_sums(a, h)) return CS_OK;
     const dim3 grid(static_cast<unsigned>((a.cols + 15) / 16), 2);
     k_norm_weights<W><<<grid, kWeightsBlock, 0, a.stream>>>(a.partials, shares, a.cols, static_cast<W*>(a.dweight),
                                                          static_cast<W*>(a.dbias));
@@ -670,6 +678,7 @@ extern "C" int cs_layer_norm_grad(const void* dy, int64_t dy_stride, const void*
                span_in_rows(mean, 4 * rows, dx, dx_stride, rows, cols, fmt) ||
                span_in_rows(rstd, 4 * rows, dx, dx_stride, rows, cols, fmt)))
         return CS_EINVAL;
+    if (!dx && !sums) return CS_OK;
     NormArgs a = {};
     a.x = x, a.dy = dy, a.weight = weight, a.rows = rows, a.cols = cols, a.x_stride = x_stride, a.dy_stride = dy_stride;
     a.out = dx, a.out_stride = dx_stride, a.mean = const_cast<float*>(mean), a.rstd = const_cast<float*>(rstd);
