@@ -422,7 +422,9 @@ Held held(int64_t cols, int32_t fmt) {
     const int64_t p = 16 / fmt_bytes(fmt), packs = (cols + p - 1) / p;
     if (cols < p) return {0, 0};
     if (packs <= 16) return {16, 1};
-    for (const int threads : {64, 256, 512, 1024}) {
+    // (us, rows that 256 threads would hold with 2 to 4 packs each / 512 with half as many: 65536 x 1500 f32 160 / 148, 32768 x 4096
+    // bf16 117 / 115; but rows of up to 4 packs by a wavefront, not by more threads: 20000 x 1500 bf16 28 / 31)
+    for (const int threads : {64, 512, 1024}) {
         const int64_t items = (packs + threads - 1) / threads;
         if (items <= 4) return {threads, static_cast<int>(items)};
     }
@@ -506,9 +508,8 @@ int norm_grad_held(const NormArgs& a, const Held& h, int shares) {
         case 64 * 8 + 2: return CALL(64, 2);                                                           \
         case 64 * 8 + 3: return CALL(64, 3);                                                           \
         case 64 * 8 + 4: return CALL(64, 4);                                                           \
-        case 256 * 8 + 2: return CALL(256, 2);                                                         \
-        case 256 * 8 + 3: return CALL(256, 3);                                                         \
-        case 256 * 8 + 4: return CALL(256, 4);                                                         \
+        case 512 * 8 + 1: return CALL(512, 1);                                                         \
+        case 512 * 8 + 2: return CALL(512, 2);                                                         \
         case 512 * 8 + 3: return CALL(512, 3);                                                         \
         case 512 * 8 + 4: return CALL(512, 4);                                                         \
         case 1024 * 8 + 3: return CALL(1024, 3);                                                       \
