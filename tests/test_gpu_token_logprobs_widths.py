@@ -84,3 +84,14 @@ def test_calls_replayed_from_a_graph(rows, vocab, top):
         torch.cuda.synchronize()
         for a, b in zip(got, (*out, dx, *([idx, lps] if top else []))):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("vocab", [200, 3000, 40_000])
+def test_a_scale_that_takes_masked_values_out_of_range(vocab):
+    """logits of 1e-12 under a scale of 1e12, masks of -1e30, which are -inf once scaled"""
+    x, target = logits_of(5, vocab, torch.float32)
+    x.mul_(1e-12)
+    x[:, ::2] = -1e30
+    target[:] = 1
+    check_forward(x, target, 3, 1e12)
+    check_gradients(x, target, 1e12)
