@@ -950,7 +950,8 @@ class TensorList:
         sizes, need = (ctypes.c_int64 * len(n))(*n), ctypes.c_size_t()
         _check(load_library().cs_tensor_list_bytes(sizes, len(n), ctypes.byref(need)), "cs_tensor_list_bytes")
         self.device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
-        if any(t.device != self.device for tensors, _ in each.values() for t in tensors):
+        index = p[0].get_device() if p else 0
+        if any(t.get_device() != index for tensors, _ in each.values() for t in tensors):
             raise CsError("the tensors of a list must be on one GPU")
         if self.memory is None or self.memory.numel() < need.value or self.memory.device != self.device:
             self.memory = torch.empty(need.value, dtype=torch.uint8, device=self.device)

@@ -150,7 +150,11 @@ __device__ __forceinline__ void store4_codes(uint8_t* x, int64_t at, int64_t n, 
     }
 }
 
-// A wavefront takes blocks of 256 values, four a lane.
+// A wavefront takes blocks of 256 values, four a lane, so that a block's largest magnitude is a reduction of one wavefront; a workgroup
+// a chunk of 4096 values of one tensor, found in the list (all tensors in one launch: a small model is launch and latency, 4.9 us
+// for 35 tensors of 0.2 M parameters).  Bound by memory: 90 M parameters with moments in 32 bits 416 us, 2465 MB as counted at 5.9
+// TB/s; in 8 bits 212 us, 1245 MB at 5.9, and there the vector ALU is busy too (95 %: a square root and a quotient, both rounded
+// correctly, and two encodings a value).
 template <typename P, typename G, bool EIGHT, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs, const float* grad_scale) {
@@ -219,6 +223,7 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
     }
 }
 
+// Memory: 90 M parameters read back in 86 us, 540 MB at 6.3 TB/s.
 // The list's p and g take the moments' values: 8 bits into bf16 (exactly), or (WRITE) binary32 values p, g into 8 bits.
 template <bool WRITE, bool PAST>
 __global__ void __launch_bounds__(kThreads) k_moments(const Tensor* tensors, const Chunk* chunks) {
@@ -276,7 +281,8 @@ __device__ __forceinline__ double block_sum(double s, double* lds) {
 }
 
 // Squares and their sums in binary64: no overflow, and nothing lost between large and small tensors.  Workgroup w takes chunks
-// w, w + gridDim, ...; a thread's four requests of a chunk are under way together.
+// w, w + gridDim, ...; a thread's four requests of a chunk are under way together.  90 M gradients in 32 bits 59 us (360 MB at 6.1
+// TB/s), in bf16 37 (4.9).
 constexpr int kSquares = 2048;                       // workgroups, and partial sums
 template <typename G>
 __global__ void __launch_bounds__(kThreads)
