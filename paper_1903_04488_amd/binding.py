@@ -784,6 +784,9 @@ CS_ADAMW_COEFS = 8
 _FMT = {torch.bfloat16: CS_FMT_BF16, torch.float16: CS_FMT_F16, torch.float32: CS_FMT_F32}
 
 
+# Small calls wait for the host, and a call for rows checks up to nine tensors.  Those below see in one expression that all of them
+# are plain (contiguous, on the GPU, of the sizes and types that are wanted) and take the addresses as they are; anything else, strided
+# rows or a mistake, goes the longer way, which names it (norm of 1 x 512: 3.3 us of checks in a call, 2.2 with this).
 def _rows(t, name: str, like=None):
     """(address, row stride) of a 2-d tensor whose rows are contiguous; of the shape and type of `like`"""
     # (a call for one token waits for the host: what is fine is seen first)
@@ -825,23 +828,45 @@ def _maybe(t, dtype, name: str, numel: int):
     return _address(t, dtype, name, numel)
 
 
-def _weights(weight, bias, x):
-    """(address, address, format) of what scales and shifts a norm's columns"""
-    dtype = weight.dtype if weight is not None else bias.dtype if bias is not None else torch.float32
+def _weights_dtype(x, *given):
+    """the type of a norm's weights: that of the rows, or float32"""
+    dtype = torch.float32
+    for w in reversed([w for w in given if w is not None]):
+        if not isinstance(w, torch.Tensor):
+            raise CsError("weight and bias must be tensors on the GPU")
+        dtype = w.dtype
     if dtype is not x.dtype and dtype is not torch.float32:
         raise CsError(f"weight and bias must have dtype {x.dtype} or float32, got {dtype}")
-    cols = x.size(1)
-    return _maybe(weight, dtype, "weight", cols), _maybe(bias, dtype, "bias", cols), _FMT[dtype]
+    return dtype
 
 
 def cs_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5):
     """x, y: [rows, cols], contiguous rows; weight, bias: [cols] or None; mean, rstd: [rows] float32 or both None"""
+    f32 = torch.float32
+    try:
+        rows, cols = x.shape
+        dt, wt = x.dtype, weight.dtype
+        if (x.is_contiguous() and x.is_cuda and dt in _FMT and cols and y.dtype is dt and y.is_contiguous() and y.is_cuda
+                and y.shape == x.shape and (wt is dt or wt is f32) and weight.is_contiguous() and weight.is_cuda
+                and weight.numel() == cols and bias.dtype is wt and bias.is_contiguous() and bias.is_cuda and bias.numel() == cols
+                and (mean is None if rstd is None else
+                     mean.dtype is f32 and mean.is_contiguous() and mean.is_cuda and mean.numel() == rows
+                     and rstd.dtype is f32 and rstd.is_contiguous() and rstd.is_cuda and rstd.numel() == rows)):
+            status = (_lib or load_library()).cs_layer_norm(
+                x.data_ptr(), rows, cols, cols, _FMT[dt], weight.data_ptr(), bias.data_ptr(), _FMT[wt], eps, y.data_ptr(), cols,
+                None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), _stream(x))
+            if status:
+                _check(status, "cs_layer_norm")
+            return
+    except (AttributeError, ValueError):
+        pass
     at, step = _rows(x, "x")
     out, out_step = _rows(y, "y", x)
     rows, cols = x.shape
-    w, b, w_fmt = _weights(weight, bias, x)
+    dtype = _weights_dtype(x, weight, bias)
     _check(load_library().cs_layer_norm(
-        at, rows, cols, step, _FMT[x.dtype], w, b, w_fmt, eps, out, out_step, _maybe(mean, torch.float32, "mean", rows),
+        at, rows, cols, step, _FMT[x.dtype], _maybe(weight, dtype, "weight", cols), _maybe(bias, dtype, "bias", cols), _FMT[dtype],
+        eps, out, out_step, _maybe(mean, torch.float32, "mean", rows),
         _maybe(rstd, torch.float32, "rstd", rows), _stream(x)), "cs_layer_norm")
 
 
@@ -853,13 +878,33 @@ def cs_layer_norm_grad_workspace_bytes(rows: int, cols: int) -> int:
 
 def cs_layer_norm_grad(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace):
     """dx, dweight, dbias: each may be None (workspace too, without the last two)"""
+    f32 = torch.float32
+    try:
+        rows, cols = x.shape
+        dt, wt = x.dtype, weight.dtype
+        if (x.is_contiguous() and x.is_cuda and dt in _FMT and cols and (wt is dt or wt is f32)
+                and dy.dtype is dt and dy.is_contiguous() and dy.is_cuda and dy.shape == x.shape
+                and dx.dtype is dt and dx.is_contiguous() and dx.is_cuda and dx.shape == x.shape
+                and weight.is_contiguous() and weight.is_cuda and weight.numel() == cols
+                and dweight.dtype is wt and dweight.is_contiguous() and dweight.is_cuda and dweight.numel() == cols
+                and dbias.dtype is wt and dbias.is_contiguous() and dbias.is_cuda and dbias.numel() == cols
+                and mean.dtype is f32 and mean.is_contiguous() and mean.is_cuda and mean.numel() == rows
+                and rstd.dtype is f32 and rstd.is_contiguous() and rstd.is_cuda and rstd.numel() == rows
+                and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
+            status = (_lib or load_library()).cs_layer_norm_grad(
+                dy.data_ptr(), cols, x.data_ptr(), cols, rows, cols, _FMT[dt], weight.data_ptr(), _FMT[wt], mean.data_ptr(),
+                rstd.data_ptr(), dx.data_ptr(), cols, dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(),
+                workspace.numel(), _stream(x))
+            if status:
+                _check(status, "cs_layer_norm_grad")
+            return
+    except (AttributeError, ValueError):
+        pass
     at, step = _rows(x, "x")
     d, d_step = _rows(dy, "dy", x)
     out, out_step = _rows(dx, "dx", x) if dx is not None else (None, 0)
     rows, cols = x.shape
-    dtype = next((w.dtype for w in (weight, dweight, dbias) if w is not None), torch.float32)
-    if dtype is not x.dtype and dtype is not torch.float32:
-        raise CsError(f"weights must have dtype {x.dtype} or float32, got {dtype}")
+    dtype = _weights_dtype(x, weight, dweight, dbias)
     _check(load_library().cs_layer_norm_grad(
         d, d_step, at, step, rows, cols, _FMT[x.dtype], _maybe(weight, dtype, "weight", cols), _FMT[dtype],
         _dev(mean, torch.float32, "mean", rows), _dev(rstd, torch.float32, "rstd", rows), out, out_step,
@@ -877,11 +922,34 @@ def cs_token_workspace_bytes(rows: int, vocab: int, top: int = 0) -> int:
 def cs_token_logprobs(logits, target, logp, entropy, lse, top_idx, top_logp, workspace, scale: float = 1.0):
     """logits: [rows, vocab]; target: [rows] int64; logp, entropy, lse: [rows] float32; top_idx, top_logp: [rows, top] int64
     and float32.  None where it is not wanted."""
+    f32, i64 = torch.float32, torch.int64
+    try:
+        rows, vocab = logits.shape
+        dt = logits.dtype
+        top = 0 if top_idx is None and top_logp is None else top_idx.shape[1]
+        if (logits.is_contiguous() and logits.is_cuda and dt in _FMT and vocab
+                and target.dtype is i64 and target.is_contiguous() and target.is_cuda and target.numel() == rows
+                and logp.dtype is f32 and logp.is_contiguous() and logp.is_cuda and logp.numel() == rows
+                and entropy.dtype is f32 and entropy.is_contiguous() and entropy.is_cuda and entropy.numel() == rows
+                and lse.dtype is f32 and lse.is_contiguous() and lse.is_cuda and lse.numel() == rows
+                and (not top or (top_idx.dtype is i64 and top_idx.is_contiguous() and top_idx.is_cuda
+                                 and top_logp.dtype is f32 and top_logp.is_contiguous() and top_logp.is_cuda
+                                 and top_idx.shape == top_logp.shape == (rows, top)))
+                and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
+            status = (_lib or load_library()).cs_token_logprobs(
+                logits.data_ptr(), rows, vocab, vocab, _FMT[dt], scale, target.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
+                lse.data_ptr(), top, top_idx.data_ptr() if top else None, top_logp.data_ptr() if top else None,
+                workspace.data_ptr(), workspace.numel(), _stream(logits))
+            if status:
+                _check(status, "cs_token_logprobs")
+            return
+    except (AttributeError, ValueError, IndexError):
+        pass
     at, step = _rows(logits, "logits")
     rows, vocab = logits.shape
     top = 0
     if top_idx is not None or top_logp is not None:
-        if top_idx is None or top_logp is None or top_idx.shape != top_logp.shape or top_idx.dim() != 2 or len(top_idx) != rows:
+        if not isinstance(top_idx, torch.Tensor) or not isinstance(top_logp, torch.Tensor) or top_idx.shape != top_logp.shape or top_idx.dim() != 2 or len(top_idx) != rows:
             raise CsError(f"top_idx and top_logp must be [{rows}, top] both")
         top = top_idx.shape[1]
     f32 = torch.float32
@@ -894,6 +962,26 @@ def cs_token_logprobs(logits, target, logp, entropy, lse, top_idx, top_logp, wor
 
 
 def cs_token_logprobs_grad(logits, target, lse, entropy, g_logp, g_entropy, dlogits, scale: float = 1.0):
+    f32 = torch.float32
+    try:
+        rows, vocab = logits.shape
+        dt = logits.dtype
+        if (logits.is_contiguous() and logits.is_cuda and dt in _FMT and vocab
+                and dlogits.dtype is dt and dlogits.is_contiguous() and dlogits.is_cuda and dlogits.shape == logits.shape
+                and target.dtype is torch.int64 and target.is_contiguous() and target.is_cuda and target.numel() == rows
+                and lse.dtype is f32 and lse.is_contiguous() and lse.is_cuda and lse.numel() == rows
+                and entropy.dtype is f32 and entropy.is_contiguous() and entropy.is_cuda and entropy.numel() == rows
+                and g_logp.dtype is f32 and g_logp.is_contiguous() and g_logp.is_cuda and g_logp.numel() == rows
+                and (g_entropy is None or (g_entropy.dtype is f32 and g_entropy.is_contiguous() and g_entropy.is_cuda
+                                           and g_entropy.numel() == rows))):
+            status = (_lib or load_library()).cs_token_logprobs_grad(
+                logits.data_ptr(), rows, vocab, vocab, _FMT[dt], scale, target.data_ptr(), lse.data_ptr(), entropy.data_ptr(),
+                g_logp.data_ptr(), None if g_entropy is None else g_entropy.data_ptr(), dlogits.data_ptr(), vocab, _stream(logits))
+            if status:
+                _check(status, "cs_token_logprobs_grad")
+            return
+    except (AttributeError, ValueError):
+        pass
     at, step = _rows(logits, "logits")
     out, out_step = _rows(dlogits, "dlogits", logits)
     rows, vocab = logits.shape
@@ -905,6 +993,29 @@ def cs_token_logprobs_grad(logits, target, lse, entropy, g_logp, g_entropy, dlog
 
 
 def cs_token_loss(logits, target, g_logp, g_entropy, logp, entropy, lse, dlogits, workspace, scale: float = 1.0):
+    f32 = torch.float32
+    try:
+        rows, vocab = logits.shape
+        dt = logits.dtype
+        if (logits.is_contiguous() and logits.is_cuda and dt in _FMT and vocab
+                and dlogits.dtype is dt and dlogits.is_contiguous() and dlogits.is_cuda and dlogits.shape == logits.shape
+                and target.dtype is torch.int64 and target.is_contiguous() and target.is_cuda and target.numel() == rows
+                and logp.dtype is f32 and logp.is_contiguous() and logp.is_cuda and logp.numel() == rows
+                and lse.dtype is f32 and lse.is_contiguous() and lse.is_cuda and lse.numel() == rows
+                and entropy.dtype is f32 and entropy.is_contiguous() and entropy.is_cuda and entropy.numel() == rows
+                and g_logp.dtype is f32 and g_logp.is_contiguous() and g_logp.is_cuda and g_logp.numel() == rows
+                and (g_entropy is None or (g_entropy.dtype is f32 and g_entropy.is_contiguous() and g_entropy.is_cuda
+                                           and g_entropy.numel() == rows))
+                and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
+            status = (_lib or load_library()).cs_token_loss(
+                logits.data_ptr(), rows, vocab, vocab, _FMT[dt], scale, target.data_ptr(), g_logp.data_ptr(),
+                None if g_entropy is None else g_entropy.data_ptr(), logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
+                dlogits.data_ptr(), vocab, workspace.data_ptr(), workspace.numel(), _stream(logits))
+            if status:
+                _check(status, "cs_token_loss")
+            return
+    except (AttributeError, ValueError):
+        pass
     at, step = _rows(logits, "logits")
     out, out_step = _rows(dlogits, "dlogits", logits)
     rows, vocab = logits.shape
