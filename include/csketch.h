@@ -580,8 +580,8 @@ int cs_token_loss(const void* logits, int64_t rows, int64_t vocab, int64_t strid
 
 /* Many tensors, for one launch over all of them.  cs_tensor_list_build writes `count` tensors' addresses and lengths into
  * `memory` (device, cs_tensor_list_bytes, 8-byte aligned) and fills *list (host), which is handed to the calls below.  Both are
- * the caller's; the list holds while the tensors stay where they are, and is built again (a few small launches) when they
- * move.  n, p, g, m, v, m_exp, v_exp: HOST arrays of `count` lengths (>= 0) and device pointers; the build has read them when it
+ * the caller's; the list holds while the tensors stay where they are, and is built again (a few small launches, behind the
+ * calls that still read `memory`) when they move.  n, p, g, m, v, m_exp, v_exp: HOST arrays of `count` lengths (>= 0) and device pointers; the build has read them when it
  * returns.
  *   p: parameters, p_fmt.  g: gradients, g_fmt.
  *   m, v, bits = 32: first and second moments, float.

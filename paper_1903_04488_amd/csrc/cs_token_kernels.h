@@ -341,7 +341,8 @@ __device__ __forceinline__ void largest_of_part(const T* row, const Row& held, i
                 float t = ranked(v[0]);
 #pragma unroll
                 for (int e = 1; e < P; ++e) t = fmaxf(t, v[e]);
-                if (static_cast<int32_t>(order_of(t) ^ 0x80000000u) >> LOW < bound) return;
+                const int32_t o = static_cast<int32_t>(order_of(t) ^ 0x80000000u) >> LOW;
+                if (o < bound || (o == bound && at_pack > bound_pack)) return;
                 const int32_t slot = atomicAdd(&sh.chosen_n, 1);
                 if (slot >= HITS) return;
                 sh.hit_pack[slot] = at_pack;
