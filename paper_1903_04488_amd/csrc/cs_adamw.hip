@@ -152,12 +152,12 @@ __device__ __forceinline__ void store4_codes(uint8_t* x, int64_t at, int64_t n, 
 
 // A wavefront takes blocks of 256 values, four a lane, so that a block's largest magnitude is a reduction of one wavefront; a workgroup
 // a chunk of 4096 values of one tensor, found in the list (all tensors in one launch: a small model is launch and latency, 4.9 us
-// for 35 tensors of 0.2 M parameters).  Bound by memory: 90 M parameters with moments in 32 bits 416 us, 2465 MB as counted at 5.9
+// for 35 tensors of 0.2 M parameters).  Bound by memory: 90 M parameters with moments in 32 bits 394 us, 2465 MB as counted at 6.3
 // TB/s; in 8 bits 212 us, 1245 MB at 5.9, and there the vector ALU is busy too (95 %: a square root and a quotient, both rounded
 // correctly, and two encodings a value).
 template <typename P, typename G, bool EIGHT, bool PAST>
 __global__ void __launch_bounds__(kThreads)
-k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs, const float* grad_scale) {
+k_adamw(const Tensor* tensors, const Chunk* chunks, int split, Coefs c, const Coefs* coefs, const float* grad_scale) {
     float scale = 1.f;
     if (grad_scale) {
         scale = *grad_scale;
@@ -165,11 +165,12 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
     }
     if (coefs) c = *coefs;
     // (from the last chunk down: the gradients' norm has just read them upwards, and the caches hold the end of them)
-    const Chunk ch = chunks[gridDim.x - 1 - blockIdx.x];
+    const unsigned place = gridDim.x - 1 - blockIdx.x;
+    const Chunk ch = chunks[place / split];
     const Tensor t = tensors[ch.tensor];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, each = kChunk / kBlock8 / split, from = place % split * each;
     const int64_t begin = static_cast<int64_t>(ch.part) * kChunk;
-    for (int k = wave; k < kChunk / kBlock8; k += kThreads / 64) {
+    for (int k = from + wave; k < from + each; k += kThreads / 64) {
         const int64_t block = begin + k * kBlock8, at = block + lane * 4;
         if (block >= t.n) return;                     // (the whole wavefront)
         float p[4], g[4], m[4], v[4], root[4];
@@ -226,12 +227,12 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, Coefs c, const Coefs* coefs,
 // Memory: 90 M parameters read back in 86 us, 540 MB at 6.3 TB/s.
 // The list's p and g take the moments' values: 8 bits into bf16 (exactly), or (WRITE) binary32 values p, g into 8 bits.
 template <bool WRITE, bool PAST>
-__global__ void __launch_bounds__(kThreads) k_moments(const Tensor* tensors, const Chunk* chunks) {
-    const Chunk ch = chunks[blockIdx.x];
+__global__ void __launch_bounds__(kThreads) k_moments(const Tensor* tensors, const Chunk* chunks, int split) {
+    const Chunk ch = chunks[blockIdx.x / split];
     const Tensor t = tensors[ch.tensor];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, each = kChunk / kBlock8 / split, from = blockIdx.x % split * each;
     const int64_t begin = static_cast<int64_t>(ch.part) * kChunk;
-    for (int k = wave; k < kChunk / kBlock8; k += kThreads / 64) {
+    for (int k = from + wave; k < from + each; k += kThreads / 64) {
         const int64_t block = begin + k * kBlock8, at = block + lane * 4;
         if (block >= t.n) return;
         float m[4], v[4];
@@ -349,7 +350,9 @@ static_assert(sizeof(Coefs) == 4 * CS_ADAMW_COEFS, "csketch.h");
 // ---------------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------------
-constexpr int64_t kMaxValues = static_cast<int64_t>(1) << 40;
+// Chunks from which moments are read back by one workgroup a chunk (52 M, 8 bits: 212 us a pass, with four 226).
+constexpr int64_t kReadWhole = 8192;
+constexpr int64_t kMaxValues = static_cast<int64_t>(1) << 40, kMaxChunks = static_cast<int64_t>(1) << 24;   // (2^32 threads a launch)
 
 int64_t chunks_of(const int64_t* n, int32_t count, bool& ok) {
     int64_t chunks = 0, values = 0;
@@ -373,22 +376,28 @@ List list_of(const cs_tensor_list* l) {
     const Tensor* t = static_cast<const Tensor*>(l->memory);
     return List{t, reinterpret_cast<const Chunk*>(t + l->count)};
 }
+// Workgroups that share a chunk: four, a block of 256 values a wavefront, so that none waits for memory four times in a row; but of
+// moments in 8 bits that go past the caches one (us a step, one / four: 0.64 M parameters, 8 bits 15.1 / 12.0; 11.5 M, 32 bits 69 / 63;
+// 90 M, 32 bits with clipping 474 / 461; 30 M, 8 bits 141 / 132; 52 M, 8 bits, past the caches 212 / 234).
+// A launch has fewer than 2^32 threads: a list of 2^22 chunks or more is not split.
+int split_of(int64_t chunks, bool one) { return one || chunks * 4 >= kMaxChunks ? 1 : 4; }
 int partials_of(const cs_tensor_list* l) { return static_cast<int>(l->chunks < kSquares ? l->chunks : kSquares); }
 bool list_ok(const cs_tensor_list* l) {
-    return l && l->count >= 0 && l->chunks >= 0 && l->chunks < (static_cast<int64_t>(1) << 31) && (l->chunks == 0 || l->memory);
+    return l && l->count >= 0 && l->chunks >= 0 && l->chunks < kMaxChunks && (l->chunks == 0 || l->memory);
 }
 
 template <typename P, typename G>
 int adamw(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
     const List at = list_of(l);
-    const unsigned grid = static_cast<unsigned>(l->chunks);
     // Parameters and moments that the memory-side cache cannot keep are read and written past it: what it keeps is
     // the gradients that their norm has just read.
     const int64_t each = fmt_bytes(l->p_fmt) + (l->bits == 8 ? 2 : 8);
     const bool past = past_caches(l->chunks * kChunk * each);
+    const int split = split_of(l->chunks, past && l->bits == 8);
+    const unsigned grid = static_cast<unsigned>(l->chunks * split);
     const auto kernel = l->bits == 8 ? (past ? k_adamw<P, G, true, true> : k_adamw<P, G, true, false>)
                                      : (past ? k_adamw<P, G, false, true> : k_adamw<P, G, false, false>);
-    kernel<<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, c, coefs, grad_scale);
+    kernel<<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, split, c, coefs, grad_scale);
     return launched();
 }
 template <typename P>
@@ -412,7 +421,7 @@ extern "C" int cs_tensor_list_bytes(const int64_t* n, int32_t count, size_t* byt
     bool ok = false;
     if (count < 0 || (count && !n) || !bytes) return CS_EINVAL;
     const int64_t chunks = chunks_of(n, count, ok);
-    if (!ok || chunks >= (static_cast<int64_t>(1) << 31)) return CS_EINVAL;
+    if (!ok || chunks >= kMaxChunks) return CS_EINVAL;
     *bytes = static_cast<size_t>(count) * sizeof(Tensor) + static_cast<size_t>(chunks) * sizeof(Chunk);
     return CS_OK;
 }
@@ -520,8 +529,10 @@ extern "C" int cs_moments_read(const cs_tensor_list* list, void* stream) {
     if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_BF16 || list->g_fmt != CS_FMT_BF16) return CS_EINVAL;
     if (list->chunks == 0) return CS_OK;
     const List at = list_of(list);
-    const auto kernel = past_caches(list->chunks * kChunk * 4) ? k_moments<false, true> : k_moments<false, false>;
-    kernel<<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
+    const bool past = past_caches(list->chunks * kChunk * 4);
+    const auto kernel = past ? k_moments<false, true> : k_moments<false, false>;
+    const int split = split_of(list->chunks, list->chunks >= kReadWhole);
+    kernel<<<static_cast<unsigned>(list->chunks * split), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks, split);
     return launched();
 }
 
@@ -529,6 +540,7 @@ extern "C" int cs_moments_write(const cs_tensor_list* list, void* stream) {
     if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_F32 || list->g_fmt != CS_FMT_F32) return CS_EINVAL;
     if (list->chunks == 0) return CS_OK;
     const List at = list_of(list);
-    k_moments<true, false><<<static_cast<unsigned>(list->chunks), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks);
+    const int split = split_of(list->chunks, false);
+    k_moments<true, false><<<static_cast<unsigned>(list->chunks * split), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks, split);
     return launched();
 }
