@@ -552,7 +552,7 @@ int cs_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x, int64_t
 /* Log probabilities of given tokens under rows of logits.  With z = scale x (scale > 0 and finite, 1 / temperature):
  *     lse = ln sum_v exp z_v,  logp = z_target - lse,  entropy = -sum_v p_v ln p_v,  p_v = exp(z_v - lse)
  * and the `top` tokens with the largest logits, largest first, equal ones lower index first, with their log probabilities.
- * logits: device, 1 <= vocab <= 2^30, rows <= 2^24.  target: device int64[rows]; one outside [0, vocab) leaves its row
+ * logits: device, 1 <= vocab <= 2^30, rows < 2^24.  target: device int64[rows]; one outside [0, vocab) leaves its row
  * out (logp 0).  logp, entropy, lse: device float[rows], each may be NULL (target too, with logp).  0 <= top <= min(vocab,
  * CS_TOKEN_MAX_TOP); top_idx, top_logp: device int64 / float[rows][top].
  * A logit of -inf is a token that cannot be.  A row of nothing else is empty: lse and every log probability are -inf, the

@@ -29,7 +29,8 @@ struct TokenOut {
     float* top_logp;
 };
 
-constexpr int64_t kTokenMaxVocab = static_cast<int64_t>(1) << 30, kTokenMaxRows = static_cast<int64_t>(1) << 24;
+constexpr int64_t kTokenMaxVocab = static_cast<int64_t>(1) << 30;
+constexpr int64_t kTokenMaxRows = (static_cast<int64_t>(1) << 24) - 1;   // (a launch has fewer than 2^32 threads)
 
 inline bool token_ok(int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale) {
     return rows_ok(rows, vocab, stride, fmt) && vocab <= kTokenMaxVocab && rows <= kTokenMaxRows && scale > 0.f && scale < INFINITY;

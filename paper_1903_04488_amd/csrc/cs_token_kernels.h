@@ -880,7 +880,7 @@ int token_forward(const TokenArgs& a) {
 template <typename T>
 int token_grad(const TokenArgs& a) {
     const int32_t packs = packs_of(a.vocab, a.fmt);
-    const int64_t most = ((static_cast<int64_t>(1) << 31) - 1) / a.rows;
+    const int64_t most = kTokenMaxRows / a.rows;
     int64_t pieces = (packs + 4 * kThreads - 1) / (4 * kThreads);
     if (pieces > most) pieces = most;
     const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_grad<T, true> : k_token_grad<T, false>;

@@ -95,3 +95,31 @@ def test_a_scale_that_takes_masked_values_out_of_range(vocab):
     target[:] = 1
     check_forward(x, target, 3, 1e12)
     check_gradients(x, target, 1e12)
+
+
+def test_the_most_rows_of_a_call():
+    """2^24 - 1 short rows, a workgroup each in the gradient: the same bits as the few rows they repeat"""
+    rows, some, vocab = (1 << 24) - 1, 4096, 3
+    x, target = logits_of(some, vocab, torch.bfloat16)
+
+    def run(x, target):
+        n = x.shape[0]
+        ws = torch.empty(max(cs.cs_token_workspace_bytes(n, vocab, 2), cs.cs_token_workspace_bytes(n, vocab, 0)), dtype=torch.uint8, device=DEV)
+        v = [torch.empty(n, device=DEV) for _ in range(6)]
+        top_idx, top_logp = torch.empty(n, 2, dtype=torch.int64, device=DEV), torch.empty(n, 2, device=DEV)
+        dx, both = torch.empty_like(x), torch.empty_like(x)
+        g = torch.full((n,), 0.5, device=DEV)
+        cs.cs_token_logprobs(x, target, v[0], v[1], v[2], top_idx, top_logp, ws)
+        cs.cs_token_logprobs_grad(x, target, v[2], v[1], g, g, dx)
+        cs.cs_token_loss(x, target, g, g, v[3], v[4], v[5], both, ws)
+        return v + [top_idx, top_logp, dx, both]
+
+    few = run(x, target)
+    times = rows // some + 1
+    many = run(x.repeat(times, 1)[:rows].contiguous(), target.repeat(times)[:rows].contiguous())
+    whole = rows // some * some
+    bits = {torch.float32: torch.int32, torch.bfloat16: torch.int16, torch.int64: torch.int64}
+    for a, b in zip(few, many):
+        a, b = a.view(bits[a.dtype]), b.view(bits[b.dtype])
+        assert bool((b[:whole].reshape(-1, *a.shape) == a).all())
+        assert torch.equal(b[whole:], a[:rows - whole])

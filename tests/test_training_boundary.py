@@ -171,3 +171,13 @@ def test_binding_refuses_cpu_tensors(lib):
                  lambda: AdamW([x], [x.clone()]), lambda: LayerNorm(w, w, 3).forward(x)):
         with pytest.raises(cs.CsError):
             call()
+
+
+def test_what_a_launch_has_no_threads_for(lib):
+    """a workgroup of 256 for a row of logits or 4096 parameters, and fewer than 2^32 threads"""
+    n = ctypes.c_size_t()
+    assert lib.cs_token_workspace_bytes((1 << 24) - 1, 3, 0, ctypes.byref(n)) == OK
+    assert lib.cs_token_workspace_bytes(1 << 24, 3, 0, ctypes.byref(n)) == EINVAL
+    assert token(lib, rows=1 << 24) == EINVAL
+    assert lib.cs_tensor_list_bytes((ctypes.c_int64 * 1)((1 << 36) - 4096), 1, ctypes.byref(n)) == OK
+    assert lib.cs_tensor_list_bytes((ctypes.c_int64 * 1)(1 << 36), 1, ctypes.byref(n)) == EINVAL
