@@ -785,8 +785,9 @@ _FMT = {torch.bfloat16: CS_FMT_BF16, torch.float16: CS_FMT_F16, torch.float32: C
 
 
 # Small calls wait for the host, and a call for rows checks up to nine tensors.  Those below see in one expression that all of them
-# are plain (contiguous, on the GPU, of the sizes and types that are wanted) and take the addresses as they are; anything else, strided
-# rows or a mistake, goes the longer way, which names it (norm of 1 x 512: 3.3 us of checks in a call, 2.2 with this).
+# are as they should be (on the GPU, of the sizes and types that are wanted, rows contiguous at any distance) and take the addresses
+# as they are; anything else goes the longer way, which names what is wrong (norm of 1 x 512: 3.3 us of checks in a call, 2.2 with this;
+# forward and backward of strided rows 31 x 20: 20.2 us a pass when strides went the longer way, 15 now).
 def _rows(t, name: str, like=None):
     """(address, row stride) of a 2-d tensor whose rows are contiguous; of the shape and type of `like`"""
     # (a call for one token waits for the host: what is fine is seen first)
@@ -845,20 +846,21 @@ def cs_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5):
     f32 = torch.float32
     try:
         rows, cols = x.shape
+        (step, one), (out_step, out_one) = x.stride(), y.stride()
         dt, wt = x.dtype, weight.dtype
-        if (x.is_contiguous() and x.is_cuda and dt in _FMT and cols and y.dtype is dt and y.is_contiguous() and y.is_cuda
+        if (one == out_one == 1 and step >= cols <= out_step and x.is_cuda and dt in _FMT and cols and y.dtype is dt and y.is_cuda
                 and y.shape == x.shape and (wt is dt or wt is f32) and weight.is_contiguous() and weight.is_cuda
                 and weight.numel() == cols and bias.dtype is wt and bias.is_contiguous() and bias.is_cuda and bias.numel() == cols
                 and (mean is None if rstd is None else
                      mean.dtype is f32 and mean.is_contiguous() and mean.is_cuda and mean.numel() == rows
                      and rstd.dtype is f32 and rstd.is_contiguous() and rstd.is_cuda and rstd.numel() == rows)):
             status = (_lib or load_library()).cs_layer_norm(
-                x.data_ptr(), rows, cols, cols, _FMT[dt], weight.data_ptr(), bias.data_ptr(), _FMT[wt], eps, y.data_ptr(), cols,
+                x.data_ptr(), rows, cols, step, _FMT[dt], weight.data_ptr(), bias.data_ptr(), _FMT[wt], eps, y.data_ptr(), out_step,
                 None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), _stream(x))
             if status:
                 _check(status, "cs_layer_norm")
             return
-    except (AttributeError, ValueError):
+    except (AttributeError, ValueError, TypeError):
         pass
     at, step = _rows(x, "x")
     out, out_step = _rows(y, "y", x)
@@ -881,10 +883,12 @@ def cs_layer_norm_grad(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
     f32 = torch.float32
     try:
         rows, cols = x.shape
+        (step, one), (d_step, d_one), (out_step, out_one) = x.stride(), dy.stride(), dx.stride()
         dt, wt = x.dtype, weight.dtype
-        if (x.is_contiguous() and x.is_cuda and dt in _FMT and cols and (wt is dt or wt is f32)
-                and dy.dtype is dt and dy.is_contiguous() and dy.is_cuda and dy.shape == x.shape
-                and dx.dtype is dt and dx.is_contiguous() and dx.is_cuda and dx.shape == x.shape
+        if (one == d_one == out_one == 1 and step >= cols and d_step >= cols <= out_step
+                and x.is_cuda and dt in _FMT and cols and (wt is dt or wt is f32)
+                and dy.dtype is dt and dy.is_cuda and dy.shape == x.shape
+                and dx.dtype is dt and dx.is_cuda and dx.shape == x.shape
                 and weight.is_contiguous() and weight.is_cuda and weight.numel() == cols
                 and dweight.dtype is wt and dweight.is_contiguous() and dweight.is_cuda and dweight.numel() == cols
                 and dbias.dtype is wt and dbias.is_contiguous() and dbias.is_cuda and dbias.numel() == cols
@@ -892,13 +896,13 @@ def cs_layer_norm_grad(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
                 and rstd.dtype is f32 and rstd.is_contiguous() and rstd.is_cuda and rstd.numel() == rows
                 and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
             status = (_lib or load_library()).cs_layer_norm_grad(
-                dy.data_ptr(), cols, x.data_ptr(), cols, rows, cols, _FMT[dt], weight.data_ptr(), _FMT[wt], mean.data_ptr(),
-                rstd.data_ptr(), dx.data_ptr(), cols, dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(),
+                dy.data_ptr(), d_step, x.data_ptr(), step, rows, cols, _FMT[dt], weight.data_ptr(), _FMT[wt], mean.data_ptr(),
+                rstd.data_ptr(), dx.data_ptr(), out_step, dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(),
                 workspace.numel(), _stream(x))
             if status:
                 _check(status, "cs_layer_norm_grad")
             return
-    except (AttributeError, ValueError):
+    except (AttributeError, ValueError, TypeError):
         pass
     at, step = _rows(x, "x")
     d, d_step = _rows(dy, "dy", x)
@@ -925,9 +929,10 @@ def cs_token_logprobs(logits, target, logp, entropy, lse, top_idx, top_logp, wor
     f32, i64 = torch.float32, torch.int64
     try:
         rows, vocab = logits.shape
+        step, one = logits.stride()
         dt = logits.dtype
         top = 0 if top_idx is None and top_logp is None else top_idx.shape[1]
-        if (logits.is_contiguous() and logits.is_cuda and dt in _FMT and vocab
+        if (one == 1 and step >= vocab and logits.is_cuda and dt in _FMT and vocab
                 and target.dtype is i64 and target.is_contiguous() and target.is_cuda and target.numel() == rows
                 and logp.dtype is f32 and logp.is_contiguous() and logp.is_cuda and logp.numel() == rows
                 and entropy.dtype is f32 and entropy.is_contiguous() and entropy.is_cuda and entropy.numel() == rows
@@ -937,13 +942,13 @@ def cs_token_logprobs(logits, target, logp, entropy, lse, top_idx, top_logp, wor
                                  and top_idx.shape == top_logp.shape == (rows, top)))
                 and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
             status = (_lib or load_library()).cs_token_logprobs(
-                logits.data_ptr(), rows, vocab, vocab, _FMT[dt], scale, target.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
+                logits.data_ptr(), rows, vocab, step, _FMT[dt], scale, target.data_ptr(), logp.data_ptr(), entropy.data_ptr(),
                 lse.data_ptr(), top, top_idx.data_ptr() if top else None, top_logp.data_ptr() if top else None,
                 workspace.data_ptr(), workspace.numel(), _stream(logits))
             if status:
                 _check(status, "cs_token_logprobs")
             return
-    except (AttributeError, ValueError, IndexError):
+    except (AttributeError, ValueError, IndexError, TypeError):
         pass
     at, step = _rows(logits, "logits")
     rows, vocab = logits.shape
@@ -965,9 +970,10 @@ def cs_token_logprobs_grad(logits, target, lse, entropy, g_logp, g_entropy, dlog
     f32 = torch.float32
     try:
         rows, vocab = logits.shape
+        (step, one), (out_step, out_one) = logits.stride(), dlogits.stride()
         dt = logits.dtype
-        if (logits.is_contiguous() and logits.is_cuda and dt in _FMT and vocab
-                and dlogits.dtype is dt and dlogits.is_contiguous() and dlogits.is_cuda and dlogits.shape == logits.shape
+        if (one == out_one == 1 and step >= vocab <= out_step and logits.is_cuda and dt in _FMT and vocab
+                and dlogits.dtype is dt and dlogits.is_cuda and dlogits.shape == logits.shape
                 and target.dtype is torch.int64 and target.is_contiguous() and target.is_cuda and target.numel() == rows
                 and lse.dtype is f32 and lse.is_contiguous() and lse.is_cuda and lse.numel() == rows
                 and entropy.dtype is f32 and entropy.is_contiguous() and entropy.is_cuda and entropy.numel() == rows
@@ -975,12 +981,12 @@ def cs_token_logprobs_grad(logits, target, lse, entropy, g_logp, g_entropy, dlog
                 and (g_entropy is None or (g_entropy.dtype is f32 and g_entropy.is_contiguous() and g_entropy.is_cuda
                                            and g_entropy.numel() == rows))):
             status = (_lib or load_library()).cs_token_logprobs_grad(
-                logits.data_ptr(), rows, vocab, vocab, _FMT[dt], scale, target.data_ptr(), lse.data_ptr(), entropy.data_ptr(),
-                g_logp.data_ptr(), None if g_entropy is None else g_entropy.data_ptr(), dlogits.data_ptr(), vocab, _stream(logits))
+                logits.data_ptr(), rows, vocab, step, _FMT[dt], scale, target.data_ptr(), lse.data_ptr(), entropy.data_ptr(),
+                g_logp.data_ptr(), None if g_entropy is None else g_entropy.data_ptr(), dlogits.data_ptr(), out_step, _stream(logits))
             if status:
                 _check(status, "cs_token_logprobs_grad")
             return
-    except (AttributeError, ValueError):
+    except (AttributeError, ValueError, TypeError):
         pass
     at, step = _rows(logits, "logits")
     out, out_step = _rows(dlogits, "dlogits", logits)
@@ -996,9 +1002,10 @@ def cs_token_loss(logits, target, g_logp, g_entropy, logp, entropy, lse, dlogits
     f32 = torch.float32
     try:
         rows, vocab = logits.shape
+        (step, one), (out_step, out_one) = logits.stride(), dlogits.stride()
         dt = logits.dtype
-        if (logits.is_contiguous() and logits.is_cuda and dt in _FMT and vocab
-                and dlogits.dtype is dt and dlogits.is_contiguous() and dlogits.is_cuda and dlogits.shape == logits.shape
+        if (one == out_one == 1 and step >= vocab <= out_step and logits.is_cuda and dt in _FMT and vocab
+                and dlogits.dtype is dt and dlogits.is_cuda and dlogits.shape == logits.shape
                 and target.dtype is torch.int64 and target.is_contiguous() and target.is_cuda and target.numel() == rows
                 and logp.dtype is f32 and logp.is_contiguous() and logp.is_cuda and logp.numel() == rows
                 and lse.dtype is f32 and lse.is_contiguous() and lse.is_cuda and lse.numel() == rows
@@ -1008,13 +1015,13 @@ def cs_token_loss(logits, target, g_logp, g_entropy, logp, entropy, lse, dlogits
                                            and g_entropy.numel() == rows))
                 and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
             status = (_lib or load_library()).cs_token_loss(
-                logits.data_ptr(), rows, vocab, vocab, _FMT[dt], scale, target.data_ptr(), g_logp.data_ptr(),
+                logits.data_ptr(), rows, vocab, step, _FMT[dt], scale, target.data_ptr(), g_logp.data_ptr(),
                 None if g_entropy is None else g_entropy.data_ptr(), logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(),
-                dlogits.data_ptr(), vocab, workspace.data_ptr(), workspace.numel(), _stream(logits))
+                dlogits.data_ptr(), out_step, workspace.data_ptr(), workspace.numel(), _stream(logits))
             if status:
                 _check(status, "cs_token_loss")
             return
-    except (AttributeError, ValueError):
+    except (AttributeError, ValueError, TypeError):
         pass
     at, step = _rows(logits, "logits")
     out, out_step = _rows(dlogits, "dlogits", logits)
