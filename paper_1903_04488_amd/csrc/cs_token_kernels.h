@@ -219,9 +219,10 @@ __device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_
     r.S = s * g;
     r.U = g * fmaf(-off, s, u);
     // Where the reference or a product leaves binary32 (values beyond 2e38: masks of the type's lowest value in a row that has
-    // nothing else; a scale beyond 1e8) and where the row holds a NaN or +inf, once more with differences of the values themselves.  (The largest
-    // value adds 1 to S.)
-    if (!(r.S >= 0.5f && r.S < INFINITY && fabsf(r.U) < INFINITY) && r.m > -INFINITY) {
+    // nothing else; a scale beyond 1e8), where the row holds a NaN or +inf, and where the reference is that large (2^22) that it may be
+    // more than 1/4 from the largest value's product (U would be a small difference of large numbers), once more with differences of the
+    // values themselves.  (The largest value adds 1 to S.)
+    if (!(r.S >= 0.5f && r.S < INFINITY && fabsf(r.U) < INFINITY && fabsf(off) <= 0.25f) && r.m > -INFINITY) {
         row_sync<THREADS>();
         s = u = 0.f;
         const int64_t end = static_cast<int64_t>(last) * P < vocab ? static_cast<int64_t>(last) * P : vocab;
