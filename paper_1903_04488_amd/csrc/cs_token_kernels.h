@@ -535,9 +535,11 @@ k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const 
 }
 
 // Gradient of a row's values: p (a + b max(l, far)), with what scale, g, h, entropy and the target make of a and b.
-//   from a log of p: l = x mul - add = ln p, p = 2^(l log2(e)):           a = -scale (g + h H),               b = -scale h
-//   from the sums:   l = x mul - add = log2 p + log2 s, p = 2^l / s:      a = -scale (g + h (H - ln s)) / s,  b = -scale h ln2 / s
+//   kLogs, from a log of p:   l = x mul - add = ln p, p = 2^(l log2(e)):       a = -scale (g + h H),               b = -scale h
+//   kSums, from the sums:     l = x mul - add = log2 p + log2 s, p = 2^l / s:  a = -scale (g + h (H - ln s)) / s,  b = -scale h ln2 / s
+//   kDiffs, from differences: l = (x - add) mul = ln p + ln S, p = e^l / S:    a = -scale (g + h (H - ln S)) / S,  b = -scale h / S
 // (a value with no probability has p = 0, l = -inf and the gradient 0).  The target's value has hot = scale g more.
+enum { kLogs, kSums, kDiffs };
 struct RowGrad {
     float mul, add, a, b, hot;
     int32_t target;                  // -1: none
@@ -551,20 +553,20 @@ struct RowGrad {
         a = -hot;
         b = g_entropy ? -scale * g_entropy[row] : 0.f;
     }
-    // LOGS: l is ln p; ENTROPY: b is not 0
-    template <bool LOGS, bool ENTROPY>
+    // ENTROPY: b is not 0
+    template <int FROM, bool ENTROPY>
     __device__ __forceinline__ float of(float x) const {
-        const float l = fmaf(x, mul, -add), p = exp2_of(LOGS ? l * kLog2e : l);
+        const float l = FROM == kDiffs ? (x - add) * mul : fmaf(x, mul, -add), p = exp2_of(FROM == kSums ? l : l * kLog2e);
         return ENTROPY ? p * fmaf(fmaxf(l, kFar), b, a) : p * a;
     }
 };
 
 // pack q of a row with the values v
-template <bool PAST, bool LOGS, bool ENTROPY, typename T, int P>
+template <bool PAST, int FROM, bool ENTROPY, typename T, int P>
 __device__ __forceinline__ void grad_pack(float (&v)[P], T* dx, int32_t vocab, int32_t q, const RowGrad& row) {
     const int32_t at = q * P;
 #pragma unroll
-    for (int e = 0; e < P; ++e) v[e] = row.template of<LOGS, ENTROPY>(v[e]);
+    for (int e = 0; e < P; ++e) v[e] = row.template of<FROM, ENTROPY>(v[e]);
     // (none: -1 lies in no pack)
     if (static_cast<uint32_t>(row.target - at) < static_cast<uint32_t>(P))
 #pragma unroll
@@ -582,7 +584,7 @@ __device__ __forceinline__ void grad_pack(float (&v)[P], T* dx, int32_t vocab, i
 }
 
 // packs [first, last) of a row
-template <bool PAST, bool LOGS, bool ENTROPY, int THREADS, typename T>
+template <bool PAST, int FROM, bool ENTROPY, int THREADS, typename T>
 __device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int32_t first, int32_t last, const RowGrad& row) {
     constexpr int P = kPack<T>;
     for (int32_t q = first + static_cast<int32_t>(threadIdx.x); q < last; q += THREADS) {
@@ -590,7 +592,7 @@ __device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int
         float v[P];
         if (at + P <= vocab) load_pack<T, P>(x + at, v);
         else load_tail(x, at, vocab, v);
-        grad_pack<PAST, LOGS, ENTROPY>(v, dx, static_cast<int32_t>(vocab), q, row);
+        grad_pack<PAST, FROM, ENTROPY>(v, dx, static_cast<int32_t>(vocab), q, row);
     }
 }
 
@@ -611,23 +613,26 @@ k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     r.empty = r.add == -INFINITY;
     if (g_entropy) {
         r.a = fmaf(r.b, entropy[row], r.a);
-        grad_packs<PAST, true, true, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
+        grad_packs<PAST, kLogs, true, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
     } else {
-        grad_packs<PAST, true, false, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
+        grad_packs<PAST, kLogs, false, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
     }
 }
 
 // What a row's gradient is computed from, with its sums at hand: relative to a binary32 number next to m k, for which s is S
-// but for what that is off; where m k leaves binary32 (or there is no m), from the logarithms.  True: the former.
+// but for what that is off; where m k is 2^22 or more, so that it may be off by more than 1/4 (and s, a power of 2 of that, out of range
+// soon), from differences to m itself: finite masks in a row that has nothing else, logits with a large offset.  True: the former.
 __device__ __forceinline__ bool grad_from_sums(RowGrad& g, const Sums& r, float log_sum, float scale) {
     const float H = log_sum - kLn2 * (r.U / r.S);
     g.empty = r.m == -INFINITY && r.S == r.S;
     g.mul = scale * kLog2e;
     g.add = r.m * g.mul;
-    if (!(fabsf(g.add) < INFINITY)) {
+    if (!(fabsf(g.add) < 4194304.f)) {
+        const float one = 1.f / r.S;
         g.mul = scale;
-        g.add = fmaf(r.m, scale, log_sum);
-        g.a = fmaf(g.b, H, g.a);
+        g.add = r.m;
+        g.a = one * fmaf(g.b, H - log_sum, g.a);
+        g.b *= one;
         return false;
     }
     const float s = r.S * exp2_of(fmaf(r.m, g.mul, -g.add)), one = 1.f / s;
@@ -711,14 +716,14 @@ struct HeldRow {
     }
 };
 
-template <bool PAST, bool LOGS, bool ENTROPY, int THREADS, int ITEMS, typename T>
+template <bool PAST, int FROM, bool ENTROPY, int THREADS, int ITEMS, typename T>
 __device__ __forceinline__ void grad_held(const HeldRow<T, THREADS, ITEMS>& held, T* dx, int32_t vocab, const RowGrad& row) {
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
         if (held.has(i)) {
             float v[kPack<T>];
             held.values(i, v);
-            grad_pack<PAST, LOGS, ENTROPY>(v, dx, vocab, held.pack(i), row);
+            grad_pack<PAST, FROM, ENTROPY>(v, dx, vocab, held.pack(i), row);
         }
 }
 
@@ -778,9 +783,9 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
         T* dx = dlogits + row * d_stride;
         RowGrad g;
         g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
-        if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, true, true, THREADS, ITEMS>(held, dx, vocab, g);
-        else if (g_entropy) grad_held<PAST, false, true, THREADS, ITEMS>(held, dx, vocab, g);
-        else grad_held<PAST, false, false, THREADS, ITEMS>(held, dx, vocab, g);
+        if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, kDiffs, true, THREADS, ITEMS>(held, dx, vocab, g);
+        else if (g_entropy) grad_held<PAST, kSums, true, THREADS, ITEMS>(held, dx, vocab, g);
+        else grad_held<PAST, kSums, false, THREADS, ITEMS>(held, dx, vocab, g);
     }
 }
 
@@ -806,9 +811,9 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
     RowGrad g;
     g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
-    if (!grad_from_sums(g, r, log_sum, scale)) grad_packs<PAST, true, true, kThreads>(x, dx, vocab, 0, packs, g);
-    else if (g_entropy) grad_packs<PAST, false, true, kThreads>(x, dx, vocab, 0, packs, g);
-    else grad_packs<PAST, false, false, kThreads>(x, dx, vocab, 0, packs, g);
+    if (!grad_from_sums(g, r, log_sum, scale)) grad_packs<PAST, kDiffs, true, kThreads>(x, dx, vocab, 0, packs, g);
+    else if (g_entropy) grad_packs<PAST, kSums, true, kThreads>(x, dx, vocab, 0, packs, g);
+    else grad_packs<PAST, kSums, false, kThreads>(x, dx, vocab, 0, packs, g);
 }
 
 // ---------------------------------------------------------------------------------------
