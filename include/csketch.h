@@ -556,7 +556,7 @@ int cs_layer_norm_grad(const void* dy, int64_t dy_stride, const void* x, int64_t
  * out (logp 0).  logp, entropy, lse: device float[rows], each may be NULL (target too, with logp).  0 <= top <= min(vocab,
  * CS_TOKEN_MAX_TOP); top_idx, top_logp: device int64 / float[rows][top].
  * A logit of -inf is a token that cannot be.  A row of nothing else is empty: lse and every log probability are -inf, the
- * entropy is 0, the alternatives are 0, 1, ...  A NaN or +inf makes its row's lse, logp and entropy NaN; as an
+ * entropy is 0, the alternatives are 0, 1, ...  (Of other rows an lse below binary32 is its lowest number.)  A NaN or +inf makes its row's lse, logp and entropy NaN; as an
  * alternative a NaN ranks with -inf.
  * workspace: device, cs_token_workspace_bytes(rows, vocab, top), 8-byte aligned (may be NULL where that is 0). */
 #define CS_TOKEN_MAX_TOP 64
@@ -568,7 +568,8 @@ int cs_token_logprobs(const void* logits, int64_t rows, int64_t vocab, int64_t s
  *     dlogits_v = scale (g_logp ([v = target] - p_v) - g_entropy p_v (ln p_v + entropy))
  * lse, entropy: what cs_token_logprobs gave for these logits and this scale.  g_logp (with target), g_entropy (with
  * entropy): device float[rows], each may be NULL (0).  dlogits: type of the logits; may be the logits (same stride).
- * Rows without a target have no g_logp; an empty row's gradient is 0. */
+ * Rows without a target have no g_logp; an empty row's gradient is 0.  p is exp(z - lse), so it is off by 2^-24 |lse|; a row
+ * whose |lse| is 256 or more is summed again by one workgroup, and its p is as exact as cs_token_loss's. */
 int cs_token_logprobs_grad(const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale,
                            const int64_t* target, const float* lse, const float* entropy, const float* g_logp,
                            const float* g_entropy, void* dlogits, int64_t d_stride, void* stream);

@@ -440,7 +440,11 @@ template <typename T>
 __device__ __forceinline__ void row_results(int64_t row, const Target<T>& target, float scale, const Sums& r, float log_sum,
                                             const TokenOut& out) {
     const bool empty = r.m == -INFINITY && r.S == r.S;
-    if (out.lse) out.lse[row] = empty ? -INFINITY : fmaf(r.m, scale, log_sum);
+    if (out.lse) {
+        // (-inf says that a row is empty: a number below binary32 is the lowest there is)
+        const float lse = fmaf(r.m, scale, log_sum);
+        out.lse[row] = empty ? -INFINITY : lse < -FLT_MAX ? -FLT_MAX : lse;
+    }
     if (out.entropy) out.entropy[row] = empty ? 0.f : log_sum - kLn2 * (r.U / r.S);
     if (out.logp) out.logp[row] = target.counts ? logp_of(target.x, r, log_sum, scale) : 0.f;
 }
@@ -561,6 +565,33 @@ struct RowGrad {
     }
 };
 
+// A row's gradient from its sums and differences to its largest value.
+__device__ __forceinline__ void grad_from_diffs(RowGrad& g, const Sums& r, float log_sum, float scale) {
+    const float H = log_sum - kLn2 * (r.U / r.S), one = 1.f / r.S;
+    g.empty = r.m == -INFINITY && r.S == r.S;
+    g.mul = scale;
+    g.add = r.m;
+    g.a = one * fmaf(g.b, H - log_sum, g.a);
+    g.b *= one;
+}
+
+// What a row's gradient is computed from, with its sums at hand: relative to a binary32 number next to m k, for which s is S
+// but for what that is off; where m k is 2^22 or more, so that it may be off by more than 1/4 (and s, a power of 2 of that, out of range
+// soon), from differences to m itself: finite masks in a row that has nothing else, logits with a large offset.  True: the former.
+__device__ __forceinline__ bool grad_from_sums(RowGrad& g, const Sums& r, float log_sum, float scale) {
+    g.mul = scale * kLog2e;
+    g.add = r.m * g.mul;
+    if (!(fabsf(g.add) < 4194304.f)) {
+        grad_from_diffs(g, r, log_sum, scale);
+        return false;
+    }
+    const float H = log_sum - kLn2 * (r.U / r.S), s = r.S * exp2_of(fmaf(r.m, g.mul, -g.add)), one = 1.f / s;
+    g.empty = r.m == -INFINITY && r.S == r.S;
+    g.a = one * fmaf(g.b, H - logf(s), g.a);
+    g.b *= one * kLn2;
+    return true;
+}
+
 // pack q of a row with the values v
 template <bool PAST, int FROM, bool ENTROPY, typename T, int P>
 __device__ __forceinline__ void grad_pack(float (&v)[P], T* dx, int32_t vocab, int32_t q, const RowGrad& row) {
@@ -596,6 +627,26 @@ __device__ __forceinline__ void grad_packs(const T* x, T* dx, int64_t vocab, int
     }
 }
 
+// A row's sums by a workgroup, a value at a time.
+template <typename T>
+__device__ __forceinline__ Sums sums_of_row(const T* x, int64_t vocab, float scale, float (&buf)[3][16]) {
+    Sums r = {-INFINITY, 0.f, 0.f};
+    for (int64_t i = threadIdx.x; i < vocab; i += kThreads) r.m = fmaxf(r.m, static_cast<float>(x[i]));
+    r.m = block_max<kThreads>(r.m, buf[0]);
+    for (int64_t i = threadIdx.x; i < vocab; i += kThreads) {
+        const float d = (static_cast<float>(x[i]) - r.m) * scale * kLog2e, e = exp2_of(d);
+        r.S += e;
+        r.U = fmaf(e, fmaxf(d, kFar), r.U);
+    }
+    block_add2<kThreads>(r.S, r.U, buf[1], buf[2]);
+    return r;
+}
+
+// From here on a row's gradient is not taken from its lse, which in binary32 is off by up to 2^-24 of itself, and so is every p: up to here
+// 1.5e-5 of p, but 1e-3 at 3e4 and all of it in a row of a finite mask alone.  The row's first workgroup sums it again and writes all of
+// it, the others leave it alone (dlogits may be the logits).
+constexpr float kFarLse = 256.f;
+
 // The gradient that is asked for later: a pass over the logits, four packs a thread, many workgroups a row.  4096 x 32001 f32
 // in 187 us, 1049 MB at 5.6 TB/s (a copy: 4.8): memory.
 template <typename T, bool PAST>
@@ -604,41 +655,27 @@ k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const 
              const float* entropy, const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int pieces,
              int32_t packs) {
     const int64_t row = blockIdx.x / static_cast<unsigned>(pieces);
-    const int32_t each = (packs + pieces - 1) / pieces;
-    const int32_t first = min(each * static_cast<int32_t>(blockIdx.x % static_cast<unsigned>(pieces)), packs);
+    const int32_t each = (packs + pieces - 1) / pieces, piece = static_cast<int32_t>(blockIdx.x % static_cast<unsigned>(pieces));
+    const int32_t first = min(each * piece, packs);
     RowGrad r;
     r.coefficients(row, vocab, scale, target ? target[row] : -1, g_logp, g_entropy);
     r.mul = scale;
     r.add = lse[row];
     r.empty = r.add == -INFINITY;
+    if (fabsf(r.add) >= kFarLse && !r.empty) {
+        __shared__ float buf[3][16];
+        if (piece) return;
+        const Sums sums = sums_of_row(logits + row * stride, vocab, scale, buf);
+        grad_from_diffs(r, sums, logf(sums.S), scale);
+        grad_packs<PAST, kDiffs, true, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, 0, packs, r);
+        return;
+    }
     if (g_entropy) {
         r.a = fmaf(r.b, entropy[row], r.a);
         grad_packs<PAST, kLogs, true, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
     } else {
         grad_packs<PAST, kLogs, false, kThreads>(logits + row * stride, dlogits + row * d_stride, vocab, first, min(first + each, packs), r);
     }
-}
-
-// What a row's gradient is computed from, with its sums at hand: relative to a binary32 number next to m k, for which s is S
-// but for what that is off; where m k is 2^22 or more, so that it may be off by more than 1/4 (and s, a power of 2 of that, out of range
-// soon), from differences to m itself: finite masks in a row that has nothing else, logits with a large offset.  True: the former.
-__device__ __forceinline__ bool grad_from_sums(RowGrad& g, const Sums& r, float log_sum, float scale) {
-    const float H = log_sum - kLn2 * (r.U / r.S);
-    g.empty = r.m == -INFINITY && r.S == r.S;
-    g.mul = scale * kLog2e;
-    g.add = r.m * g.mul;
-    if (!(fabsf(g.add) < 4194304.f)) {
-        const float one = 1.f / r.S;
-        g.mul = scale;
-        g.add = r.m;
-        g.a = one * fmaf(g.b, H - log_sum, g.a);
-        g.b *= one;
-        return false;
-    }
-    const float s = r.S * exp2_of(fmaf(r.m, g.mul, -g.add)), one = 1.f / s;
-    g.a = one * fmaf(g.b, H - logf(s), g.a);
-    g.b *= one * kLn2;
-    return true;
 }
 
 enum { kForward, kAlternatives, kLoss };
