@@ -204,7 +204,7 @@ __device__ __forceinline__ void scan_packs(const T* row, int64_t vocab, int32_t 
 
 // the sums of all threads
 template <typename T, bool TOP, int THREADS>
-__device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_t first, int32_t last, float k,
+__device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_t first, int32_t last, float scale, float k,
                                              TokenShared<THREADS>& sh, const Scan<T, TOP>& scan) {
     constexpr int P = kPack<T>;
     Sums r;
@@ -221,13 +221,13 @@ __device__ __forceinline__ Sums join_threads(const T* row, int64_t vocab, int32_
     // Where the reference or a product leaves binary32 (values beyond 2e38: masks of the type's lowest value in a row that has
     // nothing else; a scale beyond 1e8), where the row holds a NaN or +inf, and where the reference is that large (2^22) that it may be
     // more than 1/4 from the largest value's product (U would be a small difference of large numbers), once more with differences of the
-    // values themselves.  (The largest value adds 1 to S.)
+    // values themselves (and the scale itself, as k may be infinite).  (The largest value adds 1 to S.)
     if (!(r.S >= 0.5f && r.S < INFINITY && fabsf(r.U) < INFINITY && fabsf(off) <= 0.25f) && r.m > -INFINITY) {
         row_sync<THREADS>();
         s = u = 0.f;
         const int64_t end = static_cast<int64_t>(last) * P < vocab ? static_cast<int64_t>(last) * P : vocab;
         for (int64_t i = static_cast<int64_t>(first) * P + thread_of_row<THREADS>(); i < end; i += THREADS) {
-            const float d = (static_cast<float>(row[i]) - r.m) * k, x = exp2_of(d);
+            const float d = (static_cast<float>(row[i]) - r.m) * scale * kLog2e, x = exp2_of(d);
             s += x;
             u = fmaf(x, fmaxf(d, kFar), u);
         }
@@ -468,7 +468,7 @@ k_token(const T* logits, int64_t vocab, int64_t stride, float scale, const int64
     scan_packs<T, TOP, THREADS>(x, vocab, first, last, k, scan);
     Target<T> hit;
     hit.load(x, vocab, t);
-    const Sums r = join_threads<T, TOP, THREADS>(x, vocab, first, last, k, sh, scan);
+    const Sums r = join_threads<T, TOP, THREADS>(x, vocab, first, last, scale, k, sh, scan);
     const float log_sum = logf(r.S);
     const int64_t at = row * parts + part;
     if (results) row_results(row, hit, scale, r, log_sum, out);
@@ -494,7 +494,6 @@ k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     __shared__ uint64_t list[TOP ? kMaxParts * kMaxTop : 1];
     __shared__ int32_t n;
     const int64_t row = blockIdx.x;
-    const float k = scale * kLog2e;
     const int lane = threadIdx.x & 63;
     // every wavefront joins the sums for itself: a part a lane
     Sums p = {-INFINITY, 0.f, 0.f};
@@ -511,7 +510,7 @@ k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     hit.load(logits + row * stride, vocab, t);
     Sums r;
     r.m = wave_max(p.m);
-    const float d = p.m == r.m ? 0.f : (p.m - r.m) * k, f = exp2_of(d);
+    const float d = p.m == r.m ? 0.f : (p.m - r.m) * scale * kLog2e, f = exp2_of(d);
     r.S = wave_sum(p.S * f);
     r.U = wave_sum(f * fmaf(p.S, fmaxf(d, kFar), p.U));
     const float log_sum = logf(r.S);
@@ -799,7 +798,7 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
     hit.load(x, vocab, t);
     Scan<T, MODE == kAlternatives> scan;
     held.scan(scan, k);
-    const Sums r = join_threads<T, MODE == kAlternatives, THREADS>(x, vocab, 0, packs, k, sh, scan);
+    const Sums r = join_threads<T, MODE == kAlternatives, THREADS>(x, vocab, 0, packs, scale, k, sh, scan);
     const float log_sum = logf(r.S);
     if (thread_of_row<THREADS>() == 0) {
         if (results) row_results(row, hit, scale, r, log_sum, out);
@@ -842,7 +841,7 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     scan_packs<T, false, kThreads>(x, vocab, 0, packs, k, scan);
     Target<T> hit;
     hit.load(x, vocab, t);
-    const Sums r = join_threads<T, false, kThreads>(x, vocab, 0, packs, k, sh, scan);
+    const Sums r = join_threads<T, false, kThreads>(x, vocab, 0, packs, scale, k, sh, scan);
     const float log_sum = logf(r.S);
     if (threadIdx.x == 0) row_results(row, hit, scale, r, log_sum, out);
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
