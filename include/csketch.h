@@ -616,14 +616,22 @@ int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* 
  *     p = p (1 - lr weight_decay) - lr c1 (m / (sqrt(v) c2 + eps)),  c1 = 1 / (1 - beta1^step),  c2 = 1 / sqrt(1 - beta2^step)
  * in binary32, every operation rounded by itself in this order (constants in binary64, rounded once); p takes the
  * moments as they are before they are rounded to 8 bits.  s: 1, or *grad_scale_or_null (device: clipping, loss scale); where
- * that is not finite nothing is written.
- * coefs_or_null: device float[CS_ADAMW_COEFS] that cs_adamw_advance filled, in place of step and of what h says (for steps
- * that are replayed from a graph): it counts *step up (device int64) and takes lr from *lr_or_null (device double) if given. */
+ * that is not finite nothing is written.  Such a step is none, and the next one's number is the same.
+ * coefs_or_null: device float[CS_ADAMW_COEFS], in place of step and of what h says, where the number of the step lives on the GPU (steps
+ * that are replayed from a graph; steps that are not taken where their scale is not finite, which the host does not see).  They are
+ * filled by one of
+ *   cs_adamw_advance          counts *step up (device int64) and takes lr from *lr_or_null (device double) if given
+ *   cs_adamw_advance_scaled   the same, but where *grad_scale_or_null is not finite it leaves *step and coefs alone
+ *   cs_grad_norm_advance      cs_grad_norm and, with its out[1] as the scale, the latter, in the launches of the former */
 #define CS_ADAMW_COEFS 8
 typedef struct cs_adamw {
     double lr, beta1, beta2, eps, weight_decay;      /* all finite and >= 0, betas below 1 */
 } cs_adamw;
 int cs_adamw_advance(const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream);
+int cs_adamw_advance_scaled(const cs_adamw* h, int64_t* step, const double* lr_or_null, const float* grad_scale_or_null, float* coefs,
+                            void* stream);
+int cs_grad_norm_advance(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, const cs_adamw* h,
+                         int64_t* step, const double* lr_or_null, float* coefs, void* stream);
 int cs_adamw_step(const cs_adamw* h, int64_t step, const cs_tensor_list* list, const float* coefs_or_null,
                   const float* grad_scale_or_null, void* stream);
 /* Moments in 8 bits out of and into a list whose p stands for the first moment's values and g for the root's:

@@ -233,6 +233,9 @@ _SIGNATURES = {
     "cs_grad_norm": [ctypes.POINTER(CsTensorList), ctypes.c_double, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                      ctypes.c_void_p],
     "cs_adamw_advance": [ctypes.POINTER(CsAdamw), *[ctypes.c_void_p] * 4],
+    "cs_adamw_advance_scaled": [ctypes.POINTER(CsAdamw), *[ctypes.c_void_p] * 5],
+    "cs_grad_norm_advance": [ctypes.POINTER(CsTensorList), ctypes.c_double, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                             ctypes.POINTER(CsAdamw), *[ctypes.c_void_p] * 4],
     "cs_adamw_step": [ctypes.POINTER(CsAdamw), ctypes.c_int64, ctypes.POINTER(CsTensorList), *[ctypes.c_void_p] * 3],
     "cs_moments_read": [ctypes.POINTER(CsTensorList), ctypes.c_void_p],
     "cs_moments_write": [ctypes.POINTER(CsTensorList), ctypes.c_void_p],
@@ -1092,11 +1095,21 @@ def cs_grad_norm(tensors: TensorList, max_norm: float, out, workspace):
         workspace.numel(), _stream(tensors.memory)), "cs_grad_norm")
 
 
-def cs_adamw_advance(h: CsAdamw, step, coefs, lr=None):
-    """step: int64 tensor of one value, counted up; lr: float64 tensor of one value, or None for h.lr"""
-    _check(load_library().cs_adamw_advance(
+def cs_adamw_advance(h: CsAdamw, step, coefs, lr=None, grad_scale=None):
+    """step: int64 tensor of one value, counted up; lr: float64 tensor of one value, or None for h.lr; grad_scale: float32 tensor of one
+    value, nothing is done where it is not finite (cs_adamw_advance_scaled)"""
+    _check(load_library().cs_adamw_advance_scaled(
         ctypes.byref(h), _dev(step, torch.int64, "step", 1), _maybe(lr, torch.float64, "lr", 1),
-        _dev(coefs, torch.float32, "coefs", CS_ADAMW_COEFS), _stream(step)), "cs_adamw_advance")
+        _maybe(grad_scale, torch.float32, "grad_scale", 1), _dev(coefs, torch.float32, "coefs", CS_ADAMW_COEFS), _stream(step)),
+        "cs_adamw_advance")
+
+
+def cs_grad_norm_advance(tensors: TensorList, max_norm: float, out, workspace, h: CsAdamw, step, coefs, lr=None):
+    """cs_grad_norm, and cs_adamw_advance where the norm is finite"""
+    _check(load_library().cs_grad_norm_advance(
+        ctypes.byref(tensors.c), max_norm, _dev(out, torch.float32, "out", 2), _dev(workspace, torch.uint8, "workspace"),
+        workspace.numel(), ctypes.byref(h), _dev(step, torch.int64, "step", 1), _maybe(lr, torch.float64, "lr", 1),
+        _dev(coefs, torch.float32, "coefs", CS_ADAMW_COEFS), _stream(tensors.memory)), "cs_grad_norm_advance")
 
 
 def cs_adamw_step(h: CsAdamw, step: int, tensors: TensorList, coefs=None, grad_scale=None):

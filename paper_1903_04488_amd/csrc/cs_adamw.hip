@@ -95,6 +95,21 @@ __device__ __forceinline__ int32_t exponent_of(int32_t most_bits) { return max(m
 struct Coefs {
     float b1, one_b1, b2, one_b2, keep, c2, rate, eps;
 };
+// b^t by squaring: products alone, so that the host and the GPU give the same bits
+__host__ __device__ __forceinline__ double power(double b, int64_t t) {
+#pragma clang fp contract(off)
+    double r = 1.;
+    for (; t; t >>= 1, b *= b)
+        if (t & 1) r *= b;
+    return r;
+}
+__host__ __device__ __forceinline__ Coefs coefs_of(const cs_adamw& h, double lr, int64_t t) {
+#pragma clang fp contract(off)
+    const double c1 = 1. / (1. - power(h.beta1, t)), c2 = 1. / sqrt(1. - power(h.beta2, t));
+    return Coefs{static_cast<float>(h.beta1), static_cast<float>(1. - h.beta1), static_cast<float>(h.beta2),
+                 static_cast<float>(1. - h.beta2), static_cast<float>(1. - lr * h.weight_decay), static_cast<float>(c2),
+                 static_cast<float>(lr * c1), static_cast<float>(h.eps)};
+}
 
 struct Moved {
     float p, m, v, root;
@@ -319,8 +334,19 @@ k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double
     s = block_sum(s, lds);
     if (threadIdx.x == 0) partials[blockIdx.x] = s;
 }
-__global__ void __launch_bounds__(kThreads) k_grad_norm(const double* partials, int count, double max_norm, float* out) {
+// ADVANCE: and the step that a norm that is finite lets be taken is counted, and its coefficients written, by a thread that has made
+// them while the others wait for memory.
+template <bool ADVANCE>
+__global__ void __launch_bounds__(kThreads)
+k_grad_norm(const double* partials, int count, double max_norm, float* out, cs_adamw h, int64_t* step, const double* lr, Coefs* coefs) {
     __shared__ double lds[4];
+    constexpr int kCounts = 64;                       // (of another wavefront than the one that writes the norm)
+    int64_t t = 0;
+    Coefs now = {};
+    if (ADVANCE && threadIdx.x == kCounts) {
+        t = *step + 1;
+        now = coefs_of(h, lr ? *lr : h.lr, t);
+    }
     double v[kSquares / kThreads], s = 0.;
 #pragma unroll
     for (int k = 0; k < kSquares / kThreads; ++k) {
@@ -330,20 +356,20 @@ __global__ void __launch_bounds__(kThreads) k_grad_norm(const double* partials, 
 #pragma unroll
     for (int k = 0; k < kSquares / kThreads; ++k) s += v[k];
     s = block_sum(s, lds);
-    if (threadIdx.x) return;
     const double norm = sqrt(s), c = max_norm / (norm + 1e-6);
+    if (ADVANCE && threadIdx.x == kCounts && norm < INFINITY) {
+        *step = t;
+        *coefs = now;
+    }
+    if (threadIdx.x) return;
     out[0] = static_cast<float>(norm);
     out[1] = norm < INFINITY ? static_cast<float>(c < 1. ? c : 1.) : NAN;
 }
 
-__global__ void k_adamw_coefs(cs_adamw h, int64_t* step, const double* lr, Coefs* out) {
+__global__ void k_adamw_coefs(cs_adamw h, int64_t* step, const double* lr, const float* grad_scale, Coefs* out) {
+    if (grad_scale && !(fabsf(*grad_scale) < INFINITY)) return;
     const int64_t t = ++*step;
-    const double rate = lr ? *lr : h.lr;
-    const double c1 = 1. / (1. - pow(h.beta1, static_cast<double>(t)));
-    const double c2 = 1. / sqrt(1. - pow(h.beta2, static_cast<double>(t)));
-    *out = Coefs{static_cast<float>(h.beta1), static_cast<float>(1. - h.beta1), static_cast<float>(h.beta2),
-                 static_cast<float>(1. - h.beta2), static_cast<float>(1. - rate * h.weight_decay), static_cast<float>(c2),
-                 static_cast<float>(rate * c1), static_cast<float>(h.eps)};
+    *out = coefs_of(h, lr ? *lr : h.lr, t);
 }
 static_assert(sizeof(Coefs) == 4 * CS_ADAMW_COEFS, "csketch.h");
 
@@ -479,7 +505,11 @@ extern "C" int cs_grad_norm_workspace_bytes(const cs_tensor_list* list, size_t* 
     return CS_OK;
 }
 
-extern "C" int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, void* stream) {
+namespace cs {
+namespace {
+
+int grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, const cs_adamw* h,
+              int64_t* step, const double* lr, float* coefs, void* stream) {
     if (!list_ok(list) || !out || !(max_norm > 0.)) return CS_EINVAL;
     const size_t need = static_cast<size_t>(partials_of(list)) * sizeof(double);
     if (ws_bytes < need) return CS_EWORKSPACE;
@@ -496,28 +526,46 @@ extern "C" int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* 
         kernel<<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, list->chunks, partials);
         if (int rc = launched()) return rc;
     }
-    k_grad_norm<<<1, kThreads, 0, s>>>(partials, grid, max_norm, out);
+    if (step) k_grad_norm<true><<<1, kThreads, 0, s>>>(partials, grid, max_norm, out, *h, step, lr, reinterpret_cast<Coefs*>(coefs));
+    else k_grad_norm<false><<<1, kThreads, 0, s>>>(partials, grid, max_norm, out, cs_adamw{}, nullptr, nullptr, nullptr);
+    return launched();
+}
+
+}  // namespace
+}  // namespace cs
+
+extern "C" int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, void* stream) {
+    return grad_norm(list, max_norm, out, workspace, ws_bytes, nullptr, nullptr, nullptr, nullptr, stream);
+}
+
+extern "C" int cs_grad_norm_advance(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes,
+                                    const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream) {
+    if (!hyper_ok(h) || !step || !coefs) return CS_EINVAL;
+    const Span written[] = {{out, 8}, {step, 8}, {coefs, 4 * CS_ADAMW_COEFS}, {workspace, static_cast<int64_t>(ws_bytes)}};
+    for (int i = 0; i < 4; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (spans_meet(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return CS_EINVAL;
+        if (spans_meet(written[i].p, written[i].bytes, lr_or_null, 8)) return CS_EINVAL;
+    }
+    return grad_norm(list, max_norm, out, workspace, ws_bytes, h, step, lr_or_null, coefs, stream);
+}
+
+extern "C" int cs_adamw_advance_scaled(const cs_adamw* h, int64_t* step, const double* lr_or_null, const float* grad_scale_or_null,
+                                       float* coefs, void* stream) {
+    if (!hyper_ok(h) || !step || !coefs) return CS_EINVAL;
+    k_adamw_coefs<<<1, 1, 0, stream_of(stream)>>>(*h, step, lr_or_null, grad_scale_or_null, reinterpret_cast<Coefs*>(coefs));
     return launched();
 }
 
 extern "C" int cs_adamw_advance(const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream) {
-    if (!hyper_ok(h) || !step || !coefs) return CS_EINVAL;
-    k_adamw_coefs<<<1, 1, 0, stream_of(stream)>>>(*h, step, lr_or_null, reinterpret_cast<Coefs*>(coefs));
-    return launched();
+    return cs_adamw_advance_scaled(h, step, lr_or_null, nullptr, coefs, stream);
 }
 
 extern "C" int cs_adamw_step(const cs_adamw* h, int64_t step, const cs_tensor_list* list, const float* coefs_or_null,
                              const float* grad_scale_or_null, void* stream) {
     if (!hyper_ok(h) || !list_ok(list) || (!coefs_or_null && step < 1)) return CS_EINVAL;
     if (list->chunks == 0) return CS_OK;
-    Coefs c = {};
-    if (!coefs_or_null) {
-        const double c1 = 1. / (1. - pow(h->beta1, static_cast<double>(step)));
-        const double c2 = 1. / sqrt(1. - pow(h->beta2, static_cast<double>(step)));
-        c = Coefs{static_cast<float>(h->beta1), static_cast<float>(1. - h->beta1), static_cast<float>(h->beta2),
-                  static_cast<float>(1. - h->beta2), static_cast<float>(1. - h->lr * h->weight_decay),
-                  static_cast<float>(c2), static_cast<float>(h->lr * c1), static_cast<float>(h->eps)};
-    }
+    const Coefs c = coefs_or_null ? Coefs{} : coefs_of(*h, h->lr, step);
     const Coefs* dc = reinterpret_cast<const Coefs*>(coefs_or_null);
     const hipStream_t s = stream_of(stream);
     if (list->p_fmt == CS_FMT_F32) return adamw_p<float>(list, c, dc, grad_scale_or_null, s);

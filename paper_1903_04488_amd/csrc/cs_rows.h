@@ -133,6 +133,10 @@ inline bool spans_meet(const void* a, int64_t a_bytes, const void* b, int64_t b_
     const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
     return a && b && a_bytes > 0 && b_bytes > 0 && pa < pb + b_bytes && pb < pa + a_bytes;
 }
+struct Span {
+    const void* p;
+    int64_t bytes;
+};
 // rows x cols values of `fmt` whose rows are `stride` values apart: sizes in range and every address in 63 bits
 inline bool rows_ok(int64_t rows, int64_t cols, int64_t stride, int32_t fmt) {
     return rows >= 0 && cols >= 1 && stride >= cols && fmt_ok(fmt) &&

@@ -13,10 +13,6 @@ int by_type(TokenCall call, const TokenArgs& a) {
     return a.fmt == CS_FMT_F32 ? token_f32(call, a) : a.fmt == CS_FMT_BF16 ? token_bf16(call, a) : token_f16(call, a);
 }
 
-struct Span {
-    const void* p;
-    int64_t bytes;
-};
 // no two of the arrays that are written may meet, and none may meet one that is read
 template <int NW, int NR>
 bool spans_apart(const Span (&written)[NW], const Span (&read)[NR]) {

@@ -82,10 +82,11 @@ class AdamW:
     """AdamW over all tensors of a model in one launch, its moments in 32 or in 8 bits.
 
     params, grads: lists of tensors, updated and read where they are (`set_grads` after grads have moved).  max_norm: the
-    gradients are clipped to this global norm, and a step whose norm is not finite changes nothing.  m, v (m_exp, v_exp):
-    moments of a checkpoint after `steps` steps, kept and updated in place.  capturable: step number and learning rate live
-    on the GPU (`lr_now`, float64), so that a graph of step() can be replayed.  The constants may be changed between
-    steps: opt.h.lr = ..."""
+    gradients are clipped to this global norm, and a step whose norm is not finite changes nothing and does not count.  m, v
+    (m_exp, v_exp): moments of a checkpoint after `steps` steps, kept and updated in place.  capturable: step number and learning
+    rate live on the GPU (`lr_now`, float64), so that a graph of step() can be replayed.  The constants may be changed between
+    steps: opt.h.lr = ...  `steps` is the number of steps that were taken (with max_norm or capturable it is read from the GPU,
+    which waits)."""
 
     def __init__(self, params, grads, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  max_norm: float | None = None, bits: int = 32, m=None, v=None, m_exp=None, v_exp=None, steps: int = 0,
@@ -96,7 +97,7 @@ class AdamW:
             raise B.CsError("params must be a non-empty list")
         self.params, self.grads = list(params), list(grads)
         self.h = B.CsAdamw(lr, *betas, eps, weight_decay)
-        self.max_norm, self.bits, self.steps = max_norm, bits, steps
+        self.max_norm, self.bits, self._steps = max_norm, bits, steps
         self.device = self.params[0].device
         kind = torch.uint8 if bits == 8 else torch.float32
 
@@ -119,10 +120,21 @@ class AdamW:
             self.norm, self._scale = self._norm_and_scale[0], self._norm_and_scale[1:]
             self._workspace = torch.empty(B.cs_grad_norm_workspace_bytes(self.list), dtype=torch.uint8, device=self.device)
         self.step_now = self.lr_now = self.coefs = None
-        if capturable:
+        if capturable or max_norm is not None:           # (the host does not see whether a norm is finite)
             self.step_now = torch.full((1,), steps, dtype=torch.int64, device=self.device)
-            self.lr_now = torch.full((1,), lr, dtype=torch.float64, device=self.device)
             self.coefs = torch.zeros(B.CS_ADAMW_COEFS, dtype=torch.float32, device=self.device)
+        if capturable:
+            self.lr_now = torch.full((1,), lr, dtype=torch.float64, device=self.device)
+
+    @property
+    def steps(self):
+        return self._steps if self.step_now is None else int(self.step_now)
+
+    @steps.setter
+    def steps(self, n):
+        self._steps = n
+        if self.step_now is not None:
+            self.step_now.fill_(n)
 
     def set_grads(self, grads):
         """other tensors with the gradients"""
@@ -133,11 +145,13 @@ class AdamW:
     def step(self):
         """one update of params and moments; `norm` (with max_norm) is the gradients' norm, on the GPU"""
         if self.max_norm is not None:
-            B.cs_grad_norm(self.list, self.max_norm, self._norm_and_scale, self._workspace)
-        self.steps += 1
-        if self.coefs is not None:
+            B.cs_grad_norm_advance(self.list, self.max_norm, self._norm_and_scale, self._workspace, self.h, self.step_now, self.coefs,
+                                   self.lr_now)
+        elif self.coefs is not None:
             B.cs_adamw_advance(self.h, self.step_now, self.coefs, self.lr_now)
-        B.cs_adamw_step(self.h, self.steps, self.list, self.coefs, self._scale)
+        B.cs_adamw_step(self.h, self._steps + 1, self.list, self.coefs, self._scale)
+        if self.coefs is None:
+            self._steps += 1
 
 
 class MomentReader:

@@ -1,0 +1,107 @@
+"""A step whose gradients are not finite is none: it changes nothing, and the steps after it have the numbers that they would have
+had without it (their bias corrections belong to as many gradients as the moments have seen)."""
+import math
+
+import pytest
+import torch
+
+import paper_1903_04488_amd as cs
+from paper_1903_04488_amd.training import AdamW
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def tensors(seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    return [torch.randn(n, generator=gen, device=DEV) for n in (9000, 300, 1)]
+
+
+def optimizer(**more):
+    p, g = tensors(1), tensors(2)
+    return AdamW(p, g, max_norm=1.0, weight_decay=0.1, **more)
+
+
+def state(opt):
+    return [x.clone() for t in (opt.params, opt.m, opt.v, opt.m_exp or [], opt.v_exp or []) for x in t]
+
+
+def same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(state(a), state(b)))
+
+
+@pytest.mark.parametrize("capturable", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_steps_that_are_not_taken_do_not_count(bad, bits, capturable):
+    a, b = (optimizer(bits=bits, capturable=capturable) for _ in range(2))
+    for t in range(6):
+        if t in (0, 1, 4):                               # (the first ones, as with a loss scale that is too large)
+            keep = a.grads[0][5].clone()
+            a.grads[0][5] = bad
+            a.step()
+            a.grads[0][5] = keep
+        else:
+            a.step()
+            b.step()
+            assert same(a, b), t
+    assert a.steps == b.steps == 3
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_replays_of_a_graph_are_the_steps_of_a_loop(bits):
+    """bit for bit, moments in 8 bits too, with one step among them that is not taken"""
+    a, b = optimizer(bits=bits, capturable=True), optimizer(bits=bits)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        a.step()
+    torch.cuda.current_stream().wait_stream(side)
+    b.step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step()
+    for t in range(6):
+        b.h.lr = 1e-3 / (t + 1)
+        a.lr_now.fill_(b.h.lr)
+        for x in (*a.grads, *b.grads):
+            x.mul_(-0.9)
+        a.grads[1][3] = b.grads[1][3] = math.inf if t == 2 else 0.25
+        graph.replay()
+        b.step()
+        torch.cuda.synchronize()
+        assert same(a, b), t
+    assert a.steps == b.steps == 6
+
+
+def test_the_number_can_be_read_and_set():
+    for opt in (optimizer(steps=41), optimizer(steps=41, capturable=True), AdamW(tensors(1), tensors(2), steps=41)):
+        assert opt.steps == 41
+        opt.step()
+        assert opt.steps == 42
+        opt.steps = 7
+        opt.step()
+        assert opt.steps == 8
+
+
+def test_counting_by_a_scale_of_the_caller():
+    h = cs.CsAdamw(1e-3, 0.9, 0.999, 1e-8, 0.01)
+    step, coefs = torch.full((1,), 4, dtype=torch.int64, device=DEV), torch.full((cs.CS_ADAMW_COEFS,), -7.0, device=DEV)
+    for bad in (math.nan, math.inf, -math.inf):
+        cs.cs_adamw_advance(h, step, coefs, None, torch.full((1,), bad, device=DEV))
+        assert int(step) == 4 and (coefs == -7.0).all()
+    cs.cs_adamw_advance(h, step, coefs, None, torch.full((1,), 0.5, device=DEV))
+    assert int(step) == 5 and (coefs[:8] != -7.0).all()
+
+
+@pytest.mark.parametrize("t", [1, 2, 7, 1000, 123_457, 1 << 40])
+def test_the_coefficients_of_a_late_step(t):
+    """powers by squaring are off by up to t roundings of 2^-53, of which 1 - beta^t keeps beta^t's share"""
+    h = cs.CsAdamw(1e-3, 0.9, 0.999, 1e-8, 0.01)
+    step, coefs = torch.full((1,), t - 1, dtype=torch.int64, device=DEV), torch.zeros(cs.CS_ADAMW_COEFS, device=DEV)
+    cs.cs_adamw_advance(h, step, coefs)
+    got = coefs.double().tolist()
+    c1, c2 = 1 / -math.expm1(t * math.log(h.beta1)), 1 / math.sqrt(-math.expm1(t * math.log(h.beta2)))
+    for a, b in zip(got, (0.9, 1 - 0.9, 0.999, 1 - 0.999, 1 - 1e-3 * 0.01, c2, 1e-3 * c1, 1e-8)):
+        assert a == pytest.approx(b, rel=2 * U)
