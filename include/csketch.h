@@ -591,7 +591,7 @@ int cs_token_loss(const void* logits, int64_t rows, int64_t vocab, int64_t strid
  *   7 bits, 4 of them exponent e and 3 fraction f: 2^(E - 127 + e - 15) (1 + f / 8); a root's code is c of 8 bits, 4 and 4:
  *   2^(E - 127 + e - 15) (1 + f / 16); c = 0 is the value 0.  E is the exponent field of the block's largest magnitude, or
  *   16; values are rounded to nearest, halves away from 0, up to the largest code, and a root that is not 0 is at
- *   least code 1.  All bytes 0 in m and v, E = 16: moments of 0.
+ *   least code 1 (steps with a seed: below).  All bytes 0 in m and v, E = 16: moments of 0.
  * Different tensors must lie apart, as must the arrays of one tensor (the latter is checked). */
 #define CS_ADAMW_BLOCK 256
 typedef struct cs_tensor_list {
@@ -623,10 +623,22 @@ int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* 
  *   cs_adamw_advance          counts *step up (device int64) and takes lr from *lr_or_null (device double) if given
  *   cs_adamw_advance_scaled   the same, but where *grad_scale_or_null is not finite it leaves *step and coefs alone
  *   cs_grad_norm_advance      cs_grad_norm and, with its out[1] as the scale, the latter, in the launches of the former */
-#define CS_ADAMW_COEFS 8
+#define CS_ADAMW_COEFS 10
 typedef struct cs_adamw {
     double lr, beta1, beta2, eps, weight_decay;      /* all finite and >= 0, betas below 1 */
+    uint64_t seed;                                   /* of the rounding of moments in 8 bits; 0: to nearest */
 } cs_adamw;
+/* Moments in 8 bits over many steps.  Rounded to nearest (seed 0) a moment stands still wherever a step changes it by less than half
+ * a step of its code: with beta2 above 0.938 a root never gets smaller again, and at 0.999 it does not grow to what it should be
+ * either.  That is for single steps, and for moments that another program rounds so.
+ * With a seed: let p be where a value lies on the line of codes of its block (p = c at code c's value, and in between in proportion), and
+ * q the whole number next to p (halves up).  If the moment as it was before the step is not 0 and has the same q in this block, then
+ * c is floor(p + (r + 1/2) / 2^16), r one of 2^16 numbers that are as likely: up or down, right on average.  If a c of the block is
+ * beyond the largest code by that (and E below 254), E is one more, and every c 8 (first moments; roots: 16) less.  Any other c
+ * is q, up to the largest code.  In the end a first moment's c is at least 0, that of a root that is not 0 at least 1.
+ * The numbers: let base be the step-th output of SplitMix64 begun at seed, and the values of the list numbered from 0, each
+ * tensor from the next multiple of 4096 on.  Of the (j + 1)-th output of SplitMix64 begun at base, value 4j + i has the bits from 16 i on:
+ * r of its first moment and of its root. */
 int cs_adamw_advance(const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream);
 int cs_adamw_advance_scaled(const cs_adamw* h, int64_t* step, const double* lr_or_null, const float* grad_scale_or_null, float* coefs,
                             void* stream);

@@ -88,7 +88,7 @@ class CsTensorList(ctypes.Structure):
 
 
 class CsAdamw(ctypes.Structure):
-    _fields_ = [(name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")]
+    _fields_ = [*((name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")), ("seed", ctypes.c_uint64)]
 
 
 def library_path() -> str:
@@ -783,7 +783,7 @@ def cs_sketch_feedback(p, S, idx, val):
 # layer norm, token log probabilities, AdamW
 CS_TOKEN_MAX_TOP = 64
 CS_ADAMW_BLOCK = 256
-CS_ADAMW_COEFS = 8
+CS_ADAMW_COEFS = 10
 _FMT = {torch.bfloat16: CS_FMT_BF16, torch.float16: CS_FMT_F16, torch.float32: CS_FMT_F32}
 
 

@@ -8,7 +8,10 @@
 // stands for 2^(ex - 127); a code's bits are the top bits of the value's own binary32 pattern, its exponent counted from ex - 15.
 // First moment: sign, 4 exponent bits, 3 fraction bits.  Root of the second moment: 4 and 4.  (The
 // root, as its square has twice the range; and a root that is not 0 never becomes code 0, as m / eps would be a leap.)
-// Rounded to nearest, halves away from 0: half a step is 1/16 of a first moment, 1/32 of a root.
+// Rounded to nearest, halves away from 0: half a step is 1/16 of a first moment, 1/32 of a root.  By that alone a moving average stands
+// still: a step of decay changes a root by 1 - sqrt(beta2), 1 % at 0.98, which nearest undoes every time (after 5000 steps of gradients of
+// one size the roots were 1.9 times too large at 0.98, half as large as they should be at 0.999).  So, with a seed, a change that
+// nearest would undo is made with the probability of its share of a step: such a change is right on average.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -82,6 +85,39 @@ __device__ __forceinline__ uint32_t code_of_root(float x, int32_t base) {
     const int32_t c = (mag - base + (1 << 18)) >> 19;
     return mag ? static_cast<uint32_t>(min(max(c, 1), 255)) : 0u;
 }
+// Codes of a wavefront's four values a lane, which were `old` before, by chance where nearest would undo the change; `ex` becomes the
+// block's exponent.  random: 16 bits a value.  A largest value that is rounded up beyond the last code belongs to the next exponent, and 8
+// (16) codes less are the same values there.
+template <bool FIRST>
+__device__ __forceinline__ uint32_t codes_by_chance(const float (&x)[4], const float (&old)[4], const uint32_t (&random)[4], int32_t& ex) {
+    constexpr int DROP = FIRST ? 20 : 19, BINADE = FIRST ? 8 : 16, MOST = FIRST ? 127 : 255;
+    int32_t c[4];
+    bool beyond = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t base = base_of(ex), mag = bits_of(x[e]) & 0x7fffffff, before = bits_of(old[e]) & 0x7fffffff;
+        const int32_t half = 1 << (DROP - 1), near = (mag - base + half) >> DROP;
+        if (before && (before - base + half) >> DROP == near) {
+            c[e] = (mag - base + static_cast<int32_t>(random[e] << (DROP - 16) | 1u << (DROP - 17))) >> DROP;
+            beyond |= c[e] > MOST;
+        } else {
+            c[e] = min(near, MOST);
+        }
+    }
+    if (ex < 254 && __ballot(beyond)) {
+        ++ex;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] -= BINADE;
+    }
+    uint32_t codes = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int32_t code = min(max(c[e], FIRST ? 0 : 1), MOST);
+        if (FIRST) codes |= (static_cast<uint32_t>(code) | (static_cast<uint32_t>(bits_of(x[e])) >> 24 & 0x80u)) << (8 * e);
+        else codes |= (bits_of(x[e]) & 0x7fffffff ? static_cast<uint32_t>(code) : 0u) << (8 * e);
+    }
+    return codes;
+}
 __device__ __forceinline__ int32_t wave_max_bits(int32_t v) {
 #pragma unroll
     for (int d = 32; d; d >>= 1) v = max(v, __shfl_xor(v, d));
@@ -94,7 +130,15 @@ __device__ __forceinline__ int32_t exponent_of(int32_t most_bits) { return max(m
 // ---------------------------------------------------------------------------------------
 struct Coefs {
     float b1, one_b1, b2, one_b2, keep, c2, rate, eps;
+    uint32_t chance[2];                               // where the step's random numbers begin, low half first
 };
+// the n-th output (from 1) of SplitMix64 begun at `state`
+__host__ __device__ __forceinline__ uint64_t splitmix(uint64_t state, uint64_t n) {
+    uint64_t z = state + n * 0x9E3779B97F4A7C15ull;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return z ^ (z >> 31);
+}
 // b^t by squaring: products alone, so that the host and the GPU give the same bits
 __host__ __device__ __forceinline__ double power(double b, int64_t t) {
 #pragma clang fp contract(off)
@@ -106,9 +150,11 @@ __host__ __device__ __forceinline__ double power(double b, int64_t t) {
 __host__ __device__ __forceinline__ Coefs coefs_of(const cs_adamw& h, double lr, int64_t t) {
 #pragma clang fp contract(off)
     const double c1 = 1. / (1. - power(h.beta1, t)), c2 = 1. / sqrt(1. - power(h.beta2, t));
+    const uint64_t chance = splitmix(h.seed, static_cast<uint64_t>(t));
     return Coefs{static_cast<float>(h.beta1), static_cast<float>(1. - h.beta1), static_cast<float>(h.beta2),
                  static_cast<float>(1. - h.beta2), static_cast<float>(1. - lr * h.weight_decay), static_cast<float>(c2),
-                 static_cast<float>(lr * c1), static_cast<float>(h.eps)};
+                 static_cast<float>(lr * c1), static_cast<float>(h.eps),
+                 {static_cast<uint32_t>(chance), static_cast<uint32_t>(chance >> 32)}};
 }
 
 struct Moved {
@@ -169,10 +215,13 @@ __device__ __forceinline__ void store4_codes(uint8_t* x, int64_t at, int64_t n, 
 // a chunk of 4096 values of one tensor, found in the list (all tensors in one launch: a small model is launch and latency, 4.9 us
 // for 35 tensors of 0.2 M parameters).  Bound by memory: 90 M parameters with moments in 32 bits 394 us, 2465 MB as counted at 6.3
 // TB/s; in 8 bits 212 us, 1245 MB at 5.9, and there the vector ALU is busy too (95 %: a square root and a quotient, both rounded
-// correctly, and two encodings a value).
-template <typename P, typename G, bool EIGHT, bool PAST>
+// correctly, and two encodings a value).  By chance 33 us more (90 M, bf16 gradients, 235 / 267 a step): the vector ALU.  With a
+// number of its own for either moment 278.
+enum { kThirtyTwo, kNearest, kChance };               // moments: in 32 bits, in 8 to nearest, in 8 by chance
+template <typename P, typename G, int MOMENTS, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_adamw(const Tensor* tensors, const Chunk* chunks, int split, Coefs c, const Coefs* coefs, const float* grad_scale) {
+    constexpr bool EIGHT = MOMENTS != kThirtyTwo;
     float scale = 1.f;
     if (grad_scale) {
         scale = *grad_scale;
@@ -188,7 +237,7 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, int split, Coefs c, const Co
     for (int k = from + wave; k < from + each; k += kThreads / 64) {
         const int64_t block = begin + k * kBlock8, at = block + lane * 4;
         if (block >= t.n) return;                     // (the whole wavefront)
-        float p[4], g[4], m[4], v[4], root[4];
+        float p[4], g[4], m[4], v[4], root[4], old_m[4], old_root[4];
         load4<PAST>(static_cast<const P*>(t.p), at, t.n, p);
         load4(static_cast<const G*>(t.g), at, t.n, g);
         if (EIGHT) {
@@ -200,6 +249,7 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, int split, Coefs c, const Co
                 m[e] = first_of(mc >> (8 * e) & 0xff, mb);
                 const float r = root_of(vc >> (8 * e) & 0xff, vb);
                 v[e] = r * r;
+                old_m[e] = m[e], old_root[e] = r;
             }
         } else {
             load4<PAST>(static_cast<const float*>(t.m), at, t.n, m);
@@ -219,12 +269,22 @@ k_adamw(const Tensor* tensors, const Chunk* chunks, int split, Coefs c, const Co
                 mm = max(mm, bits_of(m[e]) & 0x7fffffff);
                 vm = max(vm, bits_of(root[e]) & 0x7fffffff);
             }
-            const int32_t me = exponent_of(wave_max_bits(mm)), ve = exponent_of(wave_max_bits(vm));
+            int32_t me = exponent_of(wave_max_bits(mm)), ve = exponent_of(wave_max_bits(vm));
             uint32_t mc = 0, vc = 0;
+            if constexpr (MOMENTS == kChance) {
+                // four values' numbers come from one output, 16 bits each (the same ones for both moments)
+                const uint64_t state = static_cast<uint64_t>(c.chance[1]) << 32 | c.chance[0];
+                const uint64_t z = splitmix(state, static_cast<uint64_t>(place / split) * (kChunk / 4) + static_cast<uint32_t>(k * kBlock8 / 4 + lane) + 1);
+                const uint32_t low = static_cast<uint32_t>(z), high = static_cast<uint32_t>(z >> 32);
+                const uint32_t r[4] = {low & 0xffff, low >> 16, high & 0xffff, high >> 16};
+                mc = codes_by_chance<true>(m, old_m, r, me);
+                vc = codes_by_chance<false>(root, old_root, r, ve);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                mc |= code_of_first(m[e], base_of(me)) << (8 * e);
-                vc |= code_of_root(root[e], base_of(ve)) << (8 * e);
+                for (int e = 0; e < 4; ++e) {
+                    mc |= code_of_first(m[e], base_of(me)) << (8 * e);
+                    vc |= code_of_root(root[e], base_of(ve)) << (8 * e);
+                }
             }
             store4_codes(static_cast<uint8_t*>(t.m), at, t.n, mc);
             store4_codes(static_cast<uint8_t*>(t.v), at, t.n, vc);
@@ -413,7 +473,7 @@ bool list_ok(const cs_tensor_list* l) {
 }
 
 template <typename P, typename G>
-int adamw(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
+int adamw(const cs_tensor_list* l, const Coefs& c, bool chance, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
     const List at = list_of(l);
     // Parameters and moments that the memory-side cache cannot keep are read and written past it: what it keeps is
     // the gradients that their norm has just read.
@@ -421,16 +481,17 @@ int adamw(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const flo
     const bool past = past_caches(l->chunks * kChunk * each);
     const int split = split_of(l->chunks, past && l->bits == 8);
     const unsigned grid = static_cast<unsigned>(l->chunks * split);
-    const auto kernel = l->bits == 8 ? (past ? k_adamw<P, G, true, true> : k_adamw<P, G, true, false>)
-                                     : (past ? k_adamw<P, G, false, true> : k_adamw<P, G, false, false>);
+    const auto kernel = l->bits == 32 ? (past ? k_adamw<P, G, kThirtyTwo, true> : k_adamw<P, G, kThirtyTwo, false>)
+                        : chance      ? (past ? k_adamw<P, G, kChance, true> : k_adamw<P, G, kChance, false>)
+                                      : (past ? k_adamw<P, G, kNearest, true> : k_adamw<P, G, kNearest, false>);
     kernel<<<grid, kThreads, 0, stream>>>(at.tensors, at.chunks, split, c, coefs, grad_scale);
     return launched();
 }
 template <typename P>
-int adamw_p(const cs_tensor_list* l, const Coefs& c, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
-    if (l->g_fmt == CS_FMT_F32) return adamw<P, float>(l, c, coefs, grad_scale, stream);
-    if (l->g_fmt == CS_FMT_BF16) return adamw<P, bf16>(l, c, coefs, grad_scale, stream);
-    return adamw<P, f16>(l, c, coefs, grad_scale, stream);
+int adamw_p(const cs_tensor_list* l, const Coefs& c, bool chance, const Coefs* coefs, const float* grad_scale, hipStream_t stream) {
+    if (l->g_fmt == CS_FMT_F32) return adamw<P, float>(l, c, chance, coefs, grad_scale, stream);
+    if (l->g_fmt == CS_FMT_BF16) return adamw<P, bf16>(l, c, chance, coefs, grad_scale, stream);
+    return adamw<P, f16>(l, c, chance, coefs, grad_scale, stream);
 }
 
 bool hyper_ok(const cs_adamw* h) {
@@ -568,9 +629,10 @@ extern "C" int cs_adamw_step(const cs_adamw* h, int64_t step, const cs_tensor_li
     const Coefs c = coefs_or_null ? Coefs{} : coefs_of(*h, h->lr, step);
     const Coefs* dc = reinterpret_cast<const Coefs*>(coefs_or_null);
     const hipStream_t s = stream_of(stream);
-    if (list->p_fmt == CS_FMT_F32) return adamw_p<float>(list, c, dc, grad_scale_or_null, s);
-    if (list->p_fmt == CS_FMT_BF16) return adamw_p<bf16>(list, c, dc, grad_scale_or_null, s);
-    return adamw_p<f16>(list, c, dc, grad_scale_or_null, s);
+    const bool chance = h->seed != 0;
+    if (list->p_fmt == CS_FMT_F32) return adamw_p<float>(list, c, chance, dc, grad_scale_or_null, s);
+    if (list->p_fmt == CS_FMT_BF16) return adamw_p<bf16>(list, c, chance, dc, grad_scale_or_null, s);
+    return adamw_p<f16>(list, c, chance, dc, grad_scale_or_null, s);
 }
 
 extern "C" int cs_moments_read(const cs_tensor_list* list, void* stream) {

@@ -5,6 +5,7 @@ runs inside libcsketch.so.  What they return are their own buffers, which the ne
 """
 from __future__ import annotations
 
+import warnings
 
 import torch
 
@@ -83,20 +84,29 @@ class AdamW:
 
     params, grads: lists of tensors, updated and read where they are (`set_grads` after grads have moved).  max_norm: the
     gradients are clipped to this global norm, and a step whose norm is not finite changes nothing and does not count.  m, v
-    (m_exp, v_exp): moments of a checkpoint after `steps` steps, kept and updated in place.  capturable: step number and learning
+    (m_exp, v_exp): moments of a checkpoint after `steps` steps, kept and updated in place.  seed: of the rounding to 8 bits, which
+    without one (0) is to nearest and does not follow the gradients over many steps; an optimizer that begins with moments of its own
+    has a seed, one that goes on with others is told theirs.  capturable: step number and learning
     rate live on the GPU (`lr_now`, float64), so that a graph of step() can be replayed.  The constants may be changed between
     steps: opt.h.lr = ...  `steps` is the number of steps that were taken (with max_norm or capturable it is read from the GPU,
     which waits)."""
 
     def __init__(self, params, grads, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 0.01,
                  max_norm: float | None = None, bits: int = 32, m=None, v=None, m_exp=None, v_exp=None, steps: int = 0,
-                 capturable: bool = False):
+                 capturable: bool = False, seed: int | None = None):
         if bits not in (8, 32):
             raise B.CsError(f"moments have 8 or 32 bits, not {bits}")
         if not params:
             raise B.CsError("params must be a non-empty list")
         self.params, self.grads = list(params), list(grads)
-        self.h = B.CsAdamw(lr, *betas, eps, weight_decay)
+        if seed is None:
+            seed = 1 if bits == 8 and m is None and v is None else 0
+        if not 0 <= seed < 1 << 64:
+            raise B.CsError(f"seed must be a number of 64 bits, not {seed}")
+        if bits == 8 and not seed and betas[1] > 0.938:
+            warnings.warn("moments in 8 bits that are rounded to nearest (seed 0) do not follow the gradients over many steps",
+                          stacklevel=2)
+        self.h = B.CsAdamw(lr, *betas, eps, weight_decay, seed)
         self.max_norm, self.bits, self._steps = max_norm, bits, steps
         self.device = self.params[0].device
         kind = torch.uint8 if bits == 8 else torch.float32
