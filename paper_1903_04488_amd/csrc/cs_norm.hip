@@ -86,20 +86,23 @@ k_norm_columns_any(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride,
                    const float* mean, const float* rstd, float* partials) {
     __shared__ float lds[2][4][64];
     const int lane = threadIdx.x & 63, part = threadIdx.x >> 6;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 64 + lane;
-    float dw = 0.f, db = 0.f;
-    if (c < cols)
-        for (int64_t row = static_cast<int64_t>(blockIdx.y) * 4 + part; row < rows; row += static_cast<int64_t>(gridDim.y) * 4) {
-            const float d = static_cast<float>(dy[row * dy_stride + c]);
-            dw = fmaf(d, (static_cast<float>(x[row * x_stride + c]) - mean[row]) * rstd[row], dw);
-            db += d;
-        }
-    lds[0][part][lane] = dw;
-    lds[1][part][lane] = db;
-    __syncthreads();
-    if (part < 2 && c < cols)
-        partials[(static_cast<int64_t>(blockIdx.y) * 2 + part) * cols + c] =
-            (lds[part][0][lane] + lds[part][1][lane]) + (lds[part][2][lane] + lds[part][3][lane]);
+    for (int64_t begin = static_cast<int64_t>(blockIdx.x) * 64; begin < cols; begin += static_cast<int64_t>(gridDim.x) * 64) {
+        const int64_t c = begin + lane;
+        float dw = 0.f, db = 0.f;
+        if (c < cols)
+            for (int64_t row = static_cast<int64_t>(blockIdx.y) * 4 + part; row < rows; row += static_cast<int64_t>(gridDim.y) * 4) {
+                const float d = static_cast<float>(dy[row * dy_stride + c]);
+                dw = fmaf(d, (static_cast<float>(x[row * x_stride + c]) - mean[row]) * rstd[row], dw);
+                db += d;
+            }
+        lds[0][part][lane] = dw;
+        lds[1][part][lane] = db;
+        __syncthreads();
+        if (part < 2 && c < cols)
+            partials[(static_cast<int64_t>(blockIdx.y) * 2 + part) * cols + c] =
+                (lds[part][0][lane] + lds[part][1][lane]) + (lds[part][2][lane] + lds[part][3][lane]);
+        __syncthreads();
+    }
 }
 
 // dweight and dbias from the shares' partial sums, in a fixed order: 16 columns a workgroup (64 contiguous bytes of every share), 64
@@ -113,29 +116,32 @@ k_norm_weights(const float* partials, int shares, int64_t cols, W* dweight, W* d
     W* out = blockIdx.y ? dbias : dweight;
     if (!out) return;
     const int at = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 16 + at;
-    float s = 0.f;
-    if (c < cols) {
-        const float* p = partials + static_cast<int64_t>(blockIdx.y) * cols + c;
-        int g = part;
-        for (; g + 3 * 64 < shares; g += 4 * 64) {
-            float v[4];
+    for (int64_t begin = static_cast<int64_t>(blockIdx.x) * 16; begin < cols; begin += static_cast<int64_t>(gridDim.x) * 16) {
+        const int64_t c = begin + at;
+        float s = 0.f;
+        if (c < cols) {
+            const float* p = partials + static_cast<int64_t>(blockIdx.y) * cols + c;
+            int g = part;
+            for (; g + 3 * 64 < shares; g += 4 * 64) {
+                float v[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = p[static_cast<int64_t>(g + 64 * k) * 2 * cols];
-            s += (v[0] + v[1]) + (v[2] + v[3]);
+                for (int k = 0; k < 4; ++k) v[k] = p[static_cast<int64_t>(g + 64 * k) * 2 * cols];
+                s += (v[0] + v[1]) + (v[2] + v[3]);
+            }
+            for (; g < shares; g += 64) s += p[static_cast<int64_t>(g) * 2 * cols];
         }
-        for (; g < shares; g += 64) s += p[static_cast<int64_t>(g) * 2 * cols];
-    }
-    // a wavefront's four parts, then the wavefronts'
-    s += __shfl_xor(s, 16);
-    s += __shfl_xor(s, 32);
-    if ((threadIdx.x & 63) < 16) lds[threadIdx.x >> 6][at] = s;
-    __syncthreads();
-    if (part == 0 && c < cols) {
-        s = 0.f;
+        // a wavefront's four parts, then the wavefronts'
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if ((threadIdx.x & 63) < 16) lds[threadIdx.x >> 6][at] = s;
+        __syncthreads();
+        if (part == 0 && c < cols) {
+            s = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWeightsBlock / 64; ++k) s += lds[k][at];
-        out[c] = static_cast<W>(s);
+            for (int k = 0; k < kWeightsBlock / 64; ++k) s += lds[k][at];
+            out[c] = static_cast<W>(s);
+        }
+        __syncthreads();
     }
 }
 
@@ -460,6 +466,12 @@ Held held_grad(int64_t cols, int32_t fmt) {
     return {0, 0};
 }
 
+// Workgroups of `threads` threads for columns, `each` at a time, which they take in turns: a launch has fewer than 2^32 threads in a
+// dimension, and rows up to 2^30 columns.
+unsigned column_grid(int64_t cols, int each, int threads) {
+    const int64_t n = (cols + each - 1) / each, most = (static_cast<int64_t>(1) << 32) / threads - 1;
+    return static_cast<unsigned>(n < most ? n : most);
+}
 unsigned norm_grid(int64_t rows) { return static_cast<unsigned>(rows < 4096 ? rows : 4096); }
 // workgroups of the backward pass over rows that are held in registers; each leaves partial sums of the weights' gradients
 int grad_grid(int64_t rows, const Held& h, int32_t fmt) {
@@ -572,7 +584,7 @@ int norm_grad(const NormArgs& a, int shares) {
 #undef CS_CALL
     }
     if (a.dweight || a.dbias) {
-        const dim3 grid(static_cast<unsigned>((a.cols + 63) / 64), shares);
+        const dim3 grid(column_grid(a.cols, 64, kNormBlock), shares);
         k_norm_columns_any<T><<<grid, kNormBlock, 0, a.stream>>>(dy, a.dy_stride, x, a.x_stride, a.rows, a.cols, a.mean,
                                                                  a.rstd, a.partials);
         if (int rc = launched()) return rc;
@@ -592,7 +604,7 @@ int norm_backward(const NormArgs& a) {
     if (!a.dweight && !a.dbias) return CS_OK;
     const Held h = held_grad(a.cols, std::is_same<T, float>::value ? CS_FMT_F32 : CS_FMT_BF16);
     if (a.rows && h.threads && own_sums(a, h)) return CS_OK;
-    const dim3 grid(static_cast<unsigned>((a.cols + 15) / 16), 2);
+    const dim3 grid(column_grid(a.cols, 16, kWeightsBlock), 2);
     k_norm_weights<W><<<grid, kWeightsBlock, 0, a.stream>>>(a.partials, shares, a.cols, static_cast<W*>(a.dweight),
                                                          static_cast<W*>(a.dbias));
     return launched();
