@@ -319,9 +319,12 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
     const int64_t step = static_cast<int64_t>(row_blocks) * ROWS;
     int64_t first = static_cast<int64_t>(blockIdx.x) * ROWS;         // of the workgroup's rows
     Raw<T, P> next_x[ITEMS], next_dy[ITEMS];
+    if (ROWS > 1)
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) next_x[i] = next_dy[i] = Raw<T, P>{};
     float next_mu = 0.f, next_rs = 0.f;
-    const auto request = [&](int64_t of) {
-        const int64_t r = min(of + group, rows - 1);                 // (a group without a row left: in bounds)
+    // (a group without a row left reads none: where dx is x or dy, another group may be writing it)
+    const auto request = [&](int64_t r) {
         next_mu = mean[r], next_rs = rstd[r];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
@@ -330,17 +333,18 @@ k_norm_grad(const T* dy, int64_t dy_stride, const T* x, int64_t x_stride, int64_
                 next_dy[i].load(dy + r * dy_stride + slot.at(i));
             }
     };
-    if (first < rows) request(first);
+    if (first + group < rows) request(first + group);
     for (; first < rows; first += step) {
         const int64_t row = first + group;
         const bool has_row = ROWS == 1 || row < rows;
         float v[ITEMS][P], a[ITEMS][P];
-        const float mu = next_mu, rs = next_rs;
+        // (without a row: what x was before, or 0, times 0, and dy 0)
+        const float mu = has_row ? next_mu : 0.f, rs = has_row ? next_rs : 0.f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
             for (int e = 0; e < P; ++e) v[i][e] = next_x[i][e], a[i][e] = has_row ? next_dy[i][e] : 0.f;
-        if (first + step < rows) request(first + step);          // under way while this row is worked on
+        if (row + step < rows) request(row + step);              // under way while this row is worked on
         float s[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
