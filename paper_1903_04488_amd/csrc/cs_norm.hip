@@ -658,7 +658,8 @@ extern "C" int cs_layer_norm(const void* x, int64_t rows, int64_t cols, int64_t 
         if (w && span_in_rows(w, cols * fmt_bytes(w_fmt), y, y_stride, rows, cols, fmt)) return CS_EINVAL;
     for (const void* s : {static_cast<const void*>(mean), static_cast<const void*>(rstd)})
         if (s && (span_in_rows(s, 4 * rows, y, y_stride, rows, cols, fmt) ||
-                  span_in_rows(s, 4 * rows, x, x_stride, rows, cols, fmt)))
+                  span_in_rows(s, 4 * rows, x, x_stride, rows, cols, fmt) ||
+                  spans_meet(s, 4 * rows, weight, cols * fmt_bytes(w_fmt)) || spans_meet(s, 4 * rows, bias, cols * fmt_bytes(w_fmt))))
             return CS_EINVAL;
     if (spans_meet(mean, 4 * rows, rstd, 4 * rows)) return CS_EINVAL;
     NormArgs a = {};
