@@ -468,6 +468,9 @@ List list_of(const cs_tensor_list* l) {
 // A launch has fewer than 2^32 threads: a list of 2^22 chunks or more is not split.
 int split_of(int64_t chunks, bool one) { return one || chunks * 4 >= kMaxChunks ? 1 : 4; }
 int partials_of(const cs_tensor_list* l) { return static_cast<int>(l->chunks < kSquares ? l->chunks : kSquares); }
+int64_t list_bytes(const cs_tensor_list* l) {
+    return l->count * static_cast<int64_t>(sizeof(Tensor)) + l->chunks * static_cast<int64_t>(sizeof(Chunk));
+}
 bool list_ok(const cs_tensor_list* l) {
     return l && l->count >= 0 && l->chunks >= 0 && l->chunks < kMaxChunks && (l->chunks == 0 || l->memory);
 }
@@ -575,7 +578,9 @@ int grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* wor
     const size_t need = static_cast<size_t>(partials_of(list)) * sizeof(double);
     if (ws_bytes < need) return CS_EWORKSPACE;
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7))) return CS_EINVAL;
-    if (spans_meet(out, 8, workspace, static_cast<int64_t>(need))) return CS_EINVAL;
+    const Span written[] = {{out, 8}, {need ? workspace : nullptr, static_cast<int64_t>(need)}, {step, 8}, {coefs, 4 * CS_ADAMW_COEFS}};
+    const Span read[] = {{list->memory, list_bytes(list)}, {lr, 8}};
+    if (!spans_apart(written, read)) return CS_EINVAL;
     const List at = list_of(list);
     double* partials = static_cast<double*>(workspace);
     const int grid = partials_of(list);
@@ -602,18 +607,14 @@ extern "C" int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* 
 extern "C" int cs_grad_norm_advance(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes,
                                     const cs_adamw* h, int64_t* step, const double* lr_or_null, float* coefs, void* stream) {
     if (!hyper_ok(h) || !step || !coefs) return CS_EINVAL;
-    const Span written[] = {{out, 8}, {step, 8}, {coefs, 4 * CS_ADAMW_COEFS}, {workspace, static_cast<int64_t>(ws_bytes)}};
-    for (int i = 0; i < 4; ++i) {
-        for (int j = 0; j < i; ++j)
-            if (spans_meet(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return CS_EINVAL;
-        if (spans_meet(written[i].p, written[i].bytes, lr_or_null, 8)) return CS_EINVAL;
-    }
     return grad_norm(list, max_norm, out, workspace, ws_bytes, h, step, lr_or_null, coefs, stream);
 }
 
 extern "C" int cs_adamw_advance_scaled(const cs_adamw* h, int64_t* step, const double* lr_or_null, const float* grad_scale_or_null,
                                        float* coefs, void* stream) {
     if (!hyper_ok(h) || !step || !coefs) return CS_EINVAL;
+    const Span written[] = {{step, 8}, {coefs, 4 * CS_ADAMW_COEFS}}, read[] = {{lr_or_null, 8}, {grad_scale_or_null, 4}};
+    if (!spans_apart(written, read)) return CS_EINVAL;
     k_adamw_coefs<<<1, 1, 0, stream_of(stream)>>>(*h, step, lr_or_null, grad_scale_or_null, reinterpret_cast<Coefs*>(coefs));
     return launched();
 }

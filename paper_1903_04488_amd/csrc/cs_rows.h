@@ -137,6 +137,17 @@ struct Span {
     const void* p;
     int64_t bytes;
 };
+// no two of the arrays that are written may meet, and none may meet one that is read
+template <int NW, int NR>
+bool spans_apart(const Span (&written)[NW], const Span (&read)[NR]) {
+    for (int i = 0; i < NW; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (spans_meet(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return false;
+        for (int j = 0; j < NR; ++j)
+            if (spans_meet(written[i].p, written[i].bytes, read[j].p, read[j].bytes)) return false;
+    }
+    return true;
+}
 // rows x cols values of `fmt` whose rows are `stride` values apart: sizes in range and every address in 63 bits
 inline bool rows_ok(int64_t rows, int64_t cols, int64_t stride, int32_t fmt) {
     return rows >= 0 && cols >= 1 && stride >= cols && fmt_ok(fmt) &&

@@ -13,17 +13,6 @@ int by_type(TokenCall call, const TokenArgs& a) {
     return a.fmt == CS_FMT_F32 ? token_f32(call, a) : a.fmt == CS_FMT_BF16 ? token_bf16(call, a) : token_f16(call, a);
 }
 
-// no two of the arrays that are written may meet, and none may meet one that is read
-template <int NW, int NR>
-bool spans_apart(const Span (&written)[NW], const Span (&read)[NR]) {
-    for (int i = 0; i < NW; ++i) {
-        for (int j = 0; j < i; ++j)
-            if (spans_meet(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return false;
-        for (int j = 0; j < NR; ++j)
-            if (spans_meet(written[i].p, written[i].bytes, read[j].p, read[j].bytes)) return false;
-    }
-    return true;
-}
 int64_t row_span(int64_t rows, int64_t vocab, int64_t stride, int32_t fmt) {
     return rows > 0 ? ((rows - 1) * stride + vocab) * fmt_bytes(fmt) : 0;
 }
