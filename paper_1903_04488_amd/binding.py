@@ -1070,17 +1070,20 @@ class TensorList:
                                                       for i, (t, k) in enumerate(zip(tensors, size))])
         sizes, need = (ctypes.c_int64 * len(n))(*n), ctypes.c_size_t()
         _check(load_library().cs_tensor_list_bytes(sizes, len(n), ctypes.byref(need)), "cs_tensor_list_bytes")
-        self.device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
+        device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
         index = p[0].get_device() if p else 0
         if any(t.get_device() != index for tensors, _ in each.values() for t in tensors):
             raise CsError("the tensors of a list must be on one GPU")
-        if self.memory is None or self.memory.numel() < need.value or self.memory.device != self.device:
-            self.memory = torch.empty(need.value, dtype=torch.uint8, device=self.device)
-        self.tensors = {name: list(tensors) for name, (tensors, _) in each.items()}
+        memory, c = self.memory, CsTensorList()
+        if memory is None or memory.numel() < need.value or memory.device != device:
+            memory = torch.empty(need.value, dtype=torch.uint8, device=device)
         _check(load_library().cs_tensor_list_build(
             sizes, len(n), ptrs["p"], _FMT[each["p"][1]], ptrs["g"], _FMT[each["g"][1]], ptrs["m"], ptrs["v"], bits,
-            ptrs.get("m_exp"), ptrs.get("v_exp"), self.memory.data_ptr(), self.memory.numel(), ctypes.byref(self.c),
-            _stream(self.memory)), "cs_tensor_list_build")
+            ptrs.get("m_exp"), ptrs.get("v_exp"), memory.data_ptr(), memory.numel(), ctypes.byref(c), _stream(memory)),
+            "cs_tensor_list_build")
+        # (only now: a list that could not be built anew is the one that it was, its memory and its tensors held)
+        self.device, self.memory, self.c = device, memory, c
+        self.tensors = {name: list(tensors) for name, (tensors, _) in each.items()}
 
 
 def cs_grad_norm_workspace_bytes(tensors: TensorList) -> int:
