@@ -853,12 +853,14 @@ def cs_layer_norm(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-5):
         dt, wt = x.dtype, weight.dtype
         if (one == out_one == 1 and step >= cols <= out_step and x.is_cuda and dt in _FMT and cols and y.dtype is dt and y.is_cuda
                 and y.shape == x.shape and (wt is dt or wt is f32) and weight.is_contiguous() and weight.is_cuda
-                and weight.numel() == cols and bias.dtype is wt and bias.is_contiguous() and bias.is_cuda and bias.numel() == cols
+                and weight.numel() == cols
+                and (bias is None or (bias.dtype is wt and bias.is_contiguous() and bias.is_cuda and bias.numel() == cols))
                 and (mean is None if rstd is None else
                      mean.dtype is f32 and mean.is_contiguous() and mean.is_cuda and mean.numel() == rows
                      and rstd.dtype is f32 and rstd.is_contiguous() and rstd.is_cuda and rstd.numel() == rows)):
             status = (_lib or load_library()).cs_layer_norm(
-                x.data_ptr(), rows, cols, step, _FMT[dt], weight.data_ptr(), bias.data_ptr(), _FMT[wt], eps, y.data_ptr(), out_step,
+                x.data_ptr(), rows, cols, step, _FMT[dt], weight.data_ptr(), None if bias is None else bias.data_ptr(), _FMT[wt], eps,
+                y.data_ptr(), out_step,
                 None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(), _stream(x))
             if status:
                 _check(status, "cs_layer_norm")
@@ -894,14 +896,14 @@ def cs_layer_norm_grad(dy, x, weight, mean, rstd, dx, dweight, dbias, workspace)
                 and dx.dtype is dt and dx.is_cuda and dx.shape == x.shape
                 and weight.is_contiguous() and weight.is_cuda and weight.numel() == cols
                 and dweight.dtype is wt and dweight.is_contiguous() and dweight.is_cuda and dweight.numel() == cols
-                and dbias.dtype is wt and dbias.is_contiguous() and dbias.is_cuda and dbias.numel() == cols
+                and (dbias is None or (dbias.dtype is wt and dbias.is_contiguous() and dbias.is_cuda and dbias.numel() == cols))
                 and mean.dtype is f32 and mean.is_contiguous() and mean.is_cuda and mean.numel() == rows
                 and rstd.dtype is f32 and rstd.is_contiguous() and rstd.is_cuda and rstd.numel() == rows
                 and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.is_cuda):
             status = (_lib or load_library()).cs_layer_norm_grad(
                 dy.data_ptr(), d_step, x.data_ptr(), step, rows, cols, _FMT[dt], weight.data_ptr(), _FMT[wt], mean.data_ptr(),
-                rstd.data_ptr(), dx.data_ptr(), out_step, dweight.data_ptr(), dbias.data_ptr(), workspace.data_ptr(),
-                workspace.numel(), _stream(x))
+                rstd.data_ptr(), dx.data_ptr(), out_step, dweight.data_ptr(), None if dbias is None else dbias.data_ptr(),
+                workspace.data_ptr(), workspace.numel(), _stream(x))
             if status:
                 _check(status, "cs_layer_norm_grad")
             return
