@@ -606,7 +606,7 @@ int cs_tensor_list_build(const int64_t* n, int32_t count, void* const* p, int32_
 
 /* Global norm of the gradients of a list, and the coefficient that clips it:
  *     out[0] = sqrt(sum of squares over all tensors)   (in binary64, rounded once)
- *     out[1] = min(1, max_norm / (out[0] + 1e-6)), NaN where the norm is not finite
+ *     out[1] = min(1, max_norm / (out[0] + 1e-6)), NaN where out[0] is not finite
  * out: device float[2].  max_norm > 0 (infinity: the norm alone).  workspace: device, 8-byte aligned. */
 int cs_grad_norm_workspace_bytes(const cs_tensor_list* list, size_t* bytes);
 int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* workspace, size_t ws_bytes, void* stream);

@@ -416,14 +416,16 @@ k_grad_norm(const double* partials, int count, double max_norm, float* out, cs_a
 #pragma unroll
     for (int k = 0; k < kSquares / kThreads; ++k) s += v[k];
     s = block_sum(s, lds);
+    // (finite as it is told, in binary32)
     const double norm = sqrt(s), c = max_norm / (norm + 1e-6);
-    if (ADVANCE && threadIdx.x == kCounts && norm < INFINITY) {
+    const bool finite = static_cast<float>(norm) < INFINITY;
+    if (ADVANCE && threadIdx.x == kCounts && finite) {
         *step = t;
         *coefs = now;
     }
     if (threadIdx.x) return;
     out[0] = static_cast<float>(norm);
-    out[1] = norm < INFINITY ? static_cast<float>(c < 1. ? c : 1.) : NAN;
+    out[1] = finite ? static_cast<float>(c < 1. ? c : 1.) : NAN;
 }
 
 __global__ void k_adamw_coefs(cs_adamw h, int64_t* step, const double* lr, const float* grad_scale, Coefs* out) {

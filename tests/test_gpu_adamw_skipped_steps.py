@@ -13,13 +13,13 @@ DEV = "cuda:0"
 U = 2.0 ** -24
 
 
-def tensors(seed):
+def tensors(seed, dtype=torch.float32):
     gen = torch.Generator(device=DEV).manual_seed(seed)
-    return [torch.randn(n, generator=gen, device=DEV) for n in (9000, 300, 1)]
+    return [torch.randn(n, generator=gen, device=DEV).to(dtype) for n in (9000, 300, 1)]
 
 
-def optimizer(**more):
-    p, g = tensors(1), tensors(2)
+def optimizer(g_type=torch.float32, **more):
+    p, g = tensors(1), tensors(2, g_type)
     return AdamW(p, g, max_norm=1.0, weight_decay=0.1, **more)
 
 
@@ -73,6 +73,28 @@ def test_replays_of_a_graph_are_the_steps_of_a_loop(bits):
         torch.cuda.synchronize()
         assert same(a, b), t
     assert a.steps == b.steps == 6
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("kind,g_type", [("a gradient", torch.float32), ("a gradient", torch.bfloat16), ("a gradient", torch.float16),
+                                         ("the norm", torch.float32), ("the norm", torch.bfloat16)])
+def test_both_ways_to_overflow(kind, g_type, bits):
+    """a gradient that is infinite, or gradients that are numbers of a norm that binary32 has none for (binary16 has no such ones)"""
+    a, b = optimizer(g_type, bits=bits), optimizer(g_type, bits=bits)
+    keep = a.grads[1].clone()
+    if kind == "a gradient":
+        a.grads[1][7] = 1e30 if g_type == torch.float16 else math.inf
+    else:
+        a.grads[1].fill_(2e38)
+    before = state(a)
+    a.step()
+    assert float(a.norm) == math.inf and a.steps == 0
+    assert all(torch.equal(x, y) for x, y in zip(state(a), before))
+    a.grads[1].copy_(keep)
+    for _ in range(2):
+        a.step()
+        b.step()
+    assert same(a, b) and a.steps == 2
 
 
 def test_the_number_can_be_read_and_set():
