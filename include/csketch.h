@@ -598,6 +598,7 @@ typedef struct cs_tensor_list {
     void* memory;               /* device */
     int64_t chunks;             /* pieces of work */
     int32_t count, p_fmt, g_fmt, bits;
+    int64_t values;             /* of all tensors */
 } cs_tensor_list;
 int cs_tensor_list_bytes(const int64_t* n, int32_t count, size_t* bytes);
 int cs_tensor_list_build(const int64_t* n, int32_t count, void* const* p, int32_t p_fmt, const void* const* g,

@@ -84,7 +84,7 @@ class CsParams(ctypes.Structure):
 
 class CsTensorList(ctypes.Structure):
     _fields_ = [("memory", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("count", ctypes.c_int32),
-                ("p_fmt", ctypes.c_int32), ("g_fmt", ctypes.c_int32), ("bits", ctypes.c_int32)]
+                ("p_fmt", ctypes.c_int32), ("g_fmt", ctypes.c_int32), ("bits", ctypes.c_int32), ("values", ctypes.c_int64)]
 
 
 class CsAdamw(ctypes.Structure):

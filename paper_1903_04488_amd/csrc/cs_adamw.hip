@@ -442,8 +442,9 @@ static_assert(sizeof(Coefs) == 4 * CS_ADAMW_COEFS, "csketch.h");
 constexpr int64_t kReadWhole = 8192;
 constexpr int64_t kMaxValues = static_cast<int64_t>(1) << 40, kMaxChunks = static_cast<int64_t>(1) << 24;   // (2^32 threads a launch)
 
-int64_t chunks_of(const int64_t* n, int32_t count, bool& ok) {
-    int64_t chunks = 0, values = 0;
+int64_t chunks_of(const int64_t* n, int32_t count, int64_t& values, bool& ok) {
+    int64_t chunks = 0;
+    values = 0;
     ok = true;
     for (int32_t i = 0; i < count; ++i) {
         if (n[i] < 0 || n[i] > kMaxValues || (values += n[i]) > kMaxValues) {
@@ -483,7 +484,7 @@ int adamw(const cs_tensor_list* l, const Coefs& c, bool chance, const Coefs* coe
     // Parameters and moments that the memory-side cache cannot keep are read and written past it: what it keeps is
     // the gradients that their norm has just read.
     const int64_t each = fmt_bytes(l->p_fmt) + (l->bits == 8 ? 2 : 8);
-    const bool past = past_caches(l->chunks * kChunk * each);
+    const bool past = past_caches(l->values * each);
     const int split = split_of(l->chunks, past && l->bits == 8);
     const unsigned grid = static_cast<unsigned>(l->chunks * split);
     const auto kernel = l->bits == 32 ? (past ? k_adamw<P, G, kThirtyTwo, true> : k_adamw<P, G, kThirtyTwo, false>)
@@ -511,8 +512,9 @@ using namespace cs;
 
 extern "C" int cs_tensor_list_bytes(const int64_t* n, int32_t count, size_t* bytes) {
     bool ok = false;
+    int64_t values = 0;
     if (count < 0 || (count && !n) || !bytes) return CS_EINVAL;
-    const int64_t chunks = chunks_of(n, count, ok);
+    const int64_t chunks = chunks_of(n, count, values, ok);
     if (!ok || chunks >= kMaxChunks) return CS_EINVAL;
     *bytes = static_cast<size_t>(count) * sizeof(Tensor) + static_cast<size_t>(chunks) * sizeof(Chunk);
     return CS_OK;
@@ -544,7 +546,9 @@ extern "C" int cs_tensor_list_build(const int64_t* n, int32_t count, void* const
                 if (spans_meet(at[a], size[a], at[b], size[b])) return CS_EINVAL;
     }
     bool ok = false;
-    *list = cs_tensor_list{memory, chunks_of(n, count, ok), count, p_fmt, g_fmt, bits};
+    int64_t values = 0;
+    const int64_t chunks = chunks_of(n, count, values, ok);
+    *list = cs_tensor_list{memory, chunks, count, p_fmt, g_fmt, bits, values};
     if (count == 0) return CS_OK;
     Tensor* tensors = static_cast<Tensor*>(memory);
     int64_t chunk = 0;
@@ -642,7 +646,7 @@ extern "C" int cs_moments_read(const cs_tensor_list* list, void* stream) {
     if (!list_ok(list) || list->bits != 8 || list->p_fmt != CS_FMT_BF16 || list->g_fmt != CS_FMT_BF16) return CS_EINVAL;
     if (list->chunks == 0) return CS_OK;
     const List at = list_of(list);
-    const bool past = past_caches(list->chunks * kChunk * 4);
+    const bool past = past_caches(list->values * 4);
     const auto kernel = past ? k_moments<false, true> : k_moments<false, false>;
     const int split = split_of(list->chunks, list->chunks >= kReadWhole);
     kernel<<<static_cast<unsigned>(list->chunks * split), kThreads, 0, stream_of(stream)>>>(at.tensors, at.chunks, split);

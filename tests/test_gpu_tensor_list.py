@@ -34,3 +34,10 @@ def test_a_refresh_that_is_refused_changes_nothing():
     assert tensors.c.memory == tensors.memory.data_ptr() and tensors.c.count == 900
     cs.cs_adamw_step(want.h, 5, tensors)
     assert torch.equal(q[899], want.params[0])
+
+
+def test_a_list_knows_its_values():
+    """(what decides about the caches is the values, not the pieces of work, of which a tensor of one value has one)"""
+    sizes = [1, 0, 4096, 4097, 70]
+    tensors = cs.TensorList(*([torch.zeros(n, device=DEV) for n in sizes] for _ in range(4)))
+    assert tensors.c.values == sum(sizes) and tensors.c.chunks == 5
