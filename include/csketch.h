@@ -623,7 +623,8 @@ int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* 
  * filled by one of
  *   cs_adamw_advance          counts *step up (device int64) and takes lr from *lr_or_null (device double) if given
  *   cs_adamw_advance_scaled   the same, but where *grad_scale_or_null is not finite it leaves *step and coefs alone
- *   cs_grad_norm_advance      cs_grad_norm and, with its out[1] as the scale, the latter, in the launches of the former */
+ *   cs_grad_norm_advance      cs_grad_norm, and in the same launches the number and coefficients of the step that it scales: where
+ *                             out[1] is not finite *step is left alone (and coefs are those of the step that is not taken) */
 #define CS_ADAMW_COEFS 10
 typedef struct cs_adamw {
     double lr, beta1, beta2, eps, weight_decay;      /* all finite and >= 0, betas below 1 */

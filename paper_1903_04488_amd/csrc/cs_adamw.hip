@@ -357,19 +357,32 @@ __device__ __forceinline__ double block_sum(double s, double* lds) {
 }
 
 // Squares and their sums in binary64: no overflow, and nothing lost between large and small tensors.  Workgroup w takes chunks
-// w, w + gridDim, ...; a thread's four requests of a chunk are under way together.  90 M gradients in 32 bits 59 us (360 MB at 6.1
+// w, w + workers, ...; a thread's four requests of a chunk are under way together.  90 M gradients in 32 bits 59 us (360 MB at 6.1
 // TB/s), in bf16 37 (4.9).
+// ADVANCE: one workgroup more, the first, makes the coefficients of the step that these gradients are for, if it is taken.  (By a thread of
+// k_grad_norm, which nothing hides, 2 us a step.)
 constexpr int kSquares = 2048;                       // workgroups, and partial sums
-template <typename G>
+struct Counted {
+    cs_adamw h;
+    int64_t* step;
+    const double* lr;
+    Coefs* coefs;
+};
+template <typename G, bool ADVANCE>
 __global__ void __launch_bounds__(kThreads)
-k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double* partials) {
+k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double* partials, Counted counted) {
     __shared__ double lds[4];
+    if (ADVANCE && blockIdx.x == 0) {
+        if (threadIdx.x == 0) *counted.coefs = coefs_of(counted.h, counted.lr ? *counted.lr : counted.h.lr, *counted.step + 1);
+        return;
+    }
+    const unsigned worker = blockIdx.x - ADVANCE, workers = gridDim.x - ADVANCE;
     double s = 0.;
     // (where the next chunk lies is looked up while this one's values are on their way)
-    Chunk ch = chunks[blockIdx.x];
+    Chunk ch = chunks[worker];
     int64_t n = tensors[ch.tensor].n, begin = static_cast<int64_t>(ch.part) * kChunk;
     const G* g = static_cast<const G*>(tensors[ch.tensor].g);
-    for (int64_t c = blockIdx.x; c < count;) {
+    for (int64_t c = worker; c < count;) {
         constexpr int PER = kChunk / kThreads / 4;
         float v[PER][4];
         if (begin + kChunk <= n) {
@@ -379,7 +392,7 @@ k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double
 #pragma unroll
             for (int k = 0; k < PER; ++k) load4(g, begin + (k * kThreads + threadIdx.x) * 4, n, v[k]);
         }
-        c += gridDim.x;
+        c += workers;
         if (c < count) {
             ch = chunks[c];
             n = tensors[ch.tensor].n;
@@ -392,21 +405,12 @@ k_grad_squares(const Tensor* tensors, const Chunk* chunks, int64_t count, double
             for (int e = 0; e < 4; ++e) s = fma(static_cast<double>(v[k][e]), static_cast<double>(v[k][e]), s);
     }
     s = block_sum(s, lds);
-    if (threadIdx.x == 0) partials[blockIdx.x] = s;
+    if (threadIdx.x == 0) partials[worker] = s;
 }
-// ADVANCE: and the step that a norm that is finite lets be taken is counted, and its coefficients written, by a thread that has made
-// them while the others wait for memory.
-template <bool ADVANCE>
-__global__ void __launch_bounds__(kThreads)
-k_grad_norm(const double* partials, int count, double max_norm, float* out, cs_adamw h, int64_t* step, const double* lr, Coefs* coefs) {
+// step (may be null): counted up where the norm is finite
+__global__ void __launch_bounds__(kThreads) k_grad_norm(const double* partials, int count, double max_norm, float* out, int64_t* step) {
     __shared__ double lds[4];
-    constexpr int kCounts = 64;                       // (of another wavefront than the one that writes the norm)
-    int64_t t = 0;
-    Coefs now = {};
-    if (ADVANCE && threadIdx.x == kCounts) {
-        t = *step + 1;
-        now = coefs_of(h, lr ? *lr : h.lr, t);
-    }
+    const int64_t steps = step && threadIdx.x == 0 ? *step : 0;
     double v[kSquares / kThreads], s = 0.;
 #pragma unroll
     for (int k = 0; k < kSquares / kThreads; ++k) {
@@ -416,14 +420,11 @@ k_grad_norm(const double* partials, int count, double max_norm, float* out, cs_a
 #pragma unroll
     for (int k = 0; k < kSquares / kThreads; ++k) s += v[k];
     s = block_sum(s, lds);
+    if (threadIdx.x) return;
     // (finite as it is told, in binary32)
     const double norm = sqrt(s), c = max_norm / (norm + 1e-6);
     const bool finite = static_cast<float>(norm) < INFINITY;
-    if (ADVANCE && threadIdx.x == kCounts && finite) {
-        *step = t;
-        *coefs = now;
-    }
-    if (threadIdx.x) return;
+    if (step && finite) *step = steps + 1;
     out[0] = static_cast<float>(norm);
     out[1] = finite ? static_cast<float>(c < 1. ? c : 1.) : NAN;
 }
@@ -591,15 +592,16 @@ int grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* wor
     double* partials = static_cast<double*>(workspace);
     const int grid = partials_of(list);
     const hipStream_t s = stream_of(stream);
-    if (grid) {
-        const auto kernel = list->g_fmt == CS_FMT_F32    ? k_grad_squares<float>
-                            : list->g_fmt == CS_FMT_BF16 ? k_grad_squares<bf16>
-                                                         : k_grad_squares<f16>;
-        kernel<<<grid, kThreads, 0, s>>>(at.tensors, at.chunks, list->chunks, partials);
+    if (grid || step) {
+        const auto kernel = list->g_fmt == CS_FMT_F32    ? (step ? k_grad_squares<float, true> : k_grad_squares<float, false>)
+                            : list->g_fmt == CS_FMT_BF16 ? (step ? k_grad_squares<bf16, true> : k_grad_squares<bf16, false>)
+                                                         : (step ? k_grad_squares<f16, true> : k_grad_squares<f16, false>);
+        kernel<<<grid + (step != nullptr), kThreads, 0, s>>>(
+            at.tensors, at.chunks, list->chunks, partials,
+            step ? Counted{*h, step, lr, reinterpret_cast<Coefs*>(coefs)} : Counted{});
         if (int rc = launched()) return rc;
     }
-    if (step) k_grad_norm<true><<<1, kThreads, 0, s>>>(partials, grid, max_norm, out, *h, step, lr, reinterpret_cast<Coefs*>(coefs));
-    else k_grad_norm<false><<<1, kThreads, 0, s>>>(partials, grid, max_norm, out, cs_adamw{}, nullptr, nullptr, nullptr);
+    k_grad_norm<<<1, kThreads, 0, s>>>(partials, grid, max_norm, out, step);
     return launched();
 }
 
