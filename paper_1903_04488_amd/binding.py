@@ -1111,6 +1111,21 @@ def cs_adamw_advance(h: CsAdamw, step, coefs, lr=None, grad_scale=None):
 
 def cs_grad_norm_advance(tensors: TensorList, max_norm: float, out, workspace, h: CsAdamw, step, coefs, lr=None):
     """cs_grad_norm, and cs_adamw_advance where the norm is finite"""
+    f32, lib = torch.float32, _lib or load_library()
+    try:
+        if (out.dtype is f32 and out.is_cuda and out.is_contiguous() and out.numel() == 2
+                and workspace.dtype is torch.uint8 and workspace.is_cuda and workspace.is_contiguous()
+                and step.dtype is torch.int64 and step.is_cuda and step.numel() == 1
+                and coefs.dtype is f32 and coefs.is_cuda and coefs.is_contiguous() and coefs.numel() == CS_ADAMW_COEFS
+                and (lr is None or lr.dtype is torch.float64 and lr.is_cuda and lr.numel() == 1)):
+            status = lib.cs_grad_norm_advance(
+                tensors.c, max_norm, out.data_ptr(), workspace.data_ptr(), workspace.numel(), h, step.data_ptr(),
+                None if lr is None else lr.data_ptr(), coefs.data_ptr(), _stream(tensors.memory))
+            if status:
+                _check(status, "cs_grad_norm_advance")
+            return
+    except (AttributeError, TypeError):
+        pass
     _check(load_library().cs_grad_norm_advance(
         ctypes.byref(tensors.c), max_norm, _dev(out, torch.float32, "out", 2), _dev(workspace, torch.uint8, "workspace"),
         workspace.numel(), ctypes.byref(h), _dev(step, torch.int64, "step", 1), _maybe(lr, torch.float64, "lr", 1),
@@ -1118,6 +1133,18 @@ def cs_grad_norm_advance(tensors: TensorList, max_norm: float, out, workspace, h
 
 
 def cs_adamw_step(h: CsAdamw, step: int, tensors: TensorList, coefs=None, grad_scale=None):
+    f32 = torch.float32
+    try:
+        if ((coefs is None or coefs.dtype is f32 and coefs.is_cuda and coefs.is_contiguous() and coefs.numel() == CS_ADAMW_COEFS)
+                and (grad_scale is None or grad_scale.dtype is f32 and grad_scale.is_cuda and grad_scale.numel() == 1)):
+            status = (_lib or load_library()).cs_adamw_step(
+                h, step, tensors.c, None if coefs is None else coefs.data_ptr(), None if grad_scale is None else grad_scale.data_ptr(),
+                _stream(tensors.memory))
+            if status:
+                _check(status, "cs_adamw_step")
+            return
+    except (AttributeError, TypeError):
+        pass
     _check(load_library().cs_adamw_step(
         ctypes.byref(h), step, ctypes.byref(tensors.c), _maybe(coefs, torch.float32, "coefs", CS_ADAMW_COEFS),
         _maybe(grad_scale, torch.float32, "grad_scale", 1), _stream(tensors.memory)), "cs_adamw_step")

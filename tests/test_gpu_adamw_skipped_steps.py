@@ -127,3 +127,34 @@ def test_the_coefficients_of_a_late_step(t):
     c1, c2 = 1 / -math.expm1(t * math.log(h.beta1)), 1 / math.sqrt(-math.expm1(t * math.log(h.beta2)))
     for a, b in zip(got, (0.9, 1 - 0.9, 0.999, 1 - 0.999, 1 - 1e-3 * 0.01, c2, 1e-3 * c1, 1e-8)):
         assert a == pytest.approx(b, rel=2 * U)
+
+
+def test_every_argument_is_checked():
+    opt = optimizer(capturable=True)
+    good = [opt._norm_and_scale, opt._workspace, opt.step_now, opt.coefs, opt.lr_now]
+
+    def norm(out, ws, step, coefs, lr):
+        cs.cs_grad_norm_advance(opt.list, 1.0, out, ws, opt.h, step, coefs, lr)
+
+    def wrong(a):
+        return [7, a.cpu(), a.to(torch.float16), torch.cat([a, a]), a[:0], torch.cat([a, a, a])[::3]]
+
+    for i, a in enumerate(good):
+        for bad in wrong(a):
+            if i == 1 and isinstance(bad, torch.Tensor) and bad.is_cuda and bad.dtype == torch.uint8 and bad.is_contiguous() and len(bad):
+                continue                                 # (a workspace may have any size that is enough)
+            if isinstance(bad, torch.Tensor) and bad.is_cuda and bad.shape == a.shape and bad.dtype == a.dtype and bad.is_contiguous():
+                continue                                 # (of one value every third one is the value)
+            with pytest.raises(cs.CsError):
+                norm(*good[:i], bad, *good[i + 1:])
+    for i, a in enumerate((opt.coefs, opt._scale)):
+        for bad in wrong(a):
+            if isinstance(bad, torch.Tensor) and bad.is_cuda and bad.shape == a.shape and bad.dtype == a.dtype and bad.is_contiguous():
+                continue
+            with pytest.raises(cs.CsError):
+                cs.cs_adamw_step(opt.h, 1, opt.list, *((bad, opt._scale) if i == 0 else (opt.coefs, bad)))
+    before = state(opt)
+    with pytest.raises(cs.CsError):
+        cs.cs_adamw_step(cs.CsAdamw(-1.0, 0.9, 0.9, 0.0, 0.0), 1, opt.list, opt.coefs, opt._scale)
+    norm(*good)
+    assert opt.steps == 1 and all(torch.equal(x, y) for x, y in zip(before, state(opt)))
