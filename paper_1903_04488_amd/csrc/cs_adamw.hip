@@ -467,8 +467,8 @@ List list_of(const cs_tensor_list* l) {
     return List{t, reinterpret_cast<const Chunk*>(t + l->count)};
 }
 // Workgroups that share a chunk: four, a block of 256 values a wavefront, so that none waits for memory four times in a row; but of
-// moments in 8 bits that go past the caches one (us a step, one / four: 0.64 M parameters, 8 bits 15.1 / 12.0; 11.5 M, 32 bits 69 / 63;
-// 90 M, 32 bits with clipping 474 / 461; 30 M, 8 bits 141 / 132; 52 M, 8 bits, past the caches 212 / 234).
+// moments in 8 bits that go past the caches one (us a step, one / four: 0.64 M parameters, 8 bits 15.1 / 11.7; 11.5 M, 32 bits 69 / 63;
+// 90 M, 32 bits with clipping 474 / 462; 30 M, 8 bits 141 / 132; 52 M, 8 bits, past the caches 212 / 234).
 // A launch has fewer than 2^32 threads: a list of 2^22 chunks or more is not split.
 int split_of(int64_t chunks, bool one) { return one || chunks * 4 >= kMaxChunks ? 1 : 4; }
 int partials_of(const cs_tensor_list* l) { return static_cast<int>(l->chunks < kSquares ? l->chunks : kSquares); }

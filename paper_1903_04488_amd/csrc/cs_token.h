@@ -41,7 +41,8 @@ inline int32_t packs_of(int64_t vocab, int32_t fmt) {
 }
 // Workgroups of 256 threads take a row each where there are enough rows; few rows have workgroups of 1024 (us, 1000 x 60000 bf16
 // 26 / 30 with 256; 1500 x 60000 36 / 35), and long ones of them are shared by several (1 x 130000 bf16 in 3 parts 10; a part
-// of less than 32768 values costs more for the join than it saves: 1 x 32768 f32 with alternatives 41 in 8 parts).
+// of less than 32768 values cost more for the join than it saved when rows were not held yet: 1 x 32768 f32 with alternatives 41 in 8
+// parts, which is 10 in one held row now; smaller parts of held rows have not been measured).
 inline bool few_rows(int64_t rows) { return rows < 1024; }
 inline int parts_of(int64_t rows, int64_t vocab) {
     if (!few_rows(rows)) return 1;

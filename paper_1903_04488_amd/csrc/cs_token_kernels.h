@@ -259,7 +259,8 @@ __device__ __forceinline__ void rank_list(const uint64_t* list, int32_t n, int t
 // The `top` largest of packs [first, last) of a row, in order, by emit(rank, key).  A thread (of a wavefront that has the row
 // to itself) or four neighbouring ones are a unit; of the
 // units' largest values the top-th in order (equal ones: lower pack first) is a bound that `top` values reach, so the
-// largest are among the values of the `top` units before it that reach it too: usually hardly more than `top` values, which
+// largest are among the values of the `top` units before it that reach it too: few more than `top` values where `top` is well below the
+// 64 units (at 48 and more a wavefront's row mostly has more than are listed), which
 // those threads list and which are then ranked by counting.  The bound is found bit by bit, in every wavefront by itself, a
 // unit (or four) a lane.
 template <typename T, int THREADS, bool HELD, typename Row, typename Emit>
