@@ -618,7 +618,7 @@ int cs_grad_norm(const cs_tensor_list* list, double max_norm, float* out, void* 
  * in binary32, every operation rounded by itself in this order (constants in binary64, rounded once); p takes the
  * moments as they are before they are rounded to 8 bits.  s: 1, or *grad_scale_or_null (device: clipping, loss scale); where
  * that is not finite nothing is written.  Such a step is none, and the next one's number is the same.
- * coefs_or_null: device float[CS_ADAMW_COEFS], in place of step and of what h says, where the number of the step lives on the GPU (steps
+ * coefs_or_null: device float[CS_ADAMW_COEFS], in place of step and of what h says (but for whether it has a seed), where the number of the step lives on the GPU (steps
  * that are replayed from a graph; steps that are not taken where their scale is not finite, which the host does not see).  They are
  * filled by one of
  *   cs_adamw_advance          counts *step up (device int64) and takes lr from *lr_or_null (device double) if given
@@ -631,8 +631,8 @@ typedef struct cs_adamw {
     uint64_t seed;                                   /* of the rounding of moments in 8 bits; 0: to nearest */
 } cs_adamw;
 /* Moments in 8 bits over many steps.  Rounded to nearest (seed 0) a moment stands still wherever a step changes it by less than half
- * a step of its code: with beta2 above 0.938 a root never gets smaller again, and at 0.999 it does not grow to what it should be
- * either.  That is for single steps, and for moments that another program rounds so.
+ * a step of its code: with beta2 above 0.938 a root stops falling at some of its codes, above 0.968 at all of them, and at 0.999 it does
+ * not grow to what it should be either.  That is for single steps, and for moments that another program rounds so.
  * With a seed: let p be where a value lies on the line of codes of its block (p = c at code c's value, and in between in proportion), and
  * q the whole number next to p (halves up).  If the moment as it was before the step is not 0 and has the same q in this block, then
  * c is floor(p + (r + 1/2) / 2^16), r one of 2^16 numbers that are as likely: up or down, right on average.  If a c of the block is
