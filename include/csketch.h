@@ -654,6 +654,104 @@ int cs_adamw_step(const cs_adamw* h, int64_t step, const cs_tensor_list* list, c
 int cs_moments_read(const cs_tensor_list* list, void* stream);
 int cs_moments_write(const cs_tensor_list* list, void* stream);
 
+/* Losses of answers, for training on them.  Log probabilities are float[tokens] as cs_token_logprobs gives them.
+ *
+ * Clipped policy loss.  Of a token with log probability l, entropy H, log probability l0 when it was drawn and l1 under a
+ * reference, advantage A and weight w (1 / tokens for a mean; 0 leaves a token out, whatever its values):
+ *     r = exp(l - l0),  S = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A),  K = exp(l1 - l) - (l1 - l) - 1
+ *     loss = w (-S + kl K - entropy H),  g_logp = -w ([S = r A] r A + kl (exp(l1 - l) - 1)),  g_entropy = -w entropy
+ * (log probabilities that are the same infinity are 0 apart; an exponential beyond binary32 is infinite).
+ * sums: device float[4] or NULL: of loss, of w K (0 where kl is 0), of w over the tokens where clipping decides, of w; binary64 in a fixed
+ * order, rounded once.
+ * 0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl, entropy: finite. */
+typedef struct cs_policy {
+    float clip_low, clip_high, kl, entropy;
+} cs_policy;
+/* From log probabilities.  entropy_or_null is not read where h->entropy is 0, ref_logp_or_null not where h->kl is 0.  loss, g_logp,
+ * g_entropy: device float[rows], each may be NULL.  workspace: device, 8-byte aligned. */
+int cs_policy_workspace_bytes(int64_t rows, size_t* bytes);
+int cs_policy_loss(const cs_policy* h, int64_t rows, const float* logp, const float* entropy_or_null, const float* old_logp,
+                   const float* ref_logp_or_null, const float* advantage, const float* weight, float* loss, float* g_logp, float* g_entropy,
+                   float* sums, void* workspace, size_t ws_bytes, void* stream);
+/* From logits, with their gradient: cs_token_logprobs, cs_policy_loss and cs_token_logprobs_grad of them in one call, which reads the
+ * logits once where a workgroup holds a row.  Rows whose target is outside [0, vocab) have weight 0; an empty row's gradient is 0.  loss may be
+ * NULL, sums too, dlogits may be the logits (same stride). */
+int cs_token_policy_workspace_bytes(int64_t rows, int64_t vocab, size_t* bytes);
+int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale,
+                         const int64_t* target, const float* old_logp, const float* ref_logp_or_null, const float* advantage,
+                         const float* weight, float* logp, float* entropy, float* lse, float* loss, float* sums, void* dlogits,
+                         int64_t d_stride, void* workspace, size_t ws_bytes, void* stream);
+
+/* Loss of pairs of answers.  Answers are packed after one another: answer a has the tokens [begin[a], begin[a + 1]) (device
+ * int64[2 pairs + 1], ascending; what leaves [0, tokens] is cut off there); answers 0 .. pairs - 1 are the chosen ones, the next `pairs` the rejected
+ * ones, in the same order.  With R = beta times the sum of l - l1 over an answer's tokens that count (mean: by their number; of no
+ * token: 0) and z = R_chosen - R_rejected - margin, a pair's loss is
+ *     CS_PREFERENCE_LOGISTIC  (1 - smoothing) ln(1 + exp(-z)) + smoothing ln(1 + exp(z))
+ *     CS_PREFERENCE_HINGE     max(0, 1 - z)
+ *     CS_PREFERENCE_SQUARE    ((z - 1/2) / beta)^2
+ * logp, ref_logp_or_null (0): float[tokens].  counts_or_null: device uint8[tokens], 0 leaves a token out, whatever its values.
+ * weight_or_null (1): float[pairs], a pair of weight 0 has no gradient.  loss: float[pairs], without the weight; reward: float[2 pairs], R.
+ * g_logp: float[tokens] or NULL, the gradient of the sum of weight times loss: 0 for tokens that are left out; tokens of no answer are left as
+ * they were.  sums: float[3], of weight loss, of the weight of pairs with R_chosen > R_rejected, of weight (R_chosen - R_rejected); sums are
+ * binary64 in a fixed order, rounded once.  pairs < 2^22.  workspace: device, 8-byte aligned. */
+#define CS_PREFERENCE_LOGISTIC 0
+#define CS_PREFERENCE_HINGE 1
+#define CS_PREFERENCE_SQUARE 2
+typedef struct cs_preference {
+    int32_t kind, mean;
+    float beta, smoothing, margin;           /* beta > 0, 0 <= smoothing <= 1 (logistic alone) */
+} cs_preference;
+int cs_preference_workspace_bytes(int64_t tokens, int64_t pairs, size_t* bytes);
+int cs_preference_loss(const cs_preference* h, int64_t tokens, int64_t pairs, const float* logp, const float* ref_logp_or_null,
+                       const uint8_t* counts_or_null, const int64_t* begin, const float* weight_or_null, float* loss, float* reward,
+                       float* g_logp, float* sums, void* workspace, size_t ws_bytes, void* stream);
+
+/* Matrices orthogonalised by Newton-Schulz products: X = u / (|u|_F + eps), then `steps` times
+ *     A = X X^T,  X = a X + (b A + c A A) X          ((a, b, c) = coefs[step]; of a matrix with more rows than columns with u^T)
+ * which maps singular values s to a s + b s^3 + c s^5 and leaves the singular vectors.  The coefficients have to keep singular values
+ * of at most 1 below 2 and b s^2, c s^4 below 60 (CS_EINVAL).  A matrix of zeros stays one; a NaN or infinity makes its whole matrix NaN.
+ * terms: what the products take of their factors (sums are binary32).  1: binary16; X itself and the diagonals, which go past the products,
+ * are kept longer, and the result is about 2^-10 off: for results of 16 bits.  2: two binary16 (22 bits), as exact as products in binary32.
+ *
+ * Stacks of matrices, all for the same launches: `count` matrices of rows x cols each, p_step and g_step values apart (0 will do for one), their
+ * rows p_stride and g_stride apart; m: [count][rows][cols] without gaps, or NULL (in all stacks) for a list of cs_orthogonalize, where p may
+ * be g itself.  rows, cols <= 2^20, the shorter of both <= 2^15.  cs_matrix_list_build writes a list into `memory` (device,
+ * cs_matrix_list_bytes, 8-byte aligned); it holds while the tensors stay where they are, and is built again when they move.  Different
+ * matrices must lie apart, as must the arrays of one stack (the latter is checked). */
+typedef struct cs_matrix {
+    void* p;
+    const void* g;
+    float* m;
+    int64_t count, rows, cols, p_stride, p_step, g_stride, g_step;
+} cs_matrix;
+typedef struct cs_matrix_list {
+    void* memory;                            /* device */
+    int64_t matrices, pieces, halves, fulls, work;
+    int32_t p_fmt, g_fmt, terms, tile, moments;
+} cs_matrix_list;
+int cs_matrix_list_bytes(const cs_matrix* stacks, int32_t count, int32_t terms, size_t* bytes);
+int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int32_t p_fmt, int32_t g_fmt, int32_t terms, void* memory, size_t bytes,
+                         cs_matrix_list* list, void* stream);
+/* One step of the optimizer that updates matrices by their orthogonalised momentum:
+ *     m = momentum m + s g,  u = s g + momentum m (nesterov) or m,  p = p (1 - lr weight_decay) - lr scale X(u)
+ * scale: CS_MUON_SCALE_SHAPE sqrt(max(1, rows / cols)), CS_MUON_SCALE_RMS 0.2 sqrt(max(rows, cols)), CS_MUON_SCALE_ONE 1.
+ * s: 1, or *grad_scale_or_null (device); where that is not finite nothing is written.  lr: h->lr, or *lr_or_null (device double).
+ * cs_orthogonalize: p = X(g) (of h it takes eps, steps and coefs).
+ * workspace: device, cs_muon_workspace_bytes, 16-byte aligned; its contents do not outlive the call. */
+#define CS_MUON_MAX_STEPS 16
+#define CS_MUON_SCALE_SHAPE 0
+#define CS_MUON_SCALE_RMS 1
+#define CS_MUON_SCALE_ONE 2
+typedef struct cs_muon {
+    double lr, momentum, weight_decay, eps;  /* all finite and >= 0, momentum below 1 */
+    int32_t nesterov, scale, steps, reserved;
+    double coefs[CS_MUON_MAX_STEPS][3];
+} cs_muon;
+int cs_muon_workspace_bytes(const cs_matrix_list* list, size_t* bytes);
+int cs_muon_step(const cs_muon* h, const cs_matrix_list* list, const double* lr_or_null, const float* grad_scale_or_null, void* workspace,
+                 size_t ws_bytes, void* stream);
+int cs_orthogonalize(const cs_muon* h, const cs_matrix_list* list, void* workspace, size_t ws_bytes, void* stream);
+
 const char* cs_status_string(int status);
 
 #ifdef __cplusplus

@@ -91,6 +91,37 @@ class CsAdamw(ctypes.Structure):
     _fields_ = [*((name, ctypes.c_double) for name in ("lr", "beta1", "beta2", "eps", "weight_decay")), ("seed", ctypes.c_uint64)]
 
 
+class CsPolicy(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_float) for name in ("clip_low", "clip_high", "kl", "entropy")]
+
+
+CS_PREFERENCE_LOGISTIC, CS_PREFERENCE_HINGE, CS_PREFERENCE_SQUARE = 0, 1, 2
+
+
+class CsPreference(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("mean", ctypes.c_int32), *((name, ctypes.c_float) for name in ("beta", "smoothing", "margin"))]
+
+
+CS_MUON_MAX_STEPS = 16
+CS_MUON_SCALE_SHAPE, CS_MUON_SCALE_RMS, CS_MUON_SCALE_ONE = 0, 1, 2
+
+
+class CsMatrix(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                *((name, ctypes.c_int64) for name in ("count", "rows", "cols", "p_stride", "p_step", "g_stride", "g_step"))]
+
+
+class CsMatrixList(ctypes.Structure):
+    _fields_ = [("memory", ctypes.c_void_p), *((name, ctypes.c_int64) for name in ("matrices", "pieces", "halves", "fulls", "work")),
+                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "tile", "moments"))]
+
+
+class CsMuon(ctypes.Structure):
+    _fields_ = [*((name, ctypes.c_double) for name in ("lr", "momentum", "weight_decay", "eps")),
+                *((name, ctypes.c_int32) for name in ("nesterov", "scale", "steps", "reserved")),
+                ("coefs", ctypes.c_double * 3 * CS_MUON_MAX_STEPS)]
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -236,6 +267,21 @@ _SIGNATURES = {
     "cs_adamw_advance_scaled": [ctypes.POINTER(CsAdamw), *[ctypes.c_void_p] * 5],
     "cs_grad_norm_advance": [ctypes.POINTER(CsTensorList), ctypes.c_double, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
                              ctypes.POINTER(CsAdamw), *[ctypes.c_void_p] * 4],
+    "cs_policy_workspace_bytes": [ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_policy_loss": [ctypes.POINTER(CsPolicy), ctypes.c_int64, *[ctypes.c_void_p] * 11, ctypes.c_size_t, ctypes.c_void_p],
+    "cs_token_policy_workspace_bytes": [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_token_policy_loss": [ctypes.POINTER(CsPolicy), ctypes.c_void_p, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int32,
+                             ctypes.c_float, *[ctypes.c_void_p] * 11, ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
+    "cs_preference_workspace_bytes": [ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_preference_loss": [ctypes.POINTER(CsPreference), ctypes.c_int64, ctypes.c_int64, *[ctypes.c_void_p] * 10, ctypes.c_size_t,
+                           ctypes.c_void_p],
+    "cs_matrix_list_bytes": [ctypes.POINTER(CsMatrix), ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)],
+    "cs_matrix_list_build": [ctypes.POINTER(CsMatrix), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                             ctypes.c_size_t, ctypes.POINTER(CsMatrixList), ctypes.c_void_p],
+    "cs_muon_workspace_bytes": [ctypes.POINTER(CsMatrixList), ctypes.POINTER(ctypes.c_size_t)],
+    "cs_muon_step": [ctypes.POINTER(CsMuon), ctypes.POINTER(CsMatrixList), ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                     ctypes.c_size_t, ctypes.c_void_p],
+    "cs_orthogonalize": [ctypes.POINTER(CsMuon), ctypes.POINTER(CsMatrixList), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
     "cs_adamw_step": [ctypes.POINTER(CsAdamw), ctypes.c_int64, ctypes.POINTER(CsTensorList), *[ctypes.c_void_p] * 3],
     "cs_moments_read": [ctypes.POINTER(CsTensorList), ctypes.c_void_p],
     "cs_moments_write": [ctypes.POINTER(CsTensorList), ctypes.c_void_p],
@@ -1156,3 +1202,170 @@ def cs_moments_read(tensors: TensorList):
 
 def cs_moments_write(tensors: TensorList):
     _check(load_library().cs_moments_write(ctypes.byref(tensors.c), _stream(tensors.memory)), "cs_moments_write")
+
+
+# ------------------------------------------------------------------------------------------
+# losses of answers, orthogonalised momentum
+def _same_gpu(like, **tensors):
+    """the address of every tensor (None: no address): (tensor, dtype, length or None) each, on the GPU of `like`"""
+    index = like.get_device()
+    out = []
+    for name, (t, dtype, numel) in tensors.items():
+        if t is None:
+            out.append(None)
+            continue
+        out.append(_dev(t, dtype, name, numel))
+        if t.get_device() != index:
+            raise CsError(f"{name} must be on the same GPU as the others")
+    return out
+
+
+def cs_policy_workspace_bytes(rows: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_policy_workspace_bytes(rows, ctypes.byref(n)), "cs_policy_workspace_bytes")
+    return n.value
+
+
+def _needed(h: CsPolicy, **tensors):
+    for name, t in tensors.items():
+        if t is None:
+            raise CsError(f"{name} must be given")
+
+
+def cs_policy_loss(h: CsPolicy, logp, entropy, old_logp, ref_logp, advantage, weight, loss, g_logp, g_entropy, sums, workspace):
+    """all [rows] float32 but sums [4]; entropy may be None where h.entropy is 0, ref_logp where h.kl is 0, an output where it is not
+    wanted"""
+    f32 = torch.float32
+    _dev(logp, f32, "logp")
+    _needed(h, old_logp=old_logp, advantage=advantage, weight=weight, workspace=workspace)
+    n = logp.numel()
+    at = _same_gpu(logp, logp=(logp, f32, n), entropy=(entropy, f32, n), old_logp=(old_logp, f32, n), ref_logp=(ref_logp, f32, n),
+                   advantage=(advantage, f32, n), weight=(weight, f32, n), loss=(loss, f32, n), g_logp=(g_logp, f32, n),
+                   g_entropy=(g_entropy, f32, n), sums=(sums, f32, 4), workspace=(workspace, torch.uint8, None))
+    _check(load_library().cs_policy_loss(h, n, *at, workspace.numel(), _stream(logp)), "cs_policy_loss")
+
+
+def cs_token_policy_workspace_bytes(rows: int, vocab: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_token_policy_workspace_bytes(rows, vocab, ctypes.byref(n)), "cs_token_policy_workspace_bytes")
+    return n.value
+
+
+def cs_token_policy_loss(h: CsPolicy, logits, target, old_logp, ref_logp, advantage, weight, logp, entropy, lse, loss, sums, dlogits,
+                         workspace, scale: float = 1.0):
+    """logits, dlogits: [rows, vocab]; the rest as for cs_token_loss and cs_policy_loss; loss and sums may be None"""
+    f32 = torch.float32
+    at, step = _rows(logits, "logits")
+    out, out_step = _rows(dlogits, "dlogits", logits)
+    rows, vocab = logits.shape
+    _needed(h, target=target, old_logp=old_logp, advantage=advantage, weight=weight, logp=logp, entropy=entropy, lse=lse,
+            workspace=workspace)
+    if dlogits.get_device() != logits.get_device():
+        raise CsError("dlogits must be on the same GPU as the others")
+    t, old, ref, a, w, lp, ent, ls, lo, su, ws = _same_gpu(
+        logits, target=(target, torch.int64, rows), old_logp=(old_logp, f32, rows), ref_logp=(ref_logp, f32, rows),
+        advantage=(advantage, f32, rows), weight=(weight, f32, rows), logp=(logp, f32, rows), entropy=(entropy, f32, rows),
+        lse=(lse, f32, rows), loss=(loss, f32, rows), sums=(sums, f32, 4), workspace=(workspace, torch.uint8, None))
+    _check(load_library().cs_token_policy_loss(
+        h, at, rows, vocab, step, _FMT[logits.dtype], scale, t, old, ref, a, w, lp, ent, ls, lo, su, out, out_step, ws,
+        workspace.numel(), _stream(logits)), "cs_token_policy_loss")
+
+
+def cs_preference_workspace_bytes(tokens: int, pairs: int) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_preference_workspace_bytes(tokens, pairs, ctypes.byref(n)), "cs_preference_workspace_bytes")
+    return n.value
+
+
+def cs_preference_loss(h: CsPreference, logp, ref_logp, counts, begin, weight, loss, reward, g_logp, sums, workspace):
+    """logp, ref_logp (or None), g_logp (or None): [tokens] float32; counts: [tokens] bool or uint8, or None; begin: [2 pairs + 1] int64;
+    weight (or None), loss: [pairs] float32; reward: [2 pairs], sums: [3] float32"""
+    f32 = torch.float32
+    _dev(logp, f32, "logp")
+    _dev(begin, torch.int64, "begin")
+    _needed(h, loss=loss, reward=reward, sums=sums, workspace=workspace)
+    if begin.numel() % 2 == 0:
+        raise CsError(f"begin must have 2 pairs + 1 values, got {begin.numel()}")
+    n, pairs = logp.numel(), begin.numel() // 2
+    kind = torch.bool if isinstance(counts, torch.Tensor) and counts.dtype is torch.bool else torch.uint8
+    at = _same_gpu(logp, logp=(logp, f32, n), ref_logp=(ref_logp, f32, n), counts=(counts, kind, n), begin=(begin, torch.int64, None),
+                   weight=(weight, f32, pairs), loss=(loss, f32, pairs), reward=(reward, f32, 2 * pairs), g_logp=(g_logp, f32, n),
+                   sums=(sums, f32, 3), workspace=(workspace, torch.uint8, None))
+    _check(load_library().cs_preference_loss(h, n, pairs, *at, workspace.numel(), _stream(logp)), "cs_preference_loss")
+
+
+def _stack(t, name: str, dtype, shape=None):
+    """(address, count, rows, cols, row stride, matrix step) of a matrix or a stack of matrices whose rows are contiguous"""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise CsError(f"{name} must be a tensor on the GPU")
+    if t.dtype is not dtype:
+        raise CsError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.dim() not in (2, 3) or (shape is not None and t.shape != shape):
+        raise CsError(f"{name} must have " + ("two or three dimensions" if shape is None else f"shape {tuple(shape)}") + f", got {tuple(t.shape)}")
+    count, rows, cols = (1, *t.shape) if t.dim() == 2 else t.shape
+    step, (stride, one) = (0 if t.dim() == 2 else t.stride(0)), t.stride()[-2:]
+    if t.numel() == 0:
+        return t.data_ptr(), count, rows, cols, cols, rows * cols
+    if one != 1 and cols > 1:
+        raise CsError(f"{name} must have contiguous rows")
+    stride, step = stride if rows > 1 else cols, step if count > 1 else 0
+    if stride < cols or (count > 1 and step < (rows - 1) * stride + cols):
+        raise CsError(f"{name} must have rows and matrices that do not overlap, one matrix after the other")
+    return t.data_ptr(), count, rows, cols, stride, step
+
+
+class MatrixList:
+    """Matrices, or stacks of them ([count, rows, cols]), checked once and laid out on the GPU for the same launches over all of them
+    (cs_matrix_list_build).  p: what is written; g: gradients, or what is orthogonalised; m: moments (float32, contiguous) or None.  terms: 1 or
+    2, how much of their factors the products take.  Holds the tensors; `refresh` where some have moved."""
+
+    def __init__(self, p, g, m=None, terms: int = 1):
+        self.memory, self.terms = None, terms
+        self.c = CsMatrixList()
+        self.refresh(p, g, m)
+
+    def refresh(self, p, g, m=None):
+        p, g, m = list(p), list(g), None if m is None else list(m)
+        if len(g) != len(p) or (m is not None and len(m) != len(p)):
+            raise CsError(f"p, g and m must have {len(p)} tensors each")
+        p_type, g_type = _same_dtype(p, "p"), _same_dtype(g, "g")
+        stacks = (CsMatrix * len(p))()
+        for i in range(len(p)):
+            at, count, rows, cols, p_stride, p_step = _stack(p[i], f"p[{i}]", p_type)
+            g_at, *_, g_stride, g_step = _stack(g[i], f"g[{i}]", g_type, p[i].shape)
+            moment = None
+            if m is not None:
+                moment = _dev(m[i], torch.float32, f"m[{i}]", p[i].numel())
+                if m[i].shape != p[i].shape:
+                    raise CsError(f"m[{i}] must have shape {tuple(p[i].shape)}, got {tuple(m[i].shape)}")
+            stacks[i] = CsMatrix(at, g_at, moment, count, rows, cols, p_stride, p_step, g_stride, g_step)
+        device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
+        if any(t.device != device for t in p + g + (m or [])):
+            raise CsError("the tensors of a list must be on one GPU")
+        need, c = ctypes.c_size_t(), CsMatrixList()
+        _check(load_library().cs_matrix_list_bytes(stacks, len(p), self.terms, ctypes.byref(need)), "cs_matrix_list_bytes")
+        memory = self.memory
+        if memory is None or memory.numel() < need.value or memory.device != device:
+            memory = torch.empty(need.value, dtype=torch.uint8, device=device)
+        _check(load_library().cs_matrix_list_build(stacks, len(p), _FMT[p_type], _FMT[g_type], self.terms, memory.data_ptr(), memory.numel(),
+                                                   ctypes.byref(c), _stream(memory)), "cs_matrix_list_build")
+        # (only now: a list that could not be built anew is the one that it was)
+        self.device, self.memory, self.c, self.tensors = device, memory, c, (p, g, m)
+
+
+def cs_muon_workspace_bytes(matrices: MatrixList) -> int:
+    n = ctypes.c_size_t()
+    _check(load_library().cs_muon_workspace_bytes(matrices.c, ctypes.byref(n)), "cs_muon_workspace_bytes")
+    return n.value
+
+
+def cs_muon_step(h: CsMuon, matrices: MatrixList, workspace, lr=None, grad_scale=None):
+    """lr: float64 tensor of one value in place of h.lr; grad_scale: float32 tensor of one value"""
+    lr_at, scale_at, ws = _same_gpu(matrices.memory, lr=(lr, torch.float64, 1), grad_scale=(grad_scale, torch.float32, 1),
+                                    workspace=(workspace, torch.uint8, None))
+    _check(load_library().cs_muon_step(h, matrices.c, lr_at, scale_at, ws, workspace.numel(), _stream(matrices.memory)), "cs_muon_step")
+
+
+def cs_orthogonalize(h: CsMuon, matrices: MatrixList, workspace):
+    ws, = _same_gpu(matrices.memory, workspace=(workspace, torch.uint8, None))
+    _check(load_library().cs_orthogonalize(h, matrices.c, ws, workspace.numel(), _stream(matrices.memory)), "cs_orthogonalize")

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libcsketch.so")
 SOURCES = ["cs_host.cpp", "cs_kernels.hip", "cs_lattice.hip", "cs_walk.hip", "cs_topk.hip", "cs_index.hip",
-           "cs_norm.hip", "cs_token.hip", "cs_token_f32.hip", "cs_token_bf16.hip", "cs_token_f16.hip", "cs_adamw.hip"]
+           "cs_norm.hip", "cs_token.hip", "cs_token_f32.hip", "cs_token_bf16.hip", "cs_token_f16.hip", "cs_adamw.hip",
+           "cs_policy.hip", "cs_muon.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "-shared",

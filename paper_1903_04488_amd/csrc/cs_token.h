@@ -5,6 +5,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "cs_policy.h"
 #include "cs_rows.h"
 #include "csketch.h"
 
@@ -76,9 +77,12 @@ struct TokenArgs {
     void* dlogits;
     int64_t d_stride;
     hipStream_t stream;
+    // kTokenPolicy: its inputs, losses and sums; the gradients of logp and entropy where rows are not held
+    PolicyIn policy;
+    PolicyOut policy_out;
 };
 
-enum TokenCall { kTokenForward, kTokenGrad, kTokenLoss };
+enum TokenCall { kTokenForward, kTokenGrad, kTokenLoss, kTokenPolicy };
 int token_f32(TokenCall call, const TokenArgs& a);
 int token_bf16(TokenCall call, const TokenArgs& a);
 int token_f16(TokenCall call, const TokenArgs& a);

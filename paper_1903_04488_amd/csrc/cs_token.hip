@@ -24,6 +24,13 @@ bool dlogits_ok(const TokenArgs& a) {
     return !rows_meet(a.dlogits, a.d_stride * b, a.logits, a.stride * b, a.rows, a.vocab * b);
 }
 
+// The parts of rows (a multiple of 8), then partial sums, then the gradients of few rows' log probabilities and entropies
+size_t parts_bytes8(int64_t rows, int64_t vocab) { return (token_bytes(rows, vocab, 0) + 7) / 8 * 8; }
+size_t policy_bytes(int64_t rows, int64_t vocab) {
+    if (rows == 0) return 0;
+    return parts_bytes8(rows, vocab) + static_cast<size_t>(policy_partials(rows)) * 4 * sizeof(double) + (few_rows(rows) ? 8 * static_cast<size_t>(rows) : 0);
+}
+
 }  // namespace
 }  // namespace cs
 
@@ -95,4 +102,46 @@ extern "C" int cs_token_loss(const void* logits, int64_t rows, int64_t vocab, in
     const Span rest[] = {{target, 8 * rows}, {g_logp, 4 * rows}, {g_entropy, 4 * rows}};
     if (!spans_apart(written, read) || !spans_apart(grad, rest)) return CS_EINVAL;
     return by_type(kTokenLoss, a);
+}
+
+extern "C" int cs_token_policy_workspace_bytes(int64_t rows, int64_t vocab, size_t* bytes) {
+    if (rows < 0 || rows > kTokenMaxRows || vocab < 1 || vocab > kTokenMaxVocab || !bytes) return CS_EINVAL;
+    *bytes = policy_bytes(rows, vocab);
+    return CS_OK;
+}
+
+extern "C" int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt,
+                                    float scale, const int64_t* target, const float* old_logp, const float* ref_logp,
+                                    const float* advantage, const float* weight, float* logp, float* entropy, float* lse, float* loss,
+                                    float* sums, void* dlogits, int64_t d_stride, void* workspace, size_t ws_bytes, void* stream) {
+    if (!policy_ok(h) || !token_ok(rows, vocab, stride, fmt, scale)) return CS_EINVAL;
+    if (rows == 0) return CS_OK;
+    if (!logits || !target || !old_logp || (h->kl != 0.f && !ref_logp) || !advantage || !weight || !logp || !entropy || !lse) return CS_EINVAL;
+    const size_t need = policy_bytes(rows, vocab);
+    if (ws_bytes < need) return CS_EWORKSPACE;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7)) return CS_EINVAL;
+    const float* const ref = h->kl != 0.f ? ref_logp : nullptr;
+    TokenArgs a = {};
+    a.logits = logits, a.rows = rows, a.vocab = vocab, a.stride = stride, a.fmt = fmt, a.scale = scale, a.target = target;
+    a.out = TokenOut{logp, entropy, lse, nullptr, nullptr}, a.ws = workspace;
+    a.dlogits = dlogits, a.d_stride = d_stride, a.stream = stream_of(stream);
+    a.policy = PolicyIn{*h, old_logp, ref, advantage, weight};
+    char* const more = static_cast<char*>(workspace) + parts_bytes8(rows, vocab);
+    a.policy_out = PolicyOut{loss, nullptr, nullptr, sums, reinterpret_cast<double*>(more)};
+    if (few_rows(rows)) {
+        a.policy_out.g_logp = reinterpret_cast<float*>(more + static_cast<size_t>(policy_partials(rows)) * 4 * sizeof(double));
+        a.policy_out.g_entropy = a.policy_out.g_logp + rows;
+    }
+    if (!dlogits_ok(a)) return CS_EINVAL;
+    const int64_t n = 4 * rows, dlogits_span = row_span(rows, vocab, d_stride, fmt);
+    const Span written[] = {{logp, n}, {entropy, n}, {lse, n}, {loss, n}, {sums, 16}, {workspace, static_cast<int64_t>(need)}};
+    const Span read[] = {{logits, row_span(rows, vocab, stride, fmt)}, {dlogits, dlogits_span}, {target, 8 * rows}, {old_logp, n}, {ref, n},
+                         {advantage, n}, {weight, n}};
+    const Span grad[] = {{dlogits, dlogits_span}};
+    const Span rest[] = {{target, 8 * rows}, {old_logp, n}, {ref, n}, {advantage, n}, {weight, n}};
+    if (!spans_apart(written, read) || !spans_apart(grad, rest)) return CS_EINVAL;
+    if (int rc = by_type(kTokenPolicy, a)) return rc;
+    if (!loss && !sums) return CS_OK;
+    const PolicyOut out = {loss, nullptr, nullptr, sums, a.policy_out.partials};
+    return launch_policy(a.policy, rows, logp, entropy, target, vocab, out, a.stream);
 }

@@ -438,6 +438,11 @@ struct Target {
     }
 };
 
+// (an empty row's is 0)
+__device__ __forceinline__ float entropy_of(const Sums& r, float log_sum) {
+    return r.m == -INFINITY && r.S == r.S ? 0.f : log_sum - kLn2 * (r.U / r.S);
+}
+
 template <typename T>
 __device__ __forceinline__ void row_results(int64_t row, const Target<T>& target, float scale, const Sums& r, float log_sum,
                                             const TokenOut& out) {
@@ -447,7 +452,7 @@ __device__ __forceinline__ void row_results(int64_t row, const Target<T>& target
         const float lse = fmaf(r.m, scale, log_sum);
         out.lse[row] = empty ? -INFINITY : lse < -FLT_MAX ? -FLT_MAX : lse;
     }
-    if (out.entropy) out.entropy[row] = empty ? 0.f : log_sum - kLn2 * (r.U / r.S);
+    if (out.entropy) out.entropy[row] = entropy_of(r, log_sum);
     if (out.logp) out.logp[row] = target.counts ? logp_of(target.x, r, log_sum, scale) : 0.f;
 }
 
@@ -557,6 +562,15 @@ struct RowGrad {
         hot = scale * g;
         a = -hot;
         b = g_entropy ? -scale * g_entropy[row] : 0.f;
+    }
+    // the same from the policy loss of a token whose row has these sums
+    __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const PolicyIn& policy, float logp,
+                                                 float entropy) {
+        target = t >= 0 && t < vocab ? static_cast<int32_t>(t) : -1;
+        const PolicyToken token = policy_token(policy, row, logp, entropy, target >= 0);
+        hot = scale * token.g_logp;
+        a = -hot;
+        b = -scale * token.g_entropy;
     }
     // ENTROPY: b is not 0
     template <int FROM, bool ENTROPY>
@@ -691,7 +705,7 @@ k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     }
 }
 
-enum { kForward, kAlternatives, kLoss };
+enum { kForward, kAlternatives, kLoss, kPolicy };
 
 // A row held in registers by THREADS threads, up to ITEMS packs each: one read of it for everything.  All but the last EITHER
 // packs of a thread there are.
@@ -786,7 +800,7 @@ __device__ __forceinline__ void grad_held(const HeldRow<T, THREADS, ITEMS>& held
 template <typename T, int MODE, int THREADS, int ITEMS, bool PAST>
 __global__ void __launch_bounds__(THREADS == 64 ? kThreads : THREADS)
 k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out, int top,
-             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, int parts, Parts ws) {
+             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, int parts, Parts ws, PolicyIn policy) {
     constexpr int ROWS = THREADS == 64 ? kThreads / 64 : 1, P = kPack<T>;
     __shared__ TokenShared<THREADS> shared[ROWS];
     int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + (THREADS == 64 ? threadIdx.x >> 6 : 0);
@@ -804,7 +818,7 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
     }
     const bool results = parts == 1;
     const T* x = logits + row * stride + first * P;
-    const int64_t t = MODE == kLoss || (out.logp && results) ? target[row] : -1;
+    const int64_t t = MODE == kLoss || MODE == kPolicy || (out.logp && results) ? target[row] : -1;
     const float k = scale * kLog2e;
     HeldRow<T, THREADS, ITEMS> held;
     held.load(x, vocab, packs);
@@ -829,22 +843,29 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
             }
         });
     }
-    if constexpr (MODE == kLoss) {
+    if constexpr (MODE == kLoss || MODE == kPolicy) {
         T* dx = dlogits + row * d_stride;
         RowGrad g;
-        g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
+        bool bonus;
+        if constexpr (MODE == kPolicy) {
+            g.coefficients(row, vocab, scale, t, policy, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum));
+            bonus = policy.h.entropy != 0.f;
+        } else {
+            g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
+            bonus = g_entropy;
+        }
         if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, kDiffs, true, THREADS, ITEMS>(held, dx, vocab, g);
-        else if (g_entropy) grad_held<PAST, kSums, true, THREADS, ITEMS>(held, dx, vocab, g);
+        else if (bonus) grad_held<PAST, kSums, true, THREADS, ITEMS>(held, dx, vocab, g);
         else grad_held<PAST, kSums, false, THREADS, ITEMS>(held, dx, vocab, g);
     }
 }
 
 // Forward and gradient of a row in one workgroup, for rows that no workgroup holds (more than 131 072 values of 16 bits, 65 536 of 32): the
 // second read comes from the caches.  1024 x 131072 bf16 as this 137 us, held 120.
-template <typename T, bool PAST>
+template <typename T, bool PAST, int MODE>
 __global__ void __launch_bounds__(kThreads)
 k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out,
-             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs) {
+             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, PolicyIn policy) {
     __shared__ TokenShared<kThreads> sh;
     const int64_t row = blockIdx.x;
     const T* x = logits + row * stride;
@@ -860,9 +881,16 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     if (threadIdx.x == 0) row_results(row, hit, scale, r, log_sum, out);
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
     RowGrad g;
-    g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
+    bool bonus;
+    if constexpr (MODE == kPolicy) {
+        g.coefficients(row, vocab, scale, t, policy, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum));
+        bonus = policy.h.entropy != 0.f;
+    } else {
+        g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
+        bonus = g_entropy;
+    }
     if (!grad_from_sums(g, r, log_sum, scale)) grad_packs<PAST, kDiffs, true, kThreads>(x, dx, vocab, 0, packs, g);
-    else if (g_entropy) grad_packs<PAST, kSums, true, kThreads>(x, dx, vocab, 0, packs, g);
+    else if (bonus) grad_packs<PAST, kSums, true, kThreads>(x, dx, vocab, 0, packs, g);
     else grad_packs<PAST, kSums, false, kThreads>(x, dx, vocab, 0, packs, g);
 }
 
@@ -888,13 +916,14 @@ Held held(int64_t rows, int64_t vocab, int32_t fmt, int parts) {
 }
 template <typename T, int MODE, int THREADS, int ITEMS>
 int token_held_as(const TokenArgs& a, int parts) {
-    const auto kernel = MODE == kLoss && past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_held<T, MODE, THREADS, ITEMS, MODE == kLoss>
-                                                                                   : k_token_held<T, MODE, THREADS, ITEMS, false>;
+    constexpr bool GRAD = MODE == kLoss || MODE == kPolicy;
+    const auto kernel = GRAD && past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_held<T, MODE, THREADS, ITEMS, GRAD>
+                                                                          : k_token_held<T, MODE, THREADS, ITEMS, false>;
     const int64_t grid = THREADS == 64 ? (a.rows + 3) / 4 : a.rows * parts;
     kernel<<<static_cast<unsigned>(grid), THREADS == 64 ? kThreads : THREADS, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.rows, static_cast<int32_t>(a.vocab), a.stride, a.scale, a.target, a.out, a.top, a.g_logp,
         a.g_entropy, static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt), parts,
-        parts > 1 ? parts_in(a.ws, a.rows, parts, a.top) : Parts{});
+        parts > 1 ? parts_in(a.ws, a.rows, parts, a.top) : Parts{}, a.policy);
     return launched();
 }
 template <typename T, int MODE>
@@ -945,26 +974,33 @@ int token_grad(const TokenArgs& a) {
         static_cast<T*>(a.dlogits), a.d_stride, static_cast<int>(pieces), packs);
     return launched();
 }
-template <typename T>
+template <typename T, int MODE>
 int token_loss(TokenArgs a) {
     const Held h = held(a.rows, a.vocab, a.fmt, 1);
-    if (h.threads && parts_of(a.rows, a.vocab) == 1) return token_held<T, kLoss>(a, h, 1);
+    if (h.threads && parts_of(a.rows, a.vocab) == 1) return token_held<T, MODE>(a, h, 1);
     if (few_rows(a.rows)) {
         if (int rc = token_forward<T, false>(a)) return rc;
+        if (MODE == kPolicy) {
+            PolicyOut out = {nullptr, a.policy_out.g_logp, a.policy_out.g_entropy, nullptr, nullptr};
+            if (a.policy.h.entropy == 0.f) out.g_entropy = nullptr;
+            if (int rc = launch_policy(a.policy, a.rows, a.out.logp, a.out.entropy, a.target, a.vocab, out, a.stream)) return rc;
+            a.g_logp = out.g_logp, a.g_entropy = out.g_entropy;
+        }
         a.lse = a.out.lse, a.entropy = a.out.entropy;
         return token_grad<T>(a);
     }
-    const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_loss<T, true> : k_token_loss<T, false>;
+    const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_loss<T, true, MODE> : k_token_loss<T, false, MODE>;
     kernel<<<static_cast<unsigned>(a.rows), kThreads, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.vocab, a.stride, a.scale, a.target, a.out, a.g_logp, a.g_entropy,
-        static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt));
+        static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt), a.policy);
     return launched();
 }
 
 template <typename T>
 int token(TokenCall call, const TokenArgs& a) {
     if (call == kTokenForward) return a.top ? token_forward<T, true>(a) : token_forward<T, false>(a);
-    return call == kTokenGrad ? token_grad<T>(a) : token_loss<T>(a);
+    if (call == kTokenPolicy) return token_loss<T, kPolicy>(a);
+    return call == kTokenGrad ? token_grad<T>(a) : token_loss<T, kLoss>(a);
 }
 
 }  // namespace

@@ -1,4 +1,5 @@
-"""A language model's training step on both sides of its gradient: layer norm, the loss over the vocabulary, AdamW.
+"""A language model's training step on both sides of its gradient: layer norm, the losses over the vocabulary and of answers, AdamW
+and, for matrices, orthogonalised momentum.
 
 Like the paths of pipeline.py these classes own tensors and the order of the library calls; every arithmetic step
 runs inside libcsketch.so.  What they return are their own buffers, which the next call overwrites.
@@ -77,6 +78,142 @@ class TokenLogprobs:
         B.cs_token_loss(logits, target, g_logp, g_entropy, self.logp[:n], self.entropy[:n], self.lse[:n], out,
                         self.workspace, self.scale)
         return self.logp[:n], out
+
+
+class PolicyLoss:
+    """Clipped policy loss of up to `rows` tokens, from logits or from log probabilities, with its gradients.
+
+    clip: how far below and above 1 a ratio to the behaviour policy counts.  kl: of the KL estimate against a reference, entropy: of the
+    entropy bonus (0: without).  `sums` [4], on the GPU, holds the loss, the weighted KL estimate, the weight of the tokens where
+    clipping decides, and the weight of all."""
+
+    def __init__(self, rows: int, vocab: int | None = None, clip=(0.2, 0.2), kl: float = 0.0, entropy: float = 0.0, scale: float = 1.0,
+                 device="cuda:0"):
+        self.h, self.vocab, self.scale = B.CsPolicy(*clip, kl, entropy), vocab, scale
+        f32 = dict(dtype=torch.float32, device=device)
+        self.logp, self.entropy, self.lse, self.losses, self.g_logp, self.g_entropy = (torch.empty(rows, **f32) for _ in range(6))
+        self.sums = torch.zeros(4, **f32)
+        need = B.cs_policy_workspace_bytes(rows)
+        if vocab is not None and rows:
+            # (fewer rows are shared by more workgroups each, and take up to this much)
+            need = max(B.cs_token_policy_workspace_bytes(n, vocab) for n in [*range(1, min(rows, 1024) + 1), rows])
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+
+    def loss(self, logits, target, old_logp, ref_logp, advantage, weight, out=None):
+        """(sums, gradient of the logits); logp, entropy, lse and losses are in the attributes; `out` may be logits"""
+        n = len(logits)
+        out = torch.empty_like(logits) if out is None else out
+        B.cs_token_policy_loss(self.h, logits, target, old_logp, ref_logp, advantage, weight, self.logp[:n], self.entropy[:n], self.lse[:n],
+                               self.losses[:n], self.sums, out, self.workspace, self.scale)
+        return self.sums, out
+
+    def of_logprobs(self, logp, entropy, old_logp, ref_logp, advantage, weight):
+        """(sums, gradients of logp and of entropy)"""
+        n = len(logp)
+        B.cs_policy_loss(self.h, logp, entropy, old_logp, ref_logp, advantage, weight, self.losses[:n], self.g_logp[:n],
+                         self.g_entropy[:n], self.sums, self.workspace)
+        return self.sums, self.g_logp[:n], self.g_entropy[:n]
+
+
+class PreferenceLoss:
+    """Loss of up to `pairs` pairs of answers of up to `tokens` tokens in all, with the gradient of every token's log probability.
+
+    kind: "logistic", "hinge" or "square".  mean: means over an answer's tokens instead of sums.  `sums` [3], on the GPU: the weighted loss, the weight
+    of the pairs whose chosen answer has the larger reward, the weighted difference of rewards."""
+
+    KINDS = {"logistic": B.CS_PREFERENCE_LOGISTIC, "hinge": B.CS_PREFERENCE_HINGE, "square": B.CS_PREFERENCE_SQUARE}
+
+    def __init__(self, tokens: int, pairs: int, kind: str = "logistic", beta: float = 0.1, smoothing: float = 0.0, margin: float = 0.0,
+                 mean: bool = False, device="cuda:0"):
+        if kind not in self.KINDS:
+            raise B.CsError(f"kind must be one of {list(self.KINDS)}, not {kind}")
+        self.h = B.CsPreference(self.KINDS[kind], mean, beta, smoothing, margin)
+        f32 = dict(dtype=torch.float32, device=device)
+        self.losses, self.rewards, self.sums = torch.empty(pairs, **f32), torch.empty(2 * pairs, **f32), torch.zeros(3, **f32)
+        self.g_logp = torch.zeros(tokens, **f32)
+        need = max((B.cs_preference_workspace_bytes(tokens, n) for n in range(min(pairs, 1), pairs + 1)), default=0)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+
+    def loss(self, logp, ref_logp, begin, counts=None, weight=None):
+        """(sums, gradient of logp): answers are packed after one another, the chosen ones first, and begin [2 pairs + 1] says where; a mean over
+        the pairs without a weight"""
+        pairs, n = len(begin) // 2, len(logp)
+        if weight is None:
+            weight = torch.full((pairs,), 1.0 / max(pairs, 1), device=logp.device)
+        B.cs_preference_loss(self.h, logp, ref_logp, counts, begin, weight, self.losses[:pairs], self.rewards[:2 * pairs], self.g_logp[:n],
+                             self.sums, self.workspace)
+        return self.sums, self.g_logp[:n]
+
+
+def _muon_constants(lr, momentum, nesterov, weight_decay, eps, coefs, scale):
+    coefs = [tuple(c) for c in coefs]
+    if not 1 <= len(coefs) <= B.CS_MUON_MAX_STEPS or any(len(c) != 3 for c in coefs):
+        raise B.CsError(f"coefs must be 1 to {B.CS_MUON_MAX_STEPS} triples")
+    scales = {"shape": B.CS_MUON_SCALE_SHAPE, "rms": B.CS_MUON_SCALE_RMS, "one": B.CS_MUON_SCALE_ONE}
+    if scale not in scales:
+        raise B.CsError(f"scale must be one of {list(scales)}, not {scale}")
+    h = B.CsMuon(lr, momentum, weight_decay, eps, nesterov, scales[scale], len(coefs), 0)
+    for i, c in enumerate(coefs):
+        h.coefs[i][:] = c
+    return h
+
+
+def _terms_of(tensors, terms):
+    """results of 8 bits need no more than one term"""
+    if terms is None:
+        terms = 1 if tensors and tensors[0].dtype is torch.bfloat16 else 2
+    return terms
+
+
+NEWTON_SCHULZ = ((3.4445, -4.7750, 2.0315),) * 5      # to between 0.7 and 1.2 in five steps, from singular values of 0.01 on
+
+
+class Orthogonalizer:
+    """Matrices, or stacks of them, orthogonalised by Newton-Schulz products: `inputs` are read and `outputs` written where they are (they may
+    be the same).  terms: how much of their factors the products take, by the outputs' type if None."""
+
+    def __init__(self, inputs, outputs, coefs=NEWTON_SCHULZ, eps: float = 1e-7, terms: int | None = None):
+        self.outputs = list(outputs)
+        self.h = _muon_constants(0.0, 0.0, False, 0.0, eps, coefs, "one")
+        self.list = B.MatrixList(self.outputs, inputs, terms=_terms_of(self.outputs, terms))
+        self.workspace = torch.empty(B.cs_muon_workspace_bytes(self.list), dtype=torch.uint8, device=self.list.device)
+
+    def run(self):
+        B.cs_orthogonalize(self.h, self.list, self.workspace)
+        return self.outputs
+
+
+class Muon:
+    """The optimizer that updates matrices by their orthogonalised momentum, all of a model's in the same launches (what is no matrix belongs
+    to AdamW, tables mostly too).
+
+    params, grads: lists of matrices or of stacks [count, rows, cols], updated and read where they are (`set_grads` after grads have moved).
+    m: moments of a checkpoint, float32, kept and updated in place.  scale: of the update, "shape" sqrt(max(1, rows / cols)), "rms" 0.2
+    sqrt(max(rows, cols)), which gives it the size of AdamW's, or "one".  terms: how much of their factors the products take, 1 for parameters in bfloat16
+    and 2 otherwise if None.  grad_scale: float32 tensor of one value that the gradients are multiplied by (the scale of clipping); a step where it is not
+    finite changes nothing.  lr_now: float64 tensor of one value, read by every step in place of lr, for graphs.  The constants may be changed
+    between steps: opt.h.lr = ..."""
+
+    def __init__(self, params, grads, lr: float = 0.02, momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0,
+                 eps: float = 1e-7, coefs=NEWTON_SCHULZ, scale: str = "shape", m=None, terms: int | None = None, grad_scale=None, lr_now=None):
+        if not params:
+            raise B.CsError("params must be a non-empty list")
+        self.params, self.grads = list(params), list(grads)
+        self.h = _muon_constants(lr, momentum, nesterov, weight_decay, eps, coefs, scale)
+        self.m = [torch.zeros(p.shape, dtype=torch.float32, device=p.device) for p in self.params] if m is None else list(m)
+        self.grad_scale, self.lr_now = grad_scale, lr_now
+        self.list = B.MatrixList(self.params, self.grads, self.m, _terms_of(self.params, terms))
+        self.workspace = torch.empty(B.cs_muon_workspace_bytes(self.list), dtype=torch.uint8, device=self.list.device)
+
+    def set_grads(self, grads):
+        """other tensors with the gradients"""
+        grads = list(grads)
+        self.list.refresh(self.params, grads, self.m)
+        self.grads = grads
+
+    def step(self):
+        """one update of params and moments"""
+        B.cs_muon_step(self.h, self.list, self.workspace, self.lr_now, self.grad_scale)
 
 
 class AdamW:

@@ -1,0 +1,243 @@
+"""The loss of pairs of answers against the definition in 64 bits.
+
+Sums, losses and slopes are 64 bits in the kernel too and rounded once, so every output is off by 2^-24 of itself, and by 2^-40 of the
+sizes that a difference is made of (a chain of fewer than 2^12 additions of 2^-53 each)."""
+import math
+
+import pytest
+import torch
+
+import paper_1903_04488_amd as cs
+from paper_1903_04488_amd.training import PreferenceLoss, TokenLogprobs
+from test_gpu_token_logprobs import logits_of, within
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U, FINE = 2.0 ** -24, 2.0 ** -40
+KINDS = {"logistic": cs.CS_PREFERENCE_LOGISTIC, "hinge": cs.CS_PREFERENCE_HINGE, "square": cs.CS_PREFERENCE_SQUARE}
+
+
+def batch_of(lengths, seed=1, before=0, behind=0, reference=True, masked=True):
+    """answers of these lengths, the chosen ones first"""
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    begin = torch.tensor([before] + lengths, device=DEV).cumsum(0)
+    n = before + sum(lengths) + behind
+
+    def normal():
+        return torch.randn(n, device=DEV, generator=gen)
+
+    logp = -(normal() - 1.0).exp()
+    t = {"logp": logp, "ref": logp + 0.3 * normal() if reference else None, "counts": torch.rand(n, device=DEV, generator=gen) < 0.8 if masked else None,
+         "begin": begin, "w": torch.rand(len(lengths) // 2, device=DEV, generator=gen) + 0.1}
+    if masked:                                           # nothing of a masked token counts
+        t["logp"] = torch.where(t["counts"], t["logp"], math.nan)
+    return t
+
+
+def truth(t, kind, beta, smoothing, margin, mean):
+    """values and bounds, answer by answer"""
+    begin, logp = t["begin"].tolist(), t["logp"].double()
+    n, pairs = len(logp), len(begin) // 2
+    ratio = logp - (0 if t["ref"] is None else t["ref"].double())
+    counts = torch.ones(n, dtype=torch.bool, device=DEV) if t["counts"] is None else t["counts"].bool()
+    total, number, size = [], [], []
+    at = [slice(min(max(a, 0), n), max(min(max(a, 0), n), min(b, n))) for a, b in zip(begin, begin[1:])]
+    for s in at:
+        x = ratio[s][counts[s]]
+        total.append(x.sum()), number.append(float(len(x))), size.append(x.abs().sum())
+    total, size = torch.stack(total), torch.stack(size)
+    each = beta / (torch.tensor(number, device=DEV, dtype=torch.float64).clamp(min=1.0) if mean else torch.ones(2 * pairs, dtype=torch.float64, device=DEV))
+    reward, size = each * total, each * size
+    z = (reward[:pairs] - reward[pairs:] - margin).requires_grad_()
+    if kind == "logistic":
+        soft = torch.nn.functional.softplus
+        # (softplus becomes linear beyond 20, where e^-20 is left out)
+        loss = (1 - smoothing) * (soft(-z, threshold=60)) + smoothing * soft(z, threshold=60)
+    elif kind == "hinge":
+        loss = (1 - z).clamp(min=0)
+    else:
+        loss = ((z - 0.5) / beta) ** 2
+    slope, = torch.autograd.grad(loss.sum(), z)
+    loss, z = loss.detach(), z.detach()
+    w = torch.ones(pairs, dtype=torch.float64, device=DEV) if t["w"] is None else t["w"].double()
+    off = FINE * (size[:pairs] + size[pairs:] + abs(margin))
+    steep = slope.abs() + 2 * off / beta ** 2 if kind == "square" else 1.0
+    coef = torch.cat([w * slope, -w * slope]) * each
+    e_coef = torch.cat([w, w]) * each * (2 / beta ** 2 if kind == "square" else 1.0) * torch.cat([off, off])
+    g = torch.full((n,), math.nan, dtype=torch.float64, device=DEV)
+    e_g = torch.zeros(n, dtype=torch.float64, device=DEV)
+    for a, s in enumerate(at):
+        g[s] = torch.where(counts[s], coef[a], 0.0)
+        e_g[s] = e_coef[a] + U * coef[a].abs()
+    gap = reward[:pairs] - reward[pairs:]
+    r = {"loss": loss, "reward": reward, "g_logp": g, "sums": torch.stack([(w * loss).sum(), w[gap > 0].sum(), (w * gap).sum()])}
+    r["e_loss"] = U * loss + steep * off + FINE
+    r["e_reward"] = U * reward.abs() + FINE * size
+    r["e_g_logp"] = e_g + 2.0 ** -148
+    r["e_sums"] = U * r["sums"].abs() + torch.stack([(w * r["e_loss"]).sum(), FINE * w.sum(), (w * off).sum()])
+    return r
+
+
+def run(t, kind, beta, smoothing=0.0, margin=0.0, mean=False, gradient=True):
+    n, pairs = len(t["logp"]), len(t["begin"]) // 2
+    out = {"loss": torch.full((pairs,), math.nan, device=DEV), "reward": torch.full((2 * pairs,), math.nan, device=DEV),
+           "g_logp": torch.full((n,), math.nan, device=DEV) if gradient else None, "sums": torch.full((3,), math.nan, device=DEV)}
+    ws = torch.empty(cs.cs_preference_workspace_bytes(n, pairs), dtype=torch.uint8, device=DEV)
+    cs.cs_preference_loss(cs.CsPreference(KINDS[kind], mean, beta, smoothing, margin), t["logp"], t["ref"], t["counts"], t["begin"], t["w"],
+                          *out.values(), ws)
+    return out
+
+
+def check(t, kind, beta, smoothing=0.0, margin=0.0, mean=False):
+    got, want = run(t, kind, beta, smoothing, margin, mean), truth(t, kind, beta, smoothing, margin, mean)
+    for name in ("loss", "reward", "sums"):
+        within(got[name], want[name], want["e_" + name], name)
+    outside = torch.isnan(want["g_logp"])
+    assert torch.isnan(got["g_logp"][outside]).all(), "tokens of no answer are left as they were"
+    within(got["g_logp"][~outside], want["g_logp"][~outside], want["e_g_logp"][~outside], "g_logp")
+
+
+LENGTHS = {"one": [1, 1], "none": [0, 0], "one empty": [0, 5], "few": [3, 70, 1, 65, 64, 63], "some empty": [0, 9, 0, 300, 0, 0, 7, 0],
+           "uneven": [5000, 1, 2, 4097, 1, 3], "long": [70_001, 40_000], "many": [(7 * i) % 41 for i in range(1200)],
+           "a long one among many": [20] * 300 + [30_000] + [15] * 299}
+
+
+@pytest.mark.parametrize("lengths", list(LENGTHS))
+@pytest.mark.parametrize("kind,beta,smoothing,margin", [("logistic", 0.125, 0.0, 0.0), ("logistic", 0.5, 0.25, 0.5), ("hinge", 0.25, 0.0, 0.0),
+                                                        ("square", 0.125, 0.0, -0.25)])
+@pytest.mark.parametrize("mean", [False, True])
+def test_preference_loss_matches_the_definition(lengths, kind, beta, smoothing, margin, mean):
+    check(batch_of(LENGTHS[lengths], seed=len(lengths), before=3, behind=11), kind, beta, smoothing, margin, mean)
+
+
+@pytest.mark.parametrize("lengths", ["few", "uneven", "many"])
+def test_without_a_reference_a_mask_and_weights(lengths):
+    t = batch_of(LENGTHS[lengths], reference=False, masked=False)
+    check(t | {"w": None}, "logistic", 0.25, mean=True)
+    check(t | {"counts": torch.ones(len(t["logp"]), dtype=torch.uint8, device=DEV) * 3}, "hinge", 0.25)
+
+
+def test_far_apart():
+    """rewards hundreds apart: no exponential leaves the numbers"""
+    t = batch_of([900, 800, 10, 20], masked=False)
+    for kind in KINDS:
+        check(t | {"ref": t["logp"] * torch.where(torch.arange(1730, device=DEV) < 900, 30.0, -30.0)}, kind, 0.5, 0.125 if kind == "logistic" else 0.0)
+
+
+def test_offsets_outside_the_tokens_are_cut_off():
+    t = batch_of([10, 20, 30, 40], masked=False)
+    for begin in ([-5, 10, 30, 60, 1 << 40], [0, 10, 30, 200, 300], [-(1 << 50), -3, -2, -1, 0]):
+        check(t | {"begin": torch.tensor(begin, device=DEV)}, "logistic", 0.25)
+    got = run(t | {"begin": torch.tensor([50, 10, 90, 20, 100], device=DEV)}, "logistic", 0.25)     # not ascending: no fault
+    assert torch.isfinite(got["loss"]).all()
+
+
+def test_a_pair_of_weight_zero_and_one_that_is_not_a_number():
+    t = batch_of([5, 6, 7, 8, 9, 10], masked=False)
+    t["logp"][2] = math.nan                              # pair 0
+    t["w"][0] = 0.0
+    got = run(t, "logistic", 0.25)
+    assert torch.isnan(got["loss"][0]) and torch.isfinite(got["loss"][1:]).all() and torch.isfinite(got["sums"]).all()
+    assert (got["g_logp"][:5] == 0).all() and torch.isfinite(got["g_logp"]).all()
+    for kind in KINDS:
+        got = run(t | {"w": None}, kind, 0.25)
+        assert torch.isnan(got["loss"][0]) and torch.isnan(got["g_logp"][:5]).all() and torch.isnan(got["sums"][0])
+        assert torch.isfinite(got["loss"][1:]).all() and torch.isfinite(got["g_logp"][5:18]).all()
+
+
+def test_gradient_against_differences():
+    """of the weighted loss, which is 64 bits until it is rounded: h^2 times a third derivative below 1, and 2^-24 of the loss over h"""
+    t = batch_of([30, 40, 50, 20, 10, 60], masked=False)
+    n, h = len(t["logp"]), 2.0 ** -9
+    v = torch.randn(n, device=DEV, generator=torch.Generator(device=DEV).manual_seed(2))
+    for kind in ("logistic", "square"):
+        g = run(t, kind, 0.25)["g_logp"].double()
+        up, down = t["logp"] + h * v, t["logp"] - h * v
+        f = [run(t | {"logp": x}, kind, 0.25) for x in (up, down)]
+        slope = sum(s * (t["w"].double() * r["loss"].double()).sum() for s, r in zip((1, -1), f)) / (2 * h)
+        want = (g * (up.double() - down.double())).sum() / (2 * h)
+        size = (g * v).abs().sum()
+        noise = 4 * U * float(t["w"].sum() * f[0]["loss"].max()) / h
+        assert abs(float(slope - want)) <= 1e-3 * float(size) + noise
+
+
+def test_gradient_may_be_left_out_and_no_pairs():
+    t = batch_of([30, 40, 50, 20])
+    want, got = run(t, "hinge", 0.25), run(t, "hinge", 0.25, gradient=False)
+    assert all(torch.equal(got[k], want[k]) for k in ("loss", "reward", "sums"))
+    e = torch.empty(0, device=DEV)
+    cs.cs_preference_loss(cs.CsPreference(0, 0, 0.5, 0.0, 0.0), e, None, None, torch.zeros(1, dtype=torch.int64, device=DEV), None, e, e, e,
+                          torch.empty(3, device=DEV), torch.empty(0, dtype=torch.uint8, device=DEV))
+    t["logp"], t["ref"], t["counts"], t["begin"] = e, None, None, torch.zeros(5, dtype=torch.int64, device=DEV)
+    got = run(t, "logistic", 0.5)                        # pairs of empty answers, no token at all
+    assert torch.allclose(got["loss"], torch.full((2,), math.log(2.0), device=DEV))
+
+
+def test_from_logits_and_back():
+    """log probabilities, the loss of pairs, the gradient of the logits: against automatic differentiation in 64 bits.  Log probabilities are off
+    by about 2e-6 here, each, rewards by beta times the sum of an answer's; gradients by the same share"""
+    rows, vocab = 120, 500
+    x, target = logits_of(rows, vocab, torch.float32, spread=1.0)
+    x = x.contiguous()
+    target[::5] = -1
+    begin = torch.tensor([0, 30, 45, 45, 100, 110, 117], device=DEV)
+    ref = torch.randn(rows, device=DEV) * 0.1 - 6.5
+    ref[target < 0] = 0.0
+    tk, pl = TokenLogprobs(rows, vocab), PreferenceLoss(rows, 3, beta=0.25, smoothing=0.125)
+    logp, _ = tk.forward(x, target)
+    sums, g = pl.loss(logp, ref, begin, counts=target >= 0)
+    dx = tk.backward(x, target, g)
+    X = x.double().requires_grad_()
+    lp = torch.log_softmax(X, 1).gather(1, target.clamp(min=0)[:, None])[:, 0]
+    ratio = torch.where(target >= 0, lp - ref.double(), 0.0)
+    R = 0.25 * torch.stack([ratio[a:b].sum() for a, b in zip(begin.tolist(), begin.tolist()[1:])])
+    z = R[:3] - R[3:]
+    soft = torch.nn.functional.softplus
+    loss = (0.875 * soft(-z) + 0.125 * soft(z)).mean()
+    loss.backward()
+    assert abs(float(sums[0]) - float(loss.detach())) <= 0.25 * 60 * 2e-6
+    assert (dx.double() - X.grad).abs().max() <= 1e-4 * X.grad.abs().max()
+
+
+def test_replayed_graph_and_another_stream():
+    t = batch_of(LENGTHS["many"])
+    pl = PreferenceLoss(len(t["logp"]), 600, beta=0.25)
+    logp = t["logp"].clone()
+    args = (t["ref"], t["begin"], t["counts"], t["w"])
+    pl.loss(logp, *args)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pl.loss(logp, *args)
+    for turn in range(3):
+        logp.copy_(t["logp"] * (1 + 0.1 * turn))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            want = [y.clone() for y in pl.loss(logp, *args)]
+        torch.cuda.current_stream().wait_stream(side)
+        pl.g_logp.fill_(7.0)
+        graph.replay()
+        inside = slice(0, int(t["begin"][-1]))
+        assert torch.equal(pl.sums, want[0]) and torch.equal(pl.g_logp[inside], want[1][inside])
+
+
+def test_refusals():
+    t = batch_of([3, 4, 5, 6])
+    n = 18
+    out = dict(loss=torch.empty(2, device=DEV), reward=torch.empty(4, device=DEV), g=torch.empty(n, device=DEV), sums=torch.empty(3, device=DEV))
+    ws = torch.empty(cs.cs_preference_workspace_bytes(n, 2), dtype=torch.uint8, device=DEV)
+
+    def call(h=None, **change):
+        a = dict(logp=t["logp"], ref=t["ref"], counts=t["counts"], begin=t["begin"], w=t["w"], **out, ws=ws) | change
+        cs.cs_preference_loss(h or cs.CsPreference(0, 0, 0.5, 0.0, 0.0), *a.values())
+
+    call()
+    H = cs.CsPreference
+    for bad in (dict(logp=t["logp"].double()), dict(ref=t["ref"][:4]), dict(counts=t["counts"].float()), dict(begin=t["begin"].int()),
+                dict(begin=t["begin"][:4]), dict(w=t["w"][:1]), dict(loss=None), dict(reward=out["loss"]), dict(g=t["logp"]), dict(sums=None),
+                dict(ws=ws[:8]), dict(ws=None), dict(logp=t["logp"].cpu()), dict(loss=out["reward"][:2]), dict(h=H(3, 0, 0.5, 0.0, 0.0)),
+                dict(h=H(0, 0, 0.0, 0.0, 0.0)), dict(h=H(0, 0, math.inf, 0.0, 0.0)), dict(h=H(0, 0, 0.5, 1.5, 0.0)), dict(h=H(0, 0, 0.5, 0.0, math.nan))):
+        with pytest.raises(cs.CsError):
+            call(**bad)
+    with pytest.raises(cs.CsError):
+        PreferenceLoss(4, 2, kind="linear")
