@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kEdge = 64;                    // of the pieces in which u is read, and what all sizes are rounded up to
-constexpr int kDepth = 64;                   // values of K that are in LDS at a time
+constexpr int kDepth = 64;                   // values of a row in LDS, 128 bytes
 constexpr float kUp = 1024.f, kDown = 1.f / 1024.f;
 
 typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
@@ -99,11 +99,6 @@ template <typename T>
 __device__ __forceinline__ float value_at(const void* p, int64_t at) { return static_cast<float>(static_cast<const T*>(p)[at]); }
 __device__ __forceinline__ float read(const void* p, int fmt, int64_t at) {
     return fmt == CS_FMT_F32 ? value_at<float>(p, at) : fmt == CS_FMT_BF16 ? value_at<bf16>(p, at) : value_at<f16>(p, at);
-}
-__device__ __forceinline__ void write(void* p, int fmt, int64_t at, float v) {
-    if (fmt == CS_FMT_F32) static_cast<float*>(p)[at] = v;
-    else if (fmt == CS_FMT_BF16) static_cast<bf16*>(p)[at] = static_cast<bf16>(v);
-    else static_cast<f16*>(p)[at] = static_cast<f16>(v);
 }
 __device__ __forceinline__ bool skipped(const float* grad_scale) { return grad_scale && !(fabsf(*grad_scale) < INFINITY); }
 
@@ -236,183 +231,291 @@ struct Product {
 typedef __attribute__((address_space(3))) void* LdsPointer;
 typedef const __attribute__((address_space(1))) void* GlobalPointer;
 
-// T rows of kDepth values, `stride` apart, into LDS: a row's eight packs of 16 bytes lie in the order pack ^ (row / 2 % 8), so that 16
-// lanes that read the same pack of 16 rows meet all banks once.
-template <int T>
-__device__ __forceinline__ void stage(const _Float16* from, int64_t stride, _Float16* lds) {
+// The tile of a workgroup: WI x WJ wavefronts, each with FI x FJ blocks of 16 x 16; `stages` parts of K are in LDS or on their way there.
+template <int WI_, int WJ_, int FI_, int FJ_, int STAGES_>
+struct Shape {
+    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, STAGES = STAGES_;
+    static constexpr int WAVES = WI * WJ, THREADS = WAVES * 64, TI = WI * FI * 16, TJ = WJ * FJ * 16;
+    // Blocks that belong together: a lane has GI neighbouring rows of 4 GJ neighbouring columns of the output, so that both it and its
+    // transpose are written in whole pieces of memory straight from the registers.
+    static constexpr int GI = FI < 4 ? FI : 4, GJ = FJ < 4 ? FJ : 4;
+    static constexpr int LOADS = (TI + TJ) / 8 / WAVES;                  // of 1 KB, a wavefront and stage
+    static_assert(TI % (8 * WAVES) == 0 && TJ % (8 * WAVES) == 0, "whole loads");
+};
+// The row of the left tile that is place `at` of LDS: lane l of block f (of a group of GI) has row GI l + f.
+template <typename S>
+__device__ __forceinline__ int left_row(int at) {
+    const int group = at / (16 * S::GI), in = at % (16 * S::GI);
+    return group * 16 * S::GI + in % 16 * S::GI + in / 16;
+}
+// The right one: a lane of the result has rows 4 q .. 4 q + 3 of every block, which are columns 4 GJ q + 4 f + (0 .. 3) of a group.
+template <typename S>
+__device__ __forceinline__ int right_row(int at) {
+    const int group = at / (16 * S::GJ), in = at % (16 * S::GJ), m = in % 16;
+    return group * 16 * S::GJ + m / 4 * 4 * S::GJ + in / 16 * 4 + m % 4;
+}
+
+// Rows of 128 bytes into LDS, 64 values of K (one term) or 32 values of both terms.  A row's eight packs of 16 bytes lie in the order pack ^ (place /
+// 2 % 8): 16 lanes that read the same pack of 16 rows meet all banks once.
+template <typename S, int TERMS, bool LEFT>
+__device__ __forceinline__ void stage(const _Float16* high, const _Float16* low, int64_t stride, _Float16* lds) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
-    for (int q = 0; q < T / 32; ++q) {
-        const int first = (q * 4 + wave) * 8, row = first + (lane >> 3), pack = (lane & 7) ^ (row >> 1 & 7);
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<GlobalPointer>(reinterpret_cast<uintptr_t>(from + row * stride + pack * 8)),
+    for (int q = 0; q < (LEFT ? S::TI : S::TJ) / (8 * S::WAVES); ++q) {
+        const int first = (q * S::WAVES + wave) * 8, at = first + (lane >> 3), row = LEFT ? left_row<S>(at) : right_row<S>(at);
+        const int pack = (lane & 7) ^ (at >> 1 & 7);
+        const _Float16* from = (TERMS == 2 ? (pack < 4 ? high : low) + pack % 4 * 8 : high + pack * 8) + row * stride;
+        __builtin_amdgcn_global_load_lds(reinterpret_cast<GlobalPointer>(reinterpret_cast<uintptr_t>(from)),
                                          (LdsPointer)(lds + first * kDepth), 16, 0, 0);
     }
 }
+// All but `left` of this wavefront's loads have arrived and its reads of LDS are done; then so are all wavefronts'.
+template <int LEFT>
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
 
-// C = L R^T of rows of K values, T x T a workgroup of four wavefronts.
-template <int T, int TERMS, int MODE>
-__global__ void __launch_bounds__(kThreads, 2) k_muon_product(List list, Product k, char* ws) {
-    constexpr int F = T / 32, LINE = T + 4;  // blocks of 16 a wavefront and side
-    constexpr int kStage = 2 * T * kDepth;   // halves of a turn
-    constexpr int kBytes = 2 * kStage * 2 > T * LINE * 4 ? 2 * kStage * 2 : T * LINE * 4;
-    __shared__ __align__(16) char memory[kBytes];
-    _Float16* const lds = reinterpret_cast<_Float16*>(memory);
-    const Place at = (MODE == kGram || MODE == kSquare ? list.halves : list.fulls)[blockIdx.x];
+template <int N>
+__device__ __forceinline__ void load_halves(const _Float16* p, Half8 (&v)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = *reinterpret_cast<const Half8*>(p + 8 * e);
+}
+template <int N>
+__device__ __forceinline__ void store_halves(_Float16* high, _Float16* low, const float (&v)[N]) {
+    typedef _Float16 Halves __attribute__((ext_vector_type(N < 8 ? N : 8)));
+#pragma unroll
+    for (int e = 0; e < N; e += 8) {
+        Halves hi, lo;
+#pragma unroll
+        for (int k = 0; k < (N < 8 ? N : 8); ++k) {
+            _Float16 h, l;
+            split(v[e + k] * kUp, h, l);
+            hi[k] = h, lo[k] = l;
+        }
+        *reinterpret_cast<Halves*>(high + e) = hi;
+        if (low) *reinterpret_cast<Halves*>(low + e) = lo;
+    }
+}
+
+// N neighbouring parameters from column `col` of a row on: p = keep p - lr x (keep 0: x itself)
+struct Update {
+    float lr, keep;
+    bool optimizer;
+};
+template <typename T, int N>
+__device__ __forceinline__ void update_as(const Matrix& t, const Update& u, int64_t row, int64_t col, const float (&x)[N]) {
+    if (row >= t.rows || col >= t.cols) return;
+    T* const p = static_cast<T*>(t.p) + row * t.p_stride + col;
+    if (col + N <= t.cols) {
+        constexpr int P = N < kPack<T> ? N : kPack<T>;
+#pragma unroll
+        for (int e = 0; e < N; e += P) {
+            float v[P];
+            if (u.optimizer) load_pack<T, P>(p + e, v);
+#pragma unroll
+            for (int k = 0; k < P; ++k) v[k] = u.optimizer ? fmaf(v[k], u.keep, -u.lr * x[e + k]) : x[e + k];
+            store_pack<false>(p + e, v);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (col + e < t.cols) p[e] = static_cast<T>(u.optimizer ? fmaf(static_cast<float>(p[e]), u.keep, -u.lr * x[e]) : x[e]);
+    }
+}
+template <int N>
+__device__ __forceinline__ void update(const Matrix& t, int p_fmt, const Update& u, int64_t row, int64_t col, const float (&x)[N]) {
+    if (p_fmt == CS_FMT_F32) update_as<float>(t, u, row, col, x);
+    else if (p_fmt == CS_FMT_BF16) update_as<bf16>(t, u, row, col, x);
+    else update_as<f16>(t, u, row, col, x);
+}
+
+// Workgroups of a launch go round the 8 dies: each die gets neighbouring places, whose tiles read the same rows.
+__device__ __forceinline__ int place_of_block() {
+    const int per = gridDim.x / 8, more = gridDim.x % 8, die = blockIdx.x % 8, at = blockIdx.x / 8;
+    return die * per + min(die, more) + at;
+}
+// Tiles in bands of 8 rows, column by column of a band; of a lower half those on and below the diagonal.
+__device__ __forceinline__ void tile_of(int32_t local, int32_t down, int32_t across, int32_t& ti, int32_t& tj) {
+    const int32_t band = local / (8 * across), in = local - band * 8 * across, high = min(8, down - 8 * band);
+    ti = 8 * band + in % high;
+    tj = in / high;
+}
+__device__ __forceinline__ void half_tile_of(int32_t local, int32_t down, int32_t& ti, int32_t& tj) {
+    int32_t band = static_cast<int32_t>((sqrtf(8.f * local + 1.f) - 1.f) * 0.0625f);
+    while (4 * band * (8 * band + 1) > local) --band;
+    while (4 * (band + 1) * (8 * band + 9) <= local) ++band;
+    int32_t in = local - 4 * band * (8 * band + 1);
+    const int32_t high = min(8, down - 8 * band);
+    if (in < 8 * band * high) {
+        ti = 8 * band + in % high;
+        tj = in / high;
+        return;
+    }
+    in -= 8 * band * high;
+    ti = 0;
+    while (in > ti) in -= ++ti;
+    ti += 8 * band;
+    tj = 8 * band + in;
+}
+
+// C = L R^T of rows of K values, a tile a workgroup.
+template <typename S, int TERMS, int MODE>
+__global__ void __launch_bounds__(S::THREADS, 2) k_muon_product(List list, Product k, char* ws) {
+    constexpr bool HALF = MODE == kGram || MODE == kSquare;
+    constexpr int N = 4 * S::GJ, PART = (S::TI + S::TJ) * kDepth, ROWS = S::FI, GROUPS = S::FJ / S::GJ;
+    constexpr int STEP = kDepth / TERMS;     // values of K a stage
+    __shared__ __align__(1024) _Float16 lds[S::STAGES * PART];
+    const Place at = (HALF ? list.halves : list.fulls)[place_of_block()];
     const Matrix t = list.matrices[at.matrix];
     const Work<TERMS> w(ws, t);
     int32_t ti, tj;
-    if (MODE == kGram || MODE == kSquare) {          // tiles of the lower half, row by row
-        ti = static_cast<int32_t>((sqrtf(8.f * at.local + 1.f) - 1.f) * 0.5f);
-        while (ti * (ti + 1) / 2 > at.local) --ti;
-        while ((ti + 1) * (ti + 2) / 2 <= at.local) ++ti;
-        tj = at.local - ti * (ti + 1) / 2;
-    } else {
-        ti = at.local / (t.mp / T);
-        tj = at.local % (t.mp / T);
-    }
-    const int32_t depth = MODE == kGram ? t.mp : t.np;
+    if (HALF) half_tile_of(at.local, t.np / S::TI, ti, tj);
+    else tile_of(at.local, t.np / S::TI, t.mp / S::TJ, ti, tj);
+    const int32_t depth = MODE == kGram ? t.mp : t.np, all = depth / STEP;
     const int64_t stride = depth;
-    const auto left = [&](int low) { return MODE == kGram ? w.x(low) : MODE == kSquare ? w.a(low) : w.b(low); };
-    const auto right = [&](int low) { return MODE == kGram ? w.x(low) : MODE == kSquare ? w.a(low) : w.xt(k.turn, low); };
-    const int64_t l_at = static_cast<int64_t>(ti) * T * stride, r_at = static_cast<int64_t>(tj) * T * stride;
-    const int32_t per = depth / kDepth, all = per * (TERMS == 2 ? 3 : 1);
-    // terms = 2: hi hi, then hi lo, then lo hi
-    const auto load = [&](int32_t i) {
-        const int32_t part = TERMS == 2 ? i / per : 0, q = TERMS == 2 ? i % per : i;
-        _Float16* to = lds + (i & 1) * kStage;
-        stage<T>(left(part == 2) + l_at + q * kDepth, stride, to);
-        stage<T>(right(part == 1) + r_at + q * kDepth, stride, to + T * kDepth);
+    const auto left = [&](int low) { return (MODE == kGram ? w.x(low) : MODE == kSquare ? w.a(low) : w.b(low)) + ti * S::TI * stride; };
+    const auto right = [&](int low) { return (MODE == kGram ? w.x(low) : MODE == kSquare ? w.a(low) : w.xt(k.turn, low)) + tj * S::TJ * stride; };
+    const _Float16* const l_at[2] = {left(0), left(TERMS - 1)};
+    const _Float16* const r_at[2] = {right(0), right(TERMS - 1)};
+    const auto load = [&](int32_t i, int turn) {
+        _Float16* const to = lds + turn * PART;
+        stage<S, TERMS, true>(l_at[0] + i * STEP, l_at[1] + i * STEP, stride, to);
+        stage<S, TERMS, false>(r_at[0] + i * STEP, r_at[1] + i * STEP, stride, to + S::TI * kDepth);
     };
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
-    Float4 acc[F][F] = {};
-    load(0);
-    for (int32_t i = 0; i < all; ++i) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (i + 1 < all) load(i + 1);
-        const _Float16* const l = lds + (i & 1) * kStage + (wi * (T / 2) + (lane & 15)) * kDepth;
-        const _Float16* const r = lds + (i & 1) * kStage + T * kDepth + (wj * (T / 2) + (lane & 15)) * kDepth;
-#pragma unroll
-        for (int q = 0; q < kDepth / 32; ++q) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / S::WJ, wj = wave % S::WJ;
+    Float4 acc[S::FI][S::FJ] = {};
+    const auto multiply = [&](int turn) {
+        const _Float16* const l = lds + turn * PART + (wi * S::FI * 16 + (lane & 15)) * kDepth;
+        const _Float16* const r = lds + turn * PART + (S::TI + wj * S::FJ * 16 + (lane & 15)) * kDepth;
+        Half8 lv[TERMS][S::FI], rv[TERMS][S::FJ];
+        const auto read = [&](int q, Half8(&lq)[S::FI], Half8(&rq)[S::FJ]) {
             const int pack = (((lane >> 4) + 4 * q) ^ ((lane & 15) >> 1)) * 8;
-            Half8 lv[F], rv[F];
 #pragma unroll
-            for (int f = 0; f < F; ++f) lv[f] = *reinterpret_cast<const Half8*>(l + f * 16 * kDepth + pack);
+            for (int f = 0; f < S::FI; ++f) lq[f] = *reinterpret_cast<const Half8*>(l + f * 16 * kDepth + pack);
 #pragma unroll
-            for (int f = 0; f < F; ++f) rv[f] = *reinterpret_cast<const Half8*>(r + f * 16 * kDepth + pack);
+            for (int f = 0; f < S::FJ; ++f) rq[f] = *reinterpret_cast<const Half8*>(r + f * 16 * kDepth + pack);
+        };
+        const auto add = [&](const Half8(&lq)[S::FI], const Half8(&rq)[S::FJ]) {
 #pragma unroll
-            for (int fi = 0; fi < F; ++fi)
+            for (int fi = 0; fi < S::FI; ++fi)
 #pragma unroll
-                for (int fj = 0; fj < F; ++fj) acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(lv[fi], rv[fj], acc[fi][fj], 0, 0, 0);
+                for (int fj = 0; fj < S::FJ; ++fj) acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rq[fj], lq[fi], acc[fi][fj], 0, 0, 0);
+        };
+        if constexpr (TERMS == 2) {
+            read(0, lv[0], rv[0]);
+            read(1, lv[1], rv[1]);
+            add(lv[0], rv[0]);
+            add(lv[0], rv[1]);
+            add(lv[1], rv[0]);
+        } else {
+            read(0, lv[0], rv[0]);
+            add(lv[0], rv[0]);
+            read(1, lv[0], rv[0]);
+            add(lv[0], rv[0]);
         }
+    };
+    int turn = 0, next = S::STAGES - 1;
+#pragma unroll
+    for (int i = 0; i < S::STAGES - 1; ++i)
+        if (i < all) load(i, i);
+    for (int32_t i = 0; i + 1 < all; ++i) {
+        if (i + S::STAGES - 1 <= all) arrived<(S::STAGES - 2) * S::LOADS>();
+        else arrived<0>();
+        if (i + S::STAGES - 1 < all) load(i + S::STAGES - 1, next);
+        next = next + 1 == S::STAGES ? 0 : next + 1;
+        multiply(turn);
+        turn = turn + 1 == S::STAGES ? 0 : turn + 1;
     }
-    // through LDS, so that memory is met in rows of the output and in rows of its transpose
-    __syncthreads();
-    float* const tile = reinterpret_cast<float*>(memory);
+    arrived<0>();
+    // What the last part of the output needs of A0 or X is on its way while the last products are taken.
+    const int32_t row0 = ti * S::TI + wi * S::FI * 16 + (lane & 15) * S::GI, col0 = tj * S::TJ + wj * S::FJ * 16 + (lane >> 4) * N;
+    const int64_t wide = HALF ? t.np : t.mp;             // of an output row
+    const auto row_of = [&](int fi) { return row0 + fi / S::GI * 16 * S::GI + fi % S::GI; };
+    constexpr bool READS = MODE != kGram, LOW = READS && (TERMS == 2 || !HALF);
+    Half8 hi[READS ? ROWS : 1][GROUPS][N / 8 ? N / 8 : 1], lo[LOW ? ROWS : 1][GROUPS][N / 8 ? N / 8 : 1];
+    if constexpr (READS) {
 #pragma unroll
-    for (int fi = 0; fi < F; ++fi)
+        for (int fi = 0; fi < ROWS; ++fi)
 #pragma unroll
-        for (int fj = 0; fj < F; ++fj)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                tile[(wi * (T / 2) + fi * 16 + (lane >> 4) * 4 + e) * LINE + wj * (T / 2) + fj * 16 + (lane & 15)] =
-                    acc[fi][fj][e] * (kDown * kDown);
-    __syncthreads();
-    float lr = 0.f, keep = 0.f;
-    if (MODE == kFinish) {
+            for (int g = 0; g < GROUPS; ++g) {
+                const int64_t from = row_of(fi) * wide + col0 + g * 4 * N;
+                load_halves((HALF ? w.a(0) : w.x(0)) + from, hi[fi][g]);
+                if constexpr (LOW) load_halves((HALF ? w.a(1) : w.x(1)) + from, lo[fi][g]);
+            }
+    }
+    multiply(turn);
+
+    Update u = {k.lr, k.decay, k.optimizer != 0};
+    if constexpr (MODE == kFinish) {
         if (skipped(k.grad_scale)) return;
-        lr = k.lr, keep = k.decay;
         if (k.lr_now) {
-            lr = static_cast<float>(*k.lr_now);
-            keep = static_cast<float>(1. - *k.lr_now * k.lr_decay);
+            u.lr = static_cast<float>(*k.lr_now);
+            u.keep = static_cast<float>(1. - *k.lr_now * k.lr_decay);
         }
         const float ratio = static_cast<float>(t.rows) / static_cast<float>(t.cols);
-        lr *= k.scale_rule == CS_MUON_SCALE_SHAPE ? sqrtf(fmaxf(1.f, ratio))
-              : k.scale_rule == CS_MUON_SCALE_RMS ? 0.2f * sqrtf(static_cast<float>(max(t.rows, t.cols))) : 1.f;
+        u.lr *= k.scale_rule == CS_MUON_SCALE_SHAPE ? sqrtf(fmaxf(1.f, ratio))
+                : k.scale_rule == CS_MUON_SCALE_RMS ? 0.2f * sqrtf(static_cast<float>(max(t.rows, t.cols))) : 1.f;
     }
     const bool tall = t.rows > t.cols;
-    const auto finish = [&](int64_t row, int64_t col, float x) {
-        if (row >= t.rows || col >= t.cols) return;
-        const int64_t to = row * t.p_stride + col;
-        write(t.p, k.p_fmt, to, k.optimizer ? fmaf(read(t.p, k.p_fmt, to), keep, -lr * x) : x);
-    };
-    const int64_t wide = MODE == kGram || MODE == kSquare ? t.np : t.mp;         // of an output row
-    for (int i = threadIdx.x; i < T * T / 8; i += kThreads) {
-        const int r = i / (T / 8), c = i % (T / 8) * 8, row = ti * T + r, col = tj * T + c;
-        const int64_t to = row * wide + col;
-        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = tile[r * LINE + c + e];
-        if (MODE == kGram) {
+    for (int g = 0; g < GROUPS; ++g) {
+        const int32_t col = col0 + g * 4 * N;
+        float dj[N];
+        if constexpr (MODE == kSquare) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (row == col + e) {
-                    w.da()[row] = v[e];
-                    v[e] = 0.f;
-                }
-        } else {
-            // the elements of A0 or X that go past the product
-            const Half8 hi = *reinterpret_cast<const Half8*>((MODE == kSquare ? w.a(0) : w.x(0)) + to);
-            Half8 lo = {};
-            if (TERMS == 2 || MODE != kSquare) lo = *reinterpret_cast<const Half8*>((MODE == kSquare ? w.a(1) : w.x(1)) + to);
-            const float d = MODE == kSquare ? w.da()[row] : k.a + w.db()[row];
+            for (int e = 0; e < N; e += 4) {
+                const Float4 d = *reinterpret_cast<const Float4*>(w.da() + col + e);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = (static_cast<float>(hi[e]) + static_cast<float>(lo[e])) * kDown;
-                if (MODE == kSquare) {
-                    if (row == col + e) {
-                        w.db()[row] = fmaf(k.b, d, k.c * fmaf(d, d, v[e]));
-                        v[e] = 0.f;
-                    } else {
-                        v[e] = fmaf(k.b, x, k.c * fmaf(d + w.da()[col + e], x, v[e]));
+                for (int x = 0; x < 4; ++x) dj[e + x] = d[x];
+            }
+        }
+#pragma unroll
+        for (int gi = 0; gi < S::FI; gi += S::GI) {
+            float out[S::GI][N];
+#pragma unroll
+            for (int f = 0; f < S::GI; ++f) {
+                const int fi = gi + f;
+                const int32_t row = row_of(fi);
+                const float d = MODE == kSquare ? w.da()[row] : MODE == kGram ? 0.f : k.a + w.db()[row];
+                float diagonal = 0.f;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float c = acc[fi][g * S::GJ + e / 4][e % 4] * (kDown * kDown);
+                    float x = 0.f;
+                    if constexpr (READS) {
+                        x = static_cast<float>(hi[fi][g][e / 8][e % 8]);
+                        if constexpr (LOW) x += static_cast<float>(lo[fi][g][e / 8][e % 8]);
+                        x *= kDown;
                     }
+                    out[f][e] = MODE == kGram ? c : MODE == kSquare ? fmaf(k.b, x, k.c * fmaf(d + dj[e], x, c)) : fmaf(d, x, c);
+                    if (HALF && row == col + e) {
+                        diagonal = MODE == kGram ? c : fmaf(k.b, d, k.c * fmaf(d, d, c));
+                        out[f][e] = 0.f;
+                    }
+                }
+                if (HALF && row >= col && row < col + N) (MODE == kGram ? w.da() : w.db())[row] = diagonal;
+                if constexpr (MODE == kFinish) {
+                    if (!tall) update(t, k.p_fmt, u, row, col, out[f]);
                 } else {
-                    v[e] = fmaf(d, x, v[e]);
+                    const int64_t to = row * wide + col;
+                    const auto place = [&](int low) { return (MODE == kGram ? w.a(low) : MODE == kSquare ? w.b(low) : w.x(low)) + to; };
+                    store_halves(place(0), TERMS == 2 || MODE == kApply ? place(1) : nullptr, out[f]);
+                }
+            }
+            // the transpose: of A and B the tile on the other side, of X the one that the next product reads
+            if (HALF ? ti == tj : MODE == kFinish && !tall) continue;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                float turned[S::GI];
+#pragma unroll
+                for (int f = 0; f < S::GI; ++f) turned[f] = out[f][e];
+                if constexpr (MODE == kFinish) {
+                    update(t, k.p_fmt, u, col + e, row_of(gi), turned);
+                } else {
+                    const int64_t to = static_cast<int64_t>(col + e) * t.np + row_of(gi);
+                    const auto place = [&](int low) { return (MODE == kGram ? w.a(low) : MODE == kSquare ? w.b(low) : w.xt(1 - k.turn, low)) + to; };
+                    store_halves(place(0), TERMS == 2 ? place(1) : nullptr, turned);
                 }
             }
         }
-        if (MODE == kFinish) {
-            if (!tall)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) finish(row, col + e, v[e]);
-        } else {
-            Half8 hi, lo;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                _Float16 h, l;
-                split(v[e] * kUp, h, l);
-                hi[e] = h, lo[e] = l;
-            }
-            const auto out = [&](int low) { return MODE == kGram ? w.a(low) : MODE == kSquare ? w.b(low) : w.x(low); };
-            *reinterpret_cast<Half8*>(out(0) + to) = hi;
-            if (TERMS == 2 || MODE == kApply) *reinterpret_cast<Half8*>(out(1) + to) = lo;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) tile[r * LINE + c + e] = v[e];
-    }
-    // the transpose: of A and B the tile on the other side, of X the one that the next product reads
-    if (((MODE == kGram || MODE == kSquare) && ti == tj) || (MODE == kFinish && !tall)) return;
-    __syncthreads();
-    const int64_t high = t.np;
-    for (int i = threadIdx.x; i < T * T / 8; i += kThreads) {
-        const int r = i / (T / 8), c = i % (T / 8) * 8;
-        const int64_t row = tj * T + r, col = ti * T + c;
-        Half8 hi, lo;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = tile[(c + e) * LINE + r];
-            if (MODE == kFinish) {
-                finish(row, col + e, v);
-            } else {
-                _Float16 h, l;
-                split(v * kUp, h, l);
-                hi[e] = h, lo[e] = l;
-            }
-        }
-        if (MODE == kFinish) continue;
-        const auto out = [&](int low) { return MODE == kGram ? w.a(low) : MODE == kSquare ? w.b(low) : w.xt(1 - k.turn, low); };
-        *reinterpret_cast<Half8*>(out(0) + row * high + col) = hi;
-        if (TERMS == 2) *reinterpret_cast<Half8*>(out(1) + row * high + col) = lo;
     }
 }
 
@@ -499,7 +602,10 @@ bool hyper_ok(const cs_muon* h) {
            h->scale <= CS_MUON_SCALE_ONE && steps_ok(h);
 }
 
-template <int T, int TERMS>
+using Large = Shape<2, 2, 4, 4, 2>;
+using Small = Shape<2, 2, 2, 2, 4>;
+
+template <typename S, int TERMS>
 int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const double* lr, const float* grad_scale, char* ws, hipStream_t s) {
     const List at = list_of(l);
     double* const squares = reinterpret_cast<double*>(ws + l->work);
@@ -514,16 +620,16 @@ int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const doub
         Product k = {};
         k.a = static_cast<float>(h->coefs[i][0]), k.b = static_cast<float>(h->coefs[i][1]), k.c = static_cast<float>(h->coefs[i][2]);
         k.turn = i & 1;
-        k_muon_product<T, TERMS, kGram><<<halves, kThreads, 0, s>>>(at, k, ws);
-        k_muon_product<T, TERMS, kSquare><<<halves, kThreads, 0, s>>>(at, k, ws);
+        k_muon_product<S, TERMS, kGram><<<halves, S::THREADS, 0, s>>>(at, k, ws);
+        k_muon_product<S, TERMS, kSquare><<<halves, S::THREADS, 0, s>>>(at, k, ws);
         if (i + 1 < h->steps) {
-            k_muon_product<T, TERMS, kApply><<<fulls, kThreads, 0, s>>>(at, k, ws);
+            k_muon_product<S, TERMS, kApply><<<fulls, S::THREADS, 0, s>>>(at, k, ws);
         } else {
             k.p_fmt = l->p_fmt, k.optimizer = optimizer, k.scale_rule = h->scale;
             k.lr = static_cast<float>(h->lr), k.decay = static_cast<float>(1. - h->lr * h->weight_decay);
             k.lr_decay = static_cast<float>(h->weight_decay);
             k.lr_now = lr, k.grad_scale = grad_scale;
-            k_muon_product<T, TERMS, kFinish><<<fulls, kThreads, 0, s>>>(at, k, ws);
+            k_muon_product<S, TERMS, kFinish><<<fulls, S::THREADS, 0, s>>>(at, k, ws);
         }
         if (int rc = launched()) return rc;
     }
@@ -542,8 +648,8 @@ int run(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const double*
     if (!spans_apart(written, read)) return CS_EINVAL;
     char* const ws = static_cast<char*>(workspace);
     const hipStream_t s = stream_of(stream);
-    if (l->tile == 128) return l->terms == 1 ? run_as<128, 1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<128, 2>(h, l, optimizer, lr, grad_scale, ws, s);
-    return l->terms == 1 ? run_as<64, 1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<64, 2>(h, l, optimizer, lr, grad_scale, ws, s);
+    if (l->tile == 128) return l->terms == 1 ? run_as<Large, 1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<Large, 2>(h, l, optimizer, lr, grad_scale, ws, s);
+    return l->terms == 1 ? run_as<Small, 1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<Small, 2>(h, l, optimizer, lr, grad_scale, ws, s);
 }
 
 }  // namespace
