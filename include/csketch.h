@@ -726,8 +726,8 @@ typedef struct cs_matrix {
 } cs_matrix;
 typedef struct cs_matrix_list {
     void* memory;                            /* device */
-    int64_t matrices, pieces, halves, fulls, work;
-    int32_t p_fmt, g_fmt, terms, tile, moments;
+    int64_t matrices, littles, pieces, halves, fulls, work;
+    int32_t p_fmt, g_fmt, terms, moments, half_tile, full_tile, little_cols, unused;
 } cs_matrix_list;
 int cs_matrix_list_bytes(const cs_matrix* stacks, int32_t count, int32_t terms, size_t* bytes);
 int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int32_t p_fmt, int32_t g_fmt, int32_t terms, void* memory, size_t bytes,

@@ -24,7 +24,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kEdge = 64;                    // of the pieces in which u is read, and what all sizes are rounded up to
-constexpr int kDepth = 64;                   // values of a row in LDS, 128 bytes
 constexpr float kUp = 1024.f, kDown = 1.f / 1024.f;
 
 typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
@@ -43,33 +42,45 @@ struct Matrix {
 struct Place {
     int32_t matrix, local;
 };
+// A tile of an output, with all that its workgroup has to know before its first load
+struct Tile {
+    int64_t at;
+    int32_t np, mp, ti, tj, matrix, unused;
+};
 constexpr int kBatch = 40;
 struct Batch {
     Matrix t[kBatch];
 };
 static_assert(sizeof(Batch) < 3800, "kernel arguments are limited to 4 KB");
 
-// A list in device memory: Matrix[count], then the places of all pieces, of the tiles of all lower halves of A, and of all tiles of X.
+// A list in device memory: Matrix[count], then all tiles of lower halves of A, all tiles of X, and the places of all pieces.
 struct List {
     const Matrix* matrices;
-    const Place *pieces, *halves, *fulls;
+    const Tile *halves, *fulls;
+    const Place* pieces;
 };
 
-// A matrix's part of the workspace: X, X^T twice (read and written in turns), A0, B0, each as its upper and its lower 11 bits, and the
-// diagonals of A and B.  With one term the lower bits of X alone are kept.
+// A matrix's part of the workspace: X, X^T twice (read and written in turns), A0, B0, and the diagonals of A and B.  Values are two halves, the upper
+// and the lower 11 bits.  Where the products take both (two terms) they lie in one array, 32 upper ones and then the 32 lower ones of the same
+// columns; otherwise the lower ones of X have an array of their own and there are no others.
 template <int TERMS>
 struct Work {
     _Float16* base;
     int64_t nm, nn;
     int32_t np;
-    __device__ __forceinline__ Work(char* ws, const Matrix& t)
-        : base(reinterpret_cast<_Float16*>(ws + t.at)), nm(static_cast<int64_t>(t.np) * t.mp), nn(static_cast<int64_t>(t.np) * t.np), np(t.np) {}
-    __device__ __forceinline__ _Float16* x(int low) const { return base + low * nm; }
-    __device__ __forceinline__ _Float16* xt(int turn, int low) const { return base + (2 + turn * TERMS + low) * nm; }
-    __device__ __forceinline__ _Float16* a(int low) const { return base + (2 + 2 * TERMS) * nm + low * nn; }
-    __device__ __forceinline__ _Float16* b(int low) const { return base + (2 + 2 * TERMS) * nm + (TERMS + low) * nn; }
+    __device__ __forceinline__ Work(char* ws, int64_t at, int32_t n, int32_t m)
+        : base(reinterpret_cast<_Float16*>(ws + at)), nm(static_cast<int64_t>(n) * m), nn(static_cast<int64_t>(n) * n), np(n) {}
+    __device__ __forceinline__ _Float16* x() const { return base; }
+    __device__ __forceinline__ _Float16* xt(int turn) const { return base + (2 + turn * TERMS) * nm; }
+    __device__ __forceinline__ _Float16* a() const { return base + (2 + 2 * TERMS) * nm; }
+    __device__ __forceinline__ _Float16* b() const { return base + (2 + 2 * TERMS) * nm + TERMS * nn; }
     __device__ __forceinline__ float* da() const { return reinterpret_cast<float*>(base + (2 + 2 * TERMS) * nm + 2 * TERMS * nn); }
     __device__ __forceinline__ float* db() const { return da() + np; }
+    // of an array's value, and from there to its lower half
+    static __device__ __forceinline__ int64_t place(int64_t row, int32_t col, int32_t width) {
+        return TERMS == 1 ? row * width + col : row * 2 * width + col / 32 * 64 + col % 32;
+    }
+    __device__ __forceinline__ int64_t to_low() const { return TERMS == 1 ? nm : 32; }
 };
 int64_t work_bytes(int64_t np, int64_t mp, int terms) {
     return 2 * ((2 + 2 * terms) * np * mp + 2 * terms * np * np) + 2 * 4 * np;
@@ -78,40 +89,108 @@ int64_t work_bytes(int64_t np, int64_t mp, int terms) {
 __global__ void __launch_bounds__(64) k_list_matrices(Batch b, Matrix* out, int count) {
     if (static_cast<int>(threadIdx.x) < count) out[threadIdx.x] = b.t[threadIdx.x];
 }
-// every place's matrix: the last that begins at or before it
-__global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices, int count, int which, Place* out, int64_t places) {
+// Tiles in bands of 8 rows, column by column of a band; of a lower half those on and below the diagonal.
+__device__ __forceinline__ void tile_of(int32_t local, int32_t down, int32_t across, int32_t& ti, int32_t& tj) {
+    const int32_t band = local / (8 * across), in = local - band * 8 * across, high = min(8, down - 8 * band);
+    ti = 8 * band + in % high;
+    tj = in / high;
+}
+__device__ __forceinline__ void half_tile_of(int32_t local, int32_t down, int32_t& ti, int32_t& tj) {
+    int32_t band = static_cast<int32_t>((sqrtf(8.f * local + 1.f) - 1.f) * 0.0625f);
+    while (4 * band * (8 * band + 1) > local) --band;
+    while (4 * (band + 1) * (8 * band + 9) <= local) ++band;
+    int32_t in = local - 4 * band * (8 * band + 1);
+    const int32_t high = min(8, down - 8 * band);
+    if (in < 8 * band * high) {
+        ti = 8 * band + in % high;
+        tj = in / high;
+        return;
+    }
+    in -= 8 * band * high;
+    ti = 0;
+    while (in > ti) in -= ++ti;
+    ti += 8 * band;
+    tj = 8 * band + in;
+}
+
+enum { kPieces, kHalves, kFulls };
+// The matrix of every place (the last that begins at or before it), and what there is to know of it; edge: of a tile.
+template <int WHICH, typename Out>
+__global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices, int begin, int end, int edge, Out* out, int64_t places) {
     const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     if (c >= places) return;
     const auto first = [&](int i) {
         const Matrix& t = matrices[i];
-        return which == 0 ? t.first_piece : which == 1 ? t.first_half : t.first_full;
+        return WHICH == kPieces ? t.first_piece : WHICH == kHalves ? t.first_half : t.first_full;
     };
-    int lo = 0, hi = count - 1;
+    int lo = begin, hi = end - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (first(mid) <= c) lo = mid;
         else hi = mid - 1;
     }
-    out[c] = Place{lo, static_cast<int32_t>(c - first(lo))};
+    const int32_t local = static_cast<int32_t>(c - first(lo));
+    if constexpr (WHICH == kPieces) {
+        out[c] = Place{lo, local};
+    } else {
+        const Matrix& t = matrices[lo];
+        Tile tile = {t.at, t.np, t.mp, 0, 0, lo, 0};
+        if (WHICH == kHalves) half_tile_of(local, t.np / edge, tile.ti, tile.tj);
+        else tile_of(local, t.np / edge, t.mp / edge, tile.ti, tile.tj);
+        out[c] = tile;
+    }
 }
 
-template <typename T>
-__device__ __forceinline__ float value_at(const void* p, int64_t at) { return static_cast<float>(static_cast<const T*>(p)[at]); }
-__device__ __forceinline__ float read(const void* p, int fmt, int64_t at) {
-    return fmt == CS_FMT_F32 ? value_at<float>(p, at) : fmt == CS_FMT_BF16 ? value_at<bf16>(p, at) : value_at<f16>(p, at);
-}
 __device__ __forceinline__ bool skipped(const float* grad_scale) { return grad_scale && !(fabsf(*grad_scale) < INFINITY); }
+
+// N neighbouring values of a row from column `col` on, 0 from column `cols` on
+template <typename T, int N>
+__device__ __forceinline__ void read_as(const T* row, int32_t col, int32_t cols, float (&v)[N]) {
+    if (col + N <= cols) {
+        load_pack<T, N>(row + col, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = col + e < cols ? static_cast<float>(row[col + e]) : 0.f;
+    }
+}
+template <int N>
+__device__ __forceinline__ void read_row(const void* p, int fmt, int64_t row_at, int32_t col, int32_t cols, float (&v)[N]) {
+    if (fmt == CS_FMT_F32) read_as<float, N>(static_cast<const float*>(p) + row_at, col, cols, v);
+    else if (fmt == CS_FMT_BF16) read_as<bf16, N>(static_cast<const bf16*>(p) + row_at, col, cols, v);
+    else read_as<f16, N>(static_cast<const f16*>(p) + row_at, col, cols, v);
+}
 
 struct Moment {
     float mu;
-    int nesterov;
+    int nesterov, g_fmt;
     const float* grad_scale;
 };
-// u at an element, with the moment as it is now
-__device__ __forceinline__ float direction(const Matrix& t, int g_fmt, const Moment& k, float s, int64_t row, int64_t col) {
-    if (!t.moment) return read(t.g, g_fmt, row * t.g_stride + col);
-    const float m = t.moment[row * t.cols + col];
-    return k.nesterov ? fmaf(k.mu, m, s * read(t.g, g_fmt, row * t.g_stride + col)) : m;
+// u of N neighbouring elements, 0 outside the matrix.  STEP: the moment takes the gradient first, and is written.
+template <bool STEP, int N>
+__device__ __forceinline__ void direction(const Matrix& t, const Moment& k, float s, int32_t row, int32_t col, float (&u)[N]) {
+    if (row >= t.rows || col >= t.cols) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) u[e] = 0.f;
+        return;
+    }
+    float m[N];
+    if (!t.moment || STEP || k.nesterov) read_row<N>(t.g, k.g_fmt, row * t.g_stride, col, t.cols, u);
+    if (!t.moment) return;
+    float* const at = t.moment + static_cast<int64_t>(row) * t.cols;
+    read_as<float, N>(at, col, t.cols, m);
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        if (STEP) m[e] = fmaf(k.mu, m[e], s * u[e]);
+        u[e] = k.nesterov ? fmaf(k.mu, m[e], s * u[e]) : m[e];
+    }
+    if (!STEP) return;
+    if (col + N <= t.cols) {
+        store_pack<false>(at + col, m);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (col + e < t.cols) at[col + e] = m[e];
+    }
 }
 // rows and columns [row, row + 64), [col, col + 64) of the matrix as it is given
 struct Piece {
@@ -123,47 +202,52 @@ struct Piece {
     }
 };
 
+// The sum over a workgroup of kThreads, in a fixed order, in every thread
+__device__ __forceinline__ double workgroup_sum(double sum, double (&buf)[kThreads / 64]) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = 0.;
+#pragma unroll
+    for (int w = 0; w < kThreads / 64; ++w) sum += buf[w];
+    return sum;
+}
+// 1 / (|u| + eps) from the sum of squares, or 0 for a matrix of zeros
+__device__ __forceinline__ double inverse_of(double sum, double eps) { return sum == 0. ? 0. : 1. / (sqrt(sum) + eps); }
+
+constexpr int kFour = 4;                     // neighbouring elements a thread
+
 // The moment, and a piece's sum of squares of u (binary64, a fixed order).
-__global__ void __launch_bounds__(kThreads) k_muon_moment(List list, int g_fmt, Moment k, double* squares) {
-    __shared__ double sums[kThreads / 64];
+__global__ void __launch_bounds__(kThreads) k_muon_moment(List list, Moment k, double* squares) {
+    __shared__ double buf[kThreads / 64];
     const Place at = list.pieces[blockIdx.x];
     const Matrix t = list.matrices[at.matrix];
     const Piece piece(t, at.local);
-    const bool skip = skipped(k.grad_scale);
-    const float s = k.grad_scale ? *k.grad_scale : 1.f;
     double sum = 0.;
-    for (int i = threadIdx.x; i < kEdge * kEdge; i += kThreads) {
-        const int64_t row = piece.row + i / kEdge, col = piece.col + i % kEdge;
-        if (row < t.rows && col < t.cols && !skip) {
-            if (t.moment) {
-                float& m = t.moment[row * t.cols + col];
-                m = fmaf(k.mu, m, s * read(t.g, g_fmt, row * t.g_stride + col));
-            }
-            const double u = direction(t, g_fmt, k, s, row, col);
-            sum += u * u;
+    if (!skipped(k.grad_scale)) {
+        const float s = k.grad_scale ? *k.grad_scale : 1.f;
+#pragma unroll
+        for (int i = 0; i < kEdge * kEdge / kFour; i += kThreads) {
+            const int q = i + threadIdx.x;
+            float u[kFour];
+            direction<true>(t, k, s, piece.row + q / (kEdge / kFour), piece.col + q % (kEdge / kFour) * kFour, u);
+#pragma unroll
+            for (int e = 0; e < kFour; ++e) sum = fma(static_cast<double>(u[e]), static_cast<double>(u[e]), sum);
         }
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) squares[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+    sum = workgroup_sum(sum, buf);
+    if (threadIdx.x == 0) squares[blockIdx.x] = sum;
 }
 
-// A matrix's 1 / (|u| + eps)
-__global__ void __launch_bounds__(kThreads) k_muon_norm(List list, double eps, const double* squares, double* inverse) {
-    __shared__ double sums[kThreads / 64];
+// A matrix's sum of squares, in place of its first piece's
+__global__ void __launch_bounds__(kThreads) k_muon_norm(List list, double* squares) {
+    __shared__ double buf[kThreads / 64];
     const Matrix& t = list.matrices[blockIdx.x];
     double sum = 0.;
     for (int i = threadIdx.x; i < t.pieces; i += kThreads) sum += squares[t.first_piece + i];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = sums[0] + sums[1] + sums[2] + sums[3];
-        inverse[blockIdx.x] = sum == 0. ? 0. : 1. / (sqrt(sum) + eps);
-    }
+    sum = workgroup_sum(sum, buf);
+    if (threadIdx.x == 0 && t.pieces) squares[t.first_piece] = sum;
 }
 
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
@@ -171,27 +255,41 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
     lo = static_cast<_Float16>(v - static_cast<float>(hi));
 }
 
-// X and X^T from u, zero behind the last row and column
+// X and X^T from u, zero behind the last row and column.  joined: a matrix's squares are summed already.
 template <int TERMS>
-__global__ void __launch_bounds__(kThreads) k_muon_begin(List list, int g_fmt, Moment k, const double* inverse, char* ws) {
+__global__ void __launch_bounds__(kThreads) k_muon_begin(List list, Moment k, double eps, const double* squares, bool joined, char* ws) {
     __shared__ float tile[kEdge][kEdge + 1];
+    __shared__ double buf[kThreads / 64];
     const Place at = list.pieces[blockIdx.x];
     const Matrix t = list.matrices[at.matrix];
     const Piece piece(t, at.local);
-    const Work<TERMS> w(ws, t);
+    const Work<TERMS> w(ws, t.at, t.np, t.mp);
     const float s = k.grad_scale ? *k.grad_scale : 1.f;
-    const double one = inverse[at.matrix] * static_cast<double>(kUp);
-    for (int i = threadIdx.x; i < kEdge * kEdge; i += kThreads) {
-        const int64_t row = piece.row + i / kEdge, col = piece.col + i % kEdge;
-        tile[i / kEdge][i % kEdge] =
-            row < t.rows && col < t.cols ? static_cast<float>(direction(t, g_fmt, k, s, row, col) * one) : 0.f;
+    float u[kEdge * kEdge / kFour / kThreads][kFour];
+#pragma unroll
+    for (int i = 0; i < kEdge * kEdge / kFour; i += kThreads) {
+        const int q = i + threadIdx.x;
+        direction<false>(t, k, s, piece.row + q / (kEdge / kFour), piece.col + q % (kEdge / kFour) * kFour, u[i / kThreads]);
+    }
+    double sum = 0.;
+    if (joined) {
+        sum = squares[t.first_piece];
+    } else {
+        for (int i = threadIdx.x; i < t.pieces; i += kThreads) sum += squares[t.first_piece + i];
+        sum = workgroup_sum(sum, buf);
+    }
+    const double one = inverse_of(sum, eps) * static_cast<double>(kUp);
+#pragma unroll
+    for (int i = 0; i < kEdge * kEdge / kFour; i += kThreads) {
+        const int q = i + threadIdx.x;
+#pragma unroll
+        for (int e = 0; e < kFour; ++e)
+            tile[q / (kEdge / kFour)][q % (kEdge / kFour) * kFour + e] = static_cast<float>(u[i / kThreads][e] * one);
     }
     __syncthreads();
     const bool tall = t.rows > t.cols;
     // as it is given: X of a wide matrix, X^T of a tall one; and the other way round
-    const int64_t across = tall ? t.np : t.mp, down = tall ? t.mp : t.np;
-    const auto as_is = [&](int low) { return tall ? w.xt(0, low) : w.x(low); };
-    const auto turned = [&](int low) { return tall ? w.x(low) : w.xt(0, low); };
+    _Float16 *const as_is = tall ? w.xt(0) : w.x(), *const turned = tall ? w.x() : w.xt(0);
     for (int i = threadIdx.x; i < kEdge * kEdge / 8; i += kThreads) {
         const int r = i / 8, c = i % 8 * 8;
         Half8 hi, lo;
@@ -201,46 +299,57 @@ __global__ void __launch_bounds__(kThreads) k_muon_begin(List list, int g_fmt, M
             split(tile[r][c + e], h, l);
             hi[e] = h, lo[e] = l;
         }
-        int64_t to = (piece.row + r) * across + piece.col + c;
-        *reinterpret_cast<Half8*>(as_is(0) + to) = hi;
-        if (TERMS == 2 || !tall) *reinterpret_cast<Half8*>(as_is(1) + to) = lo;
+        _Float16* to = as_is + Work<TERMS>::place(piece.row + r, piece.col + c, tall ? t.np : t.mp);
+        *reinterpret_cast<Half8*>(to) = hi;
+        if (TERMS == 2 || !tall) *reinterpret_cast<Half8*>(to + w.to_low()) = lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             _Float16 h, l;
             split(tile[c + e][r], h, l);
             hi[e] = h, lo[e] = l;
         }
-        to = (piece.col + r) * down + piece.row + c;
-        *reinterpret_cast<Half8*>(turned(0) + to) = hi;
-        if (TERMS == 2 || tall) *reinterpret_cast<Half8*>(turned(1) + to) = lo;
+        to = turned + Work<TERMS>::place(piece.col + r, piece.row + c, tall ? t.mp : t.np);
+        *reinterpret_cast<Half8*>(to) = hi;
+        if (TERMS == 2 || tall) *reinterpret_cast<Half8*>(to + w.to_low()) = lo;
     }
 }
 
 enum { kGram, kSquare, kApply, kFinish };    // A = X X^T; B = b A + c A A; X = a X + B X; the same, into the parameters
 
-struct Product {
-    float a, b, c;
-    int turn;                                // which of the two X^T is read
-    // kFinish
+// What is made of the last X: p = decay p - lr scale X, or X itself
+struct Last {
     int p_fmt, optimizer, scale_rule;
     float decay, lr, lr_decay;
     const double* lr_now;
     const float* grad_scale;
 };
+struct Steps {
+    int count;
+    float coefs[CS_MUON_MAX_STEPS][3];
+};
+struct Product {
+    float a, b, c;
+    int turn;                                // which of the two X^T is read
+    Last last;                               // kFinish
+};
 
 typedef __attribute__((address_space(3))) void* LdsPointer;
 typedef const __attribute__((address_space(1))) void* GlobalPointer;
 
-// The tile of a workgroup: WI x WJ wavefronts, each with FI x FJ blocks of 16 x 16; `stages` parts of K are in LDS or on their way there.
-template <int WI_, int WJ_, int FI_, int FJ_, int STAGES_>
+// The tile of a workgroup: WI x WJ wavefronts, each with FI x FJ blocks of 16 x 16; STAGES parts of DEPTH values of K are in LDS or on
+// their way there.  WAVES_PER_SIMD: as many as the registers are shared out for.
+template <int WI_, int WJ_, int FI_, int FJ_, int STAGES_, int DEPTH_, int WAVES_PER_SIMD_>
 struct Shape {
-    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, STAGES = STAGES_;
+    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, STAGES = STAGES_, DEPTH = DEPTH_, WAVES_PER_SIMD = WAVES_PER_SIMD_;
     static constexpr int WAVES = WI * WJ, THREADS = WAVES * 64, TI = WI * FI * 16, TJ = WJ * FJ * 16;
     // Blocks that belong together: a lane has GI neighbouring rows of 4 GJ neighbouring columns of the output, so that both it and its
     // transpose are written in whole pieces of memory straight from the registers.
-    static constexpr int GI = FI < 4 ? FI : 4, GJ = FJ < 4 ? FJ : 4;
-    static constexpr int LOADS = (TI + TJ) / 8 / WAVES;                  // of 1 KB, a wavefront and stage
-    static_assert(TI % (8 * WAVES) == 0 && TJ % (8 * WAVES) == 0, "whole loads");
+    static constexpr int GI = FI < 4 ? FI : 4, GJ = FJ;
+    static constexpr int PACKS = DEPTH / 8, ROWS = 64 / PACKS;           // of 16 bytes, a row; rows that a wavefront loads at once
+    static constexpr int LOADS = (TI + TJ) / ROWS / WAVES;               // of 1 KB, a wavefront and stage
+    static_assert(TI % (ROWS * WAVES) == 0 && TJ % (ROWS * WAVES) == 0 && FI % GI == 0 && FJ <= 4 && (DEPTH == 32 || DEPTH == 64), "");
+    // the order of a row's packs in LDS: 16 lanes that read the same pack of 16 rows meet all banks once
+    static __device__ __forceinline__ int order(int place) { return DEPTH == 64 ? place >> 1 & 7 : place >> 2 & 3; }
 };
 // The row of the left tile that is place `at` of LDS: lane l of block f (of a group of GI) has row GI l + f.
 template <typename S>
@@ -255,51 +364,48 @@ __device__ __forceinline__ int right_row(int at) {
     return group * 16 * S::GJ + m / 4 * 4 * S::GJ + in / 16 * 4 + m % 4;
 }
 
-// Rows of 128 bytes into LDS, 64 values of K (one term) or 32 values of both terms.  A row's eight packs of 16 bytes lie in the order pack ^ (place /
-// 2 % 8): 16 lanes that read the same pack of 16 rows meet all banks once.
-template <typename S, int TERMS, bool LEFT>
-__device__ __forceinline__ void stage(const _Float16* high, const _Float16* low, int64_t stride, _Float16* lds) {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// Rows of DEPTH halves into LDS, their packs of 16 bytes in the order pack ^ order(place).  The lane's offsets in memory are the same for all parts
+// of K.
+template <typename S, bool LEFT>
+struct Stage {
+    static constexpr int N = (LEFT ? S::TI : S::TJ) / (S::ROWS * S::WAVES);
+    uint32_t offset[N];
+    __device__ __forceinline__ explicit Stage(uint32_t row_bytes) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 #pragma unroll
-    for (int q = 0; q < (LEFT ? S::TI : S::TJ) / (8 * S::WAVES); ++q) {
-        const int first = (q * S::WAVES + wave) * 8, at = first + (lane >> 3), row = LEFT ? left_row<S>(at) : right_row<S>(at);
-        const int pack = (lane & 7) ^ (at >> 1 & 7);
-        const _Float16* from = (TERMS == 2 ? (pack < 4 ? high : low) + pack % 4 * 8 : high + pack * 8) + row * stride;
-        __builtin_amdgcn_global_load_lds(reinterpret_cast<GlobalPointer>(reinterpret_cast<uintptr_t>(from)),
-                                         (LdsPointer)(lds + first * kDepth), 16, 0, 0);
+        for (int q = 0; q < N; ++q) {
+            const int at = (q * S::WAVES + wave) * S::ROWS + lane / S::PACKS, row = LEFT ? left_row<S>(at) : right_row<S>(at);
+            offset[q] = row * row_bytes + ((lane % S::PACKS) ^ S::order(at)) * 16;
+        }
     }
-}
+    __device__ __forceinline__ void load(const char* from, _Float16* lds) const {
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+            __builtin_amdgcn_global_load_lds(reinterpret_cast<GlobalPointer>(reinterpret_cast<uintptr_t>(from + offset[q])),
+                                             (LdsPointer)(lds + (q * S::WAVES + wave) * 512), 16, 0, 0);
+    }
+};
 // All but `left` of this wavefront's loads have arrived and its reads of LDS are done; then so are all wavefronts'.
 template <int LEFT>
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
-
-template <int N>
-__device__ __forceinline__ void load_halves(const _Float16* p, Half8 (&v)[N]) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = *reinterpret_cast<const Half8*>(p + 8 * e);
-}
-template <int N>
-__device__ __forceinline__ void store_halves(_Float16* high, _Float16* low, const float (&v)[N]) {
-    typedef _Float16 Halves __attribute__((ext_vector_type(N < 8 ? N : 8)));
-#pragma unroll
-    for (int e = 0; e < N; e += 8) {
-        Halves hi, lo;
-#pragma unroll
-        for (int k = 0; k < (N < 8 ? N : 8); ++k) {
-            _Float16 h, l;
-            split(v[e + k] * kUp, h, l);
-            hi[k] = h, lo[k] = l;
-        }
-        *reinterpret_cast<Halves*>(high + e) = hi;
-        if (low) *reinterpret_cast<Halves*>(low + e) = lo;
-    }
-}
 
 // N neighbouring parameters from column `col` of a row on: p = keep p - lr x (keep 0: x itself)
 struct Update {
     float lr, keep;
     bool optimizer;
 };
+__device__ __forceinline__ Update update_of(const Last& k, const Matrix& t) {
+    Update u = {k.lr, k.decay, k.optimizer != 0};
+    if (k.lr_now) {
+        u.lr = static_cast<float>(*k.lr_now);
+        u.keep = static_cast<float>(1. - *k.lr_now * k.lr_decay);
+    }
+    const float ratio = static_cast<float>(t.rows) / static_cast<float>(t.cols);
+    u.lr *= k.scale_rule == CS_MUON_SCALE_SHAPE ? sqrtf(fmaxf(1.f, ratio))
+            : k.scale_rule == CS_MUON_SCALE_RMS ? 0.2f * sqrtf(static_cast<float>(max(t.rows, t.cols))) : 1.f;
+    return u;
+}
 template <typename T, int N>
 __device__ __forceinline__ void update_as(const Matrix& t, const Update& u, int64_t row, int64_t col, const float (&x)[N]) {
     if (row >= t.rows || col >= t.cols) return;
@@ -332,84 +438,53 @@ __device__ __forceinline__ int place_of_block() {
     const int per = gridDim.x / 8, more = gridDim.x % 8, die = blockIdx.x % 8, at = blockIdx.x / 8;
     return die * per + min(die, more) + at;
 }
-// Tiles in bands of 8 rows, column by column of a band; of a lower half those on and below the diagonal.
-__device__ __forceinline__ void tile_of(int32_t local, int32_t down, int32_t across, int32_t& ti, int32_t& tj) {
-    const int32_t band = local / (8 * across), in = local - band * 8 * across, high = min(8, down - 8 * band);
-    ti = 8 * band + in % high;
-    tj = in / high;
-}
-__device__ __forceinline__ void half_tile_of(int32_t local, int32_t down, int32_t& ti, int32_t& tj) {
-    int32_t band = static_cast<int32_t>((sqrtf(8.f * local + 1.f) - 1.f) * 0.0625f);
-    while (4 * band * (8 * band + 1) > local) --band;
-    while (4 * (band + 1) * (8 * band + 9) <= local) ++band;
-    int32_t in = local - 4 * band * (8 * band + 1);
-    const int32_t high = min(8, down - 8 * band);
-    if (in < 8 * band * high) {
-        ti = 8 * band + in % high;
-        tj = in / high;
-        return;
-    }
-    in -= 8 * band * high;
-    ti = 0;
-    while (in > ti) in -= ++ti;
-    ti += 8 * band;
-    tj = 8 * band + in;
-}
-
 // C = L R^T of rows of K values, a tile a workgroup.
 template <typename S, int TERMS, int MODE>
-__global__ void __launch_bounds__(S::THREADS, 2) k_muon_product(List list, Product k, char* ws) {
+__global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(List list, Product k, char* ws) {
     constexpr bool HALF = MODE == kGram || MODE == kSquare;
-    constexpr int N = 4 * S::GJ, PART = (S::TI + S::TJ) * kDepth, ROWS = S::FI, GROUPS = S::FJ / S::GJ;
-    constexpr int STEP = kDepth / TERMS;     // values of K a stage
+    constexpr int N = 4 * S::GJ, PART = (S::TI + S::TJ) * S::DEPTH, Q = S::DEPTH / 32;
+    static_assert(TERMS == 1 || Q == 2, "a row in LDS has both terms");
     __shared__ __align__(1024) _Float16 lds[S::STAGES * PART];
-    const Place at = (HALF ? list.halves : list.fulls)[place_of_block()];
-    const Matrix t = list.matrices[at.matrix];
-    const Work<TERMS> w(ws, t);
-    int32_t ti, tj;
-    if (HALF) half_tile_of(at.local, t.np / S::TI, ti, tj);
-    else tile_of(at.local, t.np / S::TI, t.mp / S::TJ, ti, tj);
-    const int32_t depth = MODE == kGram ? t.mp : t.np, all = depth / STEP;
-    const int64_t stride = depth;
-    const auto left = [&](int low) { return (MODE == kGram ? w.x(low) : MODE == kSquare ? w.a(low) : w.b(low)) + ti * S::TI * stride; };
-    const auto right = [&](int low) { return (MODE == kGram ? w.x(low) : MODE == kSquare ? w.a(low) : w.xt(k.turn, low)) + tj * S::TJ * stride; };
-    const _Float16* const l_at[2] = {left(0), left(TERMS - 1)};
-    const _Float16* const r_at[2] = {right(0), right(TERMS - 1)};
+    const Tile t = (HALF ? list.halves : list.fulls)[place_of_block()];
+    const Work<TERMS> w(ws, t.at, t.np, t.mp);
+    const int32_t depth = (MODE == kGram ? t.mp : t.np) * TERMS, all = depth / S::DEPTH;
+    const Stage<S, true> l_stage(depth * 2);
+    const Stage<S, false> r_stage(depth * 2);
+    const char* const left = reinterpret_cast<const char*>((MODE == kGram ? w.x() : MODE == kSquare ? w.a() : w.b()) +
+                                                           static_cast<int64_t>(t.ti) * S::TI * depth);
+    const char* const right = reinterpret_cast<const char*>((MODE == kGram ? w.x() : MODE == kSquare ? w.a() : w.xt(k.turn)) +
+                                                            static_cast<int64_t>(t.tj) * S::TJ * depth);
     const auto load = [&](int32_t i, int turn) {
-        _Float16* const to = lds + turn * PART;
-        stage<S, TERMS, true>(l_at[0] + i * STEP, l_at[1] + i * STEP, stride, to);
-        stage<S, TERMS, false>(r_at[0] + i * STEP, r_at[1] + i * STEP, stride, to + S::TI * kDepth);
+        l_stage.load(left + i * (S::DEPTH * 2), lds + turn * PART);
+        r_stage.load(right + i * (S::DEPTH * 2), lds + turn * PART + S::TI * S::DEPTH);
     };
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / S::WJ, wj = wave % S::WJ;
     Float4 acc[S::FI][S::FJ] = {};
     const auto multiply = [&](int turn) {
-        const _Float16* const l = lds + turn * PART + (wi * S::FI * 16 + (lane & 15)) * kDepth;
-        const _Float16* const r = lds + turn * PART + (S::TI + wj * S::FJ * 16 + (lane & 15)) * kDepth;
-        Half8 lv[TERMS][S::FI], rv[TERMS][S::FJ];
-        const auto read = [&](int q, Half8(&lq)[S::FI], Half8(&rq)[S::FJ]) {
-            const int pack = (((lane >> 4) + 4 * q) ^ ((lane & 15) >> 1)) * 8;
+        const _Float16* const l = lds + turn * PART + (wi * S::FI * 16 + (lane & 15)) * S::DEPTH;
+        const _Float16* const r = lds + turn * PART + (S::TI + wj * S::FJ * 16 + (lane & 15)) * S::DEPTH;
+        Half8 lv[Q][S::FI], rv[Q][S::FJ];
 #pragma unroll
-            for (int f = 0; f < S::FI; ++f) lq[f] = *reinterpret_cast<const Half8*>(l + f * 16 * kDepth + pack);
+        for (int q = 0; q < Q; ++q) {
+            const int pack = (((lane >> 4) + 4 * q) ^ S::order(lane & 15)) * 8;
 #pragma unroll
-            for (int f = 0; f < S::FJ; ++f) rq[f] = *reinterpret_cast<const Half8*>(r + f * 16 * kDepth + pack);
-        };
-        const auto add = [&](const Half8(&lq)[S::FI], const Half8(&rq)[S::FJ]) {
+            for (int f = 0; f < S::FI; ++f) lv[q][f] = *reinterpret_cast<const Half8*>(l + f * 16 * S::DEPTH + pack);
+#pragma unroll
+            for (int f = 0; f < S::FJ; ++f) rv[q][f] = *reinterpret_cast<const Half8*>(r + f * 16 * S::DEPTH + pack);
+        }
+        const auto add = [&](int ql, int qr) {
 #pragma unroll
             for (int fi = 0; fi < S::FI; ++fi)
 #pragma unroll
-                for (int fj = 0; fj < S::FJ; ++fj) acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rq[fj], lq[fi], acc[fi][fj], 0, 0, 0);
+                for (int fj = 0; fj < S::FJ; ++fj)
+                    acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rv[qr][fj], lv[ql][fi], acc[fi][fj], 0, 0, 0);
         };
-        if constexpr (TERMS == 2) {
-            read(0, lv[0], rv[0]);
-            read(1, lv[1], rv[1]);
-            add(lv[0], rv[0]);
-            add(lv[0], rv[1]);
-            add(lv[1], rv[0]);
-        } else {
-            read(0, lv[0], rv[0]);
-            add(lv[0], rv[0]);
-            read(1, lv[0], rv[0]);
-            add(lv[0], rv[0]);
+        add(0, 0);
+        if (TERMS == 2) {
+            add(0, Q - 1);
+            add(Q - 1, 0);
+        } else if (Q == 2) {
+            add(Q - 1, Q - 1);
         }
     };
     int turn = 0, next = S::STAGES - 1;
@@ -425,97 +500,281 @@ __global__ void __launch_bounds__(S::THREADS, 2) k_muon_product(List list, Produ
         turn = turn + 1 == S::STAGES ? 0 : turn + 1;
     }
     arrived<0>();
-    // What the last part of the output needs of A0 or X is on its way while the last products are taken.
-    const int32_t row0 = ti * S::TI + wi * S::FI * 16 + (lane & 15) * S::GI, col0 = tj * S::TJ + wj * S::FJ * 16 + (lane >> 4) * N;
-    const int64_t wide = HALF ? t.np : t.mp;             // of an output row
-    const auto row_of = [&](int fi) { return row0 + fi / S::GI * 16 * S::GI + fi % S::GI; };
+    // What the last part of the output needs of A0 or X is on its way while the last products are taken (of a tile of 256 half of it, which
+    // is what the registers have room for).
     constexpr bool READS = MODE != kGram, LOW = READS && (TERMS == 2 || !HALF);
-    Half8 hi[READS ? ROWS : 1][GROUPS][N / 8 ? N / 8 : 1], lo[LOW ? ROWS : 1][GROUPS][N / 8 ? N / 8 : 1];
-    if constexpr (READS) {
-#pragma unroll
-        for (int fi = 0; fi < ROWS; ++fi)
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                const int64_t from = row_of(fi) * wide + col0 + g * 4 * N;
-                load_halves((HALF ? w.a(0) : w.x(0)) + from, hi[fi][g]);
-                if constexpr (LOW) load_halves((HALF ? w.a(1) : w.x(1)) + from, lo[fi][g]);
-            }
-    }
-    multiply(turn);
-
-    Update u = {k.lr, k.decay, k.optimizer != 0};
-    if constexpr (MODE == kFinish) {
-        if (skipped(k.grad_scale)) return;
-        if (k.lr_now) {
-            u.lr = static_cast<float>(*k.lr_now);
-            u.keep = static_cast<float>(1. - *k.lr_now * k.lr_decay);
-        }
-        const float ratio = static_cast<float>(t.rows) / static_cast<float>(t.cols);
-        u.lr *= k.scale_rule == CS_MUON_SCALE_SHAPE ? sqrtf(fmaxf(1.f, ratio))
-                : k.scale_rule == CS_MUON_SCALE_RMS ? 0.2f * sqrtf(static_cast<float>(max(t.rows, t.cols))) : 1.f;
-    }
-    const bool tall = t.rows > t.cols;
-#pragma unroll
-    for (int g = 0; g < GROUPS; ++g) {
-        const int32_t col = col0 + g * 4 * N;
-        float dj[N];
-        if constexpr (MODE == kSquare) {
-#pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                const Float4 d = *reinterpret_cast<const Float4*>(w.da() + col + e);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) dj[e + x] = d[x];
-            }
-        }
-#pragma unroll
-        for (int gi = 0; gi < S::FI; gi += S::GI) {
-            float out[S::GI][N];
+    const int32_t row0 = t.ti * S::TI + wi * S::FI * 16 + (lane & 15) * S::GI, col = t.tj * S::TJ + wj * S::FJ * 16 + (lane >> 4) * N;
+    const int32_t wide = HALF ? t.np : t.mp;             // of an output row
+    const auto row_of = [&](int fi) { return row0 + fi / S::GI * 16 * S::GI + fi % S::GI; };
+    Half8 hi[S::GI][N / 8], lo[S::GI][N / 8];
+    const auto fetch = [&](int gi) {
+        if constexpr (READS) {
 #pragma unroll
             for (int f = 0; f < S::GI; ++f) {
-                const int fi = gi + f;
-                const int32_t row = row_of(fi);
-                const float d = MODE == kSquare ? w.da()[row] : MODE == kGram ? 0.f : k.a + w.db()[row];
-                float diagonal = 0.f;
+                const _Float16* const from = (HALF ? w.a() : w.x()) + Work<TERMS>::place(row_of(gi + f), col, wide);
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float c = acc[fi][g * S::GJ + e / 4][e % 4] * (kDown * kDown);
-                    float x = 0.f;
-                    if constexpr (READS) {
-                        x = static_cast<float>(hi[fi][g][e / 8][e % 8]);
-                        if constexpr (LOW) x += static_cast<float>(lo[fi][g][e / 8][e % 8]);
-                        x *= kDown;
-                    }
-                    out[f][e] = MODE == kGram ? c : MODE == kSquare ? fmaf(k.b, x, k.c * fmaf(d + dj[e], x, c)) : fmaf(d, x, c);
-                    if (HALF && row == col + e) {
-                        diagonal = MODE == kGram ? c : fmaf(k.b, d, k.c * fmaf(d, d, c));
-                        out[f][e] = 0.f;
-                    }
-                }
-                if (HALF && row >= col && row < col + N) (MODE == kGram ? w.da() : w.db())[row] = diagonal;
-                if constexpr (MODE == kFinish) {
-                    if (!tall) update(t, k.p_fmt, u, row, col, out[f]);
-                } else {
-                    const int64_t to = row * wide + col;
-                    const auto place = [&](int low) { return (MODE == kGram ? w.a(low) : MODE == kSquare ? w.b(low) : w.x(low)) + to; };
-                    store_halves(place(0), TERMS == 2 || MODE == kApply ? place(1) : nullptr, out[f]);
+                for (int e = 0; e < N / 8; ++e) {
+                    hi[f][e] = *reinterpret_cast<const Half8*>(from + 8 * e);
+                    if constexpr (LOW) lo[f][e] = *reinterpret_cast<const Half8*>(from + w.to_low() + 8 * e);
                 }
             }
-            // the transpose: of A and B the tile on the other side, of X the one that the next product reads
-            if (HALF ? ti == tj : MODE == kFinish && !tall) continue;
+        }
+    };
+    fetch(0);
+    multiply(turn);
+
+    Update u = {};
+    Matrix matrix;
+    if constexpr (MODE == kFinish) {
+        if (skipped(k.last.grad_scale)) return;
+        matrix = list.matrices[t.matrix];
+        u = update_of(k.last, matrix);
+    }
+    const bool tall = MODE == kFinish && matrix.rows > matrix.cols;
+    float dj[N];
+    if constexpr (MODE == kSquare) {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const Float4 d = *reinterpret_cast<const Float4*>(w.da() + col + e);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) dj[e + x] = d[x];
+        }
+    }
+    // (all in the unit of what is stored: 2^10 times; the products are 2^20 times)
+#pragma unroll
+    for (int gi = 0; gi < S::FI; gi += S::GI) {
+        if (gi) fetch(gi);
+        float out[MODE == kFinish ? S::GI : 1][N];
+#pragma unroll
+        for (int f = 0; f < S::GI; ++f) {
+            const int fi = gi + f;
+            const int32_t row = row_of(fi);
+            const float d = MODE == kSquare ? fmaf(k.c, w.da()[row], k.b) : MODE == kGram ? 0.f : k.a + w.db()[row];
+            float diagonal = 0.f;
+            float(&v)[N] = out[MODE == kFinish ? f : 0];
 #pragma unroll
             for (int e = 0; e < N; ++e) {
+                const float c = acc[fi][e / 4][e % 4];
+                float x = 0.f;
+                if constexpr (READS) x = static_cast<float>(hi[f][e / 8][e % 8]);
+                if constexpr (LOW) x += static_cast<float>(lo[f][e / 8][e % 8]);
+                if (MODE == kGram) v[e] = c * kDown;
+                else if (MODE == kSquare) v[e] = fmaf(fmaf(k.c, dj[e], d), x, c * (k.c * kDown));
+                else v[e] = fmaf(d, x, c * kDown);
+                if (HALF && row == col + e) {
+                    diagonal = MODE == kGram ? c * (kDown * kDown) : fmaf(d, dj[e], c * (k.c * kDown * kDown));
+                    v[e] = 0.f;
+                }
+            }
+            if (HALF && row >= col && row < col + N) (MODE == kGram ? w.da() : w.db())[row] = diagonal;
+            if constexpr (MODE == kFinish) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[e] *= kDown;
+                if (!tall) update(matrix, k.last.p_fmt, u, row, col, v);
+            } else {
+                _Float16* const to = (MODE == kGram ? w.a() : MODE == kSquare ? w.b() : w.x()) + Work<TERMS>::place(row, col, wide);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    hi[f][e / 8][e % 8] = static_cast<_Float16>(v[e]);
+                    lo[f][e / 8][e % 8] = static_cast<_Float16>(v[e] - static_cast<float>(hi[f][e / 8][e % 8]));
+                }
+#pragma unroll
+                for (int e = 0; e < N / 8; ++e) {
+                    *reinterpret_cast<Half8*>(to + 8 * e) = hi[f][e];
+                    if (TERMS == 2 || MODE == kApply) *reinterpret_cast<Half8*>(to + w.to_low() + 8 * e) = lo[f][e];
+                }
+            }
+        }
+        // the transpose: of A and B the tile on the other side, of X the one that the next product reads
+        if (HALF ? t.ti == t.tj : MODE == kFinish && !tall) continue;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if constexpr (MODE == kFinish) {
                 float turned[S::GI];
 #pragma unroll
                 for (int f = 0; f < S::GI; ++f) turned[f] = out[f][e];
-                if constexpr (MODE == kFinish) {
-                    update(t, k.p_fmt, u, col + e, row_of(gi), turned);
+                update(matrix, k.last.p_fmt, u, col + e, row_of(gi), turned);
+            } else {
+                typedef _Float16 Halves __attribute__((ext_vector_type(S::GI)));
+                Halves h, l;
+#pragma unroll
+                for (int f = 0; f < S::GI; ++f) h[f] = hi[f][e / 8][e % 8], l[f] = lo[f][e / 8][e % 8];
+                _Float16* const to = (MODE == kGram ? w.a() : MODE == kSquare ? w.b() : w.xt(1 - k.turn)) +
+                                     Work<TERMS>::place(col + e, row_of(gi), t.np);
+                *reinterpret_cast<Halves*>(to) = h;
+                if (TERMS == 2) *reinterpret_cast<Halves*>(to + 32) = l;
+            }
+        }
+    }
+}
+
+// A small matrix (n <= 64, m <= M) a workgroup, in one launch: X in binary32 in registers, what the products read in LDS.
+template <int M, int TERMS>
+struct Little {
+    static constexpr int N = 64, FJ = M / 32, WIDE = M + 8, HIGH = N + 8;        // (rows 16 bytes further: 16 of them meet all banks)
+    static constexpr int X = N * WIDE, XT = M * HIGH, A = N * HIGH;
+    static constexpr int HALVES = TERMS * (X + XT + 2 * A) + 2 * 2 * N;
+};
+template <int M, int TERMS>
+__global__ void __launch_bounds__(kThreads, 1) k_muon_little(List list, Moment moment, double eps, Steps steps, Last last) {
+    using L = Little<M, TERMS>;
+    constexpr int FJ = L::FJ, W = 4 * FJ;    // a lane has 2 rows of W neighbouring columns of X, and of 8 of A
+    __shared__ __align__(16) _Float16 lds[L::HALVES];
+    __shared__ double buf[kThreads / 64];
+    _Float16 *const x_at = lds, *const xt_at = x_at + TERMS * L::X, *const a_at = xt_at + TERMS * L::XT, *const b_at = a_at + TERMS * L::A;
+    float *const da = reinterpret_cast<float*>(b_at + TERMS * L::A), *const db = da + L::N;
+    if (skipped(last.grad_scale)) return;
+    const Matrix t = list.matrices[blockIdx.x];
+    const bool tall = t.rows > t.cols;
+    const float s = moment.grad_scale ? *moment.grad_scale : 1.f;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
+    const int row = wi * 32 + (lane & 15) * 2, col = wj * (M / 2) + (lane >> 4) * W, a_col = wj * 32 + (lane >> 4) * 8;
+    float x[2][W];
+    double sum = 0.;
+    if (tall) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            float u[2];
+            direction<true>(t, moment, s, col + e, row, u);
+            x[0][e] = u[0], x[1][e] = u[1];
+        }
+    } else {
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < W; e += 4) {
+                float u[4];
+                direction<true>(t, moment, s, row + f, col + e, u);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[f][e + i] = u[i];
+            }
+    }
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int e = 0; e < W; ++e) sum = fma(static_cast<double>(x[f][e]), static_cast<double>(x[f][e]), sum);
+    const double one = inverse_of(workgroup_sum(sum, buf), eps) * static_cast<double>(kUp);
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int e = 0; e < W; ++e) x[f][e] = static_cast<float>(x[f][e] * one);
+
+    // rows row, row + 1 of C columns from c on into an array of rows `step` apart, and into its transpose
+    const auto keep = [&](auto& v, _Float16* at, int step, int size, int c, _Float16* turned, int high, int turned_size) {
+        constexpr int C = sizeof(v[0]) / 4;
+        Half8 h[TERMS][2][C / 8];
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+                _Float16 hi, lo;
+                split(v[f][e], hi, lo);
+                h[0][f][e / 8][e % 8] = hi;
+                if (TERMS == 2) h[TERMS - 1][f][e / 8][e % 8] = lo;
+            }
+#pragma unroll
+        for (int low = 0; low < TERMS; ++low) {
+#pragma unroll
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+                for (int e = 0; e < C / 8; ++e) *reinterpret_cast<Half8*>(at + low * size + (row + f) * step + c + 8 * e) = h[low][f][e];
+            if (!turned) continue;
+#pragma unroll
+            for (int e = 0; e < C; ++e) {
+                typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
+                *reinterpret_cast<Half2*>(turned + low * turned_size + (c + e) * high + row) = Half2{h[low][0][e / 8][e % 8], h[low][1][e / 8][e % 8]};
+            }
+        }
+    };
+    // acc = L R^T: this wavefront's 32 rows of L and 16 F rows of R, K values
+    const auto product = [&](auto& acc, const _Float16* l, int l_step, int l_size, const _Float16* r, int r_step, int r_size, int depth) {
+        constexpr int F = sizeof(acc[0]) / sizeof(Float4);
+        const int in = lane & 15;
+        l += (wi * 32 + in * 2) * l_step + (lane >> 4) * 8;
+        r += (wj * 16 * F + in / 4 * 4 * F + in % 4) * r_step + (lane >> 4) * 8;
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int g = 0; g < F; ++g) acc[f][g] = Float4{};
+#pragma unroll
+        for (int q = 0; q < depth; q += 32) {
+            Half8 lv[TERMS][2], rv[TERMS][F];
+#pragma unroll
+            for (int low = 0; low < TERMS; ++low) {
+#pragma unroll
+                for (int f = 0; f < 2; ++f) lv[low][f] = *reinterpret_cast<const Half8*>(l + low * l_size + f * l_step + q);
+#pragma unroll
+                for (int g = 0; g < F; ++g) rv[low][g] = *reinterpret_cast<const Half8*>(r + low * r_size + 4 * g * r_step + q);
+            }
+#pragma unroll
+            for (int part = 0; part < (TERMS == 2 ? 3 : 1); ++part)
+#pragma unroll
+                for (int f = 0; f < 2; ++f)
+#pragma unroll
+                    for (int g = 0; g < F; ++g)
+                        acc[f][g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rv[part == 1 ? TERMS - 1 : 0][g], lv[part == 2 ? TERMS - 1 : 0][f], acc[f][g], 0, 0, 0);
+        }
+    };
+    for (int i = 0; i < steps.count; ++i) {
+        const float a = steps.coefs[i][0], b = steps.coefs[i][1], c = steps.coefs[i][2];
+        keep(x, x_at, L::WIDE, L::X, col, xt_at, L::HIGH, L::XT);
+        __syncthreads();
+        Float4 acc[2][2];
+        product(acc, x_at, L::WIDE, L::X, x_at, L::WIDE, L::X, M);
+        float v[2][8];
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[f][e] = acc[f][e / 4][e % 4] * kDown;
+                if (row + f == a_col + e) {
+                    da[row + f] = v[f][e] * kDown;
+                    v[f][e] = 0.f;
+                }
+            }
+        keep(v, a_at, L::HIGH, L::A, a_col, static_cast<_Float16*>(nullptr), 0, 0);
+        __syncthreads();
+        product(acc, a_at, L::HIGH, L::A, a_at, L::HIGH, L::A, L::N);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const float d = fmaf(c, da[row + f], b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float dj = da[a_col + e], p = acc[f][e / 4][e % 4];
+                if (row + f == a_col + e) {
+                    db[row + f] = fmaf(d, dj, p * (c * kDown * kDown));
+                    v[f][e] = 0.f;
                 } else {
-                    const int64_t to = static_cast<int64_t>(col + e) * t.np + row_of(gi);
-                    const auto place = [&](int low) { return (MODE == kGram ? w.a(low) : MODE == kSquare ? w.b(low) : w.xt(1 - k.turn, low)) + to; };
-                    store_halves(place(0), TERMS == 2 ? place(1) : nullptr, turned);
+                    v[f][e] = fmaf(fmaf(c, dj, d), v[f][e], p * (c * kDown));
                 }
             }
         }
+        keep(v, b_at, L::HIGH, L::A, a_col, static_cast<_Float16*>(nullptr), 0, 0);
+        __syncthreads();
+        Float4 more[2][FJ];
+        product(more, b_at, L::HIGH, L::A, xt_at, L::HIGH, L::XT, L::N);
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const float d = a + db[row + f];
+#pragma unroll
+            for (int e = 0; e < W; ++e) x[f][e] = fmaf(d, x[f][e], more[f][e / 4][e % 4] * kDown);
+        }
+        __syncthreads();
+    }
+    const Update u = update_of(last, t);
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int e = 0; e < W; ++e) x[f][e] *= kDown;
+    if (tall) {
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            const float pair[2] = {x[0][e], x[1][e]};
+            update(t, last.p_fmt, u, col + e, row, pair);
+        }
+    } else {
+#pragma unroll
+        for (int f = 0; f < 2; ++f) update(t, last.p_fmt, u, row + f, col, x[f]);
     }
 }
 
@@ -525,8 +784,9 @@ __global__ void __launch_bounds__(S::THREADS, 2) k_muon_product(List list, Produ
 constexpr int64_t kMaxSide = 1 << 20, kMaxShort = 1 << 15, kMaxMatrices = 1 << 20, kMaxPlaces = static_cast<int64_t>(1) << 24;
 
 struct Plan {
-    int64_t matrices, pieces, halves, fulls, work;   // work: bytes of all matrices
-    int tile;
+    int64_t matrices, littles, pieces, halves, fulls, work;      // work: bytes of all matrices
+    double half_steps, full_steps;                               // parts of 64 values of K, of all tiles together
+    int half_tile, full_tile;
 };
 int64_t up_to(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
 
@@ -534,46 +794,83 @@ bool stack_ok(const cs_matrix& s) {
     return s.count >= 0 && s.count <= kMaxMatrices && s.rows >= 0 && s.cols >= 0 && s.rows <= kMaxSide && s.cols <= kMaxSide &&
            (s.rows < s.cols ? s.rows : s.cols) <= kMaxShort;
 }
-// count of matrices that are there, and sizes; `each` is told of every stack
+bool there(const cs_matrix& s) { return s.count > 0 && s.rows > 0 && s.cols > 0; }
+// Matrices that a workgroup takes from their moments to their parameters (64 x 64 in 32 bits 14 us, by the other launches 70).
+bool little(const cs_matrix& s) { return (s.rows <= 64 || s.cols <= 64) && s.rows <= 128 && s.cols <= 128; }
+
+// Counts and sizes with these tiles; `each` is told of every stack that has tiles.
 template <typename F>
-bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int tile, Plan& plan, F each) {
-    plan = Plan{0, 0, 0, 0, 0, tile};
+bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int full_tile, Plan& plan, F each) {
+    plan = Plan{};
+    plan.half_tile = half_tile, plan.full_tile = full_tile;
+    const int64_t tile = half_tile > full_tile ? half_tile : full_tile;
     for (int32_t i = 0; i < n; ++i) {
         const cs_matrix& s = stacks[i];
         if (!stack_ok(s)) return false;
-        if (s.count == 0 || s.rows == 0 || s.cols == 0) continue;
-        const int64_t np = up_to(s.rows < s.cols ? s.rows : s.cols, tile), mp = up_to(s.rows < s.cols ? s.cols : s.rows, tile);
-        const int64_t down = np / tile, pieces = (np / kEdge) * (mp / kEdge), halves = down * (down + 1) / 2, fulls = down * (mp / tile);
-        each(s, np, mp, plan, pieces, halves, fulls);
+        if (!there(s)) continue;
         plan.matrices += s.count;
+        if (plan.matrices > kMaxMatrices) return false;
+        if (little(s)) {
+            plan.littles += s.count;
+            continue;
+        }
+        const int64_t np = up_to(s.rows < s.cols ? s.rows : s.cols, tile), mp = up_to(s.rows < s.cols ? s.cols : s.rows, tile);
+        const int64_t down = np / half_tile, pieces = (np / kEdge) * (mp / kEdge), halves = down * (down + 1) / 2;
+        const int64_t fulls = (np / full_tile) * (mp / full_tile);
+        each(s, np, mp, plan, pieces, halves, fulls);
         plan.pieces += s.count * pieces;
         plan.halves += s.count * halves;
         plan.fulls += s.count * fulls;
+        plan.half_steps += static_cast<double>(s.count * halves) * (np + mp) / 64;
+        plan.full_steps += static_cast<double>(s.count * fulls) * np / 64;
         plan.work += s.count * work_bytes(np, mp, terms);
-        if (plan.matrices > kMaxMatrices || plan.pieces >= kMaxPlaces) return false;
+        if (plan.pieces >= kMaxPlaces) return false;
     }
     return true;
 }
+// How long tiles take that are spread over 256 CUs, in parts of 64 values of K of one tile (us; of 64 three are on a CU at a time, of 128 two,
+// of 256 one, and fewer take less each).  4096 x 4096, one term, X by tiles of 64 / 128 / 256: 207 / 148 / 134 us; 48 x 512 x 512
+// 34 / 32 / 39, their A 17 / 15 / 23; 12 matrices of 2048 x 512, A 15 / 23 / 53, X 35 / 32 / 38; 8 of 1024 x 4096, X 170 / 135 / 125.
+double rounds(int64_t tiles, int tile) {
+    const int64_t at_once = tile == 64 ? 768 : tile == 128 ? 512 : 256, left = tiles % at_once;
+    const double full = tile == 64 ? 0.6 : tile == 128 ? 1.15 : 2.1;
+    const double rest = left == 0 ? 0. : left > at_once - 256 ? full : tile == 128 ? 0.6 : left > 256 ? 0.45 : 0.3;
+    return static_cast<double>(tiles / at_once) * full + rest;
+}
 bool plan_of(const cs_matrix* stacks, int32_t n, int terms, Plan& plan) {
     const auto none = [](const cs_matrix&, int64_t, int64_t, const Plan&, int64_t, int64_t, int64_t) {};
-    if (!plan_with(stacks, n, terms, 128, plan, none)) return false;
-    if (plan.halves >= 256) return true;
-    return plan_with(stacks, n, terms, 64, plan, none);
+    double least = INFINITY;
+    bool ok = false;
+    for (const int half_tile : {64, 128})
+        for (const int full_tile : {64, 128, 256}) {
+            Plan p;
+            // (larger tiles fill up more: they may be too many where smaller ones are not)
+            if (!plan_with(stacks, n, terms, half_tile, full_tile, p, none)) continue;
+            const double us = p.halves ? rounds(p.halves, half_tile) * p.half_steps / static_cast<double>(p.halves) +
+                                             rounds(p.fulls, full_tile) * p.full_steps / static_cast<double>(p.fulls) : 0.;
+            if (us < least) {
+                least = us;
+                plan = p;
+                ok = true;
+            }
+        }
+    return ok;
 }
 size_t list_bytes(const Plan& p) {
-    return static_cast<size_t>(p.matrices) * sizeof(Matrix) + static_cast<size_t>(p.pieces + p.halves + p.fulls) * sizeof(Place);
+    return static_cast<size_t>(p.matrices) * sizeof(Matrix) + static_cast<size_t>(p.halves + p.fulls) * sizeof(Tile) +
+           static_cast<size_t>(p.pieces) * sizeof(Place);
 }
-size_t workspace_bytes(const cs_matrix_list* l) {
-    return static_cast<size_t>(l->work) + static_cast<size_t>(l->pieces + l->matrices) * sizeof(double);
-}
+size_t workspace_bytes(const cs_matrix_list* l) { return static_cast<size_t>(l->work) + static_cast<size_t>(l->pieces) * sizeof(double); }
 List list_of(const cs_matrix_list* l) {
     const Matrix* t = static_cast<const Matrix*>(l->memory);
-    const Place* at = reinterpret_cast<const Place*>(t + l->matrices);
-    return List{t, at, at + l->pieces, at + l->pieces + l->halves};
+    const Tile* at = reinterpret_cast<const Tile*>(t + l->matrices);
+    return List{t, at, at + l->halves, reinterpret_cast<const Place*>(at + l->halves + l->fulls)};
 }
+bool tile_ok(int32_t tile) { return tile == 64 || tile == 128 || tile == 256; }
 bool list_ok(const cs_matrix_list* l) {
-    return l && l->matrices >= 0 && l->pieces >= 0 && l->halves >= 0 && l->fulls >= 0 && l->work >= 0 && (l->tile == 64 || l->tile == 128) &&
-           (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) && fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
+    return l && l->littles >= 0 && l->matrices >= l->littles && l->pieces >= 0 && l->halves >= 0 && l->fulls >= 0 && l->work >= 0 &&
+           (l->half_tile == 64 || l->half_tile == 128) && tile_ok(l->full_tile) && (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) &&
+           fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
 }
 
 // The steps keep singular values of at most 1 below 2, and B within binary16.
@@ -602,36 +899,70 @@ bool hyper_ok(const cs_muon* h) {
            h->scale <= CS_MUON_SCALE_ONE && steps_ok(h);
 }
 
-using Large = Shape<2, 2, 4, 4, 2>;
-using Small = Shape<2, 2, 2, 2, 4>;
+// A tile's wavefronts by its edge: with four on a SIMD (three of 64) one takes products while another waits; tiles of 128 of two terms have
+// fewer reads of LDS the other way round.
+template <int TILE, int TERMS>
+struct ShapeOf;
+template <int TERMS>
+struct ShapeOf<64, TERMS> : Shape<2, 2, 2, 2, 3, 64, 3> {};
+template <>
+struct ShapeOf<128, 1> : Shape<4, 2, 2, 4, 2, 64, 4> {};
+template <>
+struct ShapeOf<128, 2> : Shape<2, 4, 4, 2, 2, 64, 4> {};
+template <int TERMS>
+struct ShapeOf<256, TERMS> : Shape<2, 4, 8, 4, 2, 64, 2> {};
 
-template <typename S, int TERMS>
+template <int TERMS, int MODE, int TILE>
+int product_as(const cs_matrix_list* l, const Product& k, char* ws, hipStream_t s) {
+    const int64_t places = MODE == kGram || MODE == kSquare ? l->halves : l->fulls;
+    using S = ShapeOf<TILE, TERMS>;
+    k_muon_product<S, TERMS, MODE><<<static_cast<unsigned>(places), S::THREADS, 0, s>>>(list_of(l), k, ws);
+    return launched();
+}
+template <int TERMS, int MODE>
+int product(const cs_matrix_list* l, const Product& k, char* ws, hipStream_t s) {
+    const int tile = MODE == kGram || MODE == kSquare ? l->half_tile : l->full_tile;
+    if (tile == 64) return product_as<TERMS, MODE, 64>(l, k, ws, s);
+    if constexpr (MODE == kApply || MODE == kFinish)
+        if (tile == 256) return product_as<TERMS, MODE, 256>(l, k, ws, s);
+    return product_as<TERMS, MODE, 128>(l, k, ws, s);
+}
+
+// Pieces of a matrix up to which every workgroup that begins X sums their squares by itself, in place of a launch that does (4096 x 4096,
+// 4096 pieces: that launch is 6 us).
+constexpr int64_t kSquaresEach = 1024;
+
+template <int TERMS>
 int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const double* lr, const float* grad_scale, char* ws, hipStream_t s) {
     const List at = list_of(l);
+    const Moment moment = {static_cast<float>(h->momentum), optimizer ? h->nesterov : 0, l->g_fmt, grad_scale};
+    Last last = {l->p_fmt, optimizer, h->scale, static_cast<float>(1. - h->lr * h->weight_decay), static_cast<float>(h->lr),
+                 static_cast<float>(h->weight_decay), lr, grad_scale};
+    Steps steps = {h->steps, {}};
+    for (int i = 0; i < h->steps; ++i)
+        for (int e = 0; e < 3; ++e) steps.coefs[i][e] = static_cast<float>(h->coefs[i][e]);
+    if (l->littles) {
+        const auto kernel = l->little_cols <= 64 ? k_muon_little<64, TERMS> : k_muon_little<128, TERMS>;
+        kernel<<<static_cast<unsigned>(l->littles), kThreads, 0, s>>>(at, moment, h->eps, steps, last);
+        if (int rc = launched()) return rc;
+    }
+    if (l->matrices == l->littles) return CS_OK;
     double* const squares = reinterpret_cast<double*>(ws + l->work);
-    double* const inverse = squares + l->pieces;
-    const Moment moment = {static_cast<float>(h->momentum), optimizer ? h->nesterov : 0, grad_scale};
-    const unsigned pieces = static_cast<unsigned>(l->pieces), halves = static_cast<unsigned>(l->halves), fulls = static_cast<unsigned>(l->fulls);
-    k_muon_moment<<<pieces, kThreads, 0, s>>>(at, l->g_fmt, moment, squares);
-    k_muon_norm<<<static_cast<unsigned>(l->matrices), kThreads, 0, s>>>(at, h->eps, squares, inverse);
-    k_muon_begin<TERMS><<<pieces, kThreads, 0, s>>>(at, l->g_fmt, moment, inverse, ws);
+    const unsigned pieces = static_cast<unsigned>(l->pieces);
+    k_muon_moment<<<pieces, kThreads, 0, s>>>(at, moment, squares);
+    const bool joined = l->pieces > kSquaresEach * (l->matrices - l->littles);
+    if (joined) {
+        List others = at;
+        others.matrices += l->littles;
+        k_muon_norm<<<static_cast<unsigned>(l->matrices - l->littles), kThreads, 0, s>>>(others, squares);
+    }
+    k_muon_begin<TERMS><<<pieces, kThreads, 0, s>>>(at, moment, h->eps, squares, joined, ws);
     if (int rc = launched()) return rc;
     for (int i = 0; i < h->steps; ++i) {
-        Product k = {};
-        k.a = static_cast<float>(h->coefs[i][0]), k.b = static_cast<float>(h->coefs[i][1]), k.c = static_cast<float>(h->coefs[i][2]);
-        k.turn = i & 1;
-        k_muon_product<S, TERMS, kGram><<<halves, S::THREADS, 0, s>>>(at, k, ws);
-        k_muon_product<S, TERMS, kSquare><<<halves, S::THREADS, 0, s>>>(at, k, ws);
-        if (i + 1 < h->steps) {
-            k_muon_product<S, TERMS, kApply><<<fulls, S::THREADS, 0, s>>>(at, k, ws);
-        } else {
-            k.p_fmt = l->p_fmt, k.optimizer = optimizer, k.scale_rule = h->scale;
-            k.lr = static_cast<float>(h->lr), k.decay = static_cast<float>(1. - h->lr * h->weight_decay);
-            k.lr_decay = static_cast<float>(h->weight_decay);
-            k.lr_now = lr, k.grad_scale = grad_scale;
-            k_muon_product<S, TERMS, kFinish><<<fulls, S::THREADS, 0, s>>>(at, k, ws);
-        }
-        if (int rc = launched()) return rc;
+        const Product k = {steps.coefs[i][0], steps.coefs[i][1], steps.coefs[i][2], i & 1, last};
+        if (int rc = product<TERMS, kGram>(l, k, ws, s)) return rc;
+        if (int rc = product<TERMS, kSquare>(l, k, ws, s)) return rc;
+        if (int rc = i + 1 < h->steps ? product<TERMS, kApply>(l, k, ws, s) : product<TERMS, kFinish>(l, k, ws, s)) return rc;
     }
     return CS_OK;
 }
@@ -641,15 +972,15 @@ int run(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const double*
     if (l->matrices == 0) return CS_OK;
     const size_t need = workspace_bytes(l);
     if (ws_bytes < need) return CS_EWORKSPACE;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return CS_EINVAL;
-    const Span written[] = {{workspace, static_cast<int64_t>(need)}};
-    const Span read[] = {{l->memory, static_cast<int64_t>(list_bytes(Plan{l->matrices, l->pieces, l->halves, l->fulls, 0, 0}))}, {lr, 8},
-                         {grad_scale, 4}};
+    if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return CS_EINVAL;
+    Plan plan = {};
+    plan.matrices = l->matrices, plan.pieces = l->pieces, plan.halves = l->halves, plan.fulls = l->fulls;
+    const Span written[] = {{need ? workspace : nullptr, static_cast<int64_t>(need)}};
+    const Span read[] = {{l->memory, static_cast<int64_t>(list_bytes(plan))}, {lr, 8}, {grad_scale, 4}};
     if (!spans_apart(written, read)) return CS_EINVAL;
     char* const ws = static_cast<char*>(workspace);
     const hipStream_t s = stream_of(stream);
-    if (l->tile == 128) return l->terms == 1 ? run_as<Large, 1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<Large, 2>(h, l, optimizer, lr, grad_scale, ws, s);
-    return l->terms == 1 ? run_as<Small, 1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<Small, 2>(h, l, optimizer, lr, grad_scale, ws, s);
+    return l->terms == 1 ? run_as<1>(h, l, optimizer, lr, grad_scale, ws, s) : run_as<2>(h, l, optimizer, lr, grad_scale, ws, s);
 }
 
 }  // namespace
@@ -692,7 +1023,14 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
         if ((!same && spans_meet(s.p, p_bytes, s.g, g_bytes)) || spans_meet(s.m, m_bytes, s.p, p_bytes) || spans_meet(s.m, m_bytes, s.g, g_bytes))
             return CS_EINVAL;
     }
-    *list = cs_matrix_list{memory, plan.matrices, plan.pieces, plan.halves, plan.fulls, plan.work, p_fmt, g_fmt, terms, plan.tile, moments == 1};
+    int64_t little_cols = 0;                 // the longest side of the small ones
+    for (int32_t i = 0; i < count; ++i)
+        if (there(stacks[i]) && little(stacks[i])) {
+            const int64_t side = stacks[i].rows > stacks[i].cols ? stacks[i].rows : stacks[i].cols;
+            if (side > little_cols) little_cols = side;
+        }
+    *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.pieces, plan.halves, plan.fulls, plan.work, p_fmt, g_fmt, terms, moments == 1,
+                           plan.half_tile, plan.full_tile, static_cast<int32_t>(little_cols), 0};
     if (plan.matrices == 0) return CS_OK;
     Matrix* const matrices = static_cast<Matrix*>(memory);
     const hipStream_t st = stream_of(stream);
@@ -706,38 +1044,49 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
         done += filled;
         filled = 0;
     };
+    const auto take = [&](const cs_matrix& s, int64_t k, Matrix more) {
+        Matrix& t = b.t[filled];
+        t = more;
+        t.p = static_cast<char*>(s.p) + k * s.p_step * pb;
+        t.g = static_cast<const char*>(s.g) + k * s.g_step * gb;
+        t.moment = s.m ? s.m + k * s.rows * s.cols : nullptr;
+        t.p_stride = s.p_stride, t.g_stride = s.g_stride;
+        t.rows = static_cast<int32_t>(s.rows), t.cols = static_cast<int32_t>(s.cols);
+        if (++filled == kBatch) flush();
+    };
+    // the small ones first
+    for (int32_t i = 0; i < count; ++i)
+        if (there(stacks[i]) && little(stacks[i]))
+            for (int64_t k = 0; k < stacks[i].count; ++k) take(stacks[i], k, Matrix{});
     Plan again;
-    plan_with(stacks, count, terms, plan.tile, again, [&](const cs_matrix& s, int64_t np, int64_t mp, const Plan& at, int64_t pieces, int64_t halves, int64_t fulls) {
+    plan_with(stacks, count, terms, plan.half_tile, plan.full_tile, again,
+              [&](const cs_matrix& s, int64_t np, int64_t mp, const Plan& at, int64_t pieces, int64_t halves, int64_t fulls) {
         for (int64_t k = 0; k < s.count; ++k) {
-            Matrix& t = b.t[filled];
-            t.p = static_cast<char*>(s.p) + k * s.p_step * pb;
-            t.g = static_cast<const char*>(s.g) + k * s.g_step * gb;
-            t.moment = s.m ? s.m + k * s.rows * s.cols : nullptr;
-            t.p_stride = s.p_stride, t.g_stride = s.g_stride;
+            Matrix t = {};
             t.at = at.work + k * work_bytes(np, mp, terms);
-            t.rows = static_cast<int32_t>(s.rows), t.cols = static_cast<int32_t>(s.cols);
             t.np = static_cast<int32_t>(np), t.mp = static_cast<int32_t>(mp);
             t.first_piece = static_cast<int32_t>(at.pieces + k * pieces), t.pieces = static_cast<int32_t>(pieces);
             t.first_half = static_cast<int32_t>(at.halves + k * halves), t.first_full = static_cast<int32_t>(at.fulls + k * fulls);
-            if (++filled == kBatch) flush();
+            take(s, k, t);
         }
     });
     flush();
     if (rc) return rc;
-    Place* at = reinterpret_cast<Place*>(matrices + plan.matrices);
-    const int64_t places[3] = {plan.pieces, plan.halves, plan.fulls};
-    for (int which = 0; which < 3; ++which) {
-        k_list_places<<<static_cast<unsigned>((places[which] + kThreads - 1) / kThreads), kThreads, 0, st>>>(
-            matrices, static_cast<int>(plan.matrices), which, at, places[which]);
-        if (int e = launched()) return e;
-        at += places[which];
-    }
+    Tile* const halves = reinterpret_cast<Tile*>(matrices + plan.matrices);
+    Tile* const fulls = halves + plan.halves;
+    const auto grid = [](int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); };
+    const int first = static_cast<int>(plan.littles), n = static_cast<int>(plan.matrices);
+    if (first == n) return CS_OK;
+    k_list_places<kHalves><<<grid(plan.halves), kThreads, 0, st>>>(matrices, first, n, plan.half_tile, halves, plan.halves);
+    k_list_places<kFulls><<<grid(plan.fulls), kThreads, 0, st>>>(matrices, first, n, plan.full_tile, fulls, plan.fulls);
+    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, reinterpret_cast<Place*>(fulls + plan.fulls), plan.pieces);
+    if (int e = launched()) return e;
     return CS_OK;
 }
 
 extern "C" int cs_muon_workspace_bytes(const cs_matrix_list* list, size_t* bytes) {
     if (!list_ok(list) || !bytes) return CS_EINVAL;
-    *bytes = list->matrices ? workspace_bytes(list) : 0;
+    *bytes = workspace_bytes(list);
     return CS_OK;
 }
 

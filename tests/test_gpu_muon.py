@@ -77,7 +77,8 @@ def matrices_of(count, rows, cols, dtype=torch.float32, seed=1, steep=False):
     return x.to(dtype)
 
 
-SIZES = [(1, 1, 1), (1, 1, 70), (2, 70, 1), (1, 3, 5), (1, 64, 64), (2, 65, 63), (1, 16, 300), (3, 130, 257), (2, 257, 128), (1, 200, 1000),
+# a workgroup's own (up to 64 x 128), and in tiles of every size
+SIZES = [(1, 1, 1), (1, 1, 70), (2, 70, 1), (1, 3, 5), (1, 64, 64), (2, 65, 63), (3, 30, 64), (2, 64, 128), (2, 127, 50), (1, 65, 65), (1, 64, 129), (1, 16, 300), (3, 130, 257), (2, 257, 128), (1, 200, 1000),
          (1, 512, 512)]
 
 
@@ -104,21 +105,27 @@ def test_as_many_matrices_as_larger_tiles_are_taken_for(terms):
     check_shapes([(60, 300, 520), (1, 5, 7), (2, 1100, 900), (1, 130, 1)], terms)
 
 
-def check_shapes(shapes, terms):
+@pytest.mark.parametrize("terms", [1, 2])
+def test_the_largest_tiles(terms):
+    """as many that tiles of 256 fill the GPU"""
+    check_shapes([(4, 2000, 2030), (30, 8, 60)], terms, every=9)
+
+
+def check_shapes(shapes, terms, every=None):
     xs = [matrices_of(*s, seed=i) for i, s in enumerate(shapes)]
     outs = [torch.full_like(x, float("nan")) for x in xs]
     o = Orthogonalizer(xs, outs, terms=terms)
     o.run()
     for x, out in zip(xs, outs):
-        for i in range(0, len(x), 13 if len(x) > 20 else 5):
+        for i in range(0, len(x), every or (13 if len(x) > 20 else 5)):
             if x[i].numel():
                 want, off = steps_of(x[i], terms)
                 close(out[i], want, off, tuple(x.shape))
     # alone, in other tiles (whose sums of squares are taken in another order: the norm's last bit may differ)
     one = torch.empty_like(xs[0][3])
     Orthogonalizer([xs[0][3]], [one], terms=terms).run()
-    want, off = steps_of(xs[0][3], terms)
-    close(one, want, off)
+    off = steps_of(xs[0][3], terms)[1]
+    close(one, outs[0][3], 2 * off)
 
 
 def test_singular_values_and_vectors():
@@ -302,6 +309,7 @@ def test_refusals():
                 dict(params=[y], grads=[x], lr_now=torch.ones(1, device=DEV)), dict(params=[y], grads=[x], grad_scale=torch.ones(2, device=DEV))):
         with pytest.raises(cs.CsError):
             Muon(**bad).step()
+    x, y = matrices_of(2, 70, 200), torch.zeros(2, 70, 200, device=DEV)
     opt = Muon([y], [x])
     with pytest.raises(cs.CsError, match="workspace"):
         cs.cs_muon_step(opt.h, opt.list, opt.workspace[:100])
