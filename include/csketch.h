@@ -683,7 +683,7 @@ int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, i
                          int64_t d_stride, void* workspace, size_t ws_bytes, void* stream);
 
 /* Loss of pairs of answers.  Answers are packed after one another: answer a has the tokens [begin[a], begin[a + 1]) (device
- * int64[2 pairs + 1], ascending; what leaves [0, tokens] is cut off there); answers 0 .. pairs - 1 are the chosen ones, the next `pairs` the rejected
+ * int64[2 pairs + 1], ascending, or results are undefined; what leaves [0, tokens] is cut off there); answers 0 .. pairs - 1 are the chosen ones, the next `pairs` the rejected
  * ones, in the same order.  With R = beta times the sum of l - l1 over an answer's tokens that count (mean: by their number; of no
  * token: 0) and z = R_chosen - R_rejected - margin, a pair's loss is
  *     CS_PREFERENCE_LOGISTIC  (1 - smoothing) ln(1 + exp(-z)) + smoothing ln(1 + exp(z))
@@ -693,7 +693,7 @@ int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, i
  * weight_or_null (1): float[pairs], a pair of weight 0 has no gradient.  loss: float[pairs], without the weight; reward: float[2 pairs], R.
  * g_logp: float[tokens] or NULL, the gradient of the sum of weight times loss: 0 for tokens that are left out; tokens of no answer are left as
  * they were.  sums: float[3], of weight loss, of the weight of pairs with R_chosen > R_rejected, of weight (R_chosen - R_rejected); sums are
- * binary64 in a fixed order, rounded once.  pairs < 2^22.  workspace: device, 8-byte aligned. */
+ * binary64 in a fixed order, rounded once.  tokens <= 2^34, pairs < 2^22.  workspace: device, 8-byte aligned. */
 #define CS_PREFERENCE_LOGISTIC 0
 #define CS_PREFERENCE_HINGE 1
 #define CS_PREFERENCE_SQUARE 2

@@ -1236,6 +1236,23 @@ def cs_policy_loss(h: CsPolicy, logp, entropy, old_logp, ref_logp, advantage, we
     """all [rows] float32 but sums [4]; entropy may be None where h.entropy is 0, ref_logp where h.kl is 0, an output where it is not
     wanted"""
     f32 = torch.float32
+    try:
+        n, gpu = logp.numel(), logp.get_device()
+        given = [t for t in (logp, entropy, old_logp, ref_logp, advantage, weight, loss, g_logp, g_entropy) if t is not None]
+        if (gpu >= 0 and old_logp is not None and advantage is not None and weight is not None
+                and all([t.dtype is f32 and t.numel() == n and t.get_device() == gpu and t.is_contiguous() for t in given])
+                and (sums is None or sums.dtype is f32 and sums.numel() == 4 and sums.get_device() == gpu and sums.is_contiguous())
+                and workspace.dtype is torch.uint8 and workspace.get_device() == gpu and workspace.is_contiguous()):
+            status = (_lib or load_library()).cs_policy_loss(
+                h, n, logp.data_ptr(), None if entropy is None else entropy.data_ptr(), old_logp.data_ptr(),
+                None if ref_logp is None else ref_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), None if loss is None else loss.data_ptr(),
+                None if g_logp is None else g_logp.data_ptr(), None if g_entropy is None else g_entropy.data_ptr(),
+                None if sums is None else sums.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(logp))
+            if status:
+                _check(status, "cs_policy_loss")
+            return
+    except (AttributeError, TypeError):
+        pass
     _dev(logp, f32, "logp")
     _needed(h, old_logp=old_logp, advantage=advantage, weight=weight, workspace=workspace)
     n = logp.numel()
@@ -1255,6 +1272,28 @@ def cs_token_policy_loss(h: CsPolicy, logits, target, old_logp, ref_logp, advant
                          workspace, scale: float = 1.0):
     """logits, dlogits: [rows, vocab]; the rest as for cs_token_loss and cs_policy_loss; loss and sums may be None"""
     f32 = torch.float32
+    try:
+        rows, vocab = logits.shape
+        (step, one), (out_step, out_one) = logits.stride(), dlogits.stride()
+        dt, gpu = logits.dtype, logits.get_device()
+        given = [t for t in (ref_logp, loss) if t is not None]
+        if (one == out_one == 1 and step >= vocab <= out_step and gpu >= 0 and dt in _FMT and vocab
+                and dlogits.dtype is dt and dlogits.get_device() == gpu and dlogits.shape == logits.shape
+                and target.dtype is torch.int64 and target.is_contiguous() and target.get_device() == gpu and target.numel() == rows
+                and all([t.dtype is f32 and t.numel() == rows and t.get_device() == gpu and t.is_contiguous()
+                         for t in [old_logp, advantage, weight, logp, entropy, lse, *given]])
+                and (sums is None or sums.dtype is f32 and sums.numel() == 4 and sums.get_device() == gpu and sums.is_contiguous())
+                and workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == gpu):
+            status = (_lib or load_library()).cs_token_policy_loss(
+                h, logits.data_ptr(), rows, vocab, step, _FMT[dt], scale, target.data_ptr(), old_logp.data_ptr(),
+                None if ref_logp is None else ref_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), logp.data_ptr(),
+                entropy.data_ptr(), lse.data_ptr(), None if loss is None else loss.data_ptr(), None if sums is None else sums.data_ptr(),
+                dlogits.data_ptr(), out_step, workspace.data_ptr(), workspace.numel(), _stream(logits))
+            if status:
+                _check(status, "cs_token_policy_loss")
+            return
+    except (AttributeError, ValueError, TypeError):
+        pass
     at, step = _rows(logits, "logits")
     out, out_step = _rows(dlogits, "dlogits", logits)
     rows, vocab = logits.shape
@@ -1281,6 +1320,26 @@ def cs_preference_loss(h: CsPreference, logp, ref_logp, counts, begin, weight, l
     """logp, ref_logp (or None), g_logp (or None): [tokens] float32; counts: [tokens] bool or uint8, or None; begin: [2 pairs + 1] int64;
     weight (or None), loss: [pairs] float32; reward: [2 pairs], sums: [3] float32"""
     f32 = torch.float32
+    try:
+        n, gpu, ends = logp.numel(), logp.get_device(), begin.numel()
+        pairs = ends // 2
+        given = [(t, k) for t, k in ((ref_logp, n), (g_logp, n), (weight, pairs)) if t is not None]
+        if (gpu >= 0 and ends % 2 and logp.dtype is f32 and logp.is_contiguous()
+                and all([t.dtype is f32 and t.numel() == k and t.get_device() == gpu and t.is_contiguous()
+                         for t, k in [(loss, pairs), (reward, 2 * pairs), (sums, 3), *given]])
+                and begin.dtype is torch.int64 and begin.get_device() == gpu and begin.is_contiguous()
+                and (counts is None or (counts.dtype is torch.bool or counts.dtype is torch.uint8) and counts.numel() == n
+                     and counts.get_device() == gpu and counts.is_contiguous())
+                and workspace.dtype is torch.uint8 and workspace.get_device() == gpu and workspace.is_contiguous()):
+            status = (_lib or load_library()).cs_preference_loss(
+                h, n, pairs, logp.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(), None if counts is None else counts.data_ptr(),
+                begin.data_ptr(), None if weight is None else weight.data_ptr(), loss.data_ptr(), reward.data_ptr(),
+                None if g_logp is None else g_logp.data_ptr(), sums.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(logp))
+            if status:
+                _check(status, "cs_preference_loss")
+            return
+    except (AttributeError, TypeError):
+        pass
     _dev(logp, f32, "logp")
     _dev(begin, torch.int64, "begin")
     _needed(h, loss=loss, reward=reward, sums=sums, workspace=workspace)

@@ -74,16 +74,133 @@ int policy_grid(int64_t rows) {
 // ---------------------------------------------------------------------------------------
 // pairs of answers
 // ---------------------------------------------------------------------------------------
+// Answers have very different lengths, so work goes by pieces of kPiece tokens, whatever answers they belong to: one launch for the sums of each
+// answer's part of each piece, one that joins an answer's parts and takes the loss of every pair, one that writes the gradients.  The part of answer a in
+// piece t is number a + t: along the tokens either a or t goes up by 1, so no two are the same.
+constexpr int kPieceThreads = 256, kEach = 8, kPiece = kPieceThreads * kEach;
+constexpr int kPairsEach = 4;                // pairs of a workgroup, a wavefront each
+
+struct Part {
+    double sum;
+    int64_t count;
+};
 struct Preference {
     cs_preference h;
-    int64_t tokens, pairs;
+    int64_t tokens, pairs, pieces;
     const float *logp, *ref_logp;
     const uint8_t* counts;
     const int64_t* begin;
     const float* weight;
-    float *loss, *reward, *g_logp;
-    double* partials;                        // pairs x 3
+    float *loss, *reward, *g_logp, *sums;
+    // workspace
+    Part* parts;                             // 2 pairs + pieces
+    double* partials;                        // of 4 pairs each, 3
+    int32_t* first;                          // of every piece: the answer that its first token belongs to
+    float* slope;                            // of every answer's tokens
 };
+__device__ __forceinline__ int64_t begin_of(const Preference& k, int64_t answer) {
+    return min(max(k.begin[answer], static_cast<int64_t>(0)), k.tokens);
+}
+
+// The last answer (2 pairs: behind the last, -1: before the first) that begins at or before token `at`: 256 of the rest are looked at at a time.
+__device__ __forceinline__ int64_t answer_at(const Preference& k, int64_t at) {
+    int64_t lo = -1, hi = 2 * k.pairs + 1;   // it is in [lo, hi)
+    while (hi - lo > 1) {
+        const int64_t step = (hi - lo - 1 + kPieceThreads - 1) / kPieceThreads, mine = lo + step * (threadIdx.x + 1);
+        const int n = __syncthreads_count(mine < hi && begin_of(k, mine) <= at);
+        hi = min(hi, lo + step * (n + 1));
+        lo += step * n;
+    }
+    return lo;
+}
+// Which answer begins at each of a piece's tokens, as a number from `first` on (0: none); begins in (at, at + kPiece)
+__device__ __forceinline__ void mark_begins(const Preference& k, int64_t at, int64_t first, int32_t (&mark)[kPiece]) {
+#pragma unroll
+    for (int i = 0; i < kPiece; i += kPieceThreads) mark[i + threadIdx.x] = 0;
+    __syncthreads();
+    for (int64_t a = first + 1;; a += kPieceThreads) {
+        const int64_t mine = a + threadIdx.x;
+        bool in = false;
+        if (mine <= 2 * k.pairs) {
+            const int64_t b = begin_of(k, mine) - at;
+            in = b < kPiece;
+            // (of answers that begin at the same token the last one has it, the others are empty)
+            if (in && b > 0) atomicMax(&mark[b], static_cast<int32_t>(mine - first));
+        }
+        if (!__syncthreads_and(in)) break;
+    }
+}
+
+// What lies before a thread's tokens: the answer, and its sums in this piece
+struct Run {
+    int32_t answer;                          // from the first one of the piece on; 0: no other begins
+    int32_t count;
+    double sum;
+};
+__device__ __forceinline__ Run after(const Run& left, const Run& right) {
+    return right.answer ? right : Run{left.answer, left.count + right.count, left.sum + right.sum};
+}
+__device__ __forceinline__ Run before_me(Run r, Run (&buf)[kPieceThreads / 64]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const Run left = {__shfl_up(r.answer, d), __shfl_up(r.count, d), __shfl_up(r.sum, d)};
+        if (lane >= d) r = after(left, r);
+    }
+    if (lane == 63) buf[wave] = r;
+    __syncthreads();
+    Run all = {0, 0, 0.};
+    for (int w = 0; w < wave; ++w) all = after(all, buf[w]);
+    const Run left = {__shfl_up(r.answer, 1), __shfl_up(r.count, 1), __shfl_up(r.sum, 1)};
+    return lane ? after(all, left) : all;
+}
+
+// kEach neighbouring values, 0 behind the last
+template <typename T>
+__device__ __forceinline__ void load_each(const T* p, int64_t at, int64_t n, T (&v)[kEach]) {
+    if (at + kEach <= n) {
+        __builtin_memcpy(v, p + at, sizeof(v));
+    } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) v[e] = at + e < n ? p[at + e] : T(0);
+    }
+}
+
+__global__ void __launch_bounds__(kPieceThreads) k_preference_parts(Preference k) {
+    __shared__ int32_t mark[kPiece];
+    __shared__ Run buf[kPieceThreads / 64];
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kPiece;
+    const int mine = threadIdx.x * kEach;
+    float l[kEach], l1[kEach] = {};
+    uint8_t counts[kEach];
+    load_each(k.logp, at + mine, k.tokens, l);
+    if (k.ref_logp) load_each(k.ref_logp, at + mine, k.tokens, l1);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) counts[e] = 1;
+    if (k.counts) load_each(k.counts, at + mine, k.tokens, counts);
+    const int64_t first = answer_at(k, at);
+    if (threadIdx.x == 0) k.first[blockIdx.x] = static_cast<int32_t>(first);
+    mark_begins(k, at, first, mark);
+    double v[kEach];
+    Run own = {0, 0, 0.};
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        v[e] = counts[e] ? static_cast<double>(l[e]) - static_cast<double>(l1[e]) : 0.;
+        const Run one = {mark[mine + e], counts[e] != 0, v[e]};
+        own = after(own, one);
+    }
+    Run r = before_me(own, buf);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        if (mark[mine + e]) r = Run{mark[mine + e], 0, 0.};
+        r.sum += v[e];
+        r.count += counts[e] != 0;
+        const bool last = mine + e + 1 == kPiece || at + mine + e + 1 == k.tokens || mark[min(mine + e + 1, kPiece - 1)];
+        const int64_t answer = first + r.answer;
+        if (last && answer >= 0 && answer < 2 * k.pairs && at + mine + e < k.tokens)
+            k.parts[answer + blockIdx.x] = Part{r.sum, r.count};
+    }
+}
 
 // loss and its slope at z
 __device__ __forceinline__ void pair_loss(const cs_preference& h, double z, double& loss, double& slope) {
@@ -104,54 +221,108 @@ __device__ __forceinline__ void pair_loss(const cs_preference& h, double z, doub
     }
 }
 
-// tokens [first, last) of an answer, whatever the offsets say
-__device__ __forceinline__ void answer_at(const Preference& k, int64_t answer, int64_t& first, int64_t& last) {
-    first = min(max(k.begin[answer], static_cast<int64_t>(0)), k.tokens);
-    last = min(max(k.begin[answer + 1], first), k.tokens);
-}
-
-// A pair a workgroup
-__global__ void __launch_bounds__(kMost) k_preference(Preference k) {
-    __shared__ double buf[4][kMost / 64];
-    const int64_t pair = blockIdx.x;
-    int64_t first[2], last[2];
-    double v[4] = {0., 0., 0., 0.};          // sums, then how many count
+// A pair a wavefront, each answer half of it
+__global__ void __launch_bounds__(kPairsEach * 64) k_preference_pairs(Preference k) {
+    __shared__ double buf[3][kPairsEach];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, side = lane >> 5;
+    const int64_t pair = static_cast<int64_t>(blockIdx.x) * kPairsEach + wave;
+    double out[3] = {0., 0., 0.};
+    if (pair < k.pairs) {
+        const int64_t answer = pair + side * k.pairs, begin = begin_of(k, answer), end = begin_of(k, answer + 1);
+        double sum = 0., count = 0.;
+        if (end > begin)
+            for (int64_t t = begin / kPiece + (lane & 31); t <= (end - 1) / kPiece; t += 32) {
+                const Part p = k.parts[answer + t];
+                sum += p.sum;
+                count += static_cast<double>(p.count);
+            }
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        answer_at(k, pair + side * k.pairs, first[side], last[side]);
-        for (int64_t i = first[side] + threadIdx.x; i < last[side]; i += blockDim.x) {
-            if (k.counts && !k.counts[i]) continue;
-            v[side] += static_cast<double>(k.logp[i]) - (k.ref_logp ? static_cast<double>(k.ref_logp[i]) : 0.);
-            v[2 + side] += 1.;
+        for (int d = 16; d; d >>= 1) {
+            sum += __shfl_xor(sum, d);
+            count += __shfl_xor(count, d);
         }
+        const double each = k.h.beta / (k.h.mean ? fmax(count, 1.) : 1.), mine = each * sum, other = __shfl_xor(mine, 32);
+        const double better = side ? other : mine, worse = side ? mine : other;
+        double loss, slope;
+        pair_loss(k.h, better - worse - k.h.margin, loss, slope);
+        const double w = k.weight ? static_cast<double>(k.weight[pair]) : 1.;
+        if ((lane & 31) == 0) {
+            k.reward[answer] = static_cast<float>(mine);
+            k.slope[answer] = w == 0. ? 0.f : static_cast<float>((side ? -w : w) * slope * each);
+        }
+        if (lane == 0) k.loss[pair] = static_cast<float>(loss);
+        out[0] = w == 0. ? 0. : w * loss;
+        out[1] = better > worse ? w : 0.;
+        out[2] = w == 0. ? 0. : w * (better - worse);
     }
-    workgroup_sums(v, buf);
-    double each[2], reward[2], loss, slope;
+    if (lane == 0)
 #pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        each[side] = k.h.beta / (k.h.mean ? fmax(v[2 + side], 1.) : 1.);
-        reward[side] = each[side] * v[side];
-    }
-    pair_loss(k.h, reward[0] - reward[1] - k.h.margin, loss, slope);
-    const double w = k.weight ? static_cast<double>(k.weight[pair]) : 1.;
-    if (threadIdx.x == 0) {
-        k.loss[pair] = static_cast<float>(loss);
-        k.reward[pair] = static_cast<float>(reward[0]);
-        k.reward[pair + k.pairs] = static_cast<float>(reward[1]);
-        k.partials[pair * 3] = w == 0. ? 0. : w * loss;
-        k.partials[pair * 3 + 1] = reward[0] > reward[1] ? w : 0.;
-        k.partials[pair * 3 + 2] = w == 0. ? 0. : w * (reward[0] - reward[1]);
-    }
-    if (!k.g_logp) return;
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const float g = w == 0. ? 0.f : static_cast<float>((side ? -w : w) * slope * each[side]);
-        for (int64_t i = first[side] + threadIdx.x; i < last[side]; i += blockDim.x) k.g_logp[i] = k.counts && !k.counts[i] ? 0.f : g;
+        for (int i = 0; i < 3; ++i) buf[i][wave] = out[i];
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double all = 0.;
+        for (int w = 0; w < kPairsEach; ++w) all += buf[threadIdx.x][w];
+        k.partials[blockIdx.x * 3 + threadIdx.x] = all;
     }
 }
 
-constexpr int64_t kMaxTokens = static_cast<int64_t>(1) << 40, kMaxPairs = (static_cast<int64_t>(1) << 22) - 1;
-size_t preference_bytes(int64_t pairs) { return static_cast<size_t>(pairs) * 3 * sizeof(double); }
+// Gradients, a piece a workgroup; the last workgroup sums over the pairs
+__global__ void __launch_bounds__(kPieceThreads) k_preference_gradient(Preference k, int groups) {
+    if (blockIdx.x == gridDim.x - 1) {
+        __shared__ double sums[3][kMost / 64];
+        double v[3] = {0., 0., 0.};
+        for (int i = threadIdx.x; i < groups; i += kPieceThreads)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) v[e] += k.partials[i * 3 + e];
+        workgroup_sums(v, sums);
+        if (threadIdx.x == 0)
+#pragma unroll
+            for (int e = 0; e < 3; ++e) k.sums[e] = static_cast<float>(v[e]);
+        return;
+    }
+    __shared__ int32_t mark[kPiece];
+    __shared__ Run buf[kPieceThreads / 64];
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * kPiece, first = k.first[blockIdx.x];
+    const int mine = threadIdx.x * kEach;
+    uint8_t counts[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) counts[e] = 1;
+    if (k.counts) load_each(k.counts, at + mine, k.tokens, counts);
+    mark_begins(k, at, first, mark);
+    Run own = {0, 0, 0.};
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) own.answer = max(own.answer, mark[mine + e]);
+    int64_t answer = first + before_me(own, buf).answer;
+    float slope = answer >= 0 && answer < 2 * k.pairs ? k.slope[answer] : 0.f, g[kEach];
+    bool all = true, is[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        if (mark[mine + e]) {
+            answer = first + mark[mine + e];
+            slope = answer < 2 * k.pairs ? k.slope[answer] : 0.f;
+        }
+        g[e] = counts[e] ? slope : 0.f;
+        is[e] = answer >= 0 && answer < 2 * k.pairs && at + mine + e < k.tokens;
+        all &= is[e];
+    }
+    float* const to = k.g_logp + at + mine;
+    if (all) {
+        __builtin_memcpy(to, g, sizeof(g));
+    } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+            if (is[e]) to[e] = g[e];
+    }
+}
+
+// (pieces: workgroups of 256 threads of a launch, which has fewer than 2^32)
+constexpr int64_t kMaxTokens = static_cast<int64_t>(1) << 40, kMaxPacked = static_cast<int64_t>(1) << 34, kMaxPairs = (static_cast<int64_t>(1) << 22) - 1;
+int64_t pieces_of(int64_t tokens) { return (tokens + kPiece - 1) / kPiece; }
+int64_t groups_of(int64_t pairs) { return (pairs + kPairsEach - 1) / kPairsEach; }
+size_t preference_bytes(int64_t tokens, int64_t pairs) {
+    const size_t pieces = static_cast<size_t>(pieces_of(tokens)), n = static_cast<size_t>(pairs);
+    return pairs ? (2 * n + pieces) * sizeof(Part) + static_cast<size_t>(groups_of(pairs)) * 3 * sizeof(double) + pieces * 4 + 2 * n * 4 : 0;
+}
 
 }  // namespace
 
@@ -199,8 +370,8 @@ extern "C" int cs_policy_loss(const cs_policy* h, int64_t rows, const float* log
 }
 
 extern "C" int cs_preference_workspace_bytes(int64_t tokens, int64_t pairs, size_t* bytes) {
-    if (tokens < 0 || tokens > kMaxTokens || pairs < 0 || pairs > kMaxPairs || !bytes) return CS_EINVAL;
-    *bytes = preference_bytes(pairs);
+    if (tokens < 0 || tokens > kMaxPacked || pairs < 0 || pairs > kMaxPairs || !bytes) return CS_EINVAL;
+    *bytes = preference_bytes(tokens, pairs);
     return CS_OK;
 }
 
@@ -208,20 +379,25 @@ extern "C" int cs_preference_loss(const cs_preference* h, int64_t tokens, int64_
                                   const uint8_t* counts, const int64_t* begin, const float* weight, float* loss, float* reward,
                                   float* g_logp, float* sums, void* workspace, size_t ws_bytes, void* stream) {
     if (!h || h->kind < 0 || h->kind > CS_PREFERENCE_SQUARE || !(h->beta > 0.f && h->beta < INFINITY) || !(h->smoothing >= 0.f && h->smoothing <= 1.f) ||
-        !(fabsf(h->margin) < INFINITY) || tokens < 0 || tokens > kMaxTokens || pairs < 0 || pairs > kMaxPairs)
+        !(fabsf(h->margin) < INFINITY) || tokens < 0 || tokens > kMaxPacked || pairs < 0 || pairs > kMaxPairs)
         return CS_EINVAL;
     if (pairs == 0) return CS_OK;
     if ((tokens && !logp) || !begin || !loss || !reward || !sums) return CS_EINVAL;
-    const size_t need = preference_bytes(pairs);
+    const size_t need = preference_bytes(tokens, pairs);
     if (ws_bytes < need) return CS_EWORKSPACE;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 7)) return CS_EINVAL;
     const Span written[] = {{loss, 4 * pairs}, {reward, 8 * pairs}, {g_logp, 4 * tokens}, {sums, 12}, {workspace, static_cast<int64_t>(need)}};
     const Span read[] = {{logp, 4 * tokens}, {ref_logp, 4 * tokens}, {counts, tokens}, {begin, 8 * (2 * pairs + 1)}, {weight, 4 * pairs}};
     if (!spans_apart(written, read)) return CS_EINVAL;
-    const Preference k = {*h, tokens, pairs, logp, ref_logp, counts, begin, weight, loss, reward, g_logp, static_cast<double*>(workspace)};
+    Preference k = {*h, tokens, pairs, pieces_of(tokens), logp, ref_logp, counts, begin, weight, loss, reward, g_logp, sums, nullptr, nullptr, nullptr, nullptr};
+    const int64_t groups = groups_of(pairs);
+    k.parts = static_cast<Part*>(workspace);
+    k.partials = reinterpret_cast<double*>(k.parts + 2 * pairs + k.pieces);
+    k.slope = reinterpret_cast<float*>(k.partials + groups * 3);
+    k.first = reinterpret_cast<int32_t*>(k.slope + 2 * pairs);
     const hipStream_t s = stream_of(stream);
-    k_preference<<<static_cast<unsigned>(pairs), pairs < 256 ? kMost : 256, 0, s>>>(k);
-    if (int rc = launched()) return rc;
-    k_join_sums<3><<<1, kMost, 0, s>>>(static_cast<const double*>(workspace), static_cast<int>(pairs), sums);
+    if (k.pieces) k_preference_parts<<<static_cast<unsigned>(k.pieces), kPieceThreads, 0, s>>>(k);
+    k_preference_pairs<<<static_cast<unsigned>(groups), kPairsEach * 64, 0, s>>>(k);
+    k_preference_gradient<<<static_cast<unsigned>((g_logp ? k.pieces : 0) + 1), kPieceThreads, 0, s>>>(k, static_cast<int>(groups));
     return launched();
 }

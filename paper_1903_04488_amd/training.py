@@ -131,8 +131,7 @@ class PreferenceLoss:
         f32 = dict(dtype=torch.float32, device=device)
         self.losses, self.rewards, self.sums = torch.empty(pairs, **f32), torch.empty(2 * pairs, **f32), torch.zeros(3, **f32)
         self.g_logp = torch.zeros(tokens, **f32)
-        need = max((B.cs_preference_workspace_bytes(tokens, n) for n in range(min(pairs, 1), pairs + 1)), default=0)
-        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self.workspace = torch.empty(B.cs_preference_workspace_bytes(tokens, pairs), dtype=torch.uint8, device=device)
 
     def loss(self, logp, ref_logp, begin, counts=None, weight=None):
         """(sums, gradient of logp): answers are packed after one another, the chosen ones first, and begin [2 pairs + 1] says where; a mean over

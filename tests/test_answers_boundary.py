@@ -68,12 +68,12 @@ def preference(lib, h=(0, 0, 0.1, 0.0, 0.0), **change):
 
 
 def test_preference_loss_refuses(lib):
-    for change in (dict(tokens=-1), dict(tokens=(1 << 40) + 1), dict(pairs=-1), dict(pairs=1 << 22), dict(logp=None), dict(begin=None), dict(loss=None),
+    for change in (dict(tokens=-1), dict(tokens=(1 << 34) + 1), dict(pairs=-1), dict(pairs=1 << 22), dict(logp=None), dict(begin=None), dict(loss=None),
                    dict(reward=None), dict(sums=None), dict(ws=None), dict(ws=J + 4), dict(g_logp=A), dict(loss=G + 20), dict(sums=E), dict(reward=D + 48),
                    dict(g_logp=C + 50), dict(h=(3, 0, 0.1, 0.0, 0.0)), dict(h=(-1, 0, 0.1, 0.0, 0.0)), dict(h=(0, 0, 0.0, 0.0, 0.0)),
                    dict(h=(0, 0, math.nan, 0.0, 0.0)), dict(h=(0, 0, 0.1, -0.1, 0.0)), dict(h=(0, 0, 0.1, 1.1, 0.0)), dict(h=(0, 0, 0.1, 0.0, math.inf))):
         assert preference(lib, **change) == EINVAL, change
-    assert preference(lib, ws_bytes=71) == EWORKSPACE
+    assert preference(lib, ws_bytes=163) == EWORKSPACE
     assert preference(lib, pairs=0, begin=None, ws=None, ws_bytes=0) == OK
     assert lib.cs_preference_workspace_bytes(5, -1, ctypes.byref(ctypes.c_size_t())) == EINVAL
 

@@ -99,7 +99,8 @@ def check(t, kind, beta, smoothing=0.0, margin=0.0, mean=False):
 
 LENGTHS = {"one": [1, 1], "none": [0, 0], "one empty": [0, 5], "few": [3, 70, 1, 65, 64, 63], "some empty": [0, 9, 0, 300, 0, 0, 7, 0],
            "uneven": [5000, 1, 2, 4097, 1, 3], "long": [70_001, 40_000], "many": [(7 * i) % 41 for i in range(1200)],
-           "a long one among many": [20] * 300 + [30_000] + [15] * 299}
+           "a long one among many": [20] * 300 + [30_000] + [15] * 299, "of one token": [1] * 9000, "hardly any": [0] * 5000 + [1] + [0] * 4000 + [2] * 3 + [0] * 2,
+           "whole pieces": [2048, 2048, 4096, 2048], "next to whole pieces": [2047, 1, 2049, 4095, 2, 2046]}
 
 
 @pytest.mark.parametrize("lengths", list(LENGTHS))
@@ -128,8 +129,8 @@ def test_offsets_outside_the_tokens_are_cut_off():
     t = batch_of([10, 20, 30, 40], masked=False)
     for begin in ([-5, 10, 30, 60, 1 << 40], [0, 10, 30, 200, 300], [-(1 << 50), -3, -2, -1, 0]):
         check(t | {"begin": torch.tensor(begin, device=DEV)}, "logistic", 0.25)
-    got = run(t | {"begin": torch.tensor([50, 10, 90, 20, 100], device=DEV)}, "logistic", 0.25)     # not ascending: no fault
-    assert torch.isfinite(got["loss"]).all()
+    run(t | {"begin": torch.tensor([50, 10, 90, 20, 100], device=DEV)}, "logistic", 0.25)     # not ascending: no results, no fault
+    torch.cuda.synchronize()
 
 
 def test_a_pair_of_weight_zero_and_one_that_is_not_a_number():
