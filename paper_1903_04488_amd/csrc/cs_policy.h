@@ -57,10 +57,21 @@ __device__ __forceinline__ PolicyToken policy_token(const cs_policy& h, float lo
     t.cut = cut ? w : 0.f;
     return t;
 }
-__device__ __forceinline__ PolicyToken policy_token(const PolicyIn& in, int64_t row, float logp, float entropy, bool counts) {
-    const float w = counts ? in.weight[row] : 0.f;
-    return policy_token(in.h, logp, entropy, in.old_logp[row], in.h.kl != 0.f ? in.ref_logp[row] : 0.f, in.advantage[row], w);
+// a row's inputs, and its token
+struct PolicyRow {
+    float old_logp, ref_logp, advantage, weight;
+};
+__device__ __forceinline__ PolicyRow policy_row(const PolicyIn& in, int64_t row) {
+    return PolicyRow{in.old_logp[row], in.h.kl != 0.f ? in.ref_logp[row] : 0.f, in.advantage[row], in.weight[row]};
 }
+__device__ __forceinline__ PolicyToken policy_token(const cs_policy& h, const PolicyRow& row, float logp, float entropy, bool counts) {
+    return policy_token(h, logp, entropy, row.old_logp, row.ref_logp, row.advantage, counts ? row.weight : 0.f);
+}
+
+// What sums are taken of, a row
+struct PolicyTerms {
+    float loss, kl, cut, weight;
+};
 
 // Losses (or null), gradients (or null) and sums (or null) of `rows` tokens; target and vocab say which rows have a token
 // (target null: all).  partials: policy_partials(rows) x 4 binary64.
@@ -71,6 +82,8 @@ struct PolicyOut {
 int policy_partials(int64_t rows);
 int launch_policy(const PolicyIn& in, int64_t rows, const float* logp, const float* entropy, const int64_t* target, int64_t vocab,
                   const PolicyOut& out, hipStream_t stream);
+// The sums alone, of rows whose terms are known, in the same order
+int launch_policy_sums(const PolicyTerms* terms, int64_t rows, float* sums, double* partials, hipStream_t stream);
 bool policy_ok(const cs_policy* h);
 
 }  // namespace cs

@@ -12,20 +12,23 @@ namespace {
 
 constexpr int kMost = 1024;                  // threads of a workgroup
 
-// Sums of N binary64 numbers over a workgroup, in a fixed order; thread 0 has them
+// Sums of N binary64 numbers over a workgroup, in a fixed order; the first wavefront has them
 template <int N>
 __device__ __forceinline__ void workgroup_sums(double (&v)[N], double (&buf)[N][kMost / 64]) {
+    const int lane = threadIdx.x & 63, waves = blockDim.x / 64;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
 #pragma unroll
         for (int d = 32; d; d >>= 1) v[k] += __shfl_xor(v[k], d);
-        if ((threadIdx.x & 63) == 0) buf[k][threadIdx.x >> 6] = v[k];
+        if (lane == 0) buf[k][threadIdx.x >> 6] = v[k];
     }
     __syncthreads();
+    if (threadIdx.x >= 64) return;
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        v[k] = 0.;
-        for (unsigned w = 0; w < blockDim.x / 64; ++w) v[k] += buf[k][w];
+        v[k] = lane < waves ? buf[k][lane] : 0.;
+#pragma unroll
+        for (int d = kMost / 128; d; d >>= 1) v[k] += __shfl_xor(v[k], d);
     }
 }
 
@@ -38,11 +41,12 @@ k_policy(PolicyIn in, int64_t rows, const float* logp, const float* entropy, con
     for (int64_t row = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; row < rows; row += step) {
         const int64_t at = target ? target[row] : 0;
         const bool counts = !target || (at >= 0 && at < vocab);
-        const PolicyToken t = policy_token(in, row, logp[row], in.h.entropy != 0.f ? entropy[row] : 0.f, counts);
+        const PolicyRow given = policy_row(in, row);
+        const PolicyToken t = policy_token(in.h, given, logp[row], in.h.entropy != 0.f ? entropy[row] : 0.f, counts);
         if (out.loss) out.loss[row] = t.loss;
         if (out.g_logp) out.g_logp[row] = t.g_logp;
         if (out.g_entropy) out.g_entropy[row] = t.g_entropy;
-        sums[0] += t.loss, sums[1] += t.kl, sums[2] += t.cut, sums[3] += counts ? in.weight[row] : 0.f;
+        sums[0] += t.loss, sums[1] += t.kl, sums[2] += t.cut, sums[3] += counts ? given.weight : 0.f;
     }
     if (!out.sums) return;
     workgroup_sums(sums, buf);
@@ -51,6 +55,23 @@ k_policy(PolicyIn in, int64_t rows, const float* logp, const float* entropy, con
         for (int k = 0; k < 4; ++k) {
             if (gridDim.x == 1) out.sums[k] = static_cast<float>(sums[k]);
             else out.partials[blockIdx.x * 4 + k] = sums[k];
+        }
+}
+__global__ void __launch_bounds__(kMost) k_policy_sums(const PolicyTerms* terms, int64_t rows, float* out, double* partials) {
+    __shared__ double buf[4][kMost / 64];
+    double sums[4] = {0., 0., 0., 0.};
+    const int64_t step = static_cast<int64_t>(gridDim.x) * blockDim.x;
+#pragma unroll 8
+    for (int64_t row = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; row < rows; row += step) {
+        const PolicyTerms t = terms[row];
+        sums[0] += t.loss, sums[1] += t.kl, sums[2] += t.cut, sums[3] += t.weight;
+    }
+    workgroup_sums(sums, buf);
+    if (threadIdx.x == 0)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (gridDim.x == 1) out[k] = static_cast<float>(sums[k]);
+            else partials[blockIdx.x * 4 + k] = sums[k];
         }
 }
 template <int N>
@@ -68,7 +89,7 @@ __global__ void __launch_bounds__(kMost) k_join_sums(const double* partials, int
 
 int policy_grid(int64_t rows) {
     const int64_t grid = (rows + kMost - 1) / kMost;
-    return static_cast<int>(grid < 8 ? 1 : grid < 256 ? grid : 256);
+    return static_cast<int>(grid <= 16 ? 1 : grid < 256 ? grid : 256);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -339,6 +360,16 @@ int launch_policy(const PolicyIn& in, int64_t rows, const float* logp, const flo
     if (int rc = launched()) return rc;
     if (grid == 1 || !out.sums) return CS_OK;
     k_join_sums<4><<<1, 256, 0, stream>>>(out.partials, grid, out.sums);
+    return launched();
+}
+
+int launch_policy_sums(const PolicyTerms* terms, int64_t rows, float* sums, double* partials, hipStream_t stream) {
+    const int grid = policy_grid(rows);
+    const int64_t need = (rows + 63) / 64 * 64;
+    k_policy_sums<<<grid, static_cast<unsigned>(need < kMost ? need : kMost), 0, stream>>>(terms, rows, sums, partials);
+    if (int rc = launched()) return rc;
+    if (grid == 1) return CS_OK;
+    k_join_sums<4><<<1, 256, 0, stream>>>(partials, grid, sums);
     return launched();
 }
 

@@ -77,9 +77,11 @@ struct TokenArgs {
     void* dlogits;
     int64_t d_stride;
     hipStream_t stream;
-    // kTokenPolicy: its inputs, losses and sums; the gradients of logp and entropy where rows are not held
+    // kTokenPolicy: its inputs; losses (or null) and sums (or null); what sums are taken of, and for rows in parts the gradients of logp
+    // and entropy
     PolicyIn policy;
     PolicyOut policy_out;
+    PolicyTerms* policy_terms;
 };
 
 enum TokenCall { kTokenForward, kTokenGrad, kTokenLoss, kTokenPolicy };

@@ -24,11 +24,12 @@ bool dlogits_ok(const TokenArgs& a) {
     return !rows_meet(a.dlogits, a.d_stride * b, a.logits, a.stride * b, a.rows, a.vocab * b);
 }
 
-// The parts of rows (a multiple of 8), then partial sums, then the gradients of few rows' log probabilities and entropies
+// The parts of rows (a multiple of 8), then partial sums, then what sums are taken of, or for rows in parts the gradients of log probabilities
+// and entropies, 16 bytes a row
 size_t parts_bytes8(int64_t rows, int64_t vocab) { return (token_bytes(rows, vocab, 0) + 7) / 8 * 8; }
 size_t policy_bytes(int64_t rows, int64_t vocab) {
     if (rows == 0) return 0;
-    return parts_bytes8(rows, vocab) + static_cast<size_t>(policy_partials(rows)) * 4 * sizeof(double) + (few_rows(rows) ? 8 * static_cast<size_t>(rows) : 0);
+    return parts_bytes8(rows, vocab) + static_cast<size_t>(policy_partials(rows)) * 4 * sizeof(double) + sizeof(PolicyTerms) * static_cast<size_t>(rows);
 }
 
 }  // namespace
@@ -128,10 +129,9 @@ extern "C" int cs_token_policy_loss(const cs_policy* h, const void* logits, int6
     a.policy = PolicyIn{*h, old_logp, ref, advantage, weight};
     char* const more = static_cast<char*>(workspace) + parts_bytes8(rows, vocab);
     a.policy_out = PolicyOut{loss, nullptr, nullptr, sums, reinterpret_cast<double*>(more)};
-    if (few_rows(rows)) {
-        a.policy_out.g_logp = reinterpret_cast<float*>(more + static_cast<size_t>(policy_partials(rows)) * 4 * sizeof(double));
-        a.policy_out.g_entropy = a.policy_out.g_logp + rows;
-    }
+    char* const terms = more + static_cast<size_t>(policy_partials(rows)) * 4 * sizeof(double);
+    a.policy_terms = sums ? reinterpret_cast<PolicyTerms*>(terms) : nullptr;
+    a.policy_out.g_logp = reinterpret_cast<float*>(terms), a.policy_out.g_entropy = a.policy_out.g_logp + rows;
     if (!dlogits_ok(a)) return CS_EINVAL;
     const int64_t n = 4 * rows, dlogits_span = row_span(rows, vocab, d_stride, fmt);
     const Span written[] = {{logp, n}, {entropy, n}, {lse, n}, {loss, n}, {sums, 16}, {workspace, static_cast<int64_t>(need)}};
@@ -140,8 +140,5 @@ extern "C" int cs_token_policy_loss(const cs_policy* h, const void* logits, int6
     const Span grad[] = {{dlogits, dlogits_span}};
     const Span rest[] = {{target, 8 * rows}, {old_logp, n}, {ref, n}, {advantage, n}, {weight, n}};
     if (!spans_apart(written, read) || !spans_apart(grad, rest)) return CS_EINVAL;
-    if (int rc = by_type(kTokenPolicy, a)) return rc;
-    if (!loss && !sums) return CS_OK;
-    const PolicyOut out = {loss, nullptr, nullptr, sums, a.policy_out.partials};
-    return launch_policy(a.policy, rows, logp, entropy, target, vocab, out, a.stream);
+    return by_type(kTokenPolicy, a);
 }

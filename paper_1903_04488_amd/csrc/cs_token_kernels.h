@@ -550,6 +550,11 @@ k_token_join(const T* logits, int64_t vocab, int64_t stride, float scale, const 
 //   kDiffs, from differences: l = (x - add) mul = ln p + ln S, p = e^l / S:    a = -scale (g + h (H - ln S)) / S,  b = -scale h / S
 // (a value with no probability has p = 0, l = -inf and the gradient 0).  The target's value has hot = scale g more.
 enum { kLogs, kSums, kDiffs };
+struct PolicyRows {
+    PolicyIn in;
+    float* loss;
+    PolicyTerms* terms;
+};
 struct RowGrad {
     float mul, add, a, b, hot;
     int32_t target;                  // -1: none
@@ -563,11 +568,15 @@ struct RowGrad {
         a = -hot;
         b = g_entropy ? -scale * g_entropy[row] : 0.f;
     }
-    // the same from the policy loss of a token whose row has these sums
-    __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const PolicyIn& policy, float logp,
-                                                 float entropy) {
+    // the same from the policy loss of a row's token; writes: that thread leaves the loss and what sums are taken of
+    __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const PolicyRows& rows,
+                                                 const PolicyRow& given, float logp, float entropy, bool writes) {
         target = t >= 0 && t < vocab ? static_cast<int32_t>(t) : -1;
-        const PolicyToken token = policy_token(policy, row, logp, entropy, target >= 0);
+        const PolicyToken token = policy_token(rows.in.h, given, logp, entropy, target >= 0);
+        if (writes) {
+            if (rows.loss) rows.loss[row] = token.loss;
+            if (rows.terms) rows.terms[row] = PolicyTerms{token.loss, token.kl, token.cut, target >= 0 ? given.weight : 0.f};
+        }
         hot = scale * token.g_logp;
         a = -hot;
         b = -scale * token.g_entropy;
@@ -800,7 +809,7 @@ __device__ __forceinline__ void grad_held(const HeldRow<T, THREADS, ITEMS>& held
 template <typename T, int MODE, int THREADS, int ITEMS, bool PAST>
 __global__ void __launch_bounds__(THREADS == 64 ? kThreads : THREADS)
 k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out, int top,
-             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, int parts, Parts ws, PolicyIn policy) {
+             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, int parts, Parts ws, PolicyRows policy) {
     constexpr int ROWS = THREADS == 64 ? kThreads / 64 : 1, P = kPack<T>;
     __shared__ TokenShared<THREADS> shared[ROWS];
     int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + (THREADS == 64 ? threadIdx.x >> 6 : 0);
@@ -819,6 +828,7 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
     const bool results = parts == 1;
     const T* x = logits + row * stride + first * P;
     const int64_t t = MODE == kLoss || MODE == kPolicy || (out.logp && results) ? target[row] : -1;
+    const PolicyRow given = MODE == kPolicy ? policy_row(policy.in, row) : PolicyRow{};       // (under way while the row is read)
     const float k = scale * kLog2e;
     HeldRow<T, THREADS, ITEMS> held;
     held.load(x, vocab, packs);
@@ -848,8 +858,9 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
         RowGrad g;
         bool bonus;
         if constexpr (MODE == kPolicy) {
-            g.coefficients(row, vocab, scale, t, policy, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum));
-            bonus = policy.h.entropy != 0.f;
+            g.coefficients(row, vocab, scale, t, policy, given, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum),
+                           thread_of_row<THREADS>() == 0);
+            bonus = policy.in.h.entropy != 0.f;
         } else {
             g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
             bonus = g_entropy;
@@ -865,12 +876,13 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
 template <typename T, bool PAST, int MODE>
 __global__ void __launch_bounds__(kThreads)
 k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, TokenOut out,
-             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, PolicyIn policy) {
+             const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int32_t packs, PolicyRows policy) {
     __shared__ TokenShared<kThreads> sh;
     const int64_t row = blockIdx.x;
     const T* x = logits + row * stride;
     T* dx = dlogits + row * d_stride;
     const int64_t t = target[row];
+    const PolicyRow given = MODE == kPolicy ? policy_row(policy.in, row) : PolicyRow{};
     const float k = scale * kLog2e;
     Scan<T, false> scan;
     scan_packs<T, false, kThreads>(x, vocab, 0, packs, k, scan);
@@ -883,8 +895,9 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     RowGrad g;
     bool bonus;
     if constexpr (MODE == kPolicy) {
-        g.coefficients(row, vocab, scale, t, policy, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum));
-        bonus = policy.h.entropy != 0.f;
+        g.coefficients(row, vocab, scale, t, policy, given, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum),
+                       threadIdx.x == 0);
+        bonus = policy.in.h.entropy != 0.f;
     } else {
         g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
         bonus = g_entropy;
@@ -901,12 +914,15 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
 struct Held {
     int threads, items;
 };
-Held held(int64_t rows, int64_t vocab, int32_t fmt, int parts) {
+// Rows (or parts) up to which each has 1024 threads.  A policy loss has 512 from a row a CU on, where two rounds of 1024 would be needed (300 x 32001
+// f32 23 / 19 us).
+constexpr int64_t kFewHeldRows = 512, kFewPolicyRows = 257;
+Held held(int64_t rows, int64_t vocab, int32_t fmt, int parts, int64_t few = kFewHeldRows) {
     const int32_t all = packs_of(vocab, fmt), packs = (all + parts - 1) / parts;
     if (packs <= 256 && parts == 1) return {64, (packs + 63) / 64};
     // as many threads as there are for few rows; for many as few as have the registers, so that more rows are under way
     for (const int threads : {256, 512, 1024}) {
-        if (threads < 1024 && rows * parts < 512) continue;
+        if (threads < 1024 && rows * parts < few) continue;
         const int items = (packs + 4 * threads - 1) / (4 * threads) * 4;
         // (a part that is a pack shorter still has all but the last four packs of every thread whole)
         if (parts > 1 && all / parts <= threads * (items - 4) + 1) return {0, 0};
@@ -923,7 +939,8 @@ int token_held_as(const TokenArgs& a, int parts) {
     kernel<<<static_cast<unsigned>(grid), THREADS == 64 ? kThreads : THREADS, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.rows, static_cast<int32_t>(a.vocab), a.stride, a.scale, a.target, a.out, a.top, a.g_logp,
         a.g_entropy, static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt), parts,
-        parts > 1 ? parts_in(a.ws, a.rows, parts, a.top) : Parts{}, a.policy);
+        parts > 1 ? parts_in(a.ws, a.rows, parts, a.top) : Parts{},
+        PolicyRows{a.policy, a.policy_out.loss, a.policy_terms});
     return launched();
 }
 template <typename T, int MODE>
@@ -974,17 +991,24 @@ int token_grad(const TokenArgs& a) {
         static_cast<T*>(a.dlogits), a.d_stride, static_cast<int>(pieces), packs);
     return launched();
 }
+// (kPolicy: the sums too)
 template <typename T, int MODE>
 int token_loss(TokenArgs a) {
-    const Held h = held(a.rows, a.vocab, a.fmt, 1);
-    if (h.threads && parts_of(a.rows, a.vocab) == 1) return token_held<T, MODE>(a, h, 1);
+    const auto sums = [&] {
+        if (MODE != kPolicy || !a.policy_terms) return static_cast<int>(CS_OK);
+        return launch_policy_sums(a.policy_terms, a.rows, a.policy_out.sums, a.policy_out.partials, a.stream);
+    };
+    const Held h = held(a.rows, a.vocab, a.fmt, 1, MODE == kPolicy ? kFewPolicyRows : kFewHeldRows);
+    if (h.threads && parts_of(a.rows, a.vocab) == 1) {
+        if (int rc = token_held<T, MODE>(a, h, 1)) return rc;
+        return sums();
+    }
     if (few_rows(a.rows)) {
         if (int rc = token_forward<T, false>(a)) return rc;
         if (MODE == kPolicy) {
-            PolicyOut out = {nullptr, a.policy_out.g_logp, a.policy_out.g_entropy, nullptr, nullptr};
-            if (a.policy.h.entropy == 0.f) out.g_entropy = nullptr;
-            if (int rc = launch_policy(a.policy, a.rows, a.out.logp, a.out.entropy, a.target, a.vocab, out, a.stream)) return rc;
-            a.g_logp = out.g_logp, a.g_entropy = out.g_entropy;
+            if (a.policy.h.entropy == 0.f) a.policy_out.g_entropy = nullptr;
+            if (int rc = launch_policy(a.policy, a.rows, a.out.logp, a.out.entropy, a.target, a.vocab, a.policy_out, a.stream)) return rc;
+            a.g_logp = a.policy_out.g_logp, a.g_entropy = a.policy_out.g_entropy;
         }
         a.lse = a.out.lse, a.entropy = a.out.entropy;
         return token_grad<T>(a);
@@ -992,8 +1016,10 @@ int token_loss(TokenArgs a) {
     const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_loss<T, true, MODE> : k_token_loss<T, false, MODE>;
     kernel<<<static_cast<unsigned>(a.rows), kThreads, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.vocab, a.stride, a.scale, a.target, a.out, a.g_logp, a.g_entropy,
-        static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt), a.policy);
-    return launched();
+        static_cast<T*>(a.dlogits), a.d_stride, packs_of(a.vocab, a.fmt),
+        PolicyRows{a.policy, a.policy_out.loss, a.policy_terms});
+    if (int rc = launched()) return rc;
+    return sums();
 }
 
 template <typename T>
