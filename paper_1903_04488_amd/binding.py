@@ -113,7 +113,7 @@ class CsMatrix(ctypes.Structure):
 
 class CsMatrixList(ctypes.Structure):
     _fields_ = [("memory", ctypes.c_void_p), *((name, ctypes.c_int64) for name in ("matrices", "littles", "pieces", "halves", "fulls", "work")),
-                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_tile", "full_tile", "little_cols", "unused"))]
+                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_tile", "full_high", "full_wide", "little_cols"))]
 
 
 class CsMuon(ctypes.Structure):

@@ -16,6 +16,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "cs_rows.h"
 #include "csketch.h"
 
@@ -60,9 +62,9 @@ struct List {
     const Place* pieces;
 };
 
-// A matrix's part of the workspace: X, X^T twice (read and written in turns), A0, B0, and the diagonals of A and B.  Values are two halves, the upper
-// and the lower 11 bits.  Where the products take both (two terms) they lie in one array, 32 upper ones and then the 32 lower ones of the same
-// columns; otherwise the lower ones of X have an array of their own and there are no others.
+// A matrix's part of the workspace: X twice (read and written in turns), A0, B0, and the diagonals of A and B.  Values are two halves, the upper and the
+// lower 11 bits.  Where the products take both (two terms) they lie in one array, 32 upper ones and then the 32 lower ones of the same columns;
+// otherwise the lower ones of X have one array of their own and there are no others.
 template <int TERMS>
 struct Work {
     _Float16* base;
@@ -70,21 +72,18 @@ struct Work {
     int32_t np;
     __device__ __forceinline__ Work(char* ws, int64_t at, int32_t n, int32_t m)
         : base(reinterpret_cast<_Float16*>(ws + at)), nm(static_cast<int64_t>(n) * m), nn(static_cast<int64_t>(n) * n), np(n) {}
-    __device__ __forceinline__ _Float16* x() const { return base; }
-    __device__ __forceinline__ _Float16* xt(int turn) const { return base + (2 + turn * TERMS) * nm; }
-    __device__ __forceinline__ _Float16* a() const { return base + (2 + 2 * TERMS) * nm; }
-    __device__ __forceinline__ _Float16* b() const { return base + (2 + 2 * TERMS) * nm + TERMS * nn; }
-    __device__ __forceinline__ float* da() const { return reinterpret_cast<float*>(base + (2 + 2 * TERMS) * nm + 2 * TERMS * nn); }
+    __device__ __forceinline__ _Float16* x(int turn) const { return base + turn * TERMS * nm; }
+    __device__ __forceinline__ _Float16* x_low(int turn) const { return TERMS == 1 ? base + 2 * nm : x(turn) + 32; }
+    __device__ __forceinline__ _Float16* a() const { return base + (2 + TERMS) * nm; }
+    __device__ __forceinline__ _Float16* b() const { return a() + TERMS * nn; }
+    __device__ __forceinline__ float* da() const { return reinterpret_cast<float*>(b() + TERMS * nn); }
     __device__ __forceinline__ float* db() const { return da() + np; }
-    // of an array's value, and from there to its lower half
+    // of an array's value
     static __device__ __forceinline__ int64_t place(int64_t row, int32_t col, int32_t width) {
         return TERMS == 1 ? row * width + col : row * 2 * width + col / 32 * 64 + col % 32;
     }
-    __device__ __forceinline__ int64_t to_low() const { return TERMS == 1 ? nm : 32; }
 };
-int64_t work_bytes(int64_t np, int64_t mp, int terms) {
-    return 2 * ((2 + 2 * terms) * np * mp + 2 * terms * np * np) + 2 * 4 * np;
-}
+int64_t work_bytes(int64_t np, int64_t mp, int terms) { return 2 * ((2 + terms) * np * mp + 2 * terms * np * np) + 2 * 4 * np; }
 
 __global__ void __launch_bounds__(64) k_list_matrices(Batch b, Matrix* out, int count) {
     if (static_cast<int>(threadIdx.x) < count) out[threadIdx.x] = b.t[threadIdx.x];
@@ -114,9 +113,9 @@ __device__ __forceinline__ void half_tile_of(int32_t local, int32_t down, int32_
 }
 
 enum { kPieces, kHalves, kFulls };
-// The matrix of every place (the last that begins at or before it), and what there is to know of it; edge: of a tile.
+// The matrix of every place (the last that begins at or before it), and what there is to know of it; high, wide: of a tile.
 template <int WHICH, typename Out>
-__global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices, int begin, int end, int edge, Out* out, int64_t places) {
+__global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices, int begin, int end, int high, int wide, Out* out, int64_t places) {
     const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     if (c >= places) return;
     const auto first = [&](int i) {
@@ -135,8 +134,8 @@ __global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices
     } else {
         const Matrix& t = matrices[lo];
         Tile tile = {t.at, t.np, t.mp, 0, 0, lo, 0};
-        if (WHICH == kHalves) half_tile_of(local, t.np / edge, tile.ti, tile.tj);
-        else tile_of(local, t.np / edge, t.mp / edge, tile.ti, tile.tj);
+        if (WHICH == kHalves) half_tile_of(local, t.np / high, tile.ti, tile.tj);
+        else tile_of(local, t.np / high, t.mp / wide, tile.ti, tile.tj);
         out[c] = tile;
     }
 }
@@ -147,7 +146,14 @@ __device__ __forceinline__ bool skipped(const float* grad_scale) { return grad_s
 template <typename T, int N>
 __device__ __forceinline__ void read_as(const T* row, int32_t col, int32_t cols, float (&v)[N]) {
     if (col + N <= cols) {
-        load_pack<T, N>(row + col, v);
+        constexpr int P = N < kPack<T> ? N : kPack<T>;
+#pragma unroll
+        for (int e = 0; e < N; e += P) {
+            float part[P];
+            load_pack<T, P>(row + col + e, part);
+#pragma unroll
+            for (int k = 0; k < P; ++k) v[e + k] = part[k];
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e) v[e] = col + e < cols ? static_cast<float>(row[col + e]) : 0.f;
@@ -255,7 +261,7 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
     lo = static_cast<_Float16>(v - static_cast<float>(hi));
 }
 
-// X and X^T from u, zero behind the last row and column.  joined: a matrix's squares are summed already.
+// X from u, zero behind the last row and column.  joined: a matrix's squares are summed already.
 template <int TERMS>
 __global__ void __launch_bounds__(kThreads) k_muon_begin(List list, Moment k, double eps, const double* squares, bool joined, char* ws) {
     __shared__ float tile[kEdge][kEdge + 1];
@@ -287,30 +293,20 @@ __global__ void __launch_bounds__(kThreads) k_muon_begin(List list, Moment k, do
             tile[q / (kEdge / kFour)][q % (kEdge / kFour) * kFour + e] = static_cast<float>(u[i / kThreads][e] * one);
     }
     __syncthreads();
+    // (of a tall matrix the transpose)
     const bool tall = t.rows > t.cols;
-    // as it is given: X of a wide matrix, X^T of a tall one; and the other way round
-    _Float16 *const as_is = tall ? w.xt(0) : w.x(), *const turned = tall ? w.x() : w.xt(0);
     for (int i = threadIdx.x; i < kEdge * kEdge / 8; i += kThreads) {
         const int r = i / 8, c = i % 8 * 8;
         Half8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             _Float16 h, l;
-            split(tile[r][c + e], h, l);
+            split(tall ? tile[c + e][r] : tile[r][c + e], h, l);
             hi[e] = h, lo[e] = l;
         }
-        _Float16* to = as_is + Work<TERMS>::place(piece.row + r, piece.col + c, tall ? t.np : t.mp);
-        *reinterpret_cast<Half8*>(to) = hi;
-        if (TERMS == 2 || !tall) *reinterpret_cast<Half8*>(to + w.to_low()) = lo;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            _Float16 h, l;
-            split(tile[c + e][r], h, l);
-            hi[e] = h, lo[e] = l;
-        }
-        to = turned + Work<TERMS>::place(piece.col + r, piece.row + c, tall ? t.mp : t.np);
-        *reinterpret_cast<Half8*>(to) = hi;
-        if (TERMS == 2 || tall) *reinterpret_cast<Half8*>(to + w.to_low()) = lo;
+        const int64_t to = Work<TERMS>::place((tall ? piece.col : piece.row) + r, (tall ? piece.row : piece.col) + c, t.mp);
+        *reinterpret_cast<Half8*>(w.x(0) + to) = hi;
+        *reinterpret_cast<Half8*>(w.x_low(0) + to) = lo;
     }
 }
 
@@ -329,27 +325,28 @@ struct Steps {
 };
 struct Product {
     float a, b, c;
-    int turn;                                // which of the two X^T is read
+    int turn;                                // which of the two X is read
     Last last;                               // kFinish
 };
 
 typedef __attribute__((address_space(3))) void* LdsPointer;
 typedef const __attribute__((address_space(1))) void* GlobalPointer;
 
-// The tile of a workgroup: WI x WJ wavefronts, each with FI x FJ blocks of 16 x 16; STAGES parts of DEPTH values of K are in LDS or on
-// their way there.  WAVES_PER_SIMD: as many as the registers are shared out for.
-template <int WI_, int WJ_, int FI_, int FJ_, int STAGES_, int DEPTH_, int WAVES_PER_SIMD_>
+// The tile of a workgroup: WI x WJ wavefronts, each with FI x FJ blocks of 16 x 16; STAGES parts of 64 values of K are in LDS or on their
+// way there; AHEAD: operands are read from there a step ahead.  WAVES_PER_SIMD: as many as the registers are shared out for.
+template <int WI_, int WJ_, int FI_, int FJ_, int STAGES_, int WAVES_PER_SIMD_, bool AHEAD_>
 struct Shape {
-    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, STAGES = STAGES_, DEPTH = DEPTH_, WAVES_PER_SIMD = WAVES_PER_SIMD_;
+    static constexpr int WI = WI_, WJ = WJ_, FI = FI_, FJ = FJ_, STAGES = STAGES_, DEPTH = 64, WAVES_PER_SIMD = WAVES_PER_SIMD_;
+    static constexpr bool AHEAD = AHEAD_;
     static constexpr int WAVES = WI * WJ, THREADS = WAVES * 64, TI = WI * FI * 16, TJ = WJ * FJ * 16;
     // Blocks that belong together: a lane has GI neighbouring rows of 4 GJ neighbouring columns of the output, so that both it and its
     // transpose are written in whole pieces of memory straight from the registers.
     static constexpr int GI = FI < 4 ? FI : 4, GJ = FJ;
     static constexpr int PACKS = DEPTH / 8, ROWS = 64 / PACKS;           // of 16 bytes, a row; rows that a wavefront loads at once
     static constexpr int LOADS = (TI + TJ) / ROWS / WAVES;               // of 1 KB, a wavefront and stage
-    static_assert(TI % (ROWS * WAVES) == 0 && TJ % (ROWS * WAVES) == 0 && FI % GI == 0 && FJ <= 4 && (DEPTH == 32 || DEPTH == 64), "");
+    static_assert(TI % (ROWS * WAVES) == 0 && TJ % (ROWS * WAVES) == 0 && FI % GI == 0 && FJ <= 4, "");
     // the order of a row's packs in LDS: 16 lanes that read the same pack of 16 rows meet all banks once
-    static __device__ __forceinline__ int order(int place) { return DEPTH == 64 ? place >> 1 & 7 : place >> 2 & 3; }
+    static __device__ __forceinline__ int order(int place) { return place >> 1 & 7; }
 };
 // The row of the left tile that is place `at` of LDS: lane l of block f (of a group of GI) has row GI l + f.
 template <typename S>
@@ -386,11 +383,54 @@ struct Stage {
                                              (LdsPointer)(lds + (q * S::WAVES + wave) * 512), 16, 0, 0);
     }
 };
+// The right operand of B X: columns of X, which lies in rows.  A part of K is 64 (of two terms 32) rows of the tile's columns; LDS gives them
+// transposed (four lanes hold 16 columns of a row, and a lane gets a column of four rows).  A row's packs lie in the order pack ^ order(row): a
+// quarter of a wavefront reads four rows, which meet different banks.
+template <typename S, int TERMS>
+struct Columns {
+    static constexpr int N = S::TJ / (8 * S::WAVES), PACKS = S::TJ * TERMS / 8, WIDTH = PACKS * 8;
+    static constexpr int ODD = TERMS == 2 ? (S::GJ == 4 ? 1 : 4) : S::GJ == 4 ? 1 : PACKS == 8 ? 0 : 4;
+    static constexpr int HIGH = TERMS == 2 ? (S::GJ == 4 ? 4 : 8) : PACKS == 8 ? 4 : 8;
+    static __device__ __forceinline__ int order(int row) { return (row & 1) * ODD ^ (row >> 1 & 1) * HIGH; }
+    uint32_t offset[N];
+    __device__ __forceinline__ explicit Columns(uint32_t row_bytes) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const int at = (q * S::WAVES + wave) * 64 + lane, row = at / PACKS;
+            offset[q] = row * row_bytes + (at % PACKS ^ order(row)) * 16;
+        }
+    }
+    __device__ __forceinline__ void load(const char* from, _Float16* lds) const {
+        const int wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+            __builtin_amdgcn_global_load_lds(reinterpret_cast<GlobalPointer>(reinterpret_cast<uintptr_t>(from + offset[q])),
+                                             (LdsPointer)(lds + (q * S::WAVES + wave) * 512), 16, 0, 0);
+    }
+    // 8 values of K of a column a lane: block f of wavefront wj; q: the second 32 rows, or the lower halves
+    static __device__ __forceinline__ Half8 take(const _Float16* lds, int wj, int f, int q) {
+        typedef short Short4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) Short4* Pointer;
+        const int lane = threadIdx.x & 63, col = wj * S::FJ * 16 + (lane & 3) * 4 * S::GJ + f * 4;
+        const int in = TERMS == 1 ? col : col / 32 * 64 + col % 32 + q * 32;
+        union {
+            Short4 part[2];
+            Half8 all;
+        } v;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = (TERMS == 1 ? q * 32 : 0) + (lane >> 4) * 8 + h * 4 + (lane >> 2 & 3);
+            v.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Pointer)(lds + row * WIDTH + ((in / 8 ^ order(row)) * 8 + in % 8)));
+        }
+        return v.all;
+    }
+};
 // All but `left` of this wavefront's loads have arrived and its reads of LDS are done; then so are all wavefronts'.
 template <int LEFT>
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
 
-// N neighbouring parameters from column `col` of a row on: p = keep p - lr x (keep 0: x itself)
+// p = keep p - lr x, or x itself
 struct Update {
     float lr, keep;
     bool optimizer;
@@ -406,31 +446,73 @@ __device__ __forceinline__ Update update_of(const Last& k, const Matrix& t) {
             : k.scale_rule == CS_MUON_SCALE_RMS ? 0.2f * sqrtf(static_cast<float>(max(t.rows, t.cols))) : 1.f;
     return u;
 }
+// N neighbouring parameters from column `col` of a row on: as they are (or 0), and written
+template <int N>
+__device__ __forceinline__ void read_p(const Matrix& t, int p_fmt, int32_t row, int32_t col, float (&v)[N]) {
+    if (row < t.rows && col < t.cols) {
+        read_row<N>(t.p, p_fmt, row * t.p_stride, col, t.cols, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = 0.f;
+    }
+}
 template <typename T, int N>
-__device__ __forceinline__ void update_as(const Matrix& t, const Update& u, int64_t row, int64_t col, const float (&x)[N]) {
-    if (row >= t.rows || col >= t.cols) return;
+__device__ __forceinline__ void write_as(const Matrix& t, int32_t row, int32_t col, const float (&v)[N]) {
     T* const p = static_cast<T*>(t.p) + row * t.p_stride + col;
     if (col + N <= t.cols) {
         constexpr int P = N < kPack<T> ? N : kPack<T>;
 #pragma unroll
         for (int e = 0; e < N; e += P) {
-            float v[P];
-            if (u.optimizer) load_pack<T, P>(p + e, v);
+            float part[P];
 #pragma unroll
-            for (int k = 0; k < P; ++k) v[k] = u.optimizer ? fmaf(v[k], u.keep, -u.lr * x[e + k]) : x[e + k];
-            store_pack<false>(p + e, v);
+            for (int k = 0; k < P; ++k) part[k] = v[e + k];
+            store_pack<false>(p + e, part);
         }
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            if (col + e < t.cols) p[e] = static_cast<T>(u.optimizer ? fmaf(static_cast<float>(p[e]), u.keep, -u.lr * x[e]) : x[e]);
+            if (col + e < t.cols) p[e] = static_cast<T>(v[e]);
     }
 }
 template <int N>
-__device__ __forceinline__ void update(const Matrix& t, int p_fmt, const Update& u, int64_t row, int64_t col, const float (&x)[N]) {
-    if (p_fmt == CS_FMT_F32) update_as<float>(t, u, row, col, x);
-    else if (p_fmt == CS_FMT_BF16) update_as<bf16>(t, u, row, col, x);
-    else update_as<f16>(t, u, row, col, x);
+__device__ __forceinline__ void write_p(const Matrix& t, int p_fmt, int32_t row, int32_t col, const float (&v)[N]) {
+    if (row >= t.rows || col >= t.cols) return;
+    if (p_fmt == CS_FMT_F32) write_as<float>(t, row, col, v);
+    else if (p_fmt == CS_FMT_BF16) write_as<bf16>(t, row, col, v);
+    else write_as<f16>(t, row, col, v);
+}
+// A lane's H rows of W columns of X into the parameters (of a tall matrix into its transpose), which are all asked for first.
+template <int H, int W>
+__device__ __forceinline__ void finish(const Matrix& t, int p_fmt, const Update& u, int32_t row, int32_t col, const float (&x)[H][W]) {
+    float old[H][W];
+    if (t.rows > t.cols) {
+        if (u.optimizer)
+#pragma unroll
+            for (int e = 0; e < W; ++e) {
+                float v[H];
+                read_p(t, p_fmt, col + e, row, v);
+#pragma unroll
+                for (int f = 0; f < H; ++f) old[f][e] = v[f];
+            }
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+            float v[H];
+#pragma unroll
+            for (int f = 0; f < H; ++f) v[f] = u.optimizer ? fmaf(old[f][e], u.keep, -u.lr * x[f][e]) : x[f][e];
+            write_p(t, p_fmt, col + e, row, v);
+        }
+    } else {
+        if (u.optimizer)
+#pragma unroll
+            for (int f = 0; f < H; ++f) read_p(t, p_fmt, row + f, col, old[f]);
+#pragma unroll
+        for (int f = 0; f < H; ++f) {
+            float v[W];
+#pragma unroll
+            for (int e = 0; e < W; ++e) v[e] = u.optimizer ? fmaf(old[f][e], u.keep, -u.lr * x[f][e]) : x[f][e];
+            write_p(t, p_fmt, row + f, col, v);
+        }
+    }
 }
 
 // Workgroups of a launch go round the 8 dies: each die gets neighbouring places, whose tiles read the same rows.
@@ -442,64 +524,109 @@ __device__ __forceinline__ int place_of_block() {
 template <typename S, int TERMS, int MODE>
 __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(List list, Product k, char* ws) {
     constexpr bool HALF = MODE == kGram || MODE == kSquare;
-    constexpr int N = 4 * S::GJ, PART = (S::TI + S::TJ) * S::DEPTH, Q = S::DEPTH / 32;
-    static_assert(TERMS == 1 || Q == 2, "a row in LDS has both terms");
+    constexpr int N = 4 * S::GJ, PART = (S::TI + S::TJ) * S::DEPTH;
     __shared__ __align__(1024) _Float16 lds[S::STAGES * PART];
     const Tile t = (HALF ? list.halves : list.fulls)[place_of_block()];
     const Work<TERMS> w(ws, t.at, t.np, t.mp);
     const int32_t depth = (MODE == kGram ? t.mp : t.np) * TERMS, all = depth / S::DEPTH;
     const Stage<S, true> l_stage(depth * 2);
-    const Stage<S, false> r_stage(depth * 2);
-    const char* const left = reinterpret_cast<const char*>((MODE == kGram ? w.x() : MODE == kSquare ? w.a() : w.b()) +
+    const char* const left = reinterpret_cast<const char*>((MODE == kGram ? w.x(k.turn) : MODE == kSquare ? w.a() : w.b()) +
                                                            static_cast<int64_t>(t.ti) * S::TI * depth);
-    const char* const right = reinterpret_cast<const char*>((MODE == kGram ? w.x() : MODE == kSquare ? w.a() : w.xt(k.turn)) +
-                                                            static_cast<int64_t>(t.tj) * S::TJ * depth);
+    using Right = typename std::conditional<HALF, Stage<S, false>, Columns<S, TERMS>>::type;
+    const Right r_stage(HALF ? depth * 2 : t.mp * TERMS * 2);
+    const char* const right = reinterpret_cast<const char*>(
+        HALF ? (MODE == kGram ? w.x(k.turn) : w.a()) + static_cast<int64_t>(t.tj) * S::TJ * depth : w.x(k.turn) + t.tj * S::TJ * TERMS);
+    const int64_t r_step = HALF ? S::DEPTH * 2 : static_cast<int64_t>(t.mp) * (S::DEPTH * 2);
     const auto load = [&](int32_t i, int turn) {
         l_stage.load(left + i * (S::DEPTH * 2), lds + turn * PART);
-        r_stage.load(right + i * (S::DEPTH * 2), lds + turn * PART + S::TI * S::DEPTH);
+        r_stage.load(right + i * r_step, lds + turn * PART + S::TI * S::DEPTH);
     };
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave / S::WJ, wj = wave % S::WJ;
     Float4 acc[S::FI][S::FJ] = {};
-    const auto multiply = [&](int turn) {
-        const _Float16* const l = lds + turn * PART + (wi * S::FI * 16 + (lane & 15)) * S::DEPTH;
-        const _Float16* const r = lds + turn * PART + (S::TI + wj * S::FJ * 16 + (lane & 15)) * S::DEPTH;
-        Half8 lv[Q][S::FI], rv[Q][S::FJ];
+    // what 32 values of K take: of a part in LDS the first and the second 32 of one term, or both terms' 32
+    struct Operands {
+        Half8 l[S::FI], r[S::FJ];
+    };
+    const int l_from = (wi * S::FI * 16 + (lane & 15)) * S::DEPTH, r_from = (S::TI + wj * S::FJ * 16 + (lane & 15)) * S::DEPTH;
+    const auto take = [&](Operands& v, int turn, int q) {
+        const _Float16* const part = lds + turn * PART + ((((lane >> 4) + 4 * q) ^ S::order(lane & 15)) * 8);
 #pragma unroll
-        for (int q = 0; q < Q; ++q) {
-            const int pack = (((lane >> 4) + 4 * q) ^ S::order(lane & 15)) * 8;
+        for (int f = 0; f < S::FI; ++f) v.l[f] = *reinterpret_cast<const Half8*>(part + l_from + f * 16 * S::DEPTH);
 #pragma unroll
-            for (int f = 0; f < S::FI; ++f) lv[q][f] = *reinterpret_cast<const Half8*>(l + f * 16 * S::DEPTH + pack);
-#pragma unroll
-            for (int f = 0; f < S::FJ; ++f) rv[q][f] = *reinterpret_cast<const Half8*>(r + f * 16 * S::DEPTH + pack);
-        }
-        const auto add = [&](int ql, int qr) {
-#pragma unroll
-            for (int fi = 0; fi < S::FI; ++fi)
-#pragma unroll
-                for (int fj = 0; fj < S::FJ; ++fj)
-                    acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rv[qr][fj], lv[ql][fi], acc[fi][fj], 0, 0, 0);
-        };
-        add(0, 0);
-        if (TERMS == 2) {
-            add(0, Q - 1);
-            add(Q - 1, 0);
-        } else if (Q == 2) {
-            add(Q - 1, Q - 1);
+        for (int f = 0; f < S::FJ; ++f) {
+            if constexpr (HALF) v.r[f] = *reinterpret_cast<const Half8*>(part + r_from + f * 16 * S::DEPTH);
+            else v.r[f] = Right::take(lds + turn * PART + S::TI * S::DEPTH, wj, f, q);
         }
     };
-    int turn = 0, next = S::STAGES - 1;
+    const auto add = [&](const Half8(&l)[S::FI], const Half8(&r)[S::FJ]) {
+#pragma unroll
+        for (int fi = 0; fi < S::FI; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < S::FJ; ++fj) acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[fj], l[fi], acc[fi][fj], 0, 0, 0);
+    };
+    const auto add_second = [&](const Operands& first, const Operands& second) {
+        if (TERMS == 2) {
+            add(first.l, second.r);
+            add(second.l, first.r);
+        } else {
+            add(second.l, second.r);
+        }
+    };
 #pragma unroll
     for (int i = 0; i < S::STAGES - 1; ++i)
         if (i < all) load(i, i);
-    for (int32_t i = 0; i + 1 < all; ++i) {
-        if (i + S::STAGES - 1 <= all) arrived<(S::STAGES - 2) * S::LOADS>();
+    Operands first, second;
+    if constexpr (S::AHEAD) {
+        // Operands are read from LDS while products are taken of those before: the second half of a part's with its first half's, and the next part's
+        // first half, which has arrived by then, with the second half's.
+        static_assert(!S::AHEAD || S::STAGES == 2, "a part has the step before to arrive in");
+        if (all > 1) load(1, 1);
+        if (all > 1) arrived<S::LOADS>();
         else arrived<0>();
-        if (i + S::STAGES - 1 < all) load(i + S::STAGES - 1, next);
-        next = next + 1 == S::STAGES ? 0 : next + 1;
-        multiply(turn);
-        turn = turn + 1 == S::STAGES ? 0 : turn + 1;
+        take(first, 0, 0);
+        const auto step = [&](int32_t i, int turn, Operands& v, Operands& next) {
+            take(second, turn, 1);
+            add(v.l, v.r);
+            arrived<0>();
+            if (i + 2 < all) load(i + 2, turn);
+            take(next, turn ^ 1, 0);
+            add_second(v, second);
+        };
+        int32_t i = 0;
+        if constexpr (TERMS == 2) {                      // (an even number of parts)
+            Operands other;
+            for (; i + 2 < all; i += 2) {
+                step(i, 0, first, other);
+                step(i + 1, 1, other, first);
+            }
+            step(i, 0, first, other);
+            first = other;
+            ++i;
+        } else {
+            for (; i + 1 < all; ++i) {
+                Operands other;
+                step(i, i & 1, first, other);
+                first = other;
+            }
+        }
+        take(second, i & 1, 1);
+    } else {
+        int turn = 0, next = S::STAGES - 1;
+        for (int32_t i = 0; i + 1 < all; ++i) {
+            if (i + S::STAGES - 1 <= all) arrived<(S::STAGES - 2) * S::LOADS>();
+            else arrived<0>();
+            if (i + S::STAGES - 1 < all) load(i + S::STAGES - 1, next);
+            next = next + 1 == S::STAGES ? 0 : next + 1;
+            take(first, turn, 0);
+            take(second, turn, 1);
+            add(first.l, first.r);
+            add_second(first, second);
+            turn = turn + 1 == S::STAGES ? 0 : turn + 1;
+        }
+        arrived<0>();
+        take(first, turn, 0);
+        take(second, turn, 1);
     }
-    arrived<0>();
     // What the last part of the output needs of A0 or X is on its way while the last products are taken (of a tile of 256 half of it, which
     // is what the registers have room for).
     constexpr bool READS = MODE != kGram, LOW = READS && (TERMS == 2 || !HALF);
@@ -511,17 +638,18 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
         if constexpr (READS) {
 #pragma unroll
             for (int f = 0; f < S::GI; ++f) {
-                const _Float16* const from = (HALF ? w.a() : w.x()) + Work<TERMS>::place(row_of(gi + f), col, wide);
+                const int64_t from = Work<TERMS>::place(row_of(gi + f), col, wide);
 #pragma unroll
                 for (int e = 0; e < N / 8; ++e) {
-                    hi[f][e] = *reinterpret_cast<const Half8*>(from + 8 * e);
-                    if constexpr (LOW) lo[f][e] = *reinterpret_cast<const Half8*>(from + w.to_low() + 8 * e);
+                    hi[f][e] = *reinterpret_cast<const Half8*>((HALF ? w.a() : w.x(k.turn)) + from + 8 * e);
+                    if constexpr (LOW) lo[f][e] = *reinterpret_cast<const Half8*>((HALF ? w.a() + 32 : w.x_low(k.turn)) + from + 8 * e);
                 }
             }
         }
     };
     fetch(0);
-    multiply(turn);
+    add(first.l, first.r);
+    add_second(first, second);
 
     Update u = {};
     Matrix matrix;
@@ -530,7 +658,6 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
         matrix = list.matrices[t.matrix];
         u = update_of(k.last, matrix);
     }
-    const bool tall = MODE == kFinish && matrix.rows > matrix.cols;
     float dj[N];
     if constexpr (MODE == kSquare) {
 #pragma unroll
@@ -570,9 +697,8 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
             if constexpr (MODE == kFinish) {
 #pragma unroll
                 for (int e = 0; e < N; ++e) v[e] *= kDown;
-                if (!tall) update(matrix, k.last.p_fmt, u, row, col, v);
             } else {
-                _Float16* const to = (MODE == kGram ? w.a() : MODE == kSquare ? w.b() : w.x()) + Work<TERMS>::place(row, col, wide);
+                const int64_t to = Work<TERMS>::place(row, col, wide);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     hi[f][e / 8][e % 8] = static_cast<_Float16>(v[e]);
@@ -580,30 +706,24 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
                 }
 #pragma unroll
                 for (int e = 0; e < N / 8; ++e) {
-                    *reinterpret_cast<Half8*>(to + 8 * e) = hi[f][e];
-                    if (TERMS == 2 || MODE == kApply) *reinterpret_cast<Half8*>(to + w.to_low() + 8 * e) = lo[f][e];
+                    *reinterpret_cast<Half8*>((MODE == kGram ? w.a() : MODE == kSquare ? w.b() : w.x(1 - k.turn)) + to + 8 * e) = hi[f][e];
+                    if (TERMS == 2 || MODE == kApply)
+                        *reinterpret_cast<Half8*>((MODE == kGram ? w.a() + 32 : MODE == kSquare ? w.b() + 32 : w.x_low(1 - k.turn)) + to + 8 * e) = lo[f][e];
                 }
             }
         }
-        // the transpose: of A and B the tile on the other side, of X the one that the next product reads
-        if (HALF ? t.ti == t.tj : MODE == kFinish && !tall) continue;
+        if constexpr (MODE == kFinish) finish(matrix, k.last.p_fmt, u, row_of(gi), col, out);
+        // the tile on the other side of A and B
+        if (!HALF || t.ti == t.tj) continue;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            if constexpr (MODE == kFinish) {
-                float turned[S::GI];
+            typedef _Float16 Halves __attribute__((ext_vector_type(S::GI)));
+            Halves h, l;
 #pragma unroll
-                for (int f = 0; f < S::GI; ++f) turned[f] = out[f][e];
-                update(matrix, k.last.p_fmt, u, col + e, row_of(gi), turned);
-            } else {
-                typedef _Float16 Halves __attribute__((ext_vector_type(S::GI)));
-                Halves h, l;
-#pragma unroll
-                for (int f = 0; f < S::GI; ++f) h[f] = hi[f][e / 8][e % 8], l[f] = lo[f][e / 8][e % 8];
-                _Float16* const to = (MODE == kGram ? w.a() : MODE == kSquare ? w.b() : w.xt(1 - k.turn)) +
-                                     Work<TERMS>::place(col + e, row_of(gi), t.np);
-                *reinterpret_cast<Halves*>(to) = h;
-                if (TERMS == 2) *reinterpret_cast<Halves*>(to + 32) = l;
-            }
+            for (int f = 0; f < S::GI; ++f) h[f] = hi[f][e / 8][e % 8], l[f] = lo[f][e / 8][e % 8];
+            _Float16* const to = (MODE == kGram ? w.a() : w.b()) + Work<TERMS>::place(col + e, row_of(gi), t.np);
+            *reinterpret_cast<Halves*>(to) = h;
+            if (TERMS == 2) *reinterpret_cast<Halves*>(to + 32) = l;
         }
     }
 }
@@ -766,16 +886,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_muon_little(List list, Moment m
     for (int f = 0; f < 2; ++f)
 #pragma unroll
         for (int e = 0; e < W; ++e) x[f][e] *= kDown;
-    if (tall) {
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            const float pair[2] = {x[0][e], x[1][e]};
-            update(t, last.p_fmt, u, col + e, row, pair);
-        }
-    } else {
-#pragma unroll
-        for (int f = 0; f < 2; ++f) update(t, last.p_fmt, u, row + f, col, x[f]);
-    }
+    finish(t, last.p_fmt, u, row, col, x);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -786,7 +897,7 @@ constexpr int64_t kMaxSide = 1 << 20, kMaxShort = 1 << 15, kMaxMatrices = 1 << 2
 struct Plan {
     int64_t matrices, littles, pieces, halves, fulls, work;      // work: bytes of all matrices
     double half_steps, full_steps;                               // parts of 64 values of K, of all tiles together
-    int half_tile, full_tile;
+    int half_tile, full_high, full_wide;
 };
 int64_t up_to(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
 
@@ -800,10 +911,10 @@ bool little(const cs_matrix& s) { return (s.rows <= 64 || s.cols <= 64) && s.row
 
 // Counts and sizes with these tiles; `each` is told of every stack that has tiles.
 template <typename F>
-bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int full_tile, Plan& plan, F each) {
+bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int full_high, int full_wide, Plan& plan, F each) {
     plan = Plan{};
-    plan.half_tile = half_tile, plan.full_tile = full_tile;
-    const int64_t tile = half_tile > full_tile ? half_tile : full_tile;
+    plan.half_tile = half_tile, plan.full_high = full_high, plan.full_wide = full_wide;
+    const int64_t tile = half_tile > full_high ? half_tile : full_high;
     for (int32_t i = 0; i < n; ++i) {
         const cs_matrix& s = stacks[i];
         if (!stack_ok(s)) return false;
@@ -814,9 +925,9 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int
             plan.littles += s.count;
             continue;
         }
-        const int64_t np = up_to(s.rows < s.cols ? s.rows : s.cols, tile), mp = up_to(s.rows < s.cols ? s.cols : s.rows, tile);
+        const int64_t np = up_to(s.rows < s.cols ? s.rows : s.cols, tile), mp = up_to(s.rows < s.cols ? s.cols : s.rows, full_wide);
         const int64_t down = np / half_tile, pieces = (np / kEdge) * (mp / kEdge), halves = down * (down + 1) / 2;
-        const int64_t fulls = (np / full_tile) * (mp / full_tile);
+        const int64_t fulls = (np / full_high) * (mp / full_wide);
         each(s, np, mp, plan, pieces, halves, fulls);
         plan.pieces += s.count * pieces;
         plan.halves += s.count * halves;
@@ -828,26 +939,26 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int
     }
     return true;
 }
-// How long tiles take that are spread over 256 CUs, in parts of 64 values of K of one tile (us; of 64 three are on a CU at a time, of 128 two,
-// of 256 one, and fewer take less each).  4096 x 4096, one term, X by tiles of 64 / 128 / 256: 207 / 148 / 134 us; 48 x 512 x 512
-// 34 / 32 / 39, their A 17 / 15 / 23; 12 matrices of 2048 x 512, A 15 / 23 / 53, X 35 / 32 / 38; 8 of 1024 x 4096, X 170 / 135 / 125.
-double rounds(int64_t tiles, int tile) {
-    const int64_t at_once = tile == 64 ? 768 : tile == 128 ? 512 : 256, left = tiles % at_once;
-    const double full = tile == 64 ? 0.6 : tile == 128 ? 1.15 : 2.1;
-    const double rest = left == 0 ? 0. : left > at_once - 256 ? full : tile == 128 ? 0.6 : left > 256 ? 0.45 : 0.3;
+// How long tiles take that are spread over 256 CUs, in parts of 64 values of K of one tile (us; of 64 x 64 and 64 x 128 three are on a CU at a time, of
+// 128 x 128 two, of 256 x 256 one, and fewer take less each).
+double rounds(int64_t tiles, int high, int wide) {
+    const int64_t at_once = high == 64 ? 768 : high == 128 ? 512 : 256, left = tiles % at_once;
+    const double full = high == 64 ? (wide == 64 ? 0.6 : 0.9) : high == 128 ? 1.15 : 1.95;
+    const double rest = left == 0 ? 0. : left > at_once - 256 ? full : high == 128 ? 0.6 : left > 256 ? 0.75 * full : 0.5 * full;
     return static_cast<double>(tiles / at_once) * full + rest;
 }
 bool plan_of(const cs_matrix* stacks, int32_t n, int terms, Plan& plan) {
     const auto none = [](const cs_matrix&, int64_t, int64_t, const Plan&, int64_t, int64_t, int64_t) {};
+    static const int kFullTiles[][2] = {{64, 64}, {64, 128}, {128, 128}, {256, 256}};
     double least = INFINITY;
     bool ok = false;
     for (const int half_tile : {64, 128})
-        for (const int full_tile : {64, 128, 256}) {
+        for (const auto& full : kFullTiles) {
             Plan p;
             // (larger tiles fill up more: they may be too many where smaller ones are not)
-            if (!plan_with(stacks, n, terms, half_tile, full_tile, p, none)) continue;
-            const double us = p.halves ? rounds(p.halves, half_tile) * p.half_steps / static_cast<double>(p.halves) +
-                                             rounds(p.fulls, full_tile) * p.full_steps / static_cast<double>(p.fulls) : 0.;
+            if (!plan_with(stacks, n, terms, half_tile, full[0], full[1], p, none)) continue;
+            const double us = p.halves ? rounds(p.halves, half_tile, half_tile) * p.half_steps / static_cast<double>(p.halves) +
+                                             rounds(p.fulls, full[0], full[1]) * p.full_steps / static_cast<double>(p.fulls) : 0.;
             if (us < least) {
                 least = us;
                 plan = p;
@@ -866,10 +977,10 @@ List list_of(const cs_matrix_list* l) {
     const Tile* at = reinterpret_cast<const Tile*>(t + l->matrices);
     return List{t, at, at + l->halves, reinterpret_cast<const Place*>(at + l->halves + l->fulls)};
 }
-bool tile_ok(int32_t tile) { return tile == 64 || tile == 128 || tile == 256; }
+bool full_ok(int32_t high, int32_t wide) { return (high == 64 && wide == 128) || (high == wide && (high == 64 || high == 128 || high == 256)); }
 bool list_ok(const cs_matrix_list* l) {
     return l && l->littles >= 0 && l->matrices >= l->littles && l->pieces >= 0 && l->halves >= 0 && l->fulls >= 0 && l->work >= 0 &&
-           (l->half_tile == 64 || l->half_tile == 128) && tile_ok(l->full_tile) && (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) &&
+           (l->half_tile == 64 || l->half_tile == 128) && full_ok(l->full_high, l->full_wide) && (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) &&
            fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
 }
 
@@ -899,33 +1010,46 @@ bool hyper_ok(const cs_muon* h) {
            h->scale <= CS_MUON_SCALE_ONE && steps_ok(h);
 }
 
-// A tile's wavefronts by its edge: with four on a SIMD (three of 64) one takes products while another waits; tiles of 128 of two terms have
-// fewer reads of LDS the other way round.
-template <int TILE, int TERMS>
+// A tile's wavefronts, for symmetric products (HALF) and for B X.  Few parts of K are over soon, and more wavefronts a SIMD hide what each
+// waits for; large tiles have registers for two, and read LDS a step ahead instead.  us, symmetric products / B X:
+//   48 of 512 x 512       128 x 128 as 4 x 2 wavefronts 14.5 + 16.0 / 34.7, as 2 x 2 ahead 16.2 + 18.0 / 33.5; 64 x 128 as 2 x 2 / 31.2, as 2 x 4 / 29.6
+//   4096 x 4096           128 x 128 as 4 x 2 wavefronts 100 + 102 / 153, as 2 x 2 ahead 96.6 + 100.4 / 144; 256 x 256 / 144, ahead / 122
+//   12 of 2048 x 512, two terms   128 x 128 as 2 x 4 wavefronts 43.9 + 17.8 / 49.1, ahead 46.6 + 18.4 / 47.2; 64 x 64 31.3 + 12.4 / 60
+template <int HIGH, int WIDE, int TERMS, bool HALF>
 struct ShapeOf;
+template <int TERMS, bool HALF>
+struct ShapeOf<64, 64, TERMS, HALF> : Shape<2, 2, 2, 2, 3, 3, false> {};
 template <int TERMS>
-struct ShapeOf<64, TERMS> : Shape<2, 2, 2, 2, 3, 64, 3> {};
+struct ShapeOf<64, 128, TERMS, false> : Shape<2, 4, 2, 2, 2, 6, false> {};
 template <>
-struct ShapeOf<128, 1> : Shape<4, 2, 2, 4, 2, 64, 4> {};
+struct ShapeOf<128, 128, 1, true> : Shape<4, 2, 2, 4, 2, 4, false> {};
 template <>
-struct ShapeOf<128, 2> : Shape<2, 4, 4, 2, 2, 64, 4> {};
+struct ShapeOf<128, 128, 1, false> : Shape<2, 2, 4, 4, 2, 2, true> {};
+template <>
+struct ShapeOf<128, 128, 2, true> : Shape<2, 4, 4, 2, 2, 4, false> {};
+template <>
+struct ShapeOf<128, 128, 2, false> : Shape<2, 4, 4, 2, 2, 4, true> {};
 template <int TERMS>
-struct ShapeOf<256, TERMS> : Shape<2, 4, 8, 4, 2, 64, 2> {};
+struct ShapeOf<256, 256, TERMS, false> : Shape<2, 4, 8, 4, 2, 2, TERMS == 1> {};
 
-template <int TERMS, int MODE, int TILE>
+template <int TERMS, int MODE, int HIGH, int WIDE>
 int product_as(const cs_matrix_list* l, const Product& k, char* ws, hipStream_t s) {
-    const int64_t places = MODE == kGram || MODE == kSquare ? l->halves : l->fulls;
-    using S = ShapeOf<TILE, TERMS>;
+    constexpr bool HALF = MODE == kGram || MODE == kSquare;
+    using S = ShapeOf<HIGH, WIDE, TERMS, HALF>;
+    static_assert(S::TI == HIGH && S::TJ == WIDE, "");
+    const int64_t places = HALF ? l->halves : l->fulls;
     k_muon_product<S, TERMS, MODE><<<static_cast<unsigned>(places), S::THREADS, 0, s>>>(list_of(l), k, ws);
     return launched();
 }
 template <int TERMS, int MODE>
 int product(const cs_matrix_list* l, const Product& k, char* ws, hipStream_t s) {
-    const int tile = MODE == kGram || MODE == kSquare ? l->half_tile : l->full_tile;
-    if (tile == 64) return product_as<TERMS, MODE, 64>(l, k, ws, s);
-    if constexpr (MODE == kApply || MODE == kFinish)
-        if (tile == 256) return product_as<TERMS, MODE, 256>(l, k, ws, s);
-    return product_as<TERMS, MODE, 128>(l, k, ws, s);
+    if constexpr (MODE == kGram || MODE == kSquare) {
+        return l->half_tile == 64 ? product_as<TERMS, MODE, 64, 64>(l, k, ws, s) : product_as<TERMS, MODE, 128, 128>(l, k, ws, s);
+    } else {
+        if (l->full_high == 256) return product_as<TERMS, MODE, 256, 256>(l, k, ws, s);
+        if (l->full_high == 128) return product_as<TERMS, MODE, 128, 128>(l, k, ws, s);
+        return l->full_wide == 128 ? product_as<TERMS, MODE, 64, 128>(l, k, ws, s) : product_as<TERMS, MODE, 64, 64>(l, k, ws, s);
+    }
 }
 
 // Pieces of a matrix up to which every workgroup that begins X sums their squares by itself, in place of a launch that does (4096 x 4096,
@@ -1030,7 +1154,7 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
             if (side > little_cols) little_cols = side;
         }
     *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.pieces, plan.halves, plan.fulls, plan.work, p_fmt, g_fmt, terms, moments == 1,
-                           plan.half_tile, plan.full_tile, static_cast<int32_t>(little_cols), 0};
+                           plan.half_tile, plan.full_high, plan.full_wide, static_cast<int32_t>(little_cols)};
     if (plan.matrices == 0) return CS_OK;
     Matrix* const matrices = static_cast<Matrix*>(memory);
     const hipStream_t st = stream_of(stream);
@@ -1059,7 +1183,7 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
         if (there(stacks[i]) && little(stacks[i]))
             for (int64_t k = 0; k < stacks[i].count; ++k) take(stacks[i], k, Matrix{});
     Plan again;
-    plan_with(stacks, count, terms, plan.half_tile, plan.full_tile, again,
+    plan_with(stacks, count, terms, plan.half_tile, plan.full_high, plan.full_wide, again,
               [&](const cs_matrix& s, int64_t np, int64_t mp, const Plan& at, int64_t pieces, int64_t halves, int64_t fulls) {
         for (int64_t k = 0; k < s.count; ++k) {
             Matrix t = {};
@@ -1077,9 +1201,9 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
     const auto grid = [](int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); };
     const int first = static_cast<int>(plan.littles), n = static_cast<int>(plan.matrices);
     if (first == n) return CS_OK;
-    k_list_places<kHalves><<<grid(plan.halves), kThreads, 0, st>>>(matrices, first, n, plan.half_tile, halves, plan.halves);
-    k_list_places<kFulls><<<grid(plan.fulls), kThreads, 0, st>>>(matrices, first, n, plan.full_tile, fulls, plan.fulls);
-    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, reinterpret_cast<Place*>(fulls + plan.fulls), plan.pieces);
+    k_list_places<kHalves><<<grid(plan.halves), kThreads, 0, st>>>(matrices, first, n, plan.half_tile, plan.half_tile, halves, plan.halves);
+    k_list_places<kFulls><<<grid(plan.fulls), kThreads, 0, st>>>(matrices, first, n, plan.full_high, plan.full_wide, fulls, plan.fulls);
+    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, kEdge, reinterpret_cast<Place*>(fulls + plan.fulls), plan.pieces);
     if (int e = launched()) return e;
     return CS_OK;
 }
