@@ -100,7 +100,7 @@ def check(t, kind, beta, smoothing=0.0, margin=0.0, mean=False):
 LENGTHS = {"one": [1, 1], "none": [0, 0], "one empty": [0, 5], "few": [3, 70, 1, 65, 64, 63], "some empty": [0, 9, 0, 300, 0, 0, 7, 0],
            "uneven": [5000, 1, 2, 4097, 1, 3], "long": [70_001, 40_000], "many": [(7 * i) % 41 for i in range(1200)],
            "a long one among many": [20] * 300 + [30_000] + [15] * 299, "of one token": [1] * 9000, "hardly any": [0] * 5000 + [1] + [0] * 4000 + [2] * 3 + [0] * 2,
-           "whole pieces": [2048, 2048, 4096, 2048], "next to whole pieces": [2047, 1, 2049, 4095, 2, 2046]}
+           "whole pieces": [2048, 2048, 4096, 2048], "32 pairs": [(37 * i) % 250 for i in range(64)], "33 pairs": [(37 * i) % 250 for i in range(66)], "next to whole pieces": [2047, 1, 2049, 4095, 2, 2046]}
 
 
 @pytest.mark.parametrize("lengths", list(LENGTHS))
