@@ -145,14 +145,15 @@ __device__ __forceinline__ bool skipped(const float* grad_scale) { return grad_s
 // N neighbouring values of a row from column `col` on, 0 from column `cols` on
 template <typename T, int N>
 __device__ __forceinline__ void read_as(const T* row, int32_t col, int32_t cols, float (&v)[N]) {
-    if (col + N <= cols) {
-        constexpr int P = N < kPack<T> ? N : kPack<T>;
+    if (N > 1 && col + N <= cols) {
+        constexpr int P = N < 2 ? 2 : N < kPack<T> ? N : kPack<T>;
 #pragma unroll
         for (int e = 0; e < N; e += P) {
             float part[P];
             load_pack<T, P>(row + col + e, part);
 #pragma unroll
-            for (int k = 0; k < P; ++k) v[e + k] = part[k];
+            for (int k = 0; k < P; ++k)
+                if (e + k < N) v[e + k] = part[k];
         }
     } else {
 #pragma unroll
@@ -190,7 +191,7 @@ __device__ __forceinline__ void direction(const Matrix& t, const Moment& k, floa
         u[e] = k.nesterov ? fmaf(k.mu, m[e], s * u[e]) : m[e];
     }
     if (!STEP) return;
-    if (col + N <= t.cols) {
+    if (N > 1 && col + N <= t.cols) {
         store_pack<false>(at + col, m);
     } else {
 #pragma unroll
@@ -459,13 +460,13 @@ __device__ __forceinline__ void read_p(const Matrix& t, int p_fmt, int32_t row, 
 template <typename T, int N>
 __device__ __forceinline__ void write_as(const Matrix& t, int32_t row, int32_t col, const float (&v)[N]) {
     T* const p = static_cast<T*>(t.p) + row * t.p_stride + col;
-    if (col + N <= t.cols) {
-        constexpr int P = N < kPack<T> ? N : kPack<T>;
+    if (N > 1 && col + N <= t.cols) {
+        constexpr int P = N < 2 ? 2 : N < kPack<T> ? N : kPack<T>;
 #pragma unroll
         for (int e = 0; e < N; e += P) {
             float part[P];
 #pragma unroll
-            for (int k = 0; k < P; ++k) part[k] = v[e + k];
+            for (int k = 0; k < P; ++k) part[k] = v[e + k < N ? e + k : 0];
             store_pack<false>(p + e, part);
         }
     } else {
@@ -728,165 +729,167 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
     }
 }
 
-// A small matrix (n <= 64, m <= M) a workgroup, in one launch: X in binary32 in registers, what the products read in LDS.
+// A small matrix (n <= 64, m <= M) a workgroup, in one launch: X in binary32 in registers, what the products read in LDS.  16 wavefronts, a block
+// of 16 x 16 of A and M / 64 of X each: five steps are a chain of fifteen products and barriers (64 x 64, two terms: 2.3 us a step and
+// 4 us besides, 15.9 in all, with four wavefronts of 2 x 2 blocks 17.2; one term 11.0; by the other launches 70).
+constexpr int kLittleThreads = 1024;
 template <int M, int TERMS>
 struct Little {
-    static constexpr int N = 64, FJ = M / 32, WIDE = M + 8, HIGH = N + 8;        // (rows 16 bytes further: 16 of them meet all banks)
-    static constexpr int X = N * WIDE, XT = M * HIGH, A = N * HIGH;
-    static constexpr int HALVES = TERMS * (X + XT + 2 * A) + 2 * 2 * N;
+    static constexpr int N = 64, F = M / 64, WIDE = M + 8, HIGH = N + 8;     // (rows 16 bytes further: 16 of them meet all banks)
+    static constexpr int X = N * WIDE, A = N * HIGH;
+    static constexpr int HALVES = TERMS * (X + 2 * A) + 2 * 2 * N;
 };
+typedef _Float16 Half4 __attribute__((ext_vector_type(4)));
 template <int M, int TERMS>
-__global__ void __launch_bounds__(kThreads, 1) k_muon_little(List list, Moment moment, double eps, Steps steps, Last last) {
+__global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Moment moment, double eps, Steps steps, Last last) {
     using L = Little<M, TERMS>;
-    constexpr int FJ = L::FJ, W = 4 * FJ;    // a lane has 2 rows of W neighbouring columns of X, and of 8 of A
+    constexpr int F = L::F;                  // a lane has a row of 4 F columns of X (4 each of F blocks) and 4 of A
     __shared__ __align__(16) _Float16 lds[L::HALVES];
-    __shared__ double buf[kThreads / 64];
-    _Float16 *const x_at = lds, *const xt_at = x_at + TERMS * L::X, *const a_at = xt_at + TERMS * L::XT, *const b_at = a_at + TERMS * L::A;
+    __shared__ double buf[kLittleThreads / 64];
+    _Float16 *const x_at = lds, *const a_at = x_at + TERMS * L::X, *const b_at = a_at + TERMS * L::A;
     float *const da = reinterpret_cast<float*>(b_at + TERMS * L::A), *const db = da + L::N;
     if (skipped(last.grad_scale)) return;
     const Matrix t = list.matrices[blockIdx.x];
     const bool tall = t.rows > t.cols;
     const float s = moment.grad_scale ? *moment.grad_scale : 1.f;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 1, wj = wave & 1;
-    const int row = wi * 32 + (lane & 15) * 2, col = wj * (M / 2) + (lane >> 4) * W, a_col = wj * 32 + (lane >> 4) * 8;
-    float x[2][W];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 2, wj = wave & 3;
+    const int row = wi * 16 + (lane & 15), col = wj * (M / 4) + (lane >> 4) * 4, a_col = wj * 16 + (lane >> 4) * 4;
+    float x[F][4];
     double sum = 0.;
-    if (tall) {
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-            float u[2];
-            direction<true>(t, moment, s, col + e, row, u);
-            x[0][e] = u[0], x[1][e] = u[1];
-        }
-    } else {
+    for (int f = 0; f < F; ++f) {
+        if (tall) {
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int e = 0; e < W; e += 4) {
-                float u[4];
-                direction<true>(t, moment, s, row + f, col + e, u);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[f][e + i] = u[i];
+            for (int e = 0; e < 4; ++e) {
+                float u[1];
+                direction<true>(t, moment, s, col + 16 * f + e, row, u);
+                x[f][e] = u[0];
             }
+        } else {
+            direction<true>(t, moment, s, row, col + 16 * f, x[f]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum = fma(static_cast<double>(x[f][e]), static_cast<double>(x[f][e]), sum);
     }
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) buf[wave] = sum;
+    __syncthreads();
+    sum = buf[lane & 15];
 #pragma unroll
-        for (int e = 0; e < W; ++e) sum = fma(static_cast<double>(x[f][e]), static_cast<double>(x[f][e]), sum);
-    const double one = inverse_of(workgroup_sum(sum, buf), eps) * static_cast<double>(kUp);
+    for (int d = 8; d; d >>= 1) sum += __shfl_xor(sum, d);
+    const double one = inverse_of(sum, eps) * static_cast<double>(kUp);
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int f = 0; f < F; ++f)
 #pragma unroll
-        for (int e = 0; e < W; ++e) x[f][e] = static_cast<float>(x[f][e] * one);
+        for (int e = 0; e < 4; ++e) x[f][e] = static_cast<float>(x[f][e] * one);
 
-    // rows row, row + 1 of C columns from c on into an array of rows `step` apart, and into its transpose
-    const auto keep = [&](auto& v, _Float16* at, int step, int size, int c, _Float16* turned, int high, int turned_size) {
-        constexpr int C = sizeof(v[0]) / 4;
-        Half8 h[TERMS][2][C / 8];
+    // four neighbouring values, and their lower halves
+    const auto keep = [&](const float(&v)[4], _Float16* at, int size) {
+        Half4 h, l;
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
+        for (int e = 0; e < 4; ++e) {
+            _Float16 hi, lo;
+            split(v[e], hi, lo);
+            h[e] = hi, l[e] = lo;
+        }
+        *reinterpret_cast<Half4*>(at) = h;
+        if (TERMS == 2) *reinterpret_cast<Half4*>(at + size) = l;
+    };
+    // 8 values of K of a row a lane
+    const auto rows = [&](Half8(&v)[TERMS], const _Float16* at, int step, int size, int first, int q) {
 #pragma unroll
-            for (int e = 0; e < C; ++e) {
-                _Float16 hi, lo;
-                split(v[f][e], hi, lo);
-                h[0][f][e / 8][e % 8] = hi;
-                if (TERMS == 2) h[TERMS - 1][f][e / 8][e % 8] = lo;
-            }
-#pragma unroll
-        for (int low = 0; low < TERMS; ++low) {
-#pragma unroll
-            for (int f = 0; f < 2; ++f)
-#pragma unroll
-                for (int e = 0; e < C / 8; ++e) *reinterpret_cast<Half8*>(at + low * size + (row + f) * step + c + 8 * e) = h[low][f][e];
-            if (!turned) continue;
-#pragma unroll
-            for (int e = 0; e < C; ++e) {
-                typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
-                *reinterpret_cast<Half2*>(turned + low * turned_size + (c + e) * high + row) = Half2{h[low][0][e / 8][e % 8], h[low][1][e / 8][e % 8]};
-            }
+        for (int low = 0; low < TERMS; ++low)
+            v[low] = *reinterpret_cast<const Half8*>(at + low * size + (first + (lane & 15)) * step + (lane >> 4) * 8 + q);
+    };
+    const auto add = [&](Float4& acc, const Half8(&l)[TERMS], const Half8(&r)[TERMS]) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0], l[0], acc, 0, 0, 0);
+        if (TERMS == 2) {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[TERMS - 1], l[0], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0], l[TERMS - 1], acc, 0, 0, 0);
         }
     };
-    // acc = L R^T: this wavefront's 32 rows of L and 16 F rows of R, K values
-    const auto product = [&](auto& acc, const _Float16* l, int l_step, int l_size, const _Float16* r, int r_step, int r_size, int depth) {
-        constexpr int F = sizeof(acc[0]) / sizeof(Float4);
-        const int in = lane & 15;
-        l += (wi * 32 + in * 2) * l_step + (lane >> 4) * 8;
-        r += (wj * 16 * F + in / 4 * 4 * F + in % 4) * r_step + (lane >> 4) * 8;
-#pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int g = 0; g < F; ++g) acc[f][g] = Float4{};
+    // this wavefront's block of L L^T
+    const auto square = [&](const _Float16* at, int step, int size, int depth) {
+        Float4 acc = {};
 #pragma unroll
         for (int q = 0; q < depth; q += 32) {
-            Half8 lv[TERMS][2], rv[TERMS][F];
-#pragma unroll
-            for (int low = 0; low < TERMS; ++low) {
-#pragma unroll
-                for (int f = 0; f < 2; ++f) lv[low][f] = *reinterpret_cast<const Half8*>(l + low * l_size + f * l_step + q);
-#pragma unroll
-                for (int g = 0; g < F; ++g) rv[low][g] = *reinterpret_cast<const Half8*>(r + low * r_size + 4 * g * r_step + q);
-            }
-#pragma unroll
-            for (int part = 0; part < (TERMS == 2 ? 3 : 1); ++part)
-#pragma unroll
-                for (int f = 0; f < 2; ++f)
-#pragma unroll
-                    for (int g = 0; g < F; ++g)
-                        acc[f][g] = __builtin_amdgcn_mfma_f32_16x16x32_f16(rv[part == 1 ? TERMS - 1 : 0][g], lv[part == 2 ? TERMS - 1 : 0][f], acc[f][g], 0, 0, 0);
+            Half8 l[TERMS], r[TERMS];
+            rows(l, at, step, size, wi * 16, q);
+            rows(r, at, step, size, wj * 16, q);
+            add(acc, l, r);
         }
+        return acc;
     };
     for (int i = 0; i < steps.count; ++i) {
         const float a = steps.coefs[i][0], b = steps.coefs[i][1], c = steps.coefs[i][2];
-        keep(x, x_at, L::WIDE, L::X, col, xt_at, L::HIGH, L::XT);
+#pragma unroll
+        for (int f = 0; f < F; ++f) keep(x[f], x_at + row * L::WIDE + col + 16 * f, L::X);
         __syncthreads();
-        Float4 acc[2][2];
-        product(acc, x_at, L::WIDE, L::X, x_at, L::WIDE, L::X, M);
-        float v[2][8];
+        Float4 acc = square(x_at, L::WIDE, L::X, M);
+        float v[4];
 #pragma unroll
-        for (int f = 0; f < 2; ++f)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[f][e] = acc[f][e / 4][e % 4] * kDown;
-                if (row + f == a_col + e) {
-                    da[row + f] = v[f][e] * kDown;
-                    v[f][e] = 0.f;
-                }
-            }
-        keep(v, a_at, L::HIGH, L::A, a_col, static_cast<_Float16*>(nullptr), 0, 0);
-        __syncthreads();
-        product(acc, a_at, L::HIGH, L::A, a_at, L::HIGH, L::A, L::N);
-#pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            const float d = fmaf(c, da[row + f], b);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float dj = da[a_col + e], p = acc[f][e / 4][e % 4];
-                if (row + f == a_col + e) {
-                    db[row + f] = fmaf(d, dj, p * (c * kDown * kDown));
-                    v[f][e] = 0.f;
-                } else {
-                    v[f][e] = fmaf(fmaf(c, dj, d), v[f][e], p * (c * kDown));
-                }
+        for (int e = 0; e < 4; ++e) {
+            v[e] = acc[e] * kDown;
+            if (row == a_col + e) {
+                da[row] = v[e] * kDown;
+                v[e] = 0.f;
             }
         }
-        keep(v, b_at, L::HIGH, L::A, a_col, static_cast<_Float16*>(nullptr), 0, 0);
+        keep(v, a_at + row * L::HIGH + a_col, L::A);
         __syncthreads();
-        Float4 more[2][FJ];
-        product(more, b_at, L::HIGH, L::A, xt_at, L::HIGH, L::XT, L::N);
+        acc = square(a_at, L::HIGH, L::A, L::N);
+        const float d = fmaf(c, da[row], b);
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-            const float d = a + db[row + f];
+        for (int e = 0; e < 4; ++e) {
+            const float dj = da[a_col + e];
+            if (row == a_col + e) {
+                db[row] = fmaf(d, dj, acc[e] * (c * kDown * kDown));
+                v[e] = 0.f;
+            } else {
+                v[e] = fmaf(fmaf(c, dj, d), v[e], acc[e] * (c * kDown));
+            }
+        }
+        keep(v, b_at + row * L::HIGH + a_col, L::A);
+        __syncthreads();
+        const float keeps = a + db[row];
 #pragma unroll
-            for (int e = 0; e < W; ++e) x[f][e] = fmaf(d, x[f][e], more[f][e / 4][e % 4] * kDown);
+        for (int f = 0; f < F; ++f) {
+            acc = Float4{};
+#pragma unroll
+            for (int q = 0; q < L::N; q += 32) {
+                Half8 l[TERMS], r[TERMS];
+                rows(l, b_at, L::HIGH, L::A, wi * 16, q);
+                // columns of X, from its rows
+#pragma unroll
+                for (int low = 0; low < TERMS; ++low) {
+                    typedef short Short4 __attribute__((ext_vector_type(4)));
+                    typedef __attribute__((address_space(3))) Short4* Pointer;
+                    union {
+                        Short4 part[2];
+                        Half8 all;
+                    } of;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        of.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (Pointer)(x_at + low * L::X + (q + (lane >> 4) * 8 + h * 4 + (lane >> 2 & 3)) * L::WIDE + wj * (M / 4) + 16 * f + (lane & 3) * 4));
+                    r[low] = of.all;
+                }
+                add(acc, l, r);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[f][e] = fmaf(keeps, x[f][e], acc[e] * kDown);
         }
         __syncthreads();
     }
     const Update u = update_of(last, t);
 #pragma unroll
-    for (int f = 0; f < 2; ++f)
+    for (int f = 0; f < F; ++f) {
+        float v[1][4];
 #pragma unroll
-        for (int e = 0; e < W; ++e) x[f][e] *= kDown;
-    finish(t, last.p_fmt, u, row, col, x);
+        for (int e = 0; e < 4; ++e) v[0][e] = x[f][e] * kDown;
+        finish(t, last.p_fmt, u, row, col + 16 * f, v);
+    }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -906,7 +909,7 @@ bool stack_ok(const cs_matrix& s) {
            (s.rows < s.cols ? s.rows : s.cols) <= kMaxShort;
 }
 bool there(const cs_matrix& s) { return s.count > 0 && s.rows > 0 && s.cols > 0; }
-// Matrices that a workgroup takes from their moments to their parameters (64 x 64 in 32 bits 14 us, by the other launches 70).
+// Matrices that a workgroup takes from their moments to their parameters.
 bool little(const cs_matrix& s) { return (s.rows <= 64 || s.cols <= 64) && s.rows <= 128 && s.cols <= 128; }
 
 // Counts and sizes with these tiles; `each` is told of every stack that has tiles.
@@ -1067,7 +1070,7 @@ int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const doub
         for (int e = 0; e < 3; ++e) steps.coefs[i][e] = static_cast<float>(h->coefs[i][e]);
     if (l->littles) {
         const auto kernel = l->little_cols <= 64 ? k_muon_little<64, TERMS> : k_muon_little<128, TERMS>;
-        kernel<<<static_cast<unsigned>(l->littles), kThreads, 0, s>>>(at, moment, h->eps, steps, last);
+        kernel<<<static_cast<unsigned>(l->littles), kLittleThreads, 0, s>>>(at, moment, h->eps, steps, last);
         if (int rc = launched()) return rc;
     }
     if (l->matrices == l->littles) return CS_OK;
