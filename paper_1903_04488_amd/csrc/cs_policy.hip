@@ -331,6 +331,11 @@ __global__ void __launch_bounds__(kMost) k_preference_few(Preference k) {
             for (int64_t i = begin[s] + lane; i < end[s]; i += 64) k.g_logp[i] = !k.counts || k.counts[i] ? g : 0.f;
         }
     }
+    if (k.g_logp) {                          // tokens of no answer
+        const int64_t first = begin_of(k, 0), last = begin_of(k, 2 * k.pairs);
+        for (int64_t i = threadIdx.x; i < first; i += kMost) k.g_logp[i] = 0.f;
+        for (int64_t i = last + threadIdx.x; i < k.tokens; i += kMost) k.g_logp[i] = 0.f;
+    }
     if (lane == 0)
 #pragma unroll
         for (int i = 0; i < 3; ++i) buf[i][wave] = out[i];
@@ -370,7 +375,6 @@ __global__ void __launch_bounds__(kPieceThreads) k_preference_gradient(Preferenc
     for (int e = 0; e < kEach; ++e) own.answer = max(own.answer, mark[mine + e]);
     int64_t answer = first + before_me(own, buf).answer;
     float slope = answer >= 0 && answer < 2 * k.pairs ? k.slope[answer] : 0.f, g[kEach];
-    bool all = true, is[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
         if (mark[mine + e]) {
@@ -378,16 +382,14 @@ __global__ void __launch_bounds__(kPieceThreads) k_preference_gradient(Preferenc
             slope = answer < 2 * k.pairs ? k.slope[answer] : 0.f;
         }
         g[e] = counts[e] ? slope : 0.f;
-        is[e] = answer >= 0 && answer < 2 * k.pairs && at + mine + e < k.tokens;
-        all &= is[e];
     }
     float* const to = k.g_logp + at + mine;
-    if (all) {
+    if (at + mine + kEach <= k.tokens) {
         __builtin_memcpy(to, g, sizeof(g));
     } else {
 #pragma unroll
         for (int e = 0; e < kEach; ++e)
-            if (is[e]) to[e] = g[e];
+            if (at + mine + e < k.tokens) to[e] = g[e];
     }
 }
 

@@ -130,7 +130,7 @@ class PreferenceLoss:
         self.h = B.CsPreference(self.KINDS[kind], mean, beta, smoothing, margin)
         f32 = dict(dtype=torch.float32, device=device)
         self.losses, self.rewards, self.sums = torch.empty(pairs, **f32), torch.empty(2 * pairs, **f32), torch.zeros(3, **f32)
-        self.g_logp = torch.zeros(tokens, **f32)
+        self.g_logp = torch.empty(tokens, **f32)
         self.workspace = torch.empty(B.cs_preference_workspace_bytes(tokens, pairs), dtype=torch.uint8, device=device)
 
     def loss(self, logp, ref_logp, begin, counts=None, weight=None):
