@@ -112,8 +112,8 @@ class CsMatrix(ctypes.Structure):
 
 
 class CsMatrixList(ctypes.Structure):
-    _fields_ = [("memory", ctypes.c_void_p), *((name, ctypes.c_int64) for name in ("matrices", "littles", "pieces", "halves", "fulls", "work")),
-                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_tile", "full_high", "full_wide", "little_cols"))]
+    _fields_ = [("memory", ctypes.c_void_p), *((name, ctypes.c_int64) for name in ("matrices", "littles", "pieces", "halves", "tails", "fulls", "work")),
+                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_kind", "full_kind", "gram_slices", "square_slices", "little_cols"))]
 
 
 class CsMuon(ctypes.Structure):

@@ -55,7 +55,8 @@ struct Batch {
 };
 static_assert(sizeof(Batch) < 3800, "kernel arguments are limited to 4 KB");
 
-// A list in device memory: Matrix[count], then all tiles of lower halves of A, all tiles of X, and the places of all pieces.
+// A list in device memory: Matrix[count], then the tiles of lower halves of A (whole ones, then quarters of those that are left), all tiles of
+// X, and the places of all pieces.
 struct List {
     const Matrix* matrices;
     const Tile *halves, *fulls;
@@ -112,15 +113,18 @@ __device__ __forceinline__ void half_tile_of(int32_t local, int32_t down, int32_
     tj = 8 * band + in;
 }
 
-enum { kPieces, kHalves, kFulls };
+enum { kPieces, kHalves, kTails, kFulls };
 // The matrix of every place (the last that begins at or before it), and what there is to know of it; high, wide: of a tile.
+// kTails: quarters of tiles, from tile number `from` on.
 template <int WHICH, typename Out>
-__global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices, int begin, int end, int high, int wide, Out* out, int64_t places) {
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-    if (c >= places) return;
+__global__ void __launch_bounds__(kThreads)
+k_list_places(const Matrix* matrices, int begin, int end, int high, int wide, Out* out, int64_t places, int64_t from) {
+    const int64_t place = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (place >= places) return;
+    const int64_t c = from + (WHICH == kTails ? place / 4 : place);
     const auto first = [&](int i) {
         const Matrix& t = matrices[i];
-        return WHICH == kPieces ? t.first_piece : WHICH == kHalves ? t.first_half : t.first_full;
+        return WHICH == kPieces ? t.first_piece : WHICH == kFulls ? t.first_full : t.first_half;
     };
     int lo = begin, hi = end - 1;
     while (lo < hi) {
@@ -130,13 +134,17 @@ __global__ void __launch_bounds__(kThreads) k_list_places(const Matrix* matrices
     }
     const int32_t local = static_cast<int32_t>(c - first(lo));
     if constexpr (WHICH == kPieces) {
-        out[c] = Place{lo, local};
+        out[place] = Place{lo, local};
     } else {
         const Matrix& t = matrices[lo];
         Tile tile = {t.at, t.np, t.mp, 0, 0, lo, 0};
-        if (WHICH == kHalves) half_tile_of(local, t.np / high, tile.ti, tile.tj);
-        else tile_of(local, t.np / high, t.mp / wide, tile.ti, tile.tj);
-        out[c] = tile;
+        if (WHICH == kFulls) tile_of(local, t.np / high, t.mp / wide, tile.ti, tile.tj);
+        else half_tile_of(local, t.np / high, tile.ti, tile.tj);
+        if (WHICH == kTails) {
+            tile.ti = 2 * tile.ti + static_cast<int32_t>(place >> 1 & 1);
+            tile.tj = 2 * tile.tj + static_cast<int32_t>(place & 1);
+        }
+        out[place] = tile;
     }
 }
 
@@ -311,6 +319,7 @@ __global__ void __launch_bounds__(kThreads) k_muon_begin(List list, Moment k, do
     }
 }
 
+enum { kWhole, kPartial, kJoin };
 enum { kGram, kSquare, kApply, kFinish };    // A = X X^T; B = b A + c A A; X = a X + B X; the same, into the parameters
 
 // What is made of the last X: p = decay p - lr scale X, or X itself
@@ -328,6 +337,8 @@ struct Product {
     float a, b, c;
     int turn;                                // which of the two X is read
     Last last;                               // kFinish
+    int slices;                              // of K, and where their products are left
+    Float4* partials;
 };
 
 typedef __attribute__((address_space(3))) void* LdsPointer;
@@ -521,22 +532,29 @@ __device__ __forceinline__ int place_of_block() {
     const int per = gridDim.x / 8, more = gridDim.x % 8, die = blockIdx.x % 8, at = blockIdx.x / 8;
     return die * per + min(die, more) + at;
 }
-// C = L R^T of rows of K values, a tile a workgroup.
-template <typename S, int TERMS, int MODE>
+// C = L R^T of rows of K values, a tile a workgroup.  Few tiles with many values of K are taken in slices of K by workgroups of their own (kPartial),
+// whose products a second launch adds up (kJoin).
+template <typename S, int TERMS, int MODE, int PHASE>
 __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(List list, Product k, char* ws) {
     constexpr bool HALF = MODE == kGram || MODE == kSquare;
     constexpr int N = 4 * S::GJ, PART = (S::TI + S::TJ) * S::DEPTH;
-    __shared__ __align__(1024) _Float16 lds[S::STAGES * PART];
-    const Tile t = (HALF ? list.halves : list.fulls)[place_of_block()];
+    __shared__ __align__(1024) _Float16 lds[PHASE == kJoin ? 8 : S::STAGES * PART];
+    const int32_t place = PHASE == kPartial ? blockIdx.x / k.slices : PHASE == kJoin ? blockIdx.x : place_of_block();
+    const Tile t = (HALF ? list.halves : list.fulls)[place];
+    if (HALF && t.ti < t.tj) return;                         // (a quarter above the diagonal: the one below it is written twice)
     const Work<TERMS> w(ws, t.at, t.np, t.mp);
-    const int32_t depth = (MODE == kGram ? t.mp : t.np) * TERMS, all = depth / S::DEPTH;
+    const int32_t depth = (MODE == kGram ? t.mp : t.np) * TERMS, parts = depth / S::DEPTH;
+    // (of a slice of K the parts from `from` on)
+    const int32_t slice = PHASE == kPartial ? blockIdx.x % k.slices : 0;
+    const int32_t from = PHASE == kPartial ? static_cast<int32_t>(static_cast<int64_t>(parts) * slice / k.slices) : 0;
+    const int32_t all = (PHASE == kPartial ? static_cast<int32_t>(static_cast<int64_t>(parts) * (slice + 1) / k.slices) : parts) - from;
     const Stage<S, true> l_stage(depth * 2);
     const char* const left = reinterpret_cast<const char*>((MODE == kGram ? w.x(k.turn) : MODE == kSquare ? w.a() : w.b()) +
-                                                           static_cast<int64_t>(t.ti) * S::TI * depth);
+                                                           static_cast<int64_t>(t.ti) * S::TI * depth + from * S::DEPTH);
     using Right = typename std::conditional<HALF, Stage<S, false>, Columns<S, TERMS>>::type;
     const Right r_stage(HALF ? depth * 2 : t.mp * TERMS * 2);
     const char* const right = reinterpret_cast<const char*>(
-        HALF ? (MODE == kGram ? w.x(k.turn) : w.a()) + static_cast<int64_t>(t.tj) * S::TJ * depth : w.x(k.turn) + t.tj * S::TJ * TERMS);
+        HALF ? (MODE == kGram ? w.x(k.turn) : w.a()) + static_cast<int64_t>(t.tj) * S::TJ * depth + from * S::DEPTH : w.x(k.turn) + t.tj * S::TJ * TERMS);
     const int64_t r_step = HALF ? S::DEPTH * 2 : static_cast<int64_t>(t.mp) * (S::DEPTH * 2);
     const auto load = [&](int32_t i, int turn) {
         l_stage.load(left + i * (S::DEPTH * 2), lds + turn * PART);
@@ -573,11 +591,38 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
             add(second.l, second.r);
         }
     };
+    // of a tile's slices, a lane's blocks each: the slices' products, which the join adds up in their order
+    Float4* const sums = k.partials + (static_cast<int64_t>(place) * k.slices + slice) * (S::FI * S::FJ * S::THREADS) + threadIdx.x;
 #pragma unroll
     for (int i = 0; i < S::STAGES - 1; ++i)
-        if (i < all) load(i, i);
+        if (PHASE != kJoin && i < all) load(i, i);
     Operands first, second;
-    if constexpr (S::AHEAD) {
+    if constexpr (PHASE == kJoin) {
+#pragma unroll 4
+        for (int i = 0; i < k.slices; ++i)
+#pragma unroll
+            for (int fi = 0; fi < S::FI; ++fi)
+#pragma unroll
+                for (int fj = 0; fj < S::FJ; ++fj) acc[fi][fj] += sums[(i * S::FI * S::FJ + fi * S::FJ + fj) * S::THREADS];
+    } else if constexpr (PHASE == kPartial) {
+        int turn = 0, next = S::STAGES - 1;
+        for (int32_t i = 0; i < all; ++i) {
+            if (i + S::STAGES - 1 <= all) arrived<(S::STAGES - 2) * S::LOADS>();
+            else arrived<0>();
+            if (i + S::STAGES - 1 < all) load(i + S::STAGES - 1, next);
+            next = next + 1 == S::STAGES ? 0 : next + 1;
+            take(first, turn, 0);
+            take(second, turn, 1);
+            add(first.l, first.r);
+            add_second(first, second);
+            turn = turn + 1 == S::STAGES ? 0 : turn + 1;
+        }
+#pragma unroll
+        for (int fi = 0; fi < S::FI; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < S::FJ; ++fj) sums[(fi * S::FJ + fj) * S::THREADS] = acc[fi][fj];
+        return;
+    } else if constexpr (S::AHEAD) {
         // Operands are read from LDS while products are taken of those before: the second half of a part's with its first half's, and the next part's
         // first half, which has arrived by then, with the second half's.
         static_assert(!S::AHEAD || S::STAGES == 2, "a part has the step before to arrive in");
@@ -649,8 +694,10 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
         }
     };
     fetch(0);
-    add(first.l, first.r);
-    add_second(first, second);
+    if (PHASE == kWhole) {
+        add(first.l, first.r);
+        add_second(first, second);
+    }
 
     Update u = {};
     Matrix matrix;
@@ -897,10 +944,23 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
 // ---------------------------------------------------------------------------------------
 constexpr int64_t kMaxSide = 1 << 20, kMaxShort = 1 << 15, kMaxMatrices = 1 << 20, kMaxPlaces = static_cast<int64_t>(1) << 24;
 
+// Kinds of tiles: edges, how many are on the GPU at once, and how long they take for a part of 64 values of K and besides (us; `alone`: with no
+// more than one on a CU)
+struct Kind {
+    int high, wide, at_once;
+    double step, besides, alone;
+};
+constexpr Kind kHalfKinds[] = {{64, 64, 768, 0.5, 3., 0.28}, {128, 128, 512, 0.83, 4., 0.68}};
+constexpr Kind kFullKinds[] = {{64, 64, 768, 0.5, 3., 0.28}, {64, 128, 768, 0.95, 5., 0.5}, {128, 128, 512, 1.05, 6., 0.68}, {256, 256, 256, 1.65, 14., 1.65}};
+constexpr int kHalfKindsN = 2, kFullKindsN = 4;
+constexpr int kMaxSlices = 32;
+constexpr int64_t kPartialBytes = 64 * 64 * 4;       // of a tile's slice
+
 struct Plan {
-    int64_t matrices, littles, pieces, halves, fulls, work;      // work: bytes of all matrices
-    double half_steps, full_steps;                               // parts of 64 values of K, of all tiles together
-    int half_tile, full_high, full_wide;
+    int64_t matrices, littles, pieces, halves, tails, fulls, work;       // tails: quarters of the last tiles; work: bytes of all matrices
+    double gram_steps, square_steps, full_steps;                         // parts of 64 values of K (both halves of them), of all tiles together
+    int half_kind, full_kind;
+    int slices[2];                                                       // of K, of X X^T and of A A in tiles of 64
 };
 int64_t up_to(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
 
@@ -914,9 +974,10 @@ bool little(const cs_matrix& s) { return (s.rows <= 64 || s.cols <= 64) && s.row
 
 // Counts and sizes with these tiles; `each` is told of every stack that has tiles.
 template <typename F>
-bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int full_high, int full_wide, Plan& plan, F each) {
+bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_kind, int full_kind, Plan& plan, F each) {
     plan = Plan{};
-    plan.half_tile = half_tile, plan.full_high = full_high, plan.full_wide = full_wide;
+    plan.half_kind = half_kind, plan.full_kind = full_kind;
+    const int64_t half_tile = kHalfKinds[half_kind].high, full_high = kFullKinds[full_kind].high, full_wide = kFullKinds[full_kind].wide;
     const int64_t tile = half_tile > full_high ? half_tile : full_high;
     for (int32_t i = 0; i < n; ++i) {
         const cs_matrix& s = stacks[i];
@@ -935,56 +996,88 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_tile, int
         plan.pieces += s.count * pieces;
         plan.halves += s.count * halves;
         plan.fulls += s.count * fulls;
-        plan.half_steps += static_cast<double>(s.count * halves) * (np + mp) / 64;
-        plan.full_steps += static_cast<double>(s.count * fulls) * np / 64;
+        plan.gram_steps += static_cast<double>(s.count * halves) * mp * terms / 64;
+        plan.square_steps += static_cast<double>(s.count * halves) * np * terms / 64;
+        plan.full_steps += static_cast<double>(s.count * fulls) * np * terms / 64;
         plan.work += s.count * work_bytes(np, mp, terms);
         if (plan.pieces >= kMaxPlaces) return false;
     }
     return true;
 }
-// How long tiles take that are spread over 256 CUs, in parts of 64 values of K of one tile (us; of 64 x 64 and 64 x 128 three are on a CU at a time, of
-// 128 x 128 two, of 256 x 256 one, and fewer take less each).
-double rounds(int64_t tiles, int high, int wide) {
-    const int64_t at_once = high == 64 ? 768 : high == 128 ? 512 : 256, left = tiles % at_once;
-    const double full = high == 64 ? (wide == 64 ? 0.6 : 0.9) : high == 128 ? 1.15 : 1.95;
-    const double rest = left == 0 ? 0. : left > at_once - 256 ? full : high == 128 ? 0.6 : left > 256 ? 0.75 * full : 0.5 * full;
-    return static_cast<double>(tiles / at_once) * full + rest;
+// How long so many tiles take with so many parts of K each, in rounds of what is on the GPU at once (a last round of few takes less).
+double time_of(const Kind& kind, int64_t tiles, double steps) {
+    const int64_t left = tiles % kind.at_once;
+    const double last = left == 0 ? 0. : (left > 256 ? kind.step : kind.alone) * steps + kind.besides;
+    return static_cast<double>(tiles / kind.at_once) * (kind.step * steps + kind.besides) + last;
+}
+// The same of tiles of 64, in as many slices of K as are best; a launch to join them is 5 us (64 x 4096, two terms: X X^T 28 us whole).
+double time_in_slices(int64_t tiles, double steps, int& slices) {
+    double least = INFINITY;
+    for (int n = 1; n <= kMaxSlices && (n == 1 || (tiles * n <= 768 && n * 2 <= steps)); n *= 2) {
+        const double us = time_of(kHalfKinds[0], tiles * n, steps / n) + (n > 1 ? 5. : 0.);
+        if (us < least) {
+            least = us;
+            slices = n;
+        }
+    }
+    return least;
+}
+// A symmetric product.  Few tiles of 128 left by the last round would take nearly as long as a whole one where K is long (528 tiles of 4096 x 4096: 74 us
+// for 512 and 26 for the 16 that are left): they are taken as tiles of 64, four each, `tails` (16 us).
+double half_time(int kind, int64_t tiles, double steps, int64_t tails, int& slices) {
+    if (kind == 0) return time_in_slices(tiles, steps, slices);
+    slices = 1;
+    return time_of(kHalfKinds[1], tiles - tails / 4, steps) + (tails ? time_in_slices(tails, steps, slices) : 0.);
 }
 bool plan_of(const cs_matrix* stacks, int32_t n, int terms, Plan& plan) {
     const auto none = [](const cs_matrix&, int64_t, int64_t, const Plan&, int64_t, int64_t, int64_t) {};
-    static const int kFullTiles[][2] = {{64, 64}, {64, 128}, {128, 128}, {256, 256}};
     double least = INFINITY;
     bool ok = false;
-    for (const int half_tile : {64, 128})
-        for (const auto& full : kFullTiles) {
-            Plan p;
+    for (int half = 0; half < kHalfKindsN; ++half)
+        for (int full = 0; full < kFullKindsN; ++full) {
+            Plan whole;
             // (larger tiles fill up more: they may be too many where smaller ones are not)
-            if (!plan_with(stacks, n, terms, half_tile, full[0], full[1], p, none)) continue;
-            const double us = p.halves ? rounds(p.halves, half_tile, half_tile) * p.half_steps / static_cast<double>(p.halves) +
-                                             rounds(p.fulls, full[0], full[1]) * p.full_steps / static_cast<double>(p.fulls) : 0.;
-            if (us < least) {
-                least = us;
-                plan = p;
-                ok = true;
+            if (!plan_with(stacks, n, terms, half, full, whole, none)) continue;
+            const int64_t halves = whole.halves, left = halves % kHalfKinds[half].at_once;
+            for (const int64_t tails : {static_cast<int64_t>(0), half == 1 ? 4 * left : 0}) {
+                Plan p = whole;
+                p.halves -= tails / 4;
+                p.tails = tails;
+                const double us = halves ? half_time(half, halves, p.gram_steps / static_cast<double>(halves), tails, p.slices[0]) +
+                                               half_time(half, halves, p.square_steps / static_cast<double>(halves), tails, p.slices[1]) +
+                                               time_of(kFullKinds[full], p.fulls, p.full_steps / static_cast<double>(p.fulls)) : 0.;
+                if (us < least) {
+                    least = us;
+                    plan = p;
+                    ok = true;
+                }
             }
         }
     return ok;
 }
+// tiles of 64 that may be in slices, and what their products need of the workspace
+int64_t sliced_tiles(int half_kind, int64_t halves, int64_t tails) { return half_kind == 0 ? halves : tails; }
+int64_t partial_bytes(const cs_matrix_list* l) {
+    const int most = l->gram_slices > l->square_slices ? l->gram_slices : l->square_slices;
+    return most > 1 ? sliced_tiles(l->half_kind, l->halves, l->tails) * most * kPartialBytes : 0;
+}
 size_t list_bytes(const Plan& p) {
-    return static_cast<size_t>(p.matrices) * sizeof(Matrix) + static_cast<size_t>(p.halves + p.fulls) * sizeof(Tile) +
+    return static_cast<size_t>(p.matrices) * sizeof(Matrix) + static_cast<size_t>(p.halves + p.tails + p.fulls) * sizeof(Tile) +
            static_cast<size_t>(p.pieces) * sizeof(Place);
 }
-size_t workspace_bytes(const cs_matrix_list* l) { return static_cast<size_t>(l->work) + static_cast<size_t>(l->pieces) * sizeof(double); }
+size_t workspace_bytes(const cs_matrix_list* l) {
+    return static_cast<size_t>(l->work + partial_bytes(l)) + static_cast<size_t>(l->pieces) * sizeof(double);
+}
 List list_of(const cs_matrix_list* l) {
     const Matrix* t = static_cast<const Matrix*>(l->memory);
     const Tile* at = reinterpret_cast<const Tile*>(t + l->matrices);
-    return List{t, at, at + l->halves, reinterpret_cast<const Place*>(at + l->halves + l->fulls)};
+    return List{t, at, at + l->halves + l->tails, reinterpret_cast<const Place*>(at + l->halves + l->tails + l->fulls)};
 }
-bool full_ok(int32_t high, int32_t wide) { return (high == 64 && wide == 128) || (high == wide && (high == 64 || high == 128 || high == 256)); }
 bool list_ok(const cs_matrix_list* l) {
-    return l && l->littles >= 0 && l->matrices >= l->littles && l->pieces >= 0 && l->halves >= 0 && l->fulls >= 0 && l->work >= 0 &&
-           (l->half_tile == 64 || l->half_tile == 128) && full_ok(l->full_high, l->full_wide) && (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) &&
-           fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
+    return l && l->littles >= 0 && l->matrices >= l->littles && l->pieces >= 0 && l->halves >= 0 && l->tails >= 0 && l->fulls >= 0 &&
+           l->work >= 0 && l->half_kind >= 0 && l->half_kind < kHalfKindsN && l->full_kind >= 0 && l->full_kind < kFullKindsN &&
+           l->gram_slices >= 0 && l->gram_slices <= kMaxSlices && l->square_slices >= 0 && l->square_slices <= kMaxSlices &&
+           (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) && fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
 }
 
 // The steps keep singular values of at most 1 below 2, and B within binary16.
@@ -1035,23 +1128,37 @@ struct ShapeOf<128, 128, 2, false> : Shape<2, 4, 4, 2, 2, 4, true> {};
 template <int TERMS>
 struct ShapeOf<256, 256, TERMS, false> : Shape<2, 4, 8, 4, 2, 2, TERMS == 1> {};
 
-template <int TERMS, int MODE, int HIGH, int WIDE>
-int product_as(const cs_matrix_list* l, const Product& k, char* ws, hipStream_t s) {
-    constexpr bool HALF = MODE == kGram || MODE == kSquare;
-    using S = ShapeOf<HIGH, WIDE, TERMS, HALF>;
+template <int TERMS, int MODE, int HIGH, int WIDE, int PHASE = kWhole>
+int product_as(const List& list, int64_t places, const Product& k, char* ws, hipStream_t s) {
+    using S = ShapeOf<HIGH, WIDE, TERMS, MODE == kGram || MODE == kSquare>;
     static_assert(S::TI == HIGH && S::TJ == WIDE, "");
-    const int64_t places = HALF ? l->halves : l->fulls;
-    k_muon_product<S, TERMS, MODE><<<static_cast<unsigned>(places), S::THREADS, 0, s>>>(list_of(l), k, ws);
+    k_muon_product<S, TERMS, MODE, PHASE><<<static_cast<unsigned>(places), S::THREADS, 0, s>>>(list, k, ws);
     return launched();
 }
 template <int TERMS, int MODE>
-int product(const cs_matrix_list* l, const Product& k, char* ws, hipStream_t s) {
+int product(const cs_matrix_list* l, Product k, char* ws, hipStream_t s) {
+    List list = list_of(l);
     if constexpr (MODE == kGram || MODE == kSquare) {
-        return l->half_tile == 64 ? product_as<TERMS, MODE, 64, 64>(l, k, ws, s) : product_as<TERMS, MODE, 128, 128>(l, k, ws, s);
+        int64_t tiles = l->halves;
+        if (l->half_kind == 1) {
+            if (l->halves)
+                if (int rc = product_as<TERMS, MODE, 128, 128>(list, l->halves, k, ws, s)) return rc;
+            list.halves += l->halves;
+            tiles = l->tails;
+        }
+        if (tiles == 0) return CS_OK;
+        k.slices = MODE == kGram ? l->gram_slices : l->square_slices;
+        if (k.slices <= 1) return product_as<TERMS, MODE, 64, 64>(list, tiles, k, ws, s);       // (partial_bytes() has room for slices only)
+        k.partials = reinterpret_cast<Float4*>(ws + l->work);
+        if (int rc = product_as<TERMS, MODE, 64, 64, kPartial>(list, tiles * k.slices, k, ws, s)) return rc;
+        return product_as<TERMS, MODE, 64, 64, kJoin>(list, tiles, k, ws, s);
     } else {
-        if (l->full_high == 256) return product_as<TERMS, MODE, 256, 256>(l, k, ws, s);
-        if (l->full_high == 128) return product_as<TERMS, MODE, 128, 128>(l, k, ws, s);
-        return l->full_wide == 128 ? product_as<TERMS, MODE, 64, 128>(l, k, ws, s) : product_as<TERMS, MODE, 64, 64>(l, k, ws, s);
+        switch (l->full_kind) {
+            case 0: return product_as<TERMS, MODE, 64, 64>(list, l->fulls, k, ws, s);
+            case 1: return product_as<TERMS, MODE, 64, 128>(list, l->fulls, k, ws, s);
+            case 2: return product_as<TERMS, MODE, 128, 128>(list, l->fulls, k, ws, s);
+            default: return product_as<TERMS, MODE, 256, 256>(list, l->fulls, k, ws, s);
+        }
     }
 }
 
@@ -1074,7 +1181,7 @@ int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const doub
         if (int rc = launched()) return rc;
     }
     if (l->matrices == l->littles) return CS_OK;
-    double* const squares = reinterpret_cast<double*>(ws + l->work);
+    double* const squares = reinterpret_cast<double*>(ws + l->work + partial_bytes(l));
     const unsigned pieces = static_cast<unsigned>(l->pieces);
     k_muon_moment<<<pieces, kThreads, 0, s>>>(at, moment, squares);
     const bool joined = l->pieces > kSquaresEach * (l->matrices - l->littles);
@@ -1086,7 +1193,7 @@ int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const doub
     k_muon_begin<TERMS><<<pieces, kThreads, 0, s>>>(at, moment, h->eps, squares, joined, ws);
     if (int rc = launched()) return rc;
     for (int i = 0; i < h->steps; ++i) {
-        const Product k = {steps.coefs[i][0], steps.coefs[i][1], steps.coefs[i][2], i & 1, last};
+        const Product k = {steps.coefs[i][0], steps.coefs[i][1], steps.coefs[i][2], i & 1, last, 1, nullptr};
         if (int rc = product<TERMS, kGram>(l, k, ws, s)) return rc;
         if (int rc = product<TERMS, kSquare>(l, k, ws, s)) return rc;
         if (int rc = i + 1 < h->steps ? product<TERMS, kApply>(l, k, ws, s) : product<TERMS, kFinish>(l, k, ws, s)) return rc;
@@ -1101,7 +1208,7 @@ int run(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const double*
     if (ws_bytes < need) return CS_EWORKSPACE;
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return CS_EINVAL;
     Plan plan = {};
-    plan.matrices = l->matrices, plan.pieces = l->pieces, plan.halves = l->halves, plan.fulls = l->fulls;
+    plan.matrices = l->matrices, plan.pieces = l->pieces, plan.halves = l->halves, plan.tails = l->tails, plan.fulls = l->fulls;
     const Span written[] = {{need ? workspace : nullptr, static_cast<int64_t>(need)}};
     const Span read[] = {{l->memory, static_cast<int64_t>(list_bytes(plan))}, {lr, 8}, {grad_scale, 4}};
     if (!spans_apart(written, read)) return CS_EINVAL;
@@ -1156,8 +1263,8 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
             const int64_t side = stacks[i].rows > stacks[i].cols ? stacks[i].rows : stacks[i].cols;
             if (side > little_cols) little_cols = side;
         }
-    *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.pieces, plan.halves, plan.fulls, plan.work, p_fmt, g_fmt, terms, moments == 1,
-                           plan.half_tile, plan.full_high, plan.full_wide, static_cast<int32_t>(little_cols)};
+    *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.pieces, plan.halves, plan.tails, plan.fulls, plan.work, p_fmt, g_fmt, terms,
+                           moments == 1, plan.half_kind, plan.full_kind, plan.slices[0], plan.slices[1], static_cast<int32_t>(little_cols)};
     if (plan.matrices == 0) return CS_OK;
     Matrix* const matrices = static_cast<Matrix*>(memory);
     const hipStream_t st = stream_of(stream);
@@ -1186,7 +1293,7 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
         if (there(stacks[i]) && little(stacks[i]))
             for (int64_t k = 0; k < stacks[i].count; ++k) take(stacks[i], k, Matrix{});
     Plan again;
-    plan_with(stacks, count, terms, plan.half_tile, plan.full_high, plan.full_wide, again,
+    plan_with(stacks, count, terms, plan.half_kind, plan.full_kind, again,
               [&](const cs_matrix& s, int64_t np, int64_t mp, const Plan& at, int64_t pieces, int64_t halves, int64_t fulls) {
         for (int64_t k = 0; k < s.count; ++k) {
             Matrix t = {};
@@ -1200,13 +1307,15 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
     flush();
     if (rc) return rc;
     Tile* const halves = reinterpret_cast<Tile*>(matrices + plan.matrices);
-    Tile* const fulls = halves + plan.halves;
+    Tile *const tails = halves + plan.halves, *const fulls = tails + plan.tails;
     const auto grid = [](int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); };
     const int first = static_cast<int>(plan.littles), n = static_cast<int>(plan.matrices);
     if (first == n) return CS_OK;
-    k_list_places<kHalves><<<grid(plan.halves), kThreads, 0, st>>>(matrices, first, n, plan.half_tile, plan.half_tile, halves, plan.halves);
-    k_list_places<kFulls><<<grid(plan.fulls), kThreads, 0, st>>>(matrices, first, n, plan.full_high, plan.full_wide, fulls, plan.fulls);
-    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, kEdge, reinterpret_cast<Place*>(fulls + plan.fulls), plan.pieces);
+    const Kind &half = kHalfKinds[plan.half_kind], &full = kFullKinds[plan.full_kind];
+    if (plan.halves) k_list_places<kHalves><<<grid(plan.halves), kThreads, 0, st>>>(matrices, first, n, half.high, half.wide, halves, plan.halves, 0);
+    if (plan.tails) k_list_places<kTails><<<grid(plan.tails), kThreads, 0, st>>>(matrices, first, n, half.high, half.wide, tails, plan.tails, plan.halves);
+    k_list_places<kFulls><<<grid(plan.fulls), kThreads, 0, st>>>(matrices, first, n, full.high, full.wide, fulls, plan.fulls, 0);
+    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, kEdge, reinterpret_cast<Place*>(fulls + plan.fulls), plan.pieces, 0);
     if (int e = launched()) return e;
     return CS_OK;
 }

@@ -79,7 +79,8 @@ def matrices_of(count, rows, cols, dtype=torch.float32, seed=1, steep=False):
 
 # a workgroup's own (up to 64 x 128), and in tiles of every size
 SIZES = [(1, 1, 1), (1, 1, 70), (2, 70, 1), (1, 3, 5), (1, 64, 64), (2, 65, 63), (3, 30, 64), (2, 64, 128), (2, 127, 50), (1, 65, 65), (1, 64, 129), (1, 16, 300), (3, 130, 257), (2, 257, 128), (1, 200, 1000),
-         (1, 512, 512)]
+         (1, 512, 512),
+         (1, 60, 4000), (2, 250, 3000), (1, 2100, 330), (5, 65, 5000)]
 
 
 @pytest.mark.parametrize("count,rows,cols", SIZES)
