@@ -39,7 +39,7 @@ struct Matrix {
     int64_t p_stride, g_stride;
     int64_t at;                              // of its part of the workspace, bytes
     int32_t rows, cols, np, mp;
-    int32_t first_piece, first_half, first_full, pieces;
+    int32_t first_piece, first_half, first_full, pieces;      // (of a thin one first_piece is its first slab)
 };
 struct Place {
     int32_t matrix, local;
@@ -56,11 +56,11 @@ struct Batch {
 static_assert(sizeof(Batch) < 3800, "kernel arguments are limited to 4 KB");
 
 // A list in device memory: Matrix[count], then the tiles of lower halves of A (whole ones, then quarters of those that are left), all tiles of
-// X, and the places of all pieces.
+// X, and the places of all pieces and slabs.
 struct List {
     const Matrix* matrices;
     const Tile *halves, *fulls;
-    const Place* pieces;
+    const Place *pieces, *slabs;
 };
 
 // A matrix's part of the workspace: X twice (read and written in turns), A0, B0, and the diagonals of A and B.  Values are two halves, the upper and the
@@ -778,61 +778,26 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
 
 // A small matrix (n <= 64, m <= M) a workgroup, in one launch: X in binary32 in registers, what the products read in LDS.  16 wavefronts, a block
 // of 16 x 16 of A and M / 64 of X each: five steps are a chain of fifteen products and barriers (64 x 64, two terms: 2.3 us a step and
-// 4 us besides, 15.9 in all, with four wavefronts of 2 x 2 blocks 17.2; one term 11.0; by the other launches 70).
+// 4 us besides, 15.9 in all, with four wavefronts of 2 x 2 blocks 17.2; one term 11.0; by tiles 70.  64 x 250, two terms: 31 and by tiles 66; 1000 of
+// them 141 and 323).
 constexpr int kLittleThreads = 1024;
+typedef _Float16 Half4 __attribute__((ext_vector_type(4)));
 template <int M, int TERMS>
 struct Little {
     static constexpr int N = 64, F = M / 64, WIDE = M + 8, HIGH = N + 8;     // (rows 16 bytes further: 16 of them meet all banks)
     static constexpr int X = N * WIDE, A = N * HIGH;
     static constexpr int HALVES = TERMS * (X + 2 * A) + 2 * 2 * N;
-};
-typedef _Float16 Half4 __attribute__((ext_vector_type(4)));
-template <int M, int TERMS>
-__global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Moment moment, double eps, Steps steps, Last last) {
-    using L = Little<M, TERMS>;
-    constexpr int F = L::F;                  // a lane has a row of 4 F columns of X (4 each of F blocks) and 4 of A
-    __shared__ __align__(16) _Float16 lds[L::HALVES];
-    __shared__ double buf[kLittleThreads / 64];
-    _Float16 *const x_at = lds, *const a_at = x_at + TERMS * L::X, *const b_at = a_at + TERMS * L::A;
-    float *const da = reinterpret_cast<float*>(b_at + TERMS * L::A), *const db = da + L::N;
-    if (skipped(last.grad_scale)) return;
-    const Matrix t = list.matrices[blockIdx.x];
-    const bool tall = t.rows > t.cols;
-    const float s = moment.grad_scale ? *moment.grad_scale : 1.f;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wi = wave >> 2, wj = wave & 3;
-    const int row = wi * 16 + (lane & 15), col = wj * (M / 4) + (lane >> 4) * 4, a_col = wj * 16 + (lane >> 4) * 4;
-    float x[F][4];
-    double sum = 0.;
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-        if (tall) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float u[1];
-                direction<true>(t, moment, s, col + 16 * f + e, row, u);
-                x[f][e] = u[0];
-            }
-        } else {
-            direction<true>(t, moment, s, row, col + 16 * f, x[f]);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum = fma(static_cast<double>(x[f][e]), static_cast<double>(x[f][e]), sum);
-    }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) buf[wave] = sum;
-    __syncthreads();
-    sum = buf[lane & 15];
-#pragma unroll
-    for (int d = 8; d; d >>= 1) sum += __shfl_xor(sum, d);
-    const double one = inverse_of(sum, eps) * static_cast<double>(kUp);
-#pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[f][e] = static_cast<float>(x[f][e] * one);
+    // A lane has a row of 4 F columns of X (4 each of F blocks) and 4 of A.
+    _Float16 *const x_at, *const a_at, *const b_at;
+    float *const da, *const db;
+    const int lane, wi, wj, row, col, a_col;
+    __device__ __forceinline__ explicit Little(_Float16* lds)
+        : x_at(lds), a_at(x_at + TERMS * X), b_at(a_at + TERMS * A), da(reinterpret_cast<float*>(b_at + TERMS * A)), db(da + N),
+          lane(threadIdx.x & 63), wi(threadIdx.x >> 8), wj(threadIdx.x >> 6 & 3), row(wi * 16 + (lane & 15)),
+          col(wj * (M / 4) + (lane >> 4) * 4), a_col(wj * 16 + (lane >> 4) * 4) {}
 
     // four neighbouring values, and their lower halves
-    const auto keep = [&](const float(&v)[4], _Float16* at, int size) {
+    static __device__ __forceinline__ void keep(const float (&v)[4], _Float16* at, int size) {
         Half4 h, l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -842,22 +807,26 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
         }
         *reinterpret_cast<Half4*>(at) = h;
         if (TERMS == 2) *reinterpret_cast<Half4*>(at + size) = l;
-    };
+    }
+    __device__ __forceinline__ void keep_x(const float (&x)[F][4]) const {
+#pragma unroll
+        for (int f = 0; f < F; ++f) keep(x[f], x_at + row * WIDE + col + 16 * f, X);
+    }
     // 8 values of K of a row a lane
-    const auto rows = [&](Half8(&v)[TERMS], const _Float16* at, int step, int size, int first, int q) {
+    __device__ __forceinline__ void rows(Half8 (&v)[TERMS], const _Float16* at, int step, int size, int first, int q) const {
 #pragma unroll
         for (int low = 0; low < TERMS; ++low)
             v[low] = *reinterpret_cast<const Half8*>(at + low * size + (first + (lane & 15)) * step + (lane >> 4) * 8 + q);
-    };
-    const auto add = [&](Float4& acc, const Half8(&l)[TERMS], const Half8(&r)[TERMS]) {
+    }
+    static __device__ __forceinline__ void add(Float4& acc, const Half8 (&l)[TERMS], const Half8 (&r)[TERMS]) {
         acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0], l[0], acc, 0, 0, 0);
         if (TERMS == 2) {
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[TERMS - 1], l[0], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(r[0], l[TERMS - 1], acc, 0, 0, 0);
         }
-    };
+    }
     // this wavefront's block of L L^T
-    const auto square = [&](const _Float16* at, int step, int size, int depth) {
+    __device__ __forceinline__ Float4 square(const _Float16* at, int step, int size, int depth) const {
         Float4 acc = {};
 #pragma unroll
         for (int q = 0; q < depth; q += 32) {
@@ -867,13 +836,10 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
             add(acc, l, r);
         }
         return acc;
-    };
-    for (int i = 0; i < steps.count; ++i) {
-        const float a = steps.coefs[i][0], b = steps.coefs[i][1], c = steps.coefs[i][2];
-#pragma unroll
-        for (int f = 0; f < F; ++f) keep(x[f], x_at + row * L::WIDE + col + 16 * f, L::X);
-        __syncthreads();
-        Float4 acc = square(x_at, L::WIDE, L::X, M);
+    }
+    __device__ __forceinline__ Float4 gram() const { return square(x_at, WIDE, X, M); }
+    // B from X X^T (`acc`; 2^20 times)
+    __device__ __forceinline__ void polynomial(Float4 acc, float b, float c) const {
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -883,9 +849,9 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
                 v[e] = 0.f;
             }
         }
-        keep(v, a_at + row * L::HIGH + a_col, L::A);
+        keep(v, a_at + row * HIGH + a_col, A);
         __syncthreads();
-        acc = square(a_at, L::HIGH, L::A, L::N);
+        acc = square(a_at, HIGH, A, N);
         const float d = fmaf(c, da[row], b);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -897,16 +863,19 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
                 v[e] = fmaf(fmaf(c, dj, d), v[e], acc[e] * (c * kDown));
             }
         }
-        keep(v, b_at + row * L::HIGH + a_col, L::A);
+        keep(v, b_at + row * HIGH + a_col, A);
         __syncthreads();
+    }
+    // X = a X + B X
+    __device__ __forceinline__ void apply(float a, float (&x)[F][4]) const {
         const float keeps = a + db[row];
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            acc = Float4{};
+            Float4 acc = {};
 #pragma unroll
-            for (int q = 0; q < L::N; q += 32) {
+            for (int q = 0; q < N; q += 32) {
                 Half8 l[TERMS], r[TERMS];
-                rows(l, b_at, L::HIGH, L::A, wi * 16, q);
+                rows(l, b_at, HIGH, A, wi * 16, q);
                 // columns of X, from its rows
 #pragma unroll
                 for (int low = 0; low < TERMS; ++low) {
@@ -919,7 +888,7 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
                         of.part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (Pointer)(x_at + low * L::X + (q + (lane >> 4) * 8 + h * 4 + (lane >> 2 & 3)) * L::WIDE + wj * (M / 4) + 16 * f + (lane & 3) * 4));
+                            (Pointer)(x_at + low * X + (q + (lane >> 4) * 8 + h * 4 + (lane >> 2 & 3)) * WIDE + wj * (M / 4) + 16 * f + (lane & 3) * 4));
                     r[low] = of.all;
                 }
                 add(acc, l, r);
@@ -927,20 +896,164 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Momen
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[f][e] = fmaf(keeps, x[f][e], acc[e] * kDown);
         }
+    }
+    // u of the columns from `first` on, the moment's step taken; returns the sum of its squares, in every lane
+    __device__ __forceinline__ double begin(const Matrix& t, const Moment& moment, int32_t first, float (&x)[F][4],
+                                            double (&buf)[kLittleThreads / 64]) const {
+        const float s = moment.grad_scale ? *moment.grad_scale : 1.f;
+        double sum = 0.;
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            if (t.rows > t.cols) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float u[1];
+                    direction<true>(t, moment, s, first + col + 16 * f + e, row, u);
+                    x[f][e] = u[0];
+                }
+            } else {
+                direction<true>(t, moment, s, row, first + col + 16 * f, x[f]);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum = fma(static_cast<double>(x[f][e]), static_cast<double>(x[f][e]), sum);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) buf[threadIdx.x >> 6] = sum;
+        __syncthreads();
+        sum = buf[lane & 15];
+#pragma unroll
+        for (int d = 8; d; d >>= 1) sum += __shfl_xor(sum, d);
+        return sum;
+    }
+    __device__ __forceinline__ void end(const Matrix& t, const Last& last, int32_t first, const float (&x)[F][4]) const {
+        const Update u = update_of(last, t);
+#pragma unroll
+        for (int f = 0; f < F; ++f) {
+            float v[1][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[0][e] = x[f][e] * kDown;
+            finish(t, last.p_fmt, u, row, first + col + 16 * f, v);
+        }
+    }
+};
+template <int M, int TERMS>
+__global__ void __launch_bounds__(kLittleThreads) k_muon_little(List list, Moment moment, double eps, Steps steps, Last last) {
+    using L = Little<M, TERMS>;
+    __shared__ __align__(16) _Float16 lds[L::HALVES];
+    __shared__ double buf[kLittleThreads / 64];
+    if (skipped(last.grad_scale)) return;
+    const Matrix t = list.matrices[blockIdx.x];
+    const L w(lds);
+    float x[L::F][4];
+    const double one = inverse_of(w.begin(t, moment, 0, x, buf), eps) * static_cast<double>(kUp);
+#pragma unroll
+    for (int f = 0; f < L::F; ++f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[f][e] = static_cast<float>(x[f][e] * one);
+    for (int i = 0; i < steps.count; ++i) {
+        w.keep_x(x);
+        __syncthreads();
+        w.polynomial(w.gram(), steps.coefs[i][1], steps.coefs[i][2]);
+        w.apply(steps.coefs[i][0], x);
         __syncthreads();
     }
-    const Update u = update_of(last, t);
-#pragma unroll
-    for (int f = 0; f < F; ++f) {
-        float v[1][4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[0][e] = x[f][e] * kDown;
-        finish(t, last.p_fmt, u, row, col + 16 * f, v);
-    }
+    w.end(t, last, 0, x);
 }
 
-// ---------------------------------------------------------------------------------------
-// host side
+// A thin matrix (n <= 64, longer ones) in slabs of 256 columns, a workgroup each and a launch a step: it adds up the slabs' X X^T of the step before in
+// their order, makes B of it (every workgroup the same), takes its slab to the next X and leaves that one's X X^T.  The first launch has no norm
+// yet: it leaves u, and u u^T with u by the slab's own norm.
+constexpr int kSlab = 256, kMaxSlabs = 32;
+struct Slabs {
+    Float4* x;                               // u or X, of a slab F x kLittleThreads
+    Float4* all_sums;                        // X X^T, of a slab kLittleThreads, twice (read and written in turns)
+    double* squares;                         // a slab each
+    int32_t slabs;
+    __device__ __forceinline__ Slabs(char* ws, const Matrix& t) {
+        slabs = t.mp / kSlab;
+        x = reinterpret_cast<Float4*>(ws + t.at);
+        all_sums = x + slabs * (kSlab / 64 * kLittleThreads);
+        squares = reinterpret_cast<double*>(all_sums + 2 * slabs * kLittleThreads);
+    }
+    __device__ __forceinline__ Float4* sums(int turn) const { return all_sums + turn * slabs * kLittleThreads + threadIdx.x; }
+};
+int64_t slab_bytes(int64_t slabs) { return slabs * ((kSlab / 64 + 2) * kLittleThreads * 16 + 16); }
+
+template <int TERMS>
+__global__ void __launch_bounds__(kLittleThreads) k_muon_slab_begin(List list, Moment moment, double eps, char* ws) {
+    using L = Little<kSlab, TERMS>;
+    __shared__ __align__(16) _Float16 lds[L::HALVES];
+    __shared__ double buf[kLittleThreads / 64];
+    if (skipped(moment.grad_scale)) return;
+    const Place at = list.slabs[blockIdx.x];
+    const Matrix t = list.matrices[at.matrix];
+    const Slabs k(ws, t);
+    const L w(lds);
+    float x[L::F][4];
+    const double sum = w.begin(t, moment, at.local * kSlab, x, buf);
+    const double one = inverse_of(sum, eps) * static_cast<double>(kUp);
+#pragma unroll
+    for (int f = 0; f < L::F; ++f) {
+        k.x[(at.local * L::F + f) * kLittleThreads + threadIdx.x] = Float4{x[f][0], x[f][1], x[f][2], x[f][3]};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[f][e] = static_cast<float>(x[f][e] * one);
+    }
+    w.keep_x(x);
+    __syncthreads();
+    k.sums(0)[at.local * kLittleThreads] = w.gram();
+    if (threadIdx.x == 0) k.squares[at.local] = sum;
+}
+template <int TERMS>
+__global__ void __launch_bounds__(kLittleThreads) k_muon_slab(List list, Steps steps, int step, double eps, Last last, char* ws) {
+    using L = Little<kSlab, TERMS>;
+    __shared__ __align__(16) _Float16 lds[L::HALVES];
+    if (skipped(last.grad_scale)) return;
+    const Place at = list.slabs[blockIdx.x];
+    const Matrix t = list.matrices[at.matrix];
+    const Slabs k(ws, t);
+    const L w(lds);
+    float x[L::F][4];
+#pragma unroll
+    for (int f = 0; f < L::F; ++f) {
+        const Float4 v = k.x[(at.local * L::F + f) * kLittleThreads + threadIdx.x];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[f][e] = v[e];
+    }
+    const Float4* const sums = k.sums(step & 1);
+    Float4 acc = {};
+    if (step == 0) {
+        double sum = 0.;
+        for (int i = 0; i < k.slabs; ++i) sum += k.squares[i];
+        const double one = inverse_of(sum, eps);
+        for (int i = 0; i < k.slabs; ++i) {
+            const double own = k.squares[i], r = own == 0. ? 0. : one / inverse_of(own, eps);
+            acc += sums[i * kLittleThreads] * static_cast<float>(r * r);
+        }
+#pragma unroll
+        for (int f = 0; f < L::F; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[f][e] = static_cast<float>(x[f][e] * (one * static_cast<double>(kUp)));
+    } else {
+#pragma unroll 8
+        for (int i = 0; i < k.slabs; ++i) acc += sums[i * kLittleThreads];
+    }
+    w.keep_x(x);
+    w.polynomial(acc, steps.coefs[step][1], steps.coefs[step][2]);
+    w.apply(steps.coefs[step][0], x);
+    if (step + 1 == steps.count) {
+        w.end(t, last, at.local * kSlab, x);
+        return;
+    }
+    __syncthreads();
+    w.keep_x(x);
+#pragma unroll
+    for (int f = 0; f < L::F; ++f)
+        k.x[(at.local * L::F + f) * kLittleThreads + threadIdx.x] = Float4{x[f][0], x[f][1], x[f][2], x[f][3]};
+    __syncthreads();
+    k.sums(1 - (step & 1))[at.local * kLittleThreads] = w.gram();
+}
+
 // ---------------------------------------------------------------------------------------
 constexpr int64_t kMaxSide = 1 << 20, kMaxShort = 1 << 15, kMaxMatrices = 1 << 20, kMaxPlaces = static_cast<int64_t>(1) << 24;
 
@@ -957,7 +1070,7 @@ constexpr int kMaxSlices = 32;
 constexpr int64_t kPartialBytes = 64 * 64 * 4;       // of a tile's slice
 
 struct Plan {
-    int64_t matrices, littles, pieces, halves, tails, fulls, work;       // tails: quarters of the last tiles; work: bytes of all matrices
+    int64_t matrices, littles, thins, slabs, pieces, halves, tails, fulls, work;     // tails: quarters of the last tiles; work: bytes of all matrices
     double gram_steps, square_steps, full_steps;                         // parts of 64 values of K (both halves of them), of all tiles together
     int half_kind, full_kind;
     int slices[2];                                                       // of K, of X X^T and of A A in tiles of 64
@@ -970,7 +1083,24 @@ bool stack_ok(const cs_matrix& s) {
 }
 bool there(const cs_matrix& s) { return s.count > 0 && s.rows > 0 && s.cols > 0; }
 // Matrices that a workgroup takes from their moments to their parameters.
-bool little(const cs_matrix& s) { return (s.rows <= 64 || s.cols <= 64) && s.rows <= 128 && s.cols <= 128; }
+bool little(const cs_matrix& s) { return (s.rows <= 64 || s.cols <= 64) && s.rows <= 256 && s.cols <= 256; }
+// Matrices that may be taken in slabs, and how many of each.  All of them are if that is no more than a workgroup on every CU (us, slabs / tiles, two
+// terms: 1 of 64 x 4096 70 / 110, 16 of 64 x 4096 104 / 159, 64 of 64 x 1024 86 / 137; more than that read each other's sums too often: 400 of
+// 64 x 500 260 / 236, 10 of 64 x 8192 194 / 173).
+bool thin(const cs_matrix& s) {
+    const int64_t n = s.rows < s.cols ? s.rows : s.cols, m = s.rows < s.cols ? s.cols : s.rows;
+    return n <= 64 && !little(s) && m <= kMaxSlabs * kSlab;
+}
+int64_t slabs_of(const cs_matrix& s) { return ((s.rows < s.cols ? s.cols : s.rows) + kSlab - 1) / kSlab; }
+bool in_slabs(const cs_matrix* stacks, int32_t n) {
+    int64_t slabs = 0;
+    for (int32_t i = 0; i < n; ++i) {
+        if (!stack_ok(stacks[i])) return false;
+        if (there(stacks[i]) && thin(stacks[i])) slabs += stacks[i].count * slabs_of(stacks[i]);
+        if (slabs > 256) return false;
+    }
+    return true;
+}
 
 // Counts and sizes with these tiles; `each` is told of every stack that has tiles.
 template <typename F>
@@ -979,6 +1109,7 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_kind, int
     plan.half_kind = half_kind, plan.full_kind = full_kind;
     const int64_t half_tile = kHalfKinds[half_kind].high, full_high = kFullKinds[full_kind].high, full_wide = kFullKinds[full_kind].wide;
     const int64_t tile = half_tile > full_high ? half_tile : full_high;
+    const bool slabs_too = in_slabs(stacks, n);
     for (int32_t i = 0; i < n; ++i) {
         const cs_matrix& s = stacks[i];
         if (!stack_ok(s)) return false;
@@ -987,6 +1118,14 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_kind, int
         if (plan.matrices > kMaxMatrices) return false;
         if (little(s)) {
             plan.littles += s.count;
+            continue;
+        }
+        if (slabs_too && thin(s)) {
+            const int64_t slabs = slabs_of(s);
+            each(s, 64, slabs * kSlab, plan, slabs, 0, 0);
+            plan.thins += s.count;
+            plan.slabs += s.count * slabs;
+            plan.work += s.count * slab_bytes(slabs);
             continue;
         }
         const int64_t np = up_to(s.rows < s.cols ? s.rows : s.cols, tile), mp = up_to(s.rows < s.cols ? s.cols : s.rows, full_wide);
@@ -1063,7 +1202,7 @@ int64_t partial_bytes(const cs_matrix_list* l) {
 }
 size_t list_bytes(const Plan& p) {
     return static_cast<size_t>(p.matrices) * sizeof(Matrix) + static_cast<size_t>(p.halves + p.tails + p.fulls) * sizeof(Tile) +
-           static_cast<size_t>(p.pieces) * sizeof(Place);
+           static_cast<size_t>(p.pieces + p.slabs) * sizeof(Place);
 }
 size_t workspace_bytes(const cs_matrix_list* l) {
     return static_cast<size_t>(l->work + partial_bytes(l)) + static_cast<size_t>(l->pieces) * sizeof(double);
@@ -1071,10 +1210,11 @@ size_t workspace_bytes(const cs_matrix_list* l) {
 List list_of(const cs_matrix_list* l) {
     const Matrix* t = static_cast<const Matrix*>(l->memory);
     const Tile* at = reinterpret_cast<const Tile*>(t + l->matrices);
-    return List{t, at, at + l->halves + l->tails, reinterpret_cast<const Place*>(at + l->halves + l->tails + l->fulls)};
+    const Place* const pieces = reinterpret_cast<const Place*>(at + l->halves + l->tails + l->fulls);
+    return List{t, at, at + l->halves + l->tails, pieces, pieces + l->pieces};
 }
 bool list_ok(const cs_matrix_list* l) {
-    return l && l->littles >= 0 && l->matrices >= l->littles && l->pieces >= 0 && l->halves >= 0 && l->tails >= 0 && l->fulls >= 0 &&
+    return l && l->littles >= 0 && l->thins >= 0 && l->matrices >= l->littles + l->thins && l->slabs >= 0 && l->pieces >= 0 && l->halves >= 0 && l->tails >= 0 && l->fulls >= 0 &&
            l->work >= 0 && l->half_kind >= 0 && l->half_kind < kHalfKindsN && l->full_kind >= 0 && l->full_kind < kFullKindsN &&
            l->gram_slices >= 0 && l->gram_slices <= kMaxSlices && l->square_slices >= 0 && l->square_slices <= kMaxSlices &&
            (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) && fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
@@ -1176,19 +1316,26 @@ int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const doub
     for (int i = 0; i < h->steps; ++i)
         for (int e = 0; e < 3; ++e) steps.coefs[i][e] = static_cast<float>(h->coefs[i][e]);
     if (l->littles) {
-        const auto kernel = l->little_cols <= 64 ? k_muon_little<64, TERMS> : k_muon_little<128, TERMS>;
+        const auto kernel = l->little_cols <= 64 ? k_muon_little<64, TERMS> : l->little_cols <= 128 ? k_muon_little<128, TERMS> : k_muon_little<256, TERMS>;
         kernel<<<static_cast<unsigned>(l->littles), kLittleThreads, 0, s>>>(at, moment, h->eps, steps, last);
         if (int rc = launched()) return rc;
     }
-    if (l->matrices == l->littles) return CS_OK;
+    if (l->thins) {
+        const unsigned slabs = static_cast<unsigned>(l->slabs);
+        k_muon_slab_begin<TERMS><<<slabs, kLittleThreads, 0, s>>>(at, moment, h->eps, ws);
+        for (int i = 0; i < h->steps; ++i) k_muon_slab<TERMS><<<slabs, kLittleThreads, 0, s>>>(at, steps, i, h->eps, last, ws);
+        if (int rc = launched()) return rc;
+    }
+    const int64_t before = l->littles + l->thins;
+    if (l->matrices == before) return CS_OK;
     double* const squares = reinterpret_cast<double*>(ws + l->work + partial_bytes(l));
     const unsigned pieces = static_cast<unsigned>(l->pieces);
     k_muon_moment<<<pieces, kThreads, 0, s>>>(at, moment, squares);
-    const bool joined = l->pieces > kSquaresEach * (l->matrices - l->littles);
+    const bool joined = l->pieces > kSquaresEach * (l->matrices - before);
     if (joined) {
         List others = at;
-        others.matrices += l->littles;
-        k_muon_norm<<<static_cast<unsigned>(l->matrices - l->littles), kThreads, 0, s>>>(others, squares);
+        others.matrices += before;
+        k_muon_norm<<<static_cast<unsigned>(l->matrices - before), kThreads, 0, s>>>(others, squares);
     }
     k_muon_begin<TERMS><<<pieces, kThreads, 0, s>>>(at, moment, h->eps, squares, joined, ws);
     if (int rc = launched()) return rc;
@@ -1208,7 +1355,7 @@ int run(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const double*
     if (ws_bytes < need) return CS_EWORKSPACE;
     if (need && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15))) return CS_EINVAL;
     Plan plan = {};
-    plan.matrices = l->matrices, plan.pieces = l->pieces, plan.halves = l->halves, plan.tails = l->tails, plan.fulls = l->fulls;
+    plan.matrices = l->matrices, plan.slabs = l->slabs, plan.pieces = l->pieces, plan.halves = l->halves, plan.tails = l->tails, plan.fulls = l->fulls;
     const Span written[] = {{need ? workspace : nullptr, static_cast<int64_t>(need)}};
     const Span read[] = {{l->memory, static_cast<int64_t>(list_bytes(plan))}, {lr, 8}, {grad_scale, 4}};
     if (!spans_apart(written, read)) return CS_EINVAL;
@@ -1263,7 +1410,7 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
             const int64_t side = stacks[i].rows > stacks[i].cols ? stacks[i].rows : stacks[i].cols;
             if (side > little_cols) little_cols = side;
         }
-    *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.pieces, plan.halves, plan.tails, plan.fulls, plan.work, p_fmt, g_fmt, terms,
+    *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.thins, plan.slabs, plan.pieces, plan.halves, plan.tails, plan.fulls, plan.work, p_fmt, g_fmt, terms,
                            moments == 1, plan.half_kind, plan.full_kind, plan.slices[0], plan.slices[1], static_cast<int32_t>(little_cols)};
     if (plan.matrices == 0) return CS_OK;
     Matrix* const matrices = static_cast<Matrix*>(memory);
@@ -1288,34 +1435,40 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
         t.rows = static_cast<int32_t>(s.rows), t.cols = static_cast<int32_t>(s.cols);
         if (++filled == kBatch) flush();
     };
-    // the small ones first
+    // the small ones first, then the thin ones
     for (int32_t i = 0; i < count; ++i)
         if (there(stacks[i]) && little(stacks[i]))
             for (int64_t k = 0; k < stacks[i].count; ++k) take(stacks[i], k, Matrix{});
-    Plan again;
-    plan_with(stacks, count, terms, plan.half_kind, plan.full_kind, again,
-              [&](const cs_matrix& s, int64_t np, int64_t mp, const Plan& at, int64_t pieces, int64_t halves, int64_t fulls) {
-        for (int64_t k = 0; k < s.count; ++k) {
-            Matrix t = {};
-            t.at = at.work + k * work_bytes(np, mp, terms);
-            t.np = static_cast<int32_t>(np), t.mp = static_cast<int32_t>(mp);
-            t.first_piece = static_cast<int32_t>(at.pieces + k * pieces), t.pieces = static_cast<int32_t>(pieces);
-            t.first_half = static_cast<int32_t>(at.halves + k * halves), t.first_full = static_cast<int32_t>(at.fulls + k * fulls);
-            take(s, k, t);
-        }
-    });
+    const bool slabs_too = in_slabs(stacks, count);
+    for (const bool thins : {true, false}) {
+        Plan again;
+        plan_with(stacks, count, terms, plan.half_kind, plan.full_kind, again,
+                  [&](const cs_matrix& s, int64_t np, int64_t mp, const Plan& at, int64_t pieces, int64_t halves, int64_t fulls) {
+            if ((slabs_too && thin(s)) != thins) return;
+            for (int64_t k = 0; k < s.count; ++k) {
+                Matrix t = {};
+                t.at = at.work + k * (thins ? slab_bytes(pieces) : work_bytes(np, mp, terms));
+                t.np = static_cast<int32_t>(np), t.mp = static_cast<int32_t>(mp);
+                t.first_piece = static_cast<int32_t>((thins ? at.slabs : at.pieces) + k * pieces), t.pieces = static_cast<int32_t>(pieces);
+                t.first_half = static_cast<int32_t>(at.halves + k * halves), t.first_full = static_cast<int32_t>(at.fulls + k * fulls);
+                take(s, k, t);
+            }
+        });
+    }
     flush();
     if (rc) return rc;
     Tile* const halves = reinterpret_cast<Tile*>(matrices + plan.matrices);
     Tile *const tails = halves + plan.halves, *const fulls = tails + plan.tails;
     const auto grid = [](int64_t n) { return static_cast<unsigned>((n + kThreads - 1) / kThreads); };
-    const int first = static_cast<int>(plan.littles), n = static_cast<int>(plan.matrices);
-    if (first == n) return CS_OK;
+    const int thins = static_cast<int>(plan.littles), first = static_cast<int>(plan.littles + plan.thins), n = static_cast<int>(plan.matrices);
+    Place *const pieces = reinterpret_cast<Place*>(fulls + plan.fulls), *const slabs = pieces + plan.pieces;
+    if (plan.slabs) k_list_places<kPieces><<<grid(plan.slabs), kThreads, 0, st>>>(matrices, thins, first, kEdge, kEdge, slabs, plan.slabs, 0);
+    if (first == n) return launched();
     const Kind &half = kHalfKinds[plan.half_kind], &full = kFullKinds[plan.full_kind];
     if (plan.halves) k_list_places<kHalves><<<grid(plan.halves), kThreads, 0, st>>>(matrices, first, n, half.high, half.wide, halves, plan.halves, 0);
     if (plan.tails) k_list_places<kTails><<<grid(plan.tails), kThreads, 0, st>>>(matrices, first, n, half.high, half.wide, tails, plan.tails, plan.halves);
     k_list_places<kFulls><<<grid(plan.fulls), kThreads, 0, st>>>(matrices, first, n, full.high, full.wide, fulls, plan.fulls, 0);
-    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, kEdge, reinterpret_cast<Place*>(fulls + plan.fulls), plan.pieces, 0);
+    k_list_places<kPieces><<<grid(plan.pieces), kThreads, 0, st>>>(matrices, first, n, kEdge, kEdge, pieces, plan.pieces, 0);
     if (int e = launched()) return e;
     return CS_OK;
 }

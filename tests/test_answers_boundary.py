@@ -111,7 +111,7 @@ def test_matrix_list_refuses(lib):
 def test_muon_refuses(lib):
     def listed(moments):
         # (as a build fills it for two matrices in a tile of 64 each)
-        return cs.CsMatrixList(D, 2, 0, 2, 2, 0, 2, 1 << 16, F32, F32, 1, moments, 0, 0, 1, 1, 0)
+        return cs.CsMatrixList(D, 2, 0, 0, 0, 2, 2, 0, 2, 1 << 16, F32, F32, 1, moments, 0, 0, 1, 1, 0)
 
     def call(optimizer=True, c=None, ws=E, ws_bytes=1 << 20, lr=None, scale=None, **change):
         a = dict(lr=0.1, momentum=0.9, weight_decay=0.0, eps=1e-7, nesterov=1, rule=0, steps=1, reserved=0) | {k: v for k, v in change.items() if k != "coefs"}

@@ -77,10 +77,10 @@ def matrices_of(count, rows, cols, dtype=torch.float32, seed=1, steep=False):
     return x.to(dtype)
 
 
-# a workgroup's own (up to 64 x 128), and in tiles of every size
+# a workgroup's own (up to 64 x 256), in slabs, and in tiles of every size
 SIZES = [(1, 1, 1), (1, 1, 70), (2, 70, 1), (1, 3, 5), (1, 64, 64), (2, 65, 63), (3, 30, 64), (2, 64, 128), (2, 127, 50), (1, 65, 65), (1, 64, 129), (1, 16, 300), (3, 130, 257), (2, 257, 128), (1, 200, 1000),
          (1, 512, 512),
-         (1, 60, 4000), (2, 250, 3000), (1, 2100, 330), (5, 65, 5000)]
+         (1, 60, 4000), (3, 250, 50), (2, 256, 64), (20, 64, 4097), (7, 5000, 33), (2, 250, 3000), (1, 2100, 330), (5, 65, 5000)]
 
 
 @pytest.mark.parametrize("count,rows,cols", SIZES)
@@ -104,6 +104,11 @@ def test_many_matrices_of_many_shapes(terms):
 @pytest.mark.parametrize("terms", [1, 2])
 def test_as_many_matrices_as_larger_tiles_are_taken_for(terms):
     check_shapes([(60, 300, 520), (1, 5, 7), (2, 1100, 900), (1, 130, 1)], terms)
+
+
+@pytest.mark.parametrize("terms", [1, 2])
+def test_small_ones_thin_ones_and_others_in_one_list(terms):
+    check_shapes([(6, 30, 1000), (4, 200, 300), (5, 64, 200), (1, 3000, 64), (4, 50, 20), (1, 65, 9000)], terms)
 
 
 @pytest.mark.parametrize("terms", [1, 2])
