@@ -683,15 +683,16 @@ int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, i
                          int64_t d_stride, void* workspace, size_t ws_bytes, void* stream);
 
 /* Loss of pairs of answers.  Answers are packed after one another: answer a has the tokens [begin[a], begin[a + 1]) (device
- * int64[2 pairs + 1], ascending, or results are undefined; what leaves [0, tokens] is cut off there); answers 0 .. pairs - 1 are the chosen ones, the next `pairs` the rejected
- * ones, in the same order.  With R = beta times the sum of l - l1 over an answer's tokens that count (mean: by their number; of no
- * token: 0) and z = R_chosen - R_rejected - margin, a pair's loss is
+ * int64[2 pairs + 1], ascending, or results are undefined; what leaves [0, tokens] is cut off there); answers 0 .. pairs - 1 are the
+ * chosen ones, the next `pairs` the rejected ones, in the same order.  With R = beta times the sum of l - l1 over an answer's tokens that
+ * count (mean: by their number; of no token: 0) and z = R_chosen - R_rejected - margin, a pair's loss is
  *     CS_PREFERENCE_LOGISTIC  (1 - smoothing) ln(1 + exp(-z)) + smoothing ln(1 + exp(z))
  *     CS_PREFERENCE_HINGE     max(0, 1 - z)
  *     CS_PREFERENCE_SQUARE    ((z - 1/2) / beta)^2
  * logp, ref_logp_or_null (0): float[tokens].  counts_or_null: device uint8[tokens], 0 leaves a token out, whatever its values.
  * weight_or_null (1): float[pairs], a pair of weight 0 has no gradient.  loss: float[pairs], without the weight; reward: float[2 pairs], R.
- * g_logp: float[tokens] or NULL, the gradient of the sum of weight times loss: 0 for tokens that are left out or of no answer.  sums: float[3], of weight loss, of the weight of pairs with R_chosen > R_rejected, of weight (R_chosen - R_rejected); sums are
+ * g_logp: float[tokens] or NULL, the gradient of the sum of weight times loss: 0 for tokens that are left out or of no answer.
+ * sums: float[3], of weight loss, of the weight of pairs with R_chosen > R_rejected, of weight (R_chosen - R_rejected); sums are
  * binary64 in a fixed order, rounded once.  tokens <= 2^34, pairs < 2^22.  workspace: device, 8-byte aligned. */
 #define CS_PREFERENCE_LOGISTIC 0
 #define CS_PREFERENCE_HINGE 1
@@ -736,8 +737,8 @@ int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int32_t p_fmt, 
  * scale: CS_MUON_SCALE_SHAPE sqrt(max(1, rows / cols)), CS_MUON_SCALE_RMS 0.2 sqrt(max(rows, cols)), CS_MUON_SCALE_ONE 1.
  * s: 1, or *grad_scale_or_null (device); where that is not finite nothing is written.  lr: h->lr, or *lr_or_null (device double).
  * cs_orthogonalize: p = X(g) (of h it takes eps, steps and coefs).
- * workspace: device, cs_muon_workspace_bytes (about 6 bytes a value of a wide matrix, 8 with two terms, 4 or 8 more for each of its n x n products),
- * 16-byte aligned; its contents do not outlive the call. */
+ * workspace: device, cs_muon_workspace_bytes (about 6 bytes a value of a wide matrix, 8 with two terms, 4 or 8 more for each of its
+ * n x n products; none of matrices up to 64 x 256), 16-byte aligned; its contents do not outlive the call. */
 #define CS_MUON_MAX_STEPS 16
 #define CS_MUON_SCALE_SHAPE 0
 #define CS_MUON_SCALE_RMS 1

@@ -112,8 +112,10 @@ class CsMatrix(ctypes.Structure):
 
 
 class CsMatrixList(ctypes.Structure):
-    _fields_ = [("memory", ctypes.c_void_p), *((name, ctypes.c_int64) for name in ("matrices", "littles", "thins", "slabs", "pieces", "halves", "tails", "fulls", "work")),
-                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_kind", "full_kind", "gram_slices", "square_slices", "little_cols"))]
+    _fields_ = [("memory", ctypes.c_void_p),
+                *((name, ctypes.c_int64) for name in ("matrices", "littles", "thins", "slabs", "pieces", "halves", "tails", "fulls", "work")),
+                *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_kind", "full_kind", "gram_slices",
+                                                      "square_slices", "little_cols"))]
 
 
 class CsMuon(ctypes.Structure):

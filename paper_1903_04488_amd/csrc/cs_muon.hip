@@ -598,7 +598,7 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
         if (PHASE != kJoin && i < all) load(i, i);
     Operands first, second;
     if constexpr (PHASE == kJoin) {
-#pragma unroll 4
+#pragma unroll 8
         for (int i = 0; i < k.slices; ++i)
 #pragma unroll
             for (int fi = 0; fi < S::FI; ++fi)
@@ -897,26 +897,75 @@ struct Little {
             for (int e = 0; e < 4; ++e) x[f][e] = fmaf(keeps, x[f][e], acc[e] * kDown);
         }
     }
-    // u of the columns from `first` on, the moment's step taken; returns the sum of its squares, in every lane
-    __device__ __forceinline__ double begin(const Matrix& t, const Moment& moment, int32_t first, float (&x)[F][4],
-                                            double (&buf)[kLittleThreads / 64]) const {
-        const float s = moment.grad_scale ? *moment.grad_scale : 1.f;
-        double sum = 0.;
+    // A lane's elements of an array with the matrix's rows, of X's columns from `first` on (0 behind the end): all loads before the first conversion, as
+    // what waits here is a workgroup alone (64 x 4096: the first launch 12.9 us with the loads one after the other).
+    template <typename T>
+    __device__ __forceinline__ void read(const Matrix& t, const T* p, int64_t stride, int32_t first, float (&v)[F][4]) const {
+        T raw[F][4];
 #pragma unroll
         for (int f = 0; f < F; ++f) {
+            const int32_t at = first + col + 16 * f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) raw[f][e] = static_cast<T>(0.f);
             if (t.rows > t.cols) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float u[1];
-                    direction<true>(t, moment, s, first + col + 16 * f + e, row, u);
-                    x[f][e] = u[0];
-                }
-            } else {
-                direction<true>(t, moment, s, row, first + col + 16 * f, x[f]);
+                for (int e = 0; e < 4; ++e)
+                    if (row < t.cols && at + e < t.rows) raw[f][e] = p[(at + e) * stride + row];
+            } else if (row < t.rows && at + 4 <= t.cols) {
+                __builtin_memcpy(raw[f], p + row * stride + at, sizeof(raw[f]));
+            } else if (row < t.rows) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (at + e < t.cols) raw[f][e] = p[row * stride + at + e];
             }
+        }
+#pragma unroll
+        for (int f = 0; f < F; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[f][e] = static_cast<float>(raw[f][e]);
+    }
+    __device__ __forceinline__ void read(const Matrix& t, const void* p, int fmt, int64_t stride, int32_t first, float (&v)[F][4]) const {
+        if (fmt == CS_FMT_F32) read(t, static_cast<const float*>(p), stride, first, v);
+        else if (fmt == CS_FMT_BF16) read(t, static_cast<const bf16*>(p), stride, first, v);
+        else read(t, static_cast<const f16*>(p), stride, first, v);
+    }
+    // u of the columns from `first` on, the moment's step taken; returns the sum of its squares, in every lane
+    __device__ __forceinline__ double begin(const Matrix& t, const Moment& k, int32_t first, float (&x)[F][4],
+                                            double (&buf)[kLittleThreads / 64]) const {
+        const float s = k.grad_scale ? *k.grad_scale : 1.f;
+        float m[F][4];
+        if (t.moment) read(t, t.moment, t.cols, first, m);
+        read(t, t.g, k.g_fmt, t.g_stride, first, x);
+        if (t.moment) {
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const int32_t at = first + col + 16 * f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    m[f][e] = fmaf(k.mu, m[f][e], s * x[f][e]);
+                    x[f][e] = k.nesterov ? fmaf(k.mu, m[f][e], s * x[f][e]) : m[f][e];
+                }
+                if (t.rows > t.cols) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (row < t.cols && at + e < t.rows) t.moment[static_cast<int64_t>(at + e) * t.cols + row] = m[f][e];
+                } else if (row < t.rows) {
+                    float* const to = t.moment + static_cast<int64_t>(row) * t.cols + at;
+                    if (at + 4 <= t.cols) {
+                        __builtin_memcpy(to, m[f], sizeof(m[f]));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (at + e < t.cols) to[e] = m[f][e];
+                    }
+                }
+            }
+        }
+        double sum = 0.;
+#pragma unroll
+        for (int f = 0; f < F; ++f)
 #pragma unroll
             for (int e = 0; e < 4; ++e) sum = fma(static_cast<double>(x[f][e]), static_cast<double>(x[f][e]), sum);
-        }
 #pragma unroll
         for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
         if (lane == 0) buf[threadIdx.x >> 6] = sum;
@@ -926,14 +975,24 @@ struct Little {
         for (int d = 8; d; d >>= 1) sum += __shfl_xor(sum, d);
         return sum;
     }
-    __device__ __forceinline__ void end(const Matrix& t, const Last& last, int32_t first, const float (&x)[F][4]) const {
+    __device__ __forceinline__ void end(const Matrix& t, const Last& last, int32_t first, float (&x)[F][4]) const {
         const Update u = update_of(last, t);
+        float old[F][4];
+        if (u.optimizer) read(t, t.p, last.p_fmt, t.p_stride, first, old);
 #pragma unroll
         for (int f = 0; f < F; ++f) {
-            float v[1][4];
+            const int32_t at = first + col + 16 * f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[0][e] = x[f][e] * kDown;
-            finish(t, last.p_fmt, u, row, first + col + 16 * f, v);
+            for (int e = 0; e < 4; ++e) x[f][e] = u.optimizer ? fmaf(old[f][e], u.keep, -u.lr * (x[f][e] * kDown)) : x[f][e] * kDown;
+            if (t.rows > t.cols) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float one[1] = {x[f][e]};
+                    write_p(t, last.p_fmt, at + e, row, one);
+                }
+            } else {
+                write_p(t, last.p_fmt, row, at, x[f]);
+            }
         }
     }
 };
@@ -1149,11 +1208,12 @@ double time_of(const Kind& kind, int64_t tiles, double steps) {
     const double last = left == 0 ? 0. : (left > 256 ? kind.step : kind.alone) * steps + kind.besides;
     return static_cast<double>(tiles / kind.at_once) * (kind.step * steps + kind.besides) + last;
 }
-// The same of tiles of 64, in as many slices of K as are best; a launch to join them is 5 us (64 x 4096, two terms: X X^T 28 us whole).
+// The same of tiles of 64, in as many slices of K as are best.  A launch to join n of them is 4.5 us and 0.15 a slice (256 x 4096: X X^T 18 us whole, in
+// 32 slices 5.5 and 9.5).
 double time_in_slices(int64_t tiles, double steps, int& slices) {
     double least = INFINITY;
     for (int n = 1; n <= kMaxSlices && (n == 1 || (tiles * n <= 768 && n * 2 <= steps)); n *= 2) {
-        const double us = time_of(kHalfKinds[0], tiles * n, steps / n) + (n > 1 ? 5. : 0.);
+        const double us = time_of(kHalfKinds[0], tiles * n, steps / n) + (n > 1 ? 4.5 + 0.15 * n : 0.);
         if (us < least) {
             least = us;
             slices = n;

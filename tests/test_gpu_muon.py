@@ -159,10 +159,15 @@ def test_other_coefficients_step_by_step():
             close(out[0], want, off, (coefs[0], terms))
 
 
+# in tiles, a workgroup's own, in slabs of columns
+KINDS = [(70, 130), (40, 100), (50, 700)]
+
+
+@pytest.mark.parametrize("rows,cols", KINDS)
 @pytest.mark.parametrize("power", [-120, -60, 60, 100])
-def test_sizes_of_the_numbers_do_not_matter(power):
+def test_sizes_of_the_numbers_do_not_matter(power, rows, cols):
     """scaled by a power of 2 the result has the same bits (eps 0)"""
-    x = matrices_of(1, 70, 100)
+    x = matrices_of(1, rows, cols)
     x = torch.where(x.abs() < 2.0 ** -6, 0.0, x)         # (no subnormal numbers)
     outs = []
     for f in (1.0, 2.0 ** power):
@@ -171,13 +176,14 @@ def test_sizes_of_the_numbers_do_not_matter(power):
     assert torch.equal(*outs)
 
 
-def test_zeros_and_what_is_not_finite_stay_in_their_matrix():
-    x = matrices_of(5, 70, 130)
+@pytest.mark.parametrize("rows,cols", KINDS)
+def test_zeros_and_what_is_not_finite_stay_in_their_matrix(rows, cols):
+    x = matrices_of(5, rows, cols)
     clean = torch.empty_like(x)
     Orthogonalizer([x], [clean]).run()
     x[1] = 0.0
     x[2, 3, 4] = float("nan")
-    x[3, 69, 129] = float("inf")
+    x[3, -1, -1] = float("inf")
     out = torch.empty_like(x)
     Orthogonalizer([x], [out]).run()
     assert torch.equal(out[0], clean[0]) and torch.equal(out[4], clean[4])
@@ -186,30 +192,32 @@ def test_zeros_and_what_is_not_finite_stay_in_their_matrix():
     Orthogonalizer([x], [out], eps=0.0).run()
     assert (out[1] == 0).all()
     # rows and columns of zeros
-    y = matrices_of(1, 70, 130)
-    y[0, 5:60] = 0.0
-    y[0, :, 100:] = 0.0
+    y = matrices_of(1, rows, cols)
+    y[0, 5:-10] = 0.0
+    y[0, :, cols * 3 // 4:] = 0.0
     got = torch.empty_like(y)
     Orthogonalizer([y], [got]).run()
     want, off = steps_of(y[0], 2)
     close(got[0], want, off)
-    assert (got[0, 5:60] == 0).all() and (got[0, :, 100:] == 0).all()
+    assert (got[0, 5:-10] == 0).all() and (got[0, :, cols * 3 // 4:] == 0).all()
 
 
-def test_strides_and_in_place():
-    wide = torch.full((3, 80, 200), float("nan"), device=DEV)
-    x = matrices_of(3, 70, 130)
-    inside = wide[:, 4:74, 33:163]
+@pytest.mark.parametrize("rows,cols", KINDS + [(130, 70), (100, 40), (700, 50)])
+def test_strides_and_in_place(rows, cols):
+    wide = torch.full((3, rows + 10, cols + 70), float("nan"), device=DEV)
+    x = matrices_of(3, rows, cols)
+    inside = wide[:, 4:4 + rows, 33:33 + cols]
     inside.copy_(x)
     want = torch.empty_like(x)
     Orthogonalizer([x], [want]).run()
-    target = torch.full((3, 90, 140), 7.0, device=DEV)
-    Orthogonalizer([inside], [target[:, 10:80, 5:135]]).run()
-    assert torch.equal(target[:, 10:80, 5:135], want)
-    target[:, 10:80, 5:135] = 7.0
+    target = torch.full((3, rows + 20, cols + 10), 7.0, device=DEV)
+    at = target[:, 10:10 + rows, 5:5 + cols]
+    Orthogonalizer([inside], [at]).run()
+    assert torch.equal(at, want)
+    at.fill_(7.0)
     assert (target == 7.0).all()
     Orthogonalizer([inside], [inside]).run()
-    assert torch.equal(inside, want) and torch.isnan(wide[:, :4]).all() and torch.isnan(wide[:, :, 163:]).all()
+    assert torch.equal(inside, want) and torch.isnan(wide[:, :4]).all() and torch.isnan(wide[:, :, 33 + cols:]).all()
     Orthogonalizer([x[1]], [x[1]]).run()
     assert torch.equal(x[1], want[1])
 
@@ -231,7 +239,15 @@ def step_truth(p, g, m, h, terms, s=1.0, lr=None):
 @pytest.mark.parametrize("p_type,g_type", [("f32", "f32"), ("bf16", "bf16"), ("f32", "bf16"), ("f16", "f32"), ("bf16", "f32")])
 @pytest.mark.parametrize("nesterov,scale", [(True, "shape"), (False, "rms"), (True, "one")])
 def test_steps_of_the_optimizer(p_type, g_type, nesterov, scale):
-    shapes = [(2, 70, 130), (1, 200, 64), (3, 33, 33)]
+    check_steps([(2, 70, 130), (1, 200, 64), (3, 33, 33)], p_type, g_type, nesterov, scale)
+
+
+@pytest.mark.parametrize("p_type,g_type", [("f32", "bf16"), ("bf16", "f32"), ("f16", "f16")])
+def test_steps_of_thin_matrices(p_type, g_type):
+    check_steps([(2, 40, 1000), (1, 1300, 64), (2, 250, 61), (1, 17, 201)], p_type, g_type, True, "shape")
+
+
+def check_steps(shapes, p_type, g_type, nesterov, scale):
     p = [matrices_of(*s, TYPES[p_type], seed=i) * 0.05 for i, s in enumerate(shapes)]
     p[1] = p[1][0]
     grads = [[(matrices_of(*s, TYPES[g_type], seed=10 * t + i, steep=True) * 0.01) for i, s in enumerate(shapes)] for t in range(3)]
@@ -251,8 +267,9 @@ def test_steps_of_the_optimizer(p_type, g_type, nesterov, scale):
                 close(new, want, off + 4 * 2.0 ** -24 * float(want.norm()), i)
 
 
-def test_scaled_and_skipped_steps_and_a_rate_on_the_gpu():
-    p, g = [matrices_of(2, 70, 90)], [matrices_of(2, 70, 90, seed=2)]
+@pytest.mark.parametrize("rows,cols", KINDS)
+def test_scaled_and_skipped_steps_and_a_rate_on_the_gpu(rows, cols):
+    p, g = [matrices_of(2, rows, cols)], [matrices_of(2, rows, cols, seed=2)]
     scale, lr = torch.tensor([0.25], device=DEV), torch.tensor([0.125], dtype=torch.float64, device=DEV)
     opt = Muon(p, g, lr=9.0, weight_decay=0.1, grad_scale=scale, lr_now=lr)
     old, m_old = p[0].clone(), opt.m[0].clone()
