@@ -159,6 +159,18 @@ def test_other_coefficients_step_by_step():
             close(out[0], want, off, (coefs[0], terms))
 
 
+@pytest.mark.parametrize("count,rows,cols", [(1, 3, 300000), (2, 64, 8192), (1, 64, 8193), (1, 20000, 100), (9, 64, 8000)])
+@pytest.mark.parametrize("terms", [1, 2])
+def test_long_matrices(count, rows, cols, terms):
+    """as many slabs as there may be of one matrix and in all, and more (which are tiles)"""
+    x = matrices_of(count, rows, cols, steep=True)
+    out = torch.full_like(x, float("nan"))
+    Orthogonalizer([x], [out], terms=terms).run()
+    for i in range(0, count, 4):
+        want, off = steps_of(x[i], terms)
+        close(out[i], want, off)
+
+
 # in tiles, a workgroup's own, in slabs of columns
 KINDS = [(70, 130), (40, 100), (50, 700)]
 
