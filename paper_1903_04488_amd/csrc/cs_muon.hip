@@ -1116,14 +1116,16 @@ __global__ void __launch_bounds__(kLittleThreads) k_muon_slab(List list, Steps s
 // ---------------------------------------------------------------------------------------
 constexpr int64_t kMaxSide = 1 << 20, kMaxShort = 1 << 15, kMaxMatrices = 1 << 20, kMaxPlaces = static_cast<int64_t>(1) << 24;
 
-// Kinds of tiles: edges, how many are on the GPU at once, and how long they take for a part of 64 values of K and besides (us; `alone`: with no
-// more than one on a CU)
+// Kinds of tiles: edges, how many are on the GPU at once, and how long they take (us) for a part of 64 values of K, with one, two or three on a CU, and
+// besides.  Of 52 lists (one of 90 x 90, 200 of 100 x 100, 40 of 700 x 700, 36 of 512 x 2048, one of 4096 x 2048, ..; one and two terms) that were
+// timed in all kinds of tiles, those that these numbers choose are 0.3 % slower than the best on average and 2.5 % at most; of 16 others 1 % and
+// 5.6 %.
 struct Kind {
     int high, wide, at_once;
-    double step, besides, alone;
+    double step[3], besides;
 };
-constexpr Kind kHalfKinds[] = {{64, 64, 768, 0.5, 3., 0.28}, {128, 128, 512, 0.83, 4., 0.68}};
-constexpr Kind kFullKinds[] = {{64, 64, 768, 0.5, 3., 0.28}, {64, 128, 768, 0.95, 5., 0.5}, {128, 128, 512, 1.05, 6., 0.68}, {256, 256, 256, 1.65, 14., 1.65}};
+constexpr Kind kHalfKinds[] = {{64, 64, 768, {0.28, 0.5, 0.5}, 3.}, {128, 128, 512, {0.45, 0.87}, 8.}};
+constexpr Kind kFullKinds[] = {{64, 64, 768, {0.28, 0.5, 0.5}, 3.}, {64, 128, 768, {0.4, 0.6, 0.95}, 5.}, {128, 128, 512, {0.68, 1.05}, 6.}, {256, 256, 256, {1.65}, 14.}};
 constexpr int kHalfKindsN = 2, kFullKindsN = 4;
 constexpr int kMaxSlices = 32;
 constexpr int64_t kPartialBytes = 64 * 64 * 4;       // of a tile's slice
@@ -1204,9 +1206,9 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_kind, int
 }
 // How long so many tiles take with so many parts of K each, in rounds of what is on the GPU at once (a last round of few takes less).
 double time_of(const Kind& kind, int64_t tiles, double steps) {
-    const int64_t left = tiles % kind.at_once;
-    const double last = left == 0 ? 0. : (left > 256 ? kind.step : kind.alone) * steps + kind.besides;
-    return static_cast<double>(tiles / kind.at_once) * (kind.step * steps + kind.besides) + last;
+    const int64_t rounds = tiles / kind.at_once, left = tiles % kind.at_once;
+    const auto round = [&](int64_t on_a_cu) { return kind.step[on_a_cu - 1] * steps + kind.besides; };
+    return static_cast<double>(rounds) * round(kind.at_once / 256) + (left ? round((left + 255) / 256) : 0.);
 }
 // The same of tiles of 64, in as many slices of K as are best.  A launch to join n of them is 4.5 us and 0.15 a slice (256 x 4096: X X^T 18 us whole, in
 // 32 slices 5.5 and 9.5).
@@ -1221,8 +1223,8 @@ double time_in_slices(int64_t tiles, double steps, int& slices) {
     }
     return least;
 }
-// A symmetric product.  Few tiles of 128 left by the last round would take nearly as long as a whole one where K is long (528 tiles of 4096 x 4096: 74 us
-// for 512 and 26 for the 16 that are left): they are taken as tiles of 64, four each, `tails` (16 us).
+// A symmetric product.  Few tiles of 128 left by the last round would take nearly half as long as a whole one where K is long (528 tiles of 4096 x 4096:
+// 70 us for 512 and 29 for the 16 that are left): they are taken as tiles of 64, four each, `tails` (12 us, in slices).
 double half_time(int kind, int64_t tiles, double steps, int64_t tails, int& slices) {
     if (kind == 0) return time_in_slices(tiles, steps, slices);
     slices = 1;
