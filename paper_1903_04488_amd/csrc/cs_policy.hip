@@ -293,7 +293,9 @@ __global__ void __launch_bounds__(kPairsEach * 64) k_preference_pairs(Preference
     }
 }
 
-// Few pairs of few tokens in one launch, a pair a wavefront and turn (16 pairs of up to 400 tokens: 13.4 / 9 us)
+// Few pairs of few tokens in one launch, a pair a wavefront and turn, eight tokens of a lane under way together (16 pairs of up to 400 tokens: 13.4 us in
+// pieces, 9.0 with a token after the other, 7.8)
+constexpr int kAtOnce = 8;
 constexpr int64_t kFewPairs = 32, kFewTokens = 8192;
 __global__ void __launch_bounds__(kMost) k_preference_few(Preference k) {
     __shared__ double buf[3][kMost / 64];
@@ -309,12 +311,24 @@ __global__ void __launch_bounds__(kMost) k_preference_few(Preference k) {
         double sum[2] = {0., 0.}, count[2] = {0., 0.};
 #pragma unroll
         for (int s = 0; s < 2; ++s)
-#pragma unroll 4
-            for (int64_t i = begin[s] + lane; i < end[s]; i += 64) {
-                const bool counts = !k.counts || k.counts[i];
-                const float l = k.logp[i], l1 = k.ref_logp ? k.ref_logp[i] : 0.f;
-                sum[s] += counts ? static_cast<double>(l) - static_cast<double>(l1) : 0.;
-                count[s] += counts;
+            for (int64_t i = begin[s] + lane; i < end[s]; i += 64 * kAtOnce) {
+                float l[kAtOnce], l1[kAtOnce];
+                uint8_t counts[kAtOnce];
+#pragma unroll
+                for (int e = 0; e < kAtOnce; ++e) {
+                    const int64_t at = i + 64 * e;
+                    counts[e] = at < end[s];
+                    l[e] = l1[e] = 0.f;
+                    if (!counts[e]) continue;
+                    l[e] = k.logp[at];
+                    if (k.ref_logp) l1[e] = k.ref_logp[at];
+                    if (k.counts) counts[e] = k.counts[at];
+                }
+#pragma unroll
+                for (int e = 0; e < kAtOnce; ++e) {
+                    sum[s] += counts[e] ? static_cast<double>(l[e]) - static_cast<double>(l1[e]) : 0.;
+                    count[s] += counts[e] != 0;
+                }
             }
 #pragma unroll
         for (int s = 0; s < 2; ++s)
