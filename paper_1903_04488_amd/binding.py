@@ -1400,6 +1400,10 @@ class MatrixList:
                 if m[i].shape != p[i].shape:
                     raise CsError(f"m[{i}] must have shape {tuple(p[i].shape)}, got {tuple(m[i].shape)}")
             stacks[i] = CsMatrix(at, g_at, moment, count, rows, cols, p_stride, p_step, g_stride, g_step)
+        for name, written in (("p", p), ("m", m or [])):
+            begins = [t.data_ptr() for t in written if t.numel()]
+            if len(set(begins)) != len(begins):
+                raise CsError(f"{name} has a tensor twice")
         device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
         if any(t.device != device for t in p + g + (m or [])):
             raise CsError("the tensors of a list must be on one GPU")

@@ -158,7 +158,7 @@ def _muon_constants(lr, momentum, nesterov, weight_decay, eps, coefs, scale):
 
 
 def _terms_of(tensors, terms):
-    """results of 8 bits need no more than one term"""
+    """results of bfloat16's 8 bits need no more than one term"""
     if terms is None:
         terms = 1 if tensors and tensors[0].dtype is torch.bfloat16 else 2
     return terms

@@ -344,6 +344,12 @@ def test_refusals():
                 dict(params=[y], grads=[x], lr_now=torch.ones(1, device=DEV)), dict(params=[y], grads=[x], grad_scale=torch.ones(2, device=DEV))):
         with pytest.raises(cs.CsError):
             Muon(**bad).step()
+    with pytest.raises(cs.CsError, match="twice"):
+        Orthogonalizer([x, x + 1], [y, y])
+    with pytest.raises(cs.CsError, match="twice"):
+        Muon([y, torch.empty_like(y)], [x, x], m=[m, m])
+    Orthogonalizer([x, x], [y, torch.empty_like(y)]).run()                       # (what is read may be the same)
+    Orthogonalizer([x[:0], x[:0]], [y[:0], y[:0]]).run()
     x, y = matrices_of(2, 70, 200), torch.zeros(2, 70, 200, device=DEV)
     opt = Muon([y], [x])
     with pytest.raises(cs.CsError, match="workspace"):
