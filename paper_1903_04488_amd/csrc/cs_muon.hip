@@ -1481,11 +1481,13 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
     int filled = 0, rc = CS_OK;
     int64_t done = 0;
     const auto flush = [&] {
-        if (!filled || rc) return;
-        k_list_matrices<<<1, 64, 0, st>>>(b, matrices + done, filled);
-        rc = launched();
+        if (!filled) return;
+        if (!rc) {
+            k_list_matrices<<<1, 64, 0, st>>>(b, matrices + done, filled);
+            rc = launched();
+        }
         done += filled;
-        filled = 0;
+        filled = 0;                          // (after a launch that failed too: the next matrices need the room)
     };
     const auto take = [&](const cs_matrix& s, int64_t k, Matrix more) {
         Matrix& t = b.t[filled];

@@ -4,15 +4,17 @@ import ctypes
 import math
 import os
 import subprocess
+import sys
 
 import pytest
+import torch
 
 import paper_1903_04488_amd as cs
 from paper_1903_04488_amd import binding
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 BF16, F16, F32 = 0, 1, 2
-OK, EINVAL, EWORKSPACE = 0, -1, -2
+OK, EINVAL, EWORKSPACE, EHIP = 0, -1, -2, -3
 A, B_, C, D, E, F, G, H, I, J, K, L, M = (0x10000000 * (i + 1) for i in range(13))       # far apart
 
 
@@ -150,3 +152,21 @@ def test_structs_have_the_headers_layout(tmp_path):
 def test_the_package_names_what_the_binding_has():
     for name in ("cs_policy_loss", "cs_token_policy_loss", "cs_preference_loss", "cs_muon_step", "cs_orthogonalize", "MatrixList"):
         assert getattr(cs, name) is getattr(binding, name)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a launch that fails, for want of a GPU")
+@pytest.mark.parametrize("count,side", [(39, 70), (40, 70), (41, 70), (81, 70), (2000, 8), (300, 70)])
+def test_a_list_whose_first_launch_fails_says_so(lib, count, side):
+    """in a process of its own: what is written behind an array ends the process at the latest when the call returns"""
+    code = f"""
+import ctypes, sys
+sys.path.insert(0, {ROOT!r})
+import paper_1903_04488_amd as cs
+n = {side * side}
+stack = cs.CsMatrix({A}, {E}, {I}, {count}, {side}, {side}, {side}, n, {side}, n)
+c = cs.CsMatrixList()
+rc = cs.load_library().cs_matrix_list_build(ctypes.byref(stack), 1, {F32}, {F32}, 1, {M}, 1 << 30, ctypes.byref(c), None)
+print("status", rc)
+"""
+    done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
+    assert done.returncode == 0 and done.stdout.split() == ["status", str(EHIP)], (done.returncode, done.stderr[-500:])
