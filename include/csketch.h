@@ -662,7 +662,7 @@ int cs_moments_write(const cs_tensor_list* list, void* stream);
  *     loss = w (-S + kl K - entropy H),  g_logp = -w ([S = r A] r A + kl (exp(l1 - l) - 1)),  g_entropy = -w entropy
  * (log probabilities that are the same infinity are 0 apart; an exponential beyond binary32 is infinite).
  * sums: device float[4] or NULL: of loss, of w K (0 where kl is 0), of w over the tokens where clipping decides, of w; binary64 in a fixed
- * order, rounded once.
+ * order, rounded once.  Of no rows they are 0 (a call without a workspace, NULL, has nothing to do and leaves them alone).
  * 0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl, entropy: finite. */
 typedef struct cs_policy {
     float clip_low, clip_high, kl, entropy;

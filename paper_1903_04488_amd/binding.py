@@ -1222,6 +1222,11 @@ def _same_gpu(like, **tensors):
     return out
 
 
+def _somewhere(t):
+    """an address in place of a workspace of no bytes: of none at all a batch of nothing would leave its sums as they are"""
+    return None if t is None else t.data_ptr()
+
+
 def cs_policy_workspace_bytes(rows: int) -> int:
     n = ctypes.c_size_t()
     _check(load_library().cs_policy_workspace_bytes(rows, ctypes.byref(n)), "cs_policy_workspace_bytes")
@@ -1249,7 +1254,7 @@ def cs_policy_loss(h: CsPolicy, logp, entropy, old_logp, ref_logp, advantage, we
                 h, n, logp.data_ptr(), None if entropy is None else entropy.data_ptr(), old_logp.data_ptr(),
                 None if ref_logp is None else ref_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), None if loss is None else loss.data_ptr(),
                 None if g_logp is None else g_logp.data_ptr(), None if g_entropy is None else g_entropy.data_ptr(),
-                None if sums is None else sums.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(logp))
+                None if sums is None else sums.data_ptr(), workspace.data_ptr() or _somewhere(sums), workspace.numel(), _stream(logp))
             if status:
                 _check(status, "cs_policy_loss")
             return
@@ -1261,6 +1266,7 @@ def cs_policy_loss(h: CsPolicy, logp, entropy, old_logp, ref_logp, advantage, we
     at = _same_gpu(logp, logp=(logp, f32, n), entropy=(entropy, f32, n), old_logp=(old_logp, f32, n), ref_logp=(ref_logp, f32, n),
                    advantage=(advantage, f32, n), weight=(weight, f32, n), loss=(loss, f32, n), g_logp=(g_logp, f32, n),
                    g_entropy=(g_entropy, f32, n), sums=(sums, f32, 4), workspace=(workspace, torch.uint8, None))
+    at[-1] = at[-1] or _somewhere(sums)
     _check(load_library().cs_policy_loss(h, n, *at, workspace.numel(), _stream(logp)), "cs_policy_loss")
 
 
@@ -1290,7 +1296,7 @@ def cs_token_policy_loss(h: CsPolicy, logits, target, old_logp, ref_logp, advant
                 h, logits.data_ptr(), rows, vocab, step, _FMT[dt], scale, target.data_ptr(), old_logp.data_ptr(),
                 None if ref_logp is None else ref_logp.data_ptr(), advantage.data_ptr(), weight.data_ptr(), logp.data_ptr(),
                 entropy.data_ptr(), lse.data_ptr(), None if loss is None else loss.data_ptr(), None if sums is None else sums.data_ptr(),
-                dlogits.data_ptr(), out_step, workspace.data_ptr(), workspace.numel(), _stream(logits))
+                dlogits.data_ptr(), out_step, workspace.data_ptr() or _somewhere(sums), workspace.numel(), _stream(logits))
             if status:
                 _check(status, "cs_token_policy_loss")
             return
@@ -1308,7 +1314,7 @@ def cs_token_policy_loss(h: CsPolicy, logits, target, old_logp, ref_logp, advant
         advantage=(advantage, f32, rows), weight=(weight, f32, rows), logp=(logp, f32, rows), entropy=(entropy, f32, rows),
         lse=(lse, f32, rows), loss=(loss, f32, rows), sums=(sums, f32, 4), workspace=(workspace, torch.uint8, None))
     _check(load_library().cs_token_policy_loss(
-        h, at, rows, vocab, step, _FMT[logits.dtype], scale, t, old, ref, a, w, lp, ent, ls, lo, su, out, out_step, ws,
+        h, at, rows, vocab, step, _FMT[logits.dtype], scale, t, old, ref, a, w, lp, ent, ls, lo, su, out, out_step, ws or _somewhere(sums),
         workspace.numel(), _stream(logits)), "cs_token_policy_loss")
 
 

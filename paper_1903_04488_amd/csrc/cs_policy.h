@@ -84,6 +84,8 @@ int launch_policy(const PolicyIn& in, int64_t rows, const float* logp, const flo
                   const PolicyOut& out, hipStream_t stream);
 // The sums alone, of rows whose terms are known, in the same order
 int launch_policy_sums(const PolicyTerms* terms, int64_t rows, float* sums, double* partials, hipStream_t stream);
+// `count` sums (or null) and `tokens` gradients of nothing: 0
+int launch_nothing(float* sums, int count, float* g, int64_t tokens, hipStream_t stream);
 bool policy_ok(const cs_policy* h);
 
 }  // namespace cs

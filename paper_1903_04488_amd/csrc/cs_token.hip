@@ -116,7 +116,7 @@ extern "C" int cs_token_policy_loss(const cs_policy* h, const void* logits, int6
                                     const float* advantage, const float* weight, float* logp, float* entropy, float* lse, float* loss,
                                     float* sums, void* dlogits, int64_t d_stride, void* workspace, size_t ws_bytes, void* stream) {
     if (!policy_ok(h) || !token_ok(rows, vocab, stride, fmt, scale)) return CS_EINVAL;
-    if (rows == 0) return CS_OK;
+    if (rows == 0) return sums && workspace ? launch_nothing(sums, 4, nullptr, 0, stream_of(stream)) : CS_OK;
     if (!logits || !target || !old_logp || (h->kl != 0.f && !ref_logp) || !advantage || !weight || !logp || !entropy || !lse) return CS_EINVAL;
     const size_t need = policy_bytes(rows, vocab);
     if (ws_bytes < need) return CS_EWORKSPACE;
