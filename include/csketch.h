@@ -674,8 +674,8 @@ int cs_policy_loss(const cs_policy* h, int64_t rows, const float* logp, const fl
                    const float* ref_logp_or_null, const float* advantage, const float* weight, float* loss, float* g_logp, float* g_entropy,
                    float* sums, void* workspace, size_t ws_bytes, void* stream);
 /* From logits, with their gradient: cs_token_logprobs, cs_policy_loss and cs_token_logprobs_grad of them in one call, which reads the
- * logits once where a workgroup holds a row.  Rows whose target is outside [0, vocab) have weight 0; an empty row's gradient is 0.  loss may be
- * NULL, sums too, dlogits may be the logits (same stride). */
+ * logits once where a workgroup holds a row.  Rows whose target is outside [0, vocab) have weight 0.  The gradient of a row of weight 0 is 0, whatever
+ * its logits are, and so is an empty row's.  loss may be NULL, sums too, dlogits may be the logits (same stride). */
 int cs_token_policy_workspace_bytes(int64_t rows, int64_t vocab, size_t* bytes);
 int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, int64_t vocab, int64_t stride, int32_t fmt, float scale,
                          const int64_t* target, const float* old_logp, const float* ref_logp_or_null, const float* advantage,

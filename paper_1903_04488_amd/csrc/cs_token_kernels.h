@@ -558,7 +558,7 @@ struct PolicyRows {
 struct RowGrad {
     float mul, add, a, b, hot;
     int32_t target;                  // -1: none
-    bool empty;                      // the row has no probabilities: gradient 0
+    bool empty;                      // the row has no probabilities, or a policy loss leaves it out: gradient 0
 
     __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const float* g_logp,
                                                   const float* g_entropy) {
@@ -568,8 +568,9 @@ struct RowGrad {
         a = -hot;
         b = g_entropy ? -scale * g_entropy[row] : 0.f;
     }
-    // the same from the policy loss of a row's token; writes: that thread leaves the loss and what sums are taken of
-    __device__ __forceinline__ void coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const PolicyRows& rows,
+    // the same from the policy loss of a row's token; writes: that thread leaves the loss and what sums are taken of.  True: the row is left out,
+    // and its logits may be anything (0 times a NaN would not be 0)
+    __device__ __forceinline__ bool coefficients(int64_t row, int64_t vocab, float scale, int64_t t, const PolicyRows& rows,
                                                  const PolicyRow& given, float logp, float entropy, bool writes) {
         target = t >= 0 && t < vocab ? static_cast<int32_t>(t) : -1;
         const PolicyToken token = policy_token(rows.in.h, given, logp, entropy, target >= 0);
@@ -580,7 +581,9 @@ struct RowGrad {
         hot = scale * token.g_logp;
         a = -hot;
         b = -scale * token.g_entropy;
+        return left_out(target, given.weight);
     }
+    static __device__ __forceinline__ bool left_out(int32_t target, float weight) { return target < 0 || weight == 0.f; }
     // ENTROPY: b is not 0
     template <int FROM, bool ENTROPY>
     __device__ __forceinline__ float of(float x) const {
@@ -684,12 +687,13 @@ __device__ __forceinline__ Sums sums_of_row(const T* x, int64_t vocab, int32_t p
 constexpr float kFarLse = 256.f;
 
 // The gradient that is asked for later: a pass over the logits, four packs a thread, many workgroups a row.  4096 x 32001 f32
-// in 187 us, 1049 MB at 5.6 TB/s (a copy: 4.8): memory.
+// in 187 us, 1049 MB at 5.6 TB/s (a copy: 4.8): memory.  policy_weight: of a policy loss, whose rows of weight 0 or without a target are
+// left out; null otherwise.
 template <typename T, bool PAST>
 __global__ void __launch_bounds__(kThreads)
 k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const int64_t* target, const float* lse,
-             const float* entropy, const float* g_logp, const float* g_entropy, T* dlogits, int64_t d_stride, int pieces,
-             int32_t packs) {
+             const float* entropy, const float* g_logp, const float* g_entropy, const float* policy_weight, T* dlogits, int64_t d_stride,
+             int pieces, int32_t packs) {
     const int64_t row = blockIdx.x / static_cast<unsigned>(pieces);
     const int32_t each = (packs + pieces - 1) / pieces, piece = static_cast<int32_t>(blockIdx.x % static_cast<unsigned>(pieces));
     const int32_t first = min(each * piece, packs);
@@ -697,7 +701,7 @@ k_token_grad(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     r.coefficients(row, vocab, scale, target ? target[row] : -1, g_logp, g_entropy);
     r.mul = scale;
     r.add = lse[row];
-    r.empty = r.add == -INFINITY;
+    r.empty = r.add == -INFINITY || (policy_weight && RowGrad::left_out(r.target, policy_weight[row]));
     if (fabsf(r.add) >= kFarLse && !r.empty) {
         __shared__ float buf[3][16];
         if (piece != row % pieces) return;
@@ -856,16 +860,18 @@ k_token_held(const T* logits, int64_t rows, int32_t vocab, int64_t stride, float
     if constexpr (MODE == kLoss || MODE == kPolicy) {
         T* dx = dlogits + row * d_stride;
         RowGrad g;
-        bool bonus;
+        bool bonus, out_of_it = false;
         if constexpr (MODE == kPolicy) {
-            g.coefficients(row, vocab, scale, t, policy, given, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum),
+            out_of_it = g.coefficients(row, vocab, scale, t, policy, given, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum),
                            thread_of_row<THREADS>() == 0);
             bonus = policy.in.h.entropy != 0.f;
         } else {
             g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
             bonus = g_entropy;
         }
-        if (!grad_from_sums(g, r, log_sum, scale)) grad_held<PAST, kDiffs, true, THREADS, ITEMS>(held, dx, vocab, g);
+        const bool from_sums = grad_from_sums(g, r, log_sum, scale);
+        g.empty |= out_of_it;
+        if (!from_sums) grad_held<PAST, kDiffs, true, THREADS, ITEMS>(held, dx, vocab, g);
         else if (bonus) grad_held<PAST, kSums, true, THREADS, ITEMS>(held, dx, vocab, g);
         else grad_held<PAST, kSums, false, THREADS, ITEMS>(held, dx, vocab, g);
     }
@@ -893,16 +899,18 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
     if (threadIdx.x == 0) row_results(row, hit, scale, r, log_sum, out);
     __syncthreads();                                  // (dlogits may be the logits, whose target has been read)
     RowGrad g;
-    bool bonus;
+    bool bonus, out_of_it = false;
     if constexpr (MODE == kPolicy) {
-        g.coefficients(row, vocab, scale, t, policy, given, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum),
+        out_of_it = g.coefficients(row, vocab, scale, t, policy, given, hit.counts ? logp_of(hit.x, r, log_sum, scale) : 0.f, entropy_of(r, log_sum),
                        threadIdx.x == 0);
         bonus = policy.in.h.entropy != 0.f;
     } else {
         g.coefficients(row, vocab, scale, t, g_logp, g_entropy);
         bonus = g_entropy;
     }
-    if (!grad_from_sums(g, r, log_sum, scale)) grad_packs<PAST, kDiffs, true, kThreads>(x, dx, vocab, 0, packs, g);
+    const bool from_sums = grad_from_sums(g, r, log_sum, scale);
+    g.empty |= out_of_it;
+    if (!from_sums) grad_packs<PAST, kDiffs, true, kThreads>(x, dx, vocab, 0, packs, g);
     else if (bonus) grad_packs<PAST, kSums, true, kThreads>(x, dx, vocab, 0, packs, g);
     else grad_packs<PAST, kSums, false, kThreads>(x, dx, vocab, 0, packs, g);
 }
@@ -988,7 +996,7 @@ int token_grad(const TokenArgs& a) {
     const auto kernel = past_caches(a.rows * a.vocab * sizeof(T)) ? k_token_grad<T, true> : k_token_grad<T, false>;
     kernel<<<static_cast<unsigned>(a.rows * pieces), kThreads, 0, a.stream>>>(
         static_cast<const T*>(a.logits), a.vocab, a.stride, a.scale, a.target, a.lse, a.entropy, a.g_logp, a.g_entropy,
-        static_cast<T*>(a.dlogits), a.d_stride, static_cast<int>(pieces), packs);
+        a.policy.weight, static_cast<T*>(a.dlogits), a.d_stride, static_cast<int>(pieces), packs);
     return launched();
 }
 // (kPolicy: the sums too)
