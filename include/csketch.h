@@ -693,7 +693,8 @@ int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, i
  * weight_or_null (1): float[pairs], a pair of weight 0 has no gradient.  loss: float[pairs], without the weight; reward: float[2 pairs], R.
  * g_logp: float[tokens] or NULL, the gradient of the sum of weight times loss: 0 for tokens that are left out or of no answer.
  * sums: float[3], of weight loss, of the weight of pairs with R_chosen > R_rejected, of weight (R_chosen - R_rejected); sums are
- * binary64 in a fixed order, rounded once.  tokens <= 2^34, pairs < 2^22.  workspace: device, 8-byte aligned. */
+ * binary64 in a fixed order, rounded once.  Of no pairs sums and the gradients of all tokens are 0 (a call without a workspace, NULL, has
+ * nothing to do and leaves them alone).  tokens <= 2^34, pairs < 2^22.  workspace: device, 8-byte aligned. */
 #define CS_PREFERENCE_LOGISTIC 0
 #define CS_PREFERENCE_HINGE 1
 #define CS_PREFERENCE_SQUARE 2

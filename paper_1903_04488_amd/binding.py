@@ -1342,7 +1342,7 @@ def cs_preference_loss(h: CsPreference, logp, ref_logp, counts, begin, weight, l
             status = (_lib or load_library()).cs_preference_loss(
                 h, n, pairs, logp.data_ptr(), None if ref_logp is None else ref_logp.data_ptr(), None if counts is None else counts.data_ptr(),
                 begin.data_ptr(), None if weight is None else weight.data_ptr(), loss.data_ptr(), reward.data_ptr(),
-                None if g_logp is None else g_logp.data_ptr(), sums.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream(logp))
+                None if g_logp is None else g_logp.data_ptr(), sums.data_ptr(), workspace.data_ptr() or _somewhere(sums), workspace.numel(), _stream(logp))
             if status:
                 _check(status, "cs_preference_loss")
             return
@@ -1358,6 +1358,7 @@ def cs_preference_loss(h: CsPreference, logp, ref_logp, counts, begin, weight, l
     at = _same_gpu(logp, logp=(logp, f32, n), ref_logp=(ref_logp, f32, n), counts=(counts, kind, n), begin=(begin, torch.int64, None),
                    weight=(weight, f32, pairs), loss=(loss, f32, pairs), reward=(reward, f32, 2 * pairs), g_logp=(g_logp, f32, n),
                    sums=(sums, f32, 3), workspace=(workspace, torch.uint8, None))
+    at[-1] = at[-1] or _somewhere(sums)
     _check(load_library().cs_preference_loss(h, n, pairs, *at, workspace.numel(), _stream(logp)), "cs_preference_loss")
 
 

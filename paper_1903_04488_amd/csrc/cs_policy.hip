@@ -499,7 +499,12 @@ extern "C" int cs_preference_loss(const cs_preference* h, int64_t tokens, int64_
     if (!h || h->kind < 0 || h->kind > CS_PREFERENCE_SQUARE || !(h->beta > 0.f && h->beta < INFINITY) || !(h->smoothing >= 0.f && h->smoothing <= 1.f) ||
         !(fabsf(h->margin) < INFINITY) || tokens < 0 || tokens > kMaxPacked || pairs < 0 || pairs > kMaxPairs)
         return CS_EINVAL;
-    if (pairs == 0) return CS_OK;
+    if (pairs == 0) {
+        if (!workspace) return CS_OK;
+        const Span nothing[] = {{g_logp, 4 * tokens}, {sums, 12}}, given[] = {{logp, 4 * tokens}, {ref_logp, 4 * tokens}, {counts, tokens}, {begin, 8}};
+        if (!spans_apart(nothing, given)) return CS_EINVAL;
+        return sums || (g_logp && tokens) ? launch_nothing(sums, 3, g_logp, g_logp ? tokens : 0, stream_of(stream)) : CS_OK;
+    }
     if ((tokens && !logp) || !begin || !loss || !reward || !sums) return CS_EINVAL;
     const size_t need = preference_bytes(tokens, pairs);
     if (ws_bytes < need) return CS_EWORKSPACE;
