@@ -240,7 +240,8 @@ __device__ __forceinline__ void pair_loss(const cs_preference& h, double z, doub
         // ln(1 + e^-z) = max(-z, 0) + ln(1 + e^-|z|), and z more for the other answer
         const double e = exp(-fabs(z)), soft = log1p(e), p = (z >= 0. ? e : 1.) / (1. + e);        // p = 1 / (1 + e^z)
         const double s = h.smoothing;
-        loss = (1. - s) * (fmax(-z, 0.) + soft) + s * (fmax(z, 0.) + soft);
+        // (an answer that cannot be makes z infinite: what has no share in the loss adds 0, not 0 times that)
+        loss = (s == 1. ? 0. : (1. - s) * (fmax(-z, 0.) + soft)) + (s == 0. ? 0. : s * (fmax(z, 0.) + soft));
         slope = s - p;
         if (!(z == z)) loss = z;             // (a maximum drops a NaN)
     } else if (h.kind == CS_PREFERENCE_HINGE) {
