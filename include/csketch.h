@@ -689,6 +689,7 @@ int cs_token_policy_loss(const cs_policy* h, const void* logits, int64_t rows, i
  *     CS_PREFERENCE_LOGISTIC  (1 - smoothing) ln(1 + exp(-z)) + smoothing ln(1 + exp(z))
  *     CS_PREFERENCE_HINGE     max(0, 1 - z)
  *     CS_PREFERENCE_SQUARE    ((z - 1/2) / beta)^2
+ * (log probabilities that are the same infinity are 0 apart; rewards that are make their pair NaN).
  * logp, ref_logp_or_null (0): float[tokens].  counts_or_null: device uint8[tokens], 0 leaves a token out, whatever its values.
  * weight_or_null (1): float[pairs], a pair of weight 0 has no gradient.  loss: float[pairs], without the weight; reward: float[2 pairs], R.
  * g_logp: float[tokens] or NULL, the gradient of the sum of weight times loss: 0 for tokens that are left out or of no answer.

@@ -112,6 +112,9 @@ int policy_grid(int64_t rows) {
 constexpr int kPieceThreads = 256, kEach = 8, kPiece = kPieceThreads * kEach;
 constexpr int kPairsEach = 4;                // pairs of a workgroup, a wavefront each
 
+// a token's log ratio: equal infinities are 0 apart (a token that neither allows), as in the policy loss
+__device__ __forceinline__ double log_ratio(float l, float l1) { return l == l1 ? 0. : static_cast<double>(l) - static_cast<double>(l1); }
+
 struct Part {
     double sum;
     int64_t count;
@@ -217,7 +220,7 @@ __global__ void __launch_bounds__(kPieceThreads) k_preference_parts(Preference k
     Run own = {0, 0, 0.};
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        v[e] = counts[e] ? static_cast<double>(l[e]) - static_cast<double>(l1[e]) : 0.;
+        v[e] = counts[e] ? log_ratio(l[e], l1[e]) : 0.;
         const Run one = {mark[mine + e], counts[e] != 0, v[e]};
         own = after(own, one);
     }
@@ -337,7 +340,7 @@ __global__ void __launch_bounds__(kMost) k_preference_few(Preference k) {
                 }
 #pragma unroll
                 for (int e = 0; e < kAtOnce; ++e) {
-                    sum[s] += counts[e] ? static_cast<double>(l[e]) - static_cast<double>(l1[e]) : 0.;
+                    sum[s] += counts[e] ? log_ratio(l[e], l1[e]) : 0.;
                     count[s] += counts[e] != 0;
                 }
             }
