@@ -39,7 +39,8 @@ __device__ __forceinline__ PolicyToken policy_token(const cs_policy& h, float lo
                                                     float w) {
     if (w == 0.f) return PolicyToken{0.f, 0.f, 0.f, 0.f, 0.f};
     const float r = expf(apart(logp, old_logp));
-    const float plain = a == 0.f ? 0.f : r * a, bounded = fminf(fmaxf(r, 1.f - h.clip_low), 1.f + h.clip_high) * a;
+    // (a ratio beyond binary32 times no advantage is 0; one that is not a number stays one)
+    const float plain = a == 0.f && r == r ? 0.f : r * a, bounded = fminf(fmaxf(r, 1.f - h.clip_low), 1.f + h.clip_high) * a;
     const bool cut = plain > bounded;        // (at the border the ratio still counts)
     PolicyToken t;
     float loss = -(cut ? bounded : plain), g = cut ? 0.f : -plain;
