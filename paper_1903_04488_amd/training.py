@@ -131,6 +131,7 @@ class PreferenceLoss:
         f32 = dict(dtype=torch.float32, device=device)
         self.losses, self.rewards, self.sums = torch.empty(pairs, **f32), torch.empty(2 * pairs, **f32), torch.zeros(3, **f32)
         self.g_logp = torch.empty(tokens, **f32)
+        self.mean_weight = torch.full((pairs,), 1.0 / max(pairs, 1), **f32)          # of a call with all the pairs there is room for
         self.workspace = torch.empty(B.cs_preference_workspace_bytes(tokens, pairs), dtype=torch.uint8, device=device)
 
     def loss(self, logp, ref_logp, begin, counts=None, weight=None):
@@ -138,7 +139,10 @@ class PreferenceLoss:
         the pairs without a weight"""
         pairs, n = len(begin) // 2, len(logp)
         if weight is None:
-            weight = torch.full((pairs,), 1.0 / max(pairs, 1), device=logp.device)
+            # (of fewer pairs a tensor of the call's own: a captured call keeps what it had)
+            weight = self.mean_weight
+            if pairs != len(weight):
+                weight = torch.full((pairs,), 1.0 / max(pairs, 1), dtype=torch.float32, device=logp.device)
         B.cs_preference_loss(self.h, logp, ref_logp, counts, begin, weight, self.losses[:pairs], self.rewards[:2 * pairs], self.g_logp[:n],
                              self.sums, self.workspace)
         return self.sums, self.g_logp[:n]
