@@ -729,7 +729,7 @@ typedef struct cs_matrix {
 typedef struct cs_matrix_list {
     void* memory;                            /* device */
     int64_t matrices, littles, thins, slabs, pieces, halves, tails, fulls, work;
-    int32_t p_fmt, g_fmt, terms, moments, half_kind, full_kind, gram_slices, square_slices, little_cols;
+    int32_t p_fmt, g_fmt, terms, moments, half_kind, full_kind, gram_slices, square_slices, little_cols, most_pieces;
 } cs_matrix_list;
 int cs_matrix_list_bytes(const cs_matrix* stacks, int32_t count, int32_t terms, size_t* bytes);
 int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int32_t p_fmt, int32_t g_fmt, int32_t terms, void* memory, size_t bytes,

@@ -115,7 +115,7 @@ class CsMatrixList(ctypes.Structure):
     _fields_ = [("memory", ctypes.c_void_p),
                 *((name, ctypes.c_int64) for name in ("matrices", "littles", "thins", "slabs", "pieces", "halves", "tails", "fulls", "work")),
                 *((name, ctypes.c_int32) for name in ("p_fmt", "g_fmt", "terms", "moments", "half_kind", "full_kind", "gram_slices",
-                                                      "square_slices", "little_cols"))]
+                                                      "square_slices", "little_cols", "most_pieces"))]
 
 
 class CsMuon(ctypes.Structure):

@@ -1132,6 +1132,7 @@ constexpr int64_t kPartialBytes = 64 * 64 * 4;       // of a tile's slice
 
 struct Plan {
     int64_t matrices, littles, thins, slabs, pieces, halves, tails, fulls, work;     // tails: quarters of the last tiles; work: bytes of all matrices
+    int64_t most_pieces;                                                 // of a matrix in tiles
     double gram_steps, square_steps, full_steps;                         // parts of 64 values of K (both halves of them), of all tiles together
     int half_kind, full_kind;
     int slices[2];                                                       // of K, of X X^T and of A A in tiles of 64
@@ -1194,6 +1195,7 @@ bool plan_with(const cs_matrix* stacks, int32_t n, int terms, int half_kind, int
         const int64_t fulls = (np / full_high) * (mp / full_wide);
         each(s, np, mp, plan, pieces, halves, fulls);
         plan.pieces += s.count * pieces;
+        if (pieces > plan.most_pieces) plan.most_pieces = pieces;
         plan.halves += s.count * halves;
         plan.fulls += s.count * fulls;
         plan.gram_steps += static_cast<double>(s.count * halves) * mp * terms / 64;
@@ -1276,7 +1278,7 @@ List list_of(const cs_matrix_list* l) {
     return List{t, at, at + l->halves + l->tails, pieces, pieces + l->pieces};
 }
 bool list_ok(const cs_matrix_list* l) {
-    return l && l->littles >= 0 && l->thins >= 0 && l->matrices >= l->littles + l->thins && l->slabs >= 0 && l->pieces >= 0 && l->halves >= 0 && l->tails >= 0 && l->fulls >= 0 &&
+    return l && l->most_pieces >= 0 && l->littles >= 0 && l->thins >= 0 && l->matrices >= l->littles + l->thins && l->slabs >= 0 && l->pieces >= 0 && l->halves >= 0 && l->tails >= 0 && l->fulls >= 0 &&
            l->work >= 0 && l->half_kind >= 0 && l->half_kind < kHalfKindsN && l->full_kind >= 0 && l->full_kind < kFullKindsN &&
            l->gram_slices >= 0 && l->gram_slices <= kMaxSlices && l->square_slices >= 0 && l->square_slices <= kMaxSlices &&
            (l->terms == 1 || l->terms == 2) && fmt_ok(l->p_fmt) && fmt_ok(l->g_fmt) && (l->matrices == 0 || l->memory);
@@ -1364,8 +1366,9 @@ int product(const cs_matrix_list* l, Product k, char* ws, hipStream_t s) {
     }
 }
 
-// Pieces of a matrix up to which every workgroup that begins X sums their squares by itself, in place of a launch that does (4096 x 4096,
-// 4096 pieces: that launch is 6 us).
+// Pieces of a list's largest matrix up to which every workgroup that begins X sums their squares by itself, in place of a launch that does
+// (4096 x 4096, 4096 pieces: that launch is 6 us).  Workgroups by themselves read the square of a matrix's pieces: 8192 x 8192 beside 100 of
+// 128 x 128 216 us, with the launch 85 and 18.
 constexpr int64_t kSquaresEach = 1024;
 
 template <int TERMS>
@@ -1393,7 +1396,7 @@ int run_as(const cs_muon* h, const cs_matrix_list* l, bool optimizer, const doub
     double* const squares = reinterpret_cast<double*>(ws + l->work + partial_bytes(l));
     const unsigned pieces = static_cast<unsigned>(l->pieces);
     k_muon_moment<<<pieces, kThreads, 0, s>>>(at, moment, squares);
-    const bool joined = l->pieces > kSquaresEach * (l->matrices - before);
+    const bool joined = l->most_pieces > kSquaresEach;
     if (joined) {
         List others = at;
         others.matrices += before;
@@ -1473,7 +1476,8 @@ extern "C" int cs_matrix_list_build(const cs_matrix* stacks, int32_t count, int3
             if (side > little_cols) little_cols = side;
         }
     *list = cs_matrix_list{memory, plan.matrices, plan.littles, plan.thins, plan.slabs, plan.pieces, plan.halves, plan.tails, plan.fulls, plan.work, p_fmt, g_fmt, terms,
-                           moments == 1, plan.half_kind, plan.full_kind, plan.slices[0], plan.slices[1], static_cast<int32_t>(little_cols)};
+                           moments == 1, plan.half_kind, plan.full_kind, plan.slices[0], plan.slices[1], static_cast<int32_t>(little_cols),
+                           static_cast<int32_t>(plan.most_pieces)};
     if (plan.matrices == 0) return CS_OK;
     Matrix* const matrices = static_cast<Matrix*>(memory);
     const hipStream_t st = stream_of(stream);

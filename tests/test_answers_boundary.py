@@ -170,3 +170,19 @@ print("status", rc)
 """
     done = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True)
     assert done.returncode == 0 and done.stdout.split() == ["status", str(EHIP)], (done.returncode, done.stderr[-500:])
+
+
+def test_a_list_knows_its_largest_matrix(lib):
+    """(by it, not by the average, it is decided who sums a matrix's squares: the plan is there also where a launch fails)"""
+    def plan(*shapes):
+        at = [stack(p=A + (i << 40), g=A + (1 << 50) + (i << 40), m=None, count=n, rows=rows, cols=cols, p_stride=cols, p_step=rows * cols,
+                    g_stride=cols, g_step=rows * cols) for i, (n, rows, cols) in enumerate(shapes)]
+        return build(lib, at, nbytes=1 << 30)[1]
+
+    if torch.cuda.is_available():
+        pytest.skip("its launches must fail")
+    small, large = plan((100, 128, 128)), plan((1, 2560, 2560))
+    assert small.most_pieces == 4 and large.most_pieces == large.pieces == 1600
+    for mixed in (plan((1, 2560, 2560), (100, 128, 128)), plan((100, 128, 128), (1, 2560, 2560), (7, 20, 30))):
+        assert mixed.most_pieces >= 1600 and mixed.pieces < 1024 * mixed.matrices
+    assert plan((3, 64, 64)).most_pieces == 0
