@@ -265,7 +265,15 @@ __global__ void __launch_bounds__(kThreads) k_muon_norm(List list, double* squar
     if (threadIdx.x == 0 && t.pieces) squares[t.first_piece] = sum;
 }
 
+// A binary32 number that the compiler has to have as such.  Without it a product and sum that is rounded to binary16 in two places may be rounded
+// by way of binary32 in one and directly in the other: next to a tie the two are a step of binary16 apart, and what is left of one upper half
+// was stored beside the other (one value in ten thousand, by 2^-11 of it: some matrices with two terms 14 times as far off as the others).
+__device__ __forceinline__ float held(float v) {
+    asm("" : "+v"(v));
+    return v;
+}
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
+    v = held(v);
     hi = static_cast<_Float16>(v);
     lo = static_cast<_Float16>(v - static_cast<float>(hi));
 }
@@ -749,8 +757,9 @@ __global__ void __launch_bounds__(S::THREADS, S::WAVES_PER_SIMD) k_muon_product(
                 const int64_t to = Work<TERMS>::place(row, col, wide);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    hi[f][e / 8][e % 8] = static_cast<_Float16>(v[e]);
-                    lo[f][e / 8][e % 8] = static_cast<_Float16>(v[e] - static_cast<float>(hi[f][e / 8][e % 8]));
+                    _Float16 h = static_cast<_Float16>(v[e]), l = h;
+                    if (TERMS == 2 || MODE == kApply) split(v[e], h, l);
+                    hi[f][e / 8][e % 8] = h, lo[f][e / 8][e % 8] = l;
                 }
 #pragma unroll
                 for (int e = 0; e < N / 8; ++e) {
@@ -801,8 +810,8 @@ struct Little {
         Half4 h, l;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            _Float16 hi, lo;
-            split(v[e], hi, lo);
+            _Float16 hi = static_cast<_Float16>(v[e]), lo = hi;
+            if (TERMS == 2) split(v[e], hi, lo);
             h[e] = hi, l[e] = lo;
         }
         *reinterpret_cast<Half4*>(at) = h;
