@@ -1382,10 +1382,55 @@ def _stack(t, name: str, dtype, shape=None):
     return t.data_ptr(), count, rows, cols, stride, step
 
 
+class _Place:
+    """where a stack lies: rows of `length` bytes, `pitch` bytes apart in a matrix, matrices `step` bytes apart"""
+
+    __slots__ = ("name", "written", "index", "begin", "end", "count", "rows", "length", "pitch", "step", "one")
+
+    def __init__(self, name, written, index, at, size, count, rows, cols, stride, step):
+        self.name, self.written, self.index, self.begin, self.count, self.rows = name, written, index, at, count, rows
+        self.length, self.pitch, self.step = cols * size, stride * size, step * size
+        self.one = (rows - 1) * self.pitch + self.length
+        self.end = at + (count - 1) * self.step + self.one
+
+    def row_begins(self):
+        return (self.begin + self.step * torch.arange(self.count)[:, None] + self.pitch * torch.arange(self.rows)).flatten()
+
+
+def _apart(a: _Place, b: _Place) -> bool:
+    """whether two stacks share no byte: their spans do not meet, or they are columns of the same rows or matrices of the same stack, or else by
+    looking at every row"""
+    if a.end <= b.begin or b.end <= a.begin:
+        return True
+    off = b.begin - a.begin
+    if a.pitch == b.pitch and all(x.count == 1 or x.step % a.pitch == 0 for x in (a, b)):
+        if off % a.pitch >= a.length and -off % a.pitch >= b.length:
+            return True
+    if a.count > 1 and a.step == b.step and b.count > 1 and off % a.step >= a.one and -off % a.step >= b.one:
+        return True
+    begins = torch.cat([a.row_begins(), b.row_begins()])
+    ends = torch.cat([a.row_begins() + a.length, b.row_begins() + b.length])
+    order = begins.argsort()
+    return bool((ends[order][:-1] <= begins[order][1:]).all())
+
+
+def _all_apart(places):
+    """no matrix that is written shares memory with another one's"""
+    places = sorted(places, key=lambda x: x.begin)
+    for i, a in enumerate(places):
+        for b in places[i + 1:]:
+            if b.begin >= a.end:
+                break
+            # (the arrays of one stack are looked at by the library)
+            if a.index != b.index and (a.written or b.written) and not _apart(a, b):
+                raise CsError(f"{a.name}[{a.index}] and {b.name}[{b.index}] overlap")
+
+
 class MatrixList:
     """Matrices, or stacks of them ([count, rows, cols]), checked once and laid out on the GPU for the same launches over all of them
     (cs_matrix_list_build).  p: what is written; g: gradients, or what is orthogonalised; m: moments (float32, contiguous) or None.  terms: 1 or
-    2, how much of their factors the products take.  Holds the tensors; `refresh` where some have moved."""
+    2, how much of their factors the products take.  What is written may share no memory with another matrix's.  Holds the tensors; `refresh`
+    where some have moved."""
 
     def __init__(self, p, g, m=None, terms: int = 1):
         self.memory, self.terms = None, terms
@@ -1397,7 +1442,7 @@ class MatrixList:
         if len(g) != len(p) or (m is not None and len(m) != len(p)):
             raise CsError(f"p, g and m must have {len(p)} tensors each")
         p_type, g_type = _same_dtype(p, "p"), _same_dtype(g, "g")
-        stacks = (CsMatrix * len(p))()
+        stacks, places = (CsMatrix * len(p))(), []
         for i in range(len(p)):
             at, count, rows, cols, p_stride, p_step = _stack(p[i], f"p[{i}]", p_type)
             g_at, *_, g_stride, g_step = _stack(g[i], f"g[{i}]", g_type, p[i].shape)
@@ -1406,11 +1451,17 @@ class MatrixList:
                 moment = _dev(m[i], torch.float32, f"m[{i}]", p[i].numel())
                 if m[i].shape != p[i].shape:
                     raise CsError(f"m[{i}] must have shape {tuple(p[i].shape)}, got {tuple(m[i].shape)}")
+            if count and rows and cols:
+                places.append(_Place("p", True, i, at, p[i].element_size(), count, rows, cols, p_stride, p_step))
+                places.append(_Place("g", False, i, g_at, g[i].element_size(), count, rows, cols, g_stride, g_step))
+                if moment:
+                    places.append(_Place("m", True, i, moment, 4, count, rows, cols, cols, rows * cols))
             stacks[i] = CsMatrix(at, g_at, moment, count, rows, cols, p_stride, p_step, g_stride, g_step)
         for name, written in (("p", p), ("m", m or [])):
             begins = [t.data_ptr() for t in written if t.numel()]
             if len(set(begins)) != len(begins):
                 raise CsError(f"{name} has a tensor twice")
+        _all_apart(places)
         device = p[0].device if p else torch.device("cuda", torch.cuda.current_device())
         if any(t.device != device for t in p + g + (m or [])):
             raise CsError("the tensors of a list must be on one GPU")
