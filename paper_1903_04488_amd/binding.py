@@ -1233,7 +1233,7 @@ def cs_policy_workspace_bytes(rows: int) -> int:
     return n.value
 
 
-def _needed(h: CsPolicy, **tensors):
+def _needed(**tensors):
     for name, t in tensors.items():
         if t is None:
             raise CsError(f"{name} must be given")
@@ -1261,7 +1261,7 @@ def cs_policy_loss(h: CsPolicy, logp, entropy, old_logp, ref_logp, advantage, we
     except (AttributeError, TypeError):
         pass
     _dev(logp, f32, "logp")
-    _needed(h, old_logp=old_logp, advantage=advantage, weight=weight, workspace=workspace)
+    _needed(old_logp=old_logp, advantage=advantage, weight=weight, workspace=workspace)
     n = logp.numel()
     at = _same_gpu(logp, logp=(logp, f32, n), entropy=(entropy, f32, n), old_logp=(old_logp, f32, n), ref_logp=(ref_logp, f32, n),
                    advantage=(advantage, f32, n), weight=(weight, f32, n), loss=(loss, f32, n), g_logp=(g_logp, f32, n),
@@ -1305,7 +1305,7 @@ def cs_token_policy_loss(h: CsPolicy, logits, target, old_logp, ref_logp, advant
     at, step = _rows(logits, "logits")
     out, out_step = _rows(dlogits, "dlogits", logits)
     rows, vocab = logits.shape
-    _needed(h, target=target, old_logp=old_logp, advantage=advantage, weight=weight, logp=logp, entropy=entropy, lse=lse,
+    _needed(target=target, old_logp=old_logp, advantage=advantage, weight=weight, logp=logp, entropy=entropy, lse=lse,
             workspace=workspace)
     if dlogits.get_device() != logits.get_device():
         raise CsError("dlogits must be on the same GPU as the others")
@@ -1350,7 +1350,7 @@ def cs_preference_loss(h: CsPreference, logp, ref_logp, counts, begin, weight, l
         pass
     _dev(logp, f32, "logp")
     _dev(begin, torch.int64, "begin")
-    _needed(h, loss=loss, reward=reward, sums=sums, workspace=workspace)
+    _needed(loss=loss, reward=reward, sums=sums, workspace=workspace)
     if begin.numel() % 2 == 0:
         raise CsError(f"begin must have 2 pairs + 1 values, got {begin.numel()}")
     n, pairs = logp.numel(), begin.numel() // 2
