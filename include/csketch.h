@@ -663,7 +663,7 @@ int cs_moments_write(const cs_tensor_list* list, void* stream);
  * (log probabilities that are the same infinity are 0 apart; an exponential beyond binary32 is infinite).
  * sums: device float[4] or NULL: of loss, of w K (0 where kl is 0), of w over the tokens where clipping decides, of w; binary64 in a fixed
  * order, rounded once.  Of no rows they are 0 (a call without a workspace, NULL, has nothing to do and leaves them alone).
- * 0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl, entropy: finite. */
+ * 0 <= clip_low <= 1, 0 <= clip_high, 0 <= kl, entropy: finite; binary32, as what they multiply. */
 typedef struct cs_policy {
     float clip_low, clip_high, kl, entropy;
 } cs_policy;

@@ -34,7 +34,8 @@ __device__ __forceinline__ float beyond_line(float x) {
     return s * x * x;
 }
 
-// A token of weight 0 is left out whatever its values are.
+// A token of weight 0 is left out whatever its values are.  In binary32, as the log probabilities are: their own rounding, 2^-24 of them, mostly moves the
+// ratio by more than all that is rounded here (777 tokens: 5.7e-8 of the whole off, in 64 bits and rounded once 2.8e-8).
 __device__ __forceinline__ PolicyToken policy_token(const cs_policy& h, float logp, float entropy, float old_logp, float ref_logp, float a,
                                                     float w) {
     if (w == 0.f) return PolicyToken{0.f, 0.f, 0.f, 0.f, 0.f};

@@ -922,8 +922,10 @@ k_token_loss(const T* logits, int64_t vocab, int64_t stride, float scale, const 
 struct Held {
     int threads, items;
 };
-// Rows (or parts) up to which each has 1024 threads.  A policy loss has 512 from a row a CU on, where two rounds of 1024 would be needed (300 x 32001
-// f32 23 / 19 us).
+// Rows (or parts) up to which each has 1024 threads.  A policy loss has 512 from a row a CU on, where two rounds of 1024 would be needed (us a call,
+// 1024 / 512 threads: 257 x 32001 f32 22.2 / 18.0, 300 x 32001 23.3 / 19.1, 511 x 32001 29.7 / 23.9, 300 x 8200 10.0 / 8.4, 500 x 34000 bf16 22.3 / 17.9,
+// 270 x 65000 f16 28.8 / 25.0, 300 x 60000 f32, which needs 1024, 36.5).  The plain loss would gain as much (300 x 32001 22.0 / 18.0); it has the bits
+// that it always gave.
 constexpr int64_t kFewHeldRows = 512, kFewPolicyRows = 257;
 Held held(int64_t rows, int64_t vocab, int32_t fmt, int parts, int64_t few = kFewHeldRows) {
     const int32_t all = packs_of(vocab, fmt), packs = (all + parts - 1) / parts;
