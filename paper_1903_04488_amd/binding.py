@@ -1415,8 +1415,12 @@ def _apart(a: _Place, b: _Place) -> bool:
 
 
 def _all_apart(places):
-    """no matrix that is written shares memory with another one's"""
-    places = sorted(places, key=lambda x: x.begin)
+    """no matrix that is written shares memory with another one's (places: the arguments of _Place)"""
+    spans = sorted([(at, at + size * ((count - 1) * step + (rows - 1) * stride + cols))
+                    for _, _, _, at, size, count, rows, cols, stride, step in places])
+    if all([spans[i][1] <= spans[i + 1][0] for i in range(len(spans) - 1)]):
+        return
+    places = sorted([_Place(*x) for x in places], key=lambda x: x.begin)
     for i, a in enumerate(places):
         for b in places[i + 1:]:
             if b.begin >= a.end:
@@ -1442,7 +1446,7 @@ class MatrixList:
         if len(g) != len(p) or (m is not None and len(m) != len(p)):
             raise CsError(f"p, g and m must have {len(p)} tensors each")
         p_type, g_type = _same_dtype(p, "p"), _same_dtype(g, "g")
-        stacks, places = (CsMatrix * len(p))(), []
+        stacks, places, p_size, g_size = (CsMatrix * len(p))(), [], p_type.itemsize, g_type.itemsize
         for i in range(len(p)):
             at, count, rows, cols, p_stride, p_step = _stack(p[i], f"p[{i}]", p_type)
             g_at, *_, g_stride, g_step = _stack(g[i], f"g[{i}]", g_type, p[i].shape)
@@ -1452,10 +1456,10 @@ class MatrixList:
                 if m[i].shape != p[i].shape:
                     raise CsError(f"m[{i}] must have shape {tuple(p[i].shape)}, got {tuple(m[i].shape)}")
             if count and rows and cols:
-                places.append(_Place("p", True, i, at, p[i].element_size(), count, rows, cols, p_stride, p_step))
-                places.append(_Place("g", False, i, g_at, g[i].element_size(), count, rows, cols, g_stride, g_step))
+                places.append(("p", True, i, at, p_size, count, rows, cols, p_stride, p_step))
+                places.append(("g", False, i, g_at, g_size, count, rows, cols, g_stride, g_step))
                 if moment:
-                    places.append(_Place("m", True, i, moment, 4, count, rows, cols, cols, rows * cols))
+                    places.append(("m", True, i, moment, 4, count, rows, cols, cols, rows * cols))
             stacks[i] = CsMatrix(at, g_at, moment, count, rows, cols, p_stride, p_step, g_stride, g_step)
         for name, written in (("p", p), ("m", m or [])):
             begins = [t.data_ptr() for t in written if t.numel()]

@@ -7,8 +7,12 @@ import paper_1903_04488_amd as cs
 from paper_1903_04488_amd.binding import _all_apart, _apart, _Place
 
 
-def place(at, count, rows, cols, stride, step, name="p", written=True, index=0, size=2):
-    return _Place(name, written, index, at, size, count, rows, cols, stride, step)
+def args(at, count, rows, cols, stride, step, name="p", written=True, index=0, size=2):
+    return name, written, index, at, size, count, rows, cols, stride, step
+
+
+def place(*a, **k):
+    return _Place(*args(*a, **k))
 
 
 def bytes_of(p):
@@ -46,14 +50,14 @@ def test_parts_of_one_array():
 
 
 def test_who_may_share():
-    p = place(0, 1, 10, 10, 10, 0)
-    _all_apart([p, place(0, 1, 10, 10, 10, 0, "g", False, 0)])                                       # (its own: the library looks)
-    _all_apart([p, place(1000, 1, 9, 9, 9, 0, "g", False, 0), place(1000, 1, 9, 9, 9, 0, "g", False, 1)])     # (both are read)
-    for other in (place(20, 1, 10, 10, 10, 0, index=1), place(100, 1, 5, 5, 5, 0, "g", False, 1), place(198, 1, 5, 5, 5, 0, "m", True, 1)):
+    p = args(0, 1, 10, 10, 10, 0)
+    _all_apart([p, args(0, 1, 10, 10, 10, 0, "g", False, 0)])                                       # (its own: the library looks)
+    _all_apart([p, args(1000, 1, 9, 9, 9, 0, "g", False, 0), args(1000, 1, 9, 9, 9, 0, "g", False, 1)])     # (both are read)
+    for other in (args(20, 1, 10, 10, 10, 0, index=1), args(100, 1, 5, 5, 5, 0, "g", False, 1), args(198, 1, 5, 5, 5, 0, "m", True, 1)):
         with pytest.raises(cs.CsError, match="overlap"):
             _all_apart([other, p])
     # many side by side, and the last one over the first
-    many = [place(128 * i, 1, 300, 64, 64 * 200, 0, index=i) for i in range(200)]
+    many = [args(128 * i, 1, 300, 64, 64 * 200, 0, index=i) for i in range(200)]
     _all_apart(many)
     with pytest.raises(cs.CsError, match=r"p\[0\] and p\[200\] overlap"):
-        _all_apart(many + [place(128 * 200 * 299, 1, 1, 1, 1, 0, index=200)])
+        _all_apart(many + [args(128 * 200 * 299, 1, 1, 1, 1, 0, index=200)])
