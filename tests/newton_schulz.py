@@ -31,7 +31,7 @@ def halves(v):
     return hi, (v - hi).to(torch.float16).double()
 
 
-def emulated(u, coefs, terms, eps=1e-7, without=()):
+def emulated(u, coefs, terms, eps=1e-7, without=(), up=UP):
     if not u.any():
         return u.double()
 
@@ -44,25 +44,25 @@ def emulated(u, coefs, terms, eps=1e-7, without=()):
         return pair[0] + pair[1] if low else pair[0]
 
     x, tall = start_of(u, eps)
-    x = x.float().double() * UP
+    x = x.float().double() * up
     for a, b, c in coefs:
         X = halves(x)
         x_t = tuple(v.t().contiguous() for v in X)
-        A = product(X, x_t) / UP ** 2
+        A = product(X, x_t) / up ** 2
         d = A.diagonal().float().double()
         if "diagonals" in without:
-            d = halves(d * UP)[0] / UP
-        A0 = halves((A - torch.diag(A.diagonal())) * UP)
-        AA = product(A0, A0) / UP ** 2
+            d = halves(d * up)[0] / up
+        A0 = halves((A - torch.diag(A.diagonal())) * up)
+        AA = product(A0, A0) / up ** 2
         low = terms == 2 and "lows" not in without
-        B = (c * (d[:, None] + d[None, :]) + b) * kept(A0, low) / UP + c * AA
+        B = (c * (d[:, None] + d[None, :]) + b) * kept(A0, low) / up + c * AA
         e = (b * d + c * (d * d + AA.diagonal())).float().double()
         if "diagonals" in without:
-            e = halves(e * UP)[0] / UP
-        B0 = halves((B - torch.diag(B.diagonal())) * UP)
-        x = (a + e)[:, None] * kept(X, "x_low" not in without) + product(B0, X) / UP
+            e = halves(e * up)[0] / up
+        B0 = halves((B - torch.diag(B.diagonal())) * up)
+        x = (a + e)[:, None] * kept(X, "x_low" not in without) + product(B0, X) / up
         x = x.float().double()
-    x = x / UP
+    x = x / up
     return x.t() if tall else x
 
 
@@ -70,12 +70,21 @@ def bounds(u, coefs, terms, eps=1e-7):
     """(the result in 64 bits, how far off the whole may be in the 2-norm, and a single element).
 
     The kernels' roundings to binary16 are the emulation's, but for values that binary32's sums move past a tie and, of thin matrices, a first
-    product of numbers that are scaled otherwise: errors of the same size, so twice the emulation's.  What binary32 adds is what plain
-    products in binary32 are off by, up to the order of their sums: four times that.  Of a single element the emulation's largest, three times."""
+    product of numbers that are scaled otherwise: errors of the same size, so twice the emulation's.  Of few directions or few values an error is a
+    sum of few roundings, which may be next to nothing in one emulation by luck and not in a kernel that takes one tie otherwise: there its size is the
+    largest of eight emulations at other scales (2^(k/8) of the first: other roundings), and a tie beside it: a step of binary16, 2^-11 of the largest
+    value at most.  What binary32 adds is what plain products in binary32 are off by, up to the order of their sums: four times that, and
+    eight times of few.  Of a single element the emulation's largest, three times."""
     want = exact(u, coefs, eps)
-    half, single = emulated(u, coefs, terms, eps) - want, exact(u, coefs, eps, torch.float32) - want
+    few = min(u.shape) < 16 or u.numel() < 4096
+    halves_off = [emulated(u, coefs, terms, eps, up=UP * 2.0 ** (k / 8)) - want for k in range(8 if few else 1)]
+    whole, element = max(d.norm() for d in halves_off), max(d.abs().max() for d in halves_off)
+    single = exact(u, coefs, eps, torch.float32) - want
+    if few:
+        step = 2.0 ** (-11 * terms) * want.abs().max()
+        whole, element = whole + step, element + step
     tiny = 2.0 ** -20 * want.abs().max()
-    return (want, 2 * half.norm() + 4 * single.norm() + tiny, 3 * half.abs().max() + 8 * single.abs().max() + tiny)
+    return want, 2 * whole + (8 if few else 4) * single.norm() + tiny, 3 * element + 8 * single.abs().max() + tiny
 
 
 def within_bounds(got, want, whole, element, rounded=0.0):
